@@ -387,6 +387,67 @@ int a3po_train_step_host(const void* h_hidden, const int32_t* h_targets, const f
                          size_t stage_bytes, void* d_ws, size_t ws_bytes, float* h_loss,
                          a3po_stats* h_stats, uint32_t* d_status, void* stream);
 
+/* --------------------------------------------------------------------------------------------
+ * Row operators in front of the LM head (the layers that produce `hidden`; no counterpart in the paper).  A trainer
+ * that owns the last block of the policy runs them on the rows it then hands to a3po_token_logprobs_fwd or
+ * a3po_train_step, and runs their backward on the grad_hidden it gets back.
+ *
+ * Common to all of them: matrices are row-major [N, H], contiguous, dtype `dt` (any H >= 1; pointers aligned to their
+ * elements, 16-byte aligned rows move in 16-byte pieces); arithmetic, statistics and weight gradients are fp32 and
+ * each stored element is rounded once.  row_mask uint8 [N] or NULL: of rows with 0 nothing is read (they may hold
+ * NaN), their outputs (gradients included) are 0 and they add nothing to a weight gradient.  N <= 2^31 - 1.  Outputs
+ * must not overlap inputs.  N = 0 launches nothing, apart from the zeros of a weight gradient that is not accumulated.
+ *
+ * Norm:       xhat = (x - mean) rstd,  rstd = 1 / sqrt(mean((x - mean)^2) + eps),  y = xhat gamma + beta
+ *   A3PO_NORM_LAYER: mean = sum(x) / H;  A3PO_NORM_RMS: mean = 0 (mean and grad_beta must be NULL).
+ *   gamma [H], beta [H] or NULL: dtype dt.  mean, rstd: fp32 [N] outputs of the forward, or NULL if no backward
+ *   follows; inputs of the backward.
+ * Its backward:  gx = grad_y gamma;  grad_x = rstd (gx - [mean(gx)] - xhat mean(gx xhat))   ([.]: layer norm only)
+ *   grad_gamma = sum_t grad_y xhat, grad_beta = sum_t grad_y: fp32 [H], added to what is there when
+ *   accumulate_grad_w != 0, else overwritten; grad_beta may be NULL.  Sums are taken in a fixed order: results are
+ *   bit-identical from run to run on the same GPU model.  ws: a3po_norm_bwd_workspace_bytes(N, H), 256-byte aligned.
+ *
+ * Dropout:    d(x)[t, c] = x[t, c] 65536 / (65536 - T) if u16(t, c) >= T else 0,   T = round(65536 p), 0 <= p <= 1
+ *   (p is taken to the nearest multiple of 2^-16 and the scale is exact for that).  y = residual + d(x); residual
+ *   [N, H] or NULL.  The mask is never stored: u16(t, c) is the (c mod 8)-th of the eight 16-bit halves (low half
+ *   first) of Philox4x32-10 with key = seed and counter = (c / 8, t, low word of offset, high word of offset).
+ *   rng: device pointer to {seed, offset} (two uint64, 8-byte aligned; NULL only if p = 0), read when the kernel
+ *   runs, so a captured graph draws a new mask whenever the words have changed.  The backward (and any
+ *   recomputation) passes the same p and words; calls that need different masks differ in offset or seed.
+ *   Backward:  grad_x = d(grad_y).
+ *
+ * Join:       r = residual + d(x)  (stored),   y = norm(r)       dropout, add and norm in one pass
+ *   Backward: grad_residual = norm's grad_x of (r, grad_y) + grad_r,   grad_x = d(grad_residual before rounding);
+ *   grad_r [N, H] or NULL: the gradient that reaches r past the norm.
+ * ------------------------------------------------------------------------------------------ */
+typedef enum { A3PO_NORM_RMS = 0, A3PO_NORM_LAYER = 1 } a3po_norm_kind;
+
+int a3po_norm_fwd(const void* x, const void* gamma, const void* beta, const uint8_t* row_mask, int64_t N, int H,
+                  a3po_dtype dt, a3po_norm_kind kind, float eps, void* y, float* mean, float* rstd, void* stream);
+
+size_t a3po_norm_bwd_workspace_bytes(int64_t N, int H);
+
+int a3po_norm_bwd(const void* x, const void* gamma, const float* mean, const float* rstd, const uint8_t* row_mask,
+                  const void* grad_y, int64_t N, int H, a3po_dtype dt, a3po_norm_kind kind, void* grad_x,
+                  float* grad_gamma, float* grad_beta, int accumulate_grad_w, void* ws, size_t ws_bytes,
+                  void* stream);
+
+int a3po_dropout_fwd(const void* x, const void* residual, const uint8_t* row_mask, int64_t N, int H, a3po_dtype dt,
+                     float p, const uint64_t* rng, void* y, void* stream);
+
+int a3po_dropout_bwd(const void* grad_y, const uint8_t* row_mask, int64_t N, int H, a3po_dtype dt, float p,
+                     const uint64_t* rng, void* grad_x, void* stream);
+
+int a3po_dropout_norm_fwd(const void* x, const void* residual, float p, const uint64_t* rng, const void* gamma,
+                          const void* beta, const uint8_t* row_mask, int64_t N, int H, a3po_dtype dt,
+                          a3po_norm_kind kind, float eps, void* r, void* y, float* mean, float* rstd, void* stream);
+
+int a3po_dropout_norm_bwd(const void* r, float p, const uint64_t* rng, const void* gamma, const float* mean,
+                          const float* rstd, const uint8_t* row_mask, const void* grad_y, const void* grad_r,
+                          int64_t N, int H, a3po_dtype dt, a3po_norm_kind kind, void* grad_residual, void* grad_x,
+                          float* grad_gamma, float* grad_beta, int accumulate_grad_w, void* ws, size_t ws_bytes,
+                          void* stream);
+
 /* Bytes the host entries of this library have copied host->device in the calling process since
  * load (monotonic; for transfer accounting in benchmarks). */
 int64_t a3po_host_to_device_bytes(void);

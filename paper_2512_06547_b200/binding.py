@@ -17,6 +17,8 @@ LIB_PATH = os.path.join(_HERE, "lib", "liba3po.so")
 
 A3PO_F32 = 0
 A3PO_BF16 = 1
+A3PO_NORM_RMS = 0
+A3PO_NORM_LAYER = 1
 STATUS_TARGET_OUT_OF_RANGE = 1
 STATUS_WAIT_TIMEOUT = 2
 STATUS_KEPT_RANGE = 4
@@ -84,6 +86,19 @@ _SIGNATURES = {
     "a3po_train_step_host": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int, c_int,
                                      c_int, c_int32, c_float, c_float, c_void_p, c_void_p, c_int, c_void_p, c_void_p,
                                      c_size_t, c_void_p, c_size_t, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "a3po_norm_fwd": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int, c_int, c_int, c_float, c_void_p,
+                              c_void_p, c_void_p, c_void_p]),
+    "a3po_norm_bwd_workspace_bytes": (c_size_t, [c_int64, c_int]),
+    "a3po_norm_bwd": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int, c_int, c_int,
+                              c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_size_t, c_void_p]),
+    "a3po_dropout_fwd": (c_int, [c_void_p, c_void_p, c_void_p, c_int64, c_int, c_int, c_float, c_void_p, c_void_p,
+                                 c_void_p]),
+    "a3po_dropout_bwd": (c_int, [c_void_p, c_void_p, c_int64, c_int, c_int, c_float, c_void_p, c_void_p, c_void_p]),
+    "a3po_dropout_norm_fwd": (c_int, [c_void_p, c_void_p, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int,
+                                      c_int, c_int, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "a3po_dropout_norm_bwd": (c_int, [c_void_p, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                      c_void_p, c_int64, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_void_p,
+                                      c_int, c_void_p, c_size_t, c_void_p]),
 }
 
 _lib = None
@@ -471,3 +486,120 @@ def a3po_train_step_host(h_hidden, h_targets, h_behav_logp, h_versions, h_adv, h
         int(bool(accumulate_grad_w)), _ptr(d_grad_hidden), _ptr(d_stage), d_stage.numel(), _ptr(d_ws), d_ws.numel(),
         _ptr(h_loss), _ptr(h_stats), _ptr(d_status), _stream(stream))
     _check("a3po_train_step_host", rc)
+
+
+# ------------------------------------------------------------------------------ rows in front of the LM head
+def _row_shapes(n, h, mats, vecs=(), per_row=(), row_mask=None):
+    """Shapes of the row operators: matrices [n, h], parameters [h], per-row scalars [n]."""
+    for t in mats:
+        if t is not None and tuple(t.shape) != (n, h):
+            raise ValueError("shape mismatch")
+    for t in vecs:
+        if t is not None and t.numel() != h:
+            raise ValueError("shape mismatch")
+    for t in (*per_row, row_mask):
+        if t is not None and t.numel() != n:
+            raise ValueError("shape mismatch")
+
+
+def _rng_words(rng, p):
+    """{seed, offset}: an int64 device tensor of two words (their bits are taken as uint64)."""
+    if rng is None:
+        if p > 0:
+            raise ValueError("rng: {seed, offset} needed for p > 0")
+        return
+    _want(rng, torch.int64, "rng")
+    if rng.numel() != 2:
+        raise ValueError("rng: expected the two words {seed, offset}")
+
+
+def a3po_norm_bwd_workspace_bytes(N, H) -> int:
+    return load_library().a3po_norm_bwd_workspace_bytes(N, H)
+
+
+def a3po_norm_fwd(x, gamma, y, rstd=None, *, kind=A3PO_NORM_RMS, beta=None, mean=None, eps=1e-6, row_mask=None,
+                  stream=None):
+    """y = norm(x) gamma + beta; mean / rstd (fp32 [N]) are left for the backward when given."""
+    dt = _dtype_code(x)
+    for t, nm in ((x, "x"), (gamma, "gamma"), (beta, "beta"), (y, "y")):
+        _want(t, x.dtype, nm)
+    _want(rstd, torch.float32, "rstd"); _want(mean, torch.float32, "mean"); _want(row_mask, torch.uint8, "row_mask")
+    n, h = x.shape
+    _row_shapes(n, h, (y,), (gamma, beta), (mean, rstd), row_mask)
+    rc = load_library().a3po_norm_fwd(_ptr(x), _ptr(gamma), _ptr(beta), _ptr(row_mask), n, h, dt, kind, float(eps),
+                                      _ptr(y), _ptr(mean), _ptr(rstd), _stream(stream))
+    _check("a3po_norm_fwd", rc)
+
+
+def a3po_norm_bwd(x, gamma, rstd, grad_y, grad_x, grad_gamma, ws, *, kind=A3PO_NORM_RMS, mean=None, grad_beta=None,
+                  accumulate_grad_w=False, row_mask=None, stream=None):
+    dt = _dtype_code(x)
+    for t, nm in ((x, "x"), (gamma, "gamma"), (grad_y, "grad_y"), (grad_x, "grad_x")):
+        _want(t, x.dtype, nm)
+    for t, nm in ((rstd, "rstd"), (mean, "mean"), (grad_gamma, "grad_gamma"), (grad_beta, "grad_beta")):
+        _want(t, torch.float32, nm)
+    _want(row_mask, torch.uint8, "row_mask"); _want(ws, torch.uint8, "ws")
+    n, h = x.shape
+    _row_shapes(n, h, (grad_y, grad_x), (gamma, grad_gamma, grad_beta), (mean, rstd), row_mask)
+    rc = load_library().a3po_norm_bwd(_ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(row_mask), _ptr(grad_y), n, h,
+                                      dt, kind, _ptr(grad_x), _ptr(grad_gamma), _ptr(grad_beta),
+                                      int(bool(accumulate_grad_w)), _ptr(ws), ws.numel(), _stream(stream))
+    _check("a3po_norm_bwd", rc)
+
+
+def a3po_dropout_fwd(x, p, rng, y, *, residual=None, row_mask=None, stream=None):
+    """y = residual + dropout(x); the mask is a function of rng = {seed, offset} and the element's place."""
+    dt = _dtype_code(x)
+    _want(x, x.dtype, "x"); _want(residual, x.dtype, "residual"); _want(y, x.dtype, "y")
+    _want(row_mask, torch.uint8, "row_mask"); _rng_words(rng, p)
+    n, h = x.shape
+    _row_shapes(n, h, (residual, y), row_mask=row_mask)
+    rc = load_library().a3po_dropout_fwd(_ptr(x), _ptr(residual), _ptr(row_mask), n, h, dt, float(p), _ptr(rng),
+                                         _ptr(y), _stream(stream))
+    _check("a3po_dropout_fwd", rc)
+
+
+def a3po_dropout_bwd(grad_y, p, rng, grad_x, *, row_mask=None, stream=None):
+    dt = _dtype_code(grad_y)
+    _want(grad_y, grad_y.dtype, "grad_y"); _want(grad_x, grad_y.dtype, "grad_x")
+    _want(row_mask, torch.uint8, "row_mask"); _rng_words(rng, p)
+    n, h = grad_y.shape
+    _row_shapes(n, h, (grad_x,), row_mask=row_mask)
+    rc = load_library().a3po_dropout_bwd(_ptr(grad_y), _ptr(row_mask), n, h, dt, float(p), _ptr(rng), _ptr(grad_x),
+                                         _stream(stream))
+    _check("a3po_dropout_bwd", rc)
+
+
+def a3po_dropout_norm_fwd(x, residual, p, rng, gamma, r, y, rstd=None, *, kind=A3PO_NORM_RMS, beta=None, mean=None,
+                          eps=1e-6, row_mask=None, stream=None):
+    """r = residual + dropout(x), y = norm(r) gamma + beta, in one pass."""
+    dt = _dtype_code(x)
+    for t, nm in ((x, "x"), (residual, "residual"), (gamma, "gamma"), (beta, "beta"), (r, "r"), (y, "y")):
+        _want(t, x.dtype, nm)
+    _want(rstd, torch.float32, "rstd"); _want(mean, torch.float32, "mean"); _want(row_mask, torch.uint8, "row_mask")
+    _rng_words(rng, p)
+    n, h = x.shape
+    _row_shapes(n, h, (residual, r, y), (gamma, beta), (mean, rstd), row_mask)
+    rc = load_library().a3po_dropout_norm_fwd(_ptr(x), _ptr(residual), float(p), _ptr(rng), _ptr(gamma), _ptr(beta),
+                                              _ptr(row_mask), n, h, dt, kind, float(eps), _ptr(r), _ptr(y), _ptr(mean),
+                                              _ptr(rstd), _stream(stream))
+    _check("a3po_dropout_norm_fwd", rc)
+
+
+def a3po_dropout_norm_bwd(r, p, rng, gamma, rstd, grad_y, grad_residual, grad_x, grad_gamma, ws, *,
+                          kind=A3PO_NORM_RMS, mean=None, grad_r=None, grad_beta=None, accumulate_grad_w=False,
+                          row_mask=None, stream=None):
+    dt = _dtype_code(r)
+    for t, nm in ((r, "r"), (gamma, "gamma"), (grad_y, "grad_y"), (grad_r, "grad_r"),
+                  (grad_residual, "grad_residual"), (grad_x, "grad_x")):
+        _want(t, r.dtype, nm)
+    for t, nm in ((rstd, "rstd"), (mean, "mean"), (grad_gamma, "grad_gamma"), (grad_beta, "grad_beta")):
+        _want(t, torch.float32, nm)
+    _want(row_mask, torch.uint8, "row_mask"); _want(ws, torch.uint8, "ws"); _rng_words(rng, p)
+    n, h = r.shape
+    _row_shapes(n, h, (grad_y, grad_r, grad_residual, grad_x), (gamma, grad_gamma, grad_beta), (mean, rstd), row_mask)
+    rc = load_library().a3po_dropout_norm_bwd(_ptr(r), float(p), _ptr(rng), _ptr(gamma), _ptr(mean), _ptr(rstd),
+                                              _ptr(row_mask), _ptr(grad_y), _ptr(grad_r), n, h, dt, kind,
+                                              _ptr(grad_residual), _ptr(grad_x), _ptr(grad_gamma), _ptr(grad_beta),
+                                              int(bool(accumulate_grad_w)), _ptr(ws), ws.numel(), _stream(stream))
+    _check("a3po_dropout_norm_bwd", rc)

@@ -31,6 +31,7 @@ enum KernelId : int {
   kKLossFwd = 0, kKLossBwd, kKLossFwdBwd, kKLossFinalize, kKMaskCount, kKMaskCountFinalize, kKExpandVersions,
   kKMergePartials, kKSimtFwd, kKSimtDz, kKSimtGemm, kKTcFwd, kKTcDz, kKTcGradHidden, kKTcGradW, kKCompact, kKGrpo,
   kKSelfTest, kKTcFwdKeep, kKKeptRows, kKH2D, kKMoveRows,
+  kKNorm, kKNormBwd, kKDropout, kKFfnGate, kKFfnDown, kKFfnGradGate, kKFfnGradX, kKFfnGradW, kKFfnFew, kKFfnSimt,
   kKernelIdCount
 };
 

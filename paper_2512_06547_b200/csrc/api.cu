@@ -211,7 +211,7 @@ const char* a3po_status_string(int code) {
   }
 }
 
-int a3po_version(void) { return 2000; }
+int a3po_version(void) { return 2001; }
 
 int a3po_selftest_wait_timeout(uint32_t* status, unsigned timeout_ms, void* stream) {
   if (!status || timeout_ms == 0 || timeout_ms > 2000) return A3PO_ERR_INVALID_ARG;
@@ -226,7 +226,9 @@ const char* a3po_kernel_name(int kernel_id) {
       "loss_fwd", "loss_bwd", "loss_fwd_bwd", "loss_finalize", "mask_count", "mask_count_finalize",
       "expand_versions", "merge_partials", "lmhead_fwd_fp32pipe", "lmhead_dz_fp32pipe", "gemm_fp32pipe",
       "gemm_tn<fwd_logsoftmax>", "gemm_tn<dz>", "gemm_tn<grad_hidden>", "gemm_tn<grad_w>", "compact_rows", "grpo_advantages", "selftest",
-      "gemm_tn<fwd_logsoftmax+keep>", "kept_rows", "h2d_copies", "move_kept_rows"};
+      "gemm_tn<fwd_logsoftmax+keep>", "kept_rows", "h2d_copies", "move_kept_rows",
+      "norm_fwd", "norm_bwd", "dropout", "gemm_tn<ffn_gate_up>", "gemm_tn<ffn_down>", "gemm_tn<ffn_grad_gate_up>",
+      "gemm_tn<ffn_grad_x>", "gemm_tn<ffn_grad_w>", "ffn_few_rows", "ffn_fp32pipe"};
   return (kernel_id >= 0 && kernel_id < kKernelIdCount) ? names[kernel_id] : "?";
 }
 
