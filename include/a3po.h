@@ -448,6 +448,45 @@ int a3po_dropout_norm_bwd(const void* r, float p, const uint64_t* rng, const voi
                           float* grad_gamma, float* grad_beta, int accumulate_grad_w, void* ws, size_t ws_bytes,
                           void* stream);
 
+/* --------------------------------------------------------------------------------------------
+ * Gated feed-forward block (no counterpart in the paper: the layer of the policy below the final norm).
+ *
+ *   g = x Wg^T,  u = x Wu^T,  h = act(g) u,  y = h Wd^T           act: SiLU g / (1 + exp(-g)), or the tanh form of GELU
+ *   dh = grad_y Wd,  dg = dh u act'(g),  du = dh act(g)
+ *   grad_x = dg Wg + du Wu,  grad_Wg = dg^T x,  grad_Wu = du^T x,  grad_Wd = grad_y^T h
+ *
+ * x, y, grad_x, grad_y [N, H]; w_gate_up [2 F, H] (the F rows of Wg, then the F rows of Wu); w_down [H, F]; dtype `dt`,
+ * 16-byte aligned.  Any H and F: bf16 with H and F multiples of 8 runs on the tensor cores, the rest on the FP32 pipes.
+ * Both projections, the activation and the product are one kernel; dh never reaches memory either.  Accumulation is
+ * fp32; for bf16 the intermediates that enter a matrix product (h, dg, du) and the kept g and u are rounded to bf16.
+ *
+ * row_mask uint8 [N] or NULL: rows with 0 are skipped (of more than 32 rows only the others are multiplied): nothing
+ * of them is read, their y and grad_x are 0, they add nothing to a weight gradient.
+ * kept: device buffer of a3po_gated_ffn_kept_bytes(N, F, dt) bytes, 256-byte aligned, that receives g and u for the
+ * backward (layout private; about 4 N F bytes for bf16), or NULL when no backward follows.  The backward takes it with
+ * the forward's x, weights, row_mask, N, H, F, dt and act; it is not changed, so the backward may be repeated.
+ * grad_w_gate_up [2 F, H], grad_w_down [H, F]: dtype grad_w_dt (A3PO_F32, or dt), overwritten; with
+ * accumulate_grad_w != 0 added to (A3PO_F32 only, else A3PO_ERR_UNSUPPORTED).
+ * ws: a3po_gated_ffn_workspace_bytes(N, H, F, dt, row_mask given, backward) bytes, 256-byte aligned; for bf16 about
+ * 2 N F bytes forward and 6 N F backward, plus 2 to 3 times 2 N H with a row_mask.
+ * status: optional device word (A3PO_STATUS_WAIT_TIMEOUT).  Outputs must not overlap inputs.  N = 0 launches nothing
+ * except the zeros of weight gradients that are not accumulated.  Results are bit-identical from run to run.
+ * ------------------------------------------------------------------------------------------ */
+typedef enum { A3PO_ACT_SILU = 0, A3PO_ACT_GELU_TANH = 1 } a3po_activation;
+
+size_t a3po_gated_ffn_kept_bytes(int64_t N, int F, a3po_dtype dt);
+size_t a3po_gated_ffn_workspace_bytes(int64_t N, int H, int F, a3po_dtype dt, int has_row_mask, int is_bwd);
+
+int a3po_gated_ffn_fwd(const void* x, const void* w_gate_up, const void* w_down, const uint8_t* row_mask, int64_t N,
+                       int H, int F, a3po_dtype dt, a3po_activation act, void* y, void* kept, size_t kept_bytes,
+                       void* ws, size_t ws_bytes, uint32_t* status, void* stream);
+
+int a3po_gated_ffn_bwd(const void* x, const void* w_gate_up, const void* w_down, const uint8_t* row_mask,
+                       const void* kept, size_t kept_bytes, const void* grad_y, int64_t N, int H, int F, a3po_dtype dt,
+                       a3po_activation act, void* grad_x, void* grad_w_gate_up, void* grad_w_down,
+                       a3po_dtype grad_w_dt, int accumulate_grad_w, void* ws, size_t ws_bytes, uint32_t* status,
+                       void* stream);
+
 /* Bytes the host entries of this library have copied host->device in the calling process since
  * load (monotonic; for transfer accounting in benchmarks). */
 int64_t a3po_host_to_device_bytes(void);

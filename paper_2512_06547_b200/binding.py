@@ -17,6 +17,8 @@ LIB_PATH = os.path.join(_HERE, "lib", "liba3po.so")
 
 A3PO_F32 = 0
 A3PO_BF16 = 1
+A3PO_ACT_SILU = 0
+A3PO_ACT_GELU_TANH = 1
 A3PO_NORM_RMS = 0
 A3PO_NORM_LAYER = 1
 STATUS_TARGET_OUT_OF_RANGE = 1
@@ -99,6 +101,13 @@ _SIGNATURES = {
     "a3po_dropout_norm_bwd": (c_int, [c_void_p, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                       c_void_p, c_int64, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_void_p,
                                       c_int, c_void_p, c_size_t, c_void_p]),
+    "a3po_gated_ffn_kept_bytes": (c_size_t, [c_int64, c_int, c_int]),
+    "a3po_gated_ffn_workspace_bytes": (c_size_t, [c_int64, c_int, c_int, c_int, c_int, c_int]),
+    "a3po_gated_ffn_fwd": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int, c_int, c_int, c_int, c_void_p,
+                                   c_void_p, c_size_t, c_void_p, c_size_t, c_void_p, c_void_p]),
+    "a3po_gated_ffn_bwd": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p, c_int64, c_int,
+                                   c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_int, c_int, c_void_p, c_size_t,
+                                   c_void_p, c_void_p]),
 }
 
 _lib = None
@@ -603,3 +612,58 @@ def a3po_dropout_norm_bwd(r, p, rng, gamma, rstd, grad_y, grad_residual, grad_x,
                                               _ptr(grad_residual), _ptr(grad_x), _ptr(grad_gamma), _ptr(grad_beta),
                                               int(bool(accumulate_grad_w)), _ptr(ws), ws.numel(), _stream(stream))
     _check("a3po_dropout_norm_bwd", rc)
+
+
+# ------------------------------------------------------------------------------ gated feed-forward block
+def a3po_gated_ffn_kept_bytes(N, F, dt) -> int:
+    return load_library().a3po_gated_ffn_kept_bytes(N, F, dt)
+
+
+def a3po_gated_ffn_workspace_bytes(N, H, F, dt, has_row_mask, is_bwd) -> int:
+    return load_library().a3po_gated_ffn_workspace_bytes(N, H, F, dt, int(bool(has_row_mask)), int(bool(is_bwd)))
+
+
+def _ffn_shapes(x, w_gate_up, w_down, mats, row_mask):
+    n, h = x.shape
+    f = w_down.shape[1]
+    if tuple(w_gate_up.shape) != (2 * f, h) or w_down.shape[0] != h:
+        raise ValueError("shape mismatch")
+    _row_shapes(n, h, mats, row_mask=row_mask)
+    return n, h, f
+
+
+def a3po_gated_ffn_fwd(x, w_gate_up, w_down, y, ws, *, row_mask=None, kept=None, activation=A3PO_ACT_SILU, status=None,
+                       stream=None):
+    """y = (act(x Wg^T) * (x Wu^T)) Wd^T; w_gate_up stacks Wg and Wu.  `kept` (uint8 buffer of
+    a3po_gated_ffn_kept_bytes) is filled for a3po_gated_ffn_bwd when given."""
+    dt = _dtype_code(x)
+    for t, nm in ((x, "x"), (w_gate_up, "w_gate_up"), (w_down, "w_down"), (y, "y")):
+        _want(t, x.dtype, nm)
+    _want(row_mask, torch.uint8, "row_mask"); _want(kept, torch.uint8, "kept"); _want(ws, torch.uint8, "ws")
+    _want(status, torch.int32, "status")
+    n, h, f = _ffn_shapes(x, w_gate_up, w_down, (y,), row_mask)
+    rc = load_library().a3po_gated_ffn_fwd(_ptr(x), _ptr(w_gate_up), _ptr(w_down), _ptr(row_mask), n, h, f, dt, activation,
+                                           _ptr(y), _ptr(kept), 0 if kept is None else kept.numel(), _ptr(ws), ws.numel(),
+                                           _ptr(status), _stream(stream))
+    _check("a3po_gated_ffn_fwd", rc)
+
+
+def a3po_gated_ffn_bwd(x, w_gate_up, w_down, kept, grad_y, grad_x, grad_w_gate_up, grad_w_down, ws, *, row_mask=None,
+                       activation=A3PO_ACT_SILU, accumulate_grad_w=False, status=None, stream=None):
+    """Gradients of a3po_gated_ffn_fwd from what it kept; the weight gradients are fp32 or of the weights' type."""
+    dt = _dtype_code(x)
+    for t, nm in ((x, "x"), (w_gate_up, "w_gate_up"), (w_down, "w_down"), (grad_y, "grad_y"), (grad_x, "grad_x")):
+        _want(t, x.dtype, nm)
+    gdt = _dtype_code(grad_w_down)
+    for t, nm in ((grad_w_gate_up, "grad_w_gate_up"), (grad_w_down, "grad_w_down")):
+        _want(t, grad_w_down.dtype, nm)
+    _want(row_mask, torch.uint8, "row_mask"); _want(kept, torch.uint8, "kept"); _want(ws, torch.uint8, "ws")
+    _want(status, torch.int32, "status")
+    n, h, f = _ffn_shapes(x, w_gate_up, w_down, (grad_y, grad_x), row_mask)
+    if grad_w_gate_up.shape != w_gate_up.shape or grad_w_down.shape != w_down.shape:
+        raise ValueError("shape mismatch")
+    rc = load_library().a3po_gated_ffn_bwd(_ptr(x), _ptr(w_gate_up), _ptr(w_down), _ptr(row_mask), _ptr(kept),
+                                           kept.numel(), _ptr(grad_y), n, h, f, dt, activation, _ptr(grad_x),
+                                           _ptr(grad_w_gate_up), _ptr(grad_w_down), gdt, int(bool(accumulate_grad_w)),
+                                           _ptr(ws), ws.numel(), _ptr(status), _stream(stream))
+    _check("a3po_gated_ffn_bwd", rc)

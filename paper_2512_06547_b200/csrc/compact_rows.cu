@@ -104,7 +104,7 @@ compact_fill_kernel(const uint8_t* __restrict__ row_mask, const float* __restric
     if (t < hi) pos[t] = k ? c : -1;
     if (k) {
       idx[c] = static_cast<int>(t);
-      targets_c[c] = targets[t];
+      if (targets_c) targets_c[c] = targets[t];
       if (lse_c) lse_c[c] = lse[t];
       if (g_c) g_c[c] = g[t];
     }
@@ -122,7 +122,7 @@ compact_fill_kernel(const uint8_t* __restrict__ row_mask, const float* __restric
   for (long long c = kept + static_cast<long long>(blockIdx.x) * kCompactThreads + threadIdx.x; c < cap; c += stride) {
     if (g_c) g_c[c] = 0.f;
     if (lse_c) lse_c[c] = 0.f;
-    targets_c[c] = 0;
+    if (targets_c) targets_c[c] = 0;
     idx[c] = 0;
   }
 }

@@ -106,6 +106,13 @@ __device__ __forceinline__ void tma_reduce_add_f32_2d(const CUtensorMap* map, co
                "r"(smem_u32(smem_src)), "r"(x), "r"(y)
                : "memory");
 }
+// Three coordinates (x innermost).
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, const void* smem_src, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(
+                   reinterpret_cast<uint64_t>(map)),
+               "r"(smem_u32(smem_src)), "r"(x), "r"(y), "r"(z)
+               : "memory");
+}
 __device__ __forceinline__ void bulk_commit_group() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 // Waits until at most N of this thread's committed bulk groups still read their shared-memory source.
 template <int N>
