@@ -418,7 +418,8 @@ int a3po_train_step_host(const void* h_hidden, const int32_t* h_targets, const f
  *
  * Join:       r = residual + d(x)  (stored),   y = norm(r)       dropout, add and norm in one pass
  *   Backward: grad_residual = norm's grad_x of (r, grad_y) + grad_r,   grad_x = d(grad_residual before rounding);
- *   grad_r [N, H] or NULL: the gradient that reaches r past the norm.
+ *   grad_r [N, H] or NULL: the gradient that reaches r past the norm.  grad_x may be NULL (with p = 0: the backward of
+ *   a norm on a residual stream that nothing joined there).
  * ------------------------------------------------------------------------------------------ */
 typedef enum { A3PO_NORM_RMS = 0, A3PO_NORM_LAYER = 1 } a3po_norm_kind;
 

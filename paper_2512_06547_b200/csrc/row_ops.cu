@@ -303,7 +303,7 @@ struct NormBwdArgs {
   long long n;
   int h;
   float inv_h;
-  T* grad_x;              // gradient of x; with JOIN of the branch (through dropout)
+  T* grad_x;              // gradient of x; with JOIN of the branch (through dropout), or null: not wanted
   T* grad_residual;       // JOIN: gradient of the residual stream
   float* part;            // [parts][1 or 2][h] partial sums of dgamma (and dbeta)
   Dropout drop;
@@ -337,7 +337,7 @@ norm_bwd_kernel(const NormBwdArgs<T> a) {
 #pragma unroll
       for (int j = 0; j < kVec; ++j) z[j] = 0.f;
       for (int col = tid * kVec; col < a.h; col += TPR * kVec) {
-        store_chunk(gx_row, col, a.h, vec, z);
+        if (!JOIN || a.grad_x) store_chunk(gx_row, col, a.h, vec, z);
         if (JOIN) store_chunk(a.grad_residual + t * a.h, col, a.h, vec, z);
       }
       continue;
@@ -381,6 +381,7 @@ norm_bwd_kernel(const NormBwdArgs<T> a) {
           for (int j = 0; j < kVec; ++j) gy[i][j] += gr[j];
         }
         store_chunk(a.grad_residual + t * a.h, col, a.h, vec, gy[i]);
+        if (!a.grad_x) continue;
         if (drop) drop_chunk(gy[i], a.drop, ph, static_cast<uint32_t>(tid + i * TPR), static_cast<uint32_t>(t));
       }
       store_chunk(gx_row, col, a.h, vec, gy[i]);
@@ -509,7 +510,7 @@ norm_bwd_long_kernel(const NormBwdArgs<T> a) {
   for (int j = 0; j < kVec; ++j) z[j] = 0.f;
   if (a.row_mask && a.row_mask[t] == 0) {
     for (int col = threadIdx.x * kVec; col < a.h; col += kLongThreads * kVec) {
-      store_chunk(a.grad_x + t * a.h, col, a.h, vec, z);
+      if (!JOIN || a.grad_x) store_chunk(a.grad_x + t * a.h, col, a.h, vec, z);
       if (JOIN) store_chunk(a.grad_residual + t * a.h, col, a.h, vec, z);
     }
     return;
@@ -548,6 +549,7 @@ norm_bwd_long_kernel(const NormBwdArgs<T> a) {
         for (int j = 0; j < kVec; ++j) gy[j] += g[j];
       }
       store_chunk(a.grad_residual + t * a.h, col, a.h, vec, gy);
+      if (!a.grad_x) continue;
       if (drop) drop_chunk(gy, a.drop, ph, static_cast<uint32_t>(col / kVec), static_cast<uint32_t>(t));
     }
     store_chunk(a.grad_x + t * a.h, col, a.h, vec, gy);
@@ -764,7 +766,7 @@ int norm_bwd_entry(bool join, const void* x, const void* gamma, const float* mea
                    cudaStream_t stream) {
   A3PO_RETURN_IF(check_rows(n, h, dt));
   if (kind != A3PO_NORM_RMS && kind != A3PO_NORM_LAYER) return A3PO_ERR_UNSUPPORTED;
-  if (!gamma || !grad_gamma || (n > 0 && (!x || !rstd || !grad_y || !grad_x))) return A3PO_ERR_INVALID_ARG;
+  if (!gamma || !grad_gamma || (n > 0 && (!x || !rstd || !grad_y || (!join && !grad_x)))) return A3PO_ERR_INVALID_ARG;
   if (n > 0 && kind == A3PO_NORM_LAYER && !mean) return A3PO_ERR_INVALID_ARG;
   if (kind == A3PO_NORM_RMS && grad_beta) return A3PO_ERR_INVALID_ARG;   // an RMS norm has no beta gradient to give
   if (join) {

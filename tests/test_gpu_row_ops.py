@@ -195,6 +195,10 @@ def test_join(n, h, p, layer, dt):
                                    grad_beta=gb, row_mask=c.mask)
         G.check("dropout_norm_bwd")
         gres_ref = check_norm_bwd(c, r, mean, rstd, c.gy, gr, layer, gres, gg, gb)
+        gres2, gg2 = torch.empty_like(gres), torch.empty_like(gg)      # without the branch's gradient: the rest as before
+        a3po.a3po_dropout_norm_bwd(r, 0.0, None, c.gamma, rstd, c.gy, gres2, None, gg2, ws, kind=kind, mean=mean,
+                                   grad_r=gr, row_mask=c.mask)
+        assert torch.equal(gres, gres2) and torch.equal(gg, gg2)
         # grad_x = d(grad_residual before rounding): within the same bound, scaled
         ratio = to_np64(gx)
         ref = gres_ref * keep
