@@ -19,620 +19,156 @@
 // first.  16 bits decide one element: the drop probability is a multiple of 2^-16 and the scale is exact for it, at
 // half the integer work of 32-bit numbers (with those the multiplies, not HBM, would bound dropout).
 
-#include "a3po_common.cuh"
+#include "row_ops.cuh"
 
 namespace a3po {
 namespace {
 
-constexpr int kVec = 8;   // columns of a thread's chunk
-
-// ------------------------------------------------------------------------------------ pieces
-struct Dropout {
-  const unsigned long long* rng;  // device: {seed, offset}; null = nothing is dropped
-  uint32_t threshold;             // element dropped iff u16 < threshold
-  float scale;                    // 65536 / (65536 - threshold), 0 when everything is dropped
-};
-
-struct PhiloxState {
-  uint32_t k0, k1, o0, o1;
-  __device__ __forceinline__ void load(const unsigned long long* rng) {
-    const unsigned long long seed = rng[0], offset = rng[1];
-    k0 = static_cast<uint32_t>(seed);
-    k1 = static_cast<uint32_t>(seed >> 32);
-    o0 = static_cast<uint32_t>(offset);
-    o1 = static_cast<uint32_t>(offset >> 32);
-  }
-  __device__ __forceinline__ uint4 draw(uint32_t group, uint32_t row) const {
-    uint32_t c0 = group, c1 = row, c2 = o0, c3 = o1, a = k0, b = k1;
-#pragma unroll
-    for (int i = 0; i < 10; ++i) {
-      const uint32_t h0 = __umulhi(0xD2511F53u, c0), l0 = 0xD2511F53u * c0;
-      const uint32_t h1 = __umulhi(0xCD9E8D57u, c2), l1 = 0xCD9E8D57u * c2;
-      c0 = h1 ^ c1 ^ a;
-      c1 = l1;
-      c2 = h0 ^ c3 ^ b;
-      c3 = l0;
-      a += 0x9E3779B9u;
-      b += 0xBB67AE85u;
-    }
-    return make_uint4(c0, c1, c2, c3);
-  }
-};
-
-// x -> d(x) for the 8 columns of one chunk
-__device__ __forceinline__ void drop_chunk(float (&x)[kVec], const Dropout& d, const PhiloxState& ph, uint32_t group,
-                                           uint32_t row) {
-  const uint4 w = ph.draw(group, row);
-  const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    x[2 * j] = (words[j] & 0xffffu) >= d.threshold ? x[2 * j] * d.scale : 0.f;
-    x[2 * j + 1] = (words[j] >> 16) >= d.threshold ? x[2 * j + 1] * d.scale : 0.f;
-  }
-}
-
-// Eight columns of a row.  `vec`: rows are 16-byte aligned and h % 8 == 0, so a chunk is whole and moves in 16-byte
-// pieces; otherwise element by element, columns at and beyond h read as 0 and are not written.
-template <typename T>
-__device__ __forceinline__ void load_chunk(const T* row, int col, int h, bool vec, float (&x)[kVec]) {
-  if (vec) {
-    if (col < h) {
-      if constexpr (sizeof(T) == 2) {
-        const uint4 u = __ldcs(reinterpret_cast<const uint4*>(row + col));
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          x[2 * j] = __uint_as_float(w[j] << 16);
-          x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-        }
-      } else {
-        const float4 a = __ldcs(reinterpret_cast<const float4*>(row + col));
-        const float4 b = __ldcs(reinterpret_cast<const float4*>(row + col) + 1);
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-        x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-      }
-      return;
-    }
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) x[j] = 0.f;
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < kVec; ++j) x[j] = (col + j < h) ? to_float(row[col + j]) : 0.f;
-}
-
-template <typename T>
-__device__ __forceinline__ void store_chunk(T* row, int col, int h, bool vec, const float (&x)[kVec]) {
-  if (vec) {
-    if (col >= h) return;
-    if constexpr (sizeof(T) == 2) {
-      uint4 u;
-      uint32_t w[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
-        w[j] = *reinterpret_cast<uint32_t*>(&p);
-      }
-      u.x = w[0]; u.y = w[1]; u.z = w[2]; u.w = w[3];
-      __stcs(reinterpret_cast<uint4*>(row + col), u);
-    } else {
-      __stcs(reinterpret_cast<float4*>(row + col), make_float4(x[0], x[1], x[2], x[3]));
-      __stcs(reinterpret_cast<float4*>(row + col) + 1, make_float4(x[4], x[5], x[6], x[7]));
-    }
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < kVec; ++j)
-    if (col + j < h) row[col + j] = from_float<T>(x[j]);
-}
-
-// Parameters (gamma, beta) are shared by every row: the default load keeps them in L1.
-template <typename T>
-__device__ __forceinline__ void load_param(const T* __restrict__ p, int col, int h, bool vec, float (&x)[kVec]) {
-  if (vec && sizeof(T) == 2) {
-    uint4 u = make_uint4(0, 0, 0, 0);
-    if (col < h) u = __ldg(reinterpret_cast<const uint4*>(p + col));
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      x[2 * j] = __uint_as_float(w[j] << 16);
-      x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-    }
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < kVec; ++j) x[j] = (col + j < h) ? to_float(p[col + j]) : 0.f;
-}
-
-// Rounds to the storage type and back.
-template <typename T>
-__device__ __forceinline__ float as_stored(float x) { return to_float(from_float<T>(x)); }
-
-// Sum over the TPR threads of a row (a warp, or the whole block).
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float* sh) {
-  v = warp_sum(v);
-  if constexpr (TPR > kWarp) {
-    const int warp = threadIdx.x / kWarp;
-    __syncthreads();   // the previous use of `sh` has been read
-    if (threadIdx.x % kWarp == 0) sh[warp] = v;
-    __syncthreads();
-    float t = 0.f;
-#pragma unroll
-    for (int w = 0; w < TPR / kWarp; ++w) t += sh[w];
-    v = t;
-  }
-  return v;
-}
-template <int TPR>
-__device__ __forceinline__ float2 row_sum2(float a, float b, float2* sh) {
-  a = warp_sum(a);
-  b = warp_sum(b);
-  if constexpr (TPR > kWarp) {
-    const int warp = threadIdx.x / kWarp;
-    __syncthreads();
-    if (threadIdx.x % kWarp == 0) sh[warp] = make_float2(a, b);
-    __syncthreads();
-    a = b = 0.f;
-#pragma unroll
-    for (int w = 0; w < TPR / kWarp; ++w) {
-      a += sh[w].x;
-      b += sh[w].y;
-    }
-  }
-  return make_float2(a, b);
-}
-
-// Rows a block works on at once: blocks of 256 threads hold several rows when a row is a warp's, one otherwise.
-template <int TPR> constexpr int threads_of() { return TPR == kWarp ? 256 : TPR; }
-template <int TPR> constexpr int rows_per_block() { return TPR == kWarp ? 256 / kWarp : 1; }
-
-template <typename T>
-struct NormFwdArgs {
-  const T* x;           // normalised input; with JOIN the branch that goes through dropout
-  const T* residual;    // JOIN: residual stream
-  const T* gamma;
-  const T* beta;        // null: none
-  const uint8_t* row_mask;
-  long long n;
-  int h;
-  float eps;
-  float inv_h;
-  T* r;                 // JOIN: stored sum
-  T* y;
-  float* mean;          // null: not wanted
-  float* rstd;          // null: not wanted
-  Dropout drop;
-  int vec;
-};
-
-// One row per TPR threads, the row in registers between its statistics and its result.
-template <typename T, int TPR, int CPT, bool LAYER, bool JOIN>
-__global__ void __launch_bounds__(threads_of<TPR>())
-norm_fwd_kernel(const NormFwdArgs<T> a) {
-  __shared__ float sh[kWarp];
-  const int tid = threadIdx.x % TPR;
-  const long long t = static_cast<long long>(blockIdx.x) * rows_per_block<TPR>() + threadIdx.x / TPR;
-  if (t >= a.n) return;                 // whole warps (TPR = 32), or never (one row per block)
-  const bool vec = a.vec != 0;
-  T* y = a.y + t * a.h;
-  float v[CPT][kVec];
-  if (a.row_mask && a.row_mask[t] == 0) {   // same for all threads of the row
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) v[0][j] = 0.f;
-    for (int col = tid * kVec; col < a.h; col += TPR * kVec) {
-      store_chunk(y, col, a.h, vec, v[0]);
-      if (JOIN) store_chunk(a.r + t * a.h, col, a.h, vec, v[0]);
-    }
-    if (tid == 0) {
-      if (a.mean) a.mean[t] = 0.f;
-      if (a.rstd) a.rstd[t] = 0.f;
-    }
-    return;
-  }
-  const T* x = a.x + t * a.h;
-#pragma unroll
-  for (int i = 0; i < CPT; ++i) load_chunk(x, (tid + i * TPR) * kVec, a.h, vec, v[i]);
-  if constexpr (JOIN) {
-    float res[CPT][kVec];
-#pragma unroll
-    for (int i = 0; i < CPT; ++i) load_chunk(a.residual + t * a.h, (tid + i * TPR) * kVec, a.h, vec, res[i]);
-    const bool drop = a.drop.rng != nullptr;
-    PhiloxState ph;
-    if (drop) ph.load(a.drop.rng);
-#pragma unroll
-    for (int i = 0; i < CPT; ++i) {
-      if (drop) drop_chunk(v[i], a.drop, ph, static_cast<uint32_t>(tid + i * TPR), static_cast<uint32_t>(t));
-      // the norm is that of the stored sum, which is what the backward will read
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) v[i][j] = as_stored<T>(v[i][j] + res[i][j]);
-      store_chunk(a.r + t * a.h, (tid + i * TPR) * kVec, a.h, vec, v[i]);
-    }
-  }
-  float mean = 0.f;
-  if constexpr (LAYER) {
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < CPT; ++i)
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) s += v[i][j];
-    mean = row_sum<TPR>(s, sh) * a.inv_h;
-  }
-  float q = 0.f;
-#pragma unroll
-  for (int i = 0; i < CPT; ++i) {
-    const int col = (tid + i * TPR) * kVec;
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      if (LAYER) v[i][j] = (col + j < a.h) ? v[i][j] - mean : 0.f;
-      q = fmaf(v[i][j], v[i][j], q);
-    }
-  }
-  const float rstd = 1.0f / sqrtf(row_sum<TPR>(q, sh) * a.inv_h + a.eps);
-  if (tid == 0) {
-    if (a.mean) a.mean[t] = mean;
-    if (a.rstd) a.rstd[t] = rstd;
-  }
-#pragma unroll
-  for (int i = 0; i < CPT; ++i) {
-    const int col = (tid + i * TPR) * kVec;
-    float g[kVec];
-    load_param(a.gamma, col, a.h, vec, g);
-    if (a.beta) {
-      float b[kVec];
-      load_param(a.beta, col, a.h, vec, b);
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) v[i][j] = fmaf(v[i][j] * rstd, g[j], b[j]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) v[i][j] = v[i][j] * rstd * g[j];
-    }
-    store_chunk(y, col, a.h, vec, v[i]);
-  }
-}
-
-template <typename T>
-struct NormBwdArgs {
-  const T* x;             // what was normalised
-  const T* gamma;
-  const float* mean;      // layer norm only
-  const float* rstd;
-  const uint8_t* row_mask;
-  const T* grad_y;
-  const T* grad_r;        // JOIN: gradient that reaches the sum past the norm, or null
-  long long n;
-  int h;
-  float inv_h;
-  T* grad_x;              // gradient of x; with JOIN of the branch (through dropout), or null: not wanted
-  T* grad_residual;       // JOIN: gradient of the residual stream
-  float* part;            // [parts][1 or 2][h] partial sums of dgamma (and dbeta)
-  Dropout drop;
-  int vec;
-};
-
-// Persistent: a block (or warp, TPR = 32) takes every parts-th row and keeps its share of dgamma / dbeta in
-// registers, one column's sum per thread and column; the shares are added up by reduce_parts_kernel in index order,
-// so results do not depend on the order in which blocks run.
-template <typename T, int TPR, int CPT, bool LAYER, bool JOIN>
-__global__ void __launch_bounds__(threads_of<TPR>())
-norm_bwd_kernel(const NormBwdArgs<T> a) {
-  __shared__ float2 sh[kWarp];
-  const int tid = threadIdx.x % TPR;
-  const long long part = static_cast<long long>(blockIdx.x) * rows_per_block<TPR>() + threadIdx.x / TPR;
-  const long long parts = static_cast<long long>(gridDim.x) * rows_per_block<TPR>();
-  const bool vec = a.vec != 0;
-  float dg[CPT][kVec], db[CPT][kVec];
-#pragma unroll
-  for (int i = 0; i < CPT; ++i)
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) dg[i][j] = db[i][j] = 0.f;
-  const bool drop = JOIN && a.drop.rng != nullptr;
-  PhiloxState ph;
-  if (drop) ph.load(a.drop.rng);
-
-  for (long long t = part; t < a.n; t += parts) {
-    T* gx_row = a.grad_x + t * a.h;
-    if (a.row_mask && a.row_mask[t] == 0) {
-      float z[kVec];
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) z[j] = 0.f;
-      for (int col = tid * kVec; col < a.h; col += TPR * kVec) {
-        if (!JOIN || a.grad_x) store_chunk(gx_row, col, a.h, vec, z);
-        if (JOIN) store_chunk(a.grad_residual + t * a.h, col, a.h, vec, z);
-      }
-      continue;
-    }
-    float x[CPT][kVec], gy[CPT][kVec];
-#pragma unroll
-    for (int i = 0; i < CPT; ++i) {
-      load_chunk(a.x + t * a.h, (tid + i * TPR) * kVec, a.h, vec, x[i]);
-      load_chunk(a.grad_y + t * a.h, (tid + i * TPR) * kVec, a.h, vec, gy[i]);
-    }
-    const float rstd = a.rstd[t];
-    const float mean = LAYER ? a.mean[t] : 0.f;
-    float s0 = 0.f, s1 = 0.f;
-#pragma unroll
-    for (int i = 0; i < CPT; ++i) {
-      const int col = (tid + i * TPR) * kVec;
-      float g[kVec];
-      load_param(a.gamma, col, a.h, vec, g);
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        x[i][j] = LAYER ? (x[i][j] - mean) * rstd : x[i][j] * rstd;   // xhat (columns past h meet gy = g = 0)
-        dg[i][j] = fmaf(gy[i][j], x[i][j], dg[i][j]);
-        if (LAYER) db[i][j] += gy[i][j];
-        gy[i][j] *= g[j];
-        if (LAYER) s0 += gy[i][j];
-        s1 = fmaf(gy[i][j], x[i][j], s1);
-      }
-    }
-    const float2 s = row_sum2<TPR>(s0, s1, sh);
-    const float m0 = LAYER ? s.x * a.inv_h : 0.f, m1 = s.y * a.inv_h;
-#pragma unroll
-    for (int i = 0; i < CPT; ++i) {
-      const int col = (tid + i * TPR) * kVec;
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) gy[i][j] = (gy[i][j] - m0 - x[i][j] * m1) * rstd;
-      if constexpr (JOIN) {
-        if (a.grad_r) {
-          float gr[kVec];
-          load_chunk(a.grad_r + t * a.h, col, a.h, vec, gr);
-#pragma unroll
-          for (int j = 0; j < kVec; ++j) gy[i][j] += gr[j];
-        }
-        store_chunk(a.grad_residual + t * a.h, col, a.h, vec, gy[i]);
-        if (!a.grad_x) continue;
-        if (drop) drop_chunk(gy[i], a.drop, ph, static_cast<uint32_t>(tid + i * TPR), static_cast<uint32_t>(t));
-      }
-      store_chunk(gx_row, col, a.h, vec, gy[i]);
-    }
-  }
-  float* out = a.part + part * (LAYER ? 2 : 1) * a.h;
-#pragma unroll
-  for (int i = 0; i < CPT; ++i) {
-    const int col = (tid + i * TPR) * kVec;
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      if (col + j < a.h) {
-        out[col + j] = dg[i][j];
-        if (LAYER) out[a.h + col + j] = db[i][j];
-      }
-    }
-  }
-}
-
-// grad[c] (+)= sum over parts, in a fixed order: 8 threads per column take every 8th part, then the eight sums.
-constexpr int kReduceCols = 32, kReduceLanes = 8;
-__global__ void __launch_bounds__(kReduceCols* kReduceLanes)
-reduce_parts_kernel(const float* __restrict__ part, int parts, long long row_pitch, int h, int accumulate,
-                    float* __restrict__ grad_gamma, float* __restrict__ grad_beta) {
-  const float* src = part + (blockIdx.y ? h : 0);
-  float* dst = blockIdx.y ? grad_beta : grad_gamma;
-  if (!dst) return;
-  const int c = blockIdx.x * kReduceCols + threadIdx.x;
-  float s = 0.f;
-  if (c < h)
-    for (int p = threadIdx.y; p < parts; p += kReduceLanes) s += src[p * row_pitch + c];
-  __shared__ float sh[kReduceLanes][kReduceCols];
-  sh[threadIdx.y][threadIdx.x] = s;
-  __syncthreads();
-  if (threadIdx.y == 0 && c < h) {
-    float t = 0.f;
-#pragma unroll
-    for (int i = 0; i < kReduceLanes; ++i) t += sh[i][threadIdx.x];
-    dst[c] = accumulate ? dst[c] + t : t;
-  }
-}
-
-// Rows longer than the register form holds: the row is read again for each use (from L2), one row per block, and the
-// weight gradients are summed by a second kernel whose threads own columns.
-constexpr int kLongThreads = 1024;
-template <typename T, bool LAYER, bool JOIN>
-__global__ void __launch_bounds__(kLongThreads)
-norm_fwd_long_kernel(const NormFwdArgs<T> a) {
-  __shared__ float sh[kWarp];
-  const long long t = blockIdx.x;
-  const bool vec = a.vec != 0;
-  const bool masked = a.row_mask && a.row_mask[t] == 0;
-  T* y = a.y + t * a.h;
-  T* r = JOIN ? a.r + t * a.h : nullptr;
-  const T* x = JOIN ? r : a.x + t * a.h;
-  const bool drop = JOIN && a.drop.rng != nullptr;
-  PhiloxState ph;
-  if (drop) ph.load(a.drop.rng);
-  float s = 0.f;
-  for (int col = threadIdx.x * kVec; col < a.h; col += kLongThreads * kVec) {
-    float v[kVec];
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) v[j] = 0.f;
-    if (masked) {
-      store_chunk(y, col, a.h, vec, v);
-      if (JOIN) store_chunk(r, col, a.h, vec, v);
-      continue;
-    }
-    load_chunk(a.x + t * a.h, col, a.h, vec, v);
-    if constexpr (JOIN) {
-      float res[kVec];
-      load_chunk(a.residual + t * a.h, col, a.h, vec, res);
-      if (drop) drop_chunk(v, a.drop, ph, static_cast<uint32_t>(col / kVec), static_cast<uint32_t>(t));
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) v[j] = as_stored<T>(v[j] + res[j]);
-      store_chunk(r, col, a.h, vec, v);
-    }
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) s += v[j];
-  }
-  if (masked) {
-    if (threadIdx.x == 0) {
-      if (a.mean) a.mean[t] = 0.f;
-      if (a.rstd) a.rstd[t] = 0.f;
-    }
-    return;
-  }
-  // each thread reads back only chunks that it wrote itself
-  const float mean = LAYER ? row_sum<kLongThreads>(s, sh) * a.inv_h : 0.f;
-  float q = 0.f;
-  for (int col = threadIdx.x * kVec; col < a.h; col += kLongThreads * kVec) {
-    float v[kVec];
-    load_chunk(x, col, a.h, vec, v);
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      const float d = (col + j < a.h) ? v[j] - mean : 0.f;
-      q = fmaf(d, d, q);
-    }
-  }
-  const float rstd = 1.0f / sqrtf(row_sum<kLongThreads>(q, sh) * a.inv_h + a.eps);
-  if (threadIdx.x == 0) {
-    if (a.mean) a.mean[t] = mean;
-    if (a.rstd) a.rstd[t] = rstd;
-  }
-  for (int col = threadIdx.x * kVec; col < a.h; col += kLongThreads * kVec) {
-    float v[kVec], g[kVec], b[kVec];
-    load_chunk(x, col, a.h, vec, v);
-    load_param(a.gamma, col, a.h, vec, g);
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) b[j] = 0.f;
-    if (a.beta) load_param(a.beta, col, a.h, vec, b);
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) v[j] = fmaf((v[j] - mean) * rstd, g[j], b[j]);
-    store_chunk(y, col, a.h, vec, v);
-  }
-}
-
-template <typename T, bool LAYER, bool JOIN>
-__global__ void __launch_bounds__(kLongThreads)
-norm_bwd_long_kernel(const NormBwdArgs<T> a) {
-  __shared__ float2 sh[kWarp];
-  const long long t = blockIdx.x;
-  const bool vec = a.vec != 0;
-  float z[kVec];
-#pragma unroll
-  for (int j = 0; j < kVec; ++j) z[j] = 0.f;
-  if (a.row_mask && a.row_mask[t] == 0) {
-    for (int col = threadIdx.x * kVec; col < a.h; col += kLongThreads * kVec) {
-      if (!JOIN || a.grad_x) store_chunk(a.grad_x + t * a.h, col, a.h, vec, z);
-      if (JOIN) store_chunk(a.grad_residual + t * a.h, col, a.h, vec, z);
-    }
-    return;
-  }
-  const float rstd = a.rstd[t];
-  const float mean = LAYER ? a.mean[t] : 0.f;
-  float s0 = 0.f, s1 = 0.f;
-  for (int col = threadIdx.x * kVec; col < a.h; col += kLongThreads * kVec) {
-    float x[kVec], gy[kVec], g[kVec];
-    load_chunk(a.x + t * a.h, col, a.h, vec, x);
-    load_chunk(a.grad_y + t * a.h, col, a.h, vec, gy);
-    load_param(a.gamma, col, a.h, vec, g);
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      const float gx = gy[j] * g[j];
-      s0 += gx;
-      s1 = fmaf(gx, (x[j] - mean) * rstd, s1);
-    }
-  }
-  const float2 s = row_sum2<kLongThreads>(s0, s1, sh);
-  const float m0 = LAYER ? s.x * a.inv_h : 0.f, m1 = s.y * a.inv_h;
-  const bool drop = JOIN && a.drop.rng != nullptr;
-  PhiloxState ph;
-  if (drop) ph.load(a.drop.rng);
-  for (int col = threadIdx.x * kVec; col < a.h; col += kLongThreads * kVec) {
-    float x[kVec], gy[kVec], g[kVec];
-    load_chunk(a.x + t * a.h, col, a.h, vec, x);
-    load_chunk(a.grad_y + t * a.h, col, a.h, vec, gy);
-    load_param(a.gamma, col, a.h, vec, g);
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) gy[j] = (gy[j] * g[j] - m0 - (x[j] - mean) * rstd * m1) * rstd;
-    if constexpr (JOIN) {
-      if (a.grad_r) {
-        load_chunk(a.grad_r + t * a.h, col, a.h, vec, g);
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) gy[j] += g[j];
-      }
-      store_chunk(a.grad_residual + t * a.h, col, a.h, vec, gy);
-      if (!a.grad_x) continue;
-      if (drop) drop_chunk(gy, a.drop, ph, static_cast<uint32_t>(col / kVec), static_cast<uint32_t>(t));
-    }
-    store_chunk(a.grad_x + t * a.h, col, a.h, vec, gy);
-  }
-}
-
-// Partial weight gradients of the long form: block (x: 256 columns, y: part), rows part, part + parts, ...
-template <typename T, bool LAYER>
-__global__ void __launch_bounds__(256)
-norm_weight_long_kernel(const NormBwdArgs<T> a, int parts) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= a.h) return;
-  float dg = 0.f, db = 0.f;
-  for (long long t = blockIdx.y; t < a.n; t += parts) {
-    if (a.row_mask && a.row_mask[t] == 0) continue;
-    const float gy = to_float(a.grad_y[t * a.h + c]);
-    const float x = to_float(a.x[t * a.h + c]);
-    dg = fmaf(gy, (LAYER ? x - a.mean[t] : x) * a.rstd[t], dg);
-    db += gy;
-  }
-  float* out = a.part + static_cast<long long>(blockIdx.y) * (LAYER ? 2 : 1) * a.h;
-  out[c] = dg;
-  if (LAYER) out[a.h + c] = db;
-}
-
-// y = d(x) (+ residual), and the gradient of d(x).  Grid-stride over the N x ceil(H/8) chunks; a thread steps from
-// chunk to chunk by a fixed (rows, chunks) stride, so there is one 64-bit division per thread and none in the loop.
-// Two chunks are in flight per thread.
+// ------------------------------------------------------------------------------------ dropout (+ residual)
+// 16-byte rows: the matrix is one run of chunks; a block takes kDropThreads * U consecutive ones, every thread U of them
+// kDropThreads apart, all loads before the arithmetic, and is done: the next block's loads fill the pause that a grid-stride
+// loop has between its iterations.
 constexpr int kDropThreads = 256;
-constexpr int kDropUnroll = 2;
-template <typename T>
+template <typename T> constexpr int drop_unroll() { return sizeof(T) == 2 ? 4 : 2; }
+
+template <typename T, bool RES>
 __global__ void __launch_bounds__(kDropThreads)
-dropout_kernel(const T* __restrict__ x, const T* __restrict__ residual, const uint8_t* __restrict__ row_mask,
-               long long n, int h, Dropout drop, T* __restrict__ y, int vec_) {
-  const bool vec = vec_ != 0;
-  const int groups = (h + kVec - 1) / kVec;
-  const long long stride = static_cast<long long>(gridDim.x) * kDropThreads;
-  const long long first = static_cast<long long>(blockIdx.x) * kDropThreads + threadIdx.x;
-  const long long step_rows = stride / groups;
-  const int step_groups = static_cast<int>(stride - step_rows * groups);
-  long long row = first / groups;
-  int group = static_cast<int>(first - row * groups);
+dropout_vec_kernel(const T* __restrict__ x, const T* __restrict__ residual, const uint8_t* __restrict__ row_mask,
+                   long long chunks, int groups, double inv_groups, uint32_t magic, int shift, const Dropout drop,
+                   T* __restrict__ y) {
+  constexpr int U = drop_unroll<T>();
+  const long long first = static_cast<long long>(blockIdx.x) * (kDropThreads * U);
+  // first = row0 * groups + group0: the quotient in double is within 1 of it (first < 2^53), then put right
+  long long row0 = static_cast<long long>(static_cast<double>(first) * inv_groups);
+  long long rem = first - row0 * groups;
+  if (rem < 0) { rem += groups; --row0; }
+  if (rem >= groups) { rem -= groups; ++row0; }
+  const uint32_t at = static_cast<uint32_t>(rem) + threadIdx.x;
+  Raw<T> v[U], r[U];
+  uint32_t group[U];
+  long long row[U];
+  bool in[U], on[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const long long c = first + i * kDropThreads + threadIdx.x;
+    const uint32_t from = at + static_cast<uint32_t>(i * kDropThreads);   // groups past the start of row0
+    const uint32_t over = (__umulhi(magic, from) + from) >> shift;        // from / groups for from < 2^31
+    group[i] = from - over * static_cast<uint32_t>(groups);
+    row[i] = row0 + over;
+    in[i] = c < chunks;
+    on[i] = in[i] && (!row_mask || row_mask[row[i]] != 0);
+    if (on[i]) {
+      v[i].load(x + c * kVec);
+      if (RES) r[i].load(residual + c * kVec); else r[i].clear();
+    } else {
+      v[i].clear();
+      r[i].clear();
+    }
+  }
   PhiloxState ph;
   const bool dropping = drop.rng != nullptr;
   if (dropping) ph.load(drop.rng);
-  while (row < n) {
-    float v[kDropUnroll][kVec], res[kDropUnroll][kVec];
-    long long r[kDropUnroll];
-    int g[kDropUnroll];
-    bool on[kDropUnroll];
 #pragma unroll
-    for (int i = 0; i < kDropUnroll; ++i) {
-      r[i] = row;
-      g[i] = group;
-      row += step_rows;
-      group += step_groups;
-      if (group >= groups) {
-        group -= groups;
-        ++row;
-      }
-      on[i] = r[i] < n && (!row_mask || row_mask[r[i]] != 0);
+  for (int i = 0; i < U; ++i) {
+    F2 a[kPairs], b[kPairs];
+    v[i].get(a);
+    r[i].get(b);
+    if (dropping) {
+      bool keep[kVec];
+      keep_bits(ph.draw(group[i], static_cast<uint32_t>(row[i])), drop.below, keep);
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) v[i][j] = res[i][j] = 0.f;
-      if (on[i]) {
-        load_chunk(x + r[i] * h, g[i] * kVec, h, vec, v[i]);
-        if (residual) load_chunk(residual + r[i] * h, g[i] * kVec, h, vec, res[i]);
+      for (int j = 0; j < kPairs; ++j) {
+        const float2 e = parts(a[j]);
+        const F2 kept = f2(keep[2 * j] ? e.x : 0.f, keep[2 * j + 1] ? e.y : 0.f);
+        a[j] = RES ? fma2(kept, f2(drop.scale), b[j]) : mul2(kept, f2(drop.scale));
       }
+    } else if (RES) {
+#pragma unroll
+      for (int j = 0; j < kPairs; ++j) a[j] = add2(a[j], b[j]);
     }
-#pragma unroll
-    for (int i = 0; i < kDropUnroll; ++i) {
-      if (r[i] >= n) continue;
-      if (dropping) drop_chunk(v[i], drop, ph, static_cast<uint32_t>(g[i]), static_cast<uint32_t>(r[i]));
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) v[i][j] += res[i][j];
-      store_chunk(y + r[i] * h, g[i] * kVec, h, vec, v[i]);
+    if (in[i]) {
+      v[i].set(a);
+      v[i].store(y + (first + i * kDropThreads + threadIdx.x) * kVec);
     }
   }
 }
 
-// ------------------------------------------------------------------------------------ host side
-// Rows of the partial weight gradients at most (bounds the workspace): the more columns, the fewer blocks fill an SM.
-int max_parts(int h) { return h <= 512 ? 2048 : h <= 2048 ? 1280 : 640; }
+// Rows that start at any element: `lanes` threads (a power of two up to a warp) take 8 x lanes consecutive columns of a
+// row, every lanes-th column each, so that element loads are contiguous; see RowThreads.
+template <typename T>
+__global__ void __launch_bounds__(kDropThreads)
+dropout_any_kernel(const T* __restrict__ x, const T* __restrict__ residual, const uint8_t* __restrict__ row_mask,
+                   long long n, int h, int lanes, int segments, const Dropout drop, T* __restrict__ y) {
+  const RowThreads<false> rt(lanes);
+  PhiloxState ph;
+  const bool dropping = drop.rng != nullptr;
+  if (dropping) ph.load(drop.rng);
+  const long long items = n * segments, stride = static_cast<long long>(gridDim.x) * rt.rows;
+  for (long long base = static_cast<long long>(blockIdx.x) * rt.rows; base < items; base += stride) {
+    const long long item = base + rt.slot;
+    const long long row = items < 0x7fffffffll ? static_cast<uint32_t>(item) / static_cast<uint32_t>(segments) : item / segments;
+    const int seg0 = static_cast<int>(item - row * segments) * lanes;   // first group of the segment
+    const bool in = item < items;
+    const bool on = in && (!row_mask || row_mask[row] != 0);
+    float v[kVec], r[kVec];
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+      const int c = seg0 * kVec + j * lanes + rt.tid;
+      v[j] = on && c < h ? to_float(x[row * h + c]) : 0.f;
+      r[j] = residual && on && c < h ? to_float(residual[row * h + c]) : 0.f;
+    }
+    if (dropping) {
+      bool keep[kVec];
+      keep_bits(ph.draw(static_cast<uint32_t>(seg0 + rt.tid), static_cast<uint32_t>(row)), drop.below, keep);
+      rt.template own_bits<false>(keep);
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) v[j] = drop_add(keep[j], v[j], drop.scale, r[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) v[j] += r[j];
+    }
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+      const int c = seg0 * kVec + j * lanes + rt.tid;
+      if (in && c < h) y[row * h + c] = from_float<T>(v[j]);
+    }
+  }
+}
 
+template <typename T>
+int launch_dropout(const T* x, const T* residual, const uint8_t* row_mask, long long n, int h, const Dropout& drop, T* y,
+                   bool vec, cudaStream_t stream) {
+  const int groups = (h + kVec - 1) / kVec;
+  if (vec) {
+    const long long chunks = n * groups;
+    constexpr long long kPerBlock = kDropThreads * drop_unroll<T>();
+    const long long blocks = (chunks + kPerBlock - 1) / kPerBlock;
+    if (blocks > 0x7fffffffll) return A3PO_ERR_UNSUPPORTED;   // 2^41 chunks and more: not in any GPU's memory
+    const double inv = 1.0 / groups;
+    // division by a constant as multiplication (Granlund and Montgomery 1994): with 2^shift >= groups,
+    // m = floor(2^32 (2^shift - groups) / groups) + 1, n / groups = (floor(m n / 2^32) + n) >> shift
+    int shift = 0;
+    while ((1u << shift) < static_cast<uint32_t>(groups)) ++shift;
+    const uint32_t magic = static_cast<uint32_t>(((((1ull << shift) - groups) << 32) / groups) + 1);
+    if (residual)
+      A3PO_LAUNCH(kKDropout, stream, (dropout_vec_kernel<T, true><<<static_cast<unsigned>(blocks), kDropThreads, 0, stream>>>(
+                                         x, residual, row_mask, chunks, groups, inv, magic, shift, drop, y)));
+    else
+      A3PO_LAUNCH(kKDropout, stream, (dropout_vec_kernel<T, false><<<static_cast<unsigned>(blocks), kDropThreads, 0, stream>>>(
+                                         x, residual, row_mask, chunks, groups, inv, magic, shift, drop, y)));
+    return after_launch();
+  }
+  int lanes = 1;
+  while (lanes < kWarp && lanes < groups) lanes *= 2;
+  const int segments = (groups + lanes - 1) / lanes;
+  const long long want = (n * segments + kDropThreads / lanes - 1) / (kDropThreads / lanes);
+  const long long most = static_cast<long long>(sm_count()) * 16;
+  A3PO_LAUNCH(kKDropout, stream, (dropout_any_kernel<T><<<static_cast<unsigned>(want < most ? want : most), kDropThreads, 0,
+                                                          stream>>>(x, residual, row_mask, n, h, lanes, segments, drop, y)));
+  return after_launch();
+}
+
+// ------------------------------------------------------------------------------------ host side
 bool rows_vectorise(int h, std::initializer_list<const void*> ptrs) {
   if (h % kVec != 0) return false;
   for (const void* p : ptrs)
@@ -643,10 +179,10 @@ bool rows_vectorise(int h, std::initializer_list<const void*> ptrs) {
 // Drop probability as a multiple of 2^-16 and its exact scale.
 Dropout make_dropout(float p, const void* rng) {
   Dropout d;
-  const double t = static_cast<double>(p) * 65536.0;
-  d.threshold = static_cast<uint32_t>(__builtin_rint(t));
-  d.scale = d.threshold < 65536u ? static_cast<float>(65536.0 / (65536.0 - d.threshold)) : 0.f;
-  d.rng = d.threshold == 0u ? nullptr : static_cast<const unsigned long long*>(rng);
+  const uint32_t t = static_cast<uint32_t>(__builtin_rint(static_cast<double>(p) * 65536.0));
+  d.below = t == 0u ? 0u : (t << 16) - 1u;   // T = 65536: 2^32 - 1, which nothing exceeds
+  d.scale = t < 65536u ? static_cast<float>(65536.0 / (65536.0 - t)) : 0.f;
+  d.rng = t == 0u ? nullptr : static_cast<const unsigned long long*>(rng);
   return d;
 }
 
@@ -671,70 +207,6 @@ int check_dropout(float p, const void* rng) {
   return A3PO_OK;
 }
 
-template <typename T, int TPR, int CPT, bool LAYER, bool JOIN>
-int launch_norm_fwd(const NormFwdArgs<T>& a, cudaStream_t stream) {
-  const long long blocks = (a.n + rows_per_block<TPR>() - 1) / rows_per_block<TPR>();
-  A3PO_LAUNCH(kKNorm, stream, (norm_fwd_kernel<T, TPR, CPT, LAYER, JOIN>
-                                   <<<static_cast<unsigned>(blocks), threads_of<TPR>(), 0, stream>>>(a)));
-  return after_launch();
-}
-
-// Threads per row by row length: as few as keep at most 4 chunks (32 columns) per thread.
-template <typename T, bool LAYER, bool JOIN>
-int norm_fwd_impl(const NormFwdArgs<T>& a, cudaStream_t stream) {
-  const int groups = (a.h + kVec - 1) / kVec;
-  if (groups <= 32) return launch_norm_fwd<T, 32, 1, LAYER, JOIN>(a, stream);
-  if (groups <= 128) return launch_norm_fwd<T, 32, 4, LAYER, JOIN>(a, stream);
-  if (groups <= 256) return launch_norm_fwd<T, 128, 2, LAYER, JOIN>(a, stream);
-  if (groups <= 512) return launch_norm_fwd<T, 256, 2, LAYER, JOIN>(a, stream);
-  if (groups <= 1024) return launch_norm_fwd<T, 512, 2, LAYER, JOIN>(a, stream);
-  if (groups <= 2048) return launch_norm_fwd<T, 1024, 2, LAYER, JOIN>(a, stream);
-  A3PO_LAUNCH(kKNorm, stream, (norm_fwd_long_kernel<T, LAYER, JOIN>
-                                   <<<static_cast<unsigned>(a.n), kLongThreads, 0, stream>>>(a)));
-  return after_launch();
-}
-
-template <typename T, int TPR, int CPT, bool LAYER, bool JOIN>
-int launch_norm_bwd(const NormBwdArgs<T>& a, int* parts, cudaStream_t stream) {
-  int sms = sm_count();
-  constexpr int kRows = rows_per_block<TPR>();
-  constexpr int kThreads = threads_of<TPR>();
-  long long blocks = (a.n + kRows - 1) / kRows;
-  long long most = static_cast<long long>(sms) * (1024 / kThreads > 0 ? 1024 / kThreads : 1);
-  if (most * kRows > max_parts(a.h)) most = max_parts(a.h) / kRows;
-  if (blocks > most) blocks = most;
-  *parts = static_cast<int>(blocks) * kRows;
-  A3PO_LAUNCH(kKNormBwd, stream, (norm_bwd_kernel<T, TPR, CPT, LAYER, JOIN>
-                                      <<<static_cast<unsigned>(blocks), kThreads, 0, stream>>>(a)));
-  return after_launch();
-}
-
-template <typename T, bool LAYER, bool JOIN>
-int norm_bwd_impl(const NormBwdArgs<T>& a, float* grad_gamma, float* grad_beta, int accumulate, cudaStream_t stream) {
-  const int groups = (a.h + kVec - 1) / kVec;
-  int parts = 0;
-  if (groups <= 32) A3PO_RETURN_IF((launch_norm_bwd<T, 32, 1, LAYER, JOIN>(a, &parts, stream)));
-  else if (groups <= 64) A3PO_RETURN_IF((launch_norm_bwd<T, 32, 2, LAYER, JOIN>(a, &parts, stream)));
-  else if (groups <= 256) A3PO_RETURN_IF((launch_norm_bwd<T, 128, 2, LAYER, JOIN>(a, &parts, stream)));
-  else if (groups <= 512) A3PO_RETURN_IF((launch_norm_bwd<T, 256, 2, LAYER, JOIN>(a, &parts, stream)));
-  else if (groups <= 1024) A3PO_RETURN_IF((launch_norm_bwd<T, 512, 2, LAYER, JOIN>(a, &parts, stream)));
-  else if (groups <= 2048) A3PO_RETURN_IF((launch_norm_bwd<T, 1024, 2, LAYER, JOIN>(a, &parts, stream)));
-  else {
-    A3PO_LAUNCH(kKNormBwd, stream, (norm_bwd_long_kernel<T, LAYER, JOIN>
-                                        <<<static_cast<unsigned>(a.n), kLongThreads, 0, stream>>>(a)));
-    A3PO_RETURN_IF(after_launch());
-    parts = a.n < 64 ? static_cast<int>(a.n) : 64;
-    const dim3 grid(static_cast<unsigned>((a.h + 255) / 256), static_cast<unsigned>(parts));
-    A3PO_LAUNCH(kKNormBwd, stream, (norm_weight_long_kernel<T, LAYER><<<grid, 256, 0, stream>>>(a, parts)));
-    A3PO_RETURN_IF(after_launch());
-  }
-  const dim3 grid(static_cast<unsigned>((a.h + kReduceCols - 1) / kReduceCols), LAYER ? 2u : 1u);
-  A3PO_LAUNCH(kKNormBwd, stream, (reduce_parts_kernel<<<grid, dim3(kReduceCols, kReduceLanes), 0, stream>>>(
-                                     a.part, parts, static_cast<long long>(LAYER ? 2 : 1) * a.h, a.h, accumulate,
-                                     grad_gamma, grad_beta)));
-  return after_launch();
-}
-
 template <typename T, bool JOIN>
 int norm_fwd_typed(const void* x, const void* residual, const void* gamma, const void* beta, const uint8_t* row_mask,
                    long long n, int h, a3po_norm_kind kind, float eps, const Dropout& drop, void* r, void* y,
@@ -743,7 +215,7 @@ int norm_fwd_typed(const void* x, const void* residual, const void* gamma, const
                    static_cast<const T*>(beta), row_mask, n, h, eps, 1.0f / static_cast<float>(h),
                    static_cast<T*>(r), static_cast<T*>(y), mean, rstd, drop,
                    rows_vectorise(h, {x, residual, gamma, beta, r, y}) ? 1 : 0};
-  return kind == A3PO_NORM_LAYER ? norm_fwd_impl<T, true, JOIN>(a, stream) : norm_fwd_impl<T, false, JOIN>(a, stream);
+  return launch_norm_fwd(a, kind == A3PO_NORM_LAYER, JOIN, stream);
 }
 
 template <typename T, bool JOIN>
@@ -755,8 +227,7 @@ int norm_bwd_typed(const void* x, const void* gamma, const float* mean, const fl
                    static_cast<const T*>(grad_y), static_cast<const T*>(grad_r), n, h, 1.0f / static_cast<float>(h),
                    static_cast<T*>(grad_x), static_cast<T*>(grad_residual), part, drop,
                    rows_vectorise(h, {x, gamma, grad_y, grad_r, grad_x, grad_residual}) ? 1 : 0};
-  return kind == A3PO_NORM_LAYER ? norm_bwd_impl<T, true, JOIN>(a, grad_gamma, grad_beta, accumulate, stream)
-                                 : norm_bwd_impl<T, false, JOIN>(a, grad_gamma, grad_beta, accumulate, stream);
+  return launch_norm_bwd(a, kind == A3PO_NORM_LAYER, JOIN, grad_gamma, grad_beta, accumulate, stream);
 }
 
 int norm_bwd_entry(bool join, const void* x, const void* gamma, const float* mean, const float* rstd,
@@ -831,21 +302,12 @@ int dropout_entry(const void* x, const void* residual, const uint8_t* row_mask, 
   if (sms <= 0) return A3PO_ERR_NO_DEVICE;
   if (n == 0) return A3PO_OK;
   const Dropout drop = make_dropout(p, rng);
-  const int vec = rows_vectorise(h, {x, residual, y}) ? 1 : 0;
-  const long long chunks = n * ((h + kVec - 1) / kVec);
-  long long blocks = (chunks + kDropThreads * kDropUnroll - 1) / (kDropThreads * kDropUnroll);
-  const long long most = static_cast<long long>(sms) * 8;
-  if (blocks > most) blocks = most;
+  const bool vec = rows_vectorise(h, {x, residual, y});
   if (dt == A3PO_F32)
-    A3PO_LAUNCH(kKDropout, stream, (dropout_kernel<float><<<static_cast<unsigned>(blocks), kDropThreads, 0, stream>>>(
-                                       static_cast<const float*>(x), static_cast<const float*>(residual), row_mask, n,
-                                       h, drop, static_cast<float*>(y), vec)));
-  else
-    A3PO_LAUNCH(kKDropout, stream,
-                (dropout_kernel<__nv_bfloat16><<<static_cast<unsigned>(blocks), kDropThreads, 0, stream>>>(
-                    static_cast<const __nv_bfloat16*>(x), static_cast<const __nv_bfloat16*>(residual), row_mask, n, h,
-                    drop, static_cast<__nv_bfloat16*>(y), vec)));
-  return after_launch();
+    return launch_dropout(static_cast<const float*>(x), static_cast<const float*>(residual), row_mask, n, h, drop,
+                          static_cast<float*>(y), vec, stream);
+  return launch_dropout(static_cast<const __nv_bfloat16*>(x), static_cast<const __nv_bfloat16*>(residual), row_mask, n, h,
+                        drop, static_cast<__nv_bfloat16*>(y), vec, stream);
 }
 
 }  // namespace
@@ -863,7 +325,7 @@ int a3po_norm_fwd(const void* x, const void* gamma, const void* beta, const uint
 
 size_t a3po_norm_bwd_workspace_bytes(int64_t N, int H) {
   if (N < 0 || H <= 0) return 0;
-  const size_t parts = static_cast<size_t>(N + 7 < max_parts(H) ? N + 7 : max_parts(H));   // a block of 8 rows at most past N
+  const size_t parts = static_cast<size_t>(N < max_parts(H) ? N : max_parts(H));
   return round_up(parts * 2 * static_cast<size_t>(H) * sizeof(float), 256) + 256;
 }
 

@@ -235,7 +235,8 @@ def test_gradient_by_differences():
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_unaligned_rows(dt):
-    """Buffers that start one element past a 16-byte boundary take the element-wise path and give the same values."""
+    """Buffers that start one element past a 16-byte boundary take the element-wise path: its threads own other columns,
+    so row sums add up in another order (the same bound against the definition holds); dropout is the same bit for bit."""
     n, h = 19, 264
     c = Case(n, h, dt, 77, masked=0.2)
     def shifted(t):
@@ -247,7 +248,8 @@ def test_unaligned_rows(dt):
     y2, rstd2, mean2 = shifted(torch.zeros_like(c.x)), torch.empty(n, device=DEV), torch.empty(n, device=DEV)
     a3po.a3po_norm_fwd(shifted(c.x), shifted(c.gamma), y2, rstd2, kind=a3po.A3PO_NORM_LAYER, beta=shifted(c.beta),
                        mean=mean2, row_mask=c.mask)
-    assert torch.equal(y, y2) and torch.equal(rstd, rstd2) and torch.equal(mean, mean2)
+    check_norm_fwd(c, c.x, y, mean, rstd, c.beta, True, float(np.float32(1e-6)))
+    check_norm_fwd(c, c.x, y2, mean2, rstd2, c.beta, True, float(np.float32(1e-6)))
     d1, d2 = torch.empty_like(c.x), shifted(torch.zeros_like(c.x))
     a3po.a3po_dropout_fwd(c.x, 0.25, rng_words(), d1, residual=c.res, row_mask=c.mask)
     a3po.a3po_dropout_fwd(shifted(c.x), 0.25, rng_words(), d2, residual=shifted(c.res), row_mask=c.mask)
