@@ -144,12 +144,19 @@ def _check(fn, code):
 
 
 def _ptr(t):
-    return None if t is None else c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
+
+
+# Handle of the current stream without building a torch.cuda.Stream object (3.4 us of a small call's time).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _stream(stream=None):
-    s = torch.cuda.current_stream() if stream is None else stream
-    return c_void_p(s.cuda_stream)
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
+    return torch.cuda.current_stream().cuda_stream
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -163,7 +170,8 @@ def _dtype_code(t: torch.Tensor) -> int:
 def _want(t, dtype, name, device_type="cuda"):
     if t is None:
         return
-    if t.dtype != dtype or not t.is_contiguous() or t.device.type != device_type:
+    if t.dtype is not dtype or not t.is_contiguous() or (not t.is_cuda if device_type == "cuda"
+                                                         else t.device.type != device_type):
         raise TypeError(f"{name}: expected contiguous {dtype} tensor on {device_type}, got {t.dtype} on {t.device}")
 
 
@@ -498,17 +506,32 @@ def a3po_train_step_host(h_hidden, h_targets, h_behav_logp, h_versions, h_adv, h
 
 
 # ------------------------------------------------------------------------------ rows in front of the LM head
-def _row_shapes(n, h, mats, vecs=(), per_row=(), row_mask=None):
-    """Shapes of the row operators: matrices [n, h], parameters [h], per-row scalars [n]."""
+def _rows(x, mats, vecs=(), per_row=(), row_mask=None):
+    """dtype code, N and H of the row operators' matrices [N, H], parameters [H] and per-row scalars [N], after checking
+    that they belong together and that the kernels will run where the tensors are."""
+    dt = _dtype_code(x)
+    n, h = x.shape
+    if not x.is_cuda or x.get_device() != torch.cuda.current_device():
+        raise TypeError(f"x: expected a tensor on the current CUDA device, got {x.device}")
+    _want(x, x.dtype, "x")
     for t in mats:
-        if t is not None and tuple(t.shape) != (n, h):
-            raise ValueError("shape mismatch")
+        if t is not None:
+            if t.shape != x.shape:
+                raise ValueError("shape mismatch")
+            _want(t, x.dtype, "matrix")
     for t in vecs:
         if t is not None and t.numel() != h:
             raise ValueError("shape mismatch")
-    for t in (*per_row, row_mask):
-        if t is not None and t.numel() != n:
+    for t in per_row:
+        if t is not None:
+            _want(t, torch.float32, "per-row scalar")
+            if t.numel() != n:
+                raise ValueError("shape mismatch")
+    if row_mask is not None:
+        _want(row_mask, torch.uint8, "row_mask")
+        if row_mask.numel() != n:
             raise ValueError("shape mismatch")
+    return dt, n, h
 
 
 def _rng_words(rng, p):
@@ -529,27 +552,18 @@ def a3po_norm_bwd_workspace_bytes(N, H) -> int:
 def a3po_norm_fwd(x, gamma, y, rstd=None, *, kind=A3PO_NORM_RMS, beta=None, mean=None, eps=1e-6, row_mask=None,
                   stream=None):
     """y = norm(x) gamma + beta; mean / rstd (fp32 [N]) are left for the backward when given."""
-    dt = _dtype_code(x)
-    for t, nm in ((x, "x"), (gamma, "gamma"), (beta, "beta"), (y, "y")):
-        _want(t, x.dtype, nm)
-    _want(rstd, torch.float32, "rstd"); _want(mean, torch.float32, "mean"); _want(row_mask, torch.uint8, "row_mask")
-    n, h = x.shape
-    _row_shapes(n, h, (y,), (gamma, beta), (mean, rstd), row_mask)
-    rc = load_library().a3po_norm_fwd(_ptr(x), _ptr(gamma), _ptr(beta), _ptr(row_mask), n, h, dt, kind, float(eps),
-                                      _ptr(y), _ptr(mean), _ptr(rstd), _stream(stream))
+    dt, n, h = _rows(x, (y,), (gamma, beta), (mean, rstd), row_mask)
+    _want(gamma, x.dtype, "gamma"); _want(beta, x.dtype, "beta")
+    rc = load_library().a3po_norm_fwd(_ptr(x), _ptr(gamma), _ptr(beta), _ptr(row_mask), n, h, dt, kind, eps, _ptr(y),
+                                      _ptr(mean), _ptr(rstd), _stream(stream))
     _check("a3po_norm_fwd", rc)
 
 
 def a3po_norm_bwd(x, gamma, rstd, grad_y, grad_x, grad_gamma, ws, *, kind=A3PO_NORM_RMS, mean=None, grad_beta=None,
                   accumulate_grad_w=False, row_mask=None, stream=None):
-    dt = _dtype_code(x)
-    for t, nm in ((x, "x"), (gamma, "gamma"), (grad_y, "grad_y"), (grad_x, "grad_x")):
-        _want(t, x.dtype, nm)
-    for t, nm in ((rstd, "rstd"), (mean, "mean"), (grad_gamma, "grad_gamma"), (grad_beta, "grad_beta")):
-        _want(t, torch.float32, nm)
-    _want(row_mask, torch.uint8, "row_mask"); _want(ws, torch.uint8, "ws")
-    n, h = x.shape
-    _row_shapes(n, h, (grad_y, grad_x), (gamma, grad_gamma, grad_beta), (mean, rstd), row_mask)
+    dt, n, h = _rows(x, (grad_y, grad_x), (gamma, grad_gamma, grad_beta), (mean, rstd), row_mask)
+    _want(gamma, x.dtype, "gamma"); _want(grad_gamma, torch.float32, "grad_gamma")
+    _want(grad_beta, torch.float32, "grad_beta"); _want(ws, torch.uint8, "ws")
     rc = load_library().a3po_norm_bwd(_ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(row_mask), _ptr(grad_y), n, h,
                                       dt, kind, _ptr(grad_x), _ptr(grad_gamma), _ptr(grad_beta),
                                       int(bool(accumulate_grad_w)), _ptr(ws), ws.numel(), _stream(stream))
@@ -558,23 +572,17 @@ def a3po_norm_bwd(x, gamma, rstd, grad_y, grad_x, grad_gamma, ws, *, kind=A3PO_N
 
 def a3po_dropout_fwd(x, p, rng, y, *, residual=None, row_mask=None, stream=None):
     """y = residual + dropout(x); the mask is a function of rng = {seed, offset} and the element's place."""
-    dt = _dtype_code(x)
-    _want(x, x.dtype, "x"); _want(residual, x.dtype, "residual"); _want(y, x.dtype, "y")
-    _want(row_mask, torch.uint8, "row_mask"); _rng_words(rng, p)
-    n, h = x.shape
-    _row_shapes(n, h, (residual, y), row_mask=row_mask)
-    rc = load_library().a3po_dropout_fwd(_ptr(x), _ptr(residual), _ptr(row_mask), n, h, dt, float(p), _ptr(rng),
-                                         _ptr(y), _stream(stream))
+    dt, n, h = _rows(x, (residual, y), row_mask=row_mask)
+    _rng_words(rng, p)
+    rc = load_library().a3po_dropout_fwd(_ptr(x), _ptr(residual), _ptr(row_mask), n, h, dt, p, _ptr(rng), _ptr(y),
+                                         _stream(stream))
     _check("a3po_dropout_fwd", rc)
 
 
 def a3po_dropout_bwd(grad_y, p, rng, grad_x, *, row_mask=None, stream=None):
-    dt = _dtype_code(grad_y)
-    _want(grad_y, grad_y.dtype, "grad_y"); _want(grad_x, grad_y.dtype, "grad_x")
-    _want(row_mask, torch.uint8, "row_mask"); _rng_words(rng, p)
-    n, h = grad_y.shape
-    _row_shapes(n, h, (grad_x,), row_mask=row_mask)
-    rc = load_library().a3po_dropout_bwd(_ptr(grad_y), _ptr(row_mask), n, h, dt, float(p), _ptr(rng), _ptr(grad_x),
+    dt, n, h = _rows(grad_y, (grad_x,), row_mask=row_mask)
+    _rng_words(rng, p)
+    rc = load_library().a3po_dropout_bwd(_ptr(grad_y), _ptr(row_mask), n, h, dt, p, _ptr(rng), _ptr(grad_x),
                                          _stream(stream))
     _check("a3po_dropout_bwd", rc)
 
@@ -582,15 +590,10 @@ def a3po_dropout_bwd(grad_y, p, rng, grad_x, *, row_mask=None, stream=None):
 def a3po_dropout_norm_fwd(x, residual, p, rng, gamma, r, y, rstd=None, *, kind=A3PO_NORM_RMS, beta=None, mean=None,
                           eps=1e-6, row_mask=None, stream=None):
     """r = residual + dropout(x), y = norm(r) gamma + beta, in one pass."""
-    dt = _dtype_code(x)
-    for t, nm in ((x, "x"), (residual, "residual"), (gamma, "gamma"), (beta, "beta"), (r, "r"), (y, "y")):
-        _want(t, x.dtype, nm)
-    _want(rstd, torch.float32, "rstd"); _want(mean, torch.float32, "mean"); _want(row_mask, torch.uint8, "row_mask")
-    _rng_words(rng, p)
-    n, h = x.shape
-    _row_shapes(n, h, (residual, r, y), (gamma, beta), (mean, rstd), row_mask)
-    rc = load_library().a3po_dropout_norm_fwd(_ptr(x), _ptr(residual), float(p), _ptr(rng), _ptr(gamma), _ptr(beta),
-                                              _ptr(row_mask), n, h, dt, kind, float(eps), _ptr(r), _ptr(y), _ptr(mean),
+    dt, n, h = _rows(x, (residual, r, y), (gamma, beta), (mean, rstd), row_mask)
+    _want(gamma, x.dtype, "gamma"); _want(beta, x.dtype, "beta"); _rng_words(rng, p)
+    rc = load_library().a3po_dropout_norm_fwd(_ptr(x), _ptr(residual), p, _ptr(rng), _ptr(gamma), _ptr(beta),
+                                              _ptr(row_mask), n, h, dt, kind, eps, _ptr(r), _ptr(y), _ptr(mean),
                                               _ptr(rstd), _stream(stream))
     _check("a3po_dropout_norm_fwd", rc)
 
@@ -598,16 +601,11 @@ def a3po_dropout_norm_fwd(x, residual, p, rng, gamma, r, y, rstd=None, *, kind=A
 def a3po_dropout_norm_bwd(r, p, rng, gamma, rstd, grad_y, grad_residual, grad_x, grad_gamma, ws, *,
                           kind=A3PO_NORM_RMS, mean=None, grad_r=None, grad_beta=None, accumulate_grad_w=False,
                           row_mask=None, stream=None):
-    dt = _dtype_code(r)
-    for t, nm in ((r, "r"), (gamma, "gamma"), (grad_y, "grad_y"), (grad_r, "grad_r"),
-                  (grad_residual, "grad_residual"), (grad_x, "grad_x")):
-        _want(t, r.dtype, nm)
-    for t, nm in ((rstd, "rstd"), (mean, "mean"), (grad_gamma, "grad_gamma"), (grad_beta, "grad_beta")):
-        _want(t, torch.float32, nm)
-    _want(row_mask, torch.uint8, "row_mask"); _want(ws, torch.uint8, "ws"); _rng_words(rng, p)
-    n, h = r.shape
-    _row_shapes(n, h, (grad_y, grad_r, grad_residual, grad_x), (gamma, grad_gamma, grad_beta), (mean, rstd), row_mask)
-    rc = load_library().a3po_dropout_norm_bwd(_ptr(r), float(p), _ptr(rng), _ptr(gamma), _ptr(mean), _ptr(rstd),
+    """Gradients of the join from its stored sum r; grad_x = None: the branch's gradient is not wanted."""
+    dt, n, h = _rows(r, (grad_y, grad_r, grad_residual, grad_x), (gamma, grad_gamma, grad_beta), (mean, rstd), row_mask)
+    _want(gamma, r.dtype, "gamma"); _want(grad_gamma, torch.float32, "grad_gamma")
+    _want(grad_beta, torch.float32, "grad_beta"); _want(ws, torch.uint8, "ws"); _rng_words(rng, p)
+    rc = load_library().a3po_dropout_norm_bwd(_ptr(r), p, _ptr(rng), _ptr(gamma), _ptr(mean), _ptr(rstd),
                                               _ptr(row_mask), _ptr(grad_y), _ptr(grad_r), n, h, dt, kind,
                                               _ptr(grad_residual), _ptr(grad_x), _ptr(grad_gamma), _ptr(grad_beta),
                                               int(bool(accumulate_grad_w)), _ptr(ws), ws.numel(), _stream(stream))
@@ -623,25 +621,21 @@ def a3po_gated_ffn_workspace_bytes(N, H, F, dt, has_row_mask, is_bwd) -> int:
     return load_library().a3po_gated_ffn_workspace_bytes(N, H, F, dt, int(bool(has_row_mask)), int(bool(is_bwd)))
 
 
-def _ffn_shapes(x, w_gate_up, w_down, mats, row_mask):
-    n, h = x.shape
+def _ffn_weights(x, w_gate_up, w_down, h):
+    _want(w_gate_up, x.dtype, "w_gate_up"); _want(w_down, x.dtype, "w_down")
     f = w_down.shape[1]
     if tuple(w_gate_up.shape) != (2 * f, h) or w_down.shape[0] != h:
         raise ValueError("shape mismatch")
-    _row_shapes(n, h, mats, row_mask=row_mask)
-    return n, h, f
+    return f
 
 
 def a3po_gated_ffn_fwd(x, w_gate_up, w_down, y, ws, *, row_mask=None, kept=None, activation=A3PO_ACT_SILU, status=None,
                        stream=None):
     """y = (act(x Wg^T) * (x Wu^T)) Wd^T; w_gate_up stacks Wg and Wu.  `kept` (uint8 buffer of
     a3po_gated_ffn_kept_bytes) is filled for a3po_gated_ffn_bwd when given."""
-    dt = _dtype_code(x)
-    for t, nm in ((x, "x"), (w_gate_up, "w_gate_up"), (w_down, "w_down"), (y, "y")):
-        _want(t, x.dtype, nm)
-    _want(row_mask, torch.uint8, "row_mask"); _want(kept, torch.uint8, "kept"); _want(ws, torch.uint8, "ws")
-    _want(status, torch.int32, "status")
-    n, h, f = _ffn_shapes(x, w_gate_up, w_down, (y,), row_mask)
+    dt, n, h = _rows(x, (y,), row_mask=row_mask)
+    f = _ffn_weights(x, w_gate_up, w_down, h)
+    _want(kept, torch.uint8, "kept"); _want(ws, torch.uint8, "ws"); _want(status, torch.int32, "status")
     rc = load_library().a3po_gated_ffn_fwd(_ptr(x), _ptr(w_gate_up), _ptr(w_down), _ptr(row_mask), n, h, f, dt, activation,
                                            _ptr(y), _ptr(kept), 0 if kept is None else kept.numel(), _ptr(ws), ws.numel(),
                                            _ptr(status), _stream(stream))
@@ -651,15 +645,11 @@ def a3po_gated_ffn_fwd(x, w_gate_up, w_down, y, ws, *, row_mask=None, kept=None,
 def a3po_gated_ffn_bwd(x, w_gate_up, w_down, kept, grad_y, grad_x, grad_w_gate_up, grad_w_down, ws, *, row_mask=None,
                        activation=A3PO_ACT_SILU, accumulate_grad_w=False, status=None, stream=None):
     """Gradients of a3po_gated_ffn_fwd from what it kept; the weight gradients are fp32 or of the weights' type."""
-    dt = _dtype_code(x)
-    for t, nm in ((x, "x"), (w_gate_up, "w_gate_up"), (w_down, "w_down"), (grad_y, "grad_y"), (grad_x, "grad_x")):
-        _want(t, x.dtype, nm)
+    dt, n, h = _rows(x, (grad_y, grad_x), row_mask=row_mask)
+    f = _ffn_weights(x, w_gate_up, w_down, h)
     gdt = _dtype_code(grad_w_down)
-    for t, nm in ((grad_w_gate_up, "grad_w_gate_up"), (grad_w_down, "grad_w_down")):
-        _want(t, grad_w_down.dtype, nm)
-    _want(row_mask, torch.uint8, "row_mask"); _want(kept, torch.uint8, "kept"); _want(ws, torch.uint8, "ws")
-    _want(status, torch.int32, "status")
-    n, h, f = _ffn_shapes(x, w_gate_up, w_down, (grad_y, grad_x), row_mask)
+    _want(grad_w_gate_up, grad_w_down.dtype, "grad_w_gate_up"); _want(grad_w_down, grad_w_down.dtype, "grad_w_down")
+    _want(kept, torch.uint8, "kept"); _want(ws, torch.uint8, "ws"); _want(status, torch.int32, "status")
     if grad_w_gate_up.shape != w_gate_up.shape or grad_w_down.shape != w_down.shape:
         raise ValueError("shape mismatch")
     rc = load_library().a3po_gated_ffn_bwd(_ptr(x), _ptr(w_gate_up), _ptr(w_down), _ptr(row_mask), _ptr(kept),
