@@ -12,15 +12,17 @@
 // memory in warp order, so results are bit-identical from run to run.
 
 #include "ffn_internal.cuh"
+#include "sm100_ptx.cuh"
 
 namespace a3po {
 namespace {
 
 constexpr int kFewWarps = 8;
 constexpr int kFewThreads = kFewWarps * kWarp;
-constexpr int kRingBytes = 48 * 1024;   // weights in flight per block; four blocks fit an SM
+// Operands in flight per block: four blocks fit an SM (three with two row tiles, which need 64 KB for two k-blocks).
+constexpr int ring_bytes(int mt) { return mt == 1 ? 48 * 1024 : 64 * 1024; }
 
-__device__ __forceinline__ void copy_weight(uint32_t smem, const __nv_bfloat16* p) {   // asynchronous, past L1
+__device__ __forceinline__ void copy_16(uint32_t smem, const __nv_bfloat16* p) {   // asynchronous, past L1
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(p) : "memory");
 }
 __device__ __forceinline__ uint4 read_shared(uint32_t smem) {
@@ -39,85 +41,92 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// A lane's share of the weight stream: 16 bytes per weight block and 32-wide k-block, kDepth k-blocks ahead of their use, in
-// a ring that it fills and reads alone (no barrier).  Started before x is touched, so that in the second kernel the
-// weights are on their way while the first one still computes x.
-template <int OUT>
-struct WeightStream {
-  static constexpr int kDepth = kRingBytes / (kFewThreads * 16 * OUT);
+// A lane's share of the operands of its warp's k-blocks: 16 bytes per weight block and per token row, kDepth k-blocks ahead
+// of their use, in a ring in shared memory that the lane fills and reads alone (no barrier).  A lane takes rows
+// lane / 4 (and + 8) of each 16-row tile of x and row lane / 4 of each weight block, 8 consecutive k each.
+// MT: tiles of 16 rows; HALF: only the first 8 rows of the (single) tile exist; OUT: weight blocks.
+template <int MT, bool HALF, int OUT>
+struct Stream {
+  static constexpr int kRows = HALF ? 1 : 2 * MT;
+  static constexpr int kDepth = ring_bytes(MT) / (kFewThreads * 16 * (OUT + kRows));
+  static_assert(kDepth >= 2, "at least one k-block ahead");
   uint32_t ring;
   const __nv_bfloat16* w[OUT];
-  int k, next;   // row length; this lane's k of the next copy
-  __device__ __forceinline__ void copy(int slot) {
-    if (next < k) {
+  const __nv_bfloat16* xr[kRows];
+  bool row_on[kRows];
+  int k, step;          // row length; distance between two k-blocks of a warp
+  int w_next, x_next;   // this lane's k of the next copies
+
+  __device__ __forceinline__ uint32_t at(int slot, int o) const { return ring + (slot * (OUT + kRows) + o) * kFewThreads * 16; }
+  __device__ __forceinline__ void copy_w(int slot) {
+    if (w_next < k) {
 #pragma unroll
-      for (int o = 0; o < OUT; ++o) copy_weight(ring + (slot * OUT + o) * kFewThreads * 16, w[o] + next);
+      for (int o = 0; o < OUT; ++o) copy_16(at(slot, o), w[o] + w_next);
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-    next += kFewWarps * 32;
+    w_next += step;
   }
-  __device__ __forceinline__ void start(uint8_t* smem, int k_, int first) {
+  __device__ __forceinline__ void copy_x(int slot) {
+    if (x_next < k) {
+#pragma unroll
+      for (int i = 0; i < kRows; ++i)
+        if (row_on[i]) copy_16(at(slot, OUT + i), xr[i] + x_next);
+    }
+    x_next += step;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  // The weights may start before x is there.
+  __device__ __forceinline__ void start_weights(uint8_t* smem, int k_, int first, int step_) {
     ring = static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + threadIdx.x * 16;
     k = k_;
-    next = first;
+    step = step_;
+    w_next = x_next = first;
 #pragma unroll
-    for (int s = 0; s < kDepth; ++s) copy(s);
+    for (int s = 0; s < kDepth; ++s) copy_w(s);
+  }
+  __device__ __forceinline__ void start_x(const __nv_bfloat16* x, int n, const uint8_t* row_mask, int lane) {
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      const int r = lane / 4 + 8 * i;
+      row_on[i] = r < n && (!row_mask || row_mask[r] != 0);
+      xr[i] = x + static_cast<long long>(row_on[i] ? r : 0) * k;
+    }
+#pragma unroll
+    for (int s = 0; s < kDepth; ++s) copy_x(s);   // the first group holds the weights of all slots too
+  }
+  // acc[m][o] += x[16 m .. +16, :] . w_o[8 rows, :] over this warp's k-blocks, `first` (of lane 0), first + step, ...
+  __device__ __forceinline__ void sweep(int first, int lane, float (&acc)[MT][OUT][4]) {
+    int slot = 0;
+    for (int kb = first; kb < k; kb += step) {   // the same for all lanes: the instruction is warp-wide
+      const bool in = kb + (lane & 3) * 8 < k;   // a lane past the end of k takes part with zeros
+      asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+      uint4 wv[OUT], xv[kRows];
+#pragma unroll
+      for (int o = 0; o < OUT; ++o) wv[o] = in ? read_shared(at(slot, o)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) xv[i] = in && row_on[i] ? read_shared(at(slot, OUT + i)) : make_uint4(0, 0, 0, 0);
+      copy_w(slot);
+      copy_x(slot);
+      slot = slot + 1 == kDepth ? 0 : slot + 1;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const uint4 a = xv[HALF ? 0 : 2 * m];
+        const uint4 b = HALF ? make_uint4(0, 0, 0, 0) : xv[HALF ? 0 : 2 * m + 1];
+#pragma unroll
+        for (int o = 0; o < OUT; ++o) {
+          mma_16816(acc[m][o], a.x, b.x, a.y, b.y, wv[o].x, wv[o].y);
+          mma_16816(acc[m][o], a.z, b.z, a.w, b.w, wv[o].z, wv[o].w);
+        }
+      }
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
   }
 };
 
-// Accumulates acc[m][o] += x[16 m .. +16, :] . w_o[8 rows, :] over this warp's share of k.  A lane reads rows lane / 4
-// (and + 8) of each tile of x, row lane / 4 of each weight block, 8 consecutive k each.
-// MT: tiles of 16 rows; HALF: only the first 8 rows of the (single) tile exist; OUT: weight blocks.
-template <int MT, bool HALF, int OUT>
-__device__ __forceinline__ void sweep(const __nv_bfloat16* __restrict__ x, const bool (&row_on)[2 * MT], int n, int k,
-                                      WeightStream<OUT>& ws, int warp, int lane, float (&acc)[MT][OUT][4]) {
-  constexpr int kRows = HALF ? 1 : 2 * MT;
-  const int sub = (lane & 3) * 8;
-  const __nv_bfloat16* xr[kRows];
-#pragma unroll
-  for (int i = 0; i < kRows; ++i) {
-    const int r = lane / 4 + 8 * i;
-    xr[i] = x + static_cast<long long>(r < n ? r : n - 1) * k;
-  }
-  const int step = kFewWarps * 32;
-  uint4 ahead[kRows];   // x of the next k-block
-  auto load_x = [&](int kk) {
-#pragma unroll
-    for (int i = 0; i < kRows; ++i)
-      ahead[i] = kk < k && row_on[i] ? *reinterpret_cast<const uint4*>(xr[i] + kk) : make_uint4(0, 0, 0, 0);
-  };
-  load_x(warp * 32 + sub);
-  int slot = 0;
-  for (int kb = warp * 32; kb < k; kb += step) {   // the same for all lanes: the instruction is warp-wide
-    const int kk = kb + sub;
-    uint4 xv[kRows], wv[OUT];
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) xv[i] = ahead[i];
-    load_x(kk + step);
-    asm volatile("cp.async.wait_group %0;" ::"n"(WeightStream<OUT>::kDepth - 1) : "memory");
-#pragma unroll
-    for (int o = 0; o < OUT; ++o)   // a lane past the end of k takes part with zeros
-      wv[o] = kk < k ? read_shared(ws.ring + (slot * OUT + o) * kFewThreads * 16) : make_uint4(0, 0, 0, 0);
-    ws.copy(slot);
-    slot = slot + 1 == WeightStream<OUT>::kDepth ? 0 : slot + 1;
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      const uint4 a = xv[HALF ? 0 : 2 * m];
-      const uint4 b = HALF ? make_uint4(0, 0, 0, 0) : xv[HALF ? 0 : 2 * m + 1];
-#pragma unroll
-      for (int o = 0; o < OUT; ++o) {
-        mma_16816(acc[m][o], a.x, b.x, a.y, b.y, wv[o].x, wv[o].y);
-        mma_16816(acc[m][o], a.z, b.z, a.w, b.w, wv[o].z, wv[o].w);
-      }
-    }
-  }
-  asm volatile("cp.async.wait_group 0;" ::: "memory");
-}
-
-// The block's sums: thread (row, column) of the 16 MT x 8 tile gets the total of its element over the warps, in order.
+// The block's sums over its warps, in warp order, in shared memory: sh[o][row][col], OUT x 16 MT x 8 floats.
 template <int MT, int OUT>
 __device__ __forceinline__ void add_warps(float (&acc)[MT][OUT][4], int warp, int lane, float* sh) {
-  static_assert(kFewWarps * OUT * 16 * MT * 8 * sizeof(float) <= kRingBytes, "the sums reuse the rings' memory");
+  constexpr int kTile = OUT * 16 * MT * 8;
+  static_assert(kFewWarps * kTile * sizeof(float) <= ring_bytes(MT), "the sums reuse the rings' memory");
   __syncthreads();   // every lane is done with its ring
 #pragma unroll
   for (int m = 0; m < MT; ++m)
@@ -126,76 +135,112 @@ __device__ __forceinline__ void add_warps(float (&acc)[MT][OUT][4], int warp, in
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int row = 16 * m + lane / 4 + 8 * (e / 2), col = (lane & 3) * 2 + (e & 1);
-        sh[((warp * OUT + o) * 16 * MT + row) * 8 + col] = acc[m][o][e];
+        sh[warp * kTile + (o * 16 * MT + row) * 8 + col] = acc[m][o][e];
       }
   __syncthreads();
-}
-template <int MT, int OUT>
-__device__ __forceinline__ float warp_total(const float* sh, int o, int row, int col) {
-  float t = 0.f;
+  for (int i = threadIdx.x; i < kTile; i += kFewThreads) {
+    float t = 0.f;
 #pragma unroll
-  for (int w = 0; w < kFewWarps; ++w) t += sh[((w * OUT + o) * 16 * MT + row) * 8 + col];
+    for (int w = 0; w < kFewWarps; ++w) t += sh[w * kTile + i];
+    sh[i] = t;   // read and written by this thread alone (w = 0's entry)
+  }
+  __syncthreads();
+}
+
+// One element of the sums over the S blocks of a cluster, in rank order.
+template <int S>
+__device__ __forceinline__ float cluster_total(const float* sh, int i) {
+  if constexpr (S == 1) return sh[i];
+  float t = 0.f;
+  const uint32_t here = static_cast<uint32_t>(__cvta_generic_to_shared(sh + i));
+#pragma unroll
+  for (int r = 0; r < S; ++r) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(ptx::map_to_cta(here, r)) : "memory");
+    t += v;
+  }
   return t;
 }
 
-template <int MT, bool HALF, bool GELU>
+// S = 2: a cluster of two blocks owns 16 output columns and each block sweeps half of k.  The rows of x are then read half
+// as often as by two blocks with 8 columns each; for more than a few rows that traffic out of L2, not HBM, is the limit.
+template <int MT, bool HALF, int S, bool GELU>
 __global__ void __launch_bounds__(kFewThreads)
 few_gate_up_kernel(const __nv_bfloat16* __restrict__ x, const __nv_bfloat16* __restrict__ w_gate_up,
                    const uint8_t* __restrict__ row_mask, int n, int h, int f, __nv_bfloat16* __restrict__ hid,
                    __nv_bfloat16* __restrict__ kept) {
   extern __shared__ __align__(16) uint8_t smem[];
-  float* sh = reinterpret_cast<float*>(smem);   // after the sweep
+  constexpr int OUT = 2 * S;   // gate blocks, then up blocks
   const int warp = threadIdx.x / kWarp, lane = threadIdx.x % kWarp;
-  const int f0 = blockIdx.x * 8;
-  bool on[2 * MT];
+  const int rank = S > 1 ? static_cast<int>(blockIdx.x % S) : 0;
+  const int f0 = static_cast<int>(blockIdx.x / S) * 8 * S;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  Stream<MT, HALF, OUT> st;
 #pragma unroll
-  for (int i = 0; i < 2 * MT; ++i) {
-    const int r = lane / 4 + 8 * i;
-    on[i] = r < n && (!row_mask || row_mask[r] != 0);
+  for (int o = 0; o < OUT; ++o) {
+    int unit = f0 + (o % S) * 8 + lane / 4;
+    if (unit >= f) unit = f - 1;   // f is a multiple of 8, not of 16: the last block's columns past f are not stored
+    st.w[o] = w_gate_up + (static_cast<long long>(o / S) * f + unit) * h;
   }
-  WeightStream<2> ws;
-  ws.w[0] = w_gate_up + static_cast<long long>(f0 + lane / 4) * h;
-  ws.w[1] = w_gate_up + (static_cast<long long>(f) + f0 + lane / 4) * h;
-  ws.start(smem, h, warp * 32 + (lane & 3) * 8);
-  float acc[MT][2][4] = {};
-  sweep<MT, HALF, 2>(x, on, n, h, ws, warp, lane, acc);
-  add_warps<MT, 2>(acc, warp, lane, sh);
+  const int first = (rank * kFewWarps + warp) * 32;
+  st.start_weights(smem, h, first + (lane & 3) * 8, S * kFewWarps * 32);
+  st.start_x(x, n, row_mask, lane);
+  float acc[MT][OUT][4] = {};
+  st.sweep(first, lane, acc);
+  float* sh = reinterpret_cast<float*>(smem);
+  add_warps<MT, OUT>(acc, warp, lane, sh);
+  if (S > 1) ptx::cluster_sync_all();
+  const int c0 = f0 + rank * 8;   // this block finishes its 8 of the cluster's columns
   for (int i = threadIdx.x; i < 16 * MT * 8; i += kFewThreads) {
     const int row = i / 8, col = i % 8;
-    if (row >= n) continue;
-    const float g = warp_total<MT, 2>(sh, 0, row, col), u = warp_total<MT, 2>(sh, 1, row, col);
+    if (row >= n || c0 >= f) continue;
+    const float g = cluster_total<S>(sh, (rank * 16 * MT + row) * 8 + col);
+    const float u = cluster_total<S>(sh, ((S + rank) * 16 * MT + row) * 8 + col);
     float a, slope;
     gate_activation<GELU>(g, a, slope);
-    hid[static_cast<long long>(row) * f + f0 + col] = __float2bfloat16_rn(a * u);
+    hid[static_cast<long long>(row) * f + c0 + col] = __float2bfloat16_rn(a * u);
     if (kept) {
-      __nv_bfloat16* k = kept + kept_offset(row, f0 + col, f);
+      __nv_bfloat16* k = kept + kept_offset(row, c0 + col, f);
       k[0] = __float2bfloat16_rn(g);
       k[kKeptElems] = __float2bfloat16_rn(u);
     }
   }
+  if (S > 1) ptx::cluster_sync_all();   // the peer may still read this block's sums
 }
 
-template <int MT, bool HALF>
+// Launched while the first kernel still runs (programmatic dependent launch): the weights start at once, x = h is
+// waited for.
+template <int MT, bool HALF, int S>
 __global__ void __launch_bounds__(kFewThreads)
 few_down_kernel(const __nv_bfloat16* hid, const __nv_bfloat16* __restrict__ w_down, int n, int h, int f,
                 __nv_bfloat16* __restrict__ y) {
   extern __shared__ __align__(16) uint8_t smem[];
-  float* sh = reinterpret_cast<float*>(smem);   // after the sweep
   const int warp = threadIdx.x / kWarp, lane = threadIdx.x % kWarp;
-  const int j0 = blockIdx.x * 8;
-  bool on[2 * MT];
+  const int rank = S > 1 ? static_cast<int>(blockIdx.x % S) : 0;
+  const int j0 = static_cast<int>(blockIdx.x / S) * 8 * S;
+  Stream<MT, HALF, S> st;
 #pragma unroll
-  for (int i = 0; i < 2 * MT; ++i) on[i] = lane / 4 + 8 * i < n;
-  WeightStream<1> ws;
-  ws.w[0] = w_down + static_cast<long long>(j0 + lane / 4) * f;
-  ws.start(smem, f, warp * 32 + (lane & 3) * 8);
-  float acc[MT][1][4] = {};
-  sweep<MT, HALF, 1>(hid, on, n, f, ws, warp, lane, acc);
-  add_warps<MT, 1>(acc, warp, lane, sh);
+  for (int o = 0; o < S; ++o) {
+    int unit = j0 + o * 8 + lane / 4;
+    if (unit >= h) unit = h - 1;
+    st.w[o] = w_down + static_cast<long long>(unit) * f;
+  }
+  const int first = (rank * kFewWarps + warp) * 32;
+  st.start_weights(smem, f, first + (lane & 3) * 8, S * kFewWarps * 32);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  st.start_x(hid, n, nullptr, lane);
+  float acc[MT][S][4] = {};
+  st.sweep(first, lane, acc);
+  float* sh = reinterpret_cast<float*>(smem);
+  add_warps<MT, S>(acc, warp, lane, sh);
+  if (S > 1) ptx::cluster_sync_all();
+  const int c0 = j0 + rank * 8;
   for (int i = threadIdx.x; i < 16 * MT * 8; i += kFewThreads) {
     const int row = i / 8, col = i % 8;
-    if (row < n) y[static_cast<long long>(row) * h + j0 + col] = __float2bfloat16_rn(warp_total<MT, 1>(sh, 0, row, col));
+    if (row < n && c0 < h)
+      y[static_cast<long long>(row) * h + c0 + col] = __float2bfloat16_rn(cluster_total<S>(sh, (rank * 16 * MT + row) * 8 + col));
   }
+  if (S > 1) ptx::cluster_sync_all();
 }
 
 __global__ void __launch_bounds__(256)
@@ -207,19 +252,57 @@ select_rows_kernel(const uint4* __restrict__ src, const uint8_t* __restrict__ ro
     dst[i] = row_mask[i / vec_per_row] ? src[i] : make_uint4(0, 0, 0, 0);
 }
 
+// Launch with a cluster of `cluster` blocks; `early`: may start before the kernel ahead of it in the stream is done.
+template <typename... Params, typename... Args>
+int launch_few(void (*kernel)(Params...), int columns, int cluster, int smem, bool early, cudaStream_t s, Args... args) {
+  if (smem > 48 * 1024 &&
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
+    cudaGetLastError();
+    return A3PO_ERR_CUDA;
+  }
+  const int units = (columns + 8 * cluster - 1) / (8 * cluster);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(units * cluster));
+  cfg.blockDim = dim3(kFewThreads);
+  cfg.dynamicSmemBytes = static_cast<size_t>(smem);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  cfg.attrs = attr;
+  if (cluster > 1) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+    attr[cfg.numAttrs].val.clusterDim.x = static_cast<unsigned>(cluster);
+    attr[cfg.numAttrs].val.clusterDim.y = 1;
+    attr[cfg.numAttrs].val.clusterDim.z = 1;
+    ++cfg.numAttrs;
+  }
+  if (early) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+    ++cfg.numAttrs;
+  }
+  A3PO_LAUNCH(kKFfnFew, s, (cudaLaunchKernelEx(&cfg, kernel, args...)));
+  return after_launch();
+}
+
+// Two blocks per 16 columns once the traffic of x out of L2 counts and a block's share of k stays long enough to cover the
+// cluster's two barriers.  gate/up, 8 rows: H = 4096 31 -> 26 us for the down projection (F = 12288) and 13 rows 42 -> 28 us,
+// but H = 1536 gate/up 12.7 -> 16.5 us (three k-blocks per warp left).
+bool pair_blocks(long long n, int k) { return n > 4 && k >= 2048; }
+
 template <int MT, bool HALF>
 int few_impl(const __nv_bfloat16* x, const __nv_bfloat16* wgu, const __nv_bfloat16* wd, const uint8_t* mask, int n, int h,
              int f, a3po_activation act, __nv_bfloat16* hid, __nv_bfloat16* y, __nv_bfloat16* kept, cudaStream_t s) {
-  const unsigned fb = static_cast<unsigned>(f / 8), hb = static_cast<unsigned>(h / 8);
-  if (act == A3PO_ACT_GELU_TANH)
-    A3PO_LAUNCH(kKFfnFew, s, (few_gate_up_kernel<MT, HALF, true><<<fb, kFewThreads, kRingBytes, s>>>(x, wgu, mask, n, h, f, hid,
-                                                                                            kept)));
+  constexpr int kSmem = ring_bytes(MT);
+  const bool gelu = act == A3PO_ACT_GELU_TANH;
+  const __nv_bfloat16* hid_in = hid;
+  if (pair_blocks(n, h))
+    A3PO_RETURN_IF(launch_few(gelu ? few_gate_up_kernel<MT, HALF, 2, true> : few_gate_up_kernel<MT, HALF, 2, false>, f, 2,
+                              kSmem, false, s, x, wgu, mask, n, h, f, hid, kept));
   else
-    A3PO_LAUNCH(kKFfnFew, s, (few_gate_up_kernel<MT, HALF, false><<<fb, kFewThreads, kRingBytes, s>>>(x, wgu, mask, n, h, f, hid,
-                                                                                             kept)));
-  A3PO_RETURN_IF(after_launch());
-  A3PO_LAUNCH(kKFfnFew, s, (few_down_kernel<MT, HALF><<<hb, kFewThreads, kRingBytes, s>>>(hid, wd, n, h, f, y)));
-  return after_launch();
+    A3PO_RETURN_IF(launch_few(gelu ? few_gate_up_kernel<MT, HALF, 1, true> : few_gate_up_kernel<MT, HALF, 1, false>, f, 1,
+                              kSmem, false, s, x, wgu, mask, n, h, f, hid, kept));
+  if (pair_blocks(n, f)) return launch_few(few_down_kernel<MT, HALF, 2>, h, 2, kSmem, true, s, hid_in, wd, n, h, f, y);
+  return launch_few(few_down_kernel<MT, HALF, 1>, h, 1, kSmem, true, s, hid_in, wd, n, h, f, y);
 }
 
 }  // namespace
