@@ -463,13 +463,13 @@ int a3po_dropout_norm_bwd(const void* r, float p, const uint64_t* rng, const voi
  *
  * row_mask uint8 [N] or NULL: rows with 0 are skipped (of more than 32 rows only the others are multiplied): nothing
  * of them is read, their y and grad_x are 0, they add nothing to a weight gradient.
- * kept: device buffer of a3po_gated_ffn_kept_bytes(N, F, dt) bytes, 256-byte aligned, that receives g and u for the
- * backward (layout private; about 4 N F bytes for bf16), or NULL when no backward follows.  The backward takes it with
+ * kept: device buffer of a3po_gated_ffn_kept_bytes(N, F, dt) bytes, 256-byte aligned, that receives g, u and h for the
+ * backward (layout private; about 6 N F bytes for bf16), or NULL when no backward follows.  The backward takes it with
  * the forward's x, weights, row_mask, N, H, F, dt and act; it is not changed, so the backward may be repeated.
  * grad_w_gate_up [2 F, H], grad_w_down [H, F]: dtype grad_w_dt (A3PO_F32, or dt), overwritten; with
  * accumulate_grad_w != 0 added to (A3PO_F32 only, else A3PO_ERR_UNSUPPORTED).
  * ws: a3po_gated_ffn_workspace_bytes(N, H, F, dt, row_mask given, backward) bytes, 256-byte aligned; for bf16 about
- * 2 N F bytes forward and 6 N F backward, plus 2 to 3 times 2 N H with a row_mask.
+ * 2 N F bytes forward and 4 N F backward, plus 2 to 3 times 2 N H with a row_mask.
  * status: optional device word (A3PO_STATUS_WAIT_TIMEOUT).  Outputs must not overlap inputs.  N = 0 launches nothing
  * except the zeros of weight gradients that are not accumulated.  Results are bit-identical from run to run.
  * ------------------------------------------------------------------------------------------ */

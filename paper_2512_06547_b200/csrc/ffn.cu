@@ -35,7 +35,6 @@ struct Layout {
   char* hid = nullptr;      // forward: h
   char* z = nullptr;        // backward: dg | du | h
   float* parts = nullptr;
-  int* select = nullptr;
 };
 
 bool lay_out(Arena& ar, long long n, int h, int f, a3po_dtype dt, bool masked, bool bwd, Layout* l) {
@@ -62,9 +61,8 @@ bool lay_out(Arena& ar, long long n, int h, int f, a3po_dtype dt, bool masked, b
     l->x_c = ar.take<char>(rows * h * 2);
     l->gy_c = ar.take<char>(rows * h * 2);
   }
-  l->select = ar.take<int>(1);
-  if (bwd) l->z = ar.take<char>(cap * 3 * f * 2);
-  else l->hid = ar.take<char>(cap * f * 2);
+  if (bwd) l->z = ar.take<char>(cap * 2 * f * 2);
+  else l->hid = ar.take<char>(cap * f * 2);   // used when nothing is kept
   const size_t parts = few && !bwd ? 0 : ffn_parts_bytes(static_cast<long long>(cap), h, bwd ? 2 * f : f);
   if (parts) l->parts = ar.take<float>(parts / sizeof(float));
   return ar.ok();
@@ -88,8 +86,7 @@ extern "C" {
 size_t a3po_gated_ffn_kept_bytes(int64_t N, int F, a3po_dtype dt) {
   if (N < 0 || F <= 0) return 0;
   if (dt == A3PO_F32) return round_up(static_cast<size_t>(N) * F * 8, 256) + 256;
-  return static_cast<size_t>(compact_capacity(N)) / kKeptRows * static_cast<size_t>(kept_col_tiles(F)) * 2 * kKeptElems * 2 +
-         256;
+  return kept_gate_bytes(N, F) + static_cast<size_t>(compact_capacity(N)) * F * 2 + 256;
 }
 
 size_t a3po_gated_ffn_workspace_bytes(int64_t N, int H, int F, a3po_dtype dt, int has_row_mask, int is_bwd) {
@@ -118,15 +115,16 @@ int a3po_gated_ffn_fwd(const void* x, const void* w_gate_up, const void* w_down,
   if (!tensor_cores(dt, H, F))
     return ffn_fwd_simt(x, w_gate_up, w_down, row_mask, N, H, F, dt, act, reinterpret_cast<float*>(l.hid), y, kept,
                         stream);
+  if (kept) l.hid = static_cast<char*>(kept) + kept_gate_bytes(N, F);
   if (N <= kFewRows) return ffn_few_rows_fwd(x, w_gate_up, w_down, row_mask, N, H, F, act, l.hid, y, kept, stream);
   if (!row_mask) {
     A3PO_RETURN_IF(ffn_gate_up_tc(x, w_gate_up, N, H, F, act, l.hid, kept, nullptr, status, stream));
-    return ffn_down_tc(l.hid, w_down, N, H, F, y, l.parts, nullptr, l.select, status, stream);
+    return ffn_down_tc(l.hid, w_down, N, H, F, y, l.parts, nullptr, status, stream);
   }
   A3PO_RETURN_IF(compact_index(nullptr, row_mask, nullptr, nullptr, N, l.cb, stream));
   A3PO_RETURN_IF(gather_rows_range(x, H, l.cb.idx, l.cb.count, 0, l.cb.cap, l.x_c, stream));
   A3PO_RETURN_IF(ffn_gate_up_tc(l.x_c, w_gate_up, l.cb.cap, H, F, act, l.hid, kept, l.cb.count, status, stream));
-  A3PO_RETURN_IF(ffn_down_tc(l.hid, w_down, l.cb.cap, H, F, l.out_c, l.parts, l.cb.count, l.select, status, stream));
+  A3PO_RETURN_IF(ffn_down_tc(l.hid, w_down, l.cb.cap, H, F, l.out_c, l.parts, l.cb.count, status, stream));
   return scatter_rows(l.out_c, H, l.cb.pos, N, y, stream);
 }
 
@@ -180,9 +178,9 @@ int a3po_gated_ffn_bwd(const void* x, const void* w_gate_up, const void* w_down,
     gys = l.gy_c;
   }
   A3PO_RETURN_IF(ffn_grad_gate_up_tc(gys, w_down, kept, rows, H, F, act, l.z, count, status, stream));
-  A3PO_RETURN_IF(ffn_grad_x_tc(l.z, w_gate_up, rows, H, F, gx, l.parts, count, l.select, status, stream));
+  A3PO_RETURN_IF(ffn_grad_x_tc(l.z, w_gate_up, rows, H, F, gx, l.parts, count, status, stream));
   if (compact) A3PO_RETURN_IF(scatter_rows(l.out_c, H, l.cb.pos, N, grad_x, stream));
-  return ffn_grad_w_tc(l.z, xs, gys, rows, H, F, grad_w_gate_up, grad_w_down, grad_w_dt, accumulate_grad_w, count, status,
+  return ffn_grad_w_tc(l.z, static_cast<const char*>(kept) + kept_gate_bytes(N, F), xs, gys, rows, H, F, grad_w_gate_up, grad_w_down, grad_w_dt, accumulate_grad_w, count, status,
                        stream);
 }
 

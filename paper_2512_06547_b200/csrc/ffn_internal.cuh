@@ -12,6 +12,8 @@ namespace a3po {
 // Kept values of the forward (bf16 shapes of the tensor-core path): g and u as the backward's epilogue reads them, one
 // accumulator row per thread.  Tile (128 rows, 32 columns) holds first g then u; inside, 16-byte piece j (8 columns) of
 // row r sits at (j * 128 + r) * 16 bytes, so that the 32 rows of a warp are one contiguous 512-byte access.
+// h itself follows them, row-major [n, f]: the forward writes it for its second product anyway, and the backward then need
+// not write it again.
 constexpr int kKeptRows = 128;
 constexpr int kKeptCols = 32;
 constexpr int kKeptElems = kKeptRows * kKeptCols;   // elements of one of the two halves of a tile
@@ -20,6 +22,11 @@ __host__ __device__ inline long long kept_col_tiles(int f) { return (static_cast
 __host__ __device__ inline long long kept_offset(long long row, int col, int f) {
   const long long tile = (row / kKeptRows) * kept_col_tiles(f) + col / kKeptCols;
   return tile * 2 * kKeptElems + ((col % kKeptCols) / 8 * kKeptRows + row % kKeptRows) * 8 + col % 8;
+}
+
+// Bytes of g and u, after which h starts.
+inline size_t kept_gate_bytes(long long n, int f) {
+  return static_cast<size_t>((n + kKeptRows - 1) / kKeptRows) * static_cast<size_t>(kept_col_tiles(f)) * 2 * kKeptElems * 2;
 }
 
 #ifdef __CUDACC__
@@ -54,14 +61,14 @@ int ffn_k_parts(long long n, int cols, int k);
 size_t ffn_parts_bytes(long long n, int cols, int k);
 // y[n, h] = hid Wd^T;  dx[n, h] = [dg | du] [Wg; Wu].  `parts`: scratch of ffn_parts_bytes, or null where that is 0.
 int ffn_down_tc(const void* hid, const void* w_down, long long n, int h, int f, void* y, float* parts,
-                const int* dyn_rows, int* select, uint32_t* status, cudaStream_t stream);
-// z[n][3][f] = dg | du | h from dy and the kept values.
+                const int* dyn_rows, uint32_t* status, cudaStream_t stream);
+// z[n][2][f] = dg | du from dy and the kept values.
 int ffn_grad_gate_up_tc(const void* grad_y, const void* w_down, const void* kept, long long n, int h, int f,
                         a3po_activation act, void* z, const int* dyn_rows, uint32_t* status, cudaStream_t stream);
 int ffn_grad_x_tc(const void* z, const void* w_gate_up, long long n, int h, int f, void* grad_x, float* parts,
-                  const int* dyn_rows, int* select, uint32_t* status, cudaStream_t stream);
+                  const int* dyn_rows, uint32_t* status, cudaStream_t stream);
 // grad_w[2 f, h] = [dg | du]^T x and grad_w_down[h, f] = dy^T h.
-int ffn_grad_w_tc(const void* z, const void* x, const void* grad_y, long long n, int h, int f, void* grad_w_gate_up,
+int ffn_grad_w_tc(const void* z, const void* hid, const void* x, const void* grad_y, long long n, int h, int f, void* grad_w_gate_up,
                   void* grad_w_down, a3po_dtype grad_dt, int accumulate, const int* dyn_rows, uint32_t* status,
                   cudaStream_t stream);
 

@@ -4,7 +4,7 @@
 //             same TMEM lane 128 columns apart, so the epilogue thread that owns the row has both and writes
 //             h = act(g) u; g and u themselves never leave the SM unless a backward will need them
 //   dgate/up  A = dy, B = Wd read N-major: dh stays in TMEM; the epilogue reads the kept g and u of its elements and
-//             writes dg, du and (again) h, the operands of the three gradient contractions
+//             writes dg and du, operands of two gradient contractions (h, the third's, is the forward's own)
 //   down, dx, dW   plain contractions
 //
 // Rounding: h, dg, du and the kept g and u are bf16, because they are operands of bf16 matrix instructions (and half
@@ -30,6 +30,7 @@ template <bool GELU, bool KEEP>
 struct GateUpEpilogue {
   static constexpr int kKernelId = kKFfnGate;
   static constexpr bool kGated = true;
+  static constexpr bool kPrefetch = false;
   struct Params {
     __nv_bfloat16* hid;    // [n, f]
     __nv_bfloat16* kept;   // see ffn_internal.cuh
@@ -41,7 +42,7 @@ struct GateUpEpilogue {
   __device__ __forceinline__ void begin(const Params&, long long) {}
   __device__ __forceinline__ void chunk_pair(const Params& p, int tile_row0, int col0, uint32_t (&rg)[kEpiChunk],
                                              uint32_t (&ru)[kEpiChunk], SlabStore& st) {
-    if (KEEP && col0 < p.b_rows) {
+    if (KEEP && col0 < p.b_rows && tile_row0 < p.n) {   // a pair's second tile may lie past the buffers
       uint4* k = reinterpret_cast<uint4*>(p.kept + kept_offset(tile_row0 + st.row_in_tile, col0, p.b_rows));
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -69,27 +70,28 @@ struct GateUpEpilogue {
     if (half == 0) cur = st.acquire();
 #pragma unroll
     for (int q = 0; q < 4; ++q) *st.piece(cur, half * 4 + q) = pack8(hv, q);
-    if (half == 1) st.submit(cur, col0 - 32, tile_row0, col0 - 32 < p.b_rows, false);
+    if (half == 1) st.submit(cur, col0 - 32, tile_row0, col0 - 32 < p.b_rows && tile_row0 < p.n, false);
   }
   __device__ __forceinline__ void end(const Params&, long long, int) {}
 };
 
-// dg | du | h of 32 columns at a time: three 128-row x 64-byte slabs in the staging area and one three-dimensional
-// output tensor [rows][3][f], so that each of the three is clipped at its own column f.
+// dg | du of 32 columns at a time: two 128-row x 64-byte halves of a slab and one three-dimensional output tensor
+// [rows][2][f], so that each of the two is clipped at its own column f.
 template <bool GELU>
 struct GradGateUpEpilogue : PlainEpilogue {
+  static constexpr bool kPrefetch = true;
   static constexpr int kKernelId = kKFfnGradGate;
   struct Params {
     const __nv_bfloat16* kept;
-    __nv_bfloat16* z;   // [n][3][f]
+    __nv_bfloat16* z;   // [n][2][f]
     long long n;        // rows of z
     int f;
   };
   static int make_c_map(const Params& p, CUtensorMap* map) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return A3PO_ERR_CUDA;
-    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(p.f), 3, static_cast<cuuint64_t>(p.n)};
-    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(p.f) * 2, static_cast<cuuint64_t>(p.f) * 6};
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(p.f), 2, static_cast<cuuint64_t>(p.n)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(p.f) * 2, static_cast<cuuint64_t>(p.f) * 4};
     const cuuint32_t box[3] = {kEpiChunk, 1, static_cast<cuuint32_t>(BM)};
     const cuuint32_t estr[3] = {1, 1, 1};
     const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, p.z, dims, strides, box, estr,
@@ -99,31 +101,42 @@ struct GradGateUpEpilogue : PlainEpilogue {
   }
   static constexpr uint32_t kPart = BM * kEpiChunk * 2;   // 8 KB
   long long row;
+  uint4 next_g[4], next_u[4];   // g and u of the columns that come next
+  __device__ __forceinline__ void read_kept(const uint4* k) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      next_g[q] = __ldcs(k + q * kKeptRows);
+      next_u[q] = __ldcs(k + q * kKeptRows + kKeptElems / 8);
+    }
+  }
   __device__ __forceinline__ void begin(const Params&, long long row_) { row = row_; }
+  // before the tile's product is waited for
+  __device__ __forceinline__ void prefetch(const Params& p, int tile_row0, int col0) {
+    if (col0 < p.f && tile_row0 < p.n) read_kept(reinterpret_cast<const uint4*>(p.kept + kept_offset(row, col0, p.f)));
+  }
   // 16-byte piece j (0..3) of this thread's row in a slab of 64-byte rows with the 64-byte swizzle
   static __device__ __forceinline__ uint4* piece(uint8_t* s, int r, int j) {
     return reinterpret_cast<uint4*>(s + r * 64 + ((j ^ ((r >> 1) & 3)) << 4));
   }
   __device__ __forceinline__ void chunk(const Params& p, int tile_row0, int col0, uint32_t (&r)[kEpiChunk],
                                         SlabStore& st) {
-    if (col0 >= p.f) return;   // the same for all threads
+    if (col0 >= p.f || tile_row0 >= p.n) return;   // the same for all threads
     const uint4* k = reinterpret_cast<const uint4*>(p.kept + kept_offset(row, col0, p.f));
     uint4 kg[4], ku[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      kg[q] = __ldcs(k + q * kKeptRows);
-      ku[q] = __ldcs(k + q * kKeptRows + kKeptElems / 8);
+      kg[q] = next_g[q];
+      ku[q] = next_u[q];
     }
-    if (st.issuer) bulk_wait_group_read<0>();   // the previous 32 columns have left the staging area
-    named_barrier_sync(SlabStore::kBarrierId, 128);
-    uint8_t* s = st.slab0;   // the two slabs of the staging area are contiguous
+    if (col0 + kEpiChunk < p.f) read_kept(k + 2 * kKeptElems / 8);   // the next 32 columns, while these are worked on
+    uint4 og[4], ou[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const uint32_t wg[4] = {kg[q].x, kg[q].y, kg[q].z, kg[q].w}, wu[4] = {ku[q].x, ku[q].y, ku[q].z, ku[q].w};
-      uint32_t og[4], ou[4], oh[4];
+      uint32_t vg[4], vu[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float dg[2], du[2], hh[2];
+        float dg[2], du[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const float g = __uint_as_float(e ? wg[i] & 0xffff0000u : wg[i] << 16);
@@ -133,23 +146,27 @@ struct GradGateUpEpilogue : PlainEpilogue {
           gate_activation<GELU>(g, a, slope);
           dg[e] = dh * u * slope;
           du[e] = dh * a;
-          hh[e] = a * u;
         }
-        og[i] = pack_bf16x2(dg[0], dg[1]);
-        ou[i] = pack_bf16x2(du[0], du[1]);
-        oh[i] = pack_bf16x2(hh[0], hh[1]);
+        vg[i] = pack_bf16x2(dg[0], dg[1]);
+        vu[i] = pack_bf16x2(du[0], du[1]);
       }
-      *piece(s, st.row_in_tile, q) = make_uint4(og[0], og[1], og[2], og[3]);
-      *piece(s + kPart, st.row_in_tile, q) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
-      *piece(s + 2 * kPart, st.row_in_tile, q) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
+      og[q] = make_uint4(vg[0], vg[1], vg[2], vg[3]);
+      ou[q] = make_uint4(vu[0], vu[1], vu[2], vu[3]);
+    }
+    uint8_t* s = st.acquire();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      *piece(s, st.row_in_tile, q) = og[q];
+      *piece(s + kPart, st.row_in_tile, q) = ou[q];
     }
     fence_proxy_async_smem();
     named_barrier_sync(SlabStore::kBarrierId, 128);
     if (st.issuer) {
-#pragma unroll
-      for (int w = 0; w < 3; ++w) tma_store_3d(st.map, s + w * kPart, col0, w, tile_row0);
+      tma_store_3d(st.map, s, col0, 0, tile_row0);
+      tma_store_3d(st.map, s + kPart, col0, 1, tile_row0);
       bulk_commit_group();
     }
+    ++st.issued;
   }
   __device__ __forceinline__ void end(const Params&, long long, int) {}
 };
@@ -189,10 +206,25 @@ DynRows rows_as_m(const int* dyn_rows, long long n) {
   return d;
 }
 
+// One contraction: pairs of CTAs on 256 x 256 tiles, or single CTAs when the output has at most 128 rows.
+template <class Epi, bool A_MN, bool B_MN>
+int contract(const Operand& a, const Operand& b, const typename Epi::Params& ep, const DynRows& dyn, uint32_t* status,
+             cudaStream_t stream) {
+  if (a.mn_extent <= BM) return launch_gemm<Epi, A_MN, B_MN, 1>(a, b, 0, ep, dyn, status, stream);
+  const int forced = tuning_override("A3PO_FFN_TILE", 0);   // 1: single CTAs, 128 x 256; 2: single CTAs, 256 x 256
+  if (forced == 1 || (forced == 2 && (Epi::kGated || Epi::kPrefetch)))
+    return launch_gemm<Epi, A_MN, B_MN, 1>(a, b, 0, ep, dyn, status, stream);
+  if constexpr (!Epi::kGated && !Epi::kPrefetch) {
+    if (forced == 2) return launch_gemm<Epi, A_MN, B_MN, 2>(a, b, 0, ep, dyn, status, stream);
+  }
+  const int group = !A_MN && !B_MN ? fwd_group_m(a.k_extent, 2 * BM) : kGroupM;
+  return launch_pair_gemm<Epi, A_MN, B_MN>(a, b, 0, ep, dyn, status, stream, group, true);
+}
+
 // Rows and columns of the output are the token rows and h: a contraction over a long K with, for few tokens, far fewer
 // output tiles than SMs.
 template <int ID, bool B_MN>
-int rows_gemm(const Operand& a, const Operand& b, __nv_bfloat16* out, float* parts, const int* dyn_rows, int* select,
+int rows_gemm(const Operand& a, const Operand& b, __nv_bfloat16* out, float* parts, const int* dyn_rows,
               uint32_t* status, cudaStream_t stream) {
   const long long n = a.mn_extent;
   const int cols = static_cast<int>(b.mn_extent);
@@ -209,8 +241,7 @@ int rows_gemm(const Operand& a, const Operand& b, __nv_bfloat16* out, float* par
     return after_launch();
   }
   typename StoreBf16EpilogueT<ID>::Params ep{out, cols, n, cols, nullptr};
-  return launch_grad_gemm<StoreBf16EpilogueT<ID>, false, B_MN>(a, b, ep, rows_as_m(dyn_rows, n), true, select, status,
-                                                               stream);
+  return contract<StoreBf16EpilogueT<ID>, false, B_MN>(a, b, ep, rows_as_m(dyn_rows, n), status, stream);
 }
 
 // Weight gradient C[m, c] = A^T B over the token rows (both operands read with the token index as K).
@@ -220,10 +251,7 @@ int weight_gemm(const Operand& a, const Operand& b, const typename Epi::Params& 
   DynRows d = rows_as_m(dyn_rows, a.k_extent);
   d.is_k = 1;
   d.zero_when_empty = accumulate ? 0 : 1;
-  const int n_tiles = static_cast<int>((b.mn_extent + BN - 1) / BN);
-  if (choose_mt(a.mn_extent, n_tiles, sm_count()) == 1)
-    return launch_gemm<Epi, true, true, 1>(a, b, 0, ep, d, status, stream);
-  return launch_gemm<Epi, true, true, 2>(a, b, 0, ep, d, status, stream);
+  return contract<Epi, true, true>(a, b, ep, d, status, stream);
 }
 
 }  // namespace
@@ -235,8 +263,7 @@ int ffn_gate_up_tc(const void* x, const void* w_gate_up, long long n, int h, int
   __nv_bfloat16* k = static_cast<__nv_bfloat16*>(kept);
   const DynRows d = rows_as_m(dyn_rows, n);
 #define A3PO_GATE_UP(G, K)                                                                              \
-  launch_gemm<GateUpEpilogue<G, K>, false, false>(a, b, 0, typename GateUpEpilogue<G, K>::Params{o, k, n, f}, d, status, \
-                                                  stream)
+  contract<GateUpEpilogue<G, K>, false, false>(a, b, typename GateUpEpilogue<G, K>::Params{o, k, n, f}, d, status, stream)
   if (act == A3PO_ACT_GELU_TANH) return kept ? A3PO_GATE_UP(true, true) : A3PO_GATE_UP(true, false);
   return kept ? A3PO_GATE_UP(false, true) : A3PO_GATE_UP(false, false);
 #undef A3PO_GATE_UP
@@ -258,9 +285,9 @@ size_t ffn_parts_bytes(long long n, int cols, int k) {
 }
 
 int ffn_down_tc(const void* hid, const void* w_down, long long n, int h, int f, void* y, float* parts,
-                const int* dyn_rows, int* select, uint32_t* status, cudaStream_t stream) {
+                const int* dyn_rows, uint32_t* status, cudaStream_t stream) {
   return rows_gemm<kKFfnDown, false>(Operand{hid, n, f, f}, Operand{w_down, h, f, f}, static_cast<__nv_bfloat16*>(y),
-                                     parts, dyn_rows, select, status, stream);
+                                     parts, dyn_rows, status, stream);
 }
 
 int ffn_grad_gate_up_tc(const void* grad_y, const void* w_down, const void* kept, long long n, int h, int f,
@@ -270,24 +297,23 @@ int ffn_grad_gate_up_tc(const void* grad_y, const void* w_down, const void* kept
   const __nv_bfloat16* k = static_cast<const __nv_bfloat16*>(kept);
   __nv_bfloat16* o = static_cast<__nv_bfloat16*>(z);
   if (act == A3PO_ACT_GELU_TANH)
-    return launch_gemm<GradGateUpEpilogue<true>, false, true>(a, b, 0, GradGateUpEpilogue<true>::Params{k, o, n, f}, d,
-                                                              status, stream);
-  return launch_gemm<GradGateUpEpilogue<false>, false, true>(a, b, 0, GradGateUpEpilogue<false>::Params{k, o, n, f}, d,
-                                                             status, stream);
+    return contract<GradGateUpEpilogue<true>, false, true>(a, b, GradGateUpEpilogue<true>::Params{k, o, n, f}, d, status,
+                                                           stream);
+  return contract<GradGateUpEpilogue<false>, false, true>(a, b, GradGateUpEpilogue<false>::Params{k, o, n, f}, d, status,
+                                                          stream);
 }
 
 int ffn_grad_x_tc(const void* z, const void* w_gate_up, long long n, int h, int f, void* grad_x, float* parts,
-                  const int* dyn_rows, int* select, uint32_t* status, cudaStream_t stream) {
-  return rows_gemm<kKFfnGradX, true>(Operand{z, n, 2ll * f, 3ll * f}, Operand{w_gate_up, h, 2ll * f, h},
-                                     static_cast<__nv_bfloat16*>(grad_x), parts, dyn_rows, select, status, stream);
+                  const int* dyn_rows, uint32_t* status, cudaStream_t stream) {
+  return rows_gemm<kKFfnGradX, true>(Operand{z, n, 2ll * f, 2ll * f}, Operand{w_gate_up, h, 2ll * f, h},
+                                     static_cast<__nv_bfloat16*>(grad_x), parts, dyn_rows, status, stream);
 }
 
-int ffn_grad_w_tc(const void* z_, const void* x, const void* grad_y, long long n, int h, int f, void* grad_w_gate_up,
+int ffn_grad_w_tc(const void* z, const void* hid_, const void* x, const void* grad_y, long long n, int h, int f, void* grad_w_gate_up,
                   void* grad_w_down, a3po_dtype grad_dt, int accumulate, const int* dyn_rows, uint32_t* status,
                   cudaStream_t stream) {
-  const __nv_bfloat16* z = static_cast<const __nv_bfloat16*>(z_);
-  const Operand dgu{z, 2ll * f, n, 3ll * f}, xo{x, h, n, h};           // [dg | du]^T x
-  const Operand dy{grad_y, h, n, h}, hid{z + 2ll * f, f, n, 3ll * f};  // dy^T h
+  const Operand dgu{z, 2ll * f, n, 2ll * f}, xo{x, h, n, h};   // [dg | du]^T x
+  const Operand dy{grad_y, h, n, h}, hid{hid_, f, n, f};       // dy^T h
   if (grad_dt == A3PO_F32) {
     using Epi = StoreF32EpilogueT<kKFfnGradW>;
     A3PO_RETURN_IF((weight_gemm<Epi>(dgu, xo, Epi::Params{static_cast<float*>(grad_w_gate_up), h, 2ll * f, h, accumulate},
