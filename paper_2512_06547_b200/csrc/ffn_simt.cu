@@ -9,42 +9,79 @@ namespace {
 
 constexpr int kBK = 32, kSimtThreads = 256;
 
-// Element (m, k) of an operand: base[m * ms + k * ks], zero outside [m_dim) x [k_dim) and where the token row that
-// the element belongs to is masked out (mask_on_m: the token is m, else k; mask null: none).
+// Operand: element (m, k) at base[m * ms + k * ks], one of ms, ks being 1; zero outside [m_dim) x [k_dim) and where the
+// token row that the element belongs to is masked out (mask null: none; the token is m where k is contiguous, else k).
 template <typename T>
 struct Mat {
   const T* base;
   long long ms, ks;
   long long m_dim, k_dim;
   const uint8_t* mask;
-  bool mask_on_m;
-  __device__ __forceinline__ float at(long long m, long long k) const {
-    if (m >= m_dim || k >= k_dim) return 0.f;
-    const float v = to_float(base[m * ms + k * ks]);
-    if (mask && mask[mask_on_m ? m : k] == 0) return 0.f;   // selected, whatever v is; both loads are in flight at once
-    return v;
-  }
+  bool k_contig;   // which of the two strides is the 1 (both are where a row has one element)
 };
 
 // One TILE x kBK slice of an operand: from memory into registers, read along its contiguous index, and from there into
-// shared memory, k-major.  The next slice is on its way while the present one is multiplied.
+// shared memory, k-major.  The next slice is on its way while the present one is multiplied.  A thread's element
+// addresses differ by fixed strides, so a load costs an add and a compare besides itself.
 template <typename T, int TILE>
 struct Slice {
   static constexpr int kPer = TILE * kBK / kSimtThreads;
   float r[kPer];
-  __device__ __forceinline__ void load(const Mat<T>& a, long long m0, long long k0) {
-    const bool k_contig = a.ks == 1;
+  const T* p;          // element 0 of this thread in the slice that is loaded next
+  const uint8_t* mask; // masks by token k, at that element's k
+  long long i_step;    // elements from one of the thread's elements to the next
+  long long k_left;    // k_dim minus element 0's k
+  uint32_t rows_on;    // k contiguous: bit i, row of element i exists and is not masked out; else: all or none
+  bool k_contig;
+
+  __device__ __forceinline__ void start(const Mat<T>& a, long long m0, long long k0) {
+    const int t = threadIdx.x % kSimtThreads;
+    k_contig = a.k_contig;
+    rows_on = 0;
+    mask = nullptr;
+    if (k_contig) {
+      const long long m = m0 + t / kBK, k = k0 + t % kBK;
+      p = a.base + m * a.ms + k;
+      i_step = (kSimtThreads / kBK) * a.ms;
+      k_left = a.k_dim - k;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int e = threadIdx.x + i * kSimtThreads;
-      r[i] = k_contig ? a.at(m0 + e / kBK, k0 + e % kBK) : a.at(m0 + e % TILE, k0 + e / TILE);
+      for (int i = 0; i < kPer; ++i) {
+        const long long row = m + i * (kSimtThreads / kBK);
+        if (row < a.m_dim && (!a.mask || a.mask[row] != 0)) rows_on |= 1u << i;
+      }
+    } else {
+      const long long m = m0 + t % TILE, k = k0 + t / TILE;
+      p = a.base + m + k * a.ks;
+      i_step = (kSimtThreads / TILE) * a.ks;
+      k_left = a.k_dim - k;
+      if (m < a.m_dim) rows_on = ~0u;
+      if (a.mask) mask = a.mask + k;
     }
   }
-  __device__ __forceinline__ void store(const Mat<T>& a, float (*sh)[TILE + 4]) const {
-    const bool k_contig = a.ks == 1;
+  // the slice at p, then on to the one `ahead` k further
+  __device__ __forceinline__ void load(const Mat<T>& a, int ahead) {
+    if (k_contig) {
+      const bool in = k_left > 0;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) r[i] = in && (rows_on >> i & 1u) ? to_float(p[i * i_step]) : 0.f;
+      p += ahead;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        constexpr int kStep = kSimtThreads / TILE;
+        const bool in = rows_on && i * kStep < k_left;
+        const bool on = in && (!mask || mask[i * kStep] != 0);
+        r[i] = on ? to_float(p[i * i_step]) : 0.f;
+      }
+      p += ahead * a.ks;
+      if (mask) mask += ahead;
+    }
+    k_left -= ahead;
+  }
+  __device__ __forceinline__ void store(float (*sh)[TILE + 4]) const {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int e = threadIdx.x + i * kSimtThreads;
+      const int e = threadIdx.x % kSimtThreads + i * kSimtThreads;
       if (k_contig) sh[e % kBK][e / kBK] = r[i]; else sh[e / TILE][e % TILE] = r[i];
     }
   }
@@ -53,7 +90,7 @@ struct Slice {
 // R x R outputs per thread, 16 x 16 threads.
 template <int R>
 __device__ __forceinline__ void multiply(const float (*as)[16 * R + 4], const float (*bs)[16 * R + 4], float (&acc)[R][R]) {
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+  const int tx = threadIdx.x % 16, ty = threadIdx.x % kSimtThreads / 16;
 #pragma unroll
   for (int k = 0; k < kBK; ++k) {
     float av[R], bv[R];
@@ -68,24 +105,50 @@ __device__ __forceinline__ void multiply(const float (*as)[16 * R + 4], const fl
   }
 }
 
-// acc += A's TILE rows from m0 on times B's TILE rows from n0 on, over all of K
-template <int R, typename TA, typename TB>
-__device__ __forceinline__ void tile_product(const Mat<TA>& a, const Mat<TB>& b, long long m0, long long n0,
-                                             float (*as)[16 * R + 4], float (*bs)[16 * R + 4], float (&acc)[R][R]) {
+// A block is G groups of 256 threads that take the slices of K in turn, so that a long K over few output tiles is not one
+// block's serial loop; their sums are added in group order.
+template <int R, int G>
+struct Tiles {
+  float a[G][kBK][16 * R + 4], b[G][kBK][16 * R + 4];
+};
+
+// acc += A's 16 R rows from m0 on times B's 16 R rows from n0 on, over all of K; the total is with group 0
+template <int R, int G, typename TA, typename TB>
+__device__ __forceinline__ void tile_product(const Mat<TA>& a, const Mat<TB>& b, long long m0, long long n0, Tiles<R, G>& sh,
+                                             float (&acc)[R][R]) {
+  const int group = threadIdx.x / kSimtThreads, t = threadIdx.x % kSimtThreads;
   Slice<TA, 16 * R> sa;
   Slice<TB, 16 * R> sb;
-  sa.load(a, m0, 0);
-  sb.load(b, n0, 0);
-  for (long long k0 = 0; k0 < a.k_dim; k0 += kBK) {
+  sa.start(a, m0, group * kBK);
+  sb.start(b, n0, group * kBK);
+  sa.load(a, G * kBK);
+  sb.load(b, G * kBK);
+  for (long long k0 = 0; k0 < a.k_dim; k0 += G * kBK) {   // the same trips for all groups; slices past K are zeros
     __syncthreads();   // the previous slices have been read
-    sa.store(a, as);
-    sb.store(b, bs);
+    sa.store(sh.a[group]);
+    sb.store(sh.b[group]);
     __syncthreads();
-    if (k0 + kBK < a.k_dim) {
-      sa.load(a, m0, k0 + kBK);
-      sb.load(b, n0, k0 + kBK);
+    if (k0 + G * kBK < a.k_dim) {
+      sa.load(a, G * kBK);
+      sb.load(b, G * kBK);
     }
-    multiply<R>(as, bs, acc);
+    multiply<R>(sh.a[group], sh.b[group], acc);
+  }
+  if constexpr (G > 1) {
+    float* sums = reinterpret_cast<float*>(&sh);
+    static_assert(sizeof(sh) >= (G - 1) * kSimtThreads * R * R * sizeof(float), "sums reuse the slices");
+    __syncthreads();
+    if (group > 0) {
+#pragma unroll
+      for (int i = 0; i < R * R; ++i) sums[((group - 1) * R * R + i) * kSimtThreads + t] = acc[i / R][i % R];
+    }
+    __syncthreads();
+    if (group == 0) {
+#pragma unroll
+      for (int g = 0; g < G - 1; ++g)
+#pragma unroll
+        for (int i = 0; i < R * R; ++i) acc[i / R][i % R] += sums[(g * R * R + i) * kSimtThreads + t];
+    }
   }
 }
 
@@ -114,19 +177,22 @@ simt_gate_up_kernel(Mat<T> x, Mat<T> wg, Mat<T> wu, long long n, int f, int gelu
   const int n0 = blockIdx.y * kTile;
   float ag[R][R] = {}, au[R][R] = {};
   Slice<T, kTile> sx, sg, su;
-  sx.load(x, m0, 0);
-  sg.load(wg, n0, 0);
-  su.load(wu, n0, 0);
+  sx.start(x, m0, 0);
+  sg.start(wg, n0, 0);
+  su.start(wu, n0, 0);
+  sx.load(x, kBK);
+  sg.load(wg, kBK);
+  su.load(wu, kBK);
   for (long long k0 = 0; k0 < x.k_dim; k0 += kBK) {
     __syncthreads();
-    sx.store(x, xs);
-    sg.store(wg, gs);
-    su.store(wu, us);
+    sx.store(xs);
+    sg.store(gs);
+    su.store(us);
     __syncthreads();
     if (k0 + kBK < x.k_dim) {
-      sx.load(x, m0, k0 + kBK);
-      sg.load(wg, n0, k0 + kBK);
-      su.load(wu, n0, k0 + kBK);
+      sx.load(x, kBK);
+      sg.load(wg, kBK);
+      su.load(wu, kBK);
     }
     multiply<R>(xs, gs, ag);
     multiply<R>(xs, us, au);
@@ -150,14 +216,16 @@ simt_gate_up_kernel(Mat<T> x, Mat<T> wg, Mat<T> wu, long long n, int f, int gelu
 }
 
 // C[m, c] (+)= sum_k A(m, k) B(c, k)
-template <typename TA, typename TB, typename TC, int R>
-__global__ void __launch_bounds__(kSimtThreads)
+template <typename TA, typename TB, typename TC, int R, int G>
+__global__ void __launch_bounds__(kSimtThreads* G)
 simt_gemm_kernel(Mat<TA> a, Mat<TB> b, TC* __restrict__ c, long long ldc, int accumulate) {
   constexpr int kTile = 16 * R;
-  __shared__ float as[kBK][kTile + 4], bs[kBK][kTile + 4];
+  extern __shared__ __align__(16) uint8_t smem[];
+  Tiles<R, G>& sh = *reinterpret_cast<Tiles<R, G>*>(smem);
   const long long m0 = static_cast<long long>(blockIdx.x) * kTile, n0 = static_cast<long long>(blockIdx.y) * kTile;
   float acc[R][R] = {};
-  tile_product<R>(a, b, m0, n0, as, bs, acc);
+  tile_product<R, G>(a, b, m0, n0, sh, acc);
+  if (threadIdx.x >= kSimtThreads) return;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const long long r = m0 + threadIdx.x / 16 * R + i;
@@ -172,16 +240,18 @@ simt_gemm_kernel(Mat<TA> a, Mat<TB> b, TC* __restrict__ c, long long ldc, int ac
 }
 
 // dh = dy Wd with the gradient of the gate in the epilogue: z[r][0..2][c] = dg, du, h
-template <typename T, int R>
-__global__ void __launch_bounds__(kSimtThreads)
+template <typename T, int R, int G>
+__global__ void __launch_bounds__(kSimtThreads* G)
 simt_grad_gate_up_kernel(Mat<T> dy, Mat<T> wd, const T* __restrict__ kept, long long n, int f, int gelu,
                          float* __restrict__ z) {
   constexpr int kTile = 16 * R;
-  __shared__ float as[kBK][kTile + 4], bs[kBK][kTile + 4];
+  extern __shared__ __align__(16) uint8_t smem[];
+  Tiles<R, G>& sh = *reinterpret_cast<Tiles<R, G>*>(smem);
   const long long m0 = static_cast<long long>(blockIdx.x) * kTile;
   const int n0 = blockIdx.y * kTile;
   float acc[R][R] = {};
-  tile_product<R>(dy, wd, m0, n0, as, bs, acc);
+  tile_product<R, G>(dy, wd, m0, n0, sh, acc);
+  if (threadIdx.x >= kSimtThreads) return;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const long long r = m0 + threadIdx.x / 16 * R + i;
@@ -203,37 +273,54 @@ simt_grad_gate_up_kernel(Mat<T> dy, Mat<T> wd, const T* __restrict__ kept, long 
 dim3 tiles(long long m, long long c, int tile) {
   return dim3(static_cast<unsigned>((m + tile - 1) / tile), static_cast<unsigned>((c + tile - 1) / tile));
 }
-// 32 x 32 tiles where 64 x 64 ones would leave most SMs without a block: the time is then that of one block's K loop,
-// which a quarter of the outputs per thread makes three times shorter.
-bool small_tiles(long long m, long long c) {
+// Tile and K groups by the number of 64 x 64 tiles: 32 x 32 tiles and four groups where even those are one block per SM at
+// most (the time is one block's serial loop); 64 x 64 and four groups up to one block per SM, two up to two, else one.
+// 2,048 x 256 outputs of K = 1,536: 139 us with the first, 71 with the third.
+enum class Shape { kSmall, kSplit4, kSplit2, kPlain };
+Shape shape_of(long long m, long long c) {
   const dim3 t = tiles(m, c, 64);
-  return static_cast<long long>(t.x) * t.y < sm_count();
+  const long long blocks = static_cast<long long>(t.x) * t.y, sms = sm_count();
+  return blocks * 4 <= sms ? Shape::kSmall : blocks <= sms ? Shape::kSplit4 : blocks <= 2 * sms ? Shape::kSplit2
+                                                                                               : Shape::kPlain;
+}
+// Launches a kernel whose shared memory is a Tiles<R, G> (64 x 64 tiles of four groups take 68 KB).
+template <int R, int G, typename K, typename... Args>
+int launch_tiles(K kernel, dim3 grid, cudaStream_t s, Args... args) {
+  constexpr int kBytes = sizeof(Tiles<R, G>);
+  if (kBytes > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) != cudaSuccess) {
+    cudaGetLastError();
+    return A3PO_ERR_CUDA;
+  }
+  A3PO_LAUNCH(kKFfnSimt, s, (kernel<<<grid, kSimtThreads * G, kBytes, s>>>(args...)));
+  return after_launch();
 }
 
 template <typename TA, typename TB, typename TC>
 int gemm(const Mat<TA>& a, const Mat<TB>& b, TC* c, long long ldc, int accumulate, cudaStream_t s) {
-  if (small_tiles(a.m_dim, b.m_dim))
-    A3PO_LAUNCH(kKFfnSimt, s, (simt_gemm_kernel<TA, TB, TC, 2><<<tiles(a.m_dim, b.m_dim, 32), kSimtThreads, 0, s>>>(
-                                  a, b, c, ldc, accumulate)));
-  else
-    A3PO_LAUNCH(kKFfnSimt, s, (simt_gemm_kernel<TA, TB, TC, 4><<<tiles(a.m_dim, b.m_dim, 64), kSimtThreads, 0, s>>>(
-                                  a, b, c, ldc, accumulate)));
-  return after_launch();
+#define A3PO_GEMM(R, G)                                                                                              \
+  launch_tiles<R, G>(simt_gemm_kernel<TA, TB, TC, R, G>, tiles(a.m_dim, b.m_dim, 16 * R), s, a, b, c, ldc, accumulate)
+  switch (shape_of(a.m_dim, b.m_dim)) {
+    case Shape::kSmall: return A3PO_GEMM(2, 4);
+    case Shape::kSplit4: return A3PO_GEMM(4, 4);
+    case Shape::kSplit2: return A3PO_GEMM(4, 2);
+    default: return A3PO_GEMM(4, 1);
+  }
+#undef A3PO_GEMM
 }
 
 template <typename T>
 int fwd_impl(const T* x, const T* wgu, const T* wd, const uint8_t* mask, long long n, int h, int f, int gelu, float* hid,
              T* y, T* kept, cudaStream_t s) {
-  const Mat<T> xm{x, h, 1, n, h, mask, true}, wg{wgu, h, 1, f, h, nullptr, false},
-      wu{wgu + static_cast<long long>(f) * h, h, 1, f, h, nullptr, false};
-  if (small_tiles(n, f))
+  const Mat<T> xm{x, h, 1, n, h, mask, true}, wg{wgu, h, 1, f, h, nullptr, true},
+      wu{wgu + static_cast<long long>(f) * h, h, 1, f, h, nullptr, true};
+  if (shape_of(n, f) != Shape::kPlain)
     A3PO_LAUNCH(kKFfnSimt, s, (simt_gate_up_kernel<T, 2><<<tiles(n, f, 32), kSimtThreads, 0, s>>>(xm, wg, wu, n, f, gelu,
                                                                                                   hid, kept)));
   else
     A3PO_LAUNCH(kKFfnSimt, s, (simt_gate_up_kernel<T, 4><<<tiles(n, f, 64), kSimtThreads, 0, s>>>(xm, wg, wu, n, f, gelu,
                                                                                                   hid, kept)));
   A3PO_RETURN_IF(after_launch());
-  return gemm(Mat<float>{hid, f, 1, n, f, nullptr, false}, Mat<T>{wd, f, 1, h, f, nullptr, false}, y, h, 0, s);
+  return gemm(Mat<float>{hid, f, 1, n, f, nullptr, true}, Mat<T>{wd, f, 1, h, f, nullptr, true}, y, h, 0, s);
 }
 
 template <typename T, typename TG>
@@ -241,14 +328,16 @@ int bwd_impl(const T* x, const T* wgu, const T* wd, const uint8_t* mask, const T
              int f, int gelu, float* z, T* gx, TG* gwgu, TG* gwd, int accumulate, cudaStream_t s) {
   const long long zf = 3ll * f;
   const Mat<T> dy{gy, h, 1, n, h, mask, true}, wdt{wd, 1, f, f, h, nullptr, false};
-  if (small_tiles(n, f))
-    A3PO_LAUNCH(kKFfnSimt, s, (simt_grad_gate_up_kernel<T, 2><<<tiles(n, f, 32), kSimtThreads, 0, s>>>(dy, wdt, kept, n, f,
-                                                                                                       gelu, z)));
-  else
-    A3PO_LAUNCH(kKFfnSimt, s, (simt_grad_gate_up_kernel<T, 4><<<tiles(n, f, 64), kSimtThreads, 0, s>>>(dy, wdt, kept, n, f,
-                                                                                                       gelu, z)));
-  A3PO_RETURN_IF(after_launch());
-  A3PO_RETURN_IF(gemm(Mat<float>{z, zf, 1, n, 2ll * f, nullptr, false}, Mat<T>{wgu, 1, h, h, 2ll * f, nullptr, false}, gx,
+#define A3PO_GRAD_GATE(R, G) \
+  launch_tiles<R, G>(simt_grad_gate_up_kernel<T, R, G>, tiles(n, f, 16 * R), s, dy, wdt, kept, n, f, gelu, z)
+  switch (shape_of(n, f)) {
+    case Shape::kSmall: A3PO_RETURN_IF(A3PO_GRAD_GATE(2, 4)); break;
+    case Shape::kSplit4: A3PO_RETURN_IF(A3PO_GRAD_GATE(4, 4)); break;
+    case Shape::kSplit2: A3PO_RETURN_IF(A3PO_GRAD_GATE(4, 2)); break;
+    default: A3PO_RETURN_IF(A3PO_GRAD_GATE(4, 1));
+  }
+#undef A3PO_GRAD_GATE
+  A3PO_RETURN_IF(gemm(Mat<float>{z, zf, 1, n, 2ll * f, nullptr, true}, Mat<T>{wgu, 1, h, h, 2ll * f, nullptr, false}, gx,
                       h, 0, s));
   A3PO_RETURN_IF(gemm(Mat<float>{z, 1, zf, 2ll * f, n, nullptr, false}, Mat<T>{x, 1, h, h, n, mask, false}, gwgu, h,
                       accumulate, s));
