@@ -61,6 +61,39 @@ inline int after_launch() {
   return A3PO_OK;
 }
 
+#ifdef __CUDACC__
+// Programmatic dependent launch.  A kernel started with launch_early may begin (its set-up, barriers, tensor memory, loads of
+// constant weights) while the kernel ahead of it in the stream still runs; wait_for_previous() returns once that one has
+// finished and its writes are visible, and comes before any access to memory that anything else writes.  Kernels that
+// call allow_next() let such a successor begin once all their blocks are running.  Both are no-ops otherwise.
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+template <typename... Params, typename... Args>
+void launch_early(void (*kernel)(Params...), unsigned grid, unsigned block, size_t smem, cudaStream_t stream, int cluster,
+                  bool early, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  cfg.attrs = attr;
+  if (cluster > 1) {   // kernels without a compile-time cluster size
+    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+    attr[cfg.numAttrs].val.clusterDim.x = static_cast<unsigned>(cluster);
+    attr[cfg.numAttrs].val.clusterDim.y = 1;
+    attr[cfg.numAttrs].val.clusterDim.z = 1;
+    ++cfg.numAttrs;
+  }
+  if (early) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+    ++cfg.numAttrs;
+  }
+  cudaLaunchKernelEx(&cfg, kernel, args...);   // an error is picked up by after_launch()
+}
+#endif
+
 #define A3PO_RETURN_IF(expr)            \
   do {                                  \
     int _rc = (expr);                   \

@@ -174,7 +174,7 @@ few_gate_up_kernel(const __nv_bfloat16* __restrict__ x, const __nv_bfloat16* __r
   const int warp = threadIdx.x / kWarp, lane = threadIdx.x % kWarp;
   const int rank = S > 1 ? static_cast<int>(blockIdx.x % S) : 0;
   const int f0 = static_cast<int>(blockIdx.x / S) * 8 * S;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  allow_next();
   Stream<MT, HALF, OUT> st;
 #pragma unroll
   for (int o = 0; o < OUT; ++o) {
@@ -227,7 +227,8 @@ few_down_kernel(const __nv_bfloat16* hid, const __nv_bfloat16* __restrict__ w_do
   }
   const int first = (rank * kFewWarps + warp) * 32;
   st.start_weights(smem, f, first + (lane & 3) * 8, S * kFewWarps * 32);
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  wait_for_previous();
+  allow_next();
   st.start_x(hid, n, nullptr, lane);
   float acc[MT][S][4] = {};
   st.sweep(first, lane, acc);
@@ -261,26 +262,8 @@ int launch_few(void (*kernel)(Params...), int columns, int cluster, int smem, bo
     return A3PO_ERR_CUDA;
   }
   const int units = (columns + 8 * cluster - 1) / (8 * cluster);
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(units * cluster));
-  cfg.blockDim = dim3(kFewThreads);
-  cfg.dynamicSmemBytes = static_cast<size_t>(smem);
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  cfg.attrs = attr;
-  if (cluster > 1) {
-    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
-    attr[cfg.numAttrs].val.clusterDim.x = static_cast<unsigned>(cluster);
-    attr[cfg.numAttrs].val.clusterDim.y = 1;
-    attr[cfg.numAttrs].val.clusterDim.z = 1;
-    ++cfg.numAttrs;
-  }
-  if (early) {
-    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
-    ++cfg.numAttrs;
-  }
-  A3PO_LAUNCH(kKFfnFew, s, (cudaLaunchKernelEx(&cfg, kernel, args...)));
+  A3PO_LAUNCH(kKFfnFew, s, (launch_early(kernel, static_cast<unsigned>(units * cluster), kFewThreads,
+                                         static_cast<size_t>(smem), s, cluster, early, args...)));
   return after_launch();
 }
 

@@ -173,8 +173,10 @@ struct GradGateUpEpilogue : PlainEpilogue {
 
 // out[r, c] = sum over parts, in index order.  8 columns per thread.
 __global__ void __launch_bounds__(256)
-add_parts_kernel(const float* __restrict__ parts, int n_parts, long long part_stride, long long n, int cols,
-                 const int* __restrict__ dyn_rows, __nv_bfloat16* __restrict__ out) {
+add_parts_kernel(const float* parts, int n_parts, long long part_stride, long long n, int cols,
+                 const int* dyn_rows, __nv_bfloat16* out) {
+  wait_for_previous();
+  allow_next();
   const long long rows = dyn_rows ? (*dyn_rows < n ? *dyn_rows : n) : n;
   const int groups = cols / 8;
   const long long total = rows * groups;
@@ -206,19 +208,20 @@ DynRows rows_as_m(const int* dyn_rows, long long n) {
   return d;
 }
 
-// One contraction: pairs of CTAs on 256 x 256 tiles, or single CTAs when the output has at most 128 rows.
+// One contraction: pairs of CTAs on 256 x 256 tiles, or single CTAs when the output has at most 128 rows.  early: not
+// the first launch of a call, so that it may begin while its predecessor (one of this call's own) still runs.
 template <class Epi, bool A_MN, bool B_MN>
 int contract(const Operand& a, const Operand& b, const typename Epi::Params& ep, const DynRows& dyn, uint32_t* status,
-             cudaStream_t stream) {
-  if (a.mn_extent <= BM) return launch_gemm<Epi, A_MN, B_MN, 1>(a, b, 0, ep, dyn, status, stream);
+             cudaStream_t stream, bool early = true) {
+  if (a.mn_extent <= BM) return launch_gemm<Epi, A_MN, B_MN, 1>(a, b, 0, ep, dyn, status, stream, 1, early);
   const int forced = tuning_override("A3PO_FFN_TILE", 0);   // 1: single CTAs, 128 x 256; 2: single CTAs, 256 x 256
   if (forced == 1 || (forced == 2 && (Epi::kGated || Epi::kPrefetch)))
-    return launch_gemm<Epi, A_MN, B_MN, 1>(a, b, 0, ep, dyn, status, stream);
+    return launch_gemm<Epi, A_MN, B_MN, 1>(a, b, 0, ep, dyn, status, stream, 1, true);
   if constexpr (!Epi::kGated && !Epi::kPrefetch) {
     if (forced == 2) return launch_gemm<Epi, A_MN, B_MN, 2>(a, b, 0, ep, dyn, status, stream);
   }
   const int group = !A_MN && !B_MN ? fwd_group_m(a.k_extent, 2 * BM) : kGroupM;
-  return launch_pair_gemm<Epi, A_MN, B_MN>(a, b, 0, ep, dyn, status, stream, group, true);
+  return launch_pair_gemm<Epi, A_MN, B_MN>(a, b, 0, ep, dyn, status, stream, group, true, early);
 }
 
 // Rows and columns of the output are the token rows and h: a contraction over a long K with, for few tokens, far fewer
@@ -233,11 +236,12 @@ int rows_gemm(const Operand& a, const Operand& b, __nv_bfloat16* out, float* par
     const long long rows_pad = (n + BM - 1) / BM * BM;
     typename StoreF32EpilogueT<ID>::Params ep{parts, cols, rows_pad * k_parts, cols, 0};
     A3PO_RETURN_IF((launch_gemm<StoreF32EpilogueT<ID>, false, B_MN, 1>(a, b, 0, ep, rows_as_m(dyn_rows, n), status,
-                                                                      stream, k_parts)));
+                                                                      stream, k_parts, true)));
     const long long want = (n * (cols / 8) + 255) / 256;
     const int blocks = static_cast<int>(want < sm_count() * 8ll ? want : sm_count() * 8ll);
-    A3PO_LAUNCH(ID, stream, (add_parts_kernel<<<blocks, 256, 0, stream>>>(parts, k_parts, rows_pad * cols, n, cols,
-                                                                          dyn_rows, out)));
+    A3PO_LAUNCH(ID, stream, (launch_early(add_parts_kernel, blocks, 256, 0, stream, 1, true,
+                                          static_cast<const float*>(parts), k_parts, rows_pad * cols, n, cols, dyn_rows,
+                                          out)));
     return after_launch();
   }
   typename StoreBf16EpilogueT<ID>::Params ep{out, cols, n, cols, nullptr};
@@ -263,7 +267,7 @@ int ffn_gate_up_tc(const void* x, const void* w_gate_up, long long n, int h, int
   __nv_bfloat16* k = static_cast<__nv_bfloat16*>(kept);
   const DynRows d = rows_as_m(dyn_rows, n);
 #define A3PO_GATE_UP(G, K)                                                                              \
-  contract<GateUpEpilogue<G, K>, false, false>(a, b, typename GateUpEpilogue<G, K>::Params{o, k, n, f}, d, status, stream)
+  contract<GateUpEpilogue<G, K>, false, false>(a, b, typename GateUpEpilogue<G, K>::Params{o, k, n, f}, d, status, stream, false)
   if (act == A3PO_ACT_GELU_TANH) return kept ? A3PO_GATE_UP(true, true) : A3PO_GATE_UP(true, false);
   return kept ? A3PO_GATE_UP(false, true) : A3PO_GATE_UP(false, false);
 #undef A3PO_GATE_UP
@@ -298,9 +302,9 @@ int ffn_grad_gate_up_tc(const void* grad_y, const void* w_down, const void* kept
   __nv_bfloat16* o = static_cast<__nv_bfloat16*>(z);
   if (act == A3PO_ACT_GELU_TANH)
     return contract<GradGateUpEpilogue<true>, false, true>(a, b, GradGateUpEpilogue<true>::Params{k, o, n, f}, d, status,
-                                                           stream);
+                                                           stream, false);
   return contract<GradGateUpEpilogue<false>, false, true>(a, b, GradGateUpEpilogue<false>::Params{k, o, n, f}, d, status,
-                                                          stream);
+                                                          stream, false);
 }
 
 int ffn_grad_x_tc(const void* z, const void* w_gate_up, long long n, int h, int f, void* grad_x, float* parts,

@@ -392,28 +392,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 gemm_tn_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                const __grid_constant__ CUtensorMap map_c, ItemMap im_static, int k_blocks_static,
                typename Epi::Params ep, uint32_t* status) {
-  // Work extents: static, or derived from the device-resident row count (identical in every thread).
-  ItemMap im = im_static;
-  int k_blocks = k_blocks_static;
-  bool zero_output = false;  // K extent is empty: the product is the zero matrix
-  if (im.select != nullptr && *im.select != im.select_value) {
-    im.items = 0;
-    im.dyn_rows = nullptr;
-  }
-  if (im.dyn_rows != nullptr) {
-    long long rows = static_cast<long long>(*im.dyn_rows) - im.dyn_offset;
-    rows = rows < 0 ? 0 : (rows > im.dyn_cap ? im.dyn_cap : rows);
-    if (im.dyn_is_k) {
-      k_blocks = static_cast<int>((rows + BK - 1) / BK);
-      if (k_blocks == 0) {
-        if (im.zero_when_empty) zero_output = true;
-        else im.items = 0;
-      }
-    } else {
-      im.m_tiles = static_cast<int>((rows + BM * MT - 1) / (BM * MT));
-      im.items = static_cast<long long>(im.m_tiles) * im.splits * im.k_splits;
-    }
-  }
   using Cfg = TileCfg<MT>;
   constexpr int kStages = Cfg::kStages;
   constexpr int kAccStages = Cfg::kAccStages;
@@ -473,6 +451,31 @@ gemm_tn_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   __syncthreads();
   tcgen05_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
+  wait_for_previous();
+  allow_next();
+
+  // Work extents: static, or derived from the device-resident row count (identical in every thread).
+  ItemMap im = im_static;
+  int k_blocks = k_blocks_static;
+  bool zero_output = false;  // K extent is empty: the product is the zero matrix
+  if (im.select != nullptr && *im.select != im.select_value) {
+    im.items = 0;
+    im.dyn_rows = nullptr;
+  }
+  if (im.dyn_rows != nullptr) {
+    long long rows = static_cast<long long>(*im.dyn_rows) - im.dyn_offset;
+    rows = rows < 0 ? 0 : (rows > im.dyn_cap ? im.dyn_cap : rows);
+    if (im.dyn_is_k) {
+      k_blocks = static_cast<int>((rows + BK - 1) / BK);
+      if (k_blocks == 0) {
+        if (im.zero_when_empty) zero_output = true;
+        else im.items = 0;
+      }
+    } else {
+      im.m_tiles = static_cast<int>((rows + BM * MT - 1) / (BM * MT));
+      im.items = static_cast<long long>(im.m_tiles) * im.splits * im.k_splits;
+    }
+  }
 
   bool ok = true;
   if (warp < 2 && zero_output) {
@@ -698,23 +701,6 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                  const __grid_constant__ CUtensorMap map_c, ItemMap im_static, int k_blocks_static,
                  typename Epi::Params ep, uint32_t* status) {
   constexpr int kPairRows = 2 * BM;
-  ItemMap im = im_static;   // m_tiles counts 256-row pair tiles here
-  int k_blocks = k_blocks_static;
-  bool zero_output = false;  // K extent is empty: the product is the zero matrix
-  if (im.dyn_rows != nullptr) {
-    long long rows = static_cast<long long>(*im.dyn_rows) - im.dyn_offset;
-    rows = rows < 0 ? 0 : (rows > im.dyn_cap ? im.dyn_cap : rows);
-    if (im.dyn_is_k) {
-      k_blocks = static_cast<int>((rows + BK - 1) / BK);
-      if (k_blocks == 0) {
-        if (im.zero_when_empty) zero_output = true;
-        else im.items = 0;
-      }
-    } else {
-      im.m_tiles = static_cast<int>((rows + kPairRows - 1) / kPairRows);
-      im.items = static_cast<long long>(im.m_tiles) * im.splits;
-    }
-  }
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* smem_a = smem;
@@ -758,6 +744,26 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
   cluster_sync_all();   // the peer's barriers exist before anything signals them
   tcgen05_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
+  wait_for_previous();
+  allow_next();
+
+  ItemMap im = im_static;   // m_tiles counts 256-row pair tiles here
+  int k_blocks = k_blocks_static;
+  bool zero_output = false;  // K extent is empty: the product is the zero matrix
+  if (im.dyn_rows != nullptr) {
+    long long rows = static_cast<long long>(*im.dyn_rows) - im.dyn_offset;
+    rows = rows < 0 ? 0 : (rows > im.dyn_cap ? im.dyn_cap : rows);
+    if (im.dyn_is_k) {
+      k_blocks = static_cast<int>((rows + BK - 1) / BK);
+      if (k_blocks == 0) {
+        if (im.zero_when_empty) zero_output = true;
+        else im.items = 0;
+      }
+    } else {
+      im.m_tiles = static_cast<int>((rows + kPairRows - 1) / kPairRows);
+      im.items = static_cast<long long>(im.m_tiles) * im.splits;
+    }
+  }
 
   bool ok = true;
   if (warp < 2 && zero_output) {
@@ -996,10 +1002,10 @@ struct DynRows {
   int select_value = 0;
 };
 
-// C[M, N] = sum_k A[m, k] B[n, k];  splits = 0 means one column tile per work item.
+// C[M, N] = sum_k A[m, k] B[n, k];  splits = 0 means one column tile per work item.  early: see launch_early.
 template <class Epi, bool A_MN, bool B_MN, int MT = 1>
 int launch_gemm(const Operand& a, const Operand& b, int splits, const typename Epi::Params& ep, const DynRows& dyn,
-                uint32_t* status, cudaStream_t stream, int k_splits = 1) {
+                uint32_t* status, cudaStream_t stream, int k_splits = 1, bool early = false) {
   constexpr size_t kSmemBytes = TileCfg<MT>::kSmemBytes;
   CUtensorMap map_a, map_b, map_c;
   A3PO_RETURN_IF(make_map(&map_a, a, A_MN, BM * MT));
@@ -1040,8 +1046,8 @@ int launch_gemm(const Operand& a, const Operand& b, int splits, const typename E
   long long grid = sm_count();
   if (grid > im.items) grid = im.items;
   if (grid < 1) return A3PO_OK;
-  A3PO_LAUNCH(Epi::kKernelId, stream, (kernel<<<static_cast<unsigned>(grid), kTcThreads, kSmemBytes, stream>>>(
-                                          map_a, map_b, map_c, im, k_blocks, ep, status)));
+  A3PO_LAUNCH(Epi::kKernelId, stream, (launch_early(kernel, static_cast<unsigned>(grid), kTcThreads, kSmemBytes, stream, 1,
+                                                    early, map_a, map_b, map_c, im, k_blocks, ep, status)));
   return after_launch();
 }
 
@@ -1091,7 +1097,7 @@ int pair_capacity() {
 // group_m / paced: rasterisation group in 256-row tiles, and whether the CTAs keep in step (see ItemMap, Pace).
 template <class Epi, bool A_MN, bool B_MN>
 int launch_pair_gemm(const Operand& a, const Operand& b, int splits, const typename Epi::Params& ep, const DynRows& dyn,
-                     uint32_t* status, cudaStream_t stream, int group_m = kGroupM, bool paced = false) {
+                     uint32_t* status, cudaStream_t stream, int group_m = kGroupM, bool paced = false, bool early = false) {
   const int pairs_max = pair_capacity<Epi, A_MN, B_MN>();
   if (pairs_max <= 0) return A3PO_ERR_UNSUPPORTED;
   CUtensorMap map_a, map_b, map_c;
@@ -1122,8 +1128,8 @@ int launch_pair_gemm(const Operand& a, const Operand& b, int splits, const typen
   if (pairs > im.items) pairs = im.items;
   if (pairs < 1) return A3PO_OK;
   auto kernel = gemm_pair_kernel<Epi, A_MN, B_MN>;
-  A3PO_LAUNCH(Epi::kKernelId, stream, (kernel<<<static_cast<unsigned>(2 * pairs), kTcThreads, kPairSmemBytes, stream>>>(
-                                          map_a, map_b, map_c, im, k_blocks, ep, status)));
+  A3PO_LAUNCH(Epi::kKernelId, stream, (launch_early(kernel, static_cast<unsigned>(2 * pairs), kTcThreads, kPairSmemBytes,
+                                                    stream, 1, early, map_a, map_b, map_c, im, k_blocks, ep, status)));
   return after_launch();
 }
 
