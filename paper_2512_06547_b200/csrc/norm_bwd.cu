@@ -10,10 +10,11 @@
 namespace a3po {
 namespace {
 
-// MAXT: most threads of a block (a register limit: three blocks of 256 threads on an SM, or two
-// where three would spill; one of 512).
+// MAXT: most threads of a block, and with it a register limit: two blocks of 256 threads on an SM, one of 512.  With three,
+// a layer norm's sums spill (65,536 x 2,048 bf16: 194 us against 140) and an RMS norm gains nothing (8B-shaped batch,
+// 39 % masked: 402 against 376); only element-wise rows, which have no ring, want the third (5,001 x 1,003: 24.6 against 22.6).
 template <typename T, int CPT, bool WIDE, int MAXT, bool VEC, bool LAYER, bool JOIN>
-__global__ void __launch_bounds__(MAXT, MAXT == 256 ? (JOIN || sizeof(T) == 4 ? 2 : 3) : 1)
+__global__ void __launch_bounds__(MAXT, MAXT == 256 ? (VEC || JOIN || sizeof(T) == 4 ? 2 : 3) : 1)
 norm_bwd_kernel(const NormBwdArgs<T> a, int lanes, Turns turns) {
   constexpr int kIn = JOIN ? 3 : 2;
   constexpr int kRing = ring_rows<T>(kIn, CPT);
