@@ -459,12 +459,12 @@ int a3po_dropout_norm_bwd(const void* r, float p, const uint64_t* rng, const voi
  * x, y, grad_x, grad_y [N, H]; w_gate_up [2 F, H] (the F rows of Wg, then the F rows of Wu); w_down [H, F]; dtype `dt`,
  * 16-byte aligned.  Any H and F: bf16 with H and F multiples of 8 runs on the tensor cores, the rest on the FP32 pipes.
  * Both projections, the activation and the product are one kernel; dh never reaches memory either.  Accumulation is
- * fp32; for bf16 the intermediates that enter a matrix product (h, dg, du) and the kept g and u are rounded to bf16.
+ * fp32; for bf16 the intermediates that enter a matrix product (h, dg, du) are rounded to bf16.
  *
  * row_mask uint8 [N] or NULL: rows with 0 are skipped (of more than 32 rows only the others are multiplied): nothing
  * of them is read, their y and grad_x are 0, they add nothing to a weight gradient.
  * kept: device buffer of a3po_gated_ffn_kept_bytes(N, F, dt) bytes, 256-byte aligned, that receives g, u and h for the
- * backward (layout private; about 6 N F bytes for bf16), or NULL when no backward follows.  The backward takes it with
+ * backward (layout private; about 8 N F bytes for bf16), or NULL when no backward follows.  The backward takes it with
  * the forward's x, weights, row_mask, N, H, F, dt and act; it is not changed, so the backward may be repeated.
  * grad_w_gate_up [2 F, H], grad_w_down [H, F]: dtype grad_w_dt (A3PO_F32, or dt), overwritten; with
  * accumulate_grad_w != 0 added to (A3PO_F32 only, else A3PO_ERR_UNSUPPORTED).

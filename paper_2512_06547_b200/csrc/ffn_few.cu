@@ -168,7 +168,7 @@ template <int MT, bool HALF, int S, bool GELU>
 __global__ void __launch_bounds__(kFewThreads)
 few_gate_up_kernel(const __nv_bfloat16* __restrict__ x, const __nv_bfloat16* __restrict__ w_gate_up,
                    const uint8_t* __restrict__ row_mask, int n, int h, int f, __nv_bfloat16* __restrict__ hid,
-                   __nv_bfloat16* __restrict__ kept) {
+                   uint8_t* __restrict__ kept) {
   extern __shared__ __align__(16) uint8_t smem[];
   constexpr int OUT = 2 * S;   // gate blocks, then up blocks
   const int warp = threadIdx.x / kWarp, lane = threadIdx.x % kWarp;
@@ -200,9 +200,14 @@ few_gate_up_kernel(const __nv_bfloat16* __restrict__ x, const __nv_bfloat16* __r
     gate_activation<GELU>(g, a, slope);
     hid[static_cast<long long>(row) * f + c0 + col] = __float2bfloat16_rn(a * u);
     if (kept) {
-      __nv_bfloat16* k = kept + kept_offset(row, c0 + col, f);
-      k[0] = __float2bfloat16_rn(g);
-      k[kKeptElems] = __float2bfloat16_rn(u);
+      const int c = c0 + col, j = c % kKeptCols;
+      uint8_t* tile = kept + kept_tile(row, c, f);
+      uint8_t* upper = tile + (j / 8 * kKeptRows + row) * 16 + j % 8 * 2;
+      uint8_t* third = tile + 2 * kKeptUpper + (j / 16 * kKeptRows + row) * 16 + j % 16;
+      *reinterpret_cast<uint16_t*>(upper) = static_cast<uint16_t>(__float_as_uint(g) >> 16);
+      *reinterpret_cast<uint16_t*>(upper + kKeptUpper) = static_cast<uint16_t>(__float_as_uint(u) >> 16);
+      *third = static_cast<uint8_t>(__float_as_uint(g) >> 8);
+      third[kKeptThird] = static_cast<uint8_t>(__float_as_uint(u) >> 8);
     }
   }
   if (S > 1) ptx::cluster_sync_all();   // the peer may still read this block's sums
@@ -274,7 +279,7 @@ bool pair_blocks(long long n, int k) { return n > 4 && k >= 2048; }
 
 template <int MT, bool HALF>
 int few_impl(const __nv_bfloat16* x, const __nv_bfloat16* wgu, const __nv_bfloat16* wd, const uint8_t* mask, int n, int h,
-             int f, a3po_activation act, __nv_bfloat16* hid, __nv_bfloat16* y, __nv_bfloat16* kept, cudaStream_t s) {
+             int f, a3po_activation act, __nv_bfloat16* hid, __nv_bfloat16* y, uint8_t* kept, cudaStream_t s) {
   constexpr int kSmem = ring_bytes(MT);
   const bool gelu = act == A3PO_ACT_GELU_TANH;
   const __nv_bfloat16* hid_in = hid;
@@ -297,7 +302,7 @@ int ffn_few_rows_fwd(const void* x_, const void* w_gate_up, const void* w_down, 
   const __nv_bfloat16* wd = static_cast<const __nv_bfloat16*>(w_down);
   __nv_bfloat16* hid = static_cast<__nv_bfloat16*>(hid_);
   __nv_bfloat16* y = static_cast<__nv_bfloat16*>(y_);
-  __nv_bfloat16* kept = static_cast<__nv_bfloat16*>(kept_);
+  uint8_t* kept = static_cast<uint8_t*>(kept_);
   const int rows = static_cast<int>(n);
   if (n <= 8) return few_impl<1, true>(x, wgu, wd, row_mask, rows, h, f, act, hid, y, kept, stream);
   if (n <= 16) return few_impl<1, false>(x, wgu, wd, row_mask, rows, h, f, act, hid, y, kept, stream);

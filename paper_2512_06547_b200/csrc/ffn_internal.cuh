@@ -9,24 +9,28 @@
 
 namespace a3po {
 
-// Kept values of the forward (bf16 shapes of the tensor-core path): g and u as the backward's epilogue reads them, one
-// accumulator row per thread.  Tile (128 rows, 32 columns) holds first g then u; inside, 16-byte piece j (8 columns) of
-// row r sits at (j * 128 + r) * 16 bytes, so that the 32 rows of a warp are one contiguous 512-byte access.
-// h itself follows them, row-major [n, f]: the forward writes it for its second product anyway, and the backward then need
-// not write it again.
+// Kept values of the forward (bf16 shapes of the tensor-core path): g and u in 24 bits each (the upper 24 of the fp32 value),
+// as the backward's epilogue reads them, one accumulator row per thread.  bf16 would be a third less, but its rounding
+// of g and u is then the largest error of grad_x and grad_w_gate_up (2-norm 0.0030 against 0.0024, of which the
+// rounding of dg, du and of the results themselves is the rest); 24 bits unpack with one byte permutation per value.
+// Tile (128 rows, 32 columns), 24 KB: upper halves of g, of u, third bytes of g, of u.  Inside, 16-byte piece j of row r
+// sits at (j * 128 + r) * 16 bytes (8 columns a piece, 16 for the third bytes), so that the 32 rows of a warp are one
+// contiguous 512-byte access.
+// h itself follows the tiles, row-major [n, f] bf16: the forward writes it for its second product anyway, and the backward
+// then need not write it again.
 constexpr int kKeptRows = 128;
 constexpr int kKeptCols = 32;
-constexpr int kKeptElems = kKeptRows * kKeptCols;   // elements of one of the two halves of a tile
+constexpr int kKeptUpper = kKeptRows * kKeptCols * 2;   // bytes of the upper halves of g (or u) in a tile
+constexpr int kKeptThird = kKeptRows * kKeptCols;       // bytes of the third bytes
+constexpr int kKeptTile = 2 * (kKeptUpper + kKeptThird);
 __host__ __device__ inline long long kept_col_tiles(int f) { return (static_cast<long long>(f) + kKeptCols - 1) / kKeptCols; }
-// Element offset of column `col` of row `row` of g (u lies kKeptElems further).
-__host__ __device__ inline long long kept_offset(long long row, int col, int f) {
-  const long long tile = (row / kKeptRows) * kept_col_tiles(f) + col / kKeptCols;
-  return tile * 2 * kKeptElems + ((col % kKeptCols) / 8 * kKeptRows + row % kKeptRows) * 8 + col % 8;
+// Byte offset of the tile that holds column `col` of row `row`.
+__host__ __device__ inline long long kept_tile(long long row, int col, int f) {
+  return ((row / kKeptRows) * kept_col_tiles(f) + col / kKeptCols) * kKeptTile;
 }
-
 // Bytes of g and u, after which h starts.
 inline size_t kept_gate_bytes(long long n, int f) {
-  return static_cast<size_t>((n + kKeptRows - 1) / kKeptRows) * static_cast<size_t>(kept_col_tiles(f)) * 2 * kKeptElems * 2;
+  return static_cast<size_t>((n + kKeptRows - 1) / kKeptRows) * static_cast<size_t>(kept_col_tiles(f)) * kKeptTile;
 }
 
 #ifdef __CUDACC__
@@ -80,7 +84,7 @@ int ffn_few_rows_fwd(const void* x, const void* w_gate_up, const void* w_down, c
 int ffn_select_rows(const void* src, const uint8_t* row_mask, long long n, int h, void* dst, cudaStream_t stream);
 
 // ---- FP32-pipe kernels (ffn_simt.cu): fp32, and bf16 shapes the others do not take ----
-// kept (may be null): [2][n][f] of the storage type;  hid: fp32 [n, f];  z: fp32 [n][3][f] (dg | du | h).
+// kept (may be null): fp32 [2][n][f];  hid: fp32 [n, f];  z: fp32 [n][3][f] (dg | du | h).
 int ffn_fwd_simt(const void* x, const void* w_gate_up, const void* w_down, const uint8_t* row_mask, long long n, int h,
                  int f, a3po_dtype dt, a3po_activation act, float* hid, void* y, void* kept, cudaStream_t stream);
 int ffn_bwd_simt(const void* x, const void* w_gate_up, const void* w_down, const uint8_t* row_mask, const void* kept,

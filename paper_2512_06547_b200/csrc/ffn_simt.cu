@@ -170,7 +170,7 @@ __device__ __forceinline__ void activation_any(int gelu, float g, float& a, floa
 template <typename T, int R>
 __global__ void __launch_bounds__(kSimtThreads)
 simt_gate_up_kernel(Mat<T> x, Mat<T> wg, Mat<T> wu, long long n, int f, int gelu, float* __restrict__ hid,
-                    T* __restrict__ kept) {
+                    float* __restrict__ kept) {
   constexpr int kTile = 16 * R;
   __shared__ float xs[kBK][kTile + 4], gs[kBK][kTile + 4], us[kBK][kTile + 4];
   const long long m0 = static_cast<long long>(blockIdx.x) * kTile;
@@ -208,8 +208,8 @@ simt_gate_up_kernel(Mat<T> x, Mat<T> wg, Mat<T> wu, long long n, int f, int gelu
       activation_any(gelu, ag[i][j], a, slope);
       hid[r * f + c] = a * au[i][j];
       if (kept) {
-        kept[r * f + c] = from_float<T>(ag[i][j]);
-        kept[(n + r) * f + c] = from_float<T>(au[i][j]);
+        kept[r * f + c] = ag[i][j];
+        kept[(n + r) * f + c] = au[i][j];
       }
     }
   }
@@ -242,7 +242,7 @@ simt_gemm_kernel(Mat<TA> a, Mat<TB> b, TC* __restrict__ c, long long ldc, int ac
 // dh = dy Wd with the gradient of the gate in the epilogue: z[r][0..2][c] = dg, du, h
 template <typename T, int R, int G>
 __global__ void __launch_bounds__(kSimtThreads* G)
-simt_grad_gate_up_kernel(Mat<T> dy, Mat<T> wd, const T* __restrict__ kept, long long n, int f, int gelu,
+simt_grad_gate_up_kernel(Mat<T> dy, Mat<T> wd, const float* __restrict__ kept, long long n, int f, int gelu,
                          float* __restrict__ z) {
   constexpr int kTile = 16 * R;
   extern __shared__ __align__(16) uint8_t smem[];
@@ -259,7 +259,7 @@ simt_grad_gate_up_kernel(Mat<T> dy, Mat<T> wd, const T* __restrict__ kept, long 
     for (int j = 0; j < R; ++j) {
       const int c = n0 + threadIdx.x % 16 * R + j;
       if (r >= n || c >= f) continue;
-      const float g = to_float(kept[r * f + c]), u = to_float(kept[(n + r) * f + c]);
+      const float g = kept[r * f + c], u = kept[(n + r) * f + c];
       float a, slope;
       activation_any(gelu, g, a, slope);
       float* out = z + r * 3 * f + c;
@@ -310,7 +310,7 @@ int gemm(const Mat<TA>& a, const Mat<TB>& b, TC* c, long long ldc, int accumulat
 
 template <typename T>
 int fwd_impl(const T* x, const T* wgu, const T* wd, const uint8_t* mask, long long n, int h, int f, int gelu, float* hid,
-             T* y, T* kept, cudaStream_t s) {
+             T* y, float* kept, cudaStream_t s) {
   const Mat<T> xm{x, h, 1, n, h, mask, true}, wg{wgu, h, 1, f, h, nullptr, true},
       wu{wgu + static_cast<long long>(f) * h, h, 1, f, h, nullptr, true};
   if (shape_of(n, f) != Shape::kPlain)
@@ -324,7 +324,7 @@ int fwd_impl(const T* x, const T* wgu, const T* wd, const uint8_t* mask, long lo
 }
 
 template <typename T, typename TG>
-int bwd_impl(const T* x, const T* wgu, const T* wd, const uint8_t* mask, const T* kept, const T* gy, long long n, int h,
+int bwd_impl(const T* x, const T* wgu, const T* wd, const uint8_t* mask, const float* kept, const T* gy, long long n, int h,
              int f, int gelu, float* z, T* gx, TG* gwgu, TG* gwd, int accumulate, cudaStream_t s) {
   const long long zf = 3ll * f;
   const Mat<T> dy{gy, h, 1, n, h, mask, true}, wdt{wd, 1, f, f, h, nullptr, false};
@@ -355,7 +355,7 @@ int ffn_fwd_simt(const void* x, const void* w_gate_up, const void* w_down, const
                     row_mask, n, h, f, gelu, hid, static_cast<float*>(y), static_cast<float*>(kept), stream);
   using B = __nv_bfloat16;
   return fwd_impl(static_cast<const B*>(x), static_cast<const B*>(w_gate_up), static_cast<const B*>(w_down), row_mask, n,
-                  h, f, gelu, hid, static_cast<B*>(y), static_cast<B*>(kept), stream);
+                  h, f, gelu, hid, static_cast<B*>(y), static_cast<float*>(kept), stream);
 }
 
 int ffn_bwd_simt(const void* x, const void* w_gate_up, const void* w_down, const uint8_t* row_mask, const void* kept,
@@ -366,7 +366,7 @@ int ffn_bwd_simt(const void* x, const void* w_gate_up, const void* w_down, const
   using B = __nv_bfloat16;
 #define A3PO_FFN_BWD(T, TG)                                                                                            \
   bwd_impl(static_cast<const T*>(x), static_cast<const T*>(w_gate_up), static_cast<const T*>(w_down), row_mask,        \
-           static_cast<const T*>(kept), static_cast<const T*>(grad_y), n, h, f, gelu, z, static_cast<T*>(grad_x),      \
+           static_cast<const float*>(kept), static_cast<const T*>(grad_y), n, h, f, gelu, z, static_cast<T*>(grad_x),      \
            static_cast<TG*>(grad_w_gate_up), static_cast<TG*>(grad_w_down), accumulate, stream)
   if (dt == A3PO_F32) return A3PO_FFN_BWD(float, float);
   return grad_dt == A3PO_F32 ? A3PO_FFN_BWD(B, float) : A3PO_FFN_BWD(B, B);

@@ -7,9 +7,9 @@
 //             writes dg and du, operands of two gradient contractions (h, the third's, is the forward's own)
 //   down, dx, dW   plain contractions
 //
-// Rounding: h, dg, du and the kept g and u are bf16, because they are operands of bf16 matrix instructions (and half
-// the bytes); each costs half a step (2^-9 relative) of an element that enters a long sum.  Everything between (the
-// activation, the products, dh) is fp32.
+// Rounding: h, dg and du are bf16, because they are operands of bf16 matrix instructions; each costs half a step (2^-9
+// relative) of an element that enters a long sum.  The kept g and u are cut to 24 bits (ffn_internal.cuh).  Everything
+// between (the activation, the products, dh) is fp32.
 
 #include "ffn_internal.cuh"
 #include "gemm_tc.cuh"
@@ -26,6 +26,32 @@ __device__ __forceinline__ uint4 pack8(const float (&v)[kEpiChunk], int q) {
   return u;
 }
 
+// The upper 24 bits of 32 fp32 values: 16-byte pieces of their upper halves and of their third bytes, kKeptRows apart.
+__device__ __forceinline__ void keep24(const uint32_t (&v)[kEpiChunk], uint8_t* upper, uint8_t* third) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __byte_perm(v[q * 8 + i * 2], v[q * 8 + i * 2 + 1], 0x7632);
+    __stcs(reinterpret_cast<uint4*>(upper) + q * kKeptRows, make_uint4(w[0], w[1], w[2], w[3]));
+  }
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t* e = v + q * 16 + i * 4;
+      w[i] = __byte_perm(__byte_perm(e[0], e[1], 0x0051), __byte_perm(e[2], e[3], 0x0051), 0x5410);
+    }
+    __stcs(reinterpret_cast<uint4*>(third) + q * kKeptRows, make_uint4(w[0], w[1], w[2], w[3]));
+  }
+}
+// Value e (0 or 1) of a word of upper halves, with its third byte b (0..3) of word t; the lowest byte repeats the third,
+// which is below what is kept.
+__device__ __forceinline__ float kept24(uint32_t upper, int e, uint32_t third, int b) {
+  return __uint_as_float(__byte_perm(upper, third, (e ? 0x3200u : 0x1000u) | static_cast<uint32_t>(0x44 + b * 0x11)));
+}
+
 template <bool GELU, bool KEEP>
 struct GateUpEpilogue {
   static constexpr int kKernelId = kKFfnGate;
@@ -33,7 +59,7 @@ struct GateUpEpilogue {
   static constexpr bool kPrefetch = false;
   struct Params {
     __nv_bfloat16* hid;    // [n, f]
-    __nv_bfloat16* kept;   // see ffn_internal.cuh
+    uint8_t* kept;         // see ffn_internal.cuh
     long long n;
     int b_rows;            // f: rows of each of the two stacked matrices
   };
@@ -43,21 +69,9 @@ struct GateUpEpilogue {
   __device__ __forceinline__ void chunk_pair(const Params& p, int tile_row0, int col0, uint32_t (&rg)[kEpiChunk],
                                              uint32_t (&ru)[kEpiChunk], SlabStore& st) {
     if (KEEP && col0 < p.b_rows && tile_row0 < p.n) {   // a pair's second tile may lie past the buffers
-      uint4* k = reinterpret_cast<uint4*>(p.kept + kept_offset(tile_row0 + st.row_in_tile, col0, p.b_rows));
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        uint4 a, b;
-        a.x = pack_bf16x2(bits_to_float(rg[q * 8 + 0]), bits_to_float(rg[q * 8 + 1]));
-        a.y = pack_bf16x2(bits_to_float(rg[q * 8 + 2]), bits_to_float(rg[q * 8 + 3]));
-        a.z = pack_bf16x2(bits_to_float(rg[q * 8 + 4]), bits_to_float(rg[q * 8 + 5]));
-        a.w = pack_bf16x2(bits_to_float(rg[q * 8 + 6]), bits_to_float(rg[q * 8 + 7]));
-        b.x = pack_bf16x2(bits_to_float(ru[q * 8 + 0]), bits_to_float(ru[q * 8 + 1]));
-        b.y = pack_bf16x2(bits_to_float(ru[q * 8 + 2]), bits_to_float(ru[q * 8 + 3]));
-        b.z = pack_bf16x2(bits_to_float(ru[q * 8 + 4]), bits_to_float(ru[q * 8 + 5]));
-        b.w = pack_bf16x2(bits_to_float(ru[q * 8 + 6]), bits_to_float(ru[q * 8 + 7]));
-        __stcs(k + q * kKeptRows, a);
-        __stcs(k + q * kKeptRows + kKeptElems / 8, b);
-      }
+      uint8_t* tile = p.kept + kept_tile(tile_row0, col0, p.b_rows) + st.row_in_tile * 16;
+      keep24(rg, tile, tile + 2 * kKeptUpper);
+      keep24(ru, tile + kKeptUpper, tile + 2 * kKeptUpper + kKeptThird);
     }
     float hv[kEpiChunk];
 #pragma unroll
@@ -82,7 +96,7 @@ struct GradGateUpEpilogue : PlainEpilogue {
   static constexpr bool kPrefetch = true;
   static constexpr int kKernelId = kKFfnGradGate;
   struct Params {
-    const __nv_bfloat16* kept;
+    const uint8_t* kept;
     __nv_bfloat16* z;   // [n][2][f]
     long long n;        // rows of z
     int f;
@@ -101,18 +115,26 @@ struct GradGateUpEpilogue : PlainEpilogue {
   }
   static constexpr uint32_t kPart = BM * kEpiChunk * 2;   // 8 KB
   long long row;
-  uint4 next_g[4], next_u[4];   // g and u of the columns that come next
-  __device__ __forceinline__ void read_kept(const uint4* k) {
+  uint4 next_g[6], next_u[6];   // g and u of the columns that come next: upper halves, third bytes
+  __device__ __forceinline__ void read_kept(const Params& p, int col0) {
+    const uint8_t* tile = p.kept + kept_tile(row, col0, p.f) + (row % kKeptRows) * 16;
+    const uint4* g = reinterpret_cast<const uint4*>(tile);
+    const uint4* t = reinterpret_cast<const uint4*>(tile + 2 * kKeptUpper);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      next_g[q] = __ldcs(k + q * kKeptRows);
-      next_u[q] = __ldcs(k + q * kKeptRows + kKeptElems / 8);
+      next_g[q] = __ldcs(g + q * kKeptRows);
+      next_u[q] = __ldcs(g + kKeptUpper / 16 + q * kKeptRows);
+    }
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      next_g[4 + q] = __ldcs(t + q * kKeptRows);
+      next_u[4 + q] = __ldcs(t + kKeptThird / 16 + q * kKeptRows);
     }
   }
   __device__ __forceinline__ void begin(const Params&, long long row_) { row = row_; }
   // before the tile's product is waited for
   __device__ __forceinline__ void prefetch(const Params& p, int tile_row0, int col0) {
-    if (col0 < p.f && tile_row0 < p.n) read_kept(reinterpret_cast<const uint4*>(p.kept + kept_offset(row, col0, p.f)));
+    if (col0 < p.f && tile_row0 < p.n) read_kept(p, col0);
   }
   // 16-byte piece j (0..3) of this thread's row in a slab of 64-byte rows with the 64-byte swizzle
   static __device__ __forceinline__ uint4* piece(uint8_t* s, int r, int j) {
@@ -121,26 +143,27 @@ struct GradGateUpEpilogue : PlainEpilogue {
   __device__ __forceinline__ void chunk(const Params& p, int tile_row0, int col0, uint32_t (&r)[kEpiChunk],
                                         SlabStore& st) {
     if (col0 >= p.f || tile_row0 >= p.n) return;   // the same for all threads
-    const uint4* k = reinterpret_cast<const uint4*>(p.kept + kept_offset(row, col0, p.f));
-    uint4 kg[4], ku[4];
+    uint4 kg[6], ku[6];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < 6; ++q) {
       kg[q] = next_g[q];
       ku[q] = next_u[q];
     }
-    if (col0 + kEpiChunk < p.f) read_kept(k + 2 * kKeptElems / 8);   // the next 32 columns, while these are worked on
+    if (col0 + kEpiChunk < p.f) read_kept(p, col0 + kEpiChunk);   // the next 32 columns, while these are worked on
     uint4 og[4], ou[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const uint32_t wg[4] = {kg[q].x, kg[q].y, kg[q].z, kg[q].w}, wu[4] = {ku[q].x, ku[q].y, ku[q].z, ku[q].w};
+      const uint4 tg = kg[4 + q / 2], tu = ku[4 + q / 2];   // third bytes of columns 16 (q / 2) .. + 15
+      const uint32_t bg[2] = {q % 2 ? tg.z : tg.x, q % 2 ? tg.w : tg.y}, bu[2] = {q % 2 ? tu.z : tu.x, q % 2 ? tu.w : tu.y};
       uint32_t vg[4], vu[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float dg[2], du[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const float g = __uint_as_float(e ? wg[i] & 0xffff0000u : wg[i] << 16);
-          const float u = __uint_as_float(e ? wu[i] & 0xffff0000u : wu[i] << 16);
+          const float g = kept24(wg[i], e, bg[i / 2], (i % 2) * 2 + e);
+          const float u = kept24(wu[i], e, bu[i / 2], (i % 2) * 2 + e);
           const float dh = bits_to_float(r[q * 8 + i * 2 + e]);
           float a, slope;
           gate_activation<GELU>(g, a, slope);
@@ -264,7 +287,7 @@ int ffn_gate_up_tc(const void* x, const void* w_gate_up, long long n, int h, int
                    void* kept, const int* dyn_rows, uint32_t* status, cudaStream_t stream) {
   const Operand a{x, n, h, h}, b{w_gate_up, 2ll * f, h, h};
   __nv_bfloat16* o = static_cast<__nv_bfloat16*>(hid);
-  __nv_bfloat16* k = static_cast<__nv_bfloat16*>(kept);
+  uint8_t* k = static_cast<uint8_t*>(kept);
   const DynRows d = rows_as_m(dyn_rows, n);
 #define A3PO_GATE_UP(G, K)                                                                              \
   contract<GateUpEpilogue<G, K>, false, false>(a, b, typename GateUpEpilogue<G, K>::Params{o, k, n, f}, d, status, stream, false)
@@ -298,7 +321,7 @@ int ffn_grad_gate_up_tc(const void* grad_y, const void* w_down, const void* kept
                         a3po_activation act, void* z, const int* dyn_rows, uint32_t* status, cudaStream_t stream) {
   const Operand a{grad_y, n, h, h}, b{w_down, f, h, f};
   const DynRows d = rows_as_m(dyn_rows, n);
-  const __nv_bfloat16* k = static_cast<const __nv_bfloat16*>(kept);
+  const uint8_t* k = static_cast<const uint8_t*>(kept);
   __nv_bfloat16* o = static_cast<__nv_bfloat16*>(z);
   if (act == A3PO_ACT_GELU_TANH)
     return contract<GradGateUpEpilogue<true>, false, true>(a, b, GradGateUpEpilogue<true>::Params{k, o, n, f}, d, status,
