@@ -57,6 +57,7 @@ struct GateUpEpilogue {
   static constexpr int kKernelId = kKFfnGate;
   static constexpr bool kGated = true;
   static constexpr bool kPrefetch = false;
+  static constexpr int kGroups = 2;
   struct Params {
     __nv_bfloat16* hid;    // [n, f]
     uint8_t* kept;         // see ffn_internal.cuh
@@ -94,6 +95,7 @@ struct GateUpEpilogue {
 template <bool GELU>
 struct GradGateUpEpilogue : PlainEpilogue {
   static constexpr bool kPrefetch = true;
+  static constexpr int kGroups = 2;
   static constexpr int kKernelId = kKFfnGradGate;
   struct Params {
     const uint8_t* kept;
@@ -115,6 +117,7 @@ struct GradGateUpEpilogue : PlainEpilogue {
   }
   static constexpr uint32_t kPart = BM * kEpiChunk * 2;   // 8 KB
   long long row;
+  int end_col;                  // of the columns that this thread works through in the tile
   uint4 next_g[6], next_u[6];   // g and u of the columns that come next: upper halves, third bytes
   __device__ __forceinline__ void read_kept(const Params& p, int col0) {
     const uint8_t* tile = p.kept + kept_tile(row, col0, p.f) + (row % kKeptRows) * 16;
@@ -133,7 +136,8 @@ struct GradGateUpEpilogue : PlainEpilogue {
   }
   __device__ __forceinline__ void begin(const Params&, long long row_) { row = row_; }
   // before the tile's product is waited for
-  __device__ __forceinline__ void prefetch(const Params& p, int tile_row0, int col0) {
+  __device__ __forceinline__ void prefetch(const Params& p, int tile_row0, int col0, int cols) {
+    end_col = min(col0 + cols, p.f);
     if (col0 < p.f && tile_row0 < p.n) read_kept(p, col0);
   }
   // 16-byte piece j (0..3) of this thread's row in a slab of 64-byte rows with the 64-byte swizzle
@@ -149,7 +153,7 @@ struct GradGateUpEpilogue : PlainEpilogue {
       kg[q] = next_g[q];
       ku[q] = next_u[q];
     }
-    if (col0 + kEpiChunk < p.f) read_kept(p, col0 + kEpiChunk);   // the next 32 columns, while these are worked on
+    if (col0 + kEpiChunk < end_col) read_kept(p, col0 + kEpiChunk);   // the next 32 columns, while these are worked on
     uint4 og[4], ou[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -183,7 +187,7 @@ struct GradGateUpEpilogue : PlainEpilogue {
       *piece(s + kPart, st.row_in_tile, q) = ou[q];
     }
     fence_proxy_async_smem();
-    named_barrier_sync(SlabStore::kBarrierId, 128);
+    named_barrier_sync(st.barrier_id, 128);
     if (st.issuer) {
       tma_store_3d(st.map, s, col0, 0, tile_row0);
       tma_store_3d(st.map, s + kPart, col0, 1, tile_row0);

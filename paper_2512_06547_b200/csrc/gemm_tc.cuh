@@ -250,13 +250,16 @@ struct SlabStore {
   int row_in_tile;
   bool issuer;
   uint32_t issued = 0;
-  static constexpr int kBarrierId = 1;
+  int barrier_id = 1;   // hardware barrier of the 128 threads that share the slabs
+  bool one_slab = false;
 
   // Returns the slab to fill next; all epilogue threads call it together.
   __device__ __forceinline__ uint8_t* acquire() {
-    if (issuer) bulk_wait_group_read<1>();  // the copy that used this slab two submissions ago has read it
-    named_barrier_sync(kBarrierId, 128);
-    return (issued & 1u) ? slab1 : slab0;
+    if (issuer) {  // the copy that used this slab two submissions ago (with one slab: the last one) has read it
+      if (one_slab) bulk_wait_group_read<0>(); else bulk_wait_group_read<1>();
+    }
+    named_barrier_sync(barrier_id, 128);
+    return (issued & 1u) && !one_slab ? slab1 : slab0;
   }
   // 16-byte piece j (0..7) of this thread's row.
   __device__ __forceinline__ uint4* piece(uint8_t* s, int j) const {
@@ -265,7 +268,7 @@ struct SlabStore {
   // Hands the filled slab to the copy engine: global tile origin (x, y) in elements.
   __device__ __forceinline__ void submit(uint8_t* s, int x, int y, bool in_range, bool reduce_add) {
     fence_proxy_async_smem();
-    named_barrier_sync(kBarrierId, 128);
+    named_barrier_sync(barrier_id, 128);
     if (issuer) {
       if (in_range) {
         if (reduce_add) tma_reduce_add_f32_2d(map, s, x, y);
@@ -283,10 +286,13 @@ struct SlabStore {
 // What an epilogue may ask of the kernel.  kGated: a B tile is not 256 consecutive rows of B but the 128 rows from
 // n_tile * 128 on followed by the 128 rows from ep.b_rows + n_tile * 128 on (two stacked matrices of b_rows rows), and
 // the epilogue gets the two accumulators of a column together.
-// kPrefetch: prefetch(ep, tile_row0, col0) is called before the tile's product is waited for.
+// kPrefetch: prefetch(ep, tile_row0, col0, cols) is called before the product of those columns is waited for.
+// kGroups: groups of four epilogue warps in the pair kernel; each takes its share of a tile's columns.  Two for epilogues
+// that take longer than a tile's MMAs at a short K (4 warps cannot fill the issue slots between their barriers).
 struct PlainEpilogue {
   static constexpr bool kGated = false;
   static constexpr bool kPrefetch = false;
+  static constexpr int kGroups = 1;
 };
 
 template <int KERNEL_ID>
@@ -352,18 +358,18 @@ struct StoreF32EpilogueT : PlainEpilogue {
 };
 using StoreF32Epilogue = StoreF32EpilogueT<kKTcGradW>;
 
-// AND of a predicate over the 128 epilogue threads (hardware barrier 2).
-__device__ __forceinline__ bool all_epilogue_threads(bool pred) {
+// AND of a predicate over the 128 threads of an epilogue group (hardware barrier `id`).
+__device__ __forceinline__ bool all_epilogue_threads(bool pred, int id = 2) {
   uint32_t out;
   asm volatile(
       "{\n"
       ".reg .pred p, q;\n"
       "setp.ne.u32 q, %1, 0;\n"
-      "bar.red.and.pred p, 2, 128, q;\n"
+      "bar.red.and.pred p, %2, 128, q;\n"
       "selp.u32 %0, 1, 0, p;\n"
       "}\n"
       : "=r"(out)
-      : "r"(static_cast<uint32_t>(pred))
+      : "r"(static_cast<uint32_t>(pred)), "r"(id)
       : "memory");
   return out != 0;
 }
@@ -596,7 +602,7 @@ gemm_tn_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       const bool no_product = zero_output || it.kb_begin == it.kb_end;   // nothing was multiplied: zeros
       if (MT == 1) epi.begin(ep, static_cast<long long>(item_row0) + row_in_tile);
       for (int nt = it.n_begin; nt < it.n_end && ok; ++nt) {
-        if constexpr (Epi::kPrefetch && MT == 1) epi.prefetch(ep, item_row0, nt * BN);
+        if constexpr (Epi::kPrefetch && MT == 1) epi.prefetch(ep, item_row0, nt * BN, BN);
         // the four epilogue warps share named barriers further down: they must agree on giving up
         if (!zero_output) {
           ok = all_epilogue_threads(A3PO_TIMED_WAIT(waited, mbar_wait(&tmem_full_bar[acc], acc_phase, abort_flag)));
@@ -695,8 +701,10 @@ constexpr int kPairStages = 6;
 constexpr uint32_t kPairStageBytes = kABytes + kBBytes / 2;   // per CTA: 128 x 64 of A, 128 x 64 of B
 constexpr size_t kPairSmemBytes = 1024 + kPairStages * kPairStageBytes + 2 * kSlabBytes + 256;
 
+template <class Epi> constexpr int pair_threads() { return 2 * kWarp + Epi::kGroups * 128; }
+
 template <class Epi, bool A_MN, bool B_MN>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads<Epi>(), 1)
 gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                  const __grid_constant__ CUtensorMap map_c, ItemMap im_static, int k_blocks_static,
                  typename Epi::Params ep, uint32_t* status) {
@@ -726,7 +734,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&tmem_full_bar[i], 1);
-      mbar_init(&tmem_empty_bar[i], 8);  // used in the leader only: four epilogue warps in each CTA
+      mbar_init(&tmem_empty_bar[i], 8 * Epi::kGroups);  // used in the leader only: the epilogue warps of both CTAs
     }
     *abort_flag = 0;
     fence_mbar_init();
@@ -864,31 +872,35 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     // ------------------------------------------------------------------ epilogue warps (both CTAs)
     const int quarter = warp & 3;
     const int row_in_tile = quarter * 32 + lane;
+    const int group = (warp - 2) / 4;
+    constexpr int kShare = (Epi::kGated ? BN / 2 : BN) / kEpiChunk / Epi::kGroups;   // 32-column chunks of a group
     const uint32_t leader_tmem_empty = map_to_cta(smem_u32(&tmem_empty_bar[0]), 0);
     int acc = 0;
     uint32_t acc_phase = 0;
     Epi epi;
     SlabStore st;
-    st.slab0 = smem_slabs;
+    st.slab0 = smem_slabs + group * kSlabBytes;   // two groups: one slab each
     st.slab1 = smem_slabs + kSlabBytes;
+    st.one_slab = Epi::kGroups > 1;
+    st.barrier_id = 1 + 2 * group;
     st.map = &map_c;
     st.row_in_tile = row_in_tile;
-    st.issuer = (threadIdx.x == 2 * kWarp);
+    st.issuer = (threadIdx.x == (2 + 4 * group) * kWarp);
     for (long long i = pair_id; i < im.items && ok; i += n_pairs) {
       const Item it = decode_item(im, i, k_blocks);
       const int tile_row0 = it.m_tile * kPairRows + static_cast<int>(rank) * BM;
       epi.begin(ep, static_cast<long long>(tile_row0) + row_in_tile);
       for (int nt = it.n_begin; nt < it.n_end && ok; ++nt) {
-        if constexpr (Epi::kPrefetch) epi.prefetch(ep, tile_row0, nt * BN);
+        if constexpr (Epi::kPrefetch) epi.prefetch(ep, tile_row0, nt * BN + group * kShare * kEpiChunk, kShare * kEpiChunk);
         if (!zero_output) {
-          ok = all_epilogue_threads(mbar_wait(&tmem_full_bar[acc], acc_phase, abort_flag));
+          ok = all_epilogue_threads(mbar_wait(&tmem_full_bar[acc], acc_phase, abort_flag), 2 + 2 * group);
           if (!ok) break;
           tcgen05_fence_after_sync();
         }
         const uint32_t taddr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(acc * BN);
         if constexpr (Epi::kGated) {
 #pragma unroll 1
-          for (int c = 0; c < BN / 2 / kEpiChunk; ++c) {
+          for (int c = group * kShare; c < (group + 1) * kShare; ++c) {
             uint32_t r[kEpiChunk], r2[kEpiChunk];
             tmem_ld_32x32(taddr + static_cast<uint32_t>(c * kEpiChunk), r);
             tmem_ld_32x32(taddr + static_cast<uint32_t>(BN / 2 + c * kEpiChunk), r2);
@@ -897,7 +909,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
           }
         } else {
 #pragma unroll 1
-          for (int c = 0; c < BN / kEpiChunk; ++c) {
+          for (int c = group * kShare; c < (group + 1) * kShare; ++c) {
             uint32_t r[kEpiChunk];
             if (!zero_output) {
               tmem_ld_32x32(taddr + static_cast<uint32_t>(c * kEpiChunk), r);
@@ -1071,7 +1083,7 @@ int pair_capacity() {
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(sm_count() / 2 * 2));
-    cfg.blockDim = dim3(kTcThreads);
+    cfg.blockDim = dim3(pair_threads<Epi>());
     cfg.dynamicSmemBytes = kPairSmemBytes;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
@@ -1128,7 +1140,7 @@ int launch_pair_gemm(const Operand& a, const Operand& b, int splits, const typen
   if (pairs > im.items) pairs = im.items;
   if (pairs < 1) return A3PO_OK;
   auto kernel = gemm_pair_kernel<Epi, A_MN, B_MN>;
-  A3PO_LAUNCH(Epi::kKernelId, stream, (launch_early(kernel, static_cast<unsigned>(2 * pairs), kTcThreads, kPairSmemBytes,
+  A3PO_LAUNCH(Epi::kKernelId, stream, (launch_early(kernel, static_cast<unsigned>(2 * pairs), pair_threads<Epi>(), kPairSmemBytes,
                                                     stream, 1, early, map_a, map_b, map_c, im, k_blocks, ep, status)));
   return after_launch();
 }
