@@ -506,32 +506,47 @@ def a3po_train_step_host(h_hidden, h_targets, h_behav_logp, h_versions, h_adv, h
 
 
 # ------------------------------------------------------------------------------ rows in front of the LM head
+def _here(*tensors):
+    """Every tensor is on the current CUDA device, whose stream the kernels are launched on."""
+    device = None
+    for t in tensors:
+        if t is not None:
+            if not t.is_cuda:
+                raise TypeError(f"expected a tensor on a CUDA device, got {t.device}")
+            if device is None:
+                device = torch.cuda.current_device()
+            if t.get_device() != device:
+                raise ValueError(f"expected tensors on the current device cuda:{device}, got {t.device}")
+
+
 def _rows(x, mats, vecs=(), per_row=(), row_mask=None):
     """dtype code, N and H of the row operators' matrices [N, H], parameters [H] and per-row scalars [N], after checking
-    that they belong together and that the kernels will run where the tensors are."""
-    dt = _dtype_code(x)
-    n, h = x.shape
-    if not x.is_cuda or x.get_device() != torch.cuda.current_device():
-        raise TypeError(f"x: expected a tensor on the current CUDA device, got {x.device}")
-    _want(x, x.dtype, "x")
+    that they belong together and that the kernels will run where the tensors are.  (Small calls are bound by the host:
+    the checks look at each tensor once and say what is wrong only when something is.)"""
+    dtype, shape, device = x.dtype, x.shape, x.get_device()
+    n, h = shape
+    fine = device >= 0 and device == torch.cuda.current_device() and x.is_contiguous()
     for t in mats:
         if t is not None:
-            if t.shape != x.shape:
-                raise ValueError("shape mismatch")
-            _want(t, x.dtype, "matrix")
+            fine &= t.dtype is dtype and t.get_device() == device and t.shape == shape and t.is_contiguous()
     for t in vecs:
-        if t is not None and t.numel() != h:
-            raise ValueError("shape mismatch")
+        if t is not None:
+            fine &= t.get_device() == device and t.numel() == h
     for t in per_row:
         if t is not None:
-            _want(t, torch.float32, "per-row scalar")
-            if t.numel() != n:
-                raise ValueError("shape mismatch")
+            fine &= t.dtype is torch.float32 and t.get_device() == device and t.numel() == n and t.is_contiguous()
     if row_mask is not None:
+        fine &= (row_mask.dtype is torch.uint8 and row_mask.get_device() == device and row_mask.numel() == n
+                 and row_mask.is_contiguous())
+    if not fine:
+        _here(x, *mats, *vecs, *per_row, row_mask)
+        for t in (x, *mats):
+            _want(t, dtype, "matrix")
+        for t in per_row:
+            _want(t, torch.float32, "per-row scalar")
         _want(row_mask, torch.uint8, "row_mask")
-        if row_mask.numel() != n:
-            raise ValueError("shape mismatch")
-    return dt, n, h
+        raise ValueError("shape mismatch")
+    return _dtype_code(x), n, h
 
 
 def _rng_words(rng, p):
@@ -540,6 +555,7 @@ def _rng_words(rng, p):
         if p > 0:
             raise ValueError("rng: {seed, offset} needed for p > 0")
         return
+    _here(rng)
     _want(rng, torch.int64, "rng")
     if rng.numel() != 2:
         raise ValueError("rng: expected the two words {seed, offset}")
@@ -554,7 +570,7 @@ def a3po_norm_fwd(x, gamma, y, rstd=None, *, kind=A3PO_NORM_RMS, beta=None, mean
     """y = norm(x) gamma + beta; mean / rstd (fp32 [N]) are left for the backward when given."""
     dt, n, h = _rows(x, (y,), (gamma, beta), (mean, rstd), row_mask)
     _want(gamma, x.dtype, "gamma"); _want(beta, x.dtype, "beta")
-    rc = load_library().a3po_norm_fwd(_ptr(x), _ptr(gamma), _ptr(beta), _ptr(row_mask), n, h, dt, kind, eps, _ptr(y),
+    rc = load_library().a3po_norm_fwd(_ptr(x), _ptr(gamma), _ptr(beta), _ptr(row_mask), n, h, dt, kind, float(eps), _ptr(y),
                                       _ptr(mean), _ptr(rstd), _stream(stream))
     _check("a3po_norm_fwd", rc)
 
@@ -563,7 +579,7 @@ def a3po_norm_bwd(x, gamma, rstd, grad_y, grad_x, grad_gamma, ws, *, kind=A3PO_N
                   accumulate_grad_w=False, row_mask=None, stream=None):
     dt, n, h = _rows(x, (grad_y, grad_x), (gamma, grad_gamma, grad_beta), (mean, rstd), row_mask)
     _want(gamma, x.dtype, "gamma"); _want(grad_gamma, torch.float32, "grad_gamma")
-    _want(grad_beta, torch.float32, "grad_beta"); _want(ws, torch.uint8, "ws")
+    _want(grad_beta, torch.float32, "grad_beta"); _want(ws, torch.uint8, "ws"); _here(ws)
     rc = load_library().a3po_norm_bwd(_ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(row_mask), _ptr(grad_y), n, h,
                                       dt, kind, _ptr(grad_x), _ptr(grad_gamma), _ptr(grad_beta),
                                       int(bool(accumulate_grad_w)), _ptr(ws), ws.numel(), _stream(stream))
@@ -574,7 +590,7 @@ def a3po_dropout_fwd(x, p, rng, y, *, residual=None, row_mask=None, stream=None)
     """y = residual + dropout(x); the mask is a function of rng = {seed, offset} and the element's place."""
     dt, n, h = _rows(x, (residual, y), row_mask=row_mask)
     _rng_words(rng, p)
-    rc = load_library().a3po_dropout_fwd(_ptr(x), _ptr(residual), _ptr(row_mask), n, h, dt, p, _ptr(rng), _ptr(y),
+    rc = load_library().a3po_dropout_fwd(_ptr(x), _ptr(residual), _ptr(row_mask), n, h, dt, float(p), _ptr(rng), _ptr(y),
                                          _stream(stream))
     _check("a3po_dropout_fwd", rc)
 
@@ -582,7 +598,7 @@ def a3po_dropout_fwd(x, p, rng, y, *, residual=None, row_mask=None, stream=None)
 def a3po_dropout_bwd(grad_y, p, rng, grad_x, *, row_mask=None, stream=None):
     dt, n, h = _rows(grad_y, (grad_x,), row_mask=row_mask)
     _rng_words(rng, p)
-    rc = load_library().a3po_dropout_bwd(_ptr(grad_y), _ptr(row_mask), n, h, dt, p, _ptr(rng), _ptr(grad_x),
+    rc = load_library().a3po_dropout_bwd(_ptr(grad_y), _ptr(row_mask), n, h, dt, float(p), _ptr(rng), _ptr(grad_x),
                                          _stream(stream))
     _check("a3po_dropout_bwd", rc)
 
@@ -592,8 +608,8 @@ def a3po_dropout_norm_fwd(x, residual, p, rng, gamma, r, y, rstd=None, *, kind=A
     """r = residual + dropout(x), y = norm(r) gamma + beta, in one pass."""
     dt, n, h = _rows(x, (residual, r, y), (gamma, beta), (mean, rstd), row_mask)
     _want(gamma, x.dtype, "gamma"); _want(beta, x.dtype, "beta"); _rng_words(rng, p)
-    rc = load_library().a3po_dropout_norm_fwd(_ptr(x), _ptr(residual), p, _ptr(rng), _ptr(gamma), _ptr(beta),
-                                              _ptr(row_mask), n, h, dt, kind, eps, _ptr(r), _ptr(y), _ptr(mean),
+    rc = load_library().a3po_dropout_norm_fwd(_ptr(x), _ptr(residual), float(p), _ptr(rng), _ptr(gamma), _ptr(beta),
+                                              _ptr(row_mask), n, h, dt, kind, float(eps), _ptr(r), _ptr(y), _ptr(mean),
                                               _ptr(rstd), _stream(stream))
     _check("a3po_dropout_norm_fwd", rc)
 
@@ -604,8 +620,8 @@ def a3po_dropout_norm_bwd(r, p, rng, gamma, rstd, grad_y, grad_residual, grad_x,
     """Gradients of the join from its stored sum r; grad_x = None: the branch's gradient is not wanted."""
     dt, n, h = _rows(r, (grad_y, grad_r, grad_residual, grad_x), (gamma, grad_gamma, grad_beta), (mean, rstd), row_mask)
     _want(gamma, r.dtype, "gamma"); _want(grad_gamma, torch.float32, "grad_gamma")
-    _want(grad_beta, torch.float32, "grad_beta"); _want(ws, torch.uint8, "ws"); _rng_words(rng, p)
-    rc = load_library().a3po_dropout_norm_bwd(_ptr(r), p, _ptr(rng), _ptr(gamma), _ptr(mean), _ptr(rstd),
+    _want(grad_beta, torch.float32, "grad_beta"); _want(ws, torch.uint8, "ws"); _here(ws); _rng_words(rng, p)
+    rc = load_library().a3po_dropout_norm_bwd(_ptr(r), float(p), _ptr(rng), _ptr(gamma), _ptr(mean), _ptr(rstd),
                                               _ptr(row_mask), _ptr(grad_y), _ptr(grad_r), n, h, dt, kind,
                                               _ptr(grad_residual), _ptr(grad_x), _ptr(grad_gamma), _ptr(grad_beta),
                                               int(bool(accumulate_grad_w)), _ptr(ws), ws.numel(), _stream(stream))
@@ -635,6 +651,7 @@ def a3po_gated_ffn_fwd(x, w_gate_up, w_down, y, ws, *, row_mask=None, kept=None,
     a3po_gated_ffn_kept_bytes) is filled for a3po_gated_ffn_bwd when given."""
     dt, n, h = _rows(x, (y,), row_mask=row_mask)
     f = _ffn_weights(x, w_gate_up, w_down, h)
+    _here(w_gate_up, w_down, kept, ws, status)
     _want(kept, torch.uint8, "kept"); _want(ws, torch.uint8, "ws"); _want(status, torch.int32, "status")
     rc = load_library().a3po_gated_ffn_fwd(_ptr(x), _ptr(w_gate_up), _ptr(w_down), _ptr(row_mask), n, h, f, dt, activation,
                                            _ptr(y), _ptr(kept), 0 if kept is None else kept.numel(), _ptr(ws), ws.numel(),
@@ -647,6 +664,7 @@ def a3po_gated_ffn_bwd(x, w_gate_up, w_down, kept, grad_y, grad_x, grad_w_gate_u
     """Gradients of a3po_gated_ffn_fwd from what it kept; the weight gradients are fp32 or of the weights' type."""
     dt, n, h = _rows(x, (grad_y, grad_x), row_mask=row_mask)
     f = _ffn_weights(x, w_gate_up, w_down, h)
+    _here(w_gate_up, w_down, kept, grad_w_gate_up, grad_w_down, ws, status)
     gdt = _dtype_code(grad_w_down)
     _want(grad_w_gate_up, grad_w_down.dtype, "grad_w_gate_up"); _want(grad_w_down, grad_w_down.dtype, "grad_w_down")
     _want(kept, torch.uint8, "kept"); _want(ws, torch.uint8, "ws"); _want(status, torch.int32, "status")

@@ -21,6 +21,7 @@ norm_bwd_kernel(const NormBwdArgs<T> a, int lanes, Turns turns) {
   constexpr int kSums = LAYER ? 2 : 1;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ __align__(16) float sums[4 * RowSum<WIDE>::kSlots];
+  allow_next();
   const RowThreads<WIDE> rt(lanes);
   const Columns<T, CPT, WIDE, VEC> cols(rt, a.h);
   RowSum<WIDE> row_sum(sums);
@@ -228,8 +229,9 @@ norm_bwd_kernel(const NormBwdArgs<T> a, int lanes, Turns turns) {
 // grad[c] (+)= sum over parts, in a fixed order: 32 threads per column take every 32nd part, then the 32 sums.
 constexpr int kReduceCols = 32, kReduceLanes = 32;
 __global__ void __launch_bounds__(kReduceCols* kReduceLanes)
-reduce_parts_kernel(const float* __restrict__ part, int parts, long long row_pitch, int h, int accumulate,
-                    float* __restrict__ grad_gamma, float* __restrict__ grad_beta) {
+reduce_parts_kernel(const float* part, int parts, long long row_pitch, int h, int accumulate,
+                    float* grad_gamma, float* grad_beta) {
+  wait_for_previous();
   const float* src = part + (blockIdx.y ? h : 0);
   float* dst = blockIdx.y ? grad_beta : grad_gamma;
   if (!dst) return;
@@ -392,9 +394,10 @@ int by_alignment(const NormBwdArgs<T>& a, float* grad_gamma, float* grad_beta, i
   A3PO_RETURN_IF((a.vec ? by_length<T, true, LAYER, JOIN>(a, &parts, stream)
                         : by_length<T, false, LAYER, JOIN>(a, &parts, stream)));
   const dim3 grid(static_cast<unsigned>((a.h + kReduceCols - 1) / kReduceCols), LAYER ? 2u : 1u);
-  A3PO_LAUNCH(kKNormBwd, stream, (reduce_parts_kernel<<<grid, dim3(kReduceCols, kReduceLanes), 0, stream>>>(
-                                     a.part, parts, static_cast<long long>(LAYER ? 2 : 1) * a.h, a.h, accumulate,
-                                     grad_gamma, grad_beta)));
+  A3PO_LAUNCH(kKNormBwd, stream, (launch_early(reduce_parts_kernel, grid, dim3(kReduceCols, kReduceLanes), 0, stream, 1,
+                                               true, static_cast<const float*>(a.part), parts,
+                                               static_cast<long long>(LAYER ? 2 : 1) * a.h, a.h, accumulate, grad_gamma,
+                                               grad_beta)));
   return after_launch();
 }
 template <typename T>

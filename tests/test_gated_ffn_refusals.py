@@ -57,5 +57,5 @@ def test_sizes():
 
 def test_binding_checks_shapes_and_types():
     x, wgu, wd = torch.zeros(4, 8), torch.zeros(32, 8), torch.zeros(8, 16)
-    with pytest.raises(TypeError, match="x"):
+    with pytest.raises(TypeError, match="CUDA device"):
         a3po.a3po_gated_ffn_fwd(x, wgu, wd, x, torch.zeros(256, dtype=torch.uint8))

@@ -69,7 +69,22 @@ def test_workspace_sizes():
 def test_binding_checks_shapes_and_types():
     """The Python layer refuses before the library is called (CPU tensors are refused too)."""
     x = torch.zeros(2, 8)
-    with pytest.raises(TypeError, match="x"):
+    with pytest.raises(TypeError, match="CUDA device"):
         a3po.a3po_norm_fwd(x, torch.ones(8), torch.zeros(2, 8))
     with pytest.raises(TypeError):
         a3po.a3po_dropout_fwd(x.half(), 0.1, None, x)
+
+
+def test_binding_refuses_tensors_of_another_device(monkeypatch):
+    """The kernels run on the current device's stream; a tensor elsewhere is refused (stand-ins: no GPU is needed)."""
+    from paper_2512_06547_b200 import binding
+
+    class Stand:
+        is_cuda = True
+        device = "cuda:1"
+        def __init__(self, index): self.index = index
+        def get_device(self): return self.index
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    binding._here(Stand(0), None, Stand(0))
+    with pytest.raises(ValueError, match="current device"):
+        binding._here(Stand(0), Stand(1))
