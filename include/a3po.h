@@ -461,7 +461,7 @@ int a3po_dropout_norm_bwd(const void* r, float p, const uint64_t* rng, const voi
  * Both projections, the activation and the product are one kernel; dh never reaches memory either.  Accumulation is
  * fp32; for bf16 the intermediates that enter a matrix product (h, dg, du) are rounded to bf16.
  *
- * row_mask uint8 [N] or NULL: rows with 0 are skipped (of more than 32 rows only the others are multiplied): nothing
+ * row_mask uint8 [N] or NULL: rows with 0 are skipped (of more than a few rows only the others are multiplied): nothing
  * of them is read, their y and grad_x are 0, they add nothing to a weight gradient.
  * kept: device buffer of a3po_gated_ffn_kept_bytes(N, F, dt) bytes, 256-byte aligned, that receives g, u and h for the
  * backward (layout private; about 8 N F bytes for bf16), or NULL when no backward follows.  The backward takes it with

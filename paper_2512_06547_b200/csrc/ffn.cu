@@ -44,7 +44,7 @@ bool lay_out(Arena& ar, long long n, int h, int f, a3po_dtype dt, bool masked, b
     else l->hid = ar.take<char>(rows * f * sizeof(float));
     return ar.ok();
   }
-  const bool few = n <= kFewRows;
+  const bool few = few_rows(n, h, f);
   const size_t cap = masked && !few ? static_cast<size_t>(compact_capacity(n)) : rows;
   if (masked && !few) {
     constexpr size_t kScan = 4096;   // block counts of the row index (compact_rows.cu)
@@ -116,7 +116,7 @@ int a3po_gated_ffn_fwd(const void* x, const void* w_gate_up, const void* w_down,
     return ffn_fwd_simt(x, w_gate_up, w_down, row_mask, N, H, F, dt, act, reinterpret_cast<float*>(l.hid), y, kept,
                         stream);
   if (kept) l.hid = static_cast<char*>(kept) + kept_gate_bytes(N, F);
-  if (N <= kFewRows) return ffn_few_rows_fwd(x, w_gate_up, w_down, row_mask, N, H, F, act, l.hid, y, kept, stream);
+  if (few_rows(N, H, F)) return ffn_few_rows_fwd(x, w_gate_up, w_down, row_mask, N, H, F, act, l.hid, y, kept, stream);
   if (!row_mask) {
     A3PO_RETURN_IF(ffn_gate_up_tc(x, w_gate_up, N, H, F, act, l.hid, kept, nullptr, status, stream));
     return ffn_down_tc(l.hid, w_down, N, H, F, y, l.parts, nullptr, status, stream);
@@ -160,7 +160,7 @@ int a3po_gated_ffn_bwd(const void* x, const void* w_gate_up, const void* w_down,
   void* gx = grad_x;
   long long rows = N;
   const int* count = nullptr;
-  const bool compact = row_mask && N > kFewRows;
+  const bool compact = row_mask && !few_rows(N, H, F);
   if (compact) {
     // the same index as the forward's: the kept values are in the compact row space
     A3PO_RETURN_IF(compact_index(nullptr, row_mask, nullptr, nullptr, N, l.cb, stream));

