@@ -178,10 +178,7 @@ norm_bwd_kernel(const NormBwdArgs<T> a, int lanes, Turns turns) {
           keep_bits(ph.draw(static_cast<uint32_t>(i * rt.tpr + rt.tid), t), a.drop.below, keep);
           rt.template own_bits<VEC>(keep);
 #pragma unroll
-          for (int j = 0; j < kPairs; ++j) {
-            const float2 d = parts(gy[i][j]);
-            gy[i][j] = mul2(f2(keep[2 * j] ? d.x : 0.f, keep[2 * j + 1] ? d.y : 0.f), f2(a.drop.scale));
-          }
+          for (int j = 0; j < kPairs; ++j) gy[i][j] = drop2(keep[2 * j], keep[2 * j + 1], gy[i][j], a.drop.scale);
         }
       }
       if (t < n) cols.write(a.grad_x + off, i, gy[i]);

@@ -108,10 +108,8 @@ norm_fwd_kernel(const NormFwdArgs<T> a, int lanes, Turns turns) {
           keep_bits(ph.draw(static_cast<uint32_t>(i * rt.tpr + rt.tid), t), a.drop.below, keep);
           rt.template own_bits<VEC>(keep);
 #pragma unroll
-          for (int j = 0; j < kPairs; ++j) {   // d(x) + residual, dropped elements selected away
-            const float2 x = parts(v[i][j]);
-            v[i][j] = fma2(f2(keep[2 * j] ? x.x : 0.f, keep[2 * j + 1] ? x.y : 0.f), f2(a.drop.scale), res[i][j]);
-          }
+          for (int j = 0; j < kPairs; ++j)
+            v[i][j] = add2(drop2(keep[2 * j], keep[2 * j + 1], v[i][j], a.drop.scale), res[i][j]);
         } else {
 #pragma unroll
           for (int j = 0; j < kPairs; ++j) v[i][j] = add2(v[i][j], res[i][j]);

@@ -79,9 +79,8 @@ dropout_vec_kernel(const T* __restrict__ x, const T* __restrict__ residual, cons
       keep_bits(ph.draw(group[i], static_cast<uint32_t>(row[i])), drop.below, keep);
 #pragma unroll
       for (int j = 0; j < kPairs; ++j) {
-        const float2 e = parts(a[j]);
-        const F2 kept = f2(keep[2 * j] ? e.x : 0.f, keep[2 * j + 1] ? e.y : 0.f);
-        a[j] = RES ? fma2(kept, f2(drop.scale), b[j]) : mul2(kept, f2(drop.scale));
+        a[j] = drop2(keep[2 * j], keep[2 * j + 1], a[j], drop.scale);
+        if (RES) a[j] = add2(a[j], b[j]);
       }
     } else if (RES) {
 #pragma unroll

@@ -64,9 +64,11 @@ __device__ __forceinline__ void keep_bits(const uint4& w, uint32_t below, bool (
     keep[2 * j + 1] = words[j] > below;
   }
 }
-// d(x) + add.  Dropped elements are selected away, not multiplied by 0 (x may be infinite).
+// d(x) + add.  Dropped elements are selected away, not multiplied by 0 (x may be infinite).  The product is rounded before the
+// sum: with a scale that fp32 cannot hold (4/3, say) a fused multiply-add would carry the scale's own error into sums that
+// are ties in bf16 for the exact scale, and round those the other way.
 __device__ __forceinline__ float drop_add(bool keep, float x, float scale, float add) {
-  return fmaf(keep ? x : 0.f, scale, add);
+  return __fadd_rn(__fmul_rn(keep ? x : 0.f, scale), add);
 }
 
 __device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
@@ -109,6 +111,11 @@ __device__ __forceinline__ F2 add2(F2 a, F2 b) {
   return r;
 }
 constexpr int kPairs = kVec / 2;   // a chunk's 8 columns as pairs
+// d(x) of a pair.  Scalar products: a paired one is contracted with a paired sum that follows it (see drop_add).
+__device__ __forceinline__ F2 drop2(bool keep_lo, bool keep_hi, F2 x, float scale) {
+  const float2 v = parts(x);
+  return f2(__fmul_rn(keep_lo ? v.x : 0.f, scale), __fmul_rn(keep_hi ? v.y : 0.f, scale));
+}
 
 // One 8-column chunk as it lies in memory: 16 bytes of bf16, 32 of fp32.
 template <typename T> struct Raw;

@@ -360,3 +360,19 @@ def test_many_rows():
     gamma = torch.ones(h, dtype=torch.bfloat16, device=DEV)
     a3po.a3po_norm_fwd(x, gamma, y, eps=0.0)
     assert bool((y[-2:] == 1.0).all()) and bool((y[:2] == 1.0).all())
+
+
+def test_ties_round_as_with_the_exact_scale():
+    """p = 1/4: the scale 4/3 is not an fp32 number, but x = 3 k and x * 4/3 + residual are exact, and half of these sums are
+    ties in bf16: they go to the even neighbour."""
+    n, h = 64, 512
+    gen = np.random.default_rng(2)
+    x = torch.from_numpy((3 * gen.integers(-40, 41, (n, h))).astype(np.float32)).bfloat16().to(DEV)
+    res = torch.from_numpy((gen.integers(-128, 128, (n, h)) * 4 + 1025).astype(np.float32)).bfloat16().to(DEV)
+    keep = torch.from_numpy(orc.dropout_factors(n, h, 0.25, SEED, OFFSET) != 0).to(DEV)
+    want = torch.where(keep, x.double() * 4 / 3, torch.zeros((), device=DEV, dtype=torch.double)) + res.double()
+    want = want.float().bfloat16()                       # exact sums of integers: one rounding, ties to even
+    r, y = torch.empty_like(x), torch.empty_like(x)
+    a3po.a3po_dropout_fwd(x, 0.25, rng_words(), y, residual=res)
+    a3po.a3po_dropout_norm_fwd(x, res, 0.25, rng_words(), torch.ones(h, dtype=torch.bfloat16, device=DEV), r, torch.empty_like(x))
+    assert torch.equal(y, want) and torch.equal(r, want)
