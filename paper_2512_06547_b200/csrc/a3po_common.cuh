@@ -65,7 +65,8 @@ inline int after_launch() {
 // Programmatic dependent launch.  A kernel started with launch_early may begin (its set-up, barriers, tensor memory, loads of
 // constant weights) while the kernel ahead of it in the stream still runs; wait_for_previous() returns once that one has
 // finished and its writes are visible, and comes before any access to memory that anything else writes.  Kernels that
-// call allow_next() let such a successor begin once all their blocks are running.  Both are no-ops otherwise.
+// call allow_next() let such a successor begin once all their blocks are running.  Both are no-ops otherwise.  The first
+// launch of a call is never early: what precedes it is somebody else's kernel, and the wait covers no more than that one.
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 template <typename... Params, typename... Args>

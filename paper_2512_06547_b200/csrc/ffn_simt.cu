@@ -2,7 +2,7 @@
 // tensor-core kernels reject (H or F not a multiple of 8).  64 x 64 x 32 tiles, 4 x 4 accumulators per thread (32 x 32 and
 // 2 x 2 for small outputs), K split over thread groups of a block; the same data flow as the tensor-core path with fp32
 // intermediates.  The precision path, bound by launches and latency at the sizes it is for: forward and backward of 512 rows,
-// H 64, F 192, fp32: 68 us (six launches).  Not tuned for large shapes.
+// H 64, F 192, fp32: 60 us (six launches).  Not tuned for large shapes.
 
 #include "ffn_internal.cuh"
 
@@ -174,6 +174,7 @@ __global__ void __launch_bounds__(kSimtThreads)
 simt_gate_up_kernel(Mat<T> x, Mat<T> wg, Mat<T> wu, long long n, int f, int gelu, float* __restrict__ hid,
                     float* __restrict__ kept) {
   constexpr int kTile = 16 * R;
+  allow_next();
   __shared__ float xs[kBK][kTile + 4], gs[kBK][kTile + 4], us[kBK][kTile + 4];
   const long long m0 = static_cast<long long>(blockIdx.x) * kTile;
   const int n0 = blockIdx.y * kTile;
@@ -220,8 +221,10 @@ simt_gate_up_kernel(Mat<T> x, Mat<T> wg, Mat<T> wu, long long n, int f, int gelu
 // C[m, c] (+)= sum_k A(m, k) B(c, k)
 template <typename TA, typename TB, typename TC, int R, int G>
 __global__ void __launch_bounds__(kSimtThreads* G)
-simt_gemm_kernel(Mat<TA> a, Mat<TB> b, TC* __restrict__ c, long long ldc, int accumulate) {
+simt_gemm_kernel(Mat<TA> a, Mat<TB> b, TC* c, long long ldc, int accumulate) {
   constexpr int kTile = 16 * R;
+  wait_for_previous();
+  allow_next();
   extern __shared__ __align__(16) uint8_t smem[];
   Tiles<R, G>& sh = *reinterpret_cast<Tiles<R, G>*>(smem);
   const long long m0 = static_cast<long long>(blockIdx.x) * kTile, n0 = static_cast<long long>(blockIdx.y) * kTile;
@@ -244,9 +247,10 @@ simt_gemm_kernel(Mat<TA> a, Mat<TB> b, TC* __restrict__ c, long long ldc, int ac
 // dh = dy Wd with the gradient of the gate in the epilogue: z[r][0..2][c] = dg, du, h
 template <typename T, int R, int G>
 __global__ void __launch_bounds__(kSimtThreads* G)
-simt_grad_gate_up_kernel(Mat<T> dy, Mat<T> wd, const float* __restrict__ kept, long long n, int f, int gelu,
-                         float* __restrict__ z) {
+simt_grad_gate_up_kernel(Mat<T> dy, Mat<T> wd, const float* kept, long long n, int f, int gelu, float* z) {
   constexpr int kTile = 16 * R;
+  wait_for_previous();
+  allow_next();
   extern __shared__ __align__(16) uint8_t smem[];
   Tiles<R, G>& sh = *reinterpret_cast<Tiles<R, G>*>(smem);
   const long long m0 = static_cast<long long>(blockIdx.x) * kTile;
@@ -285,22 +289,23 @@ Shape shape_of(long long m, long long c) {
   return blocks * 4 <= sms ? Shape::kSmall : blocks <= sms ? Shape::kSplit4 : blocks <= 2 * sms ? Shape::kSplit2
                                                                                                : Shape::kPlain;
 }
-// Launches a kernel whose shared memory is a Tiles<R, G> (64 x 64 tiles of four groups take 68 KB).
+// Launches a kernel whose shared memory is a Tiles<R, G> (64 x 64 tiles of four groups take 68 KB).  early: not
+// the first launch of a call, so that it may begin while its predecessor (one of the call's own) still runs.
 template <int R, int G, typename K, typename... Args>
-int launch_tiles(K kernel, dim3 grid, cudaStream_t s, Args... args) {
+int launch_tiles(K kernel, dim3 grid, bool early, cudaStream_t s, Args... args) {
   constexpr int kBytes = sizeof(Tiles<R, G>);
   if (kBytes > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) != cudaSuccess) {
     cudaGetLastError();
     return A3PO_ERR_CUDA;
   }
-  A3PO_LAUNCH(kKFfnSimt, s, (kernel<<<grid, kSimtThreads * G, kBytes, s>>>(args...)));
+  A3PO_LAUNCH(kKFfnSimt, s, (launch_early(kernel, grid, dim3(kSimtThreads * G), kBytes, s, 1, early, args...)));
   return after_launch();
 }
 
 template <typename TA, typename TB, typename TC>
 int gemm(const Mat<TA>& a, const Mat<TB>& b, TC* c, long long ldc, int accumulate, cudaStream_t s) {
 #define A3PO_GEMM(R, G)                                                                                              \
-  launch_tiles<R, G>(simt_gemm_kernel<TA, TB, TC, R, G>, tiles(a.m_dim, b.m_dim, 16 * R), s, a, b, c, ldc, accumulate)
+  launch_tiles<R, G>(simt_gemm_kernel<TA, TB, TC, R, G>, tiles(a.m_dim, b.m_dim, 16 * R), true, s, a, b, c, ldc, accumulate)
   switch (shape_of(a.m_dim, b.m_dim)) {
     case Shape::kSmall: return A3PO_GEMM(2, 4);
     case Shape::kSplit4: return A3PO_GEMM(4, 4);
@@ -331,7 +336,7 @@ int bwd_impl(const T* x, const T* wgu, const T* wd, const uint8_t* mask, const f
   const long long zf = 3ll * f;
   const Mat<T> dy{gy, h, 1, n, h, mask, true}, wdt{wd, 1, f, f, h, nullptr, false};
 #define A3PO_GRAD_GATE(R, G) \
-  launch_tiles<R, G>(simt_grad_gate_up_kernel<T, R, G>, tiles(n, f, 16 * R), s, dy, wdt, kept, n, f, gelu, z)
+  launch_tiles<R, G>(simt_grad_gate_up_kernel<T, R, G>, tiles(n, f, 16 * R), false, s, dy, wdt, kept, n, f, gelu, z)
   switch (shape_of(n, f)) {
     case Shape::kSmall: A3PO_RETURN_IF(A3PO_GRAD_GATE(2, 4)); break;
     case Shape::kSplit4: A3PO_RETURN_IF(A3PO_GRAD_GATE(4, 4)); break;
