@@ -394,8 +394,8 @@ int a3po_train_step_host(const void* h_hidden, const int32_t* h_targets, const f
  *
  * Common to all of them: matrices are row-major [N, H], contiguous, dtype `dt` (any H >= 1; pointers aligned to their
  * elements, 16-byte aligned rows move in 16-byte pieces); arithmetic, statistics and weight gradients are fp32 and
- * each stored element is rounded once.  row_mask uint8 [N] or NULL: of rows with 0 nothing is read (they may hold
- * NaN), their outputs (gradients included) are 0 and they add nothing to a weight gradient.  N <= 2^31 - 1.  Outputs
+ * each stored element is rounded once.  row_mask uint8 [N] or NULL: of rows with 0 nothing enters a result (they may
+ * hold NaN), their outputs (gradients included) are 0 and they add nothing to a weight gradient.  N <= 2^31 - 1.  Outputs
  * must not overlap inputs.  N = 0 launches nothing, apart from the zeros of a weight gradient that is not accumulated.
  *
  * Norm:       xhat = (x - mean) rstd,  rstd = 1 / sqrt(mean((x - mean)^2) + eps),  y = xhat gamma + beta
@@ -462,7 +462,8 @@ int a3po_dropout_norm_bwd(const void* r, float p, const uint64_t* rng, const voi
  * fp32; for bf16 the intermediates that enter a matrix product (h, dg, du) are rounded to bf16.
  *
  * row_mask uint8 [N] or NULL: rows with 0 are skipped (of more than a few rows only the others are multiplied): nothing
- * of them is read, their y and grad_x are 0, they add nothing to a weight gradient.
+ * of them enters a result (they may hold NaN); with finite weights their y and grad_x are 0 and they add nothing to a
+ * weight gradient.
  * kept: device buffer of a3po_gated_ffn_kept_bytes(N, F, dt) bytes, 256-byte aligned, that receives g, u and h for the
  * backward (layout private; about 8 N F bytes for bf16), or NULL when no backward follows.  The backward takes it with
  * the forward's x, weights, row_mask, N, H, F, dt and act; it is not changed, so the backward may be repeated.

@@ -180,8 +180,8 @@ int a3po_gated_ffn_bwd(const void* x, const void* w_gate_up, const void* w_down,
   A3PO_RETURN_IF(ffn_grad_gate_up_tc(gys, w_down, kept, rows, H, F, act, l.z, count, status, stream));
   A3PO_RETURN_IF(ffn_grad_x_tc(l.z, w_gate_up, rows, H, F, gx, l.parts, count, status, stream));
   if (compact) A3PO_RETURN_IF(scatter_rows(l.out_c, H, l.cb.pos, N, grad_x, stream));
-  return ffn_grad_w_tc(l.z, static_cast<const char*>(kept) + kept_gate_bytes(N, F), xs, gys, rows, H, F, grad_w_gate_up, grad_w_down, grad_w_dt, accumulate_grad_w, count, status,
-                       stream);
+  return ffn_grad_w_tc(l.z, static_cast<const char*>(kept) + kept_gate_bytes(N, F), xs, gys, rows, H, F, grad_w_gate_up,
+                       grad_w_down, grad_w_dt, accumulate_grad_w, count, status, stream);
 }
 
 }  // extern "C"

@@ -1,5 +1,6 @@
 // Gated feed-forward block for a few rows (single tokens and small batches while serving): the weights are read once
-// and used for at most kFewRows rows (few_rows() says when), so the bound is HBM, 2 bytes per weight, and everything serves the weight stream.
+// and used for at most kFewRows rows (few_rows() says when), so the bound is HBM, 2 bytes per weight, and everything
+// serves the weight stream.
 //
 // The weights come through per-lane rings in shared memory (cp.async, 48 KB in flight per block, four blocks per SM; loaded
 // straight to registers, 40 warps per SM kept too few bytes in flight: 3.1 TB/s) and go into mma.sync.m16n8k16 with

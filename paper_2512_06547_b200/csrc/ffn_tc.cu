@@ -245,12 +245,6 @@ template <class Epi, bool A_MN, bool B_MN>
 int contract(const Operand& a, const Operand& b, const typename Epi::Params& ep, const DynRows& dyn, uint32_t* status,
              cudaStream_t stream, bool early = true) {
   if (a.mn_extent <= BM) return launch_gemm<Epi, A_MN, B_MN, 1>(a, b, 0, ep, dyn, status, stream, 1, early);
-  const int forced = tuning_override("A3PO_FFN_TILE", 0);   // 1: single CTAs, 128 x 256; 2: single CTAs, 256 x 256
-  if (forced == 1 || (forced == 2 && (Epi::kGated || Epi::kPrefetch)))
-    return launch_gemm<Epi, A_MN, B_MN, 1>(a, b, 0, ep, dyn, status, stream, 1, true);
-  if constexpr (!Epi::kGated && !Epi::kPrefetch) {
-    if (forced == 2) return launch_gemm<Epi, A_MN, B_MN, 2>(a, b, 0, ep, dyn, status, stream);
-  }
   const int group = !A_MN && !B_MN ? fwd_group_m(a.k_extent, 2 * BM) : kGroupM;
   return launch_pair_gemm<Epi, A_MN, B_MN>(a, b, 0, ep, dyn, status, stream, group, true, early);
 }
@@ -297,8 +291,9 @@ int ffn_gate_up_tc(const void* x, const void* w_gate_up, long long n, int h, int
   __nv_bfloat16* o = static_cast<__nv_bfloat16*>(hid);
   uint8_t* k = static_cast<uint8_t*>(kept);
   const DynRows d = rows_as_m(dyn_rows, n);
-#define A3PO_GATE_UP(G, K)                                                                              \
-  contract<GateUpEpilogue<G, K>, false, false>(a, b, typename GateUpEpilogue<G, K>::Params{o, k, n, f}, d, status, stream, false)
+#define A3PO_GATE_UP(G, K)                                                                                        \
+  contract<GateUpEpilogue<G, K>, false, false>(a, b, typename GateUpEpilogue<G, K>::Params{o, k, n, f}, d, status, \
+                                               stream, false)
   if (act == A3PO_ACT_GELU_TANH) return kept ? A3PO_GATE_UP(true, true) : A3PO_GATE_UP(true, false);
   return kept ? A3PO_GATE_UP(false, true) : A3PO_GATE_UP(false, false);
 #undef A3PO_GATE_UP
@@ -344,9 +339,9 @@ int ffn_grad_x_tc(const void* z, const void* w_gate_up, long long n, int h, int 
                                      static_cast<__nv_bfloat16*>(grad_x), parts, dyn_rows, status, stream);
 }
 
-int ffn_grad_w_tc(const void* z, const void* hid_, const void* x, const void* grad_y, long long n, int h, int f, void* grad_w_gate_up,
-                  void* grad_w_down, a3po_dtype grad_dt, int accumulate, const int* dyn_rows, uint32_t* status,
-                  cudaStream_t stream) {
+int ffn_grad_w_tc(const void* z, const void* hid_, const void* x, const void* grad_y, long long n, int h, int f,
+                  void* grad_w_gate_up, void* grad_w_down, a3po_dtype grad_dt, int accumulate, const int* dyn_rows,
+                  uint32_t* status, cudaStream_t stream) {
   const Operand dgu{z, 2ll * f, n, 2ll * f}, xo{x, h, n, h};   // [dg | du]^T x
   const Operand dy{grad_y, h, n, h}, hid{hid_, f, n, f};       // dy^T h
   if (grad_dt == A3PO_F32) {

@@ -5,12 +5,13 @@ an accumulation of K fp32 products relative to sum |a b|, K 2^-24 for the FP32 p
 which may truncate where they align addends, K 2^-22.  With |act'| <= 1.13, |act''| <= 1 for both activations:
   Eg = c |x| |Wg|^T, Eu likewise;  Ea = 1.13 Eg + 2^-19 |a| (the approximate exponential and reciprocal)
   forward   Eh = Ea |u| + |a| Eu + e |h|;   Ey = (Eh + c |h|) |Wd|^T + e |y|
-  backward  works on stored g, u: Eg += e |g|, Eu += e |u|;  Es = Eg + 2^-19;  Edh = c |dy| |Wd|
+  backward  works on kept g, u, k = 2^-15 (24 of their bits, cut; fp32: e): Eg += k |g|, Eu += k |u|;  Es = Eg + 2^-19;
+            Edh = c |dy| |Wd|
             Edg = Edh |u s| + |dh| (Eu |s| + |u| Es) + e |dg|,   Edu = Edh |a| + |dh| Ea + e |du|
             products of these with exact matrices add up as absolute values, plus c of the last sum and e of the store
 Products of two errors are covered by a factor 1.05 (every relative error here is below 2 %).
 Besides that the 2-norm: independent roundings of at most e have an rms of at most e / sqrt(3) each; y has two of them
-(h, y), a gradient at most five (g through the slope and through a, u, the product, the store)."""
+(h, y), a gradient two (dg or du or h, the store) and, of kept g and u and the approximate functions, less than one more."""
 import math
 
 import numpy as np
@@ -68,7 +69,8 @@ class Case:
         ea = 1.13 * eg + 2.0 ** -19 * ab(a)
         eh = ea * ab(u) + ab(a) * eu + e * ab(hid)
         ey = (eh + f * unit * ab(hid)) @ ab(wd).T + e * ab(y)
-        eg, eu = eg + e * ab(g), eu + e * ab(u)
+        k = min(e, 2.0 ** -15)
+        eg, eu = eg + k * ab(g), eu + k * ab(u)
         ea, es = 1.13 * eg + 2.0 ** -19 * ab(a), eg + 2.0 ** -19
         edh = self.h * unit * (ab(gy) @ ab(wd))
         dg, du = dh * u * s, dh * a
@@ -127,9 +129,9 @@ def test_forward_and_backward(n, h, f, dt, masked, act):
                                 activation=ACT[act], status=c.status)
         G.check("gated_ffn_bwd")
         store = torch.finfo(gdt).eps / 2
-        check("grad_x", gx, *want["grad_x"], e, 5)
-        check("grad_w_gate_up", ggu, *want["grad_w_gate_up"], e, 5, store)
-        check("grad_w_down", gd, *want["grad_w_down"], e, 5, store)
+        check("grad_x", gx, *want["grad_x"], e, 3)
+        check("grad_w_gate_up", ggu, *want["grad_w_gate_up"], e, 3, store)
+        check("grad_w_down", gd, *want["grad_w_down"], e, 3, store)
         if gdt == torch.float32:
             before_gu, before_d = ggu.clone(), gd.clone()
             a3po.a3po_gated_ffn_bwd(c.x, c.wgu, c.wd, kept, c.gy, gx, ggu, gd, c.ws(True), row_mask=c.mask,
