@@ -32,6 +32,7 @@ __device__ __forceinline__ bool keep_row(const uint8_t* row_mask, const float* g
 __global__ void __launch_bounds__(kCompactThreads)
 compact_count_kernel(const uint8_t* __restrict__ row_mask, const float* __restrict__ g, long long n,
                      long long rows_per_block, int* __restrict__ block_counts) {
+  allow_next();
   const long long lo = static_cast<long long>(blockIdx.x) * rows_per_block;
   const long long hi = (lo + rows_per_block < n) ? lo + rows_per_block : n;
   int c = 0;
@@ -49,8 +50,10 @@ compact_count_kernel(const uint8_t* __restrict__ row_mask, const float* __restri
 
 // One block: exclusive scan of up to kMaxCompactBlocks counts.
 __global__ void __launch_bounds__(1024)
-compact_offsets_kernel(const int* __restrict__ block_counts, int blocks, int* __restrict__ block_offsets,
+compact_offsets_kernel(const int* block_counts, int blocks, int* __restrict__ block_offsets,
                        int* __restrict__ count) {
+  wait_for_previous();
+  allow_next();
   __shared__ int sh[1024];
   constexpr int kPer = kMaxCompactBlocks / 1024;
   int local[kPer];
@@ -82,9 +85,11 @@ compact_offsets_kernel(const int* __restrict__ block_counts, int blocks, int* __
 __global__ void __launch_bounds__(kCompactThreads)
 compact_fill_kernel(const uint8_t* __restrict__ row_mask, const float* __restrict__ g,
                     const int32_t* __restrict__ targets, const float* __restrict__ lse, long long n, long long cap,
-                    long long rows_per_block, const int* __restrict__ block_offsets, const int* __restrict__ count,
+                    long long rows_per_block, const int* block_offsets, const int* count,
                     int* __restrict__ pos, int* __restrict__ idx, int32_t* __restrict__ targets_c,
                     float* __restrict__ lse_c, float* __restrict__ g_c) {
+  wait_for_previous();
+  allow_next();
   const long long lo = static_cast<long long>(blockIdx.x) * rows_per_block;
   const long long hi = (lo + rows_per_block < n) ? lo + rows_per_block : n;
   __shared__ int warp_base[kCompactThreads / kWarp];
@@ -128,11 +133,13 @@ compact_fill_kernel(const uint8_t* __restrict__ row_mask, const float* __restric
 }
 
 // One warp per compact row; rows in [count, round_up(count, 128)) are written as zeros so that
-// partial tiles of the GEMMs see finite data.
+// partial tiles of the GEMMs see finite data.  beside: launched early behind another gather of the same index, which it
+// waits for at its end only (see Begin in gemm_tc.cuh).
 __global__ void __launch_bounds__(kCompactThreads)
-gather_rows_kernel(const __nv_bfloat16* __restrict__ hidden, int h, const int* __restrict__ idx,
-                   const int* __restrict__ count, long long offset, long long rows,
-                   __nv_bfloat16* __restrict__ dst) {
+gather_rows_kernel(const __nv_bfloat16* __restrict__ hidden, int h, const int* idx, const int* count, long long offset,
+                   long long rows, __nv_bfloat16* __restrict__ dst, int beside) {
+  if (!beside) wait_for_previous();
+  allow_next();
   long long kept = static_cast<long long>(*count) - offset;   // kept rows inside [offset, offset + rows)
   kept = kept < 0 ? 0 : (kept > rows ? rows : kept);
   long long fill_to = (kept + 127) / 128 * 128;
@@ -150,11 +157,12 @@ gather_rows_kernel(const __nv_bfloat16* __restrict__ hidden, int h, const int* _
       for (int j = lane; j < vec_per_row; j += kWarp) out[j] = make_uint4(0u, 0u, 0u, 0u);
     }
   }
+  if (beside) wait_for_previous();
 }
 
 __global__ void __launch_bounds__(kCompactThreads)
-scatter_rows_kernel(const __nv_bfloat16* __restrict__ src_c, int h, const int* __restrict__ pos, long long n,
-                    __nv_bfloat16* __restrict__ dst) {
+scatter_rows_kernel(const __nv_bfloat16* src_c, int h, const int* pos, long long n, __nv_bfloat16* __restrict__ dst) {
+  wait_for_previous();
   const int lane = threadIdx.x % kWarp;
   const long long warps = static_cast<long long>(gridDim.x) * (kCompactThreads / kWarp);
   const int vec_per_row = h / 8;
@@ -221,41 +229,41 @@ int compact_index(const int32_t* targets, const uint8_t* row_mask, const float* 
   A3PO_LAUNCH(kKCompact, stream, (compact_count_kernel<<<blocks, kCompactThreads, 0, stream>>>(
                                      row_mask, g, n, rows_per_block, cb.block_counts)));
   A3PO_RETURN_IF(after_launch());
-  A3PO_LAUNCH(kKCompact, stream, (compact_offsets_kernel<<<1, 1024, 0, stream>>>(cb.block_counts, blocks,
-                                                                                 cb.block_offsets, cb.count)));
+  A3PO_LAUNCH(kKCompact, stream, (launch_early(compact_offsets_kernel, 1, 1024, 0, stream, 1, true, cb.block_counts,
+                                               blocks, cb.block_offsets, cb.count)));
   A3PO_RETURN_IF(after_launch());
-  A3PO_LAUNCH(kKCompact, stream, (compact_fill_kernel<<<blocks, kCompactThreads, 0, stream>>>(
-                                     row_mask, g, targets, lse, n, cb.cap, rows_per_block, cb.block_offsets, cb.count,
-                                     cb.pos, cb.idx, cb.targets_c, cb.lse_c, cb.g_c)));
+  A3PO_LAUNCH(kKCompact, stream, (launch_early(compact_fill_kernel, blocks, kCompactThreads, 0, stream, 1, true,
+                                               row_mask, g, targets, lse, n, cb.cap, rows_per_block, cb.block_offsets,
+                                               cb.count, cb.pos, cb.idx, cb.targets_c, cb.lse_c, cb.g_c)));
   return after_launch();
 }
 
 int gather_rows_range(const void* hidden, int h, const int* idx, const int* count, long long offset, long long rows,
-                      void* dst, cudaStream_t stream) {
+                      void* dst, cudaStream_t stream, bool early, bool beside) {
   if (rows <= 0) return A3PO_OK;
   int gather_blocks = sm_count() * 8;
   const long long want = (rows + 7) / 8;
   if (gather_blocks > want) gather_blocks = static_cast<int>(want);
-  A3PO_LAUNCH(kKCompact, stream, (gather_rows_kernel<<<gather_blocks, kCompactThreads, 0, stream>>>(
-                                     static_cast<const __nv_bfloat16*>(hidden), h, idx, count, offset, rows,
-                                     static_cast<__nv_bfloat16*>(dst))));
+  A3PO_LAUNCH(kKCompact, stream, (launch_early(gather_rows_kernel, gather_blocks, kCompactThreads, 0, stream, 1, early,
+                                               static_cast<const __nv_bfloat16*>(hidden), h, idx, count, offset, rows,
+                                               static_cast<__nv_bfloat16*>(dst), beside ? 1 : 0)));
   return after_launch();
 }
 
 int compact_rows(const void* hidden, int h, const int32_t* targets, const uint8_t* row_mask, const float* g,
                  const float* lse, long long n, const CompactBuffers& cb, cudaStream_t stream) {
   A3PO_RETURN_IF(compact_index(targets, row_mask, g, lse, n, cb, stream));
-  return gather_rows_range(hidden, h, cb.idx, cb.count, 0, cb.cap, cb.hidden_c, stream);
+  return gather_rows_range(hidden, h, cb.idx, cb.count, 0, cb.cap, cb.hidden_c, stream, true);
 }
 
-int scatter_rows(const void* src_c, int h, const int* pos, long long n, void* dst, cudaStream_t stream) {
+int scatter_rows(const void* src_c, int h, const int* pos, long long n, void* dst, cudaStream_t stream, bool early) {
   int blocks = sm_count() * 8;
   const long long want = (n + 7) / 8;
   if (blocks > want) blocks = static_cast<int>(want);
   if (blocks < 1) return A3PO_OK;
-  A3PO_LAUNCH(kKCompact, stream, (scatter_rows_kernel<<<blocks, kCompactThreads, 0, stream>>>(
-                                     static_cast<const __nv_bfloat16*>(src_c), h, pos, n,
-                                     static_cast<__nv_bfloat16*>(dst))));
+  A3PO_LAUNCH(kKCompact, stream, (launch_early(scatter_rows_kernel, blocks, kCompactThreads, 0, stream, 1, early,
+                                               static_cast<const __nv_bfloat16*>(src_c), h, pos, n,
+                                               static_cast<__nv_bfloat16*>(dst))));
   return after_launch();
 }
 

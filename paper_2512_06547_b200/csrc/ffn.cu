@@ -122,10 +122,10 @@ int a3po_gated_ffn_fwd(const void* x, const void* w_gate_up, const void* w_down,
     return ffn_down_tc(l.hid, w_down, N, H, F, y, l.parts, nullptr, status, stream);
   }
   A3PO_RETURN_IF(compact_index(nullptr, row_mask, nullptr, nullptr, N, l.cb, stream));
-  A3PO_RETURN_IF(gather_rows_range(x, H, l.cb.idx, l.cb.count, 0, l.cb.cap, l.x_c, stream));
+  A3PO_RETURN_IF(gather_rows_range(x, H, l.cb.idx, l.cb.count, 0, l.cb.cap, l.x_c, stream, true));
   A3PO_RETURN_IF(ffn_gate_up_tc(l.x_c, w_gate_up, l.cb.cap, H, F, act, l.hid, kept, l.cb.count, status, stream));
   A3PO_RETURN_IF(ffn_down_tc(l.hid, w_down, l.cb.cap, H, F, l.out_c, l.parts, l.cb.count, status, stream));
-  return scatter_rows(l.out_c, H, l.cb.pos, N, y, stream);
+  return scatter_rows(l.out_c, H, l.cb.pos, N, y, stream, true);
 }
 
 int a3po_gated_ffn_bwd(const void* x, const void* w_gate_up, const void* w_down, const uint8_t* row_mask,
@@ -164,8 +164,8 @@ int a3po_gated_ffn_bwd(const void* x, const void* w_gate_up, const void* w_down,
   if (compact) {
     // the same index as the forward's: the kept values are in the compact row space
     A3PO_RETURN_IF(compact_index(nullptr, row_mask, nullptr, nullptr, N, l.cb, stream));
-    A3PO_RETURN_IF(gather_rows_range(x, H, l.cb.idx, l.cb.count, 0, l.cb.cap, l.x_c, stream));
-    A3PO_RETURN_IF(gather_rows_range(grad_y, H, l.cb.idx, l.cb.count, 0, l.cb.cap, l.gy_c, stream));
+    A3PO_RETURN_IF(gather_rows_range(x, H, l.cb.idx, l.cb.count, 0, l.cb.cap, l.x_c, stream, true));
+    A3PO_RETURN_IF(gather_rows_range(grad_y, H, l.cb.idx, l.cb.count, 0, l.cb.cap, l.gy_c, stream, true, true));
     rows = l.cb.cap;
     count = l.cb.count;
     gx = l.out_c;
@@ -178,10 +178,12 @@ int a3po_gated_ffn_bwd(const void* x, const void* w_gate_up, const void* w_down,
     gys = l.gy_c;
   }
   A3PO_RETURN_IF(ffn_grad_gate_up_tc(gys, w_down, kept, rows, H, F, act, l.z, count, status, stream));
+  // Three products that read z, x, grad_y and h and write apart: each begins on the SMs that the last wave of the one
+  // before leaves idle.  Backward of 16,384 rows (62 % valid), 1536 x 4608: 821 -> 769 us with the compaction's early launches.
+  A3PO_RETURN_IF(ffn_grad_w_tc(l.z, static_cast<const char*>(kept) + kept_gate_bytes(N, F), xs, gys, rows, H, F, grad_w_gate_up,
+                               grad_w_down, grad_w_dt, accumulate_grad_w, count, status, stream));
   A3PO_RETURN_IF(ffn_grad_x_tc(l.z, w_gate_up, rows, H, F, gx, l.parts, count, status, stream));
-  if (compact) A3PO_RETURN_IF(scatter_rows(l.out_c, H, l.cb.pos, N, grad_x, stream));
-  return ffn_grad_w_tc(l.z, static_cast<const char*>(kept) + kept_gate_bytes(N, F), xs, gys, rows, H, F, grad_w_gate_up,
-                       grad_w_down, grad_w_dt, accumulate_grad_w, count, status, stream);
+  return compact ? scatter_rows(l.out_c, H, l.cb.pos, N, grad_x, stream, true) : A3PO_OK;
 }
 
 }  // extern "C"

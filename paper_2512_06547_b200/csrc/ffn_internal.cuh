@@ -69,12 +69,13 @@ int ffn_down_tc(const void* hid, const void* w_down, long long n, int h, int f, 
 // z[n][2][f] = dg | du from dy and the kept values.
 int ffn_grad_gate_up_tc(const void* grad_y, const void* w_down, const void* kept, long long n, int h, int f,
                         a3po_activation act, void* z, const int* dyn_rows, uint32_t* status, cudaStream_t stream);
-int ffn_grad_x_tc(const void* z, const void* w_gate_up, long long n, int h, int f, void* grad_x, float* parts,
-                  const int* dyn_rows, uint32_t* status, cudaStream_t stream);
 // grad_w[2 f, h] = [dg | du]^T x and grad_w_down[h, f] = dy^T h.
 int ffn_grad_w_tc(const void* z, const void* hid, const void* x, const void* grad_y, long long n, int h, int f, void* grad_w_gate_up,
                   void* grad_w_down, a3po_dtype grad_dt, int accumulate, const int* dyn_rows, uint32_t* status,
                   cudaStream_t stream);
+// grad_x[n, h] = [dg | du] w_gate_up.  Launched right behind ffn_grad_w_tc, beside which it may run.
+int ffn_grad_x_tc(const void* z, const void* w_gate_up, long long n, int h, int f, void* grad_x, float* parts,
+                  const int* dyn_rows, uint32_t* status, cudaStream_t stream);
 
 // ---- few rows (ffn_few.cu): bf16, same shapes; masked rows are read as zeros ----
 // Up to 16 rows always; up to 32 (two row tiles, twice the traffic of x out of L2) while the weights are small enough that

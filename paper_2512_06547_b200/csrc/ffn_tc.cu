@@ -232,6 +232,9 @@ add_parts_kernel(const float* parts, int n_parts, long long part_stride, long lo
   }
 }
 
+// The first contraction of a call is its first launch unless the rows were compacted before.
+Begin first_launch(const int* dyn_rows) { return dyn_rows ? Begin::kEarly : Begin::kAfter; }
+
 DynRows rows_as_m(const int* dyn_rows, long long n) {
   DynRows d;
   d.rows = dyn_rows;
@@ -239,21 +242,27 @@ DynRows rows_as_m(const int* dyn_rows, long long n) {
   return d;
 }
 
-// One contraction: pairs of CTAs on 256 x 256 tiles, or single CTAs when the output has at most 128 rows.  early: not
-// the first launch of a call, so that it may begin while its predecessor (one of this call's own) still runs.
+// Launches of fewer waves of tiles than this run unpaced: there is no time to drift apart, and a CTA that begins a tile later
+// than the others (see Begin::kBeside) would be waited for (backward of 16,384 rows of 1536 x 4608, 1 to 6 waves a launch:
+// 1,177 us paced, 1,144 unpaced; of 4096 x 12288, 10 to 21 waves, no difference between the two).
+constexpr int kPacedWaves = 8;
+
+// One contraction: pairs of CTAs on 256 x 256 tiles, or single CTAs when the output has at most 128 rows.
 template <class Epi, bool A_MN, bool B_MN>
 int contract(const Operand& a, const Operand& b, const typename Epi::Params& ep, const DynRows& dyn, uint32_t* status,
-             cudaStream_t stream, bool early = true) {
-  if (a.mn_extent <= BM) return launch_gemm<Epi, A_MN, B_MN, 1>(a, b, 0, ep, dyn, status, stream, 1, early);
+             cudaStream_t stream, Begin begin) {
+  if (a.mn_extent <= BM) return launch_gemm<Epi, A_MN, B_MN, 1>(a, b, 0, ep, dyn, status, stream, 1, begin);
   const int group = !A_MN && !B_MN ? fwd_group_m(a.k_extent, 2 * BM) : kGroupM;
-  return launch_pair_gemm<Epi, A_MN, B_MN>(a, b, 0, ep, dyn, status, stream, group, true, early);
+  const long long tiles = ((a.mn_extent + 2 * BM - 1) / (2 * BM)) * ((b.mn_extent + BN - 1) / BN);
+  const bool paced = 2 * tiles >= kPacedWaves * sm_count();
+  return launch_pair_gemm<Epi, A_MN, B_MN>(a, b, 0, ep, dyn, status, stream, group, paced, begin);
 }
 
 // Rows and columns of the output are the token rows and h: a contraction over a long K with, for few tokens, far fewer
 // output tiles than SMs.
 template <int ID, bool B_MN>
 int rows_gemm(const Operand& a, const Operand& b, __nv_bfloat16* out, float* parts, const int* dyn_rows,
-              uint32_t* status, cudaStream_t stream) {
+              uint32_t* status, cudaStream_t stream, Begin begin) {
   const long long n = a.mn_extent;
   const int cols = static_cast<int>(b.mn_extent);
   const int k_parts = parts ? ffn_k_parts(n, cols, static_cast<int>(a.k_extent)) : 1;
@@ -261,7 +270,7 @@ int rows_gemm(const Operand& a, const Operand& b, __nv_bfloat16* out, float* par
     const long long rows_pad = (n + BM - 1) / BM * BM;
     typename StoreF32EpilogueT<ID>::Params ep{parts, cols, rows_pad * k_parts, cols, 0};
     A3PO_RETURN_IF((launch_gemm<StoreF32EpilogueT<ID>, false, B_MN, 1>(a, b, 0, ep, rows_as_m(dyn_rows, n), status,
-                                                                      stream, k_parts, true)));
+                                                                      stream, k_parts, begin)));
     const long long want = (n * (cols / 8) + 255) / 256;
     const int blocks = static_cast<int>(want < sm_count() * 8ll ? want : sm_count() * 8ll);
     A3PO_LAUNCH(ID, stream, (launch_early(add_parts_kernel, blocks, 256, 0, stream, 1, true,
@@ -270,17 +279,17 @@ int rows_gemm(const Operand& a, const Operand& b, __nv_bfloat16* out, float* par
     return after_launch();
   }
   typename StoreBf16EpilogueT<ID>::Params ep{out, cols, n, cols, nullptr};
-  return contract<StoreBf16EpilogueT<ID>, false, B_MN>(a, b, ep, rows_as_m(dyn_rows, n), status, stream);
+  return contract<StoreBf16EpilogueT<ID>, false, B_MN>(a, b, ep, rows_as_m(dyn_rows, n), status, stream, begin);
 }
 
 // Weight gradient C[m, c] = A^T B over the token rows (both operands read with the token index as K).
 template <class Epi>
 int weight_gemm(const Operand& a, const Operand& b, const typename Epi::Params& ep, int accumulate,
-                const int* dyn_rows, uint32_t* status, cudaStream_t stream) {
+                const int* dyn_rows, uint32_t* status, cudaStream_t stream, Begin begin) {
   DynRows d = rows_as_m(dyn_rows, a.k_extent);
   d.is_k = 1;
   d.zero_when_empty = accumulate ? 0 : 1;
-  return contract<Epi, true, true>(a, b, ep, d, status, stream);
+  return contract<Epi, true, true>(a, b, ep, d, status, stream, begin);
 }
 
 }  // namespace
@@ -293,7 +302,7 @@ int ffn_gate_up_tc(const void* x, const void* w_gate_up, long long n, int h, int
   const DynRows d = rows_as_m(dyn_rows, n);
 #define A3PO_GATE_UP(G, K)                                                                                        \
   contract<GateUpEpilogue<G, K>, false, false>(a, b, typename GateUpEpilogue<G, K>::Params{o, k, n, f}, d, status, \
-                                               stream, false)
+                                               stream, first_launch(dyn_rows))
   if (act == A3PO_ACT_GELU_TANH) return kept ? A3PO_GATE_UP(true, true) : A3PO_GATE_UP(true, false);
   return kept ? A3PO_GATE_UP(false, true) : A3PO_GATE_UP(false, false);
 #undef A3PO_GATE_UP
@@ -317,7 +326,7 @@ size_t ffn_parts_bytes(long long n, int cols, int k) {
 int ffn_down_tc(const void* hid, const void* w_down, long long n, int h, int f, void* y, float* parts,
                 const int* dyn_rows, uint32_t* status, cudaStream_t stream) {
   return rows_gemm<kKFfnDown, false>(Operand{hid, n, f, f}, Operand{w_down, h, f, f}, static_cast<__nv_bfloat16*>(y),
-                                     parts, dyn_rows, status, stream);
+                                     parts, dyn_rows, status, stream, Begin::kEarly);
 }
 
 int ffn_grad_gate_up_tc(const void* grad_y, const void* w_down, const void* kept, long long n, int h, int f,
@@ -328,15 +337,15 @@ int ffn_grad_gate_up_tc(const void* grad_y, const void* w_down, const void* kept
   __nv_bfloat16* o = static_cast<__nv_bfloat16*>(z);
   if (act == A3PO_ACT_GELU_TANH)
     return contract<GradGateUpEpilogue<true>, false, true>(a, b, GradGateUpEpilogue<true>::Params{k, o, n, f}, d, status,
-                                                           stream, false);
+                                                           stream, first_launch(dyn_rows));
   return contract<GradGateUpEpilogue<false>, false, true>(a, b, GradGateUpEpilogue<false>::Params{k, o, n, f}, d, status,
-                                                          stream, false);
+                                                          stream, first_launch(dyn_rows));
 }
 
 int ffn_grad_x_tc(const void* z, const void* w_gate_up, long long n, int h, int f, void* grad_x, float* parts,
                   const int* dyn_rows, uint32_t* status, cudaStream_t stream) {
   return rows_gemm<kKFfnGradX, true>(Operand{z, n, 2ll * f, 2ll * f}, Operand{w_gate_up, h, 2ll * f, h},
-                                     static_cast<__nv_bfloat16*>(grad_x), parts, dyn_rows, status, stream);
+                                     static_cast<__nv_bfloat16*>(grad_x), parts, dyn_rows, status, stream, Begin::kBeside);
 }
 
 int ffn_grad_w_tc(const void* z, const void* hid_, const void* x, const void* grad_y, long long n, int h, int f,
@@ -347,15 +356,15 @@ int ffn_grad_w_tc(const void* z, const void* hid_, const void* x, const void* gr
   if (grad_dt == A3PO_F32) {
     using Epi = StoreF32EpilogueT<kKFfnGradW>;
     A3PO_RETURN_IF((weight_gemm<Epi>(dgu, xo, Epi::Params{static_cast<float*>(grad_w_gate_up), h, 2ll * f, h, accumulate},
-                                     accumulate, dyn_rows, status, stream)));
+                                     accumulate, dyn_rows, status, stream, Begin::kEarly)));
     return weight_gemm<Epi>(dy, hid, Epi::Params{static_cast<float*>(grad_w_down), f, h, f, accumulate}, accumulate,
-                            dyn_rows, status, stream);
+                            dyn_rows, status, stream, Begin::kBeside);
   }
   using Epi = StoreBf16EpilogueT<kKFfnGradW>;
   A3PO_RETURN_IF((weight_gemm<Epi>(dgu, xo, Epi::Params{static_cast<__nv_bfloat16*>(grad_w_gate_up), h, 2ll * f, h, nullptr},
-                                   0, dyn_rows, status, stream)));
+                                   0, dyn_rows, status, stream, Begin::kEarly)));
   return weight_gemm<Epi>(dy, hid, Epi::Params{static_cast<__nv_bfloat16*>(grad_w_down), f, h, f, nullptr}, 0, dyn_rows,
-                          status, stream);
+                          status, stream, Begin::kBeside);
 }
 
 }  // namespace a3po

@@ -78,7 +78,18 @@ struct ItemMap {
   // stored s * k_split_rows rows further down, and the caller adds the parts up.
   int k_splits;
   long long k_split_rows;
+  int beside;   // see Begin::kBeside
 };
+
+// When a launch may begin, relative to the one ahead of it in the stream.
+//   kAfter   once that one has finished
+//   kEarly   while it runs, up to the point where its results are needed (see launch_early)
+//   kBeside  the same, but its results are never needed: the two share inputs only, and both are launches of one call.  The
+//            CTAs take their first tiles on the SMs that the last wave of the launch ahead leaves idle, and wait for it
+//            at their end instead, so that whoever waits for this launch has waited for both.
+// A kBeside launch follows one that waits for its own predecessor before it allows a successor (or another kBeside launch
+// behind such a one): when it begins, everything that both read is there.
+enum class Begin { kAfter, kEarly, kBeside };
 
 struct Item {
   int m_tile;
@@ -457,7 +468,7 @@ gemm_tn_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   __syncthreads();
   tcgen05_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
-  wait_for_previous();
+  if (!im_static.beside) wait_for_previous();
   allow_next();
 
   // Work extents: static, or derived from the device-resident row count (identical in every thread).
@@ -671,6 +682,7 @@ gemm_tn_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     tcgen05_fence_after_sync();
     tmem_dealloc(tmem_base, kTmemCols);
   }
+  if (im_static.beside) wait_for_previous();
 #ifdef A3PO_TUNING
   if (threadIdx.x == 0 && g_trace != nullptr) {
     const unsigned int slot = atomicAdd(&g_trace_next, 1u);
@@ -752,7 +764,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
   cluster_sync_all();   // the peer's barriers exist before anything signals them
   tcgen05_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
-  wait_for_previous();
+  if (!im_static.beside) wait_for_previous();
   allow_next();
 
   ItemMap im = im_static;   // m_tiles counts 256-row pair tiles here
@@ -947,6 +959,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     tcgen05_fence_after_sync();
     tmem_dealloc_pair(tmem_base, kTmemCols);
   }
+  if (im_static.beside) wait_for_previous();
 }
 
 // ------------------------------------------------------------------------------------ host side
@@ -1014,10 +1027,10 @@ struct DynRows {
   int select_value = 0;
 };
 
-// C[M, N] = sum_k A[m, k] B[n, k];  splits = 0 means one column tile per work item.  early: see launch_early.
+// C[M, N] = sum_k A[m, k] B[n, k];  splits = 0 means one column tile per work item.
 template <class Epi, bool A_MN, bool B_MN, int MT = 1>
 int launch_gemm(const Operand& a, const Operand& b, int splits, const typename Epi::Params& ep, const DynRows& dyn,
-                uint32_t* status, cudaStream_t stream, int k_splits = 1, bool early = false) {
+                uint32_t* status, cudaStream_t stream, int k_splits = 1, Begin begin = Begin::kAfter) {
   constexpr size_t kSmemBytes = TileCfg<MT>::kSmemBytes;
   CUtensorMap map_a, map_b, map_c;
   A3PO_RETURN_IF(make_map(&map_a, a, A_MN, BM * MT));
@@ -1035,6 +1048,7 @@ int launch_gemm(const Operand& a, const Operand& b, int splits, const typename E
                               : tuning_override("A3PO_GROUP_M_GRAD", kGroupM);
   im.k_splits = k_splits > 1 ? k_splits : 1;
   im.k_split_rows = static_cast<long long>(im.m_tiles) * BM * MT;
+  im.beside = begin == Begin::kBeside;
   im.items *= im.k_splits;
   im.dyn_rows = dyn.rows;
   im.dyn_is_k = dyn.is_k;
@@ -1059,7 +1073,7 @@ int launch_gemm(const Operand& a, const Operand& b, int splits, const typename E
   if (grid > im.items) grid = im.items;
   if (grid < 1) return A3PO_OK;
   A3PO_LAUNCH(Epi::kKernelId, stream, (launch_early(kernel, static_cast<unsigned>(grid), kTcThreads, kSmemBytes, stream, 1,
-                                                    early, map_a, map_b, map_c, im, k_blocks, ep, status)));
+                                                    begin != Begin::kAfter, map_a, map_b, map_c, im, k_blocks, ep, status)));
   return after_launch();
 }
 
@@ -1109,7 +1123,8 @@ int pair_capacity() {
 // group_m / paced: rasterisation group in 256-row tiles, and whether the CTAs keep in step (see ItemMap, Pace).
 template <class Epi, bool A_MN, bool B_MN>
 int launch_pair_gemm(const Operand& a, const Operand& b, int splits, const typename Epi::Params& ep, const DynRows& dyn,
-                     uint32_t* status, cudaStream_t stream, int group_m = kGroupM, bool paced = false, bool early = false) {
+                     uint32_t* status, cudaStream_t stream, int group_m = kGroupM, bool paced = false,
+                     Begin begin = Begin::kAfter) {
   const int pairs_max = pair_capacity<Epi, A_MN, B_MN>();
   if (pairs_max <= 0) return A3PO_ERR_UNSUPPORTED;
   CUtensorMap map_a, map_b, map_c;
@@ -1135,13 +1150,15 @@ int launch_pair_gemm(const Operand& a, const Operand& b, int splits, const typen
   im.pace = !paced || tuning_override("A3PO_PACE_OFF", 0) == 1 ? nullptr : next_pace_block();
   im.k_splits = 1;
   im.k_split_rows = 0;
+  im.beside = begin == Begin::kBeside;
   const int k_blocks = static_cast<int>((a.k_extent + BK - 1) / BK);
   long long pairs = pairs_max;
   if (pairs > im.items) pairs = im.items;
   if (pairs < 1) return A3PO_OK;
   auto kernel = gemm_pair_kernel<Epi, A_MN, B_MN>;
   A3PO_LAUNCH(Epi::kKernelId, stream, (launch_early(kernel, static_cast<unsigned>(2 * pairs), pair_threads<Epi>(), kPairSmemBytes,
-                                                    stream, 1, early, map_a, map_b, map_c, im, k_blocks, ep, status)));
+                                                    stream, 1, begin != Begin::kAfter, map_a, map_b, map_c, im, k_blocks, ep,
+                                                    status)));
   return after_launch();
 }
 

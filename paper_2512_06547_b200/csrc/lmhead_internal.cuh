@@ -45,10 +45,11 @@ int compact_rows(const void* hidden, int h, const int32_t* targets, const uint8_
 // of hidden rows for compact rows [offset, offset + rows) into dst (zero rows up to the next multiple of 128).
 int compact_index(const int32_t* targets, const uint8_t* row_mask, const float* g, const float* lse, long long n,
                   const CompactBuffers& cb, cudaStream_t stream);
+// early, beside: see launch_early, and Begin in gemm_tc.cuh.
 int gather_rows_range(const void* hidden, int h, const int* idx, const int* count, long long offset, long long rows,
-                      void* dst, cudaStream_t stream);
+                      void* dst, cudaStream_t stream, bool early = false, bool beside = false);
 // dst[t, :] = src_c[pos[t], :] for kept rows, zero otherwise.
-int scatter_rows(const void* src_c, int h, const int* pos, long long n, void* dst, cudaStream_t stream);
+int scatter_rows(const void* src_c, int h, const int* pos, long long n, void* dst, cudaStream_t stream, bool early = false);
 
 // ---- tcgen05 / TMEM / TMA kernels (lmhead_tc.cu), bf16 only ----
 bool lmhead_tc_supported(const void* hidden, const void* w, long long n, int h, int v);
