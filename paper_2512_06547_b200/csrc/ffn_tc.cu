@@ -202,33 +202,74 @@ struct GradGateUpEpilogue : PlainEpilogue {
   __device__ __forceinline__ void end(const Params&, long long, int) {}
 };
 
-// out[r, c] = sum over parts, in index order.  8 columns per thread.
+// Partial products of a K split, fp32: part s of output row r at [s][r].  The tensor is three-dimensional so that the copy
+// engine clips each part at the rows that exist (of a 128-row tile a few are real when few tokens come).
+template <int KERNEL_ID>
+struct StorePartsEpilogue : PlainEpilogue {
+  static constexpr int kKernelId = KERNEL_ID;
+  struct Params {
+    float* c;
+    long long n;          // rows of a part
+    int rows_pad;         // from part to part; tile rows count on through the parts (ItemMap::k_split_rows)
+    int parts;
+    int n_cols;           // multiple of 8
+  };
+  static int make_c_map(const Params& p, CUtensorMap* map) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return A3PO_ERR_CUDA;
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(p.n_cols), static_cast<cuuint64_t>(p.n),
+                                static_cast<cuuint64_t>(p.parts)};
+    const cuuint64_t row = static_cast<cuuint64_t>(p.n_cols) * sizeof(float);
+    const cuuint64_t strides[2] = {row, row * static_cast<cuuint64_t>(p.rows_pad)};
+    const cuuint32_t box[3] = {kEpiChunk, static_cast<cuuint32_t>(BM), 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, p.c, dims, strides, box, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? A3PO_OK : A3PO_ERR_CUDA;
+  }
+  __device__ __forceinline__ void begin(const Params&, long long) {}
+  __device__ __forceinline__ void chunk(const Params& p, int tile_row0, int col0, uint32_t (&r)[kEpiChunk], SlabStore& st) {
+    uint8_t* s = st.acquire();
+#pragma unroll
+    for (int q = 0; q < 8; ++q) *st.piece(s, q) = make_uint4(r[q * 4 + 0], r[q * 4 + 1], r[q * 4 + 2], r[q * 4 + 3]);
+    fence_proxy_async_smem();
+    named_barrier_sync(st.barrier_id, 128);
+    if (st.issuer) {
+      const int part = tile_row0 / p.rows_pad, row0 = tile_row0 - part * p.rows_pad;
+      if (col0 < p.n_cols && row0 < p.n) tma_store_3d(st.map, s, col0, row0, part);
+      bulk_commit_group();
+    }
+    ++st.issued;
+  }
+  __device__ __forceinline__ void end(const Params&, long long, int) {}
+};
+
+// out[r, c] = sum over parts, in index order.  4 columns per thread, 8 parts on their way at a time.
+constexpr int kAddCols = 4, kAddBatch = 8;
 __global__ void __launch_bounds__(256)
 add_parts_kernel(const float* parts, int n_parts, long long part_stride, long long n, int cols,
                  const int* dyn_rows, __nv_bfloat16* out) {
   wait_for_previous();
   allow_next();
   const long long rows = dyn_rows ? (*dyn_rows < n ? *dyn_rows : n) : n;
-  const int groups = cols / 8;
-  const long long total = rows * groups;
+  const long long total = rows * (cols / kAddCols);
   for (long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; i < total;
        i += static_cast<long long>(gridDim.x) * 256) {
-    const float* src = parts + i * 8;
-    float v[8];
+    const float* src = parts + i * kAddCols;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p0 = 0; p0 < n_parts; p0 += kAddBatch) {
+      float4 a[kAddBatch];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = 0.f;
-    for (int p = 0; p < n_parts; ++p) {
-      const float4 a = __ldcs(reinterpret_cast<const float4*>(src + p * part_stride));
-      const float4 b = __ldcs(reinterpret_cast<const float4*>(src + p * part_stride) + 1);
-      v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
-      v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+      for (int k = 0; k < kAddBatch; ++k)
+        a[k] = p0 + k < n_parts ? __ldcs(reinterpret_cast<const float4*>(src + (p0 + k) * part_stride))
+                                : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < kAddBatch; ++k) {
+        v.x += a[k].x; v.y += a[k].y; v.z += a[k].z; v.w += a[k].w;
+      }
     }
-    uint4 u;
-    u.x = pack_bf16x2(v[0], v[1]);
-    u.y = pack_bf16x2(v[2], v[3]);
-    u.z = pack_bf16x2(v[4], v[5]);
-    u.w = pack_bf16x2(v[6], v[7]);
-    reinterpret_cast<uint4*>(out)[i] = u;
+    reinterpret_cast<uint2*>(out)[i] = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
   }
 }
 
@@ -268,10 +309,10 @@ int rows_gemm(const Operand& a, const Operand& b, __nv_bfloat16* out, float* par
   const int k_parts = parts ? ffn_k_parts(n, cols, static_cast<int>(a.k_extent)) : 1;
   if (k_parts > 1) {
     const long long rows_pad = (n + BM - 1) / BM * BM;
-    typename StoreF32EpilogueT<ID>::Params ep{parts, cols, rows_pad * k_parts, cols, 0};
-    A3PO_RETURN_IF((launch_gemm<StoreF32EpilogueT<ID>, false, B_MN, 1>(a, b, 0, ep, rows_as_m(dyn_rows, n), status,
-                                                                      stream, k_parts, begin)));
-    const long long want = (n * (cols / 8) + 255) / 256;
+    typename StorePartsEpilogue<ID>::Params ep{parts, n, static_cast<int>(rows_pad), k_parts, cols};
+    A3PO_RETURN_IF((launch_gemm<StorePartsEpilogue<ID>, false, B_MN, 1>(a, b, 0, ep, rows_as_m(dyn_rows, n), status,
+                                                                       stream, k_parts, begin)));
+    const long long want = (n * (cols / kAddCols) + 255) / 256;
     const int blocks = static_cast<int>(want < sm_count() * 8ll ? want : sm_count() * 8ll);
     A3PO_LAUNCH(ID, stream, (launch_early(add_parts_kernel, blocks, 256, 0, stream, 1, true,
                                           static_cast<const float*>(parts), k_parts, rows_pad * cols, n, cols, dyn_rows,
