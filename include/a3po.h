@@ -399,7 +399,7 @@ int a3po_train_step_host(const void* h_hidden, const int32_t* h_targets, const f
  * must not overlap inputs.  N = 0 launches nothing, apart from the zeros of a weight gradient that is not accumulated.
  *
  * Norm:       xhat = (x - mean) rstd,  rstd = 1 / sqrt(mean((x - mean)^2) + eps),  y = xhat gamma + beta
- *   A3PO_NORM_LAYER: mean = sum(x) / H;  A3PO_NORM_RMS: mean = 0 (mean and grad_beta must be NULL).
+ *   A3PO_NORM_LAYER: mean = sum(x) / H;  A3PO_NORM_RMS: mean = 0 (the argument mean must be NULL).  Either takes a beta.
  *   gamma [H], beta [H] or NULL: dtype dt.  mean, rstd: fp32 [N] outputs of the forward, or NULL if no backward
  *   follows; inputs of the backward.
  * Its backward:  gx = grad_y gamma;  grad_x = rstd (gx - [mean(gx)] - xhat mean(gx xhat))   ([.]: layer norm only)

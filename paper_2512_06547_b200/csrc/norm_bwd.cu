@@ -341,6 +341,31 @@ norm_weight_long_kernel(const NormBwdArgs<T> a, int parts) {
   if (LAYER) out[a.h + c] = db;
 }
 
+// Partial sums of dbeta for an RMS norm that has a beta, in a pass over grad_y of its own: block (x: 1024 columns, 8 per
+// thread; y: part), rows part, part + parts, ...  Bound by that pass and its two launches: 65,536 x 2,048 bf16 144 -> 214 us,
+// 5,001 x 1,003 21 -> 34.  Asked of the main kernel (a layer norm's form without means) it would cost every layer norm a
+// branch: 4,000 x 12,001 bf16, whose registers spill, 384 -> 566 us.
+constexpr int kBetaThreads = 128;
+template <typename T>
+__global__ void __launch_bounds__(kBetaThreads)
+norm_beta_kernel(const NormBwdArgs<T> a, int parts) {
+  const int col = (blockIdx.x * kBetaThreads + threadIdx.x) * kVec;
+  if (col >= a.h) return;
+  float sum[kVec] = {};
+#pragma unroll 4
+  for (long long t = blockIdx.y; t < a.n; t += parts) {
+    if (a.row_mask && a.row_mask[t] == 0) continue;
+    float gy[kVec];
+    load_chunk(a.grad_y + t * a.h, col, a.h, a.vec != 0, gy);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) sum[j] += gy[j];
+  }
+  float* out = a.part + static_cast<long long>(blockIdx.y) * a.h;
+#pragma unroll
+  for (int j = 0; j < kVec; ++j)
+    if (col + j < a.h) out[col + j] = sum[j];
+}
+
 
 template <typename T, int CPT, bool WIDE, int MAXT, bool VEC, bool LAYER, bool JOIN>
 int launch(const NormBwdArgs<T>& a, int threads, int lanes, int* parts, cudaStream_t stream) {
@@ -397,22 +422,38 @@ int by_length(const NormBwdArgs<T>& a, int* parts, cudaStream_t stream) {
   return after_launch();
 }
 
+// grad[c] (+)= the parts' sums: dgamma, and with `layer` dbeta behind it.
+int reduce_parts(const float* part, int parts, int h, bool layer, int accumulate, float* grad_gamma, float* grad_beta,
+                 cudaStream_t stream) {
+  // 16 columns per block as long as that is a block per SM at most, else 32: 3,000 x 2,048, RMS norm, 14.4 us a call against 15.1,
+  // 300 x 4,096 14.4 against 12.5 (inputs in L2).
+  const bool fine = (h + 15) / 16 * (layer ? 2 : 1) <= sm_count();
+  const int cols = fine ? 16 : 32;
+  const dim3 grid(static_cast<unsigned>((h + cols - 1) / cols), layer ? 2u : 1u);
+  A3PO_LAUNCH(kKNormBwd, stream, (launch_early(fine ? reduce_parts_kernel<16> : reduce_parts_kernel<32>, grid,
+                                               dim3(cols, kReduceThreads / cols), 0, stream, 1, true, part, parts,
+                                               static_cast<long long>(layer ? 2 : 1) * h, h, accumulate, grad_gamma,
+                                               grad_beta)));
+  return after_launch();
+}
+
 template <typename T, bool LAYER, bool JOIN>
 int by_alignment(const NormBwdArgs<T>& a, float* grad_gamma, float* grad_beta, int accumulate, cudaStream_t stream) {
   int parts = 0;
   A3PO_RETURN_IF((a.vec ? by_length<T, true, LAYER, JOIN>(a, &parts, stream)
                         : by_length<T, false, LAYER, JOIN>(a, &parts, stream)));
-  // 16 columns per block as long as that is a block per SM at most, else 32: 3,000 x 2,048, RMS norm, 14.4 us a call against 15.1,
-  // 300 x 4,096 14.4 against 12.5 (inputs in L2).
-  const bool fine = (a.h + 15) / 16 * (LAYER ? 2 : 1) <= sm_count();
-  const int cols = fine ? 16 : 32;
-  const dim3 grid(static_cast<unsigned>((a.h + cols - 1) / cols), LAYER ? 2u : 1u);
-  A3PO_LAUNCH(kKNormBwd, stream, (launch_early(fine ? reduce_parts_kernel<16> : reduce_parts_kernel<32>, grid,
-                                               dim3(cols, kReduceThreads / cols), 0, stream, 1, true,
-                                               static_cast<const float*>(a.part), parts,
-                                               static_cast<long long>(LAYER ? 2 : 1) * a.h, a.h, accumulate, grad_gamma,
-                                               grad_beta)));
-  return after_launch();
+  A3PO_RETURN_IF(reduce_parts(a.part, parts, a.h, LAYER, accumulate, grad_gamma, grad_beta, stream));
+  if (LAYER || !grad_beta) return A3PO_OK;
+  // a few blocks per SM; the workspace holds two sums of min(n, max_parts) rows
+  const unsigned columns = static_cast<unsigned>((a.h + kBetaThreads * kVec - 1) / (kBetaThreads * kVec));
+  long long want = (8ll * sm_count() + columns - 1) / columns;
+  if (want > max_parts(a.h)) want = max_parts(a.h);
+  if (want > a.n) want = a.n;
+  parts = static_cast<int>(want);
+  A3PO_LAUNCH(kKNormBwd, stream, (norm_beta_kernel<T><<<dim3(columns, static_cast<unsigned>(parts)), kBetaThreads, 0, stream>>>(
+                                     a, parts)));
+  A3PO_RETURN_IF(after_launch());
+  return reduce_parts(a.part, parts, a.h, false, accumulate, grad_beta, nullptr, stream);
 }
 template <typename T>
 int by_kind(const NormBwdArgs<T>& a, bool layer, bool join, float* gg, float* gb, int acc, cudaStream_t s) {

@@ -239,7 +239,7 @@ int norm_bwd_entry(bool join, const void* x, const void* gamma, const float* mea
   if (kind != A3PO_NORM_RMS && kind != A3PO_NORM_LAYER) return A3PO_ERR_UNSUPPORTED;
   if (!gamma || !grad_gamma || (n > 0 && (!x || !rstd || !grad_y || (!join && !grad_x)))) return A3PO_ERR_INVALID_ARG;
   if (n > 0 && kind == A3PO_NORM_LAYER && !mean) return A3PO_ERR_INVALID_ARG;
-  if (kind == A3PO_NORM_RMS && grad_beta) return A3PO_ERR_INVALID_ARG;   // an RMS norm has no beta gradient to give
+  if (kind == A3PO_NORM_RMS && mean) return A3PO_ERR_INVALID_ARG;   // an RMS norm has none, as in the forward
   if (join) {
     if (n > 0 && !grad_residual) return A3PO_ERR_INVALID_ARG;
     A3PO_RETURN_IF(check_dropout(p, rng));

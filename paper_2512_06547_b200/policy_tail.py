@@ -24,11 +24,12 @@ from . import binding as b
 class PolicyTail:
     """Buffers and calls for batches of exactly n rows.
 
-    params: dict with gamma_in [H], w_gate_up [2 F, H], w_down [H, F], gamma_out [H], w [V, H], and for layer norms
-    optionally beta_in, beta_out [H]; all of `dtype`."""
+    params: dict with gamma_in [H], w_gate_up [2 F, H], w_down [H, F], gamma_out [H], w [V, H], and optionally beta_in,
+    beta_out [H]; all of `dtype`.  beta: gradients of beta_in and beta_out are wanted (default: of layer norms); without
+    them a pass refuses params that hold a beta."""
 
     def __init__(self, n, h, f, v, dtype=torch.bfloat16, *, kind=b.A3PO_NORM_RMS, activation=b.A3PO_ACT_SILU, dropout_p=0.0,
-                 eps=1e-6, device="cuda"):
+                 eps=1e-6, beta=None, device="cuda"):
         self.n, self.h, self.f, self.v = n, h, f, v
         self.kind, self.activation, self.p, self.eps = kind, activation, float(dropout_p), eps
         layer = kind == b.A3PO_NORM_LAYER
@@ -41,7 +42,8 @@ class PolicyTail:
         self.logp, self.lse, self.grad_logp, self.loss = f32(n), f32(n), f32(n), f32(1)
         self.grad_hidden, self.grad_r1, self.grad_y, self.grad_a, self.grad_r0 = rows(), rows(), rows(), rows(), rows()
         self.grads = {"gamma_in": f32(h), "gamma_out": f32(h), "w_gate_up": f32(2 * f, h), "w_down": f32(h, f), "w": f32(v, h)}
-        if layer:
+        self.beta = layer if beta is None else bool(beta)
+        if self.beta:
             self.grads.update(beta_in=f32(h), beta_out=f32(h))
         self.stats = b.new_stats(device)
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
@@ -55,7 +57,9 @@ class PolicyTail:
         """One pass.  batch: targets, behav_logp, versions, current_version, adv, mask, clip_eps as a3po_train_step takes
         them.  Returns a dict of this object's own buffers: loss, stats, logp, status, grad_r0 and grads (by parameter,
         fp32; added to what they hold with accumulate_grads)."""
-        mask, layer, g = batch["mask"], self.kind == b.A3PO_NORM_LAYER, self.grads
+        if not self.beta and (params.get("beta_in") is not None or params.get("beta_out") is not None):
+            raise ValueError("params hold a beta, but this PolicyTail was made without gradients for it (beta=True)")
+        mask, g = batch["mask"], self.grads
         norm = dict(kind=self.kind, row_mask=mask)
         b.a3po_norm_fwd(r0, params["gamma_in"], self.a, self.rstd_in, beta=params.get("beta_in"), mean=self.mean_in,
                         eps=self.eps, **norm)
