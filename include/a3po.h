@@ -456,8 +456,9 @@ int a3po_dropout_norm_bwd(const void* r, float p, const uint64_t* rng, const voi
  *   dh = grad_y Wd,  dg = dh u act'(g),  du = dh act(g)
  *   grad_x = dg Wg + du Wu,  grad_Wg = dg^T x,  grad_Wu = du^T x,  grad_Wd = grad_y^T h
  *
- * x, y, grad_x, grad_y [N, H]; w_gate_up [2 F, H] (the F rows of Wg, then the F rows of Wu); w_down [H, F]; dtype `dt`,
- * 16-byte aligned.  Any H and F: bf16 with H and F multiples of 8 runs on the tensor cores, the rest on the FP32 pipes.
+ * x, y, grad_x, grad_y [N, H]; w_gate_up [2 F, H] (the F rows of Wg, then the F rows of Wu); w_down [H, F]; dtype `dt`.
+ * Any H and F: bf16 with H and F multiples of 8 runs on the tensor cores and wants every matrix 16-byte aligned, the rest
+ * runs on the FP32 pipes and takes pointers aligned to their elements.
  * Both projections, the activation and the product are one kernel; dh never reaches memory either.  Accumulation is
  * fp32; for bf16 the intermediates that enter a matrix product (h, dg, du) are rounded to bf16.
  *

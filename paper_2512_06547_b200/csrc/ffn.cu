@@ -12,6 +12,8 @@ size_t elt(a3po_dtype dt) { return dt == A3PO_F32 ? 4 : 2; }
 
 // The family is a function of dtype and shape alone, so that forward and backward agree on the kept layout.
 bool tensor_cores(a3po_dtype dt, int h, int f) { return dt == A3PO_BF16 && h % 8 == 0 && f % 8 == 0; }
+// The tensor-core and few-row kernels move 16 bytes at a time, the FP32-pipe kernels elements (of type `dt`).
+size_t row_alignment(a3po_dtype dt, int h, int f) { return tensor_cores(dt, h, f) ? 16 : elt(dt); }
 
 int check(const void* x, const void* w_gate_up, const void* w_down, long long n, int h, int f, a3po_dtype dt,
           a3po_activation act) {
@@ -19,10 +21,11 @@ int check(const void* x, const void* w_gate_up, const void* w_down, long long n,
   if (dt != A3PO_F32 && dt != A3PO_BF16) return A3PO_ERR_UNSUPPORTED;
   if (act != A3PO_ACT_SILU && act != A3PO_ACT_GELU_TANH) return A3PO_ERR_UNSUPPORTED;
   if (n > INT_MAX - 256 || f > INT_MAX / 4 || h > INT_MAX / 4) return A3PO_ERR_UNSUPPORTED;
-  // the FP32-pipe kernels have one block row of 64 columns per grid row
+  // the FP32-pipe kernels have a grid row for every 32 (or 64) columns
   if (!tensor_cores(dt, h, f) && (f > 65535 * 32 || h > 65535 * 32)) return A3PO_ERR_UNSUPPORTED;
   if (!w_gate_up || !w_down || (n > 0 && !x)) return A3PO_ERR_INVALID_ARG;
-  if (!aligned_to(x, 16) || !aligned_to(w_gate_up, 16) || !aligned_to(w_down, 16)) return A3PO_ERR_UNSUPPORTED;
+  const size_t align = row_alignment(dt, h, f);
+  if (!aligned_to(x, align) || !aligned_to(w_gate_up, align) || !aligned_to(w_down, align)) return A3PO_ERR_UNSUPPORTED;
   return A3PO_OK;
 }
 
@@ -102,7 +105,7 @@ int a3po_gated_ffn_fwd(const void* x, const void* w_gate_up, const void* w_down,
                        size_t ws_bytes, uint32_t* status, void* stream_) {
   A3PO_RETURN_IF(check(x, w_gate_up, w_down, N, H, F, dt, act));
   if (N > 0 && !y) return A3PO_ERR_INVALID_ARG;
-  if (!aligned_to(y, 16)) return A3PO_ERR_UNSUPPORTED;
+  if (!aligned_to(y, row_alignment(dt, H, F))) return A3PO_ERR_UNSUPPORTED;
   if (kept && (!aligned_to(kept, 256) || kept_bytes < a3po_gated_ffn_kept_bytes(N, F, dt))) return A3PO_ERR_WORKSPACE;
   if (!ws || !aligned_to(ws, 256) || ws_bytes < a3po_gated_ffn_workspace_bytes(N, H, F, dt, row_mask != nullptr, 0))
     return A3PO_ERR_WORKSPACE;
@@ -136,9 +139,10 @@ int a3po_gated_ffn_bwd(const void* x, const void* w_gate_up, const void* w_down,
   if (!grad_w_gate_up || !grad_w_down || (N > 0 && (!grad_y || !grad_x || !kept))) return A3PO_ERR_INVALID_ARG;
   if (grad_w_dt != A3PO_F32 && grad_w_dt != dt) return A3PO_ERR_UNSUPPORTED;
   if (accumulate_grad_w && grad_w_dt != A3PO_F32) return A3PO_ERR_UNSUPPORTED;   // every addition would round to bf16
-  for (const void* p : {grad_y, static_cast<const void*>(grad_x), static_cast<const void*>(grad_w_gate_up),
-                        static_cast<const void*>(grad_w_down)})
-    if (!aligned_to(p, 16)) return A3PO_ERR_UNSUPPORTED;
+  const size_t align = row_alignment(dt, H, F), align_w = tensor_cores(dt, H, F) ? 16 : elt(grad_w_dt);
+  if (!aligned_to(grad_y, align) || !aligned_to(grad_x, align) || !aligned_to(grad_w_gate_up, align_w) ||
+      !aligned_to(grad_w_down, align_w))
+    return A3PO_ERR_UNSUPPORTED;
   if (kept && (!aligned_to(kept, 256) || kept_bytes < a3po_gated_ffn_kept_bytes(N, F, dt))) return A3PO_ERR_WORKSPACE;
   if (!ws || !aligned_to(ws, 256) || ws_bytes < a3po_gated_ffn_workspace_bytes(N, H, F, dt, row_mask != nullptr, 1))
     return A3PO_ERR_WORKSPACE;
