@@ -392,7 +392,7 @@ int a3po_train_step_host(const void* h_hidden, const int32_t* h_targets, const f
  * that owns the last block of the policy runs them on the rows it then hands to a3po_token_logprobs_fwd or
  * a3po_train_step, and runs their backward on the grad_hidden it gets back.
  *
- * Common to all of them: matrices are row-major [N, H], contiguous, dtype `dt` (any H >= 1; pointers aligned to their
+ * Common to all of them: matrices are row-major [N, H], contiguous, dtype `dt` (1 <= H <= 2^30; pointers aligned to their
  * elements, 16-byte aligned rows move in 16-byte pieces); arithmetic, statistics and weight gradients are fp32 and
  * each stored element is rounded once.  row_mask uint8 [N] or NULL: of rows with 0 nothing enters a result (they may
  * hold NaN), their outputs (gradients included) are 0 and they add nothing to a weight gradient.  N <= 2^31 - 1.  Outputs

@@ -190,6 +190,7 @@ int check_rows(long long n, int h, a3po_dtype dt) {
   if (n < 0 || h <= 0) return A3PO_ERR_INVALID_ARG;
   if (dt != A3PO_F32 && dt != A3PO_BF16) return A3PO_ERR_UNSUPPORTED;
   if (n > 0x7fffffffll) return A3PO_ERR_UNSUPPORTED;   // one grid dimension of rows, one 32-bit counter word
+  if (h > 1 << 30) return A3PO_ERR_UNSUPPORTED;        // columns are int, and the loops over them step past the end
   return A3PO_OK;
 }
 
