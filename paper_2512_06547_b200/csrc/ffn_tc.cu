@@ -292,10 +292,12 @@ constexpr int kPacedWaves = 8;
 template <class Epi, bool A_MN, bool B_MN>
 int contract(const Operand& a, const Operand& b, const typename Epi::Params& ep, const DynRows& dyn, uint32_t* status,
              cudaStream_t stream, Begin begin) {
-  if (a.mn_extent <= BM) return launch_gemm<Epi, A_MN, B_MN, 1>(a, b, 0, ep, dyn, status, stream, 1, begin);
+  const bool pairs = a.mn_extent > BM;
+  const int rows = pairs ? 2 * BM : BM;
+  const long long tiles = ((a.mn_extent + rows - 1) / rows) * ((b.mn_extent + BN - 1) / BN);
+  const bool paced = (pairs ? 2 : 1) * tiles >= kPacedWaves * sm_count();
+  if (!pairs) return launch_gemm<Epi, A_MN, B_MN, 1>(a, b, 0, ep, dyn, status, stream, 1, begin, paced);
   const int group = !A_MN && !B_MN ? fwd_group_m(a.k_extent, 2 * BM) : kGroupM;
-  const long long tiles = ((a.mn_extent + 2 * BM - 1) / (2 * BM)) * ((b.mn_extent + BN - 1) / BN);
-  const bool paced = 2 * tiles >= kPacedWaves * sm_count();
   return launch_pair_gemm<Epi, A_MN, B_MN>(a, b, 0, ep, dyn, status, stream, group, paced, begin);
 }
 

@@ -1042,10 +1042,10 @@ struct DynRows {
   int select_value = 0;
 };
 
-// C[M, N] = sum_k A[m, k] B[n, k];  splits = 0 means one column tile per work item.
+// C[M, N] = sum_k A[m, k] B[n, k];  splits = 0 means one column tile per work item.  paced: the CTAs keep in step (see Pace).
 template <class Epi, bool A_MN, bool B_MN, int MT = 1>
 int launch_gemm(const Operand& a, const Operand& b, int splits, const typename Epi::Params& ep, const DynRows& dyn,
-                uint32_t* status, cudaStream_t stream, int k_splits = 1, Begin begin = Begin::kAfter) {
+                uint32_t* status, cudaStream_t stream, int k_splits = 1, Begin begin = Begin::kAfter, bool paced = true) {
   constexpr size_t kSmemBytes = TileCfg<MT>::kSmemBytes;
   CUtensorMap map_a, map_b, map_c;
   A3PO_RETURN_IF(make_map(&map_a, a, A_MN, BM * MT));
@@ -1077,7 +1077,7 @@ int launch_gemm(const Operand& a, const Operand& b, int splits, const typename E
   im.pace_slack = tuning_override("A3PO_PACE_SLACK", kPaceSlack);
   if (im.pace_slack > kPaceRing / 2) im.pace_slack = kPaceRing / 2;   // a slot must not be reused while waited on
   // CTAs on parts of one tile read different k-blocks: nothing to keep in step
-  im.pace = tuning_override("A3PO_PACE_OFF", 0) == 1 || im.k_splits > 1 ? nullptr : next_pace_block();
+  im.pace = !paced || tuning_override("A3PO_PACE_OFF", 0) == 1 || im.k_splits > 1 ? nullptr : next_pace_block();
   const int k_blocks = static_cast<int>((a.k_extent + BK - 1) / BK);
   auto kernel = gemm_tn_kernel<Epi, A_MN, B_MN, MT>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemBytes)) !=
