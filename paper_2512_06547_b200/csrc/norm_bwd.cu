@@ -398,17 +398,18 @@ int by_length(const NormBwdArgs<T>& a, int* parts, cudaStream_t stream) {
     while (lanes < groups) lanes *= 2;
     return launch<T, 1, false, kNarrowThreads, VEC, LAYER, JOIN>(a, kNarrowThreads, lanes, parts, stream);
   }
-  // element-wise rows: one chunk per thread as long as that fits, for more loads in flight
-  if constexpr (!VEC) {
+  // 16-byte rows: two chunks per thread; element-wise rows: one as long as that fits, for more loads in flight
+  if constexpr (VEC) {
+    if (groups <= 64) return launch<T, 2, false, kNarrowThreads, VEC, LAYER, JOIN>(a, kNarrowThreads, kWarp, parts, stream);
+    if (groups <= 2 * kNarrowThreads)
+      return launch<T, 2, true, kNarrowThreads, VEC, LAYER, JOIN>(a, static_cast<int>(round_up((groups + 1) / 2, kWarp)), 0, parts, stream);
+  } else {
     if (groups <= kNarrowThreads)
       return launch<T, 1, true, kNarrowThreads, VEC, LAYER, JOIN>(a, static_cast<int>(round_up(groups, kWarp)), 0, parts,
                                                                   stream);
     if (groups <= kWideThreads)
       return launch<T, 1, true, kWideThreads, VEC, LAYER, JOIN>(a, static_cast<int>(round_up(groups, kWarp)), 0, parts, stream);
   }
-  if (groups <= 64) return launch<T, 2, false, kNarrowThreads, VEC, LAYER, JOIN>(a, kNarrowThreads, kWarp, parts, stream);
-  if (groups <= 2 * kNarrowThreads)
-    return launch<T, 2, true, kNarrowThreads, VEC, LAYER, JOIN>(a, static_cast<int>(round_up((groups + 1) / 2, kWarp)), 0, parts, stream);
   if (groups <= 2 * kWideThreads)
     return launch<T, 2, true, kWideThreads, VEC, LAYER, JOIN>(a, static_cast<int>(round_up((groups + 1) / 2, kWarp)), 0, parts, stream);
   if (groups <= 4 * kWideThreads)
