@@ -62,6 +62,8 @@ struct GateUpEpilogue {
   static constexpr bool kGated = true;
   static constexpr bool kPrefetch = false;
   static constexpr int kGroups = 2;
+  static constexpr bool kChained = true;
+  static constexpr bool kSplitK = false;
   struct Params {
     __nv_bfloat16* hid;    // [n, f]
     uint8_t* kept;         // see ffn_internal.cuh
@@ -98,6 +100,7 @@ struct GateUpEpilogue {
 // [rows][2][f], so that each of the two is clipped at its own column f.
 template <bool GELU>
 struct GradGateUpEpilogue : PlainEpilogue {
+  static constexpr bool kChained = true;
   static constexpr bool kPrefetch = true;
   static constexpr int kGroups = 2;
   static constexpr int kKernelId = kKFfnGradGate;
@@ -207,6 +210,8 @@ struct GradGateUpEpilogue : PlainEpilogue {
 template <int KERNEL_ID>
 struct StorePartsEpilogue : PlainEpilogue {
   static constexpr int kKernelId = KERNEL_ID;
+  static constexpr bool kChained = true;
+  static constexpr bool kSplitK = true;
   struct Params {
     float* c;
     long long n;          // rows of a part

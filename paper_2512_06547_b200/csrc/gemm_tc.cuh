@@ -105,12 +105,13 @@ struct Item {
   long long row_shift;
 };
 
+template <bool SPLIT_K>
 __device__ __forceinline__ Item decode_item(const ItemMap& im, long long i, int k_blocks) {
   Item it;
   it.kb_begin = 0;
   it.kb_end = k_blocks;
   it.row_shift = 0;
-  if (im.k_splits > 1) {
+  if (SPLIT_K && im.k_splits > 1) {
     const int part = static_cast<int>(i % im.k_splits);
     i /= im.k_splits;
     it.kb_begin = static_cast<int>(static_cast<long long>(part) * k_blocks / im.k_splits);
@@ -304,15 +305,21 @@ struct SlabStore {
 // kPrefetch: prefetch(ep, tile_row0, col0, cols) is called before the product of those columns is waited for.
 // kGroups: groups of four epilogue warps in the pair kernel; each takes its share of a tile's columns.  Two for epilogues
 // that take longer than a tile's MMAs at a short K (4 warps cannot fill the issue slots between their barriers).
+// kChained: launches may begin early, or let a successor begin (see Begin).  kSplitK: launches may split K.  Both are
+// compile-time, because the LM head's kernels, which do neither, took 0.5-1 % longer with the code for them (forward of
+// 9,029 rows of 1536 x 151,936 3,108 -> 3,125 us, backward 6,680 -> 6,753).
 struct PlainEpilogue {
   static constexpr bool kGated = false;
   static constexpr bool kPrefetch = false;
   static constexpr int kGroups = 1;
+  static constexpr bool kChained = false;
+  static constexpr bool kSplitK = false;
 };
 
 template <int KERNEL_ID>
 struct StoreBf16EpilogueT : PlainEpilogue {
   static constexpr int kKernelId = KERNEL_ID;
+  static constexpr bool kChained = KERNEL_ID != kKTcGradHidden;
   struct Params {
     __nv_bfloat16* c;
     long long ldc;
@@ -351,6 +358,7 @@ using StoreBf16Epilogue = StoreBf16EpilogueT<kKTcGradHidden>;
 template <int KERNEL_ID>
 struct StoreF32EpilogueT : PlainEpilogue {
   static constexpr int kKernelId = KERNEL_ID;
+  static constexpr bool kChained = KERNEL_ID != kKTcGradW;
   struct Params {
     float* c;
     long long ldc;
@@ -373,8 +381,23 @@ struct StoreF32EpilogueT : PlainEpilogue {
 };
 using StoreF32Epilogue = StoreF32EpilogueT<kKTcGradW>;
 
-// AND of a predicate over the 128 threads of an epilogue group (hardware barrier `id`).
-__device__ __forceinline__ bool all_epilogue_threads(bool pred, int id = 2) {
+// AND of a predicate over the 128 epilogue threads (hardware barrier 2).
+__device__ __forceinline__ bool all_epilogue_threads(bool pred) {
+  uint32_t out;
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q;\n"
+      "setp.ne.u32 q, %1, 0;\n"
+      "bar.red.and.pred p, 2, 128, q;\n"
+      "selp.u32 %0, 1, 0, p;\n"
+      "}\n"
+      : "=r"(out)
+      : "r"(static_cast<uint32_t>(pred))
+      : "memory");
+  return out != 0;
+}
+// The same over one of several groups (hardware barrier `id`).
+__device__ __forceinline__ bool all_epilogue_threads(bool pred, int id) {
   uint32_t out;
   asm volatile(
       "{\n"
@@ -472,8 +495,9 @@ gemm_tn_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   __syncthreads();
   tcgen05_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
-  if (im_static.ahead > 0 && threadIdx.x == 0) {   // with a device-side row count the tile may be another: only a hint is lost
-    const Item it = decode_item(im_static, blockIdx.x, k_blocks_static);
+  // with a device-side row count the tile may be another: only a hint is lost
+  if (Epi::kSplitK && im_static.ahead > 0 && threadIdx.x == 0) {
+    const Item it = decode_item<Epi::kSplitK>(im_static, blockIdx.x, k_blocks_static);
     for (int kb = it.kb_begin; kb < it.kb_end && kb < it.kb_begin + im_static.ahead; ++kb) {
       if (B_MN) {
 #pragma unroll
@@ -483,8 +507,10 @@ gemm_tn_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       }
     }
   }
-  if (!im_static.beside) wait_for_previous();
-  allow_next();
+  if constexpr (Epi::kChained) {
+    if (!im_static.beside) wait_for_previous();
+    allow_next();
+  }
 
   // Work extents: static, or derived from the device-resident row count (identical in every thread).
   ItemMap im = im_static;
@@ -505,7 +531,7 @@ gemm_tn_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       }
     } else {
       im.m_tiles = static_cast<int>((rows + BM * MT - 1) / (BM * MT));
-      im.items = static_cast<long long>(im.m_tiles) * im.splits * im.k_splits;
+      im.items = static_cast<long long>(im.m_tiles) * im.splits * (Epi::kSplitK ? im.k_splits : 1);
     }
   }
 
@@ -531,7 +557,7 @@ gemm_tn_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         pace.slack = im.pace_slack;
       }
       for (long long i = blockIdx.x; i < im.items && ok; i += gridDim.x) {
-        const Item it = decode_item(im, i, k_blocks);
+        const Item it = decode_item<Epi::kSplitK>(im, i, k_blocks);
         for (int nt = it.n_begin; nt < it.n_end && ok; ++nt) {
           for (int kb = it.kb_begin; kb < it.kb_end; ++kb) {
             if (paced && kb % im.pace_period == 0) pace.arrive_and_wait();
@@ -582,7 +608,7 @@ gemm_tn_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       int acc = 0;
       uint32_t acc_phase = 0;
       for (long long i = blockIdx.x; i < im.items && ok; i += gridDim.x) {
-        const Item it = decode_item(im, i, k_blocks);
+        const Item it = decode_item<Epi::kSplitK>(im, i, k_blocks);
         for (int nt = it.n_begin; nt < it.n_end && ok; ++nt) {
           if (!A3PO_TIMED_WAIT(waited2, mbar_wait(&tmem_empty_bar[acc], acc_phase ^ 1u, abort_flag))) { ok = false; break; }
           tcgen05_fence_after_sync();
@@ -623,7 +649,7 @@ gemm_tn_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     st.row_in_tile = row_in_tile;
     st.issuer = (threadIdx.x == 2 * kWarp);
     for (long long i = blockIdx.x; i < im.items && ok; i += gridDim.x) {
-      const Item it = decode_item(im, i, k_blocks);
+      const Item it = decode_item<Epi::kSplitK>(im, i, k_blocks);
       const int item_row0 = it.m_tile * (BM * MT);
       const bool no_product = zero_output || it.kb_begin == it.kb_end;   // nothing was multiplied: zeros
       if (MT == 1) epi.begin(ep, static_cast<long long>(item_row0) + row_in_tile);
@@ -697,7 +723,7 @@ gemm_tn_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     tcgen05_fence_after_sync();
     tmem_dealloc(tmem_base, kTmemCols);
   }
-  if (im_static.beside) wait_for_previous();
+  if (Epi::kChained && im_static.beside) wait_for_previous();
 #ifdef A3PO_TUNING
   if (threadIdx.x == 0 && g_trace != nullptr) {
     const unsigned int slot = atomicAdd(&g_trace_next, 1u);
@@ -779,8 +805,10 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
   cluster_sync_all();   // the peer's barriers exist before anything signals them
   tcgen05_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
-  if (!im_static.beside) wait_for_previous();
-  allow_next();
+  if constexpr (Epi::kChained) {
+    if (!im_static.beside) wait_for_previous();
+    allow_next();
+  }
 
   ItemMap im = im_static;   // m_tiles counts 256-row pair tiles here
   int k_blocks = k_blocks_static;
@@ -822,7 +850,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         pace.slack = im.pace_slack;
       }
       for (long long i = pair_id; i < im.items && ok; i += n_pairs) {
-        const Item it = decode_item(im, i, k_blocks);
+        const Item it = decode_item<Epi::kSplitK>(im, i, k_blocks);
         const int row0 = it.m_tile * kPairRows + static_cast<int>(rank) * BM;
         for (int nt = it.n_begin; nt < it.n_end && ok; ++nt) {
           int col0 = nt * BN + static_cast<int>(rank) * (BN / 2);
@@ -872,7 +900,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
       int acc = 0;
       uint32_t acc_phase = 0;
       for (long long i = pair_id; i < im.items && ok; i += n_pairs) {
-        const Item it = decode_item(im, i, k_blocks);
+        const Item it = decode_item<Epi::kSplitK>(im, i, k_blocks);
         for (int nt = it.n_begin; nt < it.n_end && ok; ++nt) {
           if (!mbar_wait(&tmem_empty_bar[acc], acc_phase ^ 1u, abort_flag)) { ok = false; break; }
           tcgen05_fence_after_sync();
@@ -914,7 +942,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     st.row_in_tile = row_in_tile;
     st.issuer = (threadIdx.x == (2 + 4 * group) * kWarp);
     for (long long i = pair_id; i < im.items && ok; i += n_pairs) {
-      const Item it = decode_item(im, i, k_blocks);
+      const Item it = decode_item<Epi::kSplitK>(im, i, k_blocks);
       const int tile_row0 = it.m_tile * kPairRows + static_cast<int>(rank) * BM;
       epi.begin(ep, static_cast<long long>(tile_row0) + row_in_tile);
       for (int nt = it.n_begin; nt < it.n_end && ok; ++nt) {
@@ -974,7 +1002,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     tcgen05_fence_after_sync();
     tmem_dealloc_pair(tmem_base, kTmemCols);
   }
-  if (im_static.beside) wait_for_previous();
+  if (Epi::kChained && im_static.beside) wait_for_previous();
 }
 
 // ------------------------------------------------------------------------------------ host side
@@ -1061,6 +1089,8 @@ int launch_gemm(const Operand& a, const Operand& b, int splits, const typename E
   im.group_m = splits > 0 ? tuning_override("A3PO_GROUP_M", fwd_group_m(a.k_extent))
                : kForwardLike ? tuning_override("A3PO_GROUP_M_DZ", fwd_group_m(a.k_extent, BM * MT))
                               : tuning_override("A3PO_GROUP_M_GRAD", kGroupM);
+  if (!Epi::kSplitK && k_splits > 1) return A3PO_ERR_UNSUPPORTED;
+  if (!Epi::kChained && begin != Begin::kAfter) return A3PO_ERR_UNSUPPORTED;
   im.k_splits = k_splits > 1 ? k_splits : 1;
   im.k_split_rows = static_cast<long long>(im.m_tiles) * BM * MT;
   im.beside = begin == Begin::kBeside;
@@ -1141,6 +1171,7 @@ template <class Epi, bool A_MN, bool B_MN>
 int launch_pair_gemm(const Operand& a, const Operand& b, int splits, const typename Epi::Params& ep, const DynRows& dyn,
                      uint32_t* status, cudaStream_t stream, int group_m = kGroupM, bool paced = false,
                      Begin begin = Begin::kAfter) {
+  if (!Epi::kChained && begin != Begin::kAfter) return A3PO_ERR_UNSUPPORTED;
   const int pairs_max = pair_capacity<Epi, A_MN, B_MN>();
   if (pairs_max <= 0) return A3PO_ERR_UNSUPPORTED;
   CUtensorMap map_a, map_b, map_c;
