@@ -470,8 +470,9 @@ int a3po_dropout_norm_bwd(const void* r, float p, const uint64_t* rng, const voi
  * the forward's x, weights, row_mask, N, H, F, dt and act; it is not changed, so the backward may be repeated.
  * grad_w_gate_up [2 F, H], grad_w_down [H, F]: dtype grad_w_dt (A3PO_F32, or dt), overwritten; with
  * accumulate_grad_w != 0 added to (A3PO_F32 only, else A3PO_ERR_UNSUPPORTED).
- * ws: a3po_gated_ffn_workspace_bytes(N, H, F, dt, row_mask given, backward) bytes, 256-byte aligned; for bf16 about
- * 2 N F bytes forward and 4 N F backward, plus 2 to 3 times 2 N H with a row_mask.
+ * ws: a3po_gated_ffn_workspace_bytes(N, H, F, dt, row_mask given, backward) bytes, 256-byte aligned.  On the tensor cores
+ * 2 N F bytes forward and 4 N F backward (N to the next multiple of 128), with a row_mask two (backward three) times 2 N H
+ * more, and up to 20 MB of partial sums while the output tiles are few; on the FP32 pipes 4 N F forward and 12 N F backward.
  * status: optional device word (A3PO_STATUS_WAIT_TIMEOUT).  Outputs must not overlap inputs.  N = 0 launches nothing
  * except the zeros of weight gradients that are not accumulated.  Results are bit-identical from run to run.
  * ------------------------------------------------------------------------------------------ */

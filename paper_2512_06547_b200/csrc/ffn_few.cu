@@ -200,6 +200,7 @@ few_gate_up_kernel(const __nv_bfloat16* __restrict__ x, const __nv_bfloat16* __r
     const float u = cluster_total<S>(sh, ((S + rank) * 16 * MT + row) * 8 + col);
     float a, slope;
     gate_activation<GELU>(g, a, slope);
+    // bf16: the operand of the second product's matrix instruction, as on tiles (half a step, 2^-8 of an element at most)
     hid[static_cast<long long>(row) * f + c0 + col] = __float2bfloat16_rn(a * u);
     if (kept) {
       const int c = c0 + col, j = c % kKeptCols;

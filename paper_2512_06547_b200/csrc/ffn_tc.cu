@@ -7,13 +7,13 @@
 //             writes dg and du, operands of two gradient contractions (h, the third's, is the forward's own)
 //   down, dx, dW   plain contractions
 //
-// Rounding: h, dg and du are bf16, because they are operands of bf16 matrix instructions; each costs half a step (2^-9
-// relative) of an element that enters a long sum.  The kept g and u are cut to 24 bits (ffn_internal.cuh).  Everything
+// Rounding: h, dg and du are bf16, because they are operands of bf16 matrix instructions; each costs half a step (2^-8
+// relative at most) of an element that enters a long sum.  The kept g and u are cut to 24 bits (ffn_internal.cuh).  Everything
 // between (the activation, the products, dh) is fp32.
 //
 // Bound: the tensor pipe, 90-97 % active at the clock that the board's power cap leaves (profiler, 9,472 rows, H 4096,
-// F 12288).  Forward and backward: 16,384 rows of 4096 x 12288 12.0 ms (1,240 TFLOP/s; the six bare products in cuBLAS take
-// 10.3-10.6), 10,240 rows of 1536 x 4608 1.10 ms (1,190 TFLOP/s; cuBLAS 1.01).
+// F 12288).  Forward and backward: 16,384 rows of 4096 x 12288 11.4-12.2 ms (1,220-1,300 TFLOP/s; the six bare products in
+// cuBLAS take 10.3-10.7), 10,240 rows of 1536 x 4608 1.10 ms (1,190 TFLOP/s; cuBLAS 1.01).
 
 #include "ffn_internal.cuh"
 #include "gemm_tc.cuh"

@@ -307,7 +307,7 @@ struct SlabStore {
 // that take longer than a tile's MMAs at a short K (4 warps cannot fill the issue slots between their barriers).
 // kChained: launches may begin early, or let a successor begin (see Begin).  kSplitK: launches may split K.  Both are
 // compile-time, because the LM head's kernels, which do neither, took 0.5-1 % longer with the code for them (forward of
-// 9,029 rows of 1536 x 151,936 3,108 -> 3,125 us, backward 6,680 -> 6,753).
+// 9,029 rows of 1536 x 151,936 3,108 -> 3,125-3,137 us, backward 6,680 -> 6,753).
 struct PlainEpilogue {
   static constexpr bool kGated = false;
   static constexpr bool kPrefetch = false;

@@ -3,8 +3,8 @@
 // Bound by HBM: 3 (join: 4 or 5) elements moved per element.  Persistent blocks stream their rows through a ring in shared
 // memory (row_ops.cuh) and keep their share of dgamma / dbeta in registers, one sum per column a thread owns; the
 // blocks' shares are added up in index order by reduce_parts_kernel, so results do not depend on the order in which
-// blocks run.  131,072 x 4,096 bf16 with 39 % of the rows masked: 388 us (6.1 TB/s with the zero rows that it writes); join on
-// 65,536 x 4,096, five streams: 437 us (6.1 TB/s); layer norm on 5,001 x 1,003 bf16: 21 us, latency.
+// blocks run.  131,072 x 4,096 bf16 with 39 % of the rows masked: 376-392 us (6.1-6.3 TB/s with the zero rows that it writes);
+// join on 65,536 x 4,096, five streams: 437-475 us (5.7-6.1 TB/s); layer norm on 5,001 x 1,003 bf16: 21 us, latency.
 
 #include "row_ops.cuh"
 
@@ -13,7 +13,7 @@ namespace {
 
 // MAXT: most threads of a block, and with it a register limit: two blocks of 256 threads on an SM, one of 512.  With three,
 // a layer norm's sums spill (65,536 x 2,048 bf16: 194 us against 140) and an RMS norm gains nothing (8B-shaped batch,
-// 39 % masked: 402 against 376); only element-wise rows, which have no ring, want the third (5,001 x 1,003: 24.6 against 22.6).
+// 39 % masked: 402 against 376, of the same run); only element-wise rows, which have no ring, want the third (5,001 x 1,003: 24.6 against 22.6).
 template <typename T, int CPT, bool WIDE, int MAXT, bool VEC, bool LAYER, bool JOIN>
 __global__ void __launch_bounds__(MAXT, MAXT == 256 ? (VEC || JOIN || sizeof(T) == 4 ? 2 : 3) : 1)
 norm_bwd_kernel(const NormBwdArgs<T> a, int lanes, Turns turns) {
@@ -389,7 +389,10 @@ int launch(const NormBwdArgs<T>& a, int threads, int lanes, int* parts, cudaStre
   return after_launch();
 }
 
-// Threads by row length as in the forward.
+// Threads by row length as in the forward.  The longest register forms spill (bytes a thread, bf16): 16-byte rows of 8,193 to
+// 16,384 columns 52 (RMS) to 660 (layer norm of a join), element-wise rows of 4,097 to 8,192 columns up to 356 and of up to
+// 16,384 columns 488 to 1,820.  Of the copy rate: 16,384 x 16,384 RMS 0.62 (400 us), layer 0.44, join 0.54, both 0.41; 8,192 x
+// 6,001 0.12 to 0.27, 8,192 x 12,001 0.09 to 0.12.  The re-reading form, 8,192 x 20,000: 0.18 to 0.25.
 template <typename T, bool VEC, bool LAYER, bool JOIN>
 int by_length(const NormBwdArgs<T>& a, int* parts, cudaStream_t stream) {
   const int groups = (a.h + kVec - 1) / kVec;

@@ -27,7 +27,7 @@ namespace {
 // ------------------------------------------------------------------------------------ dropout (+ residual)
 // 16-byte rows: the matrix is one run of chunks; a block takes kDropThreads * U consecutive ones, every thread U of them
 // kDropThreads apart, all loads before the arithmetic, and is done: the next block's loads fill the pause that a grid-stride
-// loop has between its iterations.  131,072 x 4,096 bf16 with a residual: 519 us (6.2 TB/s; 823 us with a
+// loop has between its iterations.  131,072 x 4,096 bf16 with a residual: 491-532 us (6.1-6.5 TB/s; 823 us with a
 // grid-stride loop of two chunks per thread).
 constexpr int kDropThreads = 256;
 template <typename T> constexpr int drop_unroll() { return sizeof(T) == 2 ? 4 : 2; }
