@@ -491,6 +491,84 @@ int a3po_gated_ffn_bwd(const void* x, const void* w_gate_up, const void* w_down,
                        a3po_dtype grad_w_dt, int accumulate_grad_w, void* ws, size_t ws_bytes, uint32_t* status,
                        void* stream);
 
+/* --------------------------------------------------------------------------------------------
+ * Sampling of one token per row of logits (no counterpart in the paper: the rollout's side of the policy).  What it leaves in
+ * `logp` is the behaviour log-prob that the loss takes as behav_logp, by the definition of a3po_token_logprobs_fwd.
+ *
+ * A row with logits l (NaN counts as -inf) and temperature t, t <= 0 meaning greedy (with t = 1 below):
+ *   w_i = exp((l_i - max l) / t);  tokens are ranked by l, of equal logits the lower index first
+ *   top_k  keeps the k first ranks (k <= 0 or k >= V: all);
+ *   top_p  keeps of those the fewest first ranks whose weights reach top_p times the sum of theirs (top_p >= 1: all);
+ *   min_p  keeps of those the ones with w_i >= min_p (min_p <= 0: all);   the first rank is always kept, greedy keeps it alone
+ *   token     = the first kept i, in index order, at which the running sum of the kept weights exceeds u times their sum
+ *   logp      = log(w_token / sum of all w),   kept_logp = log(w_token / sum of the kept w)
+ *   n_kept    = number of kept tokens with a logit above -inf
+ * Weights carry 2^-32 of their value and sums 53 bits (the mass that top_p compares: multiples of 2^-43 of the largest weight),
+ * added in a fixed order: results are bit-identical from run to run, and a token differs from the one that exact sums give
+ * only where u lies within that of a border.
+ *
+ * logits [N, V], dtype `dt`, rows row_stride >= V elements apart, pointer aligned to its elements.  temperature, top_k, top_p,
+ * min_p: [N] or NULL (1, off, off, off); u fp32 [N] in [0, 1) (below 0 or NaN: 0; from 1 on: the last kept token).
+ * token int32 [N]; logp, kept_logp fp32 [N] and n_kept int32 [N] or NULL.  A row with row_mask 0 (uint8 [N] or NULL) is not read;
+ * it, and a row without a logit above -inf, gets token -1, logp 0, kept_logp 0, n_kept 0.
+ * With any of top_k, top_p, min_p a row has to fit the shared memory of eight SMs: V <= 393,216 (fp32) or 786,432 (bf16), else
+ * A3PO_ERR_UNSUPPORTED.  ws: a3po_sample_workspace_bytes(N, V), 256-byte aligned.  Outputs must not overlap inputs.
+ * ------------------------------------------------------------------------------------------ */
+size_t a3po_sample_workspace_bytes(int64_t N, int V);
+
+int a3po_sample(const void* logits, int64_t row_stride, const uint8_t* row_mask, int64_t N, int V, a3po_dtype dt,
+                const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
+                int32_t* token, float* logp, float* kept_logp, int32_t* n_kept, void* ws, size_t ws_bytes,
+                void* stream);
+
+/* --------------------------------------------------------------------------------------------
+ * AdamW over many tensors at once (no counterpart in the paper: what consumes the gradients of the step).
+ *
+ *   s  = min(1, max_grad_norm / (norm + 1e-6)),  norm over all gradients of the call;  s = 1 if max_grad_norm = 0
+ *   t  = *step + 1,  g = s grad
+ *   m' = beta1 m + (1 - beta1) g,   v' = beta2 v + (1 - beta2) g^2
+ *   w' = w - lr (weight_decay w + (m' / (1 - beta1^t)) / (sqrt(v' / (1 - beta2^t)) + eps))
+ *
+ * One a3po_adamw_tensor per tensor, n elements each (contiguous; 0 is valid):
+ *   weight   dtype weight_dt.  master: fp32 copy that is updated and then rounded into `weight` (weight_dt = A3PO_BF16 only), or
+ *            NULL: the weight itself is read, updated in fp32 and rounded once
+ *   grad     dtype grad_dt, not changed
+ *   m, v     state_bits = 32: fp32.  state_bits = 8: one byte per element in blocks of 256, with fp32 scales of
+ *            ceil(n / 256) blocks in m_scale and v_scale (all bytes and scales 0: states of 0).  A byte stands for
+ *            q(c) scale with q(c) = c below 8, else (8 + c mod 8) 2^(c div 8 - 1); in m bit 7 is the sign and c the rest.
+ *            New states are rounded to the nearest q of scale = (largest of the block) / q(largest code), halves to the even
+ *            code; a second moment above 0 is not rounded to 0.  The update itself uses the states before rounding.
+ *   weight_decay   of this tensor
+ * Pointers are aligned to their elements; tensors whose pointers allow it (four elements) move in wide pieces.  Tensors must not
+ * overlap one another.  The table is read by the host during the call and travels in the kernels' arguments.
+ * lr: fp32 device scalar.  step: int64 device scalar, steps taken so far, advanced by the call.  grad_norm: fp32 device
+ * scalar or NULL (the norm before clipping).  When the norm is asked for (grad_norm given or max_grad_norm > 0) and is not
+ * finite, nothing but grad_norm is written and *step stays.  beta1, beta2 in [0, 1), eps > 0.
+ * ws: a3po_adamw_workspace_bytes(count), 256-byte aligned.  The norm is a sum in 64 bits in a fixed order; results are
+ * bit-identical from run to run.
+ *
+ * a3po_adamw_state_values: what the bytes of an 8-bit state (is_signed: m) stand for, fp32 [n].
+ * ------------------------------------------------------------------------------------------ */
+typedef struct {
+  void* weight;
+  float* master;
+  const void* grad;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  int64_t n;
+  float weight_decay;
+} a3po_adamw_tensor;
+
+size_t a3po_adamw_workspace_bytes(int count);
+
+int a3po_adamw_step(const a3po_adamw_tensor* tensors, int count, a3po_dtype weight_dt, a3po_dtype grad_dt, int state_bits,
+                    double beta1, double beta2, float eps, float max_grad_norm, const float* lr, int64_t* step,
+                    float* grad_norm, void* ws, size_t ws_bytes, void* stream);
+
+int a3po_adamw_state_values(const uint8_t* codes, const float* scales, int64_t n, int is_signed, float* values, void* stream);
+
 /* Bytes the host entries of this library have copied host->device in the calling process since
  * load (monotonic; for transfer accounting in benchmarks). */
 int64_t a3po_host_to_device_bytes(void);

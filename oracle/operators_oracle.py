@@ -110,3 +110,89 @@ def gated_ffn_bwd(x, w_gate_up, w_down, grad_y, act="silu", mask=None):
     dh = gy @ wd
     dgu = np.concatenate([dh * u * da, dh * a], axis=1)
     return dgu @ wgu, dgu.T @ x, gy.T @ (a * u)
+
+
+# ------------------------------------------------------------------------------ sampling
+def sample_row(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """One row: token, logp, kept_logp, n_kept, and what they come from (w: all weights, kept: truth values by index).
+    None where no logit is above -inf."""
+    l = np.asarray(logits, dtype=np.float64)
+    l = np.where(np.isnan(l), -np.inf, l)
+    if not (l > -np.inf).any():
+        return None
+    top = l.max()
+    t = float(temperature) if temperature > 0 else 1.0
+    with np.errstate(invalid="ignore"):
+        w = np.where(l == top, 1.0, np.exp((l - top) / t))
+    order = np.lexsort((np.arange(l.size), -l))
+    n = l.size if top_k <= 0 else min(int(top_k), l.size)
+    if temperature <= 0:
+        n = 1
+    run = np.cumsum(w[order[:n]])
+    if float(np.float32(top_p)) < 1 and temperature > 0:
+        share = max(float(np.float32(top_p)), 0.0) * run[-1]
+        n = 1 + int((run[:-1] < share).sum())
+    if min_p > 0 and temperature > 0:
+        n = max(1, int((w[order[:n]] >= float(np.float32(min_p))).sum()))
+    kept = np.zeros(l.size, dtype=bool)
+    kept[order[:n]] = True
+    kept &= l > -np.inf
+    sums = np.cumsum(np.where(kept, w, 0.0))
+    over = np.flatnonzero(sums > max(float(u), 0.0) * sums[-1]) if u == u else np.flatnonzero(sums > 0)
+    token = int(over[0]) if over.size else int(np.flatnonzero(kept & (w > 0))[-1])
+    z = 0.0 if l[token] == top else (l[token] - top) / t
+    return dict(token=token, logp=z - np.log(w.sum()), kept_logp=z - np.log(sums[-1]), n_kept=int(kept.sum()), w=w,
+                kept=kept, sums=sums, order=order, z=z)
+
+
+# ------------------------------------------------------------------------------ AdamW
+STATE_BLOCK = 256
+
+
+def state_table(codes):
+    return np.array([c if c < 8 else (8 + c % 8) << (c // 8 - 1) for c in range(codes)], dtype=np.float64)
+
+
+def state_decode(codes, scales, signed):
+    """Values of an 8-bit state: codes [n], scales [ceil(n / 256)]."""
+    codes = np.asarray(codes, dtype=np.int64)
+    scale = np.repeat(np.asarray(scales, dtype=np.float64), STATE_BLOCK)[:codes.size]
+    if not signed:
+        return state_table(256)[codes] * scale
+    return state_table(128)[codes % 128] * np.where(codes >= 128, -1.0, 1.0) * scale
+
+
+def state_encode(x, signed):
+    """codes (uint8), scales (fp32) of values x [n], by search among the table's values; halves go to the even code."""
+    x = np.asarray(x, dtype=np.float64)
+    table = state_table(128 if signed else 256)
+    codes, scales = np.zeros(x.size, dtype=np.uint8), np.zeros(-(-x.size // STATE_BLOCK), dtype=np.float32)
+    for i in range(scales.size):
+        part = x[i * STATE_BLOCK:(i + 1) * STATE_BLOCK]
+        scales[i] = np.float32(np.abs(part).max() / table[-1])
+        a = np.abs(part) / np.float64(scales[i]) if scales[i] > 0 else np.zeros(part.size)
+        mid = (table[1:] + table[:-1]) / 2
+        c = np.searchsorted(mid, a, side="left")
+        tie = (c < mid.size) & (a == mid[np.minimum(c, mid.size - 1)]) & (c % 2 == 1)
+        c = c + tie
+        if signed:
+            c = np.where(part < 0, c + 128, c)
+        elif scales[i] > 0:
+            c = np.where(part > 0, np.maximum(c, 1), c)
+        codes[i * STATE_BLOCK:(i + 1) * STATE_BLOCK] = c
+    return codes, scales
+
+
+def adamw(w, g, m, v, t, lr, beta1, beta2, eps, decay, scale=1.0):
+    """One step on one tensor (t: number of this step): w', m', v'."""
+    g = np.asarray(g, dtype=np.float64) * scale
+    m = beta1 * m + (1 - beta1) * g
+    v = beta2 * v + (1 - beta2) * g * g
+    step = m / (1 - beta1 ** t) / (np.sqrt(v / (1 - beta2 ** t)) + eps)
+    return w - lr * (decay * w + step), m, v
+
+
+def clip_scale(grads, max_norm):
+    """Global norm of a list of gradients, and the factor that clipping puts on them (an fp32 number)."""
+    norm = math.sqrt(sum(float((np.asarray(g, dtype=np.float64) ** 2).sum()) for g in grads))
+    return norm, float(np.float32(min(1.0, max_norm / (norm + 1e-6)))) if max_norm > 0 else 1.0

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
 
 import torch
 
@@ -28,6 +28,12 @@ STATUS_KEPT_RANGE = 4
 
 class A3poStats(ctypes.Structure):
     _fields_ = [("n_valid", c_int64), ("n_clipped", c_int64), ("iw_max", c_float), ("iw_min", c_float)]
+
+
+class A3poAdamWTensor(ctypes.Structure):
+    """One entry of a3po_adamw_step's table (device addresses)."""
+    _fields_ = [("weight", c_void_p), ("master", c_void_p), ("grad", c_void_p), ("m", c_void_p), ("v", c_void_p),
+                ("m_scale", c_void_p), ("v_scale", c_void_p), ("n", c_int64), ("weight_decay", c_float)]
 
 
 class A3poError(RuntimeError):
@@ -108,6 +114,13 @@ _SIGNATURES = {
     "a3po_gated_ffn_bwd": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p, c_int64, c_int,
                                    c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_int, c_int, c_void_p, c_size_t,
                                    c_void_p, c_void_p]),
+    "a3po_sample_workspace_bytes": (c_size_t, [c_int64, c_int]),
+    "a3po_sample": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int, c_int, c_void_p, c_void_p, c_void_p, c_void_p,
+                            c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "a3po_adamw_workspace_bytes": (c_size_t, [c_int]),
+    "a3po_adamw_step": (c_int, [c_void_p, c_int, c_int, c_int, c_int, c_double, c_double, c_float, c_float, c_void_p, c_void_p,
+                                c_void_p, c_void_p, c_size_t, c_void_p]),
+    "a3po_adamw_state_values": (c_int, [c_void_p, c_void_p, c_int64, c_int, c_void_p, c_void_p]),
 }
 
 _lib = None
@@ -675,3 +688,67 @@ def a3po_gated_ffn_bwd(x, w_gate_up, w_down, kept, grad_y, grad_x, grad_w_gate_u
                                            _ptr(grad_w_gate_up), _ptr(grad_w_down), gdt, int(bool(accumulate_grad_w)),
                                            _ptr(ws), ws.numel(), _ptr(status), _stream(stream))
     _check("a3po_gated_ffn_bwd", rc)
+
+
+# ------------------------------------------------------------------------------ sampling
+def a3po_sample_workspace_bytes(N, V) -> int:
+    return load_library().a3po_sample_workspace_bytes(N, V)
+
+
+def a3po_sample(logits, u, token, ws, *, temperature=None, top_k=None, top_p=None, min_p=None, row_mask=None, logp=None,
+                kept_logp=None, n_kept=None, stream=None):
+    """One token per row of logits [N, V] (rows may lie apart) from given random numbers u in [0, 1); token -1: nothing to
+    sample.  logp: of the whole softmax (the behaviour log-prob of the loss), kept_logp: among the tokens that the filters
+    kept, n_kept of them.  temperature, top_p, min_p (fp32) and top_k (int32): one value per row, or None."""
+    dt = _dtype_code(logits)
+    if logits.dim() != 2:
+        raise ValueError("logits: expected [N, V]")
+    n, v = logits.shape
+    if not logits.is_cuda or (v > 1 and logits.stride(1) != 1) or (n > 1 and logits.stride(0) < v):
+        raise TypeError("logits: expected rows of neighbouring elements on cuda")
+    _here(logits, u, token, ws, temperature, top_k, top_p, min_p, row_mask, logp, kept_logp, n_kept)
+    for t, ty, nm in ((u, torch.float32, "u"), (token, torch.int32, "token"), (temperature, torch.float32, "temperature"),
+                      (top_k, torch.int32, "top_k"), (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p"),
+                      (row_mask, torch.uint8, "row_mask"), (logp, torch.float32, "logp"),
+                      (kept_logp, torch.float32, "kept_logp"), (n_kept, torch.int32, "n_kept")):
+        if t is not None:
+            _want(t, ty, nm)
+            if t.numel() != n:
+                raise ValueError(f"{nm}: expected one value per row")
+    _want(ws, torch.uint8, "ws")
+    rc = load_library().a3po_sample(_ptr(logits), logits.stride(0) if n > 1 else v, _ptr(row_mask), n, v, dt,
+                                    _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(token),
+                                    _ptr(logp), _ptr(kept_logp), _ptr(n_kept), _ptr(ws), ws.numel(), _stream(stream))
+    _check("a3po_sample", rc)
+
+
+# ------------------------------------------------------------------------------ AdamW
+def a3po_adamw_workspace_bytes(count) -> int:
+    return load_library().a3po_adamw_workspace_bytes(count)
+
+
+def a3po_adamw_step(table, weight_dt, grad_dt, state_bits, lr, step, ws, *, beta1=0.9, beta2=0.999, eps=1e-8,
+                    max_grad_norm=0.0, grad_norm=None, stream=None):
+    """One AdamW step over the tensors of `table`, a ctypes array of A3poAdamWTensor (optimizer.AdamW builds it from
+    tensors, which it checks)."""
+    _here(lr, step, ws, grad_norm)
+    _want(lr, torch.float32, "lr"); _want(step, torch.int64, "step"); _want(ws, torch.uint8, "ws")
+    _want(grad_norm, torch.float32, "grad_norm")
+    if lr.numel() != 1 or step.numel() != 1 or (grad_norm is not None and grad_norm.numel() != 1):
+        raise ValueError("lr, step and grad_norm: expected one element")
+    rc = load_library().a3po_adamw_step(ctypes.addressof(table), len(table), weight_dt, grad_dt, state_bits, beta1, beta2,
+                                        eps, max_grad_norm, _ptr(lr), _ptr(step), _ptr(grad_norm), _ptr(ws), ws.numel(),
+                                        _stream(stream))
+    _check("a3po_adamw_step", rc)
+
+
+def a3po_adamw_state_values(codes, scales, values, *, signed, stream=None):
+    """values (fp32) = what the bytes of an 8-bit optimizer state stand for."""
+    _here(codes, scales, values)
+    _want(codes, torch.uint8, "codes"); _want(scales, torch.float32, "scales"); _want(values, torch.float32, "values")
+    n = codes.numel()
+    if values.numel() != n or scales.numel() != -(-n // 256):
+        raise ValueError("shape mismatch")
+    _check("a3po_adamw_state_values",
+           load_library().a3po_adamw_state_values(_ptr(codes), _ptr(scales), n, int(bool(signed)), _ptr(values),
+                                                  _stream(stream)))

@@ -32,6 +32,7 @@ enum KernelId : int {
   kKMergePartials, kKSimtFwd, kKSimtDz, kKSimtGemm, kKTcFwd, kKTcDz, kKTcGradHidden, kKTcGradW, kKCompact, kKGrpo,
   kKSelfTest, kKTcFwdKeep, kKKeptRows, kKH2D, kKMoveRows,
   kKNorm, kKNormBwd, kKDropout, kKFfnGate, kKFfnDown, kKFfnGradGate, kKFfnGradX, kKFfnGradW, kKFfnFew, kKFfnSimt,
+  kKSample, kKSampleFilter, kKAdamNorm, kKAdamStep, kKLinear, kKLinearGradZ, kKLinearGradX, kKLinearGradW, kKLinearFew, kKLinearSimt,
   kKernelIdCount
 };
 

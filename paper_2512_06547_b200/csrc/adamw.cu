@@ -1,0 +1,477 @@
+// AdamW over many tensors at once, with the global gradient norm and its clip in the same call.
+//
+//   s  = min(1, max_norm / (norm + 1e-6)),  norm = sqrt(sum of the squares of all gradients),  g = s grad
+//   m' = b1 m + (1 - b1) g,   v' = b2 v + (1 - b2) g^2
+//   w' = w - lr (decay w + (m' / (1 - b1^t)) / (sqrt(v' / (1 - b2^t)) + eps))
+//
+// Three launches: sums of squares (64 bits, one number per block), the numbers of the step (norm, s, bias corrections; they
+// stay on the device, so that a captured graph follows them), the update.  The tensors come as a table in the kernel's
+// arguments: no table in device memory to keep, and a captured graph has its own.
+//
+// States are fp32, or 8 bits in blocks of 256 elements with an fp32 scale each: value = q(code) scale,
+// q(c) = c for c < 8, else (8 + c mod 8) 2^(c div 8 - 1).  First moment: a sign and codes to 127, q to 245,760 (half a step is
+// at most 1/16 of a value); second moment: codes to 255, q to 1.6e10, so that the smallest square root that is not 0 is
+// 1/127,000 of the largest.  A second moment above 0 is stored as 1 at least: 0 would leave eps alone under a first moment
+// that is not 0.  A block is a warp's work: its largest value is a warp reduction.
+// What is rounded to a code is computed in 64 bits, as a code is a step of several percent and two evaluations in 32 bits
+// would disagree about one in 10^5 of them; the update itself is fp32.
+//
+// Bound: HBM (32 bits: 30 bytes an element with fp32 gradients and masters beside bf16 weights, 18 with 8 bits, and 4 more for
+// the norm); with states of 8 bits the issue slots are about as far.
+
+#include <climits>
+
+#include "a3po_common.cuh"
+
+namespace a3po {
+namespace {
+
+constexpr int kBlock = 256;                 // elements that share a scale
+constexpr int kThreads = 256, kWarps = kThreads / kWarp;
+constexpr int kChunk = kWarps * kBlock;     // elements that a block takes at a time
+constexpr int kNormBlocks = 2048;           // sums of squares at most
+constexpr int kSmallTable = 32, kLargeTable = 400;
+
+struct Entry {
+  void* weight;
+  float* master;
+  const void* grad;
+  void *m, *v;
+  float *m_scale, *v_scale;
+  long long n;
+  float decay;
+  int wide;   // every pointer allows accesses of four elements
+};
+template <int CAP>
+struct Table {
+  Entry e[CAP];
+  int first[CAP + 1];   // chunks before entry i
+  int count;
+};
+
+struct Numbers {   // of the step, device memory
+  double g1, g2;   // (1 - b1) s and (1 - b2) s^2
+  float scale, lr, inv_bc1, inv_bc2;
+  int skip;
+};
+
+// Entry that holds a chunk.
+template <int CAP>
+__device__ __forceinline__ int entry_of(const Table<CAP>& t, int chunk) {
+  int lo = 0, hi = t.count - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (t.first[mid] <= chunk) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+// A lane's eight elements of a block of 256: four neighbours at 4 lane and at 128 + 4 lane where pointers allow it, else
+// element lane + 32 i.
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, int lane, int left, bool wide, float (&x)[8]) {
+  if (wide) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const T* q = p + h * 128 + lane * 4;
+      if (sizeof(T) == 4) {
+        const float4 f = __ldcs(reinterpret_cast<const float4*>(q));
+        x[h * 4] = f.x; x[h * 4 + 1] = f.y; x[h * 4 + 2] = f.z; x[h * 4 + 3] = f.w;
+      } else {
+        const uint2 u = __ldcs(reinterpret_cast<const uint2*>(q));
+        x[h * 4] = __uint_as_float(u.x << 16); x[h * 4 + 1] = __uint_as_float(u.x & 0xffff0000u);
+        x[h * 4 + 2] = __uint_as_float(u.y << 16); x[h * 4 + 3] = __uint_as_float(u.y & 0xffff0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = lane + 32 * i < left ? to_float(p[lane + 32 * i]) : 0.f;
+  }
+}
+__device__ __forceinline__ void store8(float* p, int lane, int left, bool wide, const float (&x)[8]) {
+  if (wide) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      __stcs(reinterpret_cast<float4*>(p + h * 128 + lane * 4), make_float4(x[h * 4], x[h * 4 + 1], x[h * 4 + 2], x[h * 4 + 3]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (lane + 32 * i < left) p[lane + 32 * i] = x[i];
+  }
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, int lane, int left, bool wide, const float (&x)[8]) {
+  if (wide) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const __nv_bfloat162 a = __floats2bfloat162_rn(x[h * 4], x[h * 4 + 1]), b = __floats2bfloat162_rn(x[h * 4 + 2], x[h * 4 + 3]);
+      uint2 u;
+      u.x = *reinterpret_cast<const uint32_t*>(&a);
+      u.y = *reinterpret_cast<const uint32_t*>(&b);
+      __stcs(reinterpret_cast<uint2*>(p + h * 128 + lane * 4), u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (lane + 32 * i < left) p[lane + 32 * i] = __float2bfloat16_rn(x[i]);
+  }
+}
+__device__ __forceinline__ void load8(const uint8_t* p, int lane, int left, bool wide, int (&c)[8]) {
+  if (wide) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t u = __ldcs(reinterpret_cast<const uint32_t*>(p + h * 128 + lane * 4));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[h * 4 + i] = u >> (8 * i) & 255;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = lane + 32 * i < left ? p[lane + 32 * i] : 0;
+  }
+}
+__device__ __forceinline__ void store8(uint8_t* p, int lane, int left, bool wide, const int (&c)[8]) {
+  if (wide) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      __stcs(reinterpret_cast<uint32_t*>(p + h * 128 + lane * 4),
+             static_cast<uint32_t>(c[h * 4] | c[h * 4 + 1] << 8 | c[h * 4 + 2] << 16 | c[h * 4 + 3] << 24));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (lane + 32 * i < left) p[lane + 32 * i] = static_cast<uint8_t>(c[i]);
+  }
+}
+
+// ------------------------------------------------------------------------------------ norm
+template <typename G, int CAP>
+__global__ void __launch_bounds__(kThreads)
+grad_norm_kernel(const __grid_constant__ Table<CAP> t, double* sums, int later) {
+  __shared__ double part[kWarps];
+  if (later) wait_for_previous();
+  allow_next();
+  const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
+  const int chunks = t.first[t.count];
+  int chunk = static_cast<int>(static_cast<long long>(chunks) * blockIdx.x / gridDim.x);
+  const int end = static_cast<int>(static_cast<long long>(chunks) * (blockIdx.x + 1) / gridDim.x);
+  double sum = 0.0;
+  int i = chunk < end ? entry_of(t, chunk) : 0;
+  for (; chunk < end; ++chunk) {
+    while (chunk >= t.first[i + 1]) ++i;
+    const Entry& e = t.e[i];
+    const long long at = static_cast<long long>(chunk - t.first[i]) * kChunk + warp * kBlock;
+    if (at >= e.n) continue;
+    const int left = static_cast<int>(e.n - at < kBlock ? e.n - at : kBlock);
+    float g[8];
+    load8(static_cast<const G*>(e.grad) + at, lane, left, e.wide && left == kBlock, g);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum = fma(static_cast<double>(g[k]), static_cast<double>(g[k]), sum);
+  }
+  sum = warp_sum(sum);
+  if (lane == 0) part[warp] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double s = 0.0;
+#pragma unroll
+    for (int k = 0; k < kWarps; ++k) s += part[k];
+    sums[blockIdx.x] = s;
+  }
+}
+
+// ------------------------------------------------------------------------------------ numbers of the step
+__global__ void __launch_bounds__(kThreads)
+step_numbers_kernel(const double* sums, int count, double b1, double b2, float max_norm, const float* lr, long long* step,
+                    float* grad_norm, Numbers* out) {
+  __shared__ double part[kWarps];
+  wait_for_previous();
+  allow_next();
+  double s = 0.0;
+  for (int i = threadIdx.x; i < count; i += kThreads) s += sums[i];
+  s = warp_sum(s);
+  if (threadIdx.x % kWarp == 0) part[threadIdx.x / kWarp] = s;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  s = 0.0;
+#pragma unroll
+  for (int k = 0; k < kWarps; ++k) s += part[k];
+  const double norm = sqrt(s);
+  float scale = 1.f;
+  if (max_norm > 0.f) scale = static_cast<float>(fmin(static_cast<double>(max_norm) / (norm + 1e-6), 1.0));
+  const bool skip = !isfinite(norm);
+  if (grad_norm) *grad_norm = static_cast<float>(norm);
+  const long long t = *step + 1;
+  if (!skip) *step = t;
+  out->g1 = (1.0 - b1) * scale;
+  out->g2 = (1.0 - b2) * scale * scale;
+  out->scale = scale;
+  out->lr = *lr;
+  out->inv_bc1 = static_cast<float>(1.0 / (1.0 - pow(b1, static_cast<double>(t))));
+  out->inv_bc2 = static_cast<float>(1.0 / (1.0 - pow(b2, static_cast<double>(t))));
+  out->skip = skip;
+}
+
+// ------------------------------------------------------------------------------------ update
+__host__ __device__ __forceinline__ double code_value(int c) {
+  return c < 8 ? static_cast<double>(c) : static_cast<double>(static_cast<long long>(8 + c % 8) << (c / 8 - 1));
+}
+// The code nearest to x >= 0 (in units of the scale): the leading four bits, halves to the even code.
+__device__ __forceinline__ int code_of(double x, int top) {
+  int c;
+  if (x < 8.0) {
+    c = __double2int_rn(x);
+  } else {
+    const unsigned long long b = static_cast<unsigned long long>(__double_as_longlong(x));
+    c = static_cast<int>((b + ((1ull << 48) - 1) + (b >> 49 & 1)) >> 49) - ((1023 + 3) << 3) + 8;
+  }
+  return c < top ? c : top;
+}
+// Largest of non-negative numbers over the warp (ordered as their bits are).
+__device__ __forceinline__ double warp_max64(double v) {
+  const uint32_t hi = static_cast<uint32_t>(__double2hiint(v)), lo = static_cast<uint32_t>(__double2loint(v));
+  const uint32_t top = __reduce_max_sync(0xffffffffu, hi);
+  const uint32_t low = __reduce_max_sync(0xffffffffu, hi == top ? lo : 0u);
+  return __hiloint2double(static_cast<int>(top), static_cast<int>(low));
+}
+
+template <typename W, typename G, int BITS, int CAP>
+__global__ void __launch_bounds__(kThreads)
+adamw_kernel(const __grid_constant__ Table<CAP> t, const Numbers* numbers, double b1, double b2, float eps) {
+  __shared__ double q[BITS == 8 ? 256 : 1];
+  if (BITS == 8) {
+    q[threadIdx.x] = code_value(threadIdx.x);
+    __syncthreads();
+  }
+  wait_for_previous();
+  allow_next();
+  const Numbers s = *numbers;
+  if (s.skip) return;   // gradients that are not finite: nothing changes
+  const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
+  const int chunks = t.first[t.count];
+  int chunk = static_cast<int>(static_cast<long long>(chunks) * blockIdx.x / gridDim.x);
+  const int end = static_cast<int>(static_cast<long long>(chunks) * (blockIdx.x + 1) / gridDim.x);
+  int i = chunk < end ? entry_of(t, chunk) : 0;
+  const float f1 = static_cast<float>(b1), f2 = static_cast<float>(b2);
+  const float h1 = static_cast<float>(1.0 - b1), h2 = static_cast<float>(1.0 - b2);
+  for (; chunk < end; ++chunk) {
+    while (chunk >= t.first[i + 1]) ++i;
+    const Entry& e = t.e[i];
+    const long long at = static_cast<long long>(chunk - t.first[i]) * kChunk + warp * kBlock;
+    if (at >= e.n) continue;   // the same for the warp
+    const int left = static_cast<int>(e.n - at < kBlock ? e.n - at : kBlock);
+    const bool wide = e.wide && left == kBlock;
+    float w[8], g[8], m[8], v[8];
+    if (sizeof(W) == 2 && e.master) load8(static_cast<const float*>(e.master) + at, lane, left, wide, w);
+    else load8(static_cast<const W*>(e.weight) + at, lane, left, wide, w);
+    load8(static_cast<const G*>(e.grad) + at, lane, left, wide, g);
+    if constexpr (BITS == 32) {
+      float* pm = static_cast<float*>(e.m) + at;
+      float* pv = static_cast<float*>(e.v) + at;
+      load8(pm, lane, left, wide, m);
+      load8(pv, lane, left, wide, v);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float x = g[k] * s.scale;
+        m[k] = fmaf(f1, m[k], h1 * x);
+        v[k] = fmaf(f2, v[k], h2 * x * x);
+      }
+      store8(pm, lane, left, wide, m);
+      store8(pv, lane, left, wide, v);
+    } else {
+      uint8_t* pm = static_cast<uint8_t*>(e.m) + at;
+      uint8_t* pv = static_cast<uint8_t*>(e.v) + at;
+      float *pms = e.m_scale + at / kBlock, *pvs = e.v_scale + at / kBlock;
+      int cm[8], cv[8];
+      load8(pm, lane, left, wide, cm);
+      load8(pv, lane, left, wide, cv);
+      const double ms = b1 * static_cast<double>(*pms), vs = b2 * static_cast<double>(*pvs);
+      double dm[8], dv[8], top_m = 0.0, top_v = 0.0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const double x = static_cast<double>(g[k]);
+        const double was = q[cm[k] & 127];
+        dm[k] = fma(cm[k] & 128 ? -was : was, ms, s.g1 * x);
+        dv[k] = fma(q[cv[k]], vs, s.g2 * (x * x));
+        top_m = fmax(top_m, fabs(dm[k]));
+        top_v = fmax(top_v, dv[k]);
+        m[k] = static_cast<float>(dm[k]);
+        v[k] = static_cast<float>(dv[k]);
+      }
+      const float new_ms = static_cast<float>(warp_max64(top_m) / code_value(127));
+      const float new_vs = static_cast<float>(warp_max64(top_v) / code_value(255));
+      const double inv_m = new_ms > 0.f ? 1.0 / static_cast<double>(new_ms) : 0.0;
+      const double inv_v = new_vs > 0.f ? 1.0 / static_cast<double>(new_vs) : 0.0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        cm[k] = code_of(fabs(dm[k]) * inv_m, 127) | (dm[k] < 0.0 ? 128 : 0);
+        cv[k] = code_of(dv[k] * inv_v, 255);
+        if (cv[k] == 0 && dv[k] > 0.0 && inv_v > 0.0) cv[k] = 1;
+      }
+      store8(pm, lane, left, wide, cm);
+      store8(pv, lane, left, wide, cv);
+      if (lane == 0) {
+        *pms = new_ms;
+        *pvs = new_vs;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float step = __fdividef(m[k] * s.inv_bc1, __fsqrt_rn(v[k] * s.inv_bc2) + eps);
+      w[k] = fmaf(-s.lr, fmaf(e.decay, w[k], step), w[k]);
+    }
+    if (sizeof(W) == 2 && e.master) store8(e.master + at, lane, left, wide, w);
+    store8(static_cast<W*>(e.weight) + at, lane, left, wide, w);
+  }
+}
+
+// ------------------------------------------------------------------------------------ host side
+bool aligned4(const void* p, size_t elt) { return aligned_to(p, 4 * elt); }
+
+template <int CAP>
+void fill(Table<CAP>* t, const a3po_adamw_tensor* tensors, int count, size_t ws, size_t gs, int bits) {
+  t->count = count;
+  int chunks = 0;
+  for (int i = 0; i < count; ++i) {
+    const a3po_adamw_tensor& x = tensors[i];
+    Entry& e = t->e[i];
+    e = Entry{x.weight, x.master, x.grad, x.m, x.v, x.m_scale, x.v_scale, x.n, x.weight_decay, 0};
+    const size_t ss = bits == 8 ? 1 : 4;
+    e.wide = aligned4(x.weight, ws) && aligned4(x.master, 4) && aligned4(x.grad, gs) && aligned4(x.m, ss) && aligned4(x.v, ss);
+    t->first[i] = chunks;
+    chunks += static_cast<int>((x.n + kChunk - 1) / kChunk);
+  }
+  t->first[count] = chunks;
+}
+
+template <typename W, typename G, int BITS, int CAP>
+int launch_update(const Table<CAP>& t, const Numbers* numbers, double b1, double b2, float eps, cudaStream_t s) {
+  const int chunks = t.first[t.count], most = sm_count() * 8;
+  if (chunks == 0) return A3PO_OK;
+  A3PO_LAUNCH(kKAdamStep, s, (launch_early(adamw_kernel<W, G, BITS, CAP>, chunks < most ? chunks : most, kThreads, 0, s, 1,
+                                           true, t, numbers, b1, b2, eps)));
+  return after_launch();
+}
+
+template <int CAP>
+int update(const a3po_adamw_tensor* tensors, int count, a3po_dtype wdt, a3po_dtype gdt, int bits, const Numbers* numbers,
+           double b1, double b2, float eps, cudaStream_t s) {
+  using B = __nv_bfloat16;
+  Table<CAP> t;
+  fill(&t, tensors, count, wdt == A3PO_F32 ? 4 : 2, gdt == A3PO_F32 ? 4 : 2, bits);
+#define A3PO_UPDATE(W, G)                                                                                      \
+  (bits == 8 ? launch_update<W, G, 8>(t, numbers, b1, b2, eps, s) : launch_update<W, G, 32>(t, numbers, b1, b2, eps, s))
+  if (wdt == A3PO_F32) return gdt == A3PO_F32 ? A3PO_UPDATE(float, float) : A3PO_UPDATE(float, B);
+  return gdt == A3PO_F32 ? A3PO_UPDATE(B, float) : A3PO_UPDATE(B, B);
+#undef A3PO_UPDATE
+}
+
+// Sums of squares of one table; returns their number through `blocks`.
+template <int CAP>
+int norm_sums(const a3po_adamw_tensor* tensors, int count, a3po_dtype gdt, double* sums, int room, bool later, int* blocks,
+              cudaStream_t s) {
+  Table<CAP> t;
+  fill(&t, tensors, count, 1, gdt == A3PO_F32 ? 4 : 2, 8);
+  for (int i = 0; i < count; ++i) t.e[i].wide = aligned4(tensors[i].grad, gdt == A3PO_F32 ? 4 : 2);
+  const int chunks = t.first[t.count];
+  int grid = sm_count() * 6 < chunks ? sm_count() * 6 : chunks;
+  if (grid > room) grid = room;
+  *blocks = grid;
+  if (grid == 0) return A3PO_OK;
+  if (gdt == A3PO_F32)
+    A3PO_LAUNCH(kKAdamNorm, s, (launch_early(grad_norm_kernel<float, CAP>, grid, kThreads, 0, s, 1, later, t, sums, later ? 1 : 0)));
+  else
+    A3PO_LAUNCH(kKAdamNorm, s, (launch_early(grad_norm_kernel<__nv_bfloat16, CAP>, grid, kThreads, 0, s, 1, later, t, sums,
+                                             later ? 1 : 0)));
+  return after_launch();
+}
+
+int norm_room(int count) {   // sums: kNormBlocks for each table of kLargeTable tensors
+  return (count + kLargeTable - 1) / kLargeTable * kNormBlocks;
+}
+
+__global__ void __launch_bounds__(256)
+state_values_kernel(const uint8_t* __restrict__ codes, const float* __restrict__ scales, long long n, int is_signed,
+                    float* __restrict__ out) {
+  for (long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<long long>(gridDim.x) * 256) {
+    const int c = codes[i];
+    const float v = static_cast<float>(code_value(is_signed ? c & 127 : c)) * scales[i / kBlock];
+    out[i] = is_signed && (c & 128) ? -v : v;
+  }
+}
+
+}  // namespace
+}  // namespace a3po
+
+using namespace a3po;
+
+extern "C" {
+
+size_t a3po_adamw_workspace_bytes(int count) {
+  if (count < 0) return 0;
+  return round_up(sizeof(Numbers), 256) + round_up(static_cast<size_t>(norm_room(count)) * sizeof(double), 256) + 256;
+}
+
+int a3po_adamw_step(const a3po_adamw_tensor* tensors, int count, a3po_dtype weight_dt, a3po_dtype grad_dt, int state_bits,
+                    double beta1, double beta2, float eps, float max_grad_norm, const float* lr, int64_t* step,
+                    float* grad_norm, void* ws, size_t ws_bytes, void* stream_) {
+  if (count < 0 || (count > 0 && !tensors) || !lr || !step) return A3PO_ERR_INVALID_ARG;
+  if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps > 0.f) || !(max_grad_norm >= 0.f))
+    return A3PO_ERR_INVALID_ARG;
+  if ((weight_dt != A3PO_F32 && weight_dt != A3PO_BF16) || (grad_dt != A3PO_F32 && grad_dt != A3PO_BF16)) return A3PO_ERR_UNSUPPORTED;
+  if (state_bits != 8 && state_bits != 32) return A3PO_ERR_UNSUPPORTED;
+  if (!aligned_to(lr, 4) || !aligned_to(step, 8) || !aligned_to(grad_norm, 4)) return A3PO_ERR_UNSUPPORTED;
+  const size_t wsz = weight_dt == A3PO_F32 ? 4 : 2, gsz = grad_dt == A3PO_F32 ? 4 : 2, ssz = state_bits == 8 ? 1 : 4;
+  long long chunks = 0;
+  for (int i = 0; i < count; ++i) {
+    const a3po_adamw_tensor& t = tensors[i];
+    if (t.n < 0 || (t.n > 0 && (!t.weight || !t.grad || !t.m || !t.v))) return A3PO_ERR_INVALID_ARG;
+    if (t.n > 0 && state_bits == 8 && (!t.m_scale || !t.v_scale)) return A3PO_ERR_INVALID_ARG;
+    if (t.master && weight_dt == A3PO_F32) return A3PO_ERR_INVALID_ARG;   // the weights are the masters
+    if (!aligned_to(t.weight, wsz) || !aligned_to(t.master, 4) || !aligned_to(t.grad, gsz) || !aligned_to(t.m, ssz) ||
+        !aligned_to(t.v, ssz) || !aligned_to(t.m_scale, 4) || !aligned_to(t.v_scale, 4))
+      return A3PO_ERR_UNSUPPORTED;
+    if (t.n > (1ll << 41)) return A3PO_ERR_UNSUPPORTED;
+    chunks += (t.n + kChunk - 1) / kChunk;
+  }
+  if (chunks > INT_MAX) return A3PO_ERR_UNSUPPORTED;
+  if (!ws || !aligned_to(ws, 256) || ws_bytes < a3po_adamw_workspace_bytes(count)) return A3PO_ERR_WORKSPACE;
+  if (sm_count() <= 0) return A3PO_ERR_NO_DEVICE;
+  cudaStream_t stream = as_stream(stream_);
+  Arena ar(ws, ws_bytes);
+  Numbers* numbers = ar.take<Numbers>(1);
+  double* sums = ar.take<double>(static_cast<size_t>(norm_room(count)));
+  if (!ar.ok()) return A3PO_ERR_WORKSPACE;
+  int total = 0;
+  bool launched = false;
+  if (max_grad_norm > 0.f || grad_norm) {
+    for (int i = 0; i < count; i += kLargeTable) {
+      const int part = count - i < kLargeTable ? count - i : kLargeTable;
+      int blocks = 0;
+      if (part <= kSmallTable) A3PO_RETURN_IF(norm_sums<kSmallTable>(tensors + i, part, grad_dt, sums + total, kNormBlocks, launched, &blocks, stream));
+      else A3PO_RETURN_IF(norm_sums<kLargeTable>(tensors + i, part, grad_dt, sums + total, kNormBlocks, launched, &blocks, stream));
+      total += blocks;
+      launched |= blocks > 0;
+    }
+  }
+  A3PO_LAUNCH(kKAdamNorm, stream, (launch_early(step_numbers_kernel, 1, kThreads, 0, stream, 1, launched,
+                                                static_cast<const double*>(sums), total, beta1, beta2, max_grad_norm, lr,
+                                                reinterpret_cast<long long*>(step), grad_norm, numbers)));
+  A3PO_RETURN_IF(after_launch());
+  for (int i = 0; i < count; i += kLargeTable) {
+    const int part = count - i < kLargeTable ? count - i : kLargeTable;
+    if (part <= kSmallTable) A3PO_RETURN_IF(update<kSmallTable>(tensors + i, part, weight_dt, grad_dt, state_bits, numbers, beta1, beta2, eps, stream));
+    else A3PO_RETURN_IF(update<kLargeTable>(tensors + i, part, weight_dt, grad_dt, state_bits, numbers, beta1, beta2, eps, stream));
+  }
+  return A3PO_OK;
+}
+
+int a3po_adamw_state_values(const uint8_t* codes, const float* scales, int64_t n, int is_signed, float* values, void* stream_) {
+  if (n < 0 || (n > 0 && (!codes || !scales || !values))) return A3PO_ERR_INVALID_ARG;
+  if (!aligned_to(scales, 4) || !aligned_to(values, 4)) return A3PO_ERR_UNSUPPORTED;
+  if (sm_count() <= 0) return A3PO_ERR_NO_DEVICE;
+  if (n == 0) return A3PO_OK;
+  cudaStream_t stream = as_stream(stream_);
+  const long long want = (n + 255) / 256, most = sm_count() * 16ll;
+  A3PO_LAUNCH(kKAdamStep, stream, (state_values_kernel<<<static_cast<unsigned>(want < most ? want : most), 256, 0, stream>>>(
+                                      codes, scales, n, is_signed, values)));
+  return after_launch();
+}
+
+}  // extern "C"

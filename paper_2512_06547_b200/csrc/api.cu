@@ -228,7 +228,9 @@ const char* a3po_kernel_name(int kernel_id) {
       "gemm_tn<fwd_logsoftmax>", "gemm_tn<dz>", "gemm_tn<grad_hidden>", "gemm_tn<grad_w>", "compact_rows", "grpo_advantages", "selftest",
       "gemm_tn<fwd_logsoftmax+keep>", "kept_rows", "h2d_copies", "move_kept_rows",
       "norm_fwd", "norm_bwd", "dropout", "gemm_tn<ffn_gate_up>", "gemm_tn<ffn_down>", "gemm_tn<ffn_grad_gate_up>",
-      "gemm_tn<ffn_grad_x>", "gemm_tn<ffn_grad_w>", "ffn_few_rows", "ffn_fp32pipe"};
+      "gemm_tn<ffn_grad_x>", "gemm_tn<ffn_grad_w>", "ffn_few_rows", "ffn_fp32pipe",
+      "sample", "sample_filter", "grad_norm", "adamw", "gemm_tn<linear>", "linear_grad_z", "gemm_tn<linear_grad_x>",
+      "gemm_tn<linear_grad_w>", "linear_few_rows", "linear_fp32pipe"};
   return (kernel_id >= 0 && kernel_id < kKernelIdCount) ? names[kernel_id] : "?";
 }
 

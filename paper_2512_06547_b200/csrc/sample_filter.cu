@@ -1,0 +1,640 @@
+// Sampling from rows with filters (top-k, top-p, min-p).  A row is spread over the shared memory of a cluster of up to
+// eight blocks, so that HBM is read once and all that follows runs on the copy:
+//
+//   largest logit, sum of all weights
+//   border of top-k: the key (the logit's bits, ordered) of the k-th token, by histograms of the key's leading bits, 11 at a
+//     time: at most three (bf16: two), each added up over the cluster and searched from the top
+//   border of top-p: the same with the weights of a histogram's keys instead of their number, as whole numbers of 2^-43, so
+//     that sums do not depend on the order of the atomics.  Tokens lighter than (1 - p) / V of all weight cannot be at the
+//     border and are not counted
+//   border of min-p: a logit
+//   ties at the border: kept up to an index, the c-th of them
+//   sums of the kept weights by stretches of the row, and the token in the stretch that the random number falls into
+//
+// A block's warps own stretches of neighbouring logits, and every sum is taken in a fixed order: results are
+// bit-identical from run to run.
+// Bound: latency (histograms and cluster barriers, about 2 us a level); several clusters share an SM.
+
+#include "sample.cuh"
+#include "sm100_ptx.cuh"
+
+namespace a3po {
+namespace {
+
+constexpr int kThreads = 512, kWarps = kThreads / kWarp, kMaxCluster = 8;
+constexpr int kBinBits = 11, kBins = 1 << kBinBits;
+constexpr int kMaxSlice = 196608;        // bytes of a row in one block
+constexpr int kSlots = 32;
+constexpr double kFixed = 8796093022208.0;   // 2^43: a weight as a whole number
+
+using u32 = uint32_t;
+using u64 = unsigned long long;
+
+__device__ __forceinline__ u32 key_of(float l) {
+  const u32 b = __float_as_uint(l);
+  return b ^ (b >> 31 ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float of_key(u32 k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); }
+// Keys as wide as the logits: a bf16 key is the upper half of the fp32 one.
+template <typename T> constexpr int key_drop() { return sizeof(T) == 2 ? 16 : 0; }
+template <typename T> __device__ __forceinline__ u32 tkey(float l) { return key_of(l) >> key_drop<T>(); }
+template <typename T> __device__ __forceinline__ float of_tkey(u32 k) {
+  const float l = of_key(k << key_drop<T>());
+  return sizeof(T) == 2 ? __uint_as_float(__float_as_uint(l) & 0xffff0000u) : l;
+}
+
+__device__ __forceinline__ u64 fixed_of(double w) {   // rounded to the nearest multiple of 2^-43; 0 <= w <= 1
+  constexpr double kMagic = 6755399441055744.0;       // 1.5 2^52
+  return static_cast<u64>(__double_as_longlong(fma(w, kFixed, kMagic)) - __double_as_longlong(kMagic));
+}
+
+struct Shared {
+  double table[kPowSteps];
+  u64 slot[kSlots][kMaxCluster];   // what the blocks of the cluster tell one another, each slot once
+  u64 part[2][kWarps];
+  int warp_count[kWarps];
+  u32 lo[kBins], hi[kBins];
+};
+
+__device__ __forceinline__ void store_remote(u64* here, u32 rank, u64 v) {
+  const u32 at = ptx::map_to_cta(static_cast<u32>(__cvta_generic_to_shared(here)), rank);
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(at), "l"(v) : "memory");
+}
+__device__ __forceinline__ u32 load_remote(const u32* here, u32 rank) {
+  const u32 at = ptx::map_to_cta(static_cast<u32>(__cvta_generic_to_shared(here)), rank);
+  u32 v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
+
+__device__ __forceinline__ u64 warp_sum64(u64 v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+template <typename T>
+struct Row {
+  Shared& sh;
+  const uint4* data;       // this block's slice, 16-byte pieces; places outside the slice hold -inf
+  int vecs;
+  int base;                // index in the row of place 0
+  int cluster, rank;
+  int flip, slot;
+  int lane, warp, v0, v1;  // this warp's pieces
+
+  __device__ __forceinline__ Row(Shared& s) : sh(s) {}
+
+  // ---- the cluster
+  __device__ __forceinline__ u64* tell(u64 v) {   // v: the same in all threads.  Seen by the others after sync()
+    u64* s = sh.slot[slot++];
+    if (threadIdx.x < static_cast<unsigned>(cluster)) store_remote(s + rank, threadIdx.x, v);
+    return s;
+  }
+  __device__ __forceinline__ void sync() { ptx::cluster_sync_all(); }
+  // Sum over the block's threads, in warp order, in all threads.
+  __device__ __forceinline__ u64 block_sum(u64 v) {
+    v = warp_sum64(v);
+    u64* p = sh.part[flip ^= 1];
+    if (lane == 0) p[warp] = v;
+    __syncthreads();
+    u64 t = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) t += p[i];
+    return t;
+  }
+  __device__ __forceinline__ double block_sum(double v) {
+    v = warp_sum(v);
+    u64* p = sh.part[flip ^= 1];
+    if (lane == 0) p[warp] = static_cast<u64>(__double_as_longlong(v));
+    __syncthreads();
+    double t = 0.0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) t += __longlong_as_double(static_cast<long long>(p[i]));
+    return t;
+  }
+  __device__ __forceinline__ u64 cluster_sum(u64 v) {
+    const u64* s = tell(block_sum(v));
+    sync();
+    u64 t = 0;
+    for (int r = 0; r < cluster; ++r) t += s[r];
+    return t;
+  }
+  __device__ __forceinline__ double cluster_sum(double v) {
+    const u64* s = tell(static_cast<u64>(__double_as_longlong(block_sum(v))));
+    sync();
+    double t = 0.0;
+    for (int r = 0; r < cluster; ++r) t += __longlong_as_double(static_cast<long long>(s[r]));
+    return t;
+  }
+  __device__ __forceinline__ u64 cluster_max(u32 v) {   // of 32-bit keys
+    v = __reduce_max_sync(0xffffffffu, v);
+    u64* p = sh.part[flip ^= 1];
+    if (lane == 0) p[warp] = v;
+    __syncthreads();
+    u64 t = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) t = max(t, p[i]);
+    const u64* s = tell(t);
+    sync();
+    for (int r = 0; r < cluster; ++r) t = max(t, s[r]);
+    return t;
+  }
+
+  // ---- the slice.  f(l, index) for the logits of this thread
+  __device__ __forceinline__ Vec<T> piece(int j) const {
+    const uint4 u = data[j];
+    Vec<T> v;
+    v.w[0] = u.x; v.w[1] = u.y; v.w[2] = u.z; v.w[3] = u.w;
+    return v;
+  }
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+    for (int j = v0 + lane; j < v1; j += kWarp) {
+      const Vec<T> v = piece(j);
+#pragma unroll
+      for (int e = 0; e < per_vec<T>(); ++e) f(v.at(e), base + j * per_vec<T>() + e);
+    }
+  }
+
+  // ---- the border of the `need` largest (each counting for amount(l)): the key at which the sum over larger keys and its own
+  // reaches `need`, among keys lo .. hi; above: the sum over larger keys.
+  template <bool MASS, class F>
+  __device__ __forceinline__ u32 border(u32 lo, u32 hi, u64 need, F amount, u64& above) {
+    above = 0;
+    for (;;) {
+      const u32 range = hi - lo;
+      const int bits = 32 - __clz(range);
+      const int shift = bits > kBinBits ? bits - kBinBits : 0;
+      for (int i = threadIdx.x; i < kBins; i += kThreads) {
+        sh.lo[i] = 0;
+        if (MASS) sh.hi[i] = 0;
+      }
+      __syncthreads();
+      each([&](float l, int) {
+        const u32 k = tkey<T>(l);
+        if (k < lo || k > hi) return;
+        const u32 bin = (k - lo) >> shift;
+        if (!MASS) {
+          atomicAdd(&sh.lo[bin], 1u);
+        } else {   // 64 bits from two words: the carry goes with the thread that saw it
+          const u64 x = amount(l);
+          const u32 xl = static_cast<u32>(x), old = atomicAdd(&sh.lo[bin], xl);
+          const u32 xh = static_cast<u32>(x >> 32) + (old + xl < old ? 1u : 0u);
+          if (xh) atomicAdd(&sh.hi[bin], xh);
+        }
+      });
+      sync();
+      // Rank 0 adds up the highest bins of the cluster, the last rank the lowest; a thread takes neighbouring ones, from
+      // the top down.
+      const int mine = kBins / cluster, per = (mine + kThreads - 1) / kThreads;
+      const int top = kBins - rank * mine;   // bins top - 1, top - 2, ...
+      u64 got[kBins / kThreads], sum = 0;
+#pragma unroll
+      for (int i = 0; i < kBins / kThreads; ++i) {
+        got[i] = 0;
+        const int at = static_cast<int>(threadIdx.x) * per + i;
+        if (i < per && at < mine) {
+          u32 words_hi = 0;
+          for (int r = 0; r < cluster; ++r) {
+            got[i] += load_remote(&sh.lo[top - 1 - at], r);
+            if (MASS) words_hi += load_remote(&sh.hi[top - 1 - at], r);
+          }
+          got[i] += static_cast<u64>(words_hi) << 32;
+          sum += got[i];
+        }
+      }
+      u64 inc = sum;
+#pragma unroll
+      for (int o = 1; o < kWarp; o <<= 1) {
+        const u64 y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+      }
+      u64* p = sh.part[flip ^= 1];
+      if (lane == kWarp - 1) p[warp] = inc;
+      __syncthreads();
+      u64 total = 0;
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) {
+        if (i < warp) inc += p[i];
+        total += p[i];
+      }
+      const u64* totals = tell(total);
+      u64* said_bin = sh.slot[slot++];
+      u64* said_above = sh.slot[slot++];
+      sync();
+      u64 before = 0;
+      int owner = cluster - 1;   // where rounding leaves `need` past the sum of all: the lowest bin that holds anything
+      for (int r = 0; r < cluster; ++r) {
+        if (before + totals[r] >= need) {
+          owner = r;
+          break;
+        }
+        if (r < cluster - 1) before += totals[r];
+      }
+      if (owner == rank) {
+        u64 run = before + inc - sum;   // over the bins above this thread's
+        const bool last = threadIdx.x == kThreads - 1;
+        if (run < need && (run + sum >= need || last)) {
+          int bin = 0;
+          u64 at = run;
+          bool found = false;
+#pragma unroll
+          for (int i = 0; i < kBins / kThreads; ++i) {
+            if (i < per && !found) {
+              bin = top - 1 - (static_cast<int>(threadIdx.x) * per + i);
+              at = run;
+              run += got[i];
+              found = run >= need;
+            }
+          }
+          if (bin < 0) bin = 0;
+          for (int r = 0; r < cluster; ++r) {
+            store_remote(said_bin, r, static_cast<u64>(bin));
+            store_remote(said_above, r, at);
+          }
+        }
+      }
+      sync();
+      const u32 bin = static_cast<u32>(said_bin[0]);
+      above += said_above[0];
+      need -= min(need - 1, said_above[0]);
+      lo += bin << shift;
+      if (shift == 0) return min(lo, hi);
+      hi = min(hi, lo + ((1u << shift) - 1u));
+      if (lo >= hi) return hi;
+    }
+  }
+};
+
+// The lowest place at which the running sum of x over a warp's stretch exceeds `want`; where rounding leaves none, the last with x > 0.
+// x(l, index): 0 for what does not count.
+template <typename T, class F>
+__device__ __forceinline__ int find_in_stretch(const Row<T>& row, double want, F x, float& picked) {
+  constexpr int VE = per_vec<T>();
+  double run = 0.0;
+  int last = -1;
+  float last_l = 0.f;
+  const int lane = row.lane;
+  for (int j0 = row.v0; j0 < row.v1; j0 += kWarp) {
+    const int j = j0 + lane;
+    double got[VE], sum = 0.0;
+    float l[VE];
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      got[e] = 0.0;
+      l[e] = -INFINITY;
+    }
+    if (j < row.v1) {
+      const Vec<T> v = row.piece(j);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        l[e] = v.at(e);
+        got[e] = x(l[e], row.base + j * VE + e);
+        sum += got[e];
+        if (got[e] > 0.0) {
+          last = row.base + j * VE + e;
+          last_l = l[e];
+        }
+      }
+    }
+    double inc = sum;
+#pragma unroll
+    for (int o = 1; o < kWarp; o <<= 1) {
+      const double y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
+    }
+    double prev = __shfl_up_sync(0xffffffffu, inc, 1);
+    prev = lane ? run + prev : run;
+    inc += run;
+    const unsigned over = __ballot_sync(0xffffffffu, sum > 0.0 && inc > want);   // inc is a tree of its own in each lane
+    if (over) {
+      const int src = __ffs(over) - 1;
+      int token = last;
+      float tl = last_l;
+      if (lane == src) {
+#pragma unroll
+        for (int e = VE - 1; e >= 0; --e) {
+          double upto = prev;
+#pragma unroll
+          for (int q = 0; q <= e; ++q) upto += got[q];
+          if (upto > want && got[e] > 0.0) {
+            token = row.base + j * VE + e;
+            tl = l[e];
+          }
+        }
+      }
+      picked = __shfl_sync(0xffffffffu, tl, src);
+      return __shfl_sync(0xffffffffu, token, src);
+    }
+    run = __shfl_sync(0xffffffffu, inc, kWarp - 1);
+  }
+  const int top = __reduce_max_sync(0xffffffffu, last);
+  const unsigned who = __ballot_sync(0xffffffffu, last == top);
+  picked = __shfl_sync(0xffffffffu, last_l, __ffs(who) - 1);
+  return top;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 2)
+sample_filter_kernel(SampleArgs a, int cluster, int slice) {
+  constexpr int VE = per_vec<T>();
+  extern __shared__ __align__(16) uint8_t smem[];
+  Shared& sh = *reinterpret_cast<Shared*>(smem);
+  uint4* data = reinterpret_cast<uint4*>(smem + (sizeof(Shared) + 15) / 16 * 16);
+  const int row_id = blockIdx.x / cluster;
+  if (a.row_mask && a.row_mask[row_id] == 0) {   // the same for the whole cluster
+    if (blockIdx.x % cluster == 0 && threadIdx.x == 0) a.put(row_id, -1, 0.0, 0.0, 0);
+    return;
+  }
+  Row<T> row(sh);
+  row.cluster = cluster;
+  row.rank = static_cast<int>(blockIdx.x % cluster);
+  row.flip = row.slot = 0;
+  row.lane = threadIdx.x % kWarp;
+  row.warp = threadIdx.x / kWarp;
+  for (int i = threadIdx.x; i < kPowSteps; i += kThreads) sh.table[i] = kPow2.t[i];
+
+  // ---- the slice into shared memory, NaN as -inf and -0 as 0
+  const int from = row.rank * slice, len = max(0, min(slice, a.v - from));
+  const T* l = static_cast<const T*>(a.logits) + row_id * a.ld + from;
+  const int head = head_of(l);
+  row.data = data;
+  row.vecs = len > 0 ? (head + len + VE - 1) / VE : 0;
+  row.base = from - head;
+  const int stretch = (row.vecs + kWarps - 1) / kWarps;
+  row.v0 = min(row.warp * stretch, row.vecs);
+  row.v1 = min(row.v0 + stretch, row.vecs);
+  constexpr int kAtOnce = 4;
+  u32 top = key_of(-INFINITY);
+  for (int j0 = row.v0 + row.lane; j0 < row.v1; j0 += kWarp * kAtOnce) {
+    Vec<T> v[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int j = j0 + i * kWarp;
+      if (j < row.v1) v[i] = load_vec(l, j * VE - head, len);
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int j = j0 + i * kWarp;
+      if (j >= row.v1) continue;
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        const float x = __fadd_rn(fmaxf(v[i].at(e), -INFINITY), 0.f);
+        top = max(top, key_of(x));
+        const u32 b = __float_as_uint(x);
+        if (sizeof(T) == 4) v[i].w[e] = b;
+        else v[i].w[e / 2] = e & 1 ? (v[i].w[e / 2] & 0xffffu) | (b & 0xffff0000u) : (v[i].w[e / 2] & 0xffff0000u) | b >> 16;
+      }
+      data[j] = make_uint4(v[i].w[0], v[i].w[1], v[i].w[2], v[i].w[3]);   // a warp reads its own stretch alone
+    }
+  }
+  row.sync();   // every block of the cluster runs: its shared memory may be written to
+  const float m = of_key(static_cast<u32>(row.cluster_max(top)));
+  if (!(m > -INFINITY)) {   // the same for the whole cluster
+    if (row.rank == 0 && threadIdx.x == 0) a.put(row_id, -1, 0.0, 0.0, 0);
+    row.sync();
+    return;
+  }
+  bool greedy;
+  const float t = a.temp(row_id, greedy);
+  Weights w;
+  w.set(m, t);
+  constexpr bool kExact = exact_diff<T>();
+  const double* table = sh.table;
+  auto weight = [&](float x) { return w.template operator()<kExact>(x, table); };
+  const int top_k = a.top_k ? a.top_k[row_id] : 0;
+  const float top_p = a.top_p ? a.top_p[row_id] : 1.f, min_p = a.min_p ? a.min_p[row_id] : 0.f;
+  const bool by_mass = top_p < 1.f && !greedy;
+
+  // ---- the sum of all weights; whole numbers too where shares of it are asked for
+  double total;
+  u64 all = 0;
+  {
+    double s = 0.0;
+    float low = 0.f;
+    if (by_mass && !(top_k > 0 && top_k < a.v)) {
+      row.each([&](float x, int) {
+        const double y = weight(x);
+        s += y;
+        all += fixed_of(y);
+      });
+      all = row.cluster_sum(all);
+    } else {
+      row.each([&](float x, int) {
+        double t64;
+        float t32, p;
+        if (w.template parts<kExact>(x, table, t64, t32, p)) {
+          s += t64;
+          low = fmaf(t32, p, low);
+        }
+      });
+    }
+    total = row.cluster_sum(s + static_cast<double>(low));
+  }
+
+  // ---- what is kept: keys above `edge`, and of those equal to it the first `ties` in index order
+  const u32 none = tkey<T>(-INFINITY), best = tkey<T>(m);
+  u32 edge = none;
+  int ties = 0;
+  if (greedy) {
+    edge = best;
+    ties = 1;
+  } else {
+    u64 above;
+    if (top_k > 0 && top_k < a.v) {
+      const u32 k = row.template border<false>(none, best, static_cast<u64>(top_k), [](float) { return 0ull; }, above);
+      if (k > none) {
+        edge = k;
+        ties = top_k - static_cast<int>(above);
+      }
+      if (by_mass) {   // the mass that top-p has a share of
+        const u32 e = edge;
+        all = 0;
+        row.each([&](float x, int) {
+          if (tkey<T>(x) > e) all += fixed_of(weight(x));
+        });
+        all = row.cluster_sum(all);
+        if (edge > none) all += static_cast<u64>(ties) * fixed_of(weight(of_tkey<T>(edge)));
+      }
+    }
+    if (by_mass) {
+      // 2^-48 less: a share that is reached exactly is reached
+      const double share = static_cast<double>(fmaxf(top_p, 0.f)) * static_cast<double>(all) * (1.0 - 0x1p-48);
+      const u64 need = share > 1.0 ? static_cast<u64>(ceil(share)) : 1;
+      u32 lo = edge;
+      if (edge == none) {   // lighter than (1 - p) / V of all: even together they are not the part that is left out
+        const double cut = (1.0 - static_cast<double>(fmaxf(top_p, 0.f))) * total / a.v * 0.999;
+        const double bound = static_cast<double>(m) + log(cut) * static_cast<double>(t);
+        const float f = bound < static_cast<double>(m) ? __double2float_rd(bound) : m;
+        lo = min(max(tkey<T>(f), none), best);
+      }
+      const u32 k = row.template border<true>(lo, best, need, [&](float x) { return fixed_of(weight(x)); }, above);
+      const u64 each = fixed_of(weight(of_tkey<T>(k)));
+      u64 c = each > 0 && need > above ? (need - above + each - 1) / each : 1;
+      if (c < 1) c = 1;
+      if (c > static_cast<u64>(a.v)) c = a.v;
+      if (k > edge || edge == none) {
+        edge = k;
+        ties = static_cast<int>(c);
+      } else if (static_cast<int>(c) < ties) {
+        ties = static_cast<int>(c);
+      }
+    }
+    if (min_p > 1.f) {
+      edge = best;
+      ties = 1;
+    } else if (min_p > 0.f) {
+      const double bound = static_cast<double>(m) + log(static_cast<double>(min_p)) * static_cast<double>(t);
+      float f = __double2float_ru(bound);   // the smallest logit that stays
+      if (f > m) f = m;
+      u32 k = tkey<T>(f + 0.f);
+      if (of_tkey<T>(k) < f) ++k;
+      if (k > edge) {
+        edge = k;
+        ties = INT_MAX;
+      }
+    }
+    if (edge == none) ties = 0;
+  }
+
+  // ---- the index of the last tie that is kept
+  int limit = INT_MAX;
+  if (ties < a.v && ties > 0) {
+    int c = 0;
+    row.each([&](float x, int) { c += tkey<T>(x) == edge ? 1 : 0; });
+    c = __reduce_add_sync(0xffffffffu, c);
+    if (row.lane == 0) sh.warp_count[row.warp] = c;
+    __syncthreads();
+    int block = 0, mine = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      if (i == row.warp) mine = block;
+      block += sh.warp_count[i];
+    }
+    const u64* s = row.tell(static_cast<u64>(block));
+    u64* said = sh.slot[row.slot++];
+    row.sync();
+    int before = 0, sum = 0;
+    for (int r = 0; r < cluster; ++r) {
+      if (r == row.rank) before = sum;
+      sum += static_cast<int>(s[r]);
+    }
+    if (sum > ties) {
+      const int from_here = ties - before - mine;   // the from_here-th of this warp's ties is the last
+      if (from_here >= 1 && from_here <= c) {
+        float unused;
+        const int at = find_in_stretch(row, from_here - 0.5, [&](float x, int) { return tkey<T>(x) == edge ? 1.0 : 0.0; },
+                                       unused);
+        if (row.lane == 0)
+          for (int r = 0; r < cluster; ++r) store_remote(said, r, static_cast<u64>(at));
+      }
+      row.sync();
+      limit = static_cast<int>(said[0]);
+    }
+  }
+  auto kept = [&](float x, int i) {
+    const u32 k = tkey<T>(x);
+    return k > edge || (k == edge && ties > 0 && i <= limit);
+  };
+
+  // ---- the kept weights by stretches
+  double s = 0.0;
+  int count = 0;
+  row.each([&](float x, int i) {
+    if (kept(x, i)) {
+      s += weight(x);
+      ++count;
+    }
+  });
+  s = warp_sum(s);
+  count = __reduce_add_sync(0xffffffffu, count);
+  __syncthreads();   // warp_count has been read
+  u64* sums = sh.part[row.flip ^= 1];
+  if (row.lane == 0) {
+    sums[row.warp] = static_cast<u64>(__double_as_longlong(s));
+    sh.warp_count[row.warp] = count;
+  }
+  __syncthreads();
+  double block = 0.0, mine = 0.0;
+  int block_count = 0;
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) {
+    if (i == row.warp) mine = block;
+    block += __longlong_as_double(static_cast<long long>(sums[i]));
+    block_count += sh.warp_count[i];
+  }
+  const u64* all_sums = row.tell(static_cast<u64>(__double_as_longlong(block)));
+  const u64* all_counts = row.tell(static_cast<u64>(block_count));
+  row.sync();
+  double kept_total = 0.0;
+  int kept_count = 0;
+  for (int r = 0; r < cluster; ++r) {
+    kept_total += __longlong_as_double(static_cast<long long>(all_sums[r]));
+    kept_count += static_cast<int>(all_counts[r]);
+  }
+  const double target = static_cast<double>(fmaxf(a.u[row_id], 0.f)) * kept_total;   // NaN and what is below 0 count as 0
+  // the block, and in it the stretch, that the target falls into; past the end the last that has any
+  double run = 0.0, at = 0.0;
+  int owner = 0;
+  for (int r = 0; r < cluster; ++r) {
+    const double x = __longlong_as_double(static_cast<long long>(all_sums[r]));
+    if (!(x > 0.0)) continue;
+    owner = r;
+    at = run;
+    run += x;
+    if (target < run) break;
+  }
+  if (owner == row.rank) {
+    const double rest = target - at;
+    double upto = 0.0, first = 0.0;
+    int who = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      const double x = __longlong_as_double(static_cast<long long>(sums[i]));
+      if (x > 0.0 && (upto <= rest || i == 0)) {
+        who = i;
+        first = upto;
+      }
+      upto += x;
+    }
+    if (who == row.warp) {
+      float picked;
+      const int token = find_in_stretch(row, rest - first, [&](float x, int i) { return kept(x, i) ? weight(x) : 0.0; }, picked);
+      if (row.lane == 0) {
+        const double z = picked == m ? 0.0 : (static_cast<double>(picked) - static_cast<double>(m)) / static_cast<double>(t);
+        a.put(row_id, token, z - log(total), z - log(kept_total), kept_count);
+      }
+    }
+  }
+  row.sync();   // no block leaves while another may still write to it
+}
+
+template <typename T>
+int filter_impl(const SampleArgs& a, cudaStream_t stream) {
+  // Blocks per row: as many as leave each at most 48 KB of logits (two blocks and their histograms share an SM then).
+  int cluster = 1;
+  while (cluster < kMaxCluster && static_cast<long long>(a.v) * static_cast<int>(sizeof(T)) > 49152ll * cluster) cluster *= 2;
+  const int slice = ((a.v + cluster - 1) / cluster + 7) / 8 * 8;
+  const size_t smem = (sizeof(Shared) + 15) / 16 * 16 + (static_cast<size_t>(slice) * sizeof(T) + 47) / 16 * 16;
+  if (cudaFuncSetAttribute(sample_filter_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) !=
+      cudaSuccess) {
+    cudaGetLastError();
+    return A3PO_ERR_CUDA;
+  }
+  A3PO_LAUNCH(kKSampleFilter, stream, (launch_early(sample_filter_kernel<T>, static_cast<unsigned>(a.n) * cluster, kThreads,
+                                                    smem, stream, cluster, false, a, cluster, slice)));
+  return after_launch();
+}
+
+}  // namespace
+
+long long sample_filter_max_v(a3po_dtype dt) { return static_cast<long long>(kMaxCluster) * kMaxSlice / (dt == A3PO_F32 ? 4 : 2); }
+
+int sample_filter(const void* args, a3po_dtype dt, cudaStream_t stream) {
+  const SampleArgs& a = *static_cast<const SampleArgs*>(args);
+  if (a.n > INT_MAX / kMaxCluster) return A3PO_ERR_UNSUPPORTED;
+  return dt == A3PO_F32 ? filter_impl<float>(a, stream) : filter_impl<__nv_bfloat16>(a, stream);
+}
+
+}  // namespace a3po

@@ -1,0 +1,302 @@
+// Sampling from rows without a filter: the logits are read once, front to back, by warps that know nothing of one another.
+//
+//   first kernel   a warp per segment of 1,024 logits: its largest m_s and S_s = sum exp((l - m_s) / t)
+//   second kernel  a block per row: m = max m_s, W = sum S_s exp((m_s - m) / t); the segment in which the running sum passes
+//                  u W is read again, by one warp, which finds the token
+//
+// Bound: the instructions of a weight (sample.cuh) for bf16 logits, HBM and those about alike for fp32.
+
+#include "sample.cuh"
+
+namespace a3po {
+namespace {
+
+constexpr int kSegment = 1024;   // elements, counted from the aligned start of a row
+constexpr int kSumThreads = 256, kPickThreads = 128;
+
+struct Segments {   // per row and segment, of rows that take part
+  double* sum;
+  float* max;
+  int* count;       // logits above -inf
+  int per_row;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kSumThreads)
+sample_sums_kernel(SampleArgs a, Segments out, int items) {
+  constexpr int VE = per_vec<T>(), kVecs = kSegment / VE / kWarp;
+  __shared__ double table[kPowSteps];
+  allow_next();
+  for (int i = threadIdx.x; i < kPowSteps; i += kSumThreads) table[i] = kPow2.t[i];
+  __syncthreads();
+  const int lane = threadIdx.x % kWarp;
+  const int warps = gridDim.x * (kSumThreads / kWarp);
+  for (int item = blockIdx.x * (kSumThreads / kWarp) + threadIdx.x / kWarp; item < items; item += warps) {
+    const int row = item / out.per_row, seg = item - row * out.per_row;
+    if (a.row_mask && a.row_mask[row] == 0) continue;
+    const T* l = static_cast<const T*>(a.logits) + row * a.ld;
+    const int head = head_of(l), first = seg * kSegment - head;
+    Vec<T> v[kVecs];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) v[i] = load_vec(l, first + (i * kWarp + lane) * VE, a.v);
+    bool greedy;
+    const float t = a.temp(row, greedy);
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+      for (int e = 0; e < VE; ++e) m = fmaxf(m, v[i].at(e));   // passes over NaN
+    m = warp_max(m);
+    double sum = 0.0;
+    if (m > -INFINITY) {
+      Weights w;
+      w.set(m, t);
+      float low = 0.f;
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+          double t64;
+          float t32, p;
+          if (w.parts<exact_diff<T>()>(v[i].at(e), table, t64, t32, p)) {
+            sum += t64;
+            low = fmaf(t32, p, low);
+          }
+        }
+      sum = warp_sum(sum + static_cast<double>(low));
+    }
+    if (a.n_kept) {
+      int c = 0;
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+        for (int e = 0; e < VE; ++e) c += v[i].at(e) > -INFINITY ? 1 : 0;
+      c = __reduce_add_sync(0xffffffffu, c);
+      if (lane == 0) out.count[item] = c;
+    }
+    if (lane == 0) {
+      out.sum[item] = sum;
+      out.max[item] = m;
+    }
+  }
+}
+
+// Inclusive sum over the block in thread order; `before`: that of the threads below.  (Each is a tree of its own, so a
+// thread that adds nothing may end a rounding away from its neighbour: only threads that add something are asked for.)
+__device__ __forceinline__ double block_scan(double x, double* sh, double& before, double& total) {
+  const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
+  double inc = x;
+#pragma unroll
+  for (int o = 1; o < kWarp; o <<= 1) {
+    const double y = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += y;
+  }
+  if (lane == kWarp - 1) sh[warp] = inc;
+  __syncthreads();
+  double base = 0.0;
+  total = 0.0;
+#pragma unroll
+  for (int i = 0; i < kPickThreads / kWarp; ++i) {
+    if (i == warp) base = total;
+    total += sh[i];
+  }
+  double prev = __shfl_up_sync(0xffffffffu, inc, 1);
+  before = lane ? base + prev : base;
+  return lane == kWarp - 1 ? base + sh[warp] : base + inc;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kPickThreads)
+sample_pick_kernel(SampleArgs a, Segments in) {
+  constexpr int VE = per_vec<T>();
+  __shared__ double table[kPowSteps], sh_scan[kPickThreads / kWarp], sh_target, sh_total;
+  __shared__ float sh_max[kPickThreads / kWarp];
+  __shared__ int sh_seg, sh_first, sh_last, sh_count;
+  const int row = blockIdx.x, lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
+  if (a.row_mask && a.row_mask[row] == 0) {
+    if (threadIdx.x == 0) a.put(row, -1, 0.0, 0.0, 0);
+    return;
+  }
+  for (int i = threadIdx.x; i < kPowSteps; i += kPickThreads) table[i] = kPow2.t[i];
+  if (threadIdx.x == 0) {
+    sh_seg = sh_first = INT_MAX;
+    sh_last = -1;
+    sh_count = 0;
+  }
+  bool greedy;
+  const float t = a.temp(row, greedy);
+  const double inv_t = 1.0 / static_cast<double>(t);
+  wait_for_previous();
+  const double* sums = in.sum + static_cast<long long>(row) * in.per_row;
+  const float* maxes = in.max + static_cast<long long>(row) * in.per_row;
+  const int* counts = in.count + static_cast<long long>(row) * in.per_row;
+  // a thread takes `per` neighbouring segments
+  const int per = (in.per_row + kPickThreads - 1) / kPickThreads;
+  const int s0 = min(static_cast<int>(threadIdx.x) * per, in.per_row), s1 = min(s0 + per, in.per_row);
+  float m = -INFINITY;
+  int count = 0;
+  for (int s = s0; s < s1; ++s) {
+    m = fmaxf(m, maxes[s]);
+    if (a.n_kept) count += counts[s];
+  }
+  m = warp_max(m);
+  if (lane == 0) sh_max[warp] = m;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kPickThreads / kWarp; ++i) m = fmaxf(m, sh_max[i]);
+  if (!(m > -INFINITY)) {   // nothing to sample; the same for all threads
+    if (threadIdx.x == 0) a.put(row, -1, 0.0, 0.0, 0);
+    return;
+  }
+  if (a.n_kept) {
+    count = __reduce_add_sync(0xffffffffu, count);
+    if (lane == 0) atomicAdd(&sh_count, count);   // whole numbers: in any order
+  }
+  // what a segment's sum counts for in the row's
+  auto factor = [&](float seg_max) {
+    return seg_max == m ? 1.0 : exp((static_cast<double>(seg_max) - static_cast<double>(m)) * inv_t);
+  };
+  double mine = 0.0;
+  for (int s = s0; s < s1; ++s)
+    if (maxes[s] > -INFINITY) mine += sums[s] * factor(maxes[s]);
+  double before, total;
+  const double upto = block_scan(mine, sh_scan, before, total);
+  const double target = static_cast<double>(fmaxf(a.u[row], 0.f)) * total;   // NaN and what is below 0 count as 0
+  if (mine > 0.0) {
+    if (target < upto) atomicMin(&sh_first, static_cast<int>(threadIdx.x));
+    atomicMax(&sh_last, static_cast<int>(threadIdx.x));
+  }
+  __syncthreads();
+  // the thread whose share the target falls into; past the end (u >= 1): the last that has any
+  const bool here = static_cast<int>(threadIdx.x) == (sh_first < kPickThreads ? sh_first : sh_last);
+  if (greedy) {
+    for (int s = s0; s < s1; ++s)
+      if (maxes[s] == m) {
+        atomicMin(&sh_seg, s);
+        break;
+      }
+  } else if (here) {
+    double run = before, at = before;
+    int seg = -1;
+    for (int s = s0; s < s1; ++s) {
+      if (!(maxes[s] > -INFINITY)) continue;
+      const double x = sums[s] * factor(maxes[s]);
+      if (!(x > 0.0)) continue;
+      seg = s;
+      at = run;
+      run += x;
+      if (target < run) break;
+    }
+    sh_seg = seg;
+    sh_target = (target - at) / factor(maxes[seg]);
+  }
+  if (threadIdx.x == 0) sh_total = total;
+  __syncthreads();
+  if (warp != 0) return;
+  const int seg = min(sh_seg, in.per_row - 1);
+  const T* l = static_cast<const T*>(a.logits) + row * a.ld;
+  const int head = head_of(l);
+  const float seg_max = maxes[seg];
+  Weights w;
+  w.set(seg_max, t);
+  double run = 0.0;
+  const double want = greedy ? 0.0 : sh_target;
+  int token = -1;         // of this lane
+  float picked = 0.f;
+  int last = -1;          // the last element with a weight: rounding may leave the target past the segment's sum
+  float last_l = 0.f;
+  for (int i = 0; i < kSegment / VE / kWarp; ++i) {
+    const int first = seg * kSegment - head + (i * kWarp + lane) * VE;
+    const Vec<T> v = load_vec(l, first, a.v);
+    double x[VE], sum = 0.0;
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      const float le = v.at(e);
+      x[e] = greedy ? (le == m ? 1.0 : 0.0) : w.template operator()<exact_diff<T>()>(le, table);
+      sum += x[e];
+      if (x[e] > 0.0) {
+        last = first + e;
+        last_l = le;
+      }
+    }
+    double inc = sum;
+#pragma unroll
+    for (int o = 1; o < kWarp; o <<= 1) {
+      const double y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
+    }
+    double prev = __shfl_up_sync(0xffffffffu, inc, 1);
+    prev = lane ? run + prev : run;
+    inc += run;
+    const unsigned over = __ballot_sync(0xffffffffu, sum > 0.0 && inc > want);
+    if (over) {
+      if (lane == __ffs(over) - 1) {
+        double at = prev;
+        token = last;        // of this vector, unless one before it passes the target
+        picked = last_l;
+#pragma unroll
+        for (int e = VE - 1; e >= 0; --e) {   // from the back: the first that passes is written last
+          double upto_e = at;
+#pragma unroll
+          for (int q = 0; q <= e; ++q) upto_e += x[q];
+          if (upto_e > want && x[e] > 0.0) {
+            token = first + e;
+            picked = v.at(e);
+          }
+        }
+      }
+      const int src = __ffs(over) - 1;
+      token = __shfl_sync(0xffffffffu, token, src);
+      picked = __shfl_sync(0xffffffffu, picked, src);
+      break;
+    }
+    run = __shfl_sync(0xffffffffu, inc, kWarp - 1);
+  }
+  if (token < 0) {
+    const int top = __reduce_max_sync(0xffffffffu, last);
+    const unsigned who = __ballot_sync(0xffffffffu, last == top);
+    token = top;
+    picked = __shfl_sync(0xffffffffu, last_l, __ffs(who) - 1);
+  }
+  if (lane == 0) {
+    const double z = picked == m ? 0.0 : (static_cast<double>(picked) - static_cast<double>(m)) * inv_t;
+    const double lp = z - log(sh_total);
+    a.put(row, token, lp, greedy ? 0.0 : lp, greedy ? 1 : sh_count);
+  }
+}
+
+template <typename T>
+int stream_impl(const SampleArgs& a, const Segments& seg, cudaStream_t stream) {
+  const int items = a.n * seg.per_row;
+  constexpr int kWarps = kSumThreads / kWarp;
+  const int want = (items + kWarps - 1) / kWarps, most = sm_count() * 8;
+  A3PO_LAUNCH(kKSample, stream, (sample_sums_kernel<T><<<want < most ? want : most, kSumThreads, 0, stream>>>(a, seg, items)));
+  A3PO_RETURN_IF(after_launch());
+  A3PO_LAUNCH(kKSample, stream, (launch_early(sample_pick_kernel<T>, a.n, kPickThreads, 0, stream, 1, true, a, seg)));
+  return after_launch();
+}
+
+// A row that starts inside 16 bytes needs up to 7 places before its first element.
+long long segments_per_row(int v) { return (static_cast<long long>(v) + 7 + kSegment - 1) / kSegment; }
+
+}  // namespace
+
+size_t sample_stream_bytes(long long n, int v) {
+  const size_t items = static_cast<size_t>(n) * static_cast<size_t>(segments_per_row(v));
+  return round_up(items * sizeof(double), 256) + round_up(items * sizeof(float), 256) + round_up(items * sizeof(int), 256);
+}
+
+int sample_stream(const void* args, a3po_dtype dt, void* ws, cudaStream_t stream) {
+  const SampleArgs& a = *static_cast<const SampleArgs*>(args);
+  const size_t items = static_cast<size_t>(a.n) * static_cast<size_t>(segments_per_row(a.v));
+  if (items > static_cast<size_t>(INT_MAX) / 2) return A3PO_ERR_UNSUPPORTED;
+  Arena ar(ws, sample_stream_bytes(a.n, a.v));
+  Segments seg;
+  seg.sum = ar.take<double>(items);
+  seg.max = ar.take<float>(items);
+  seg.count = ar.take<int>(items);
+  seg.per_row = static_cast<int>(segments_per_row(a.v));
+  return dt == A3PO_F32 ? stream_impl<float>(a, seg, stream) : stream_impl<__nv_bfloat16>(a, seg, stream);
+}
+
+}  // namespace a3po

@@ -1,0 +1,113 @@
+"""AdamW over a list of tensors through a3po_adamw_step: one call for the gradient norm, its clip and the update of every
+tensor, with states in 32 or 8 bits and fp32 masters of bf16 weights.  The count of steps and the learning rate are device words,
+so a step can be captured into a CUDA graph (after one uncaptured step) and replayed with another rate."""
+from __future__ import annotations
+
+import torch
+
+from . import binding as b
+
+STATE_BLOCK = 256   # elements of an 8-bit state that share a scale
+
+
+def decode_state(codes, scales, *, signed, out=None):
+    """fp32 values of an 8-bit state: codes uint8 [n], scales fp32 [ceil(n / 256)]; signed: a first moment."""
+    out = torch.empty(codes.shape, dtype=torch.float32, device=codes.device) if out is None else out
+    b.a3po_adamw_state_values(codes, scales, out, signed=signed)
+    return out
+
+
+def _like(given, weights, dtype, name, sizes=None):
+    sizes = [w.numel() for w in weights] if sizes is None else sizes
+    if given is None:
+        return [torch.zeros(n, dtype=dtype, device=w.device) for n, w in zip(sizes, weights)]
+    given = list(given)
+    if len(given) != len(weights):
+        raise ValueError(f"{name}: expected one tensor per weight")
+    for t, n in zip(given, sizes):
+        b._want(t, dtype, name)
+        if t.numel() != n:
+            raise ValueError(f"{name}: expected {n} elements, got {t.numel()}")
+    b._here(*given)
+    return given
+
+
+class AdamW:
+    """weights: contiguous tensors of one type (fp32 or bf16), updated in place by step(grads).
+
+    lr: a number, or an fp32 device scalar that the caller changes between steps.  weight_decay: a number, or one per weight.
+    max_grad_norm: 0 for no clipping; grad_norm holds the norm of the last step's gradients before clipping either way.  A
+    step whose norm is not finite changes nothing.  state_bits: 32 or 8.  masters: True (bf16 weights) keeps an fp32
+    copy of each weight, which is what is updated; a list gives the copies.  m, v, m_scales, v_scales, step: states to go on from
+    (kept and updated in place), as this object's attributes of these names hold them."""
+
+    def __init__(self, weights, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, *, max_grad_norm=0.0, state_bits=32,
+                 masters=None, m=None, v=None, m_scales=None, v_scales=None, step=None):
+        self.weights = list(weights)
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits: 8 or 32")
+        dtype = self.weights[0].dtype if self.weights else torch.float32
+        self._weight_dt = b._dtype_code(self.weights[0]) if self.weights else b.A3PO_F32
+        for w in self.weights:
+            b._want(w, dtype, "weights")
+        b._here(*self.weights)
+        if len({w.data_ptr() for w in self.weights if w.numel()}) < sum(w.numel() > 0 for w in self.weights):
+            raise ValueError("weights: the same tensor twice")
+        device = self.weights[0].device if self.weights else torch.device("cuda", torch.cuda.current_device())
+        count = len(self.weights)
+        decay = [float(weight_decay)] * count if isinstance(weight_decay, (int, float)) else [float(d) for d in weight_decay]
+        if len(decay) != count:
+            raise ValueError("weight_decay: expected a number or one per weight")
+        if masters is True:
+            masters = [w.float() for w in self.weights]
+        if masters is not None and masters is not False:
+            if dtype == torch.float32:
+                raise ValueError("masters: fp32 weights are their own")
+            self.masters = _like(masters, self.weights, torch.float32, "masters")
+        else:
+            self.masters = None
+        state = torch.uint8 if state_bits == 8 else torch.float32
+        self.m, self.v = _like(m, self.weights, state, "m"), _like(v, self.weights, state, "v")
+        self.m_scales = self.v_scales = None
+        if state_bits == 8:
+            blocks = [-(-w.numel() // STATE_BLOCK) for w in self.weights]
+            self.m_scales = _like(m_scales, self.weights, torch.float32, "m_scales", blocks)
+            self.v_scales = _like(v_scales, self.weights, torch.float32, "v_scales", blocks)
+        elif m_scales is not None or v_scales is not None:
+            raise ValueError("m_scales, v_scales: of states of 8 bits only")
+        self.lr = lr if isinstance(lr, torch.Tensor) else torch.full((1,), float(lr), device=device)
+        self.steps = torch.zeros(1, dtype=torch.int64, device=device) if step is None else step
+        self.grad_norm = torch.zeros(1, device=device)
+        self.state_bits, self.eps, self.max_grad_norm = state_bits, float(eps), float(max_grad_norm)
+        self.beta1, self.beta2 = float(betas[0]), float(betas[1])
+        self._ws = b.new_workspace(b.a3po_adamw_workspace_bytes(count), device)
+        self._table = (b.A3poAdamWTensor * count)()
+        self._grads, self._grad_dt = [None] * count, b.A3PO_F32
+        at = lambda tensors, i: None if tensors is None else tensors[i].data_ptr()
+        for i, w in enumerate(self.weights):
+            self._table[i] = b.A3poAdamWTensor(w.data_ptr(), at(self.masters, i), None, at(self.m, i), at(self.v, i),
+                                               at(self.m_scales, i), at(self.v_scales, i), w.numel(), decay[i])
+
+    def step(self, grads, *, stream=None):
+        """grads: one tensor per weight, of its size, all fp32 or all bf16."""
+        if len(grads) != len(self.weights):
+            raise ValueError("grads: expected one tensor per weight")
+        fresh = [i for i, g in enumerate(grads) if g is not self._grads[i]]
+        dtype = grads[0].dtype if grads else torch.float32
+        for i, g in enumerate(grads):
+            if g.dtype is not dtype:
+                raise TypeError("grads: expected tensors of one type")
+        for i in fresh:
+            g = grads[i]
+            b._want(g, dtype, "grads")
+            b._here(g)
+            if g.numel() != self.weights[i].numel():
+                raise ValueError("grads: expected the size of the weight")
+        if grads:
+            self._grad_dt = b._dtype_code(grads[0])
+        for i, g in enumerate(grads):   # storage may have moved under a tensor that was seen before
+            self._table[i].grad = g.data_ptr()
+            self._grads[i] = g
+        b.a3po_adamw_step(self._table, self._weight_dt, self._grad_dt, self.state_bits, self.lr, self.steps, self._ws,
+                          beta1=self.beta1, beta2=self.beta2, eps=self.eps, max_grad_norm=self.max_grad_norm,
+                          grad_norm=self.grad_norm, stream=stream)
