@@ -22,7 +22,7 @@ def test_refusals(lib):
     n, v = 8, 1000
     wb = a3po.a3po_sample_workspace_bytes(n, v)
     assert wb > 0 and a3po.a3po_sample_workspace_bytes(-1, v) == 0 and a3po.a3po_sample_workspace_bytes(n, 0) == 0
-    assert a3po.a3po_sample_workspace_bytes(2 * n, v) > wb
+    assert a3po.a3po_sample_workspace_bytes(200 * n, v) > wb
 
     def call(logits=ONE, ld=v, n=n, v=v, dt=F32, t=None, k=None, p=None, mp=None, u=ONE, token=ONE, logp=None, klp=None,
              kept=None, ws=ONE, wbytes=1 << 40):
