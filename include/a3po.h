@@ -476,7 +476,8 @@ int a3po_dropout_norm_bwd(const void* r, float p, const uint64_t* rng, const voi
  * status: optional device word (A3PO_STATUS_WAIT_TIMEOUT).  Outputs must not overlap inputs.  N = 0 launches nothing
  * except the zeros of weight gradients that are not accumulated.  Results are bit-identical from run to run.
  * ------------------------------------------------------------------------------------------ */
-typedef enum { A3PO_ACT_SILU = 0, A3PO_ACT_GELU_TANH = 1 } a3po_activation;
+/* A3PO_ACT_NONE is for the linear operator; the gated block refuses it. */
+typedef enum { A3PO_ACT_SILU = 0, A3PO_ACT_GELU_TANH = 1, A3PO_ACT_NONE = 2 } a3po_activation;
 
 size_t a3po_gated_ffn_kept_bytes(int64_t N, int F, a3po_dtype dt);
 size_t a3po_gated_ffn_workspace_bytes(int64_t N, int H, int F, a3po_dtype dt, int has_row_mask, int is_bwd);
@@ -490,6 +491,42 @@ int a3po_gated_ffn_bwd(const void* x, const void* w_gate_up, const void* w_down,
                        a3po_activation act, void* grad_x, void* grad_w_gate_up, void* grad_w_down,
                        a3po_dtype grad_w_dt, int accumulate_grad_w, void* ws, size_t ws_bytes, uint32_t* status,
                        void* stream);
+
+/* --------------------------------------------------------------------------------------------
+ * Linear operator (no counterpart in the paper): projections onto the residual stream, biased layers, the logits of the next token.
+ *
+ *   z = x W^T + bias,   y = act(z) + residual                       act: none, SiLU or the tanh form of GELU
+ *   dz = grad_y act'(z),  grad_x = dz W,  grad_w = dz^T x,  grad_bias = sum of the rows of dz,  grad_residual = grad_y
+ *
+ * x, grad_x [N, K]; w, grad_w [M, K]; bias [M] or NULL; residual [N, M] or NULL; y, grad_y [N, M]; dtype `dt`, y also A3PO_F32 (y_dt).
+ * Any K and M up to 2,097,120: bf16 with K and M multiples of 8 runs on the tensor cores and wants every matrix 16-byte
+ * aligned, the rest runs on the FP32 pipes and takes pointers aligned to their elements.  One kernel does the product, bias,
+ * activation and residual (two where few output tiles are split along K).  Accumulation is fp32 and y is rounded once; for bf16
+ * with an activation dz is rounded to bf16 as an operand of the products, not for grad_bias.
+ *
+ * row_mask uint8 [N] or NULL: rows with 0 are skipped (of more than a few rows only the others are multiplied): nothing of
+ * them enters a result (they may hold NaN); with finite weights their y (residual included) and grad_x are 0 and they add
+ * nothing to grad_w and grad_bias.  Their grad_residual is 0 too: callers that use grad_y for it mask it.
+ * kept: device buffer of a3po_linear_kept_bytes(N, M, dt, act) bytes, 256-byte aligned, that receives z for the backward
+ * (layout private, 4 N M bytes), or NULL when no backward follows or there is no activation (0 bytes).  The backward takes it
+ * with the forward's row_mask, N, K, M, dt and act, and does not change it.
+ * grad_x, grad_w, grad_bias: each may be NULL (not wanted), not all.  grad_w: dtype grad_w_dt (A3PO_F32, or dt); grad_bias: fp32.
+ * Both are overwritten, or with accumulate != 0 added to (A3PO_F32 only, else A3PO_ERR_UNSUPPORTED).
+ * ws: a3po_linear_workspace_bytes(N, K, M, dt, act, row_mask given, backward) bytes, 256-byte aligned.
+ * status: optional device word (A3PO_STATUS_WAIT_TIMEOUT).  Outputs must not overlap inputs.  N = 0 launches nothing except the
+ * zeros of gradients that are not accumulated.  Results are bit-identical from run to run.
+ * ------------------------------------------------------------------------------------------ */
+size_t a3po_linear_kept_bytes(int64_t N, int M, a3po_dtype dt, a3po_activation act);
+size_t a3po_linear_workspace_bytes(int64_t N, int K, int M, a3po_dtype dt, a3po_activation act, int has_row_mask, int is_bwd);
+
+int a3po_linear_fwd(const void* x, const void* w, const void* bias, const void* residual, const uint8_t* row_mask, int64_t N,
+                    int K, int M, a3po_dtype dt, a3po_activation act, void* y, a3po_dtype y_dt, void* kept,
+                    size_t kept_bytes, void* ws, size_t ws_bytes, uint32_t* status, void* stream);
+
+int a3po_linear_bwd(const void* x, const void* w, const uint8_t* row_mask, const void* kept, size_t kept_bytes,
+                    const void* grad_y, int64_t N, int K, int M, a3po_dtype dt, a3po_activation act, void* grad_x,
+                    void* grad_w, a3po_dtype grad_w_dt, float* grad_bias, int accumulate, void* ws, size_t ws_bytes,
+                    uint32_t* status, void* stream);
 
 /* --------------------------------------------------------------------------------------------
  * Sampling of one token per row of logits (no counterpart in the paper: the rollout's side of the policy).  What it leaves in

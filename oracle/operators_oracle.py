@@ -196,3 +196,25 @@ def clip_scale(grads, max_norm):
     """Global norm of a list of gradients, and the factor that clipping puts on them (an fp32 number)."""
     norm = math.sqrt(sum(float((np.asarray(g, dtype=np.float64) ** 2).sum()) for g in grads))
     return norm, float(np.float32(min(1.0, max_norm / (norm + 1e-6)))) if max_norm > 0 else 1.0
+
+
+# ------------------------------------------------------------------------------ linear operator
+def linear_activation(name, z):
+    """act(z) and its slope; "none" is z itself."""
+    return (z, np.ones_like(z)) if name == "none" else activation(name, z)
+
+
+def linear_fwd(x, w, bias=None, residual=None, act="none", mask=None):
+    z = _select(mask, x) @ np.asarray(w, dtype=np.float64).T
+    if bias is not None:
+        z = z + bias
+    y = linear_activation(act, z)[0]
+    if residual is not None:
+        y = y + _select(mask, residual)
+    return _select(mask, y), z
+
+
+def linear_bwd(x, w, z, grad_y, act="none", mask=None):
+    """grad_x, grad_w, grad_bias and dz."""
+    dz = _select(mask, grad_y) * np.where(np.isfinite(z), linear_activation(act, z)[1], 0.0)
+    return dz @ np.asarray(w, dtype=np.float64), dz.T @ _select(mask, x), dz.sum(axis=0), dz

@@ -19,6 +19,7 @@ A3PO_F32 = 0
 A3PO_BF16 = 1
 A3PO_ACT_SILU = 0
 A3PO_ACT_GELU_TANH = 1
+A3PO_ACT_NONE = 2
 A3PO_NORM_RMS = 0
 A3PO_NORM_LAYER = 1
 STATUS_TARGET_OUT_OF_RANGE = 1
@@ -121,6 +122,12 @@ _SIGNATURES = {
     "a3po_adamw_step": (c_int, [c_void_p, c_int, c_int, c_int, c_int, c_double, c_double, c_float, c_float, c_void_p, c_void_p,
                                 c_void_p, c_void_p, c_size_t, c_void_p]),
     "a3po_adamw_state_values": (c_int, [c_void_p, c_void_p, c_int64, c_int, c_void_p, c_void_p]),
+    "a3po_linear_kept_bytes": (c_size_t, [c_int64, c_int, c_int, c_int]),
+    "a3po_linear_workspace_bytes": (c_size_t, [c_int64, c_int, c_int, c_int, c_int, c_int, c_int]),
+    "a3po_linear_fwd": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int, c_int, c_int, c_int, c_void_p,
+                                c_int, c_void_p, c_size_t, c_void_p, c_size_t, c_void_p, c_void_p]),
+    "a3po_linear_bwd": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p, c_int64, c_int, c_int, c_int, c_int,
+                                c_void_p, c_void_p, c_int, c_void_p, c_int, c_void_p, c_size_t, c_void_p, c_void_p]),
 }
 
 _lib = None
@@ -688,6 +695,72 @@ def a3po_gated_ffn_bwd(x, w_gate_up, w_down, kept, grad_y, grad_x, grad_w_gate_u
                                            _ptr(grad_w_gate_up), _ptr(grad_w_down), gdt, int(bool(accumulate_grad_w)),
                                            _ptr(ws), ws.numel(), _ptr(status), _stream(stream))
     _check("a3po_gated_ffn_bwd", rc)
+
+
+# ------------------------------------------------------------------------------ linear operator
+def a3po_linear_kept_bytes(N, M, dt, activation=A3PO_ACT_NONE) -> int:
+    return load_library().a3po_linear_kept_bytes(N, M, dt, activation)
+
+
+def a3po_linear_workspace_bytes(N, K, M, dt, activation=A3PO_ACT_NONE, has_row_mask=False, is_bwd=False) -> int:
+    return load_library().a3po_linear_workspace_bytes(N, K, M, dt, activation, int(bool(has_row_mask)), int(bool(is_bwd)))
+
+
+def _linear_shapes(x, w, sides, row_mask):
+    """N, K and M after checking x [N, K], w [M, K], `sides` [N, M] of x's type and the mask."""
+    dt = _dtype_code(x)
+    if x.dim() != 2 or w.dim() != 2 or w.shape[1] != x.shape[1]:
+        raise ValueError("shape mismatch")
+    (n, k), m = x.shape, w.shape[0]
+    _here(x, w, *sides, row_mask)
+    _want(x, x.dtype, "x"); _want(w, x.dtype, "w"); _want(row_mask, torch.uint8, "row_mask")
+    for t in sides:
+        _want(t, x.dtype, "matrix [N, M]")
+        if t is not None and tuple(t.shape) != (n, m):
+            raise ValueError("shape mismatch")
+    if row_mask is not None and row_mask.numel() != n:
+        raise ValueError("shape mismatch")
+    return dt, n, k, m
+
+
+def a3po_linear_fwd(x, w, y, ws, *, bias=None, residual=None, row_mask=None, kept=None, activation=A3PO_ACT_NONE,
+                    status=None, stream=None):
+    """y = act(x w^T + bias) + residual; y has x's type or is fp32.  `kept` (uint8 buffer of a3po_linear_kept_bytes) is filled for
+    a3po_linear_bwd when given; without an activation there is nothing to keep."""
+    dt, n, k, m = _linear_shapes(x, w, (residual,), row_mask)
+    _here(y, bias, kept, ws, status)
+    _want(bias, x.dtype, "bias"); _want(kept, torch.uint8, "kept"); _want(ws, torch.uint8, "ws")
+    _want(status, torch.int32, "status")
+    if y.dtype != torch.float32:
+        _want(y, x.dtype, "y")
+    _want(y, y.dtype, "y")
+    if tuple(y.shape) != (n, m) or (bias is not None and bias.numel() != m):
+        raise ValueError("shape mismatch")
+    rc = load_library().a3po_linear_fwd(_ptr(x), _ptr(w), _ptr(bias), _ptr(residual), _ptr(row_mask), n, k, m, dt, activation,
+                                        _ptr(y), _dtype_code(y), _ptr(kept), 0 if kept is None else kept.numel(), _ptr(ws),
+                                        ws.numel(), _ptr(status), _stream(stream))
+    _check("a3po_linear_fwd", rc)
+
+
+def a3po_linear_bwd(x, w, grad_y, grad_x, grad_w, ws, *, kept=None, grad_bias=None, row_mask=None,
+                    activation=A3PO_ACT_NONE, accumulate_grad_w=False, status=None, stream=None):
+    """Gradients of a3po_linear_fwd; grad_x, grad_w or both may be None.  grad_w is fp32 or of the weights' type, grad_bias fp32;
+    the residual's gradient is grad_y itself."""
+    dt, n, k, m = _linear_shapes(x, w, (grad_y,), row_mask)
+    _here(grad_x, grad_w, grad_bias, kept, ws, status)
+    _want(grad_x, x.dtype, "grad_x"); _want(grad_bias, torch.float32, "grad_bias"); _want(kept, torch.uint8, "kept")
+    _want(ws, torch.uint8, "ws"); _want(status, torch.int32, "status")
+    gdt = A3PO_F32 if grad_w is None else _dtype_code(grad_w)
+    if grad_w is not None:
+        _want(grad_w, grad_w.dtype, "grad_w")
+    if ((grad_x is not None and grad_x.shape != x.shape) or (grad_w is not None and grad_w.shape != w.shape)
+            or (grad_bias is not None and grad_bias.numel() != m)):
+        raise ValueError("shape mismatch")
+    rc = load_library().a3po_linear_bwd(_ptr(x), _ptr(w), _ptr(row_mask), _ptr(kept), 0 if kept is None else kept.numel(),
+                                        _ptr(grad_y), n, k, m, dt, activation, _ptr(grad_x), _ptr(grad_w), gdt,
+                                        _ptr(grad_bias), int(bool(accumulate_grad_w)), _ptr(ws), ws.numel(), _ptr(status),
+                                        _stream(stream))
+    _check("a3po_linear_bwd", rc)
 
 
 # ------------------------------------------------------------------------------ sampling

@@ -1,0 +1,350 @@
+// The linear operator on the sm_100a tensor cores: the contractions of gemm_tc.cuh with bias, activation, residual and the kept z
+// in the epilogue, so that nothing but y (and z, for a backward) leaves the SM.
+//
+// Rounding: y is rounded once; dz is bf16, because it is an operand of bf16 matrix instructions (half a step, 2^-8 of an
+// element at most, that enters a long sum), but its column sums, the bias gradient, are taken of the fp32 values.
+//
+// Bound: the tensor pipe (the products are those of the feed-forward block, see ffn_tc.cu).
+
+#include "contract.cuh"
+#include "linear_internal.cuh"
+
+namespace a3po {
+namespace {
+
+// 8 consecutive bf16 as fp32.
+__device__ __forceinline__ void unpack8(const uint4& u, float (&v)[8]) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+
+template <int ACT, bool KEEP, typename OUT>
+struct LinearEpilogue : PlainEpilogue {
+  static constexpr int kKernelId = kKLinear;
+  static constexpr bool kChained = true;
+  static constexpr bool kPrefetch = true;
+  static constexpr int kGroups = 2;
+  struct Params {
+    OUT* y;
+    const __nv_bfloat16 *bias, *residual;
+    uint8_t* kept;
+    const int *row_index, *count;
+    long long n;
+    int m;
+  };
+  static int make_c_map(const Params& p, CUtensorMap* map) {
+    return make_out_map(map, p.y, sizeof(OUT), p.m, p.n, p.m);
+  }
+  const __nv_bfloat16* res;   // this thread's row of the residual, or null
+  int end_col;
+  uint4 next[4];              // its next 32 columns
+  uint8_t* cur;
+  __device__ __forceinline__ void begin(const Params& p, long long row) {
+    res = nullptr;
+    if (p.residual && row < (p.count ? *p.count : p.n))
+      res = p.residual + (p.row_index ? p.row_index[row] : row) * static_cast<long long>(p.m);
+  }
+  __device__ __forceinline__ void read_residual(int col0) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      next[q] = res && col0 + q * 8 < end_col ? __ldcs(reinterpret_cast<const uint4*>(res + col0) + q) : make_uint4(0, 0, 0, 0);
+  }
+  __device__ __forceinline__ void prefetch(const Params& p, int, int col0, int cols) {
+    end_col = min(col0 + cols, p.m);
+    if (p.residual) read_residual(col0);
+  }
+  __device__ __forceinline__ void chunk(const Params& p, int tile_row0, int col0, uint32_t (&r)[kEpiChunk], SlabStore& st) {
+    float v[kEpiChunk];
+    const bool in = col0 < p.m && tile_row0 < p.n;   // the same for all threads
+    if (p.bias && col0 < p.m) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float b[8] = {};
+        if (col0 + q * 8 < p.m) unpack8(__ldg(reinterpret_cast<const uint4*>(p.bias + col0) + q), b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[q * 8 + i] = bits_to_float(r[q * 8 + i]) + b[i];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kEpiChunk; ++j) v[j] = bits_to_float(r[j]);
+    }
+    if (KEEP && in) {   // a pair's second tile may lie past the buffer
+      uint8_t* tile = p.kept + z_tile(tile_row0, col0, p.m) + st.row_in_tile * 16;
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        __stcs(reinterpret_cast<float4*>(tile) + q * kZRows, make_float4(v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]));
+    }
+    if (ACT != kActNone) {
+#pragma unroll
+      for (int j = 0; j < kEpiChunk; ++j) {
+        float a, slope;
+        linear_activation<ACT>(v[j], a, slope);
+        v[j] = a;
+      }
+    }
+    if (p.residual) {
+      uint4 now[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) now[q] = next[q];
+      if (col0 + kEpiChunk < end_col) read_residual(col0 + kEpiChunk);   // while these are worked on
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float b[8];
+        unpack8(now[q], b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[q * 8 + i] += b[i];
+      }
+    }
+    if constexpr (sizeof(OUT) == 4) {
+      uint8_t* s = st.acquire();
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        *st.piece(s, q) = make_uint4(__float_as_uint(v[q * 4]), __float_as_uint(v[q * 4 + 1]), __float_as_uint(v[q * 4 + 2]),
+                                     __float_as_uint(v[q * 4 + 3]));
+      st.submit(s, col0, tile_row0, in, false);
+    } else {
+      const int half = (col0 >> 5) & 1;   // a slab holds 64 columns
+      if (half == 0) cur = st.acquire();
+#pragma unroll
+      for (int q = 0; q < 4; ++q) *st.piece(cur, half * 4 + q) = pack8(v, q);
+      if (half == 1) st.submit(cur, col0 - 32, tile_row0, col0 - 32 < p.m && tile_row0 < p.n, false);
+    }
+  }
+  __device__ __forceinline__ void end(const Params&, long long, int) {}
+};
+
+// The same after the parts of a K split: 4 columns per thread, the parts in index order, 8 on their way at a time.
+template <int ACT, bool KEEP, typename OUT>
+__global__ void __launch_bounds__(256)
+linear_add_parts_kernel(const float* parts, int n_parts, long long part_stride, typename LinearEpilogue<ACT, KEEP, OUT>::Params p) {
+  wait_for_previous();
+  allow_next();
+  const long long rows = p.count ? (*p.count < p.n ? *p.count : p.n) : p.n;
+  const int vecs = p.m / kAddCols;
+  const long long total = rows * vecs;
+  for (long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; i < total;
+       i += static_cast<long long>(gridDim.x) * 256) {
+    const float* src = parts + i * kAddCols;
+    float v[4] = {};
+    for (int p0 = 0; p0 < n_parts; p0 += kAddBatch) {
+      float4 a[kAddBatch];
+#pragma unroll
+      for (int k = 0; k < kAddBatch; ++k)
+        a[k] = p0 + k < n_parts ? __ldcs(reinterpret_cast<const float4*>(src + (p0 + k) * part_stride))
+                                : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < kAddBatch; ++k) {
+        v[0] += a[k].x; v[1] += a[k].y; v[2] += a[k].z; v[3] += a[k].w;
+      }
+    }
+    const long long row = i / vecs;
+    const int col = static_cast<int>(i - row * vecs) * kAddCols;
+    if (p.bias) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] += to_float(p.bias[col + j]);
+    }
+    if (KEEP) {
+      uint8_t* tile = p.kept + z_tile(row, col, p.m);
+      reinterpret_cast<float4*>(tile)[col % kZCols / 4 * kZRows + row % kZRows] = make_float4(v[0], v[1], v[2], v[3]);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float a, slope;
+      linear_activation<ACT>(v[j], a, slope);
+      v[j] = a;
+    }
+    if (p.residual) {
+      const __nv_bfloat16* res = p.residual + (p.row_index ? p.row_index[row] : row) * static_cast<long long>(p.m) + col;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] += to_float(res[j]);
+    }
+    if constexpr (sizeof(OUT) == 4) reinterpret_cast<float4*>(p.y)[i] = make_float4(v[0], v[1], v[2], v[3]);
+    else reinterpret_cast<uint2*>(p.y)[i] = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  }
+}
+
+template <int ACT, bool KEEP, typename OUT>
+int fwd_impl(const LinearFwd& c) {
+  using Epi = LinearEpilogue<ACT, KEEP, OUT>;
+  const Operand a{c.x, c.n, c.k, c.k}, b{c.w, c.m, c.k, c.k};
+  typename Epi::Params ep;
+  ep.y = static_cast<OUT*>(c.y);
+  ep.bias = static_cast<const __nv_bfloat16*>(c.bias);
+  ep.residual = static_cast<const __nv_bfloat16*>(c.residual);
+  ep.kept = static_cast<uint8_t*>(c.kept);
+  ep.row_index = c.row_index;
+  ep.count = c.count;
+  ep.n = c.n;
+  ep.m = c.m;
+  const Begin begin = first_launch(c.count);
+  const int k_parts = c.parts ? ffn_k_parts(c.n, c.m, c.k) : 1;
+  if (k_parts > 1) {
+    const long long rows_pad = (c.n + BM - 1) / BM * BM;
+    typename StorePartsEpilogue<kKLinear>::Params sp{c.parts, c.n, static_cast<int>(rows_pad), k_parts, c.m};
+    A3PO_RETURN_IF((launch_gemm<StorePartsEpilogue<kKLinear>, false, false, 1>(a, b, 0, sp, rows_as_m(c.count, c.n), c.status,
+                                                                             c.stream, k_parts, begin)));
+    const long long want = (c.n * (c.m / kAddCols) + 255) / 256;
+    const int blocks = static_cast<int>(want < sm_count() * 8ll ? want : sm_count() * 8ll);
+    A3PO_LAUNCH(kKLinear, c.stream, (launch_early(linear_add_parts_kernel<ACT, KEEP, OUT>, blocks, 256, 0, c.stream, 1, true,
+                                                  static_cast<const float*>(c.parts), k_parts, rows_pad * c.m, ep)));
+    return after_launch();
+  }
+  return contract<Epi, false, false>(a, b, ep, rows_as_m(c.count, c.n), c.status, c.stream, begin);
+}
+
+// ------------------------------------------------------------------------------------ dz and its column sums
+// A block takes 128 rows, one per thread, and kGradCols columns in steps of 32.
+constexpr int kGradCols = 128;
+template <int ACT>
+__global__ void __launch_bounds__(kZRows)
+linear_grad_z_kernel(const __nv_bfloat16* grad_y, const uint8_t* kept, long long n, int m, const int* row_index,
+                     const int* count, const uint8_t* row_mask, __nv_bfloat16* dz, float* sums) {
+  __shared__ float part[kZRows / kWarp][kZCols];
+  wait_for_previous();
+  allow_next();
+  const long long rows = count ? (*count < n ? *count : n) : n;
+  const long long row0 = static_cast<long long>(blockIdx.x) * kZRows, row = row0 + threadIdx.x;
+  if (row0 >= rows) return;
+  const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
+  const bool live = row < rows && (!row_mask || row_mask[row] != 0);
+  const __nv_bfloat16* gy = live ? grad_y + (row_index ? row_index[row] : row) * static_cast<long long>(m) : nullptr;
+  const int c_end = min(static_cast<int>(blockIdx.y + 1) * kGradCols, m);
+  for (int c0 = blockIdx.y * kGradCols; c0 < c_end; c0 += kZCols) {
+    float v[kZCols];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float g[8] = {};
+      if (live && c0 + q * 8 < m) unpack8(__ldcs(reinterpret_cast<const uint4*>(gy + c0) + q), g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[q * 8 + i] = g[i];
+    }
+    if (ACT != kActNone && live) {   // columns of the last tile past m hold nothing: v is 0 there, and stays so
+      const float4* tile = reinterpret_cast<const float4*>(kept + z_tile(row, c0, m)) + threadIdx.x;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        if (c0 + q * 4 >= m) continue;
+        const float4 z4 = __ldcs(tile + q * kZRows);
+        const float z[4] = {z4.x, z4.y, z4.z, z4.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float a, slope;
+          linear_activation<ACT>(z[i], a, slope);
+          v[q * 4 + i] *= slope;
+        }
+      }
+    }
+    if (dz && row < (n + kZRows - 1) / kZRows * kZRows) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (c0 + q * 8 < m && (count || row < n)) reinterpret_cast<uint4*>(dz + row * m + c0)[q] = pack8(v, q);
+    }
+    if (sums) {
+      // lane c ends with the warp's sum of column c: each step halves the columns that a lane still adds
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+#pragma unroll
+        for (int i = 0; i < o; ++i) {
+          const bool up = (lane & o) != 0;
+          const float other = __shfl_xor_sync(0xffffffffu, up ? v[i] : v[i + o], o);
+          v[i] = (up ? v[i + o] : v[i]) + other;
+        }
+      }
+      part[warp][lane] = v[0];
+      __syncthreads();
+      if (threadIdx.x < kZCols && c0 + static_cast<int>(threadIdx.x) < m) {
+        float t = 0.f;
+#pragma unroll
+        for (int w = 0; w < kZRows / kWarp; ++w) t += part[w][threadIdx.x];
+        sums[static_cast<long long>(blockIdx.x) * m + c0 + threadIdx.x] = t;
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// 32 columns per block; 32 groups of threads share the blocks of rows and are added in order.
+__global__ void __launch_bounds__(1024)
+linear_grad_bias_kernel(const float* sums, long long blocks, const int* count, int m, float* grad_bias, int accumulate) {
+  __shared__ float part[32][33];
+  wait_for_previous();
+  allow_next();
+  if (count) {
+    const long long have = (static_cast<long long>(*count) + kZRows - 1) / kZRows;
+    if (have < blocks) blocks = have;
+  }
+  const int x = threadIdx.x % 32, y = threadIdx.x / 32;
+  const int col = blockIdx.x * 32 + x;
+  float t = 0.f;
+  if (col < m)
+    for (long long b = y; b < blocks; b += 32) t += sums[b * m + col];
+  part[y][x] = t;
+  __syncthreads();
+  if (y == 0 && col < m) {
+    t = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) t += part[i][x];
+    grad_bias[col] = accumulate ? grad_bias[col] + t : t;
+  }
+}
+
+}  // namespace
+
+int linear_fwd_tc(const LinearFwd& c) {
+  using B = __nv_bfloat16;
+  if (c.act == kActNone) return c.y_f32 ? fwd_impl<kActNone, false, float>(c) : fwd_impl<kActNone, false, B>(c);
+#define A3PO_LINEAR(ACT)                                                                               \
+  (c.kept ? (c.y_f32 ? fwd_impl<ACT, true, float>(c) : fwd_impl<ACT, true, B>(c))                      \
+          : (c.y_f32 ? fwd_impl<ACT, false, float>(c) : fwd_impl<ACT, false, B>(c)))
+  return c.act == kActSilu ? A3PO_LINEAR(kActSilu) : A3PO_LINEAR(kActGelu);
+#undef A3PO_LINEAR
+}
+
+int linear_grad_z(const void* grad_y, const void* kept, long long n, int m, Act act, const int* row_index, const int* count,
+                  const uint8_t* row_mask, void* dz, float* sums, bool early, cudaStream_t stream) {
+  const dim3 grid(static_cast<unsigned>((n + kZRows - 1) / kZRows), static_cast<unsigned>((m + kGradCols - 1) / kGradCols));
+  using B = __nv_bfloat16;
+#define A3PO_GRAD_Z(ACT)                                                                                                  \
+  A3PO_LAUNCH(kKLinearGradZ, stream, (launch_early(linear_grad_z_kernel<ACT>, grid, dim3(kZRows), 0, stream, 1, early,         \
+                                                   static_cast<const B*>(grad_y), static_cast<const uint8_t*>(kept), n, m, \
+                                                   row_index, count, row_mask, static_cast<B*>(dz), sums)))
+  if (act == kActNone) A3PO_GRAD_Z(kActNone);
+  else if (act == kActSilu) A3PO_GRAD_Z(kActSilu);
+  else A3PO_GRAD_Z(kActGelu);
+#undef A3PO_GRAD_Z
+  return after_launch();
+}
+
+int linear_grad_bias(const float* sums, long long blocks, const int* count, int m, float* grad_bias, int accumulate,
+                     cudaStream_t stream) {
+  A3PO_LAUNCH(kKLinearGradZ, stream, (launch_early(linear_grad_bias_kernel, static_cast<unsigned>((m + 31) / 32), 1024, 0, stream,
+                                                   1, true, sums, blocks, count, m, grad_bias, accumulate)));
+  return after_launch();
+}
+
+int linear_grads_tc(const void* dz, const void* x, const void* w, long long n, int k, int m, void* grad_x, void* grad_w,
+                    a3po_dtype grad_dt, int accumulate, float* parts, const int* count, bool first, uint32_t* status,
+                    cudaStream_t stream) {
+  Begin begin = first ? Begin::kAfter : Begin::kEarly;
+  if (grad_w) {
+    const Operand a{dz, m, n, m}, b{x, k, n, k};   // dz^T x
+    if (grad_dt == A3PO_F32) {
+      using Epi = StoreF32EpilogueT<kKLinearGradW>;
+      A3PO_RETURN_IF((weight_gemm<Epi>(a, b, typename Epi::Params{static_cast<float*>(grad_w), k, m, k, accumulate}, accumulate,
+                                       count, status, stream, begin)));
+    } else {
+      using Epi = StoreBf16EpilogueT<kKLinearGradW>;
+      A3PO_RETURN_IF((weight_gemm<Epi>(a, b, typename Epi::Params{static_cast<__nv_bfloat16*>(grad_w), k, m, k, nullptr}, 0,
+                                       count, status, stream, begin)));
+    }
+    begin = Begin::kBeside;   // it reads what the weight gradient reads and writes apart from it
+  }
+  if (!grad_x) return A3PO_OK;
+  return rows_gemm<kKLinearGradX, true>(Operand{dz, n, m, m}, Operand{w, k, m, k}, static_cast<__nv_bfloat16*>(grad_x), parts,
+                                        count, status, stream, begin);
+}
+
+}  // namespace a3po
