@@ -19,6 +19,7 @@
 // Bound: HBM (32 bits: 30 bytes an element with fp32 gradients and masters beside bf16 weights, 18 with 8 bits, and 4 more for
 // the norm); with states of 8 bits the issue slots are about as far.
 
+#include <cfloat>
 #include <climits>
 
 #include "a3po_common.cuh"
@@ -115,29 +116,26 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, int lane, int left, boo
       if (lane + 32 * i < left) p[lane + 32 * i] = __float2bfloat16_rn(x[i]);
   }
 }
-__device__ __forceinline__ void load8(const uint8_t* p, int lane, int left, bool wide, int (&c)[8]) {
+// Codes as they lie in two words: element k of the lane is byte k % 4 of word k / 4.
+__device__ __forceinline__ void load8(const uint8_t* p, int lane, int left, bool wide, uint32_t (&c)[2]) {
   if (wide) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint32_t u = __ldcs(reinterpret_cast<const uint32_t*>(p + h * 128 + lane * 4));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) c[h * 4 + i] = u >> (8 * i) & 255;
-    }
+    for (int h = 0; h < 2; ++h) c[h] = __ldcs(reinterpret_cast<const uint32_t*>(p + h * 128 + lane * 4));
   } else {
+    c[0] = c[1] = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = lane + 32 * i < left ? p[lane + 32 * i] : 0;
+    for (int i = 0; i < 8; ++i)
+      if (lane + 32 * i < left) c[i / 4] |= static_cast<uint32_t>(p[lane + 32 * i]) << (i % 4 * 8);
   }
 }
-__device__ __forceinline__ void store8(uint8_t* p, int lane, int left, bool wide, const int (&c)[8]) {
+__device__ __forceinline__ void store8(uint8_t* p, int lane, int left, bool wide, const uint32_t (&c)[2]) {
   if (wide) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      __stcs(reinterpret_cast<uint32_t*>(p + h * 128 + lane * 4),
-             static_cast<uint32_t>(c[h * 4] | c[h * 4 + 1] << 8 | c[h * 4 + 2] << 16 | c[h * 4 + 3] << 24));
+    for (int h = 0; h < 2; ++h) __stcs(reinterpret_cast<uint32_t*>(p + h * 128 + lane * 4), c[h]);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (lane + 32 * i < left) p[lane + 32 * i] = static_cast<uint8_t>(c[i]);
+      if (lane + 32 * i < left) p[lane + 32 * i] = static_cast<uint8_t>(c[i / 4] >> (i % 4 * 8));
   }
 }
 
@@ -209,34 +207,107 @@ step_numbers_kernel(const double* sums, int count, double b1, double b2, float m
 }
 
 // ------------------------------------------------------------------------------------ update
-__host__ __device__ __forceinline__ double code_value(int c) {
+// sqrt(x) + eps to two steps.  The fast root takes x below 2^-126 for 0, which is seen beside a tiny eps only.
+__device__ __forceinline__ float root_plus(float x, float eps) {
+  if (eps < 1e-12f) return __fsqrt_rn(x) + eps;
+  float y;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y + eps;
+}
+__host__ __device__ constexpr double code_value(int c) {
   return c < 8 ? static_cast<double>(c) : static_cast<double>(static_cast<long long>(8 + c % 8) << (c / 8 - 1));
 }
-// The code nearest to x >= 0 (in units of the scale): the leading four bits, halves to the even code.
+// The code nearest to x >= 0 (in units of the scale), halves to the even code.  From 8 on it is the leading four bits of x: three
+// below the exponent, rounded by an addition that carries into it.  Below 8 the codes are the whole numbers, which are those
+// of x + 8 less 8.
+constexpr int kEight = 0x40200000;   // upper word of 8.0
+// half a step less one, and what takes the bits of 8.0 to code 8
+constexpr unsigned long long kRoundCode = (1ull << 48) - 1 - (static_cast<unsigned long long>((kEight >> 17) - 8) << 49);
 __device__ __forceinline__ int code_of(double x, int top) {
-  int c;
-  if (x < 8.0) {
-    c = __double2int_rn(x);
-  } else {
-    const unsigned long long b = static_cast<unsigned long long>(__double_as_longlong(x));
-    c = static_cast<int>((b + ((1ull << 48) - 1) + (b >> 49 & 1)) >> 49) - ((1023 + 3) << 3) + 8;
-  }
-  return c < top ? c : top;
+  const bool small = __double2hiint(x) < kEight;
+  if (small) x += 8.0;
+  const int hi = __double2hiint(x);
+  const int odd = hi >> 17 & 1, more = __double2loint(x) != 0 ? 1 : 0;
+  const int c = (hi + 0xffff + (odd | more)) >> 17;
+  return min(c - ((kEight >> 17) - (small ? 0 : 8)), top);
 }
-// Largest of non-negative numbers over the warp (ordered as their bits are).
-__device__ __forceinline__ double warp_max64(double v) {
-  const uint32_t hi = static_cast<uint32_t>(__double2hiint(v)), lo = static_cast<uint32_t>(__double2loint(v));
-  const uint32_t top = __reduce_max_sync(0xffffffffu, hi);
-  const uint32_t low = __reduce_max_sync(0xffffffffu, hi == top ? lo : 0u);
-  return __hiloint2double(static_cast<int>(top), static_cast<int>(low));
+__device__ __forceinline__ uint32_t min3u(uint32_t a, uint32_t b, uint32_t c) { return __vimin3_u32(a, b, c); }
+__device__ __forceinline__ uint32_t max3u(uint32_t a, uint32_t b, uint32_t c) { return __vimax3_u32(a, b, c); }
+// Largest over the warp of eight non-negative numbers a lane, ordered as their bits are: the upper words first, then the lower
+// words of those that share the largest.
+__device__ __forceinline__ double warp_max64(const double (&v)[8]) {
+  uint32_t hi = 0;
+#pragma unroll
+  for (int k = 0; k < 8; k += 2)
+    hi = max3u(hi, static_cast<uint32_t>(__double2hiint(v[k])) & 0x7fffffffu, static_cast<uint32_t>(__double2hiint(v[k + 1])) & 0x7fffffffu);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  uint32_t lo = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if ((static_cast<uint32_t>(__double2hiint(v[k])) & 0x7fffffffu) == hi) lo = max(lo, static_cast<uint32_t>(__double2loint(v[k])));
+  lo = __reduce_max_sync(0xffffffffu, lo);
+  return __hiloint2double(static_cast<int>(hi), static_cast<int>(lo));
+}
+
+// 1 / x for normal x: the fp32 quotient and two steps of Newton's iteration.
+__device__ __forceinline__ double reciprocal(float x) {
+  const double d = static_cast<double>(x);
+  double r = static_cast<double>(__frcp_rn(x));
+  r = fma(r, fma(-d, r, 1.0), r);
+  return fma(r, fma(-d, r, 1.0), r);
+}
+
+// New first (second) moments of a block of 256, in 64 bits, stored as codes and a scale; out: their fp32 values.
+template <bool FIRST>
+__device__ __forceinline__ void new_states(uint8_t* codes, float* scale, uint32_t (&c)[2], float old, const double* q, double b,
+                                           double more, int lane, int left, bool wide, const float (&g)[8], float (&out)[8]) {
+  constexpr int kTop = FIRST ? 127 : 255;
+  const double was = b * static_cast<double>(old);
+  double x[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const double gk = static_cast<double>(g[k]);
+    x[k] = fma(q[c[k / 4] >> (k % 4 * 8) & 255], was, more * (FIRST ? gk : gk * gk));
+    out[k] = static_cast<float>(x[k]);
+  }
+  const float now = static_cast<float>(warp_max64(x) * (1.0 / code_value(kTop)));
+  const double inv = now >= FLT_MIN ? reciprocal(now) : now > 0.f ? 1.0 / static_cast<double>(now) : 0.0;
+  uint32_t least = 0xffffffffu;
+#pragma unroll
+  for (int k = 0; k < 8; k += 2)
+    least = min3u(least, static_cast<uint32_t>(__double2hiint(fabs(x[k]) * inv)), static_cast<uint32_t>(__double2hiint(fabs(x[k + 1]) * inv)));
+  uint32_t byte[8];
+  if (__all_sync(0xffffffffu, least >= static_cast<uint32_t>(kEight)) && now >= FLT_MIN) {
+    // all codes from 8 on (nearly every block): the leading four bits and nothing else
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const unsigned long long u = static_cast<unsigned long long>(__double_as_longlong(fabs(x[k]) * inv));
+      const uint32_t r = static_cast<uint32_t>((u + (u >> 49 & 1) + kRoundCode) >> 49);
+      byte[k] = FIRST ? (r & 0x7fu) | (static_cast<uint32_t>(__double2hiint(x[k])) >> 24 & 0x80u) : r;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      byte[k] = static_cast<uint32_t>(code_of(fabs(x[k]) * inv, kTop));
+      if (FIRST) byte[k] |= x[k] < 0.0 ? 128u : 0u;
+      else if (byte[k] == 0 && x[k] > 0.0 && now > 0.f) byte[k] = 1;
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    c[h] = __byte_perm(__byte_perm(byte[h * 4], byte[h * 4 + 1], 0x0040), __byte_perm(byte[h * 4 + 2], byte[h * 4 + 3], 0x0040), 0x5410);
+  store8(codes, lane, left, wide, c);
+  if (lane == 0) *scale = now;
 }
 
 template <typename W, typename G, int BITS, int CAP>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
 adamw_kernel(const __grid_constant__ Table<CAP> t, const Numbers* numbers, double b1, double b2, float eps) {
-  __shared__ double q[BITS == 8 ? 256 : 1];
+  __shared__ double q[BITS == 8 ? 512 : 1];   // values of the codes, first moment (with the sign) and second
   if (BITS == 8) {
-    q[threadIdx.x] = code_value(threadIdx.x);
+    const int c = threadIdx.x;
+    q[c] = c < 128 ? code_value(c) : -code_value(c - 128);
+    q[256 + c] = code_value(c);
     __syncthreads();
   }
   wait_for_previous();
@@ -275,45 +346,18 @@ adamw_kernel(const __grid_constant__ Table<CAP> t, const Numbers* numbers, doubl
       store8(pm, lane, left, wide, m);
       store8(pv, lane, left, wide, v);
     } else {
-      uint8_t* pm = static_cast<uint8_t*>(e.m) + at;
-      uint8_t* pv = static_cast<uint8_t*>(e.v) + at;
-      float *pms = e.m_scale + at / kBlock, *pvs = e.v_scale + at / kBlock;
-      int cm[8], cv[8];
+      uint8_t *pm = static_cast<uint8_t*>(e.m) + at, *pv = static_cast<uint8_t*>(e.v) + at;
+      float *ms = e.m_scale + at / kBlock, *vs = e.v_scale + at / kBlock;
+      uint32_t cm[2], cv[2];
       load8(pm, lane, left, wide, cm);
       load8(pv, lane, left, wide, cv);
-      const double ms = b1 * static_cast<double>(*pms), vs = b2 * static_cast<double>(*pvs);
-      double dm[8], dv[8], top_m = 0.0, top_v = 0.0;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const double x = static_cast<double>(g[k]);
-        const double was = q[cm[k] & 127];
-        dm[k] = fma(cm[k] & 128 ? -was : was, ms, s.g1 * x);
-        dv[k] = fma(q[cv[k]], vs, s.g2 * (x * x));
-        top_m = fmax(top_m, fabs(dm[k]));
-        top_v = fmax(top_v, dv[k]);
-        m[k] = static_cast<float>(dm[k]);
-        v[k] = static_cast<float>(dv[k]);
-      }
-      const float new_ms = static_cast<float>(warp_max64(top_m) / code_value(127));
-      const float new_vs = static_cast<float>(warp_max64(top_v) / code_value(255));
-      const double inv_m = new_ms > 0.f ? 1.0 / static_cast<double>(new_ms) : 0.0;
-      const double inv_v = new_vs > 0.f ? 1.0 / static_cast<double>(new_vs) : 0.0;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        cm[k] = code_of(fabs(dm[k]) * inv_m, 127) | (dm[k] < 0.0 ? 128 : 0);
-        cv[k] = code_of(dv[k] * inv_v, 255);
-        if (cv[k] == 0 && dv[k] > 0.0 && inv_v > 0.0) cv[k] = 1;
-      }
-      store8(pm, lane, left, wide, cm);
-      store8(pv, lane, left, wide, cv);
-      if (lane == 0) {
-        *pms = new_ms;
-        *pvs = new_vs;
-      }
+      const float old_ms = *ms, old_vs = *vs;
+      new_states<true>(pm, ms, cm, old_ms, q, b1, s.g1, lane, left, wide, g, m);
+      new_states<false>(pv, vs, cv, old_vs, q + 256, b2, s.g2, lane, left, wide, g, v);
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const float step = __fdividef(m[k] * s.inv_bc1, __fsqrt_rn(v[k] * s.inv_bc2) + eps);
+      const float step = m[k] * s.inv_bc1 * fast_rcp(root_plus(v[k] * s.inv_bc2, eps));
       w[k] = fmaf(-s.lr, fmaf(e.decay, w[k], step), w[k]);
     }
     if (sizeof(W) == 2 && e.master) store8(e.master + at, lane, left, wide, w);
@@ -386,14 +430,23 @@ int norm_room(int count) {   // sums: kNormBlocks for each table of kLargeTable 
   return (count + kLargeTable - 1) / kLargeTable * kNormBlocks;
 }
 
+// Four codes per thread and step where the pointers allow it.  Bound: HBM, 5 bytes an element.
 __global__ void __launch_bounds__(256)
-state_values_kernel(const uint8_t* __restrict__ codes, const float* __restrict__ scales, long long n, int is_signed,
+state_values_kernel(const uint8_t* __restrict__ codes, const float* __restrict__ scales, long long n, int is_signed, int wide,
                     float* __restrict__ out) {
-  for (long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<long long>(gridDim.x) * 256) {
-    const int c = codes[i];
-    const float v = static_cast<float>(code_value(is_signed ? c & 127 : c)) * scales[i / kBlock];
-    out[i] = is_signed && (c & 128) ? -v : v;
+  __shared__ float q[256];
+  const int c = threadIdx.x;
+  q[c] = static_cast<float>(!is_signed ? code_value(c) : c < 128 ? code_value(c) : -code_value(c - 128));
+  __syncthreads();
+  const long long me = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x, all = static_cast<long long>(gridDim.x) * 256;
+  const long long quads = wide ? n / 4 : 0;
+  for (long long i = me; i < quads; i += all) {
+    const uint32_t u = __ldcs(reinterpret_cast<const uint32_t*>(codes) + i);
+    const float s = __ldg(scales + i / (kBlock / 4));
+    __stcs(reinterpret_cast<float4*>(out) + i,
+           make_float4(q[u & 255] * s, q[u >> 8 & 255] * s, q[u >> 16 & 255] * s, q[u >> 24] * s));
   }
+  for (long long i = quads * 4 + me; i < n; i += all) out[i] = q[codes[i]] * scales[i / kBlock];
 }
 
 }  // namespace
@@ -468,9 +521,10 @@ int a3po_adamw_state_values(const uint8_t* codes, const float* scales, int64_t n
   if (sm_count() <= 0) return A3PO_ERR_NO_DEVICE;
   if (n == 0) return A3PO_OK;
   cudaStream_t stream = as_stream(stream_);
-  const long long want = (n + 255) / 256, most = sm_count() * 16ll;
+  const int wide = aligned_to(codes, 4) && aligned_to(values, 16);
+  const long long per = wide ? 1024 : 256, want = (n + per - 1) / per, most = sm_count() * 64ll;
   A3PO_LAUNCH(kKAdamStep, stream, (state_values_kernel<<<static_cast<unsigned>(want < most ? want : most), 256, 0, stream>>>(
-                                      codes, scales, n, is_signed, values)));
+                                      codes, scales, n, is_signed, wide, values)));
   return after_launch();
 }
 

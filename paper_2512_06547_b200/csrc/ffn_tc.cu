@@ -54,6 +54,7 @@ struct GateUpEpilogue {
   static constexpr int kGroups = 2;
   static constexpr bool kChained = true;
   static constexpr bool kSplitK = false;
+  static constexpr int kPromote = 0;
   struct Params {
     __nv_bfloat16* hid;    // [n, f]
     uint8_t* kept;         // see ffn_internal.cuh

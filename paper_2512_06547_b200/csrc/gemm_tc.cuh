@@ -308,12 +308,16 @@ struct SlabStore {
 // kChained: launches may begin early, or let a successor begin (see Begin).  kSplitK: launches may split K.  Both are
 // compile-time, because the LM head's kernels, which do neither, took 0.5-1 % longer with the code for them (forward of
 // 9,029 rows of 1536 x 151,936 3,108 -> 3,125-3,137 us, backward 6,680 -> 6,753).
+// kPromote (pair kernel): k-blocks after which the accumulators are added to fp32 sums in the epilogue's registers and start
+// anew; 0: never.  The tensor cores cut every addition off instead of rounding it, so a sum of K = 16,384 is 1.5e-4 off
+// (2-norm); of 512 at a time, with rounded additions between them, 5e-6.  For outputs that stay in fp32.
 struct PlainEpilogue {
   static constexpr bool kGated = false;
   static constexpr bool kPrefetch = false;
   static constexpr int kGroups = 1;
   static constexpr bool kChained = false;
   static constexpr bool kSplitK = false;
+  static constexpr int kPromote = 0;
 };
 
 template <int KERNEL_ID>
@@ -902,10 +906,13 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
       for (long long i = pair_id; i < im.items && ok; i += n_pairs) {
         const Item it = decode_item<Epi::kSplitK>(im, i, k_blocks);
         for (int nt = it.n_begin; nt < it.n_end && ok; ++nt) {
+          int kb0 = 0, kb1;
+          do {
+          kb1 = Epi::kPromote > 0 ? min(kb0 + Epi::kPromote, k_blocks) : k_blocks;
           if (!mbar_wait(&tmem_empty_bar[acc], acc_phase ^ 1u, abort_flag)) { ok = false; break; }
           tcgen05_fence_after_sync();
           const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(acc * BN);
-          for (int kb = 0; kb < k_blocks; ++kb) {
+          for (int kb = kb0; kb < kb1; ++kb) {
             if (!mbar_wait(&full_bar[stage], phase, abort_flag)) { ok = false; break; }
             tcgen05_fence_after_sync();
             const uint32_t sa = smem_u32(smem_a + stage * kABytes);
@@ -914,12 +921,14 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             const uint64_t desc_b = B_MN ? umma_desc_mn_major_sw128(sb, kMnBlockBytes) : umma_desc_k_major_sw128(sb);
 #pragma unroll
             for (int k = 0; k < BK / 16; ++k)
-              umma_bf16_pair(tmem_d, desc_a + a_step * k, desc_b + b_step * k, idesc, (kb | k) != 0 ? 1u : 0u);
+              umma_bf16_pair(tmem_d, desc_a + a_step * k, desc_b + b_step * k, idesc, ((kb - kb0) | k) != 0 ? 1u : 0u);
             umma_commit_pair(&empty_bar[stage], 3);   // both CTAs may refill the stage
             if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
           }
           if (ok) umma_commit_pair(&tmem_full_bar[acc], 3);
           if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+          kb0 = kb1;
+          } while (Epi::kPromote > 0 && kb0 < k_blocks && ok);
         }
       }
     }
@@ -947,6 +956,37 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
       epi.begin(ep, static_cast<long long>(tile_row0) + row_in_tile);
       for (int nt = it.n_begin; nt < it.n_end && ok; ++nt) {
         if constexpr (Epi::kPrefetch) epi.prefetch(ep, tile_row0, nt * BN + group * kShare * kEpiChunk, kShare * kEpiChunk);
+        if constexpr (Epi::kPromote > 0) {
+          float sum[kShare][kEpiChunk] = {};
+          for (int kb0 = 0; kb0 < k_blocks; kb0 += Epi::kPromote) {
+            ok = all_epilogue_threads(mbar_wait(&tmem_full_bar[acc], acc_phase, abort_flag), 2 + 2 * group);
+            if (!ok) break;
+            tcgen05_fence_after_sync();
+            const uint32_t from = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) +
+                                  static_cast<uint32_t>(acc * BN + group * kShare * kEpiChunk);
+#pragma unroll
+            for (int c = 0; c < 2 * kShare; ++c) {   // 16 columns at a time: the sums leave no more registers
+              uint32_t r[kEpiChunk / 2];
+              tmem_ld_32x16(from + static_cast<uint32_t>(c * kEpiChunk / 2), r);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < kEpiChunk / 2; ++j) sum[c / 2][c % 2 * (kEpiChunk / 2) + j] += bits_to_float(r[j]);
+            }
+            tcgen05_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(leader_tmem_empty + static_cast<uint32_t>(acc * sizeof(uint64_t)));
+            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+          }
+          if (!ok) break;
+#pragma unroll
+          for (int c = 0; c < kShare; ++c) {
+            uint32_t r[kEpiChunk];
+#pragma unroll
+            for (int j = 0; j < kEpiChunk; ++j) r[j] = __float_as_uint(sum[c][j]);
+            epi.chunk(ep, tile_row0, nt * BN + (group * kShare + c) * kEpiChunk, r, st);
+          }
+          continue;
+        }
         if (!zero_output) {
           ok = all_epilogue_threads(mbar_wait(&tmem_full_bar[acc], acc_phase, abort_flag), 2 + 2 * group);
           if (!ok) break;

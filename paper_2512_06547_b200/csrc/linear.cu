@@ -66,7 +66,7 @@ bool lay_out(Arena& ar, long long n, int k, int m, a3po_dtype dt, Act act, bool 
     l->sums = ar.take<float>((cap + kZRows - 1) / kZRows * m);
   }
   const size_t parts = !bwd && linear_few(n, k, m) ? 0 : bwd ? ffn_parts_bytes(static_cast<long long>(cap), k, m)
-                                                             : ffn_parts_bytes(static_cast<long long>(cap), m, k);
+                                                             : linear_parts_bytes(static_cast<long long>(cap), k, m);
   if (parts) l->parts = ar.take<float>(parts / sizeof(float));
   return ar.ok();
 }

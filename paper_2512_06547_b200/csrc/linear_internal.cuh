@@ -51,6 +51,9 @@ struct LinearFwd {
 
 // ---- tcgen05 kernels (linear_tc.cu): bf16, k % 8 == 0, m % 8 == 0, 16-byte aligned operands
 int linear_fwd_tc(const LinearFwd& c);
+// K parts of a product with few output tiles, and the fp32 scratch for them whatever y's type.
+int linear_k_parts(long long n, int k, int m, bool y_f32);
+size_t linear_parts_bytes(long long n, int k, int m);
 // dz (bf16 [rows to the next multiple of 128][m], or null) and, of blocks of 128 rows, its column sums (fp32, or null) from dy and
 // what was kept.  Row i is row row_index[i] of dy (null: i); rows from *count (null: n) on, and rows with row_mask 0, are zeros.
 int linear_grad_z(const void* grad_y, const void* kept, long long n, int m, Act act, const int* row_index, const int* count,

@@ -22,12 +22,21 @@ __device__ __forceinline__ void unpack8(const uint4& u, float (&v)[8]) {
   }
 }
 
+// Outputs that stay in fp32 are sums of 512 products at a time (see PlainEpilogue::kPromote).
+constexpr int kSumBlocks = 8;
+
+struct WeightGradEpilogue : StoreF32EpilogueT<kKLinearGradW> {
+  static constexpr int kGroups = 2;
+  static constexpr int kPromote = kSumBlocks;
+};
+
 template <int ACT, bool KEEP, typename OUT>
 struct LinearEpilogue : PlainEpilogue {
   static constexpr int kKernelId = kKLinear;
   static constexpr bool kChained = true;
   static constexpr bool kPrefetch = true;
   static constexpr int kGroups = 2;
+  static constexpr int kPromote = sizeof(OUT) == 4 ? kSumBlocks : 0;
   struct Params {
     OUT* y;
     const __nv_bfloat16 *bias, *residual;
@@ -181,7 +190,7 @@ int fwd_impl(const LinearFwd& c) {
   ep.n = c.n;
   ep.m = c.m;
   const Begin begin = first_launch(c.count);
-  const int k_parts = c.parts ? ffn_k_parts(c.n, c.m, c.k) : 1;
+  const int k_parts = c.parts ? linear_k_parts(c.n, c.k, c.m, sizeof(OUT) == 4) : 1;
   if (k_parts > 1) {
     const long long rows_pad = (c.n + BM - 1) / BM * BM;
     typename StorePartsEpilogue<kKLinear>::Params sp{c.parts, c.n, static_cast<int>(rows_pad), k_parts, c.m};
@@ -293,6 +302,20 @@ linear_grad_bias_kernel(const float* sums, long long blocks, const int* count, i
 
 }  // namespace
 
+// As ffn_k_parts; parts of fp32 outputs are at most 512 long, or the product is not split (more than 16 of them: the parts would be
+// more traffic than the weights).
+int linear_k_parts(long long n, int k, int m, bool y_f32) {
+  const int parts = ffn_k_parts(n, m, k);
+  if (!y_f32 || parts == 1) return parts;
+  const int need = (k + kSumBlocks * BK - 1) / (kSumBlocks * BK);
+  return need > 16 ? 1 : need > parts ? need : parts;
+}
+
+size_t linear_parts_bytes(long long n, int k, int m) {
+  const int a = linear_k_parts(n, k, m, false), b = linear_k_parts(n, k, m, true), parts = a > b ? a : b;
+  return parts > 1 ? static_cast<size_t>((n + BM - 1) / BM * BM) * m * parts * sizeof(float) : 0;
+}
+
 int linear_fwd_tc(const LinearFwd& c) {
   using B = __nv_bfloat16;
   if (c.act == kActNone) return c.y_f32 ? fwd_impl<kActNone, false, float>(c) : fwd_impl<kActNone, false, B>(c);
@@ -332,7 +355,7 @@ int linear_grads_tc(const void* dz, const void* x, const void* w, long long n, i
   if (grad_w) {
     const Operand a{dz, m, n, m}, b{x, k, n, k};   // dz^T x
     if (grad_dt == A3PO_F32) {
-      using Epi = StoreF32EpilogueT<kKLinearGradW>;
+      using Epi = WeightGradEpilogue;
       A3PO_RETURN_IF((weight_gemm<Epi>(a, b, typename Epi::Params{static_cast<float*>(grad_w), k, m, k, accumulate}, accumulate,
                                        count, status, stream, begin)));
     } else {

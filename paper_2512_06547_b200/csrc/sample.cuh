@@ -5,12 +5,13 @@
 // A random number (or a share of the mass) is compared with running sums of weights, and the token has to be the one that
 // exact sums give, whatever order they are added in.  Sums of fp32 exponentials (2^-23 each) would move a border between two
 // tokens of a flat row of 150,000 by a tenth of a token; fp64 exponentials take the time of several passes over the logits.  So:
-// with d = l - m and e its rounding error (both fp32; two-sum of Knuth), y = (d + e) log2(e) / t as an unevaluated pair of
-// fp32 numbers, y = k + j / 128 + f with |f| <= 2^-8, and
+// with d = l - m and e its rounding error (both fp32; two-sum of Knuth) and y = (d + e) log2(e) / t, the sum of d log2(e) / t and
+// 1.5 2^16 rounds y to k + j / 128, two fused products leave f = y - k - j / 128 with |f| <= 2^-8 exact to 2^-32, and
 //   w = 2^k T[j] (1 + p),  T[j] = 2^(j / 128) in 64 bits,  p = 2^f - 1 from the first three terms of its series.
-// The error is that of p: half a step of an fp32 number of at most 0.0027, below 2^-32 of w.  d = 0 gives 1 exactly.  Sums take
-// T in 64 bits and T p, 400 times smaller, in 32, so that no value is converted between the two types: per element 20
-// (bf16) to 26 instructions, of which one is a 64-bit one.
+// The error is that of f and p: half a step of fp32 numbers of at most 0.004, below 2^-31 of w.  d = 0 gives 1 exactly.  Sums
+// take T in 64 bits and T p, 400 times smaller, in 32, so that no value is converted between the two types, and the fp32 part
+// runs on pairs: 14 (bf16) to 17 instructions per logit, of which one is a 64-bit one (39 without the pairs, with checks for what
+// a warp's logits do not hold, and with conflicts on a table that is not there once per lane of a half-warp).
 #pragma once
 
 #include <cfloat>
@@ -45,58 +46,146 @@ constexpr PowTable make_pow_table() {   // T[j]: product of the roots 2^(1/2), 2
 }
 __device__ const PowTable kPow2 = make_pow_table();
 
+// In shared memory the table is there once for each lane of a half-warp (the lanes whose 64-bit accesses go out together).
+// An entry is T[j] 2^-64, so that the upper 32 bits of its fp32 form are two shifted words (below), with what the bits of the
+// rounded sum add to its upper word taken off beforehand.
+template <int COPIES> struct SharedTable;   // COPIES: 16, or 1 where few weights are taken
+constexpr uint32_t kRoundBits = 0x47c00000u;   // 98304.f = 1.5 2^16, whose last bit is 2^-7
+constexpr float kRound = 98304.f;
+template <int COPIES> struct SharedTable {
+  uint2 e[kPowSteps * COPIES];
+};
+template <int COPIES>
+__device__ __forceinline__ void fill_table(SharedTable<COPIES>& t, int thread, int threads) {
+  for (int i = thread; i < kPowSteps * COPIES; i += threads) {
+    const int j = i / COPIES;
+    const double v = kPow2.t[j] * 0x1p-64;
+    t.e[i] = make_uint2(static_cast<uint32_t>(__double2loint(v)),
+                        static_cast<uint32_t>(__double2hiint(v)) - ((kRoundBits + static_cast<uint32_t>(j)) << 13));
+  }
+}
+
+struct F2 {
+  unsigned long long u;
+};
+__device__ __forceinline__ F2 f2(float x, float y) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.u) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ float2 both(F2 a) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.u));
+  return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.u) : "l"(a.u), "l"(b.u), "l"(c.u));
+  return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
+  return r;
+}
+
+// A sum of weights: high 2^64 - low 2^-64.
+struct WeightSum {
+  double high = 0.0;
+  F2 low = {0ull};
+  __device__ __forceinline__ double value() const {
+    const float2 l = both(low);
+    return fma(-(static_cast<double>(l.x) + static_cast<double>(l.y)), 0x1p-64, high * 0x1p64);
+  }
+};
+
+constexpr float kA = 0.693147180559945f, kB = 0.240226506959101f, kC = 0.0555041086648216f;   // ln 2^n / n!
+
+template <int COPIES>
 struct Weights {
   float max, c_hi, c_lo;   // c = log2(e) / t
   float floor;             // differences below count as this one (w = 2^-100): what is that small adds nothing to a sum that holds a 1
   float zero;              // differences below have weight 0, as exp in 64 bits has
   bool at_inf;             // the largest logit is infinite: it alone has weight
+  const uint2* table;      // this lane's copy
 
-  __device__ __forceinline__ void set(float row_max, float temperature) {
+  __device__ __forceinline__ void set_max(float row_max) {
     max = row_max;
     at_inf = row_max == INFINITY;
+  }
+  __device__ __forceinline__ void set_temperature(float temperature, const SharedTable<COPIES>& t) {
+    table = t.e + threadIdx.x % COPIES;
     const double c = fmin(1.4426950408889634 / static_cast<double>(temperature), 1e37);
     c_hi = static_cast<float>(c);
     c_lo = static_cast<float>(c - static_cast<double>(c_hi));
     floor = static_cast<float>(-100.0 / c);
     zero = fmaxf(static_cast<float>(-745.13321910194122 * static_cast<double>(temperature)), -FLT_MAX);
   }
-  // hi, lo: 2^k T[j], f32 the same rounded down to 32 bits; p as above.  False: the weight is 0.
+  // 2^(k - 64) T[j] for the bits of a rounded sum, and -2^(k + 64) T[j] cut to 32 bits: the exponent field of the former, 959 + k, has
+  // lost its upper two bits there, and its third is the sign.
+  __device__ __forceinline__ void entry(float s, double& t64, float& t32) const {
+    const uint32_t bits = __float_as_uint(s);
+    const uint2 e = table[(bits & (kPowSteps - 1)) * COPIES];
+    const uint32_t hi = e.y + (bits << 13);
+    t64 = __hiloint2double(static_cast<int>(hi), static_cast<int>(e.x));
+    t32 = __uint_as_float(__funnelshift_l(e.x, hi, 3));
+  }
+  // Two logits whose differences lie between floor and 0.
   template <bool EXACT_DIFF>
-  __device__ __forceinline__ bool parts(float l, const double* table, double& t64, float& t32, float& p) const {
+  __device__ __forceinline__ void add(F2 l, WeightSum& sum) const {
+    // a - b as fma(b, -1, a), rounded once as the difference is: a pair has no sign to turn
+    const F2 minus = f2(-1.f, -1.f), round = f2(kRound, kRound);
+    const F2 d = add2(l, f2(-max, -max)), c = f2(c_hi, c_hi);
+    const F2 s = fma2(d, c, round);
+    F2 f = fma2(d, f2(c_lo, c_lo), fma2(d, c, fma2(s, minus, round)));
+    if (!EXACT_DIFF) {
+      const F2 back = fma2(l, minus, d);
+      const F2 e = fma2(add2(f2(max, max), back), minus, fma2(fma2(back, minus, d), minus, l));
+      f = fma2(e, c, f);
+    }
+    const F2 q = fma2(f, fma2(f, f2(kC, kC), f2(kB, kB)), f2(kA, kA));
+    const float2 s2 = both(s);
+    double ta, tb;
+    float a, b;
+    entry(s2.x, ta, a);
+    entry(s2.y, tb, b);
+    sum.high += ta;
+    sum.high += tb;
+    sum.low = fma2(mul2(f, f2(a, b)), q, sum.low);
+  }
+  static __device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
+    return r;
+  }
+  // Any logit.
+  template <bool EXACT_DIFF>
+  __device__ __forceinline__ double operator()(float l) const {
     float d = __fsub_rn(l, max), e = 0.f;
     if (!EXACT_DIFF) {
       const float back = __fsub_rn(d, l);
       e = __fsub_rn(__fsub_rn(l, __fsub_rn(d, back)), __fadd_rn(max, back));
     }
     if (at_inf) d = l == max ? 0.f : -INFINITY;
-    const bool some = d >= zero;   // false for NaN
-    d = fmaxf(d, floor);
-    const float y = __fmul_rn(d, c_hi);
-    float y_lo = fmaf(d, c_lo, fmaf(d, c_hi, -y));
-    if (!EXACT_DIFF && !at_inf) y_lo = fmaf(e, c_hi, y_lo);
-    constexpr float kRound = 98304.f;   // 1.5 2^16: the sum's last bit is 2^-7
-    const float s = __fadd_rn(y, kRound);
-    const float f = __fadd_rn(__fsub_rn(y, __fsub_rn(s, kRound)), y_lo);
-    const int i = __float_as_int(s) - 0x47c00000;   // 128 k + j
-    constexpr float kA = 0.693147180559945f, kB = 0.240226506959101f, kC = 0.0555041086648216f;   // ln 2^n / n!
-    p = f * fmaf(f, fmaf(f, kC, kB), kA);
-    const double t = table[i & (kPowSteps - 1)];
-    const int hi = __double2hiint(t) + ((i >> 7) << 20), lo = __double2loint(t);
-    t64 = __hiloint2double(hi, lo);
-    t32 = __int_as_float(static_cast<int>(__funnelshift_l(lo, hi - 0x38000000, 3)));
-    return some;
-  }
-  template <bool EXACT_DIFF>
-  __device__ __forceinline__ double operator()(float l, const double* table) const {
+    if (!(d >= zero)) return 0.0;   // NaN too
+    if (d < floor) {
+      d = floor;
+      e = 0.f;
+    }
+    const float s = fmaf(d, c_hi, kRound);
+    float f = fmaf(d, c_lo, fmaf(d, c_hi, __fsub_rn(kRound, s)));
+    if (!EXACT_DIFF && !at_inf) f = fmaf(e, c_hi, f);
+    const float p = f * fmaf(f, fmaf(f, kC, kB), kA);
     double t64;
-    float t32, p;
-    const bool some = parts<EXACT_DIFF>(l, table, t64, t32, p);
-    return some ? fma(t64, static_cast<double>(p), t64) : 0.0;
+    float t32;
+    entry(s, t64, t32);
+    t64 *= 0x1p64;
+    return fma(t64, static_cast<double>(p), t64);
   }
 };
 
 // The difference of two bf16 numbers is an fp32 number unless one is 2^16 times smaller than the other; the rounding (2^-25
-// of the difference) of those few is left in.
+// of the difference, of logits that are close to 0 beside the largest) is left in.
 template <typename T> constexpr bool exact_diff() { return sizeof(T) == 2; }
 
 // Logits are read 16 bytes at a time from the 16-byte boundary at or below the row's (or slice's) first element on: `head`
@@ -112,7 +201,51 @@ template <typename T> struct Vec {
     if (sizeof(T) == 4) return __uint_as_float(w[e]);
     return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
   }
+  __device__ __forceinline__ F2 pair(int e) const { return f2(at(e), at(e + 1)); }   // e even
 };
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float min3_nan(float a, float b, float c) {
+  float d;
+  asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// The largest (NaN passed over) and the smallest (NaN if there is one) of N vectors' logits.
+template <typename T, int N>
+__device__ __forceinline__ void extremes(const Vec<T> (&v)[N], float& most, float& least) {
+  if constexpr (sizeof(T) == 4) {
+    most = v[0].at(0);
+    least = v[0].at(0);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        most = max3(most, v[i].at(e), v[i].at(e + 1));
+        least = min3_nan(least, v[i].at(e), v[i].at(e + 1));
+      }
+  } else {
+    uint32_t hi = v[0].w[0], lo = v[0].w[0];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        asm("max.bf16x2 %0, %0, %1;" : "+r"(hi) : "r"(v[i].w[e]));
+        asm("min.NaN.bf16x2 %0, %0, %1;" : "+r"(lo) : "r"(v[i].w[e]));
+      }
+    const float a = __uint_as_float(hi << 16), b = __uint_as_float(hi & 0xffff0000u);
+    const float c = __uint_as_float(lo << 16), d = __uint_as_float(lo & 0xffff0000u);
+    most = fmaxf(a, b);
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(least) : "f"(c), "f"(d));
+  }
+}
+__device__ __forceinline__ float warp_max_any(float v) {   // NaN only if all are
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
 // Elements first .. first + per_vec - 1 of a row of n (first may be negative).
 template <typename T>
 __device__ __forceinline__ Vec<T> load_vec(const T* row, int first, int n) {

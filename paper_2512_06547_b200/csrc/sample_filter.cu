@@ -49,7 +49,7 @@ __device__ __forceinline__ u64 fixed_of(double w) {   // rounded to the nearest 
 }
 
 struct Shared {
-  double table[kPowSteps];
+  SharedTable<16> table;
   u64 slot[kSlots][kMaxCluster];   // what the blocks of the cluster tell one another, each slot once
   u64 part[2][kWarps];
   int warp_count[kWarps];
@@ -353,7 +353,7 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
   row.flip = row.slot = 0;
   row.lane = threadIdx.x % kWarp;
   row.warp = threadIdx.x / kWarp;
-  for (int i = threadIdx.x; i < kPowSteps; i += kThreads) sh.table[i] = kPow2.t[i];
+  fill_table(sh.table, threadIdx.x, kThreads);
 
   // ---- the slice into shared memory, NaN as -inf and -0 as 0
   const int from = row.rank * slice, len = max(0, min(slice, a.v - from));
@@ -398,11 +398,11 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
   }
   bool greedy;
   const float t = a.temp(row_id, greedy);
-  Weights w;
-  w.set(m, t);
+  Weights<16> w;
+  w.set_temperature(t, sh.table);
+  w.set_max(m);
   constexpr bool kExact = exact_diff<T>();
-  const double* table = sh.table;
-  auto weight = [&](float x) { return w.template operator()<kExact>(x, table); };
+  auto weight = [&](float x) { return w.template operator()<kExact>(x); };
   const int top_k = a.top_k ? a.top_k[row_id] : 0;
   const float top_p = a.top_p ? a.top_p[row_id] : 1.f, min_p = a.min_p ? a.min_p[row_id] : 0.f;
   const bool by_mass = top_p < 1.f && !greedy;
@@ -412,7 +412,6 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
   u64 all = 0;
   {
     double s = 0.0;
-    float low = 0.f;
     if (by_mass && !(top_k > 0 && top_k < a.v)) {
       row.each([&](float x, int) {
         const double y = weight(x);
@@ -421,16 +420,22 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
       });
       all = row.cluster_sum(all);
     } else {
-      row.each([&](float x, int) {
-        double t64;
-        float t32, p;
-        if (w.template parts<kExact>(x, table, t64, t32, p)) {
-          s += t64;
-          low = fmaf(t32, p, low);
+      WeightSum fast;
+      for (int j = row.v0 + row.lane; j < row.v1; j += kWarp) {
+        const Vec<T> v[1] = {row.piece(j)};
+        float most, least;
+        extremes(v, most, least);
+        if (least - m >= w.floor && least > -INFINITY) {
+#pragma unroll
+          for (int e = 0; e < VE; e += 2) w.template add<kExact>(v[0].pair(e), fast);
+        } else {
+#pragma unroll
+          for (int e = 0; e < VE; ++e) s += weight(v[0].at(e));
         }
-      });
+      }
+      s += fast.value();
     }
-    total = row.cluster_sum(s + static_cast<double>(low));
+    total = row.cluster_sum(s);
   }
 
   // ---- what is kept: keys above `edge`, and of those equal to it the first `ties` in index order

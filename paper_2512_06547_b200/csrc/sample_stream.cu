@@ -21,59 +21,97 @@ struct Segments {   // per row and segment, of rows that take part
   int per_row;
 };
 
+// v[i] without an array that the compiler has to put into memory.
+template <typename T, int N>
+__device__ __forceinline__ Vec<T> select(const Vec<T> (&v)[N], int i) {
+  Vec<T> r = v[0];
+#pragma unroll
+  for (int k = 1; k < N; ++k)
+    if (k == i) r = v[k];
+  return r;
+}
+
 template <typename T>
-__global__ void __launch_bounds__(kSumThreads)
-sample_sums_kernel(SampleArgs a, Segments out, int items) {
+#ifndef SB
+#define SB 4
+#endif
+__global__ void __launch_bounds__(kSumThreads, SB)
+sample_sums_kernel(SampleArgs a, Segments out, long long items) {
   constexpr int VE = per_vec<T>(), kVecs = kSegment / VE / kWarp;
-  __shared__ double table[kPowSteps];
+  __shared__ SharedTable<16> table;
   allow_next();
-  for (int i = threadIdx.x; i < kPowSteps; i += kSumThreads) table[i] = kPow2.t[i];
+  fill_table(table, threadIdx.x, kSumThreads);
   __syncthreads();
+  // a warp takes neighbouring segments, so that what belongs to a row is looked up once per row
   const int lane = threadIdx.x % kWarp;
-  const int warps = gridDim.x * (kSumThreads / kWarp);
-  for (int item = blockIdx.x * (kSumThreads / kWarp) + threadIdx.x / kWarp; item < items; item += warps) {
-    const int row = item / out.per_row, seg = item - row * out.per_row;
-    if (a.row_mask && a.row_mask[row] == 0) continue;
-    const T* l = static_cast<const T*>(a.logits) + row * a.ld;
-    const int head = head_of(l), first = seg * kSegment - head;
+  const long long warps = static_cast<long long>(gridDim.x) * (kSumThreads / kWarp);
+  const long long me = static_cast<long long>(blockIdx.x) * (kSumThreads / kWarp) + threadIdx.x / kWarp;
+  int item = static_cast<int>(items * me / warps);
+  const int end = static_cast<int>(items * (me + 1) / warps);
+  int row = item / out.per_row, seg = item - row * out.per_row;
+  const T* l = nullptr;
+  int head = 0;
+  bool on = false;
+  Weights<16> w;
+  for (bool fresh = true; item < end; ++item, ++seg) {
+    if (seg == out.per_row) {
+      seg = 0;
+      ++row;
+      fresh = true;
+    }
+    if (fresh) {
+      fresh = false;
+      on = !a.row_mask || a.row_mask[row] != 0;
+      l = static_cast<const T*>(a.logits) + row * a.ld;
+      head = head_of(l);
+      bool greedy;
+      w.set_temperature(a.temp(row, greedy), table);
+    }
+    if (!on) continue;
+    const int first = seg * kSegment - head;
     Vec<T> v[kVecs];
+    if (first >= 0 && first + kSegment <= a.v) {   // the same for the warp
+      const uint4* p = reinterpret_cast<const uint4*>(l + first) + lane;
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) v[i] = load_vec(l, first + (i * kWarp + lane) * VE, a.v);
-    bool greedy;
-    const float t = a.temp(row, greedy);
-    float m = -INFINITY;
+      for (int i = 0; i < kVecs; ++i) {
+        const uint4 u = __ldcs(p + i * kWarp);
+        v[i].w[0] = u.x; v[i].w[1] = u.y; v[i].w[2] = u.z; v[i].w[3] = u.w;
+      }
+    } else {
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i)
-#pragma unroll
-      for (int e = 0; e < VE; ++e) m = fmaxf(m, v[i].at(e));   // passes over NaN
-    m = warp_max(m);
+      for (int i = 0; i < kVecs; ++i) v[i] = load_vec(l, first + (i * kWarp + lane) * VE, a.v);
+    }
+    float m, least;
+    extremes(v, m, least);
+    m = warp_max_any(m);
+    if (!(m > -INFINITY)) m = -INFINITY;
     double sum = 0.0;
+    int count = 0;
     if (m > -INFINITY) {
-      Weights w;
-      w.set(m, t);
-      float low = 0.f;
+      w.set_max(m);
+      // no infinity, NaN or end of a row among the warp's logits, and none that is negligible: nearly always
+      if (__all_sync(0xffffffffu, least - m >= w.floor && least > -INFINITY)) {
+        WeightSum s;
 #pragma unroll
-      for (int i = 0; i < kVecs; ++i)
+        for (int i = 0; i < kVecs; ++i)
 #pragma unroll
-        for (int e = 0; e < VE; ++e) {
-          double t64;
-          float t32, p;
-          if (w.parts<exact_diff<T>()>(v[i].at(e), table, t64, t32, p)) {
-            sum += t64;
-            low = fmaf(t32, p, low);
+          for (int e = 0; e < VE; e += 2) w.template add<exact_diff<T>()>(v[i].pair(e), s);
+        sum = s.value();
+        count = kSegment;
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+          for (int e = 0; e < VE; ++e) {
+            const float x = select(v, i).at(e);
+            sum += w.template operator()<exact_diff<T>()>(x);
+            count += x > -INFINITY ? 1 : 0;
           }
-        }
-      sum = warp_sum(sum + static_cast<double>(low));
+        count = __reduce_add_sync(0xffffffffu, count);
+      }
+      sum = warp_sum(sum);
     }
-    if (a.n_kept) {
-      int c = 0;
-#pragma unroll
-      for (int i = 0; i < kVecs; ++i)
-#pragma unroll
-        for (int e = 0; e < VE; ++e) c += v[i].at(e) > -INFINITY ? 1 : 0;
-      c = __reduce_add_sync(0xffffffffu, c);
-      if (lane == 0) out.count[item] = c;
-    }
+    if (lane == 0 && a.n_kept) out.count[item] = count;
     if (lane == 0) {
       out.sum[item] = sum;
       out.max[item] = m;
@@ -109,7 +147,8 @@ template <typename T>
 __global__ void __launch_bounds__(kPickThreads)
 sample_pick_kernel(SampleArgs a, Segments in) {
   constexpr int VE = per_vec<T>();
-  __shared__ double table[kPowSteps], sh_scan[kPickThreads / kWarp], sh_target, sh_total;
+  __shared__ SharedTable<1> table;
+  __shared__ double sh_scan[kPickThreads / kWarp], sh_target, sh_total;
   __shared__ float sh_max[kPickThreads / kWarp];
   __shared__ int sh_seg, sh_first, sh_last, sh_count;
   const int row = blockIdx.x, lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
@@ -117,7 +156,7 @@ sample_pick_kernel(SampleArgs a, Segments in) {
     if (threadIdx.x == 0) a.put(row, -1, 0.0, 0.0, 0);
     return;
   }
-  for (int i = threadIdx.x; i < kPowSteps; i += kPickThreads) table[i] = kPow2.t[i];
+  fill_table(table, threadIdx.x, kPickThreads);
   if (threadIdx.x == 0) {
     sh_seg = sh_first = INT_MAX;
     sh_last = -1;
@@ -197,8 +236,9 @@ sample_pick_kernel(SampleArgs a, Segments in) {
   const T* l = static_cast<const T*>(a.logits) + row * a.ld;
   const int head = head_of(l);
   const float seg_max = maxes[seg];
-  Weights w;
-  w.set(seg_max, t);
+  Weights<1> w;
+  w.set_temperature(t, table);
+  w.set_max(seg_max);
   double run = 0.0;
   const double want = greedy ? 0.0 : sh_target;
   int token = -1;         // of this lane
@@ -212,7 +252,7 @@ sample_pick_kernel(SampleArgs a, Segments in) {
 #pragma unroll
     for (int e = 0; e < VE; ++e) {
       const float le = v.at(e);
-      x[e] = greedy ? (le == m ? 1.0 : 0.0) : w.template operator()<exact_diff<T>()>(le, table);
+      x[e] = greedy ? (le == m ? 1.0 : 0.0) : w.template operator()<exact_diff<T>()>(le);
       sum += x[e];
       if (x[e] > 0.0) {
         last = first + e;
@@ -270,7 +310,7 @@ int stream_impl(const SampleArgs& a, const Segments& seg, cudaStream_t stream) {
   const int items = a.n * seg.per_row;
   constexpr int kWarps = kSumThreads / kWarp;
   const int want = (items + kWarps - 1) / kWarps, most = sm_count() * 8;
-  A3PO_LAUNCH(kKSample, stream, (sample_sums_kernel<T><<<want < most ? want : most, kSumThreads, 0, stream>>>(a, seg, items)));
+  A3PO_LAUNCH(kKSample, stream, (sample_sums_kernel<T><<<want < most ? want : most, kSumThreads, 0, stream>>>(a, seg, static_cast<long long>(items))));
   A3PO_RETURN_IF(after_launch());
   A3PO_LAUNCH(kKSample, stream, (launch_early(sample_pick_kernel<T>, a.n, kPickThreads, 0, stream, 1, true, a, seg)));
   return after_launch();
