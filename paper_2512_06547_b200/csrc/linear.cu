@@ -33,7 +33,6 @@ int check(long long n, int k, int m, a3po_dtype dt, a3po_activation act_, Act* a
 struct Layout {
   CompactBuffers cb{};
   char* x_c = nullptr;     // rows of x that take part (or x with masked rows zeroed)
-  char* out_c = nullptr;   // y or grad_x in the compact row space
   char* dz = nullptr;
   float* sums = nullptr;   // column sums of dz by blocks of rows
   float* parts = nullptr;
@@ -58,7 +57,6 @@ bool lay_out(Arena& ar, long long n, int k, int m, a3po_dtype dt, Act act, bool 
     l->cb.block_offsets = ar.take<int>(kScan);
     l->cb.pos = ar.take<int>(rows);
     l->cb.idx = ar.take<int>(cap);
-    l->out_c = ar.take<char>(bwd ? cap * k * 2 : cap * m * 4);
   }
   if (compact || (masked && bwd)) l->x_c = ar.take<char>(cap * k * 2);
   if (bwd) {
@@ -123,7 +121,7 @@ int a3po_linear_fwd(const void* x, const void* w, const void* bias, const void* 
   Arena ar(ws, ws_bytes);
   Layout l;
   if (!lay_out(ar, N, K, M, dt, act, row_mask != nullptr, false, &l)) return A3PO_ERR_WORKSPACE;
-  LinearFwd c{x, w, bias, residual, N, K, M, act, y, y_dt == A3PO_F32, kept, l.parts, row_mask, nullptr, nullptr, status,
+  LinearFwd c{x, w, bias, residual, N, K, M, act, y, y_dt == A3PO_F32, kept, l.parts, row_mask, nullptr, nullptr, N, status,
               as_stream(stream_)};
   if (!tc) return linear_fwd_simt(c, dt);
   if (linear_few(N, K, M)) return linear_few_rows_fwd(c);
@@ -132,11 +130,9 @@ int a3po_linear_fwd(const void* x, const void* w, const void* bias, const void* 
   A3PO_RETURN_IF(gather_rows_range(x, K, l.cb.idx, l.cb.count, 0, l.cb.cap, l.x_c, c.stream, true));
   c.x = l.x_c;
   c.n = l.cb.cap;
-  c.y = l.out_c;
   c.row_index = l.cb.idx;
   c.count = l.cb.count;
-  A3PO_RETURN_IF(linear_fwd_tc(c));
-  return scatter_rows(l.out_c, c.y_f32 ? 2 * M : M, l.cb.pos, N, y, c.stream, true);   // in pieces of 16 bytes, whatever they hold
+  return linear_fwd_tc(c);
 }
 
 int a3po_linear_bwd(const void* x, const void* w, const uint8_t* row_mask, const void* kept, size_t kept_bytes,
@@ -197,9 +193,8 @@ int a3po_linear_bwd(const void* x, const void* w, const uint8_t* row_mask, const
   }
   if (grad_bias) A3PO_RETURN_IF(linear_grad_bias(l.sums, (rows + kZRows - 1) / kZRows, count, M, grad_bias, accumulate, stream));
   if (!grad_x && !grad_w) return A3PO_OK;
-  A3PO_RETURN_IF(linear_grads_tc(dz, xs, w, rows, K, M, compact && grad_x ? l.out_c : grad_x, grad_w, grad_w_dt, accumulate,
-                                 l.parts, count, first, status, stream));
-  return compact && grad_x ? scatter_rows(l.out_c, K, l.cb.pos, N, grad_x, stream, true) : A3PO_OK;
+  return linear_grads_tc(dz, xs, w, rows, K, M, grad_x, grad_w, grad_w_dt, accumulate, l.parts, index, count, row_mask, N, first,
+                         status, stream);
 }
 
 }  // extern "C"

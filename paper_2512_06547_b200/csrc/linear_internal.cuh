@@ -32,8 +32,8 @@ __device__ __forceinline__ void linear_activation(float z, float& a, float& slop
 }
 #endif
 
-// One forward call.  Tensor cores with a row mask: x, y and kept are in the compact row space, of which `count` rows exist;
-// row_index[i] is row i's place in the residual.
+// One forward call.  Tensor cores with a row mask: x and kept are in the compact row space of n rows, of which `count` exist;
+// row_index[i] is row i's place among the `rows` rows of y and the residual.
 struct LinearFwd {
   const void *x, *w, *bias, *residual;
   long long n;
@@ -43,8 +43,9 @@ struct LinearFwd {
   bool y_f32;
   void* kept;
   float* parts;               // scratch of a K split, or null
-  const uint8_t* row_mask;    // few rows and FP32 pipes
+  const uint8_t* row_mask;
   const int *row_index, *count;
+  long long rows;
   uint32_t* status;
   cudaStream_t stream;
 };
@@ -61,10 +62,11 @@ int linear_grad_z(const void* grad_y, const void* kept, long long n, int m, Act 
 // grad_bias (+)= the sums of `blocks` blocks (rows / 128 of *count where it is given).
 int linear_grad_bias(const float* sums, long long blocks, const int* count, int m, float* grad_bias, int accumulate,
                      cudaStream_t stream);
-// grad_w[m, k] = dz^T x, grad_x[n, k] = dz W (either null: not wanted).  first: the call's first launch.
+// grad_w[m, k] = dz^T x, grad_x = dz W (either null: not wanted), the latter's rows at row_index[i] of `rows` where that is given.
+// first: the call's first launch.
 int linear_grads_tc(const void* dz, const void* x, const void* w, long long n, int k, int m, void* grad_x, void* grad_w,
-                    a3po_dtype grad_dt, int accumulate, float* parts, const int* count, bool first, uint32_t* status,
-                    cudaStream_t stream);
+                    a3po_dtype grad_dt, int accumulate, float* parts, const int* row_index, const int* count,
+                    const uint8_t* row_mask, long long rows, bool first, uint32_t* status, cudaStream_t stream);
 
 // ---- few rows (linear_few.cu)
 int linear_few_rows_fwd(const LinearFwd& c);

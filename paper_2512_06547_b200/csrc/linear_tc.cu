@@ -22,6 +22,13 @@ __device__ __forceinline__ void unpack8(const uint4& u, float (&v)[8]) {
   }
 }
 
+// 32 bytes at a 32-byte boundary.
+__device__ __forceinline__ void store_32(void* p, const uint4& a, const uint4& b) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w),
+               "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+               : "memory");
+}
+
 // Outputs that stay in fp32 are sums of 512 products at a time (see PlainEpilogue::kPromote).
 constexpr int kSumBlocks = 8;
 
@@ -30,9 +37,11 @@ struct WeightGradEpilogue : StoreF32EpilogueT<kKLinearGradW> {
   static constexpr int kPromote = kSumBlocks;
 };
 
-template <int ACT, bool KEEP, typename OUT>
+// SCATTER: the rows are those of a compact row space and go straight to their places row_index[i] (32 bytes a store: whole
+// sectors), so that no pass has to move them there; otherwise through the copy engine.
+template <int ACT, bool KEEP, typename OUT, bool SCATTER = false, int KERNEL_ID = kKLinear>
 struct LinearEpilogue : PlainEpilogue {
-  static constexpr int kKernelId = kKLinear;
+  static constexpr int kKernelId = KERNEL_ID;
   static constexpr bool kChained = true;
   static constexpr bool kPrefetch = true;
   static constexpr int kGroups = 2;
@@ -41,21 +50,27 @@ struct LinearEpilogue : PlainEpilogue {
     OUT* y;
     const __nv_bfloat16 *bias, *residual;
     uint8_t* kept;
-    const int *row_index, *count;
+    const int *row_index, *count;   // SCATTER
     long long n;
     int m;
+    int whole_sectors;              // SCATTER: rows start at 32-byte boundaries and end there
   };
   static int make_c_map(const Params& p, CUtensorMap* map) {
     return make_out_map(map, p.y, sizeof(OUT), p.m, p.n, p.m);
   }
   const __nv_bfloat16* res;   // this thread's row of the residual, or null
+  OUT* out;                   // SCATTER: its row of y, or null
   int end_col;
   uint4 next[4];              // its next 32 columns
   uint8_t* cur;
   __device__ __forceinline__ void begin(const Params& p, long long row) {
     res = nullptr;
-    if (p.residual && row < (p.count ? *p.count : p.n))
-      res = p.residual + (p.row_index ? p.row_index[row] : row) * static_cast<long long>(p.m);
+    out = nullptr;
+    if (!SCATTER && !p.residual) return;
+    if (row >= (SCATTER ? min(static_cast<long long>(*p.count), p.n) : p.n)) return;
+    const long long at = (SCATTER ? p.row_index[row] : row) * static_cast<long long>(p.m);
+    if (SCATTER) out = p.y + at;
+    if (p.residual) res = p.residual + at;
   }
   __device__ __forceinline__ void read_residual(int col0) {
 #pragma unroll
@@ -108,7 +123,30 @@ struct LinearEpilogue : PlainEpilogue {
         for (int i = 0; i < 8; ++i) v[q * 8 + i] += b[i];
       }
     }
-    if constexpr (sizeof(OUT) == 4) {
+    if constexpr (SCATTER) {
+      if (!out) return;   // no barriers on this path
+      constexpr int kPer = 32 / sizeof(OUT), kStores = kEpiChunk / kPer;
+#pragma unroll
+      for (int q = 0; q < kStores; ++q) {
+        const int c = col0 + q * kPer;
+        if (c >= p.m) break;
+        uint4 a, b;
+        if constexpr (sizeof(OUT) == 4) {
+          const float* f = v + q * 8;
+          a = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+          b = make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
+        } else {
+          a = pack8(v, 2 * q);
+          b = pack8(v, 2 * q + 1);
+        }
+        if (p.whole_sectors) {
+          store_32(out + c, a, b);
+        } else {   // rows start at multiples of 16 bytes, and the second half may lie past the row
+          *reinterpret_cast<uint4*>(out + c) = a;
+          if (c + kPer / 2 < p.m) *reinterpret_cast<uint4*>(out + c + kPer / 2) = b;
+        }
+      }
+    } else if constexpr (sizeof(OUT) == 4) {
       uint8_t* s = st.acquire();
 #pragma unroll
       for (int q = 0; q < 8; ++q)
@@ -127,9 +165,9 @@ struct LinearEpilogue : PlainEpilogue {
 };
 
 // The same after the parts of a K split: 4 columns per thread, the parts in index order, 8 on their way at a time.
-template <int ACT, bool KEEP, typename OUT>
+template <class Epi, int ACT, bool KEEP, typename OUT>
 __global__ void __launch_bounds__(256)
-linear_add_parts_kernel(const float* parts, int n_parts, long long part_stride, typename LinearEpilogue<ACT, KEEP, OUT>::Params p) {
+linear_add_parts_kernel(const float* parts, int n_parts, long long part_stride, typename Epi::Params p) {
   wait_for_previous();
   allow_next();
   const long long rows = p.count ? (*p.count < p.n ? *p.count : p.n) : p.n;
@@ -166,20 +204,56 @@ linear_add_parts_kernel(const float* parts, int n_parts, long long part_stride, 
       linear_activation<ACT>(v[j], a, slope);
       v[j] = a;
     }
+    const long long at = (p.row_index ? p.row_index[row] : row) * static_cast<long long>(p.m) + col;
     if (p.residual) {
-      const __nv_bfloat16* res = p.residual + (p.row_index ? p.row_index[row] : row) * static_cast<long long>(p.m) + col;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] += to_float(res[j]);
+      for (int j = 0; j < 4; ++j) v[j] += to_float(p.residual[at + j]);
     }
-    if constexpr (sizeof(OUT) == 4) reinterpret_cast<float4*>(p.y)[i] = make_float4(v[0], v[1], v[2], v[3]);
-    else reinterpret_cast<uint2*>(p.y)[i] = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    if constexpr (sizeof(OUT) == 4) *reinterpret_cast<float4*>(p.y + at) = make_float4(v[0], v[1], v[2], v[3]);
+    else *reinterpret_cast<uint2*>(p.y + at) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
   }
 }
 
-template <int ACT, bool KEEP, typename OUT>
-int fwd_impl(const LinearFwd& c) {
-  using Epi = LinearEpilogue<ACT, KEEP, OUT>;
-  const Operand a{c.x, c.n, c.k, c.k}, b{c.w, c.m, c.k, c.k};
+// Zeros for the rows that take no part.  It depends on nothing that the kernel ahead of it does, and runs beside it.
+__global__ void __launch_bounds__(256)
+linear_zero_rows_kernel(const uint8_t* row_mask, long long n, int vec_per_row, uint4* dst) {
+  const int lane = threadIdx.x % kWarp;
+  const long long warps = static_cast<long long>(gridDim.x) * (256 / kWarp);
+  for (long long t = static_cast<long long>(blockIdx.x) * (256 / kWarp) + threadIdx.x / kWarp; t < n; t += warps) {
+    if (row_mask[t] != 0) continue;
+    for (int j = lane; j < vec_per_row; j += kWarp) __stcs(dst + t * vec_per_row + j, make_uint4(0, 0, 0, 0));
+  }
+  wait_for_previous();
+}
+int zero_rows(const uint8_t* row_mask, long long n, int m, int elt, void* dst, cudaStream_t stream) {
+  const long long want = (n + 7) / 8;
+  const int blocks = static_cast<int>(want < sm_count() * 4ll ? want : sm_count() * 4ll);
+  A3PO_LAUNCH(kKLinear, stream, (launch_early(linear_zero_rows_kernel, blocks, 256, 0, stream, 1, true, row_mask, n, m * elt / 16,
+                                              static_cast<uint4*>(dst))));
+  return after_launch();
+}
+
+// The product with its epilogue: in K parts, or at once.
+template <class Epi, int ACT, bool KEEP, typename OUT, bool B_MN>
+int product(const Operand& a, const Operand& b, const typename Epi::Params& ep, float* parts, int k_parts, uint32_t* status,
+            cudaStream_t stream, Begin begin) {
+  if (k_parts > 1) {
+    const long long rows_pad = (ep.n + BM - 1) / BM * BM;
+    using Parts = StorePartsEpilogue<Epi::kKernelId>;
+    typename Parts::Params sp{parts, ep.n, static_cast<int>(rows_pad), k_parts, ep.m};
+    A3PO_RETURN_IF((launch_gemm<Parts, false, B_MN, 1>(a, b, 0, sp, rows_as_m(ep.count, ep.n), status, stream, k_parts, begin)));
+    const long long want = (ep.n * (ep.m / kAddCols) + 255) / 256;
+    const int blocks = static_cast<int>(want < sm_count() * 8ll ? want : sm_count() * 8ll);
+    A3PO_LAUNCH(Epi::kKernelId, stream, (launch_early(linear_add_parts_kernel<Epi, ACT, KEEP, OUT>, blocks, 256, 0, stream, 1, true,
+                                                      static_cast<const float*>(parts), k_parts, rows_pad * ep.m, ep)));
+    return after_launch();
+  }
+  return contract<Epi, false, B_MN>(a, b, ep, rows_as_m(ep.count, ep.n), status, stream, begin);
+}
+
+template <int ACT, bool KEEP, typename OUT, bool SCATTER>
+int fwd_typed(const LinearFwd& c) {
+  using Epi = LinearEpilogue<ACT, KEEP, OUT, SCATTER>;
   typename Epi::Params ep;
   ep.y = static_cast<OUT*>(c.y);
   ep.bias = static_cast<const __nv_bfloat16*>(c.bias);
@@ -189,67 +263,74 @@ int fwd_impl(const LinearFwd& c) {
   ep.count = c.count;
   ep.n = c.n;
   ep.m = c.m;
-  const Begin begin = first_launch(c.count);
-  const int k_parts = c.parts ? linear_k_parts(c.n, c.k, c.m, sizeof(OUT) == 4) : 1;
-  if (k_parts > 1) {
-    const long long rows_pad = (c.n + BM - 1) / BM * BM;
-    typename StorePartsEpilogue<kKLinear>::Params sp{c.parts, c.n, static_cast<int>(rows_pad), k_parts, c.m};
-    A3PO_RETURN_IF((launch_gemm<StorePartsEpilogue<kKLinear>, false, false, 1>(a, b, 0, sp, rows_as_m(c.count, c.n), c.status,
-                                                                             c.stream, k_parts, begin)));
-    const long long want = (c.n * (c.m / kAddCols) + 255) / 256;
-    const int blocks = static_cast<int>(want < sm_count() * 8ll ? want : sm_count() * 8ll);
-    A3PO_LAUNCH(kKLinear, c.stream, (launch_early(linear_add_parts_kernel<ACT, KEEP, OUT>, blocks, 256, 0, c.stream, 1, true,
-                                                  static_cast<const float*>(c.parts), k_parts, rows_pad * c.m, ep)));
-    return after_launch();
-  }
-  return contract<Epi, false, false>(a, b, ep, rows_as_m(c.count, c.n), c.status, c.stream, begin);
+  ep.whole_sectors = aligned_to(c.y, 32) && c.m * sizeof(OUT) % 32 == 0;
+  return product<Epi, ACT, KEEP, OUT, false>(Operand{c.x, c.n, c.k, c.k}, Operand{c.w, c.m, c.k, c.k}, ep, c.parts,
+                                             c.parts ? linear_k_parts(c.n, c.k, c.m, sizeof(OUT) == 4) : 1, c.status, c.stream,
+                                             first_launch(c.count));
+}
+template <int ACT, bool KEEP, typename OUT>
+int fwd_impl(const LinearFwd& c) {
+  if (!c.row_index) return fwd_typed<ACT, KEEP, OUT, false>(c);
+  A3PO_RETURN_IF((fwd_typed<ACT, KEEP, OUT, true>(c)));
+  return zero_rows(c.row_mask, c.rows, c.m, sizeof(OUT), c.y, c.stream);
 }
 
 // ------------------------------------------------------------------------------------ dz and its column sums
-// A block takes 128 rows, one per thread, and kGradCols columns in steps of 32.
-constexpr int kGradCols = 128;
+// A block takes 128 rows and 64 columns.  dy and dz are read and written in whole rows of 128 bytes and change hands in shared
+// memory (16-byte pieces, swizzled), because z and the sums want one row per thread.
+constexpr int kGradCols = 64;
 template <int ACT>
 __global__ void __launch_bounds__(kZRows)
 linear_grad_z_kernel(const __nv_bfloat16* grad_y, const uint8_t* kept, long long n, int m, const int* row_index,
                      const int* count, const uint8_t* row_mask, __nv_bfloat16* dz, float* sums) {
-  __shared__ float part[kZRows / kWarp][kZCols];
+  __shared__ __align__(16) uint4 tile[kZRows * 8];
+  __shared__ float part[kZRows / kWarp][kGradCols];
   wait_for_previous();
   allow_next();
   const long long rows = count ? (*count < n ? *count : n) : n;
-  const long long row0 = static_cast<long long>(blockIdx.x) * kZRows, row = row0 + threadIdx.x;
+  const long long row0 = static_cast<long long>(blockIdx.x) * kZRows;
   if (row0 >= rows) return;
   const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
-  const bool live = row < rows && (!row_mask || row_mask[row] != 0);
-  const __nv_bfloat16* gy = live ? grad_y + (row_index ? row_index[row] : row) * static_cast<long long>(m) : nullptr;
-  const int c_end = min(static_cast<int>(blockIdx.y + 1) * kGradCols, m);
-  for (int c0 = blockIdx.y * kGradCols; c0 < c_end; c0 += kZCols) {
+  const int c0 = blockIdx.y * kGradCols, j = threadIdx.x % 8;   // this thread's piece of a row while rows are copied
+  const bool in = c0 + j * 8 < m;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = i * 16 + threadIdx.x / 8;
+    const long long row = row0 + r;
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (in && row < rows && (!row_mask || row_mask[row] != 0))
+      u = __ldcs(reinterpret_cast<const uint4*>(grad_y + (row_index ? row_index[row] : row) * static_cast<long long>(m) + c0) + j);
+    tile[r * 8 + (j ^ (r & 7))] = u;
+  }
+  const int r = threadIdx.x;
+  const long long row = row0 + r;
+  const bool live = row < rows && (!row_mask || row_mask[row] != 0);   // else dy is 0, and what was kept may be anything
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int c = c0 + half * kZCols;
+    float z[kZCols];
+    if (ACT != kActNone) {
+      const float4* from = reinterpret_cast<const float4*>(kept + z_tile(row, c, m)) + r;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const float4 f = live && c + q * 4 < m ? __ldcs(from + q * kZRows) : make_float4(0.f, 0.f, 0.f, 0.f);
+        z[q * 4] = f.x; z[q * 4 + 1] = f.y; z[q * 4 + 2] = f.z; z[q * 4 + 3] = f.w;
+      }
+    }
+    if (half == 0) __syncthreads();
     float v[kZCols];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      float g[8] = {};
-      if (live && c0 + q * 8 < m) unpack8(__ldcs(reinterpret_cast<const uint4*>(gy + c0) + q), g);
+      float g[8];
+      uint4& u = tile[r * 8 + ((half * 4 + q) ^ (r & 7))];
+      unpack8(u, g);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[q * 8 + i] = g[i];
-    }
-    if (ACT != kActNone && live) {   // columns of the last tile past m hold nothing: v is 0 there, and stays so
-      const float4* tile = reinterpret_cast<const float4*>(kept + z_tile(row, c0, m)) + threadIdx.x;
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        if (c0 + q * 4 >= m) continue;
-        const float4 z4 = __ldcs(tile + q * kZRows);
-        const float z[4] = {z4.x, z4.y, z4.z, z4.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float a, slope;
-          linear_activation<ACT>(z[i], a, slope);
-          v[q * 4 + i] *= slope;
-        }
+      for (int i = 0; i < 8; ++i) {
+        float a, slope = 1.f;
+        if (ACT != kActNone) linear_activation<ACT>(z[q * 8 + i], a, slope);
+        v[q * 8 + i] = g[i] * slope;
       }
-    }
-    if (dz && row < (n + kZRows - 1) / kZRows * kZRows) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (c0 + q * 8 < m && (count || row < n)) reinterpret_cast<uint4*>(dz + row * m + c0)[q] = pack8(v, q);
+      u = pack8(v, q);
     }
     if (sums) {
       // lane c ends with the warp's sum of column c: each step halves the columns that a lane still adds
@@ -262,16 +343,23 @@ linear_grad_z_kernel(const __nv_bfloat16* grad_y, const uint8_t* kept, long long
           v[i] = (up ? v[i + o] : v[i]) + other;
         }
       }
-      part[warp][lane] = v[0];
-      __syncthreads();
-      if (threadIdx.x < kZCols && c0 + static_cast<int>(threadIdx.x) < m) {
-        float t = 0.f;
-#pragma unroll
-        for (int w = 0; w < kZRows / kWarp; ++w) t += part[w][threadIdx.x];
-        sums[static_cast<long long>(blockIdx.x) * m + c0 + threadIdx.x] = t;
-      }
-      __syncthreads();
+      part[warp][half * kZCols + lane] = v[0];
     }
+  }
+  __syncthreads();
+  if (dz) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int to = i * 16 + threadIdx.x / 8;
+      // rows past the last one are zeros up to the next multiple of 128, where the buffer has them
+      if (in && (count || row0 + to < n)) reinterpret_cast<uint4*>(dz + (row0 + to) * m + c0)[j] = tile[to * 8 + (j ^ (to & 7))];
+    }
+  }
+  if (sums && threadIdx.x < kGradCols && c0 + static_cast<int>(threadIdx.x) < m) {
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < kZRows / kWarp; ++w) t += part[w][threadIdx.x];
+    sums[static_cast<long long>(blockIdx.x) * m + c0 + threadIdx.x] = t;
   }
 }
 
@@ -349,8 +437,8 @@ int linear_grad_bias(const float* sums, long long blocks, const int* count, int 
 }
 
 int linear_grads_tc(const void* dz, const void* x, const void* w, long long n, int k, int m, void* grad_x, void* grad_w,
-                    a3po_dtype grad_dt, int accumulate, float* parts, const int* count, bool first, uint32_t* status,
-                    cudaStream_t stream) {
+                    a3po_dtype grad_dt, int accumulate, float* parts, const int* row_index, const int* count,
+                    const uint8_t* row_mask, long long rows, bool first, uint32_t* status, cudaStream_t stream) {
   Begin begin = first ? Begin::kAfter : Begin::kEarly;
   if (grad_w) {
     const Operand a{dz, m, n, m}, b{x, k, n, k};   // dz^T x
@@ -366,8 +454,15 @@ int linear_grads_tc(const void* dz, const void* x, const void* w, long long n, i
     begin = Begin::kBeside;   // it reads what the weight gradient reads and writes apart from it
   }
   if (!grad_x) return A3PO_OK;
-  return rows_gemm<kKLinearGradX, true>(Operand{dz, n, m, m}, Operand{w, k, m, k}, static_cast<__nv_bfloat16*>(grad_x), parts,
-                                        count, status, stream, begin);
+  const Operand a{dz, n, m, m}, b{w, k, m, k};   // dz W
+  if (!row_index)
+    return rows_gemm<kKLinearGradX, true>(a, b, static_cast<__nv_bfloat16*>(grad_x), parts, count, status, stream, begin);
+  using Epi = LinearEpilogue<kActNone, false, __nv_bfloat16, true, kKLinearGradX>;
+  typename Epi::Params ep{static_cast<__nv_bfloat16*>(grad_x), nullptr, nullptr, nullptr, row_index, count, n, k,
+                          aligned_to(grad_x, 32) && k % 16 == 0};
+  A3PO_RETURN_IF((product<Epi, kActNone, false, __nv_bfloat16, true>(a, b, ep, parts, parts ? ffn_k_parts(n, k, m) : 1, status,
+                                                                     stream, begin)));
+  return zero_rows(row_mask, rows, k, 2, grad_x, stream);
 }
 
 }  // namespace a3po
