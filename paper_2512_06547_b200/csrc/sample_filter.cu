@@ -24,11 +24,13 @@ namespace {
 constexpr int kThreads = 512, kWarps = kThreads / kWarp, kMaxCluster = 8;
 constexpr int kBinBits = 11, kBins = 1 << kBinBits;
 constexpr int kMaxSlice = 196608;        // bytes of a row in one block
-constexpr int kSlots = 32;
+constexpr int kSlots = 40;
+constexpr int kList = kBins;             // candidates that one block finishes alone
 constexpr double kFixed = 8796093022208.0;   // 2^43: a weight as a whole number
 
 using u32 = uint32_t;
 using u64 = unsigned long long;
+static_assert(kList * sizeof(u64) == 2 * kBins * sizeof(u32), "the list takes the histograms' place");
 
 __device__ __forceinline__ u32 key_of(float l) {
   const u32 b = __float_as_uint(l);
@@ -52,8 +54,14 @@ struct Shared {
   SharedTable<16> table;
   u64 slot[kSlots][kMaxCluster];   // what the blocks of the cluster tell one another, each slot once
   u64 part[2][kWarps];
+  double stretch[kWarps];          // sums of the warps' weights
   int warp_count[kWarps];
-  u32 lo[kBins], hi[kBins];
+  union {
+    struct {
+      u32 lo[kBins], hi[kBins];    // histograms
+    };
+    u64 list[kList];               // the first block's: candidates in index order (ordered bits, index)
+  };
 };
 
 __device__ __forceinline__ void store_remote(u64* here, u32 rank, u64 v) {
@@ -139,6 +147,47 @@ struct Row {
     sync();
     for (int r = 0; r < cluster; ++r) t = max(t, s[r]);
     return t;
+  }
+
+  __device__ __forceinline__ u64 block_min(u64 v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = min(v, __shfl_xor_sync(0xffffffffu, v, o));
+    u64* p = sh.part[flip ^= 1];
+    if (lane == 0) p[warp] = v;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) v = min(v, p[i]);
+    return v;
+  }
+  __device__ __forceinline__ u64 cluster_min(u64 v) {
+    v = block_min(v);
+    const u64* s = tell(v);
+    sync();
+    for (int r = 0; r < cluster; ++r) v = min(v, s[r]);
+    return v;
+  }
+  // Sum over the threads below this one; total: over all.
+  template <typename S>
+  __device__ __forceinline__ S scan(S x, S& total) {
+    S inc = x;
+#pragma unroll
+    for (int o = 1; o < kWarp; o <<= 1) {
+      const S y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
+    }
+    static_assert(sizeof(S) <= sizeof(u64), "");
+    S* p = reinterpret_cast<S*>(sh.part[flip ^= 1]);
+    if (lane == kWarp - 1) p[warp] = inc;
+    __syncthreads();
+    S before = __shfl_up_sync(0xffffffffu, inc, 1);
+    if (lane == 0) before = 0;
+    total = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      if (i < warp) before += p[i];
+      total += p[i];
+    }
+    return before;
   }
 
   // ---- the slice.  f(l, index) for the logits of this thread
@@ -335,6 +384,217 @@ __device__ __forceinline__ int find_in_stretch(const Row<T>& row, double want, F
   return top;
 }
 
+// Rows whose kept tokens are among a few candidates.  The logits are counted by their distance to the largest, in steps of a
+// 64th (top-p: a 128th) of the temperature; the first step that has, with all above it, k tokens, or more than the share p of
+// the mass if every token of a step had the least weight of the step, bounds what top-k or top-p can keep (min-p's bound is known
+// beforehand).  If that leaves at most kList tokens, the first block gets them in index order, sorts a copy, cuts it and samples,
+// and the others are done.  One pass over the logits and three cluster barriers less than a level of the histograms above takes;
+// false: the row is not of this kind (the same for the whole cluster).
+template <typename T, class W>
+__device__ __forceinline__ bool sample_from_candidates(Row<T>& row, const SampleArgs& a, int row_id, const W& w, float t, double total,
+                                                       int top_k, float top_p, float min_p, u64* sorted) {
+  constexpr int VE = per_vec<T>();
+  Shared& sh = row.sh;
+  const bool by_count = top_k > 0 && top_k < a.v, by_mass = top_p < 1.f, by_min = min_p > 0.f;
+  const bool mass_alone = by_mass && !by_count;
+  const float steps = mass_alone ? 128.f : 64.f, scale = steps / t;
+  if (w.at_inf || !(scale < 1e30f)) return false;
+  // ---- counts
+  for (int i = threadIdx.x; i < kBins; i += kThreads) sh.lo[i] = 0;
+  __syncthreads();
+  auto distance = [&](float l) { return __fmul_rn(__fsub_rn(w.max, l), scale); };
+  row.each([&](float l, int) {
+    const float x = distance(l);
+    if (x < static_cast<float>(kBins)) atomicAdd(&sh.lo[static_cast<int>(x)], 1u);   // false for NaN
+  });
+  row.sync();
+  const int mine = kBins / row.cluster, per = (mine + kThreads - 1) / kThreads;
+  const int first = static_cast<int>(threadIdx.x) * per;   // of this block's bins
+  constexpr int kMost = kBins / kThreads;
+  u32 got[kMost];
+  u32 count = 0;
+  double mass = 0.0;
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    got[i] = 0;
+    if (i < per && first + i < mine) {
+      const int b = row.rank * mine + first + i;
+      for (int r = 0; r < row.cluster; ++r) got[i] += load_remote(&sh.lo[b], r);
+      count += got[i];
+      if (mass_alone) mass += static_cast<double>(got[i]) * static_cast<double>(expf(static_cast<float>(b + 1) * (-1.f / steps)));
+    }
+  }
+  u32 block_count;
+  double block_mass = 0.0;
+  u32 cum = row.scan(count, block_count);
+  double cum_mass = mass_alone ? row.scan(mass, block_mass) : 0.0;
+  const u64* counts = row.tell(block_count);
+  const u64* masses = row.tell(static_cast<u64>(__double_as_longlong(block_mass)));
+  row.sync();
+  for (int r = 0; r < row.rank; ++r) {
+    cum += static_cast<u32>(counts[r]);
+    cum_mass += __longlong_as_double(static_cast<long long>(masses[r]));
+  }
+  const double enough = static_cast<double>(fmaxf(top_p, 0.f)) * total * (1.0 + 1e-5);   // expf and the distance are not exact
+  int min_bin = INT_MAX;   // the first bin that lies below what min-p keeps
+  if (by_min && !by_mass) {
+    const float at = min_p >= 1.f ? 0.f : -logf(min_p) * steps;
+    if (at < static_cast<float>(kBins - 3)) min_bin = static_cast<int>(at) + 2;
+  }
+  u64 best = ~0ull;
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    if (i < per && first + i < mine) {
+      const int b = row.rank * mine + first + i;
+      cum += got[i];
+      if (mass_alone) cum_mass += static_cast<double>(got[i]) * static_cast<double>(expf(static_cast<float>(b + 1) * (-1.f / steps)));
+      const bool stop = (by_count && cum >= static_cast<u32>(top_k)) || (mass_alone && cum_mass >= enough) || b >= min_bin;
+      if (stop && best == ~0ull) best = static_cast<u64>(b) << 32 | cum;
+    }
+  }
+  best = row.cluster_min(best);
+  const int n = static_cast<int>(best & 0xffffffffu);
+  if (best == ~0ull || n > kList) return false;
+  const float limit = static_cast<float>(static_cast<int>(best >> 32) + 1);
+
+  // ---- candidates, in index order, to the first block
+  int c = 0;
+  for (int j = row.v0 + row.lane; j < row.v1; j += kWarp) {
+    const Vec<T> v = row.piece(j);
+#pragma unroll
+    for (int e = 0; e < VE; ++e) c += distance(v.at(e)) < limit ? 1 : 0;
+  }
+  c = __reduce_add_sync(0xffffffffu, c);
+  if (row.lane == 0) sh.warp_count[row.warp] = c;
+  __syncthreads();
+  int block = 0, at = 0;
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) {
+    if (i == row.warp) at = block;
+    block += sh.warp_count[i];
+  }
+  const u64* blocks = row.tell(static_cast<u64>(block));
+  row.sync();   // after this no histogram is read any more
+  for (int r = 0; r < row.rank; ++r) at += static_cast<int>(blocks[r]);
+  if (c > 0) {
+    for (int j0 = row.v0; j0 < row.v1; j0 += kWarp) {
+      const int j = j0 + row.lane;
+      u32 in = 0;
+      Vec<T> v;
+      if (j < row.v1) {
+        v = row.piece(j);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) in |= distance(v.at(e)) < limit ? 1u << e : 0u;
+      }
+      if (!__any_sync(0xffffffffu, in != 0)) continue;
+      int inc = __popc(in);
+#pragma unroll
+      for (int o = 1; o < kWarp; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (row.lane >= o) inc += y;
+      }
+      int to = at + inc - __popc(in);
+      at += __shfl_sync(0xffffffffu, inc, kWarp - 1);
+      if (in) {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+          if (in >> e & 1u) {   // larger logits first, then lower indexes: ascending
+            if (to < kList)
+              store_remote(&sh.list[to], 0, static_cast<u64>(~key_of(v.at(e))) << 32 | static_cast<u32>(row.base + j * VE + e));
+            ++to;
+          }
+        }
+      }
+    }
+  }
+  row.sync();
+  if (row.rank != 0) return true;
+
+  // ---- the first block alone from here on
+  int size = kWarp;
+  while (size < n) size *= 2;
+  for (int i = threadIdx.x; i < size; i += kThreads) sorted[i] = i < n ? sh.list[i] : ~0ull;
+  for (int k = 2; k <= size; k *= 2) {          // bitonic sort
+    for (int j = k / 2; j > 0; j /= 2) {
+      __syncthreads();
+      for (int i = threadIdx.x; i < size / 2; i += kThreads) {
+        const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
+        const u64 x = sorted[lo], y = sorted[hi];
+        if ((x > y) == ((lo & k) == 0)) {
+          sorted[lo] = y;
+          sorted[hi] = x;
+        }
+      }
+    }
+  }
+  __syncthreads();
+  auto logit = [](u64 entry) { return of_key(~static_cast<u32>(entry >> 32)); };
+  // how many of the sorted are kept; a thread takes neighbours
+  constexpr int kEach = kList / kThreads;
+  const int s0 = static_cast<int>(threadIdx.x) * kEach;
+  int kept = by_count ? min(n, top_k) : n;
+  if (by_mass) {
+    u64 x[kEach], sum = 0, all = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      x[i] = s0 + i < kept ? fixed_of(w.template operator()<exact_diff<T>()>(logit(sorted[s0 + i]))) : 0;
+      sum += x[i];
+    }
+    u64 run = row.scan(sum, all);
+    const double of = by_count ? static_cast<double>(all) : total * kFixed;
+    const double share = static_cast<double>(fmaxf(top_p, 0.f)) * of * (1.0 - 0x1p-48);
+    const u64 need = share > 1.0 ? static_cast<u64>(ceil(share)) : 1;
+    u64 upto = kept;   // tokens with all of `need`
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      run += x[i];
+      if (s0 + i < kept && run >= need && upto > static_cast<u64>(s0 + i + 1)) upto = s0 + i + 1;
+    }
+    kept = static_cast<int>(row.block_min(upto));
+  }
+  if (by_min) {
+    if (min_p > 1.f) {
+      kept = 1;
+    } else {
+      const double bound = static_cast<double>(w.max) + log(static_cast<double>(min_p)) * static_cast<double>(t);
+      u64 upto = kept;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i)
+        if (s0 + i < kept && static_cast<double>(logit(sorted[s0 + i])) < bound && upto > static_cast<u64>(s0 + i)) upto = s0 + i;
+      kept = max(1, static_cast<int>(row.block_min(upto)));
+    }
+  }
+  const u64 last_kept = sorted[kept - 1];
+  // in index order again
+  double x[kEach], sum = 0.0, all;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    x[i] = s0 + i < n && sh.list[s0 + i] <= last_kept ? w.template operator()<exact_diff<T>()>(logit(sh.list[s0 + i])) : 0.0;
+    sum += x[i];
+  }
+  double run = row.scan(sum, all);
+  const double target = static_cast<double>(fmaxf(a.u[row_id], 0.f)) * all;
+  // the first that passes the target; past the end the last that has a weight
+  u64 pick = ~0ull;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    run += x[i];
+    if (x[i] > 0.0) {
+      const u64 me = static_cast<u64>(run > target ? s0 + i : 2 * kList - (s0 + i));
+      pick = min(pick, me);
+    }
+  }
+  pick = row.block_min(pick);
+  if (threadIdx.x == 0) {
+    const int at_list = static_cast<int>(pick < kList ? pick : 2 * kList - pick);
+    const u64 entry = sh.list[at_list];
+    const float l = logit(entry);
+    const double z = l == w.max ? 0.0 : (static_cast<double>(l) - static_cast<double>(w.max)) / static_cast<double>(t);
+    a.put(row_id, static_cast<int>(entry & 0xffffffffu), z - log(total), z - log(all), kept);
+  }
+  return true;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 2)
 sample_filter_kernel(SampleArgs a, int cluster, int slice) {
@@ -407,35 +667,36 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
   const float top_p = a.top_p ? a.top_p[row_id] : 1.f, min_p = a.min_p ? a.min_p[row_id] : 0.f;
   const bool by_mass = top_p < 1.f && !greedy;
 
-  // ---- the sum of all weights; whole numbers too where shares of it are asked for
+  // ---- the sum of all weights
   double total;
-  u64 all = 0;
   {
     double s = 0.0;
-    if (by_mass && !(top_k > 0 && top_k < a.v)) {
-      row.each([&](float x, int) {
-        const double y = weight(x);
-        s += y;
-        all += fixed_of(y);
-      });
-      all = row.cluster_sum(all);
-    } else {
-      WeightSum fast;
-      for (int j = row.v0 + row.lane; j < row.v1; j += kWarp) {
-        const Vec<T> v[1] = {row.piece(j)};
-        float most, least;
-        extremes(v, most, least);
-        if (least - m >= w.floor && least > -INFINITY) {
+    WeightSum fast;
+    for (int j = row.v0 + row.lane; j < row.v1; j += kWarp) {
+      const Vec<T> v[1] = {row.piece(j)};
+      float most, least;
+      extremes(v, most, least);
+      if (least - m >= w.floor && least > -INFINITY) {
 #pragma unroll
-          for (int e = 0; e < VE; e += 2) w.template add<kExact>(v[0].pair(e), fast);
-        } else {
+        for (int e = 0; e < VE; e += 2) w.template add<kExact>(v[0].pair(e), fast);
+      } else {
 #pragma unroll
-          for (int e = 0; e < VE; ++e) s += weight(v[0].at(e));
-        }
+        for (int e = 0; e < VE; ++e) s += weight(v[0].at(e));
       }
-      s += fast.value();
     }
+    s += fast.value();
+    const double stretch_sum = warp_sum(s);
+    if (row.lane == 0) sh.stretch[row.warp] = stretch_sum;
     total = row.cluster_sum(s);
+  }
+  const bool by_count = top_k > 0 && top_k < a.v && !greedy, by_min = min_p > 0.f && !greedy;
+  if ((by_count || by_mass || by_min) &&
+      sample_from_candidates(row, a, row_id, w, t, total, top_k, top_p, min_p, reinterpret_cast<u64*>(data)))
+    return;
+  u64 all = 0;
+  if (by_mass && !by_count) {   // whole numbers: shares of it are asked for
+    row.each([&](float x, int) { all += fixed_of(weight(x)); });
+    all = row.cluster_sum(all);
   }
 
   // ---- what is kept: keys above `edge`, and of those equal to it the first `ties` in index order
@@ -546,13 +807,18 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
   // ---- the kept weights by stretches
   double s = 0.0;
   int count = 0;
-  row.each([&](float x, int i) {
-    if (kept(x, i)) {
-      s += weight(x);
-      ++count;
-    }
-  });
-  s = warp_sum(s);
+  if (edge == none) {   // all of them: their sums are there
+    row.each([&](float x, int) { count += x > -INFINITY ? 1 : 0; });
+    s = sh.stretch[row.warp];
+  } else {
+    row.each([&](float x, int i) {
+      if (kept(x, i)) {
+        s += weight(x);
+        ++count;
+      }
+    });
+    s = warp_sum(s);
+  }
   count = __reduce_add_sync(0xffffffffu, count);
   __syncthreads();   // warp_count has been read
   u64* sums = sh.part[row.flip ^= 1];
@@ -621,7 +887,9 @@ int filter_impl(const SampleArgs& a, cudaStream_t stream) {
   int cluster = 1;
   while (cluster < kMaxCluster && static_cast<long long>(a.v) * static_cast<int>(sizeof(T)) > 49152ll * cluster) cluster *= 2;
   const int slice = ((a.v + cluster - 1) / cluster + 7) / 8 * 8;
-  const size_t smem = (sizeof(Shared) + 15) / 16 * 16 + (static_cast<size_t>(slice) * sizeof(T) + 47) / 16 * 16;
+  size_t room = (static_cast<size_t>(slice) * sizeof(T) + 47) / 16 * 16;
+  if (room < kList * sizeof(u64)) room = kList * sizeof(u64);   // the sorted candidates take the slice's place
+  const size_t smem = (sizeof(Shared) + 15) / 16 * 16 + room;
   if (cudaFuncSetAttribute(sample_filter_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) !=
       cudaSuccess) {
     cudaGetLastError();
