@@ -75,6 +75,15 @@ __device__ __forceinline__ u32 load_remote(const u32* here, u32 rank) {
   return v;
 }
 
+// Sum of a word over the cluster, all loads on their way at once.
+__device__ __forceinline__ void add_remote(const u32* here, int cluster, u64& sum) {
+  u32 v[kMaxCluster];
+#pragma unroll
+  for (int r = 0; r < kMaxCluster; ++r) v[r] = r < cluster ? load_remote(here, r) : 0;
+#pragma unroll
+  for (int r = 0; r < kMaxCluster; ++r) sum += v[r];
+}
+
 __device__ __forceinline__ u64 warp_sum64(u64 v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -244,12 +253,10 @@ struct Row {
         got[i] = 0;
         const int at = static_cast<int>(threadIdx.x) * per + i;
         if (i < per && at < mine) {
-          u32 words_hi = 0;
-          for (int r = 0; r < cluster; ++r) {
-            got[i] += load_remote(&sh.lo[top - 1 - at], r);
-            if (MASS) words_hi += load_remote(&sh.hi[top - 1 - at], r);
-          }
-          got[i] += static_cast<u64>(words_hi) << 32;
+          u64 words_hi = 0;
+          add_remote(&sh.lo[top - 1 - at], cluster, got[i]);
+          if (MASS) add_remote(&sh.hi[top - 1 - at], cluster, words_hi);
+          got[i] += words_hi << 32;
           sum += got[i];
         }
       }
@@ -384,17 +391,24 @@ __device__ __forceinline__ int find_in_stretch(const Row<T>& row, double want, F
   return top;
 }
 
+// The share that top-p asks for; 2^-48 less, so that one that is reached exactly is reached.
+__device__ __forceinline__ u64 share_of(double all, float top_p) {
+  const double share = static_cast<double>(fmaxf(top_p, 0.f)) * all * (1.0 - 0x1p-48);
+  return share > 1.0 ? static_cast<u64>(ceil(share)) : 1;
+}
+
 // Rows whose kept tokens are among a few candidates.  The logits are counted by their distance to the largest, in steps of a
 // 64th (top-p: a 128th) of the temperature; the first step that has, with all above it, k tokens, or more than the share p of
 // the mass if every token of a step had the least weight of the step, bounds what top-k or top-p can keep (min-p's bound is known
-// beforehand).  If that leaves at most kList tokens, the first block gets them in index order, sorts a copy, cuts it and samples,
-// and the others are done.  One pass over the logits and three cluster barriers less than a level of the histograms above takes;
+// beforehand).  If that leaves at most kList tokens, the first block gets them in index order, finds the borders among them and
+// samples, and the others are done.  One pass over the logits and three cluster barriers less than a level of the histograms above takes;
 // false: the row is not of this kind (the same for the whole cluster).
 template <typename T, class W>
 __device__ __forceinline__ bool sample_from_candidates(Row<T>& row, const SampleArgs& a, int row_id, const W& w, float t, double total,
-                                                       int top_k, float top_p, float min_p, u64* sorted) {
+                                                       int top_k, float top_p, float min_p, u64* bins) {
   constexpr int VE = per_vec<T>();
   Shared& sh = row.sh;
+  u64* among = bins + kBins;
   const bool by_count = top_k > 0 && top_k < a.v, by_mass = top_p < 1.f, by_min = min_p > 0.f;
   const bool mass_alone = by_mass && !by_count;
   const float steps = mass_alone ? 128.f : 64.f, scale = steps / t;
@@ -419,7 +433,9 @@ __device__ __forceinline__ bool sample_from_candidates(Row<T>& row, const Sample
     got[i] = 0;
     if (i < per && first + i < mine) {
       const int b = row.rank * mine + first + i;
-      for (int r = 0; r < row.cluster; ++r) got[i] += load_remote(&sh.lo[b], r);
+      u64 all = 0;
+      add_remote(&sh.lo[b], row.cluster, all);
+      got[i] = static_cast<u32>(all);
       count += got[i];
       if (mass_alone) mass += static_cast<double>(got[i]) * static_cast<double>(expf(static_cast<float>(b + 1) * (-1.f / steps)));
     }
@@ -511,68 +527,111 @@ __device__ __forceinline__ bool sample_from_candidates(Row<T>& row, const Sample
   if (row.rank != 0) return true;
 
   // ---- the first block alone from here on
-  int size = kWarp;
-  while (size < n) size *= 2;
-  for (int i = threadIdx.x; i < size; i += kThreads) sorted[i] = i < n ? sh.list[i] : ~0ull;
-  for (int k = 2; k <= size; k *= 2) {          // bitonic sort
-    for (int j = k / 2; j > 0; j /= 2) {
+  auto logit = [](u64 entry) { return of_key(~static_cast<u32>(entry >> 32)); };
+  constexpr int kEach = kList / kThreads;
+  const int s0 = static_cast<int>(threadIdx.x) * kEach;   // this thread's of the list
+  u64 last = ~0ull;                                       // the last entry, in rank order, that is kept
+  if (by_count || by_mass) {
+    // top-k's border, then, of the mass above it, top-p's: sums by step, the step that they pass `need` in, and its entries one
+    // against another
+    u64 need = static_cast<u64>(top_k);
+    bool weigh = !by_count;
+    if (weigh) need = share_of(total * kFixed, top_p);
+    for (;;) {
       __syncthreads();
-      for (int i = threadIdx.x; i < size / 2; i += kThreads) {
-        const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
-        const u64 x = sorted[lo], y = sorted[hi];
-        if ((x > y) == ((lo & k) == 0)) {
-          sorted[lo] = y;
-          sorted[hi] = x;
+      for (int i = threadIdx.x; i < kBins; i += kThreads) bins[i] = 0;
+      if (threadIdx.x == 0) sh.warp_count[0] = 0;
+      __syncthreads();
+      u64 x[kEach], all = 0;
+      int bin[kEach];
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        x[i] = 0;
+        bin[i] = -1;
+        if (s0 + i < n && sh.list[s0 + i] <= last) {
+          const float l = logit(sh.list[s0 + i]);
+          x[i] = weigh ? fixed_of(w.template operator()<exact_diff<T>()>(l)) : 1;
+          bin[i] = static_cast<int>(distance(l));
+          atomicAdd(&bins[bin[i]], x[i]);   // whole numbers: in any order
         }
       }
-    }
-  }
-  __syncthreads();
-  auto logit = [](u64 entry) { return of_key(~static_cast<u32>(entry >> 32)); };
-  // how many of the sorted are kept; a thread takes neighbours
-  constexpr int kEach = kList / kThreads;
-  const int s0 = static_cast<int>(threadIdx.x) * kEach;
-  int kept = by_count ? min(n, top_k) : n;
-  if (by_mass) {
-    u64 x[kEach], sum = 0, all = 0;
+      __syncthreads();
+      u64 own[kMost], sum = 0;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      x[i] = s0 + i < kept ? fixed_of(w.template operator()<exact_diff<T>()>(logit(sorted[s0 + i]))) : 0;
-      sum += x[i];
-    }
-    u64 run = row.scan(sum, all);
-    const double of = by_count ? static_cast<double>(all) : total * kFixed;
-    const double share = static_cast<double>(fmaxf(top_p, 0.f)) * of * (1.0 - 0x1p-48);
-    const u64 need = share > 1.0 ? static_cast<u64>(ceil(share)) : 1;
-    u64 upto = kept;   // tokens with all of `need`
+      for (int i = 0; i < kMost; ++i) {
+        own[i] = bins[static_cast<int>(threadIdx.x) * kMost + i];
+        sum += own[i];
+      }
+      u64 run = row.scan(sum, all);
+      if (weigh && by_count) need = share_of(static_cast<double>(all), top_p);
+      u64 found = ~0ull;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      run += x[i];
-      if (s0 + i < kept && run >= need && upto > static_cast<u64>(s0 + i + 1)) upto = s0 + i + 1;
+      for (int i = 0; i < kMost; ++i) {
+        run += own[i];
+        if (run >= need && found == ~0ull) found = static_cast<u64>(static_cast<int>(threadIdx.x) * kMost + i);
+      }
+      found = row.block_min(found);
+      if (found != ~0ull) {   // else fewer than k tokens, or rounding: all of them
+        const int step = static_cast<int>(found);
+        if (static_cast<int>(threadIdx.x) == step / kMost) {   // the sum over the steps before it
+          u64 before = run;
+#pragma unroll
+          for (int i = kMost - 1; i >= 0; --i)
+            if (i >= step % kMost) before -= own[i];
+          sh.slot[kSlots - 1][0] = before;
+        }
+        // the step's entries and what they count for into one place (the sums by step have been read)
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          if (bin[i] == step) {
+            const int to = atomicAdd(&sh.warp_count[0], 1);   // in any order: what follows compares all with all
+            among[to] = sh.list[s0 + i];
+            bins[to] = x[i];
+          }
+        }
+        __syncthreads();
+        const int m = sh.warp_count[0];
+        const u64 before = sh.slot[kSlots - 1][0];
+        u64 border = ~0ull;
+        for (int i = threadIdx.x; i < m; i += kThreads) {
+          const u64 me = among[i];
+          u64 upto = before;   // with all entries of the step up to and with this one
+          for (int j = 0; j < m; ++j) upto += among[j] <= me ? bins[j] : 0;
+          if (upto >= need) border = min(border, me);
+        }
+        last = min(last, row.block_min(border));
+      }
+      if (weigh || !by_mass) break;
+      weigh = true;
     }
-    kept = static_cast<int>(row.block_min(upto));
   }
   if (by_min) {
-    if (min_p > 1.f) {
-      kept = 1;
-    } else {
-      const double bound = static_cast<double>(w.max) + log(static_cast<double>(min_p)) * static_cast<double>(t);
-      u64 upto = kept;
+    const double bound = static_cast<double>(w.max) + log(static_cast<double>(min_p)) * static_cast<double>(t);
+    u64 top = ~0ull, low = 0;
 #pragma unroll
-      for (int i = 0; i < kEach; ++i)
-        if (s0 + i < kept && static_cast<double>(logit(sorted[s0 + i])) < bound && upto > static_cast<u64>(s0 + i)) upto = s0 + i;
-      kept = max(1, static_cast<int>(row.block_min(upto)));
+    for (int i = 0; i < kEach; ++i) {
+      if (s0 + i >= n) continue;
+      const u64 entry = sh.list[s0 + i];
+      top = min(top, entry);
+      if (static_cast<double>(logit(entry)) >= bound) low = max(low, entry);
     }
+    top = row.block_min(top);              // the first rank is kept whatever min-p is
+    low = ~row.block_min(~low);
+    last = min(last, min_p > 1.f ? top : max(top, low));
   }
-  const u64 last_kept = sorted[kept - 1];
-  // in index order again
+  // the weights of what is kept, in index order
   double x[kEach], sum = 0.0, all;
+  u32 kept = 0;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
-    x[i] = s0 + i < n && sh.list[s0 + i] <= last_kept ? w.template operator()<exact_diff<T>()>(logit(sh.list[s0 + i])) : 0.0;
+    const bool in = s0 + i < n && sh.list[s0 + i] <= last;
+    x[i] = in ? w.template operator()<exact_diff<T>()>(logit(sh.list[s0 + i])) : 0.0;
     sum += x[i];
+    kept += in ? 1 : 0;
   }
   double run = row.scan(sum, all);
+  u32 all_kept;
+  row.scan(kept, all_kept);
   const double target = static_cast<double>(fmaxf(a.u[row_id], 0.f)) * all;
   // the first that passes the target; past the end the last that has a weight
   u64 pick = ~0ull;
@@ -590,7 +649,7 @@ __device__ __forceinline__ bool sample_from_candidates(Row<T>& row, const Sample
     const u64 entry = sh.list[at_list];
     const float l = logit(entry);
     const double z = l == w.max ? 0.0 : (static_cast<double>(l) - static_cast<double>(w.max)) / static_cast<double>(t);
-    a.put(row_id, static_cast<int>(entry & 0xffffffffu), z - log(total), z - log(all), kept);
+    a.put(row_id, static_cast<int>(entry & 0xffffffffu), z - log(total), z - log(all), static_cast<int>(all_kept));
   }
   return true;
 }
@@ -671,20 +730,24 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
   double total;
   {
     double s = 0.0;
-    WeightSum fast;
-    for (int j = row.v0 + row.lane; j < row.v1; j += kWarp) {
-      const Vec<T> v[1] = {row.piece(j)};
-      float most, least;
-      extremes(v, most, least);
-      if (least - m >= w.floor && least > -INFINITY) {
+    if (w.floor > -1e37f && fabsf(m) < 1e6f * -w.floor) {   // the limit below is a number well under m
+      // What is -inf or far below the largest counts as its 2^-100th here, which no sum that holds a 1 shows.
+      const float least = m + w.floor;
+      WeightSum even, odd;
+      for (int j0 = row.v0 + row.lane; j0 < row.v1; j0 += 2 * kWarp) {
+        const int j1 = j0 + kWarp;
+        const Vec<T> x = row.piece(j0), y = row.piece(min(j1, row.v1 - 1));
 #pragma unroll
-        for (int e = 0; e < VE; e += 2) w.template add<kExact>(v[0].pair(e), fast);
-      } else {
+        for (int e = 0; e < VE; e += 2) w.template add<kExact>(f2(fmaxf(x.at(e), least), fmaxf(x.at(e + 1), least)), even);
+        if (j1 < row.v1) {
 #pragma unroll
-        for (int e = 0; e < VE; ++e) s += weight(v[0].at(e));
+          for (int e = 0; e < VE; e += 2) w.template add<kExact>(f2(fmaxf(y.at(e), least), fmaxf(y.at(e + 1), least)), odd);
+        }
       }
+      s = even.value() + odd.value();
+    } else {
+      row.each([&](float x, int) { s += weight(x); });
     }
-    s += fast.value();
     const double stretch_sum = warp_sum(s);
     if (row.lane == 0) sh.stretch[row.warp] = stretch_sum;
     total = row.cluster_sum(s);
@@ -693,16 +756,11 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
   if ((by_count || by_mass || by_min) &&
       sample_from_candidates(row, a, row_id, w, t, total, top_k, top_p, min_p, reinterpret_cast<u64*>(data)))
     return;
-  u64 all = 0;
-  if (by_mass && !by_count) {   // whole numbers: shares of it are asked for
-    row.each([&](float x, int) { all += fixed_of(weight(x)); });
-    all = row.cluster_sum(all);
-  }
-
   // ---- what is kept: keys above `edge`, and of those equal to it the first `ties` in index order
   const u32 none = tkey<T>(-INFINITY), best = tkey<T>(m);
   u32 edge = none;
   int ties = 0;
+  double of = total * kFixed;   // the mass that top-p has a share of
   if (greedy) {
     edge = best;
     ties = 1;
@@ -714,20 +772,19 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
         edge = k;
         ties = top_k - static_cast<int>(above);
       }
-      if (by_mass) {   // the mass that top-p has a share of
+      if (by_mass) {
         const u32 e = edge;
-        all = 0;
+        u64 all = 0;
         row.each([&](float x, int) {
           if (tkey<T>(x) > e) all += fixed_of(weight(x));
         });
         all = row.cluster_sum(all);
         if (edge > none) all += static_cast<u64>(ties) * fixed_of(weight(of_tkey<T>(edge)));
+        of = static_cast<double>(all);
       }
     }
     if (by_mass) {
-      // 2^-48 less: a share that is reached exactly is reached
-      const double share = static_cast<double>(fmaxf(top_p, 0.f)) * static_cast<double>(all) * (1.0 - 0x1p-48);
-      const u64 need = share > 1.0 ? static_cast<u64>(ceil(share)) : 1;
+      const u64 need = share_of(of, top_p);
       u32 lo = edge;
       if (edge == none) {   // lighter than (1 - p) / V of all: even together they are not the part that is left out
         const double cut = (1.0 - static_cast<double>(fmaxf(top_p, 0.f))) * total / a.v * 0.999;
@@ -810,6 +867,11 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
   if (edge == none) {   // all of them: their sums are there
     row.each([&](float x, int) { count += x > -INFINITY ? 1 : 0; });
     s = sh.stretch[row.warp];
+    if (s < 0x1p-60) {   // perhaps nothing but what counts as 2^-100 there and as 0 here
+      s = 0.0;
+      row.each([&](float x, int) { s += weight(x); });
+      s = warp_sum(s);
+    }
   } else {
     row.each([&](float x, int i) {
       if (kept(x, i)) {
@@ -883,12 +945,17 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
 
 template <typename T>
 int filter_impl(const SampleArgs& a, cudaStream_t stream) {
-  // Blocks per row: as many as leave each at most 48 KB of logits (two blocks and their histograms share an SM then).
+  // Blocks per row: two share an SM, each with at most 76 KB of logits (eight blocks of up to kMaxSlice where that does not do).
+  // More than that, up to eight of at least 8 KB, while all rows still run at once.
   int cluster = 1;
-  while (cluster < kMaxCluster && static_cast<long long>(a.v) * static_cast<int>(sizeof(T)) > 49152ll * cluster) cluster *= 2;
+  const long long bytes = static_cast<long long>(a.v) * static_cast<int>(sizeof(T));
+  while (cluster < kMaxCluster && bytes > 77824ll * cluster) cluster *= 2;
+  while (cluster < kMaxCluster && bytes > 16384ll * cluster && 2ll * cluster * a.n <= 2ll * sm_count()) cluster *= 2;
   const int slice = ((a.v + cluster - 1) / cluster + 7) / 8 * 8;
   size_t room = (static_cast<size_t>(slice) * sizeof(T) + 47) / 16 * 16;
-  if (room < kList * sizeof(u64)) room = kList * sizeof(u64);   // the sorted candidates take the slice's place
+  // the first block's sums by step, and one step's candidates, take the slice's place
+  constexpr size_t kAlone = (kBins + kList) * sizeof(u64);
+  if (room < kAlone) room = kAlone;
   const size_t smem = (sizeof(Shared) + 15) / 16 * 16 + room;
   if (cudaFuncSetAttribute(sample_filter_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) !=
       cudaSuccess) {

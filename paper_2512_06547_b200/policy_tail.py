@@ -1,4 +1,5 @@
-"""The last feed-forward block of the policy, the final norm, the LM head and the A-3PO loss as one training pass.
+"""The last feed-forward block of the policy, the final norm, the LM head and the A-3PO loss as one training pass, the same
+layers with the sampling of the next token as one rollout pass, and the update of their weights.
 
 For trainers that own the tail of the network: everything from the residual stream `r0` [N, H] that enters the last
 block's feed-forward half to the loss, and back to grad_r0, through the library's calls:
@@ -13,12 +14,21 @@ Rows with mask 0 (padding) take no part in any of them and get zero gradients.  
 largest batch and reused by every pass; a pass launches on the current stream, never synchronises and can be captured
 into a CUDA graph (after one uncaptured pass).  The random numbers of dropout come from the device words
 rng = {seed, offset}: a trainer advances the offset between passes (in place, so a captured graph follows).
+
+PolicySampler runs the forward half on the rows whose next token is wanted, and draws it:
+
+    logits       = hidden W^T                                        a3po_linear_fwd (fp32)
+    token, logp  = temperature, top-k, top-p, min-p; random numbers  a3po_sample
+
+where logp is what the loss takes as behav_logp.  PolicyTail.optimizer makes an AdamW over the pass's parameters, and
+PolicyTail.update takes its step with the gradients that the last pass left.
 """
 from __future__ import annotations
 
 import torch
 
 from . import binding as b
+from .optimizer import AdamW
 
 
 class PolicyTail:
@@ -30,7 +40,7 @@ class PolicyTail:
 
     def __init__(self, n, h, f, v, dtype=torch.bfloat16, *, kind=b.A3PO_NORM_RMS, activation=b.A3PO_ACT_SILU, dropout_p=0.0,
                  eps=1e-6, beta=None, device="cuda"):
-        self.n, self.h, self.f, self.v = n, h, f, v
+        self.n, self.h, self.f, self.v, self.dtype = n, h, f, v, dtype
         self.kind, self.activation, self.p, self.eps = kind, activation, float(dropout_p), eps
         layer = kind == b.A3PO_NORM_LAYER
         dt = b.A3PO_F32 if dtype == torch.float32 else b.A3PO_BF16
@@ -83,3 +93,52 @@ class PolicyTail:
                                 grad_beta=g.get("beta_in"), accumulate_grad_w=accumulate_grads, **norm)
         return {"loss": self.loss, "stats": self.stats, "logp": self.logp, "status": self.status,
                 "grad_r0": self.grad_r0, "grads": g}
+
+    def optimizer(self, params, *, weight_decay=0.01, **kw):
+        """AdamW over `params` (in the order of self.grads), with fp32 masters of bf16 weights; norms do not decay.  kw as for
+        AdamW."""
+        weights = [params[k] for k in self.grads]
+        if self.dtype != torch.float32:
+            kw.setdefault("masters", True)
+        return AdamW(weights, weight_decay=[float(weight_decay) if w.dim() > 1 else 0.0 for w in weights], **kw)
+
+    def update(self, optimizer):
+        """The optimizer's step with the gradients that the last pass left (fp32), on the current stream."""
+        optimizer.step(list(self.grads.values()))
+
+
+class PolicySampler:
+    """Buffers and calls for drawing the next token of n rows of the residual stream at once (single tokens while serving,
+    batches of rollouts).  params as PolicyTail takes them.  A pass launches on the current stream, never synchronises and can
+    be captured into a CUDA graph (after one uncaptured pass)."""
+
+    def __init__(self, n, h, f, v, dtype=torch.bfloat16, *, kind=b.A3PO_NORM_RMS, activation=b.A3PO_ACT_SILU, eps=1e-6,
+                 device="cuda"):
+        self.kind, self.activation, self.eps = kind, activation, eps
+        dt = b.A3PO_F32 if dtype == torch.float32 else b.A3PO_BF16
+        rows = lambda: torch.empty((n, h), dtype=dtype, device=device)
+        per_row = lambda dtype: torch.empty(n, dtype=dtype, device=device)
+        self.a, self.y, self.r1, self.hidden = rows(), rows(), rows(), rows()
+        self.logits = torch.empty((n, v), dtype=torch.float32, device=device)
+        self.token, self.n_kept = per_row(torch.int32), per_row(torch.int32)
+        self.logp, self.kept_logp = per_row(torch.float32), per_row(torch.float32)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        self.ws = b.new_workspace(max(b.a3po_gated_ffn_workspace_bytes(n, h, f, dt, True, False),
+                                      b.a3po_linear_workspace_bytes(n, h, v, dt, has_row_mask=True),
+                                      b.a3po_sample_workspace_bytes(n, v)), device)
+
+    def __call__(self, r0, params, u, *, temperature=None, top_k=None, top_p=None, min_p=None, row_mask=None):
+        """r0 [n, H], u fp32 [n] in [0, 1); the rest as a3po_sample takes it (rows with row_mask 0 have finished: token -1).
+        Returns a dict of this object's own buffers: token, logp (of the whole softmax at the row's temperature), kept_logp
+        (among the tokens that the filters kept), n_kept, logits, hidden and status."""
+        norm = dict(kind=self.kind, eps=self.eps, row_mask=row_mask)
+        b.a3po_norm_fwd(r0, params["gamma_in"], self.a, beta=params.get("beta_in"), **norm)
+        b.a3po_gated_ffn_fwd(self.a, params["w_gate_up"], params["w_down"], self.y, self.ws, row_mask=row_mask,
+                             activation=self.activation, status=self.status)
+        b.a3po_dropout_norm_fwd(self.y, r0, 0.0, None, params["gamma_out"], self.r1, self.hidden, beta=params.get("beta_out"),
+                                **norm)
+        b.a3po_linear_fwd(self.hidden, params["w"], self.logits, self.ws, row_mask=row_mask, status=self.status)
+        b.a3po_sample(self.logits, u, self.token, self.ws, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p,
+                      row_mask=row_mask, logp=self.logp, kept_logp=self.kept_logp, n_kept=self.n_kept)
+        return {"token": self.token, "logp": self.logp, "kept_logp": self.kept_logp, "n_kept": self.n_kept,
+                "logits": self.logits, "hidden": self.hidden, "status": self.status}
