@@ -1,19 +1,20 @@
 // Sampling from rows with filters (top-k, top-p, min-p).  A row is spread over the shared memory of a cluster of up to
 // eight blocks, so that HBM is read once and all that follows runs on the copy:
 //
-//   largest logit, sum of all weights
-//   border of top-k: the key (the logit's bits, ordered) of the k-th token, by histograms of the key's leading bits, 11 at a
-//     time: at most three (bf16: two), each added up over the cluster and searched from the top
-//   border of top-p: the same with the weights of a histogram's keys instead of their number, as whole numbers of 2^-43, so
-//     that sums do not depend on the order of the atomics.  Tokens lighter than (1 - p) / V of all weight cannot be at the
-//     border and are not counted
-//   border of min-p: a logit
-//   ties at the border: kept up to an index, the c-th of them
-//   sums of the kept weights by stretches of the row, and the token in the stretch that the random number falls into
+//   largest logit and sum of all weights: warps of neighbouring logits by themselves, then blocks, then the cluster
+//   how many logits lie at which distance from the largest, in 2,048 steps, added up in the first block.  The counts bound what
+//     top-k or top-p can keep: the first step that has, with all above it, k tokens, or the share p of the mass even if every
+//     token of a step has the least weight of the step (min-p's bound is known beforehand)
+//   few candidates (up to 2,048): the first block gets them in index order and finishes alone
+//   more: the exact mass of the steps in which top-p's border may lie, the tokens of the one step that holds the border, which the
+//     first block puts in order, and another pass over the kept ones
+//   rows whose borders the steps do not bound (more tokens on one step than the block holds, a border far from the largest
+//     logit): the border's key (the logit's bits, ordered) by histograms of the key's leading bits, 11 at a time
 //
-// A block's warps own stretches of neighbouring logits, and every sum is taken in a fixed order: results are
-// bit-identical from run to run.
-// Bound: latency (histograms and cluster barriers, about 2 us a level); several clusters share an SM.
+// Masses that are compared are whole numbers of 2^-43, so that they do not depend on the order of atomics, and all other sums are
+// taken in a fixed order: results are bit-identical from run to run.
+// Bound: latency.  A row is a chain of passes of a microsecond or two and four to nine cluster barriers of half a one; for many rows
+// the instructions of the passes (40 to 70 a logit).
 
 #include "sample.cuh"
 #include "sm100_ptx.cuh"
@@ -24,7 +25,7 @@ namespace {
 constexpr int kThreads = 512, kWarps = kThreads / kWarp, kMaxCluster = 8;
 constexpr int kBinBits = 11, kBins = 1 << kBinBits;
 constexpr int kMaxSlice = 196608;        // bytes of a row in one block
-constexpr int kSlots = 40;
+constexpr int kSlots = 48;
 constexpr int kList = kBins;             // candidates that one block finishes alone
 constexpr double kFixed = 8796093022208.0;   // 2^43: a weight as a whole number
 
@@ -54,13 +55,15 @@ struct Shared {
   SharedTable<16> table;
   u64 slot[kSlots][kMaxCluster];   // what the blocks of the cluster tell one another, each slot once
   u64 part[2][kWarps];
-  double stretch[kWarps];          // sums of the warps' weights
+  double stretch[kWarps];          // sums of the warps' weights, relative to the largest of each
+  float stretch_max[kWarps];
+  double total;                    // of the row, relative to its largest logit
   int warp_count[kWarps];
   union {
-    struct {
+    struct __align__(16) {
       u32 lo[kBins], hi[kBins];    // histograms
     };
-    u64 list[kList];               // the first block's: candidates in index order (ordered bits, index)
+    u64 list[kList];               // the first block's: candidates (ordered bits, index)
   };
 };
 
@@ -73,6 +76,27 @@ __device__ __forceinline__ u32 load_remote(const u32* here, u32 rank) {
   u32 v;
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
   return v;
+}
+
+__device__ __forceinline__ u64 load_remote(const u64* here, u32 rank) {
+  const u32 at = ptx::map_to_cta(static_cast<u32>(__cvta_generic_to_shared(here)), rank);
+  u64 v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint4 load_remote4(const u32* here, u32 rank) {
+  const u32 at = ptx::map_to_cta(static_cast<u32>(__cvta_generic_to_shared(here)), rank);
+  uint4 v;
+  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ u32 take_from_remote(u32* here, u32 rank, u32 v) {   // the value before
+  const u32 at = ptx::map_to_cta(static_cast<u32>(__cvta_generic_to_shared(here)), rank);
+  u32 old;
+  asm volatile("atom.relaxed.cluster.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(at), "r"(v) : "memory");
+  return old;
 }
 
 // Sum of a word over the cluster, all loads on their way at once.
@@ -107,6 +131,11 @@ struct Row {
     u64* s = sh.slot[slot++];
     if (threadIdx.x < static_cast<unsigned>(cluster)) store_remote(s + rank, threadIdx.x, v);
     return s;
+  }
+  // The next slot, for a thread that tells everyone by itself (say); read at [0].
+  __device__ __forceinline__ u64* next_slot() { return sh.slot[slot++]; }
+  __device__ __forceinline__ void say(u64* s, u64 v) const {
+    for (int r = 0; r < cluster; ++r) store_remote(s, r, v);
   }
   __device__ __forceinline__ void sync() { ptx::cluster_sync_all(); }
   // Sum over the block's threads, in warp order, in all threads.
@@ -144,20 +173,6 @@ struct Row {
     for (int r = 0; r < cluster; ++r) t += __longlong_as_double(static_cast<long long>(s[r]));
     return t;
   }
-  __device__ __forceinline__ u64 cluster_max(u32 v) {   // of 32-bit keys
-    v = __reduce_max_sync(0xffffffffu, v);
-    u64* p = sh.part[flip ^= 1];
-    if (lane == 0) p[warp] = v;
-    __syncthreads();
-    u64 t = 0;
-#pragma unroll
-    for (int i = 0; i < kWarps; ++i) t = max(t, p[i]);
-    const u64* s = tell(t);
-    sync();
-    for (int r = 0; r < cluster; ++r) t = max(t, s[r]);
-    return t;
-  }
-
   __device__ __forceinline__ u64 block_min(u64 v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v = min(v, __shfl_xor_sync(0xffffffffu, v, o));
@@ -205,6 +220,33 @@ struct Row {
     Vec<T> v;
     v.w[0] = u.x; v.w[1] = u.y; v.w[2] = u.z; v.w[3] = u.w;
     return v;
+  }
+  // Sum of the weights of the logits that `in` takes: pairs, of which one that is not taken (or far below the largest) counts as
+  // its 2^-100th; a sum below 2^-60 is taken again one by one (`in` is asked twice).
+  template <class W, class F>
+  __device__ __forceinline__ double weigh(const W& w, F in) const {
+    double s = 0.0;
+    if (w.floor > -1e37f && fabsf(w.max) < 1e6f * -w.floor) {   // the limit below is a number well under the largest
+      const float least = w.max + w.floor;
+      WeightSum even, odd;
+      for (int j = v0 + lane; j < v1; j += kWarp) {
+        const Vec<T> v = piece(j);
+#pragma unroll
+        for (int e = 0; e < per_vec<T>(); e += 2) {
+          const int i = base + j * per_vec<T>() + e;
+          const float x = v.at(e), y = v.at(e + 1);
+          w.template add<exact_diff<T>()>(f2(in(x, i) ? fmaxf(x, least) : least, in(y, i + 1) ? fmaxf(y, least) : least),
+                                          e % 4 ? odd : even);
+        }
+      }
+      s = warp_sum(even.value() + odd.value());
+      if (s >= 0x1p-60) return s;
+      s = 0.0;
+    }
+    each([&](float x, int i) {
+      if (in(x, i)) s += w.template operator()<exact_diff<T>()>(x);
+    });
+    return warp_sum(s);
   }
   template <class F>
   __device__ __forceinline__ void each(F f) const {
@@ -397,261 +439,432 @@ __device__ __forceinline__ u64 share_of(double all, float top_p) {
   return share > 1.0 ? static_cast<u64>(ceil(share)) : 1;
 }
 
-// Rows whose kept tokens are among a few candidates.  The logits are counted by their distance to the largest, in steps of a
-// 64th (top-p: a 128th) of the temperature; the first step that has, with all above it, k tokens, or more than the share p of
-// the mass if every token of a step had the least weight of the step, bounds what top-k or top-p can keep (min-p's bound is known
-// beforehand).  If that leaves at most kList tokens, the first block gets them in index order, finds the borders among them and
-// samples, and the others are done.  One pass over the logits and three cluster barriers less than a level of the histograms above takes;
-// false: the row is not of this kind (the same for the whole cluster).
+// A token as a number: larger logits first, then lower indexes.
+__device__ __forceinline__ u64 entry_of(float l, int index) { return static_cast<u64>(~key_of(l)) << 32 | static_cast<u32>(index); }
+__device__ __forceinline__ float logit_of(u64 entry) { return of_key(~static_cast<u32>(entry >> 32)); }
+
+// What one row asks for.
+struct Ask {
+  int top_k;
+  float top_p, min_p;
+  bool by_count, by_mass, by_min;
+  double min_bound;   // the smallest logit that min-p keeps
+};
+
+// Steps of distance to the largest logit: a 64th of the temperature each, a 128th for top-p alone (whose bound is the sharper the
+// finer they are; 99 % of the mass is out of its reach).
+struct Steps {
+  float max, scale;
+  __device__ __forceinline__ float distance(float l) const { return __fmul_rn(__fsub_rn(max, l), scale); }
+};
+
+// Among m entries and what they count for: the last one, in rank order, that is kept, when the entries before them count `before`
+// and all up to it have to count `need`; ~0: all of them do not.
+template <class R>
+__device__ __forceinline__ u64 border_among(R& row, const u64* entries, const u64* amounts, int m, u64 before, u64 need) {
+  u64 border = ~0ull;
+  for (int i = threadIdx.x; i < m; i += kThreads) {
+    const u64 me = entries[i];
+    u64 upto = before;
+#pragma unroll 4
+    for (int j = 0; j < m; ++j) upto += entries[j] <= me ? amounts[j] : 0;
+    if (upto >= need) border = min(border, me);
+  }
+  return row.block_min(border);
+}
+
+// The first block with n candidates in index order in `list`; the rest of the cluster is done.
+// scratch: two arrays of kList words besides.
 template <typename T, class W>
-__device__ __forceinline__ bool sample_from_candidates(Row<T>& row, const SampleArgs& a, int row_id, const W& w, float t, double total,
-                                                       int top_k, float top_p, float min_p, u64* bins) {
-  constexpr int VE = per_vec<T>();
+__device__ __forceinline__ void finish_alone(Row<T>& row, const SampleArgs& a, int row_id, const W& w, const Steps& steps, float t,
+                                             double total, const Ask& ask, const u64* list, int n, u64* bins, u64* among) {
   Shared& sh = row.sh;
-  u64* among = bins + kBins;
-  const bool by_count = top_k > 0 && top_k < a.v, by_mass = top_p < 1.f, by_min = min_p > 0.f;
-  const bool mass_alone = by_mass && !by_count;
-  const float steps = mass_alone ? 128.f : 64.f, scale = steps / t;
-  if (w.at_inf || !(scale < 1e30f)) return false;
-  // ---- counts
-  for (int i = threadIdx.x; i < kBins; i += kThreads) sh.lo[i] = 0;
-  __syncthreads();
-  auto distance = [&](float l) { return __fmul_rn(__fsub_rn(w.max, l), scale); };
-  row.each([&](float l, int) {
-    const float x = distance(l);
-    if (x < static_cast<float>(kBins)) atomicAdd(&sh.lo[static_cast<int>(x)], 1u);   // false for NaN
-  });
-  row.sync();
-  const int mine = kBins / row.cluster, per = (mine + kThreads - 1) / kThreads;
-  const int first = static_cast<int>(threadIdx.x) * per;   // of this block's bins
-  constexpr int kMost = kBins / kThreads;
-  u32 got[kMost];
-  u32 count = 0;
-  double mass = 0.0;
-#pragma unroll
-  for (int i = 0; i < kMost; ++i) {
-    got[i] = 0;
-    if (i < per && first + i < mine) {
-      const int b = row.rank * mine + first + i;
-      u64 all = 0;
-      add_remote(&sh.lo[b], row.cluster, all);
-      got[i] = static_cast<u32>(all);
-      count += got[i];
-      if (mass_alone) mass += static_cast<double>(got[i]) * static_cast<double>(expf(static_cast<float>(b + 1) * (-1.f / steps)));
-    }
-  }
-  u32 block_count;
-  double block_mass = 0.0;
-  u32 cum = row.scan(count, block_count);
-  double cum_mass = mass_alone ? row.scan(mass, block_mass) : 0.0;
-  const u64* counts = row.tell(block_count);
-  const u64* masses = row.tell(static_cast<u64>(__double_as_longlong(block_mass)));
-  row.sync();
-  for (int r = 0; r < row.rank; ++r) {
-    cum += static_cast<u32>(counts[r]);
-    cum_mass += __longlong_as_double(static_cast<long long>(masses[r]));
-  }
-  const double enough = static_cast<double>(fmaxf(top_p, 0.f)) * total * (1.0 + 1e-5);   // expf and the distance are not exact
-  int min_bin = INT_MAX;   // the first bin that lies below what min-p keeps
-  if (by_min && !by_mass) {
-    const float at = min_p >= 1.f ? 0.f : -logf(min_p) * steps;
-    if (at < static_cast<float>(kBins - 3)) min_bin = static_cast<int>(at) + 2;
-  }
-  u64 best = ~0ull;
-#pragma unroll
-  for (int i = 0; i < kMost; ++i) {
-    if (i < per && first + i < mine) {
-      const int b = row.rank * mine + first + i;
-      cum += got[i];
-      if (mass_alone) cum_mass += static_cast<double>(got[i]) * static_cast<double>(expf(static_cast<float>(b + 1) * (-1.f / steps)));
-      const bool stop = (by_count && cum >= static_cast<u32>(top_k)) || (mass_alone && cum_mass >= enough) || b >= min_bin;
-      if (stop && best == ~0ull) best = static_cast<u64>(b) << 32 | cum;
-    }
-  }
-  best = row.cluster_min(best);
-  const int n = static_cast<int>(best & 0xffffffffu);
-  if (best == ~0ull || n > kList) return false;
-  const float limit = static_cast<float>(static_cast<int>(best >> 32) + 1);
-
-  // ---- candidates, in index order, to the first block
-  int c = 0;
-  for (int j = row.v0 + row.lane; j < row.v1; j += kWarp) {
-    const Vec<T> v = row.piece(j);
-#pragma unroll
-    for (int e = 0; e < VE; ++e) c += distance(v.at(e)) < limit ? 1 : 0;
-  }
-  c = __reduce_add_sync(0xffffffffu, c);
-  if (row.lane == 0) sh.warp_count[row.warp] = c;
-  __syncthreads();
-  int block = 0, at = 0;
-#pragma unroll
-  for (int i = 0; i < kWarps; ++i) {
-    if (i == row.warp) at = block;
-    block += sh.warp_count[i];
-  }
-  const u64* blocks = row.tell(static_cast<u64>(block));
-  row.sync();   // after this no histogram is read any more
-  for (int r = 0; r < row.rank; ++r) at += static_cast<int>(blocks[r]);
-  if (c > 0) {
-    for (int j0 = row.v0; j0 < row.v1; j0 += kWarp) {
-      const int j = j0 + row.lane;
-      u32 in = 0;
-      Vec<T> v;
-      if (j < row.v1) {
-        v = row.piece(j);
-#pragma unroll
-        for (int e = 0; e < VE; ++e) in |= distance(v.at(e)) < limit ? 1u << e : 0u;
-      }
-      if (!__any_sync(0xffffffffu, in != 0)) continue;
-      int inc = __popc(in);
-#pragma unroll
-      for (int o = 1; o < kWarp; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, inc, o);
-        if (row.lane >= o) inc += y;
-      }
-      int to = at + inc - __popc(in);
-      at += __shfl_sync(0xffffffffu, inc, kWarp - 1);
-      if (in) {
-#pragma unroll
-        for (int e = 0; e < VE; ++e) {
-          if (in >> e & 1u) {   // larger logits first, then lower indexes: ascending
-            if (to < kList)
-              store_remote(&sh.list[to], 0, static_cast<u64>(~key_of(v.at(e))) << 32 | static_cast<u32>(row.base + j * VE + e));
-            ++to;
-          }
-        }
-      }
-    }
-  }
-  row.sync();
-  if (row.rank != 0) return true;
-
-  // ---- the first block alone from here on
-  auto logit = [](u64 entry) { return of_key(~static_cast<u32>(entry >> 32)); };
+  auto weight = [&](u64 entry) { return w.template operator()<exact_diff<T>()>(logit_of(entry)); };
   constexpr int kEach = kList / kThreads;
-  const int s0 = static_cast<int>(threadIdx.x) * kEach;   // this thread's of the list
-  u64 last = ~0ull;                                       // the last entry, in rank order, that is kept
-  if (by_count || by_mass) {
-    // top-k's border, then, of the mass above it, top-p's: sums by step, the step that they pass `need` in, and its entries one
-    // against another
-    u64 need = static_cast<u64>(top_k);
-    bool weigh = !by_count;
-    if (weigh) need = share_of(total * kFixed, top_p);
-    for (;;) {
-      __syncthreads();
-      for (int i = threadIdx.x; i < kBins; i += kThreads) bins[i] = 0;
-      if (threadIdx.x == 0) sh.warp_count[0] = 0;
-      __syncthreads();
-      u64 x[kEach], all = 0;
-      int bin[kEach];
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        x[i] = 0;
-        bin[i] = -1;
-        if (s0 + i < n && sh.list[s0 + i] <= last) {
-          const float l = logit(sh.list[s0 + i]);
-          x[i] = weigh ? fixed_of(w.template operator()<exact_diff<T>()>(l)) : 1;
-          bin[i] = static_cast<int>(distance(l));
-          atomicAdd(&bins[bin[i]], x[i]);   // whole numbers: in any order
+  double x[kEach], sum = 0.0, all;
+  u32 kept = 0, all_kept;
+  int s0;
+  constexpr int kFew = 192;
+  if (n <= kFew) {
+    // one candidate per thread, compared with all: its rank and the mass before it
+    s0 = threadIdx.x;
+    const bool in = s0 < n;
+    const u64 me = in ? list[s0] : ~0ull;
+    const double weigh = in ? weight(me) : 0.0;
+    const u64 fixed = in ? fixed_of(weigh) : 0;
+    ulonglong2* pair = reinterpret_cast<ulonglong2*>(among);
+    if (in) pair[s0] = make_ulonglong2(me, fixed);
+    __syncthreads();
+    u32 rank = 0;
+    u64 before = 0;
+    if (row.warp * kWarp < n) {
+      for (int j = 0; j < n; ++j) {
+        const ulonglong2 other = pair[j];
+        if (other.x < me) {
+          ++rank;
+          before += other.y;
         }
       }
-      __syncthreads();
-      u64 own[kMost], sum = 0;
+    }
+    bool on = in && (!ask.by_count || rank < static_cast<u32>(ask.top_k));
+    if (ask.by_mass) {
+      const double of = ask.by_count ? static_cast<double>(row.block_sum(on ? fixed : 0)) : total * kFixed;
+      on = on && before < share_of(of, ask.top_p);
+    }
+    if (ask.by_min) on = on && (rank == 0 || (ask.min_p <= 1.f && static_cast<double>(logit_of(me)) >= ask.min_bound));
+    kept = on ? 1 : 0;
+    x[0] = on ? weigh : 0.0;
+    sum = x[0];
 #pragma unroll
-      for (int i = 0; i < kMost; ++i) {
-        own[i] = bins[static_cast<int>(threadIdx.x) * kMost + i];
-        sum += own[i];
-      }
-      u64 run = row.scan(sum, all);
-      if (weigh && by_count) need = share_of(static_cast<double>(all), top_p);
-      u64 found = ~0ull;
-#pragma unroll
-      for (int i = 0; i < kMost; ++i) {
-        run += own[i];
-        if (run >= need && found == ~0ull) found = static_cast<u64>(static_cast<int>(threadIdx.x) * kMost + i);
-      }
-      found = row.block_min(found);
-      if (found != ~0ull) {   // else fewer than k tokens, or rounding: all of them
-        const int step = static_cast<int>(found);
-        if (static_cast<int>(threadIdx.x) == step / kMost) {   // the sum over the steps before it
-          u64 before = run;
-#pragma unroll
-          for (int i = kMost - 1; i >= 0; --i)
-            if (i >= step % kMost) before -= own[i];
-          sh.slot[kSlots - 1][0] = before;
-        }
-        // the step's entries and what they count for into one place (the sums by step have been read)
+    for (int i = 1; i < kEach; ++i) x[i] = 0.0;
+  } else {
+    s0 = static_cast<int>(threadIdx.x) * kEach;
+    u64 last = ~0ull;   // the last entry, in rank order, that is kept
+    if (ask.by_count || ask.by_mass) {
+      // top-k's border, then, of the mass above it, top-p's: sums by step, the step that they pass `need` in, its entries
+      constexpr int kMost = kBins / kThreads;
+      u64 need = static_cast<u64>(ask.top_k);
+      bool weigh = !ask.by_count;
+      if (weigh) need = share_of(total * kFixed, ask.top_p);
+      for (;;) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < kBins; i += kThreads) bins[i] = 0;
+        if (threadIdx.x == 0) sh.warp_count[0] = 0;
+        __syncthreads();
+        u64 f[kEach], mass = 0;
+        int bin[kEach];
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-          if (bin[i] == step) {
-            const int to = atomicAdd(&sh.warp_count[0], 1);   // in any order: what follows compares all with all
-            among[to] = sh.list[s0 + i];
-            bins[to] = x[i];
+          f[i] = 0;
+          bin[i] = -1;
+          if (s0 + i < n && list[s0 + i] <= last) {
+            f[i] = weigh ? fixed_of(weight(list[s0 + i])) : 1;
+            bin[i] = static_cast<int>(steps.distance(logit_of(list[s0 + i])));
+            atomicAdd(&bins[bin[i]], f[i]);   // whole numbers: in any order
           }
         }
         __syncthreads();
-        const int m = sh.warp_count[0];
-        const u64 before = sh.slot[kSlots - 1][0];
-        u64 border = ~0ull;
-        for (int i = threadIdx.x; i < m; i += kThreads) {
-          const u64 me = among[i];
-          u64 upto = before;   // with all entries of the step up to and with this one
-          for (int j = 0; j < m; ++j) upto += among[j] <= me ? bins[j] : 0;
-          if (upto >= need) border = min(border, me);
+        u64 own[kMost], part = 0;
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+          own[i] = bins[static_cast<int>(threadIdx.x) * kMost + i];
+          part += own[i];
         }
-        last = min(last, row.block_min(border));
+        u64 run = row.scan(part, mass);
+        if (weigh && ask.by_count) need = share_of(static_cast<double>(mass), ask.top_p);
+        u64 found = ~0ull, before = 0;
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+          if (run < need && run + own[i] >= need) {
+            found = static_cast<u64>(static_cast<int>(threadIdx.x) * kMost + i);
+            before = run;
+          }
+          run += own[i];
+        }
+        if (found != ~0ull) sh.slot[kSlots - 1][0] = before;   // one thread
+        found = row.block_min(found);
+        if (found != ~0ull) {   // else fewer than k tokens, or rounding: all of them
+          // the step's entries and what they count for into one place (the sums by step have been read)
+#pragma unroll
+          for (int i = 0; i < kEach; ++i) {
+            if (bin[i] == static_cast<int>(found)) {
+              const int to = atomicAdd(&sh.warp_count[0], 1);   // in any order: what follows compares all with all
+              among[to] = list[s0 + i];
+              bins[to] = f[i];
+            }
+          }
+          __syncthreads();
+          last = min(last, border_among(row, among, bins, sh.warp_count[0], sh.slot[kSlots - 1][0], need));
+        }
+        if (weigh || !ask.by_mass) break;
+        weigh = true;
       }
-      if (weigh || !by_mass) break;
-      weigh = true;
     }
-  }
-  if (by_min) {
-    const double bound = static_cast<double>(w.max) + log(static_cast<double>(min_p)) * static_cast<double>(t);
-    u64 top = ~0ull, low = 0;
+    if (ask.by_min) {
+      u64 top = ~0ull, low = 0;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        if (s0 + i >= n) continue;
+        const u64 entry = list[s0 + i];
+        top = min(top, entry);
+        if (static_cast<double>(logit_of(entry)) >= ask.min_bound) low = max(low, entry);
+      }
+      top = row.block_min(top);              // the first rank is kept whatever min-p is
+      low = ~row.block_min(~low);
+      last = min(last, ask.min_p > 1.f ? top : max(top, low));
+    }
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      if (s0 + i >= n) continue;
-      const u64 entry = sh.list[s0 + i];
-      top = min(top, entry);
-      if (static_cast<double>(logit(entry)) >= bound) low = max(low, entry);
+      const bool in = s0 + i < n && list[s0 + i] <= last;
+      x[i] = in ? weight(list[s0 + i]) : 0.0;
+      sum += x[i];
+      kept += in ? 1 : 0;
     }
-    top = row.block_min(top);              // the first rank is kept whatever min-p is
-    low = ~row.block_min(~low);
-    last = min(last, min_p > 1.f ? top : max(top, low));
   }
   // the weights of what is kept, in index order
-  double x[kEach], sum = 0.0, all;
-  u32 kept = 0;
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const bool in = s0 + i < n && sh.list[s0 + i] <= last;
-    x[i] = in ? w.template operator()<exact_diff<T>()>(logit(sh.list[s0 + i])) : 0.0;
-    sum += x[i];
-    kept += in ? 1 : 0;
-  }
   double run = row.scan(sum, all);
-  u32 all_kept;
   row.scan(kept, all_kept);
-  const double target = static_cast<double>(fmaxf(a.u[row_id], 0.f)) * all;
+  const double target = static_cast<double>(fmaxf(a.u[row_id], 0.f)) * all;   // NaN and what is below 0 count as 0
   // the first that passes the target; past the end the last that has a weight
   u64 pick = ~0ull;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
     run += x[i];
-    if (x[i] > 0.0) {
-      const u64 me = static_cast<u64>(run > target ? s0 + i : 2 * kList - (s0 + i));
-      pick = min(pick, me);
-    }
+    if (x[i] > 0.0) pick = min(pick, static_cast<u64>(run > target ? s0 + i : 2 * kList - (s0 + i)));
   }
   pick = row.block_min(pick);
   if (threadIdx.x == 0) {
-    const int at_list = static_cast<int>(pick < kList ? pick : 2 * kList - pick);
-    const u64 entry = sh.list[at_list];
-    const float l = logit(entry);
+    const u64 entry = list[pick < kList ? pick : 2 * kList - pick];
+    const float l = logit_of(entry);
     const double z = l == w.max ? 0.0 : (static_cast<double>(l) - static_cast<double>(w.max)) / static_cast<double>(t);
     a.put(row_id, static_cast<int>(entry & 0xffffffffu), z - log(total), z - log(all), static_cast<int>(all_kept));
   }
-  return true;
+}
+
+enum class Way { kDone, kBorder, kKeys };   // sampled; the border is known; it is not
+
+// A row by steps.  kBorder: `border` is the last entry, in rank order, that top-k and top-p keep.  The same for the whole cluster.
+template <typename T, class W>
+__device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a, int row_id, const W& w, float t, const Ask& ask,
+                                               u64* scratch, u64& border) {
+  constexpr int VE = per_vec<T>();
+  Shared& sh = row.sh;
+  const bool mass_alone = ask.by_mass && !ask.by_count;
+  const float per_t = mass_alone ? 128.f : 64.f;
+  const Steps steps{w.max, per_t / t};
+  if (w.at_inf || !(steps.scale < 1e30f)) {
+    __syncthreads();   // the row's total is there (see the kernel)
+    return Way::kKeys;
+  }
+  // ---- counts, to the first block
+  row.each([&](float l, int) {
+    const float x = steps.distance(l);
+    if (x < static_cast<float>(kBins)) atomicAdd(&sh.lo[static_cast<int>(x)], 1u);   // false for NaN
+  });
+  __syncthreads();   // and the row's total is there
+  const double total = sh.total;
+  u64* said = row.next_slot();        // step, candidates
+  u64* said_range = row.next_slot();  // first step in which the border may lie, tokens before it
+  row.sync();
+  if (row.rank == 0) {
+    constexpr int kMost = kBins / kThreads;
+    static_assert(kMost == 4, "a thread's steps are one 16-byte load");
+    const int first = static_cast<int>(threadIdx.x) * kMost;
+    u32 got[kMost] = {}, count = 0, all_count;
+    float least[kMost];   // weights at the far end of each step
+    double mass = 0.0, all_mass;
+    {
+      uint4 v[kMaxCluster];
+#pragma unroll
+      for (int r = 0; r < kMaxCluster; ++r) v[r] = r < row.cluster ? load_remote4(&sh.lo[first], r) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int r = 0; r < kMaxCluster; ++r) {
+        got[0] += v[r].x; got[1] += v[r].y; got[2] += v[r].z; got[3] += v[r].w;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+      count += got[i];
+      if (mass_alone) {
+        least[i] = expf(static_cast<float>(first + i + 1) * (-1.f / per_t));
+        mass += static_cast<double>(got[i]) * static_cast<double>(least[i]);
+      }
+    }
+    u32 cum = row.scan(count, all_count);
+    double cum_mass = mass_alone ? row.scan(mass, all_mass) : 0.0;
+    const double share = static_cast<double>(fmaxf(ask.top_p, 0.f)) * total;
+    const double enough = share * (1.0 + 1e-5);   // expf and the distances are not exact
+    // the same mass with the weights at the near ends, which is 1 / far_near as much, is not enough
+    const double too_little = share * static_cast<double>(expf(-1.f / per_t)) * (1.0 - 1e-5);
+    int min_bin = INT_MAX;   // the first step that lies below what min-p keeps
+    if (ask.by_min && !ask.by_mass) {
+      const float at = ask.min_p >= 1.f ? 0.f : -logf(ask.min_p) * per_t;
+      if (at < static_cast<float>(kBins - 3)) min_bin = static_cast<int>(at) + 2;
+    }
+    u64 best = ~0ull, low = ~0ull;
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+      const int b = first + i;
+      const u32 before = cum;
+      cum += got[i];
+      if (mass_alone) cum_mass += static_cast<double>(got[i]) * static_cast<double>(least[i]);
+      const bool by_count = ask.by_count && cum >= static_cast<u32>(ask.top_k);
+      if (best == ~0ull && (by_count || (mass_alone && cum_mass >= enough) || b >= min_bin)) best = static_cast<u64>(b) << 32 | cum;
+      if (low == ~0ull && (mass_alone ? cum_mass >= too_little : by_count)) low = static_cast<u64>(b) << 32 | before;
+    }
+    best = row.block_min(best);
+    low = row.block_min(low);
+    if (threadIdx.x == 0) {
+      row.say(said, best);
+      row.say(said_range, low);
+    }
+  }
+  row.sync();
+  const u64 best = said[0], low = said_range[0];
+  if (best == ~0ull) return Way::kKeys;
+  const int n = static_cast<int>(best & 0xffffffffu), end = static_cast<int>(best >> 32) + 1;
+  const float limit = static_cast<float>(end);
+  const int region = kList / row.cluster;   // of the list, for each block
+
+  if (n <= kList) {
+    // ---- candidates, in index order, to the first block
+    int c = 0;
+    for (int j = row.v0 + row.lane; j < row.v1; j += kWarp) {
+      const Vec<T> v = row.piece(j);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) c += steps.distance(v.at(e)) < limit ? 1 : 0;
+    }
+    c = __reduce_add_sync(0xffffffffu, c);
+    if (row.lane == 0) sh.warp_count[row.warp] = c;
+    __syncthreads();
+    int block = 0, at = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      if (i == row.warp) at = block;
+      block += sh.warp_count[i];
+    }
+    const u64* blocks = row.tell(static_cast<u64>(block));
+    if (c > 0) {
+      for (int j0 = row.v0; j0 < row.v1; j0 += kWarp) {
+        const int j = j0 + row.lane;
+        u32 in = 0;
+        Vec<T> v;
+        if (j < row.v1) {
+          v = row.piece(j);
+#pragma unroll
+          for (int e = 0; e < VE; ++e) in |= steps.distance(v.at(e)) < limit ? 1u << e : 0u;
+        }
+        if (!__any_sync(0xffffffffu, in != 0)) continue;
+        int inc = __popc(in);
+#pragma unroll
+        for (int o = 1; o < kWarp; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, inc, o);
+          if (row.lane >= o) inc += y;
+        }
+        int to = at + inc - __popc(in);
+        at += __shfl_sync(0xffffffffu, inc, kWarp - 1);
+        if (in) {
+#pragma unroll
+          for (int e = 0; e < VE; ++e) {
+            if (in >> e & 1u) {
+              if (to < region) store_remote(&sh.list[row.rank * region + to], 0, entry_of(v.at(e), row.base + j * VE + e));
+              ++to;
+            }
+          }
+        }
+      }
+    }
+    row.sync();
+    bool fits = true;
+    for (int r = 0; r < row.cluster; ++r) fits &= blocks[r] <= static_cast<u64>(region);
+    if (fits) {
+      if (row.rank != 0) return Way::kDone;
+      // one behind another; the step's sums and candidates then take the list's place and what follows it
+      for (int i = threadIdx.x; i < n; i += kThreads) {
+        int from = i, r = 0;
+        while (from >= static_cast<int>(blocks[r])) from -= static_cast<int>(blocks[r++]);
+        scratch[i] = sh.list[r * region + from];
+      }
+      __syncthreads();
+      finish_alone(row, a, row_id, w, steps, t, total, ask, scratch, n, sh.list, scratch + kList);
+      return Way::kDone;
+    }
+    return Way::kKeys;   // too many of them in one block, whose histograms may be gone
+  }
+  if ((ask.by_count && ask.by_mass) || low == ~0ull) return Way::kKeys;
+
+  // ---- the step that holds the border, and what lies before it
+  const int step0 = static_cast<int>(low >> 32);
+  u64 need = static_cast<u64>(ask.top_k), before = low & 0xffffffffu;
+  int step = step0;
+  u64* slot_step = row.next_slot();
+  u64* slot_before = row.next_slot();
+  if (mass_alone) {
+    const int range = end - step0;
+    need = share_of(total * kFixed, ask.top_p);
+    u64* own = reinterpret_cast<u64*>(sh.lo);   // 8 bytes a step: up to kBins steps, the histograms have been read
+    __syncthreads();
+    for (int i = threadIdx.x; i < range; i += kThreads) own[i] = 0;
+    __syncthreads();
+    const float sure = static_cast<float>(step0);
+    row.each([&](float l, int) {
+      const float x = steps.distance(l);
+      if (x >= sure && x < limit)
+        atomicAdd(&own[static_cast<int>(x) - step0], fixed_of(w.template operator()<exact_diff<T>()>(l)));
+    });
+    double sum = row.weigh(w, [&](float l, int) { return steps.distance(l) < sure; });
+    sum = row.block_sum(row.lane == 0 ? sum : 0.0);
+    u64* sums = row.tell(static_cast<u64>(__double_as_longlong(sum)));
+    row.sync();
+    if (row.rank == 0) {
+      // by step over the cluster
+      double below = 0.0;
+      for (int r = 0; r < row.cluster; ++r) below += __longlong_as_double(static_cast<long long>(sums[r]));
+      u64 run = static_cast<u64>(__double2ll_rn(below * kFixed));
+      u64 found = ~0ull;
+      for (int i0 = 0; i0 < range && found == ~0ull; i0 += kThreads) {
+        u64 m = 0, all;
+        if (i0 + static_cast<int>(threadIdx.x) < range)
+          for (int r = 0; r < row.cluster; ++r) m += load_remote(&own[i0 + threadIdx.x], r);
+        const u64 pre = run + row.scan(m, all);
+        const bool here = pre < need && pre + m >= need;
+        if (here) sh.slot[kSlots - 1][0] = pre;
+        found = row.block_min(here ? static_cast<u64>(step0 + i0 + static_cast<int>(threadIdx.x)) : ~0ull);
+        run += all;
+      }
+      if (threadIdx.x == 0) {
+        row.say(slot_step, found);
+        row.say(slot_before, sh.slot[kSlots - 1][0]);
+      }
+    }
+    row.sync();
+    if (slot_step[0] == ~0ull) return Way::kKeys;
+    step = static_cast<int>(slot_step[0]);
+    before = slot_before[0];
+  }
+  // ---- the step's tokens, in any order, to the first block
+  u64* said_border = row.next_slot();
+  u32* taken = reinterpret_cast<u32*>(&sh.warp_count[0]);
+  if (threadIdx.x == 0) *taken = 0;
+  row.sync();   // nobody reads what the list takes the place of
+  const float from = static_cast<float>(step), to = static_cast<float>(step + 1);
+  auto on_step = [&](float l) {
+    const float x = steps.distance(l);
+    return x >= from && x < to;
+  };
+  int mine = 0;
+  row.each([&](float l, int) { mine += on_step(l) ? 1 : 0; });
+  int inc = mine;
+#pragma unroll
+  for (int o = 1; o < kWarp; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, inc, o);
+    if (row.lane >= o) inc += y;
+  }
+  u32 at = 0;
+  if (row.lane == kWarp - 1 && inc > 0) at = take_from_remote(taken, 0, static_cast<u32>(inc));
+  at = __shfl_sync(0xffffffffu, at, kWarp - 1) + static_cast<u32>(inc - mine);
+  if (mine > 0)
+    row.each([&](float l, int i) {
+      if (!on_step(l)) return;
+      if (at < kList) store_remote(&sh.list[at], 0, entry_of(l, i));
+      ++at;
+    });
+  row.sync();
+  if (row.rank == 0) {
+    const int m = static_cast<int>(*taken);
+    u64 found = ~0ull;
+    if (m <= kList / 2) {   // the slice is still needed: the amounts take the list's other half
+      u64* amounts = sh.list + kList / 2;
+      for (int i = threadIdx.x; i < m; i += kThreads)
+        amounts[i] = mass_alone ? fixed_of(w.template operator()<exact_diff<T>()>(logit_of(sh.list[i]))) : 1;
+      __syncthreads();
+      found = border_among(row, sh.list, amounts, m, before, need);
+    }
+    if (threadIdx.x == 0) row.say(said_border, found);
+  }
+  row.sync();
+  border = said_border[0];
+  return border == ~0ull ? Way::kKeys : Way::kBorder;
 }
 
 template <typename T>
@@ -666,13 +879,13 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
     if (blockIdx.x % cluster == 0 && threadIdx.x == 0) a.put(row_id, -1, 0.0, 0.0, 0);
     return;
   }
+  cluster_arrive();   // waited for before anything is written to another block's shared memory
   Row<T> row(sh);
   row.cluster = cluster;
   row.rank = static_cast<int>(blockIdx.x % cluster);
   row.flip = row.slot = 0;
   row.lane = threadIdx.x % kWarp;
   row.warp = threadIdx.x / kWarp;
-  fill_table(sh.table, threadIdx.x, kThreads);
 
   // ---- the slice into shared memory, NaN as -inf and -0 as 0
   const int from = row.rank * slice, len = max(0, min(slice, a.v - from));
@@ -686,13 +899,20 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
   row.v1 = min(row.v0 + stretch, row.vecs);
   constexpr int kAtOnce = 4;
   u32 top = key_of(-INFINITY);
-  for (int j0 = row.v0 + row.lane; j0 < row.v1; j0 += kWarp * kAtOnce) {
+  bool table = false;
+  for (int j0 = row.v0 + row.lane; ; j0 += kWarp * kAtOnce) {
     Vec<T> v[kAtOnce];
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
       const int j = j0 + i * kWarp;
       if (j < row.v1) v[i] = load_vec(l, j * VE - head, len);
     }
+    if (!table) {   // while the first of them are on their way
+      table = true;
+      fill_table(sh.table, threadIdx.x, kThreads);
+      for (int i = threadIdx.x; i < kBins; i += kThreads) sh.lo[i] = 0;
+    }
+    if (j0 >= row.v1) break;
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
       const int j = j0 + i * kWarp;
@@ -708,157 +928,215 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
       data[j] = make_uint4(v[i].w[0], v[i].w[1], v[i].w[2], v[i].w[3]);   // a warp reads its own stretch alone
     }
   }
-  row.sync();   // every block of the cluster runs: its shared memory may be written to
-  const float m = of_key(static_cast<u32>(row.cluster_max(top)));
-  if (!(m > -INFINITY)) {   // the same for the whole cluster
-    if (row.rank == 0 && threadIdx.x == 0) a.put(row_id, -1, 0.0, 0.0, 0);
-    row.sync();
-    return;
-  }
+  __syncthreads();   // the table
+
+  // ---- the sums of the warps' weights, relative to their largest, and from them the row's
   bool greedy;
   const float t = a.temp(row_id, greedy);
   Weights<16> w;
   w.set_temperature(t, sh.table);
-  w.set_max(m);
   constexpr bool kExact = exact_diff<T>();
   auto weight = [&](float x) { return w.template operator()<kExact>(x); };
-  const int top_k = a.top_k ? a.top_k[row_id] : 0;
-  const float top_p = a.top_p ? a.top_p[row_id] : 1.f, min_p = a.min_p ? a.min_p[row_id] : 0.f;
-  const bool by_mass = top_p < 1.f && !greedy;
-
-  // ---- the sum of all weights
-  double total;
+  const float own_max = of_key(__reduce_max_sync(0xffffffffu, top));
+  w.set_max(own_max);
   {
     double s = 0.0;
-    if (w.floor > -1e37f && fabsf(m) < 1e6f * -w.floor) {   // the limit below is a number well under m
-      // What is -inf or far below the largest counts as its 2^-100th here, which no sum that holds a 1 shows.
-      const float least = m + w.floor;
-      WeightSum even, odd;
-      for (int j0 = row.v0 + row.lane; j0 < row.v1; j0 += 2 * kWarp) {
-        const int j1 = j0 + kWarp;
-        const Vec<T> x = row.piece(j0), y = row.piece(min(j1, row.v1 - 1));
+    if (own_max > -INFINITY) {
+      if (w.floor > -1e37f && fabsf(own_max) < 1e6f * -w.floor) {   // the limit below is a number well under the largest
+        // What is -inf or far below the largest counts as its 2^-100th here, which no sum that holds a 1 shows.
+        const float least = own_max + w.floor;
+        WeightSum even, odd;
+        for (int j0 = row.v0 + row.lane; j0 < row.v1; j0 += 2 * kWarp) {
+          const int j1 = j0 + kWarp;
+          const Vec<T> x = row.piece(j0), y = row.piece(min(j1, row.v1 - 1));
 #pragma unroll
-        for (int e = 0; e < VE; e += 2) w.template add<kExact>(f2(fmaxf(x.at(e), least), fmaxf(x.at(e + 1), least)), even);
-        if (j1 < row.v1) {
+          for (int e = 0; e < VE; e += 2) w.template add<kExact>(f2(fmaxf(x.at(e), least), fmaxf(x.at(e + 1), least)), even);
+          if (j1 < row.v1) {
 #pragma unroll
-          for (int e = 0; e < VE; e += 2) w.template add<kExact>(f2(fmaxf(y.at(e), least), fmaxf(y.at(e + 1), least)), odd);
+            for (int e = 0; e < VE; e += 2) w.template add<kExact>(f2(fmaxf(y.at(e), least), fmaxf(y.at(e + 1), least)), odd);
+          }
         }
+        s = even.value() + odd.value();
+      } else {
+        row.each([&](float x, int) { s += weight(x); });
       }
-      s = even.value() + odd.value();
-    } else {
-      row.each([&](float x, int) { s += weight(x); });
     }
-    const double stretch_sum = warp_sum(s);
-    if (row.lane == 0) sh.stretch[row.warp] = stretch_sum;
-    total = row.cluster_sum(s);
+    s = warp_sum(s);
+    if (row.lane == 0) {
+      sh.stretch[row.warp] = s;
+      sh.stretch_max[row.warp] = own_max;
+    }
   }
-  const bool by_count = top_k > 0 && top_k < a.v && !greedy, by_min = min_p > 0.f && !greedy;
-  if ((by_count || by_mass || by_min) &&
-      sample_from_candidates(row, a, row_id, w, t, total, top_k, top_p, min_p, reinterpret_cast<u64*>(data)))
+  // what a sum relative to x counts for relative to y
+  auto factor = [&](float x, float y) {
+    return x == y ? 1.0 : x > -INFINITY ? exp((static_cast<double>(x) - static_cast<double>(y)) / static_cast<double>(t)) : 0.0;
+  };
+  cluster_wait();
+  __syncthreads();
+  u64* maxes = row.next_slot();
+  u64* block_sums = row.next_slot();
+  if (row.warp == 0) {
+    const float x = row.lane < kWarps ? sh.stretch_max[row.lane] : -INFINITY;
+    const float most = of_key(__reduce_max_sync(0xffffffffu, key_of(x)));
+    const double s = warp_sum(row.lane < kWarps ? sh.stretch[row.lane] * factor(x, most) : 0.0);
+    if (row.lane < cluster) {
+      store_remote(maxes + row.rank, row.lane, key_of(most));
+      store_remote(block_sums + row.rank, row.lane, static_cast<u64>(__double_as_longlong(s)));
+    }
+  }
+  row.sync();
+  u32 top_key = 0;
+  for (int r = 0; r < cluster; ++r) top_key = max(top_key, static_cast<u32>(maxes[r]));
+  const float m = of_key(top_key);
+  if (!(m > -INFINITY)) {   // the same for the whole cluster
+    if (row.rank == 0 && threadIdx.x == 0) a.put(row_id, -1, 0.0, 0.0, 0);
     return;
-  // ---- what is kept: keys above `edge`, and of those equal to it the first `ties` in index order
+  }
+  if (row.warp == kWarps - 1) {   // read after the next barrier of the block
+    const double s = row.lane < cluster ? __longlong_as_double(static_cast<long long>(block_sums[row.lane])) *
+                                              factor(of_key(static_cast<u32>(maxes[row.lane])), m)
+                                        : 0.0;
+    const double all = warp_sum(s);
+    if (row.lane == 0) sh.total = all;
+  }
+  w.set_max(m);
+
+  // ---- greedy: the first of the largest
+  if (greedy) {
+    u64 first = ~0ull;
+    row.each([&](float x, int i) {
+      if (x == m) first = min(first, static_cast<u64>(i));
+    });
+    first = row.cluster_min(first);
+    if (row.rank == 0 && threadIdx.x == 0) a.put(row_id, static_cast<int>(first), -log(sh.total), 0.0, 1);
+    return;
+  }
+
+  Ask ask;
+  ask.top_k = a.top_k ? a.top_k[row_id] : 0;
+  ask.top_p = a.top_p ? a.top_p[row_id] : 1.f;
+  ask.min_p = a.min_p ? a.min_p[row_id] : 0.f;
+  ask.by_count = ask.top_k > 0 && ask.top_k < a.v;
+  ask.by_mass = ask.top_p < 1.f;
+  ask.by_min = ask.min_p > 0.f;
+  ask.min_bound = ask.by_min ? static_cast<double>(m) + log(static_cast<double>(ask.min_p)) * static_cast<double>(t) : 0.0;
+
+  // ---- what is kept: keys above `edge`, and of those equal to it the indexes up to `limit`
   const u32 none = tkey<T>(-INFINITY), best = tkey<T>(m);
   u32 edge = none;
-  int ties = 0;
-  double of = total * kFixed;   // the mass that top-p has a share of
-  if (greedy) {
-    edge = best;
-    ties = 1;
-  } else {
-    u64 above;
-    if (top_k > 0 && top_k < a.v) {
-      const u32 k = row.template border<false>(none, best, static_cast<u64>(top_k), [](float) { return 0ull; }, above);
-      if (k > none) {
-        edge = k;
-        ties = top_k - static_cast<int>(above);
+  int limit = -1;
+  bool many = false;   // more than a few thousand are kept, as far as is known
+  if (ask.by_count || ask.by_mass || ask.by_min) {
+    u64 border = 0;
+    const Way way = sample_by_steps(row, a, row_id, w, t, ask, reinterpret_cast<u64*>(data), border);
+    if (way == Way::kDone) return;
+    const double total = sh.total;
+    if (way == Way::kBorder) {
+      edge = tkey<T>(logit_of(border));
+      limit = static_cast<int>(border & 0xffffffffu);
+      many = true;
+    } else {
+      int ties = 0;
+      u64 above;
+      double of = total * kFixed;   // the mass that top-p has a share of
+      if (ask.by_count) {
+        const u32 k = row.template border<false>(none, best, static_cast<u64>(ask.top_k), [](float) { return 0ull; }, above);
+        if (k > none) {
+          edge = k;
+          ties = ask.top_k - static_cast<int>(above);
+        }
+        if (ask.by_mass) {
+          const u32 e = edge;
+          u64 all = 0;
+          row.each([&](float x, int) {
+            if (tkey<T>(x) > e) all += fixed_of(weight(x));
+          });
+          all = row.cluster_sum(all);
+          if (edge > none) all += static_cast<u64>(ties) * fixed_of(weight(of_tkey<T>(edge)));
+          of = static_cast<double>(all);
+        }
       }
-      if (by_mass) {
-        const u32 e = edge;
-        u64 all = 0;
-        row.each([&](float x, int) {
-          if (tkey<T>(x) > e) all += fixed_of(weight(x));
-        });
-        all = row.cluster_sum(all);
-        if (edge > none) all += static_cast<u64>(ties) * fixed_of(weight(of_tkey<T>(edge)));
-        of = static_cast<double>(all);
+      if (ask.by_mass) {
+        const u64 need = share_of(of, ask.top_p);
+        u32 lo = edge;
+        if (edge == none) {   // lighter than (1 - p) / V of all: even together they are not the part that is left out
+          const double cut = (1.0 - static_cast<double>(fmaxf(ask.top_p, 0.f))) * total / a.v * 0.999;
+          const double bound = static_cast<double>(m) + log(cut) * static_cast<double>(t);
+          const float f = bound < static_cast<double>(m) ? __double2float_rd(bound) : m;
+          lo = min(max(tkey<T>(f), none), best);
+        }
+        const u32 k = row.template border<true>(lo, best, need, [&](float x) { return fixed_of(weight(x)); }, above);
+        const u64 each = fixed_of(weight(of_tkey<T>(k)));
+        u64 c = each > 0 && need > above ? (need - above + each - 1) / each : 1;
+        if (c < 1) c = 1;
+        if (c > static_cast<u64>(a.v)) c = a.v;
+        if (k > edge || edge == none) {
+          edge = k;
+          ties = static_cast<int>(c);
+        } else if (static_cast<int>(c) < ties) {
+          ties = static_cast<int>(c);
+        }
+      }
+      // the index of the last tie that is kept
+      if (edge > none) {
+        int c = 0;
+        row.each([&](float x, int) { c += tkey<T>(x) == edge ? 1 : 0; });
+        c = __reduce_add_sync(0xffffffffu, c);
+        __syncthreads();
+        if (row.lane == 0) sh.warp_count[row.warp] = c;
+        __syncthreads();
+        int block = 0, mine = 0;
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) {
+          if (i == row.warp) mine = block;
+          block += sh.warp_count[i];
+        }
+        const u64* s = row.tell(static_cast<u64>(block));
+        u64* said = row.next_slot();
+        row.sync();
+        int before = 0, sum = 0;
+        for (int r = 0; r < cluster; ++r) {
+          if (r == row.rank) before = sum;
+          sum += static_cast<int>(s[r]);
+        }
+        limit = INT_MAX;
+        if (sum > ties) {
+          const int from_here = ties - before - mine;   // the from_here-th of this warp's ties is the last
+          if (from_here >= 1 && from_here <= c) {
+            float unused;
+            const int at = find_in_stretch(row, from_here - 0.5, [&](float x, int) { return tkey<T>(x) == edge ? 1.0 : 0.0; },
+                                           unused);
+            if (row.lane == 0) row.say(said, static_cast<u64>(at));
+          }
+          row.sync();
+          limit = static_cast<int>(said[0]);
+        }
       }
     }
-    if (by_mass) {
-      const u64 need = share_of(of, top_p);
-      u32 lo = edge;
-      if (edge == none) {   // lighter than (1 - p) / V of all: even together they are not the part that is left out
-        const double cut = (1.0 - static_cast<double>(fmaxf(top_p, 0.f))) * total / a.v * 0.999;
-        const double bound = static_cast<double>(m) + log(cut) * static_cast<double>(t);
-        const float f = bound < static_cast<double>(m) ? __double2float_rd(bound) : m;
-        lo = min(max(tkey<T>(f), none), best);
-      }
-      const u32 k = row.template border<true>(lo, best, need, [&](float x) { return fixed_of(weight(x)); }, above);
-      const u64 each = fixed_of(weight(of_tkey<T>(k)));
-      u64 c = each > 0 && need > above ? (need - above + each - 1) / each : 1;
-      if (c < 1) c = 1;
-      if (c > static_cast<u64>(a.v)) c = a.v;
-      if (k > edge || edge == none) {
-        edge = k;
-        ties = static_cast<int>(c);
-      } else if (static_cast<int>(c) < ties) {
-        ties = static_cast<int>(c);
-      }
-    }
-    if (min_p > 1.f) {
+    if (ask.min_p > 1.f) {   // the first rank alone: the first of the largest
+      u64 first = ~0ull;
+      row.each([&](float x, int i) {
+        if (x == m) first = min(first, static_cast<u64>(i));
+      });
       edge = best;
-      ties = 1;
-    } else if (min_p > 0.f) {
-      const double bound = static_cast<double>(m) + log(static_cast<double>(min_p)) * static_cast<double>(t);
-      float f = __double2float_ru(bound);   // the smallest logit that stays
+      limit = static_cast<int>(row.cluster_min(first));
+    } else if (ask.by_min) {
+      float f = __double2float_ru(ask.min_bound);   // the smallest logit that stays
       if (f > m) f = m;
       u32 k = tkey<T>(f + 0.f);
       if (of_tkey<T>(k) < f) ++k;
       if (k > edge) {
         edge = k;
-        ties = INT_MAX;
+        limit = INT_MAX;
       }
     }
-    if (edge == none) ties = 0;
+  } else {
+    __syncthreads();   // the total
   }
-
-  // ---- the index of the last tie that is kept
-  int limit = INT_MAX;
-  if (ties < a.v && ties > 0) {
-    int c = 0;
-    row.each([&](float x, int) { c += tkey<T>(x) == edge ? 1 : 0; });
-    c = __reduce_add_sync(0xffffffffu, c);
-    if (row.lane == 0) sh.warp_count[row.warp] = c;
-    __syncthreads();
-    int block = 0, mine = 0;
-#pragma unroll
-    for (int i = 0; i < kWarps; ++i) {
-      if (i == row.warp) mine = block;
-      block += sh.warp_count[i];
-    }
-    const u64* s = row.tell(static_cast<u64>(block));
-    u64* said = sh.slot[row.slot++];
-    row.sync();
-    int before = 0, sum = 0;
-    for (int r = 0; r < cluster; ++r) {
-      if (r == row.rank) before = sum;
-      sum += static_cast<int>(s[r]);
-    }
-    if (sum > ties) {
-      const int from_here = ties - before - mine;   // the from_here-th of this warp's ties is the last
-      if (from_here >= 1 && from_here <= c) {
-        float unused;
-        const int at = find_in_stretch(row, from_here - 0.5, [&](float x, int) { return tkey<T>(x) == edge ? 1.0 : 0.0; },
-                                       unused);
-        if (row.lane == 0)
-          for (int r = 0; r < cluster; ++r) store_remote(said, r, static_cast<u64>(at));
-      }
-      row.sync();
-      limit = static_cast<int>(said[0]);
-    }
-  }
+  const double total = sh.total;
   auto kept = [&](float x, int i) {
     const u32 k = tkey<T>(x);
-    return k > edge || (k == edge && ties > 0 && i <= limit);
+    return k > edge || (k == edge && i <= limit);
   };
 
   // ---- the kept weights by stretches
@@ -866,12 +1144,15 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
   int count = 0;
   if (edge == none) {   // all of them: their sums are there
     row.each([&](float x, int) { count += x > -INFINITY ? 1 : 0; });
-    s = sh.stretch[row.warp];
+    s = sh.stretch[row.warp] * factor(sh.stretch_max[row.warp], m);
     if (s < 0x1p-60) {   // perhaps nothing but what counts as 2^-100 there and as 0 here
       s = 0.0;
       row.each([&](float x, int) { s += weight(x); });
       s = warp_sum(s);
     }
+  } else if (many) {
+    row.each([&](float x, int i) { count += kept(x, i) ? 1 : 0; });
+    s = row.weigh(w, kept);
   } else {
     row.each([&](float x, int i) {
       if (kept(x, i)) {
@@ -889,11 +1170,10 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
     sh.warp_count[row.warp] = count;
   }
   __syncthreads();
-  double block = 0.0, mine = 0.0;
+  double block = 0.0;
   int block_count = 0;
 #pragma unroll
   for (int i = 0; i < kWarps; ++i) {
-    if (i == row.warp) mine = block;
     block += __longlong_as_double(static_cast<long long>(sums[i]));
     block_count += sh.warp_count[i];
   }
@@ -918,29 +1198,27 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
     run += x;
     if (target < run) break;
   }
-  if (owner == row.rank) {
-    const double rest = target - at;
-    double upto = 0.0, first = 0.0;
-    int who = 0;
+  if (owner != row.rank) return;
+  const double rest = target - at;
+  double upto = 0.0, first = 0.0;
+  int who = 0;
 #pragma unroll
-    for (int i = 0; i < kWarps; ++i) {
-      const double x = __longlong_as_double(static_cast<long long>(sums[i]));
-      if (x > 0.0 && (upto <= rest || i == 0)) {
-        who = i;
-        first = upto;
-      }
-      upto += x;
+  for (int i = 0; i < kWarps; ++i) {
+    const double x = __longlong_as_double(static_cast<long long>(sums[i]));
+    if (x > 0.0 && (upto <= rest || i == 0)) {
+      who = i;
+      first = upto;
     }
-    if (who == row.warp) {
-      float picked;
-      const int token = find_in_stretch(row, rest - first, [&](float x, int i) { return kept(x, i) ? weight(x) : 0.0; }, picked);
-      if (row.lane == 0) {
-        const double z = picked == m ? 0.0 : (static_cast<double>(picked) - static_cast<double>(m)) / static_cast<double>(t);
-        a.put(row_id, token, z - log(total), z - log(kept_total), kept_count);
-      }
+    upto += x;
+  }
+  if (who == row.warp) {
+    float picked;
+    const int token = find_in_stretch(row, rest - first, [&](float x, int i) { return kept(x, i) ? weight(x) : 0.0; }, picked);
+    if (row.lane == 0) {
+      const double z = picked == m ? 0.0 : (static_cast<double>(picked) - static_cast<double>(m)) / static_cast<double>(t);
+      a.put(row_id, token, z - log(total), z - log(kept_total), kept_count);
     }
   }
-  row.sync();   // no block leaves while another may still write to it
 }
 
 template <typename T>
