@@ -706,19 +706,35 @@ def a3po_linear_workspace_bytes(N, K, M, dt, activation=A3PO_ACT_NONE, has_row_m
     return load_library().a3po_linear_workspace_bytes(N, K, M, dt, activation, int(bool(has_row_mask)), int(bool(is_bwd)))
 
 
-def _linear_shapes(x, w, sides, row_mask):
-    """N, K and M after checking x [N, K], w [M, K], `sides` [N, M] of x's type and the mask."""
+def _linear_shapes(x, w, same, f32, others, row_mask):
+    """dtype code, N, K and M after checking x [N, K], w [M, K] and, as (tensor, shape, elements): `same` of x's type, `f32` of
+    fp32 (`others`: a tensor's own type), all contiguous on the current device."""
     dt = _dtype_code(x)
     if x.dim() != 2 or w.dim() != 2 or w.shape[1] != x.shape[1]:
         raise ValueError("shape mismatch")
     (n, k), m = x.shape, w.shape[0]
-    _here(x, w, *sides, row_mask)
-    _want(x, x.dtype, "x"); _want(w, x.dtype, "w"); _want(row_mask, torch.uint8, "row_mask")
-    for t in sides:
-        _want(t, x.dtype, "matrix [N, M]")
-        if t is not None and tuple(t.shape) != (n, m):
-            raise ValueError("shape mismatch")
-    if row_mask is not None and row_mask.numel() != n:
+    device, dtype = x.get_device(), x.dtype
+    fine = (device >= 0 and device == torch.cuda.current_device() and x.is_contiguous() and w.dtype is dtype
+            and w.get_device() == device and w.is_contiguous())
+    sizes = {"nk": (n, k), "nm": (n, m), "mk": (m, k), "m": (m,)}
+    for tensors, ty in ((same, dtype), (f32, torch.float32), (others, None)):
+        for t, size in tensors:
+            if t is not None:
+                fine &= ((ty is None or t.dtype is ty) and t.get_device() == device and t.is_contiguous()
+                         and (size == "" or (t.numel() == m if size == "m" else t.shape == sizes[size])))
+    if row_mask is not None:
+        fine &= (row_mask.dtype is torch.uint8 and row_mask.get_device() == device and row_mask.numel() == n
+                 and row_mask.is_contiguous())
+    if not fine:   # say what is wrong
+        every = [t for t, _ in same + f32 + others]
+        _here(x, w, *every, row_mask)
+        _want(x, dtype, "x"); _want(w, dtype, "w"); _want(row_mask, torch.uint8, "row_mask")
+        for tensors, ty in ((same, dtype), (f32, torch.float32)):
+            for t, _ in tensors:
+                _want(t, ty, "matrix or vector")
+        for t, _ in others:
+            if t is not None:
+                _want(t, t.dtype, "matrix or buffer")
         raise ValueError("shape mismatch")
     return dt, n, k, m
 
@@ -727,15 +743,12 @@ def a3po_linear_fwd(x, w, y, ws, *, bias=None, residual=None, row_mask=None, kep
                     status=None, stream=None):
     """y = act(x w^T + bias) + residual; y has x's type or is fp32.  `kept` (uint8 buffer of a3po_linear_kept_bytes) is filled for
     a3po_linear_bwd when given; without an activation there is nothing to keep."""
-    dt, n, k, m = _linear_shapes(x, w, (residual,), row_mask)
-    _here(y, bias, kept, ws, status)
-    _want(bias, x.dtype, "bias"); _want(kept, torch.uint8, "kept"); _want(ws, torch.uint8, "ws")
-    _want(status, torch.int32, "status")
-    if y.dtype != torch.float32:
-        _want(y, x.dtype, "y")
-    _want(y, y.dtype, "y")
-    if tuple(y.shape) != (n, m) or (bias is not None and bias.numel() != m):
-        raise ValueError("shape mismatch")
+    own = ((residual, "nm"), (bias, "m"))
+    f32, same = (((y, "nm"),), own) if y.dtype is torch.float32 else ((), own + ((y, "nm"),))
+    dt, n, k, m = _linear_shapes(x, w, same, f32, ((kept, ""), (ws, ""), (status, "")), row_mask)
+    if (kept is not None and kept.dtype is not torch.uint8) or ws.dtype is not torch.uint8 or (
+            status is not None and status.dtype is not torch.int32):
+        raise TypeError("kept and ws: expected uint8 buffers; status: int32")
     rc = load_library().a3po_linear_fwd(_ptr(x), _ptr(w), _ptr(bias), _ptr(residual), _ptr(row_mask), n, k, m, dt, activation,
                                         _ptr(y), _dtype_code(y), _ptr(kept), 0 if kept is None else kept.numel(), _ptr(ws),
                                         ws.numel(), _ptr(status), _stream(stream))
@@ -746,16 +759,12 @@ def a3po_linear_bwd(x, w, grad_y, grad_x, grad_w, ws, *, kept=None, grad_bias=No
                     activation=A3PO_ACT_NONE, accumulate_grad_w=False, status=None, stream=None):
     """Gradients of a3po_linear_fwd; grad_x, grad_w or both may be None.  grad_w is fp32 or of the weights' type, grad_bias fp32;
     the residual's gradient is grad_y itself."""
-    dt, n, k, m = _linear_shapes(x, w, (grad_y,), row_mask)
-    _here(grad_x, grad_w, grad_bias, kept, ws, status)
-    _want(grad_x, x.dtype, "grad_x"); _want(grad_bias, torch.float32, "grad_bias"); _want(kept, torch.uint8, "kept")
-    _want(ws, torch.uint8, "ws"); _want(status, torch.int32, "status")
     gdt = A3PO_F32 if grad_w is None else _dtype_code(grad_w)
-    if grad_w is not None:
-        _want(grad_w, grad_w.dtype, "grad_w")
-    if ((grad_x is not None and grad_x.shape != x.shape) or (grad_w is not None and grad_w.shape != w.shape)
-            or (grad_bias is not None and grad_bias.numel() != m)):
-        raise ValueError("shape mismatch")
+    dt, n, k, m = _linear_shapes(x, w, ((grad_y, "nm"), (grad_x, "nk")), ((grad_bias, "m"),),
+                                 ((grad_w, "mk"), (kept, ""), (ws, ""), (status, "")), row_mask)
+    if (kept is not None and kept.dtype is not torch.uint8) or ws.dtype is not torch.uint8 or (
+            status is not None and status.dtype is not torch.int32):
+        raise TypeError("kept and ws: expected uint8 buffers; status: int32")
     rc = load_library().a3po_linear_bwd(_ptr(x), _ptr(w), _ptr(row_mask), _ptr(kept), 0 if kept is None else kept.numel(),
                                         _ptr(grad_y), n, k, m, dt, activation, _ptr(grad_x), _ptr(grad_w), gdt,
                                         _ptr(grad_bias), int(bool(accumulate_grad_w)), _ptr(ws), ws.numel(), _ptr(status),
@@ -773,23 +782,35 @@ def a3po_sample(logits, u, token, ws, *, temperature=None, top_k=None, top_p=Non
     """One token per row of logits [N, V] (rows may lie apart) from given random numbers u in [0, 1); token -1: nothing to
     sample.  logp: of the whole softmax (the behaviour log-prob of the loss), kept_logp: among the tokens that the filters
     kept, n_kept of them.  temperature, top_p, min_p (fp32) and top_k (int32): one value per row, or None."""
-    dt = _dtype_code(logits)
     if logits.dim() != 2:
         raise ValueError("logits: expected [N, V]")
     n, v = logits.shape
-    if not logits.is_cuda or (v > 1 and logits.stride(1) != 1) or (n > 1 and logits.stride(0) < v):
-        raise TypeError("logits: expected rows of neighbouring elements on cuda")
-    _here(logits, u, token, ws, temperature, top_k, top_p, min_p, row_mask, logp, kept_logp, n_kept)
-    for t, ty, nm in ((u, torch.float32, "u"), (token, torch.int32, "token"), (temperature, torch.float32, "temperature"),
-                      (top_k, torch.int32, "top_k"), (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p"),
-                      (row_mask, torch.uint8, "row_mask"), (logp, torch.float32, "logp"),
-                      (kept_logp, torch.float32, "kept_logp"), (n_kept, torch.int32, "n_kept")):
+    ld, step = logits.stride()
+    device = logits.get_device()
+    fine = (device >= 0 and device == torch.cuda.current_device() and (step == 1 or v == 1) and (ld >= v or n <= 1)
+            and ws.dtype is torch.uint8 and ws.get_device() == device and ws.is_contiguous())
+    for t in (u, temperature, top_p, min_p, logp, kept_logp):
         if t is not None:
+            fine &= t.dtype is torch.float32 and t.get_device() == device and t.numel() == n and t.is_contiguous()
+    for t in (token, top_k, n_kept):
+        if t is not None:
+            fine &= t.dtype is torch.int32 and t.get_device() == device and t.numel() == n and t.is_contiguous()
+    if row_mask is not None:
+        fine &= (row_mask.dtype is torch.uint8 and row_mask.get_device() == device and row_mask.numel() == n
+                 and row_mask.is_contiguous())
+    dt = _dtype_code(logits)
+    if not fine:   # say what is wrong
+        if not logits.is_cuda or (v > 1 and step != 1) or (n > 1 and ld < v):
+            raise TypeError("logits: expected rows of neighbouring elements on cuda")
+        _here(logits, u, token, ws, temperature, top_k, top_p, min_p, row_mask, logp, kept_logp, n_kept)
+        for t, ty, nm in ((u, torch.float32, "u"), (token, torch.int32, "token"), (temperature, torch.float32, "temperature"),
+                          (top_k, torch.int32, "top_k"), (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p"),
+                          (row_mask, torch.uint8, "row_mask"), (logp, torch.float32, "logp"),
+                          (kept_logp, torch.float32, "kept_logp"), (n_kept, torch.int32, "n_kept")):
             _want(t, ty, nm)
-            if t.numel() != n:
-                raise ValueError(f"{nm}: expected one value per row")
-    _want(ws, torch.uint8, "ws")
-    rc = load_library().a3po_sample(_ptr(logits), logits.stride(0) if n > 1 else v, _ptr(row_mask), n, v, dt,
+        _want(ws, torch.uint8, "ws")
+        raise ValueError("expected one value per row")
+    rc = load_library().a3po_sample(_ptr(logits), ld if n > 1 else v, _ptr(row_mask), n, v, dt,
                                     _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(token),
                                     _ptr(logp), _ptr(kept_logp), _ptr(n_kept), _ptr(ws), ws.numel(), _stream(stream))
     _check("a3po_sample", rc)

@@ -2,7 +2,7 @@
 //
 //   first kernel   a warp per segment of 1,024 logits: its largest m_s and S_s = sum exp((l - m_s) / t)
 //   second kernel  a block per row: m = max m_s, W = sum S_s exp((m_s - m) / t); the segment in which the running sum passes
-//                  u W is read again, by one warp, which finds the token
+//                  u W is read again, and the token found in it
 //
 // Bound: the instructions of a weight (sample.cuh) for bf16 logits, HBM and those about alike for fp32.
 
@@ -32,17 +32,14 @@ __device__ __forceinline__ Vec<T> select(const Vec<T> (&v)[N], int i) {
 }
 
 template <typename T>
-#ifndef SB
-#define SB 4
-#endif
-__global__ void __launch_bounds__(kSumThreads, SB)
+__global__ void __launch_bounds__(kSumThreads)
 sample_sums_kernel(SampleArgs a, Segments out, long long items) {
   constexpr int VE = per_vec<T>(), kVecs = kSegment / VE / kWarp;
   __shared__ SharedTable<16> table;
   allow_next();
-  fill_table(table, threadIdx.x, kSumThreads);
-  __syncthreads();
-  // a warp takes neighbouring segments, so that what belongs to a row is looked up once per row
+  // A warp takes neighbouring segments, so that what belongs to a row is looked up once per row.  bf16: the next segment is on its
+  // way while one is worked on (fp32 segments take the registers that this needs).
+  constexpr bool kAhead = sizeof(T) == 2;
   const int lane = threadIdx.x % kWarp;
   const long long warps = static_cast<long long>(gridDim.x) * (kSumThreads / kWarp);
   const long long me = static_cast<long long>(blockIdx.x) * (kSumThreads / kWarp) + threadIdx.x / kWarp;
@@ -52,24 +49,13 @@ sample_sums_kernel(SampleArgs a, Segments out, long long items) {
   const T* l = nullptr;
   int head = 0;
   bool on = false;
-  Weights<16> w;
-  for (bool fresh = true; item < end; ++item, ++seg) {
-    if (seg == out.per_row) {
-      seg = 0;
-      ++row;
-      fresh = true;
-    }
-    if (fresh) {
-      fresh = false;
-      on = !a.row_mask || a.row_mask[row] != 0;
-      l = static_cast<const T*>(a.logits) + row * a.ld;
-      head = head_of(l);
-      bool greedy;
-      w.set_temperature(a.temp(row, greedy), table);
-    }
-    if (!on) continue;
+  auto enter = [&]() {   // a row
+    on = row < a.n && (!a.row_mask || a.row_mask[row] != 0);
+    l = static_cast<const T*>(a.logits) + row * a.ld;
+    head = head_of(l);
+  };
+  auto load = [&](Vec<T> (&v)[kVecs]) {
     const int first = seg * kSegment - head;
-    Vec<T> v[kVecs];
     if (first >= 0 && first + kSegment <= a.v) {   // the same for the warp
       const uint4* p = reinterpret_cast<const uint4*>(l + first) + lane;
 #pragma unroll
@@ -81,6 +67,43 @@ sample_sums_kernel(SampleArgs a, Segments out, long long items) {
 #pragma unroll
       for (int i = 0; i < kVecs; ++i) v[i] = load_vec(l, first + (i * kWarp + lane) * VE, a.v);
     }
+  };
+  Weights<16> w;
+  Vec<T> next[kAhead ? kVecs : 1];
+  if (item < end) {
+    enter();
+    if constexpr (kAhead) {
+      if (on) load(next);
+    }
+  }
+  fill_table(table, threadIdx.x, kSumThreads);
+  __syncthreads();
+  bool fresh = true;
+  while (item < end) {
+    if (fresh) {
+      bool greedy;
+      if (on) w.set_temperature(a.temp(row, greedy), table);
+    }
+    const int here = item;
+    const bool work = on;
+    Vec<T> v[kVecs];
+    if constexpr (kAhead) {
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i) v[i] = next[i];
+    } else {
+      if (work) load(v);
+    }
+    ++item;
+    fresh = ++seg == out.per_row;
+    if (fresh) {
+      seg = 0;
+      ++row;
+      enter();
+    }
+    if constexpr (kAhead) {
+      if (item < end && on) load(next);
+    }
+    if (!work) continue;
     float m, least;
     extremes(v, m, least);
     m = warp_max_any(m);
@@ -111,10 +134,10 @@ sample_sums_kernel(SampleArgs a, Segments out, long long items) {
       }
       sum = warp_sum(sum);
     }
-    if (lane == 0 && a.n_kept) out.count[item] = count;
+    if (lane == 0 && a.n_kept) out.count[here] = count;
     if (lane == 0) {
-      out.sum[item] = sum;
-      out.max[item] = m;
+      out.sum[here] = sum;
+      out.max[here] = m;
     }
   }
 }
@@ -148,9 +171,9 @@ __global__ void __launch_bounds__(kPickThreads)
 sample_pick_kernel(SampleArgs a, Segments in) {
   constexpr int VE = per_vec<T>();
   __shared__ SharedTable<1> table;
-  __shared__ double sh_scan[kPickThreads / kWarp], sh_target, sh_total;
+  __shared__ double sh_scan[kPickThreads / kWarp], sh_target;
   __shared__ float sh_max[kPickThreads / kWarp];
-  __shared__ int sh_seg, sh_first, sh_last, sh_count;
+  __shared__ int sh_seg, sh_first, sh_last, sh_count, sh_best[kPickThreads / kWarp];
   const int row = blockIdx.x, lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
   if (a.row_mask && a.row_mask[row] == 0) {
     if (threadIdx.x == 0) a.put(row, -1, 0.0, 0.0, 0);
@@ -229,79 +252,55 @@ sample_pick_kernel(SampleArgs a, Segments in) {
     sh_seg = seg;
     sh_target = (target - at) / factor(maxes[seg]);
   }
-  if (threadIdx.x == 0) sh_total = total;
   __syncthreads();
-  if (warp != 0) return;
+  // the segment again, in index order, 8 neighbours per thread
   const int seg = min(sh_seg, in.per_row - 1);
   const T* l = static_cast<const T*>(a.logits) + row * a.ld;
-  const int head = head_of(l);
-  const float seg_max = maxes[seg];
+  constexpr int kEach = kSegment / kPickThreads;
+  const int first = seg * kSegment - head_of(l) + static_cast<int>(threadIdx.x) * kEach;
   Weights<1> w;
   w.set_temperature(t, table);
-  w.set_max(seg_max);
-  double run = 0.0;
+  w.set_max(maxes[seg]);
+  float x[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach / VE; ++i) {
+    const Vec<T> v = load_vec(l, first + i * VE, a.v);
+#pragma unroll
+    for (int e = 0; e < VE; ++e) x[i * VE + e] = v.at(e);
+  }
+  double y[kEach], sum = 0.0, all;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    y[e] = greedy ? (x[e] == m ? 1.0 : 0.0) : w.template operator()<exact_diff<T>()>(x[e]);
+    sum += y[e];
+  }
+  double run;
+  block_scan(sum, sh_scan, run, all);
   const double want = greedy ? 0.0 : sh_target;
-  int token = -1;         // of this lane
+  // the first that passes the target; rounding may leave it past the segment's sum: then the last that has a weight
+  int pick = INT_MAX;
   float picked = 0.f;
-  int last = -1;          // the last element with a weight: rounding may leave the target past the segment's sum
-  float last_l = 0.f;
-  for (int i = 0; i < kSegment / VE / kWarp; ++i) {
-    const int first = seg * kSegment - head + (i * kWarp + lane) * VE;
-    const Vec<T> v = load_vec(l, first, a.v);
-    double x[VE], sum = 0.0;
 #pragma unroll
-    for (int e = 0; e < VE; ++e) {
-      const float le = v.at(e);
-      x[e] = greedy ? (le == m ? 1.0 : 0.0) : w.template operator()<exact_diff<T>()>(le);
-      sum += x[e];
-      if (x[e] > 0.0) {
-        last = first + e;
-        last_l = le;
-      }
+  for (int e = 0; e < kEach; ++e) {
+    run += y[e];
+    const int place = static_cast<int>(threadIdx.x) * kEach + e;
+    const int me = run > want ? place : 2 * kSegment - place;
+    if (y[e] > 0.0 && me < pick) {
+      pick = me;
+      picked = x[e];
     }
-    double inc = sum;
-#pragma unroll
-    for (int o = 1; o < kWarp; o <<= 1) {
-      const double y = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += y;
-    }
-    double prev = __shfl_up_sync(0xffffffffu, inc, 1);
-    prev = lane ? run + prev : run;
-    inc += run;
-    const unsigned over = __ballot_sync(0xffffffffu, sum > 0.0 && inc > want);
-    if (over) {
-      if (lane == __ffs(over) - 1) {
-        double at = prev;
-        token = last;        // of this vector, unless one before it passes the target
-        picked = last_l;
-#pragma unroll
-        for (int e = VE - 1; e >= 0; --e) {   // from the back: the first that passes is written last
-          double upto_e = at;
-#pragma unroll
-          for (int q = 0; q <= e; ++q) upto_e += x[q];
-          if (upto_e > want && x[e] > 0.0) {
-            token = first + e;
-            picked = v.at(e);
-          }
-        }
-      }
-      const int src = __ffs(over) - 1;
-      token = __shfl_sync(0xffffffffu, token, src);
-      picked = __shfl_sync(0xffffffffu, picked, src);
-      break;
-    }
-    run = __shfl_sync(0xffffffffu, inc, kWarp - 1);
   }
-  if (token < 0) {
-    const int top = __reduce_max_sync(0xffffffffu, last);
-    const unsigned who = __ballot_sync(0xffffffffu, last == top);
-    token = top;
-    picked = __shfl_sync(0xffffffffu, last_l, __ffs(who) - 1);
-  }
-  if (lane == 0) {
+  const int best = __reduce_min_sync(0xffffffffu, pick);
+  if (lane == 0) sh_best[warp] = best;
+  __syncthreads();
+  int chosen = INT_MAX;
+#pragma unroll
+  for (int i = 0; i < kPickThreads / kWarp; ++i) chosen = min(chosen, sh_best[i]);
+  if (pick == chosen && pick < INT_MAX) {   // one thread: places differ
+    const int place = pick < kSegment ? pick : 2 * kSegment - pick;
     const double z = picked == m ? 0.0 : (static_cast<double>(picked) - static_cast<double>(m)) * inv_t;
-    const double lp = z - log(sh_total);
-    a.put(row, token, lp, greedy ? 0.0 : lp, greedy ? 1 : sh_count);
+    const double lp = z - log(total);
+    a.put(row, first - static_cast<int>(threadIdx.x) * kEach + place, lp, greedy ? 0.0 : lp, greedy ? 1 : sh_count);
   }
 }
 
@@ -309,7 +308,9 @@ template <typename T>
 int stream_impl(const SampleArgs& a, const Segments& seg, cudaStream_t stream) {
   const int items = a.n * seg.per_row;
   constexpr int kWarps = kSumThreads / kWarp;
-  const int want = (items + kWarps - 1) / kWarps, most = sm_count() * 8;
+  // few segments go to as many SMs as there are
+  const int want = items < sm_count() * kWarps ? (items < sm_count() ? items : sm_count()) : (items + kWarps - 1) / kWarps;
+  const int most = sm_count() * 8;
   A3PO_LAUNCH(kKSample, stream, (sample_sums_kernel<T><<<want < most ? want : most, kSumThreads, 0, stream>>>(a, seg, static_cast<long long>(items))));
   A3PO_RETURN_IF(after_launch());
   A3PO_LAUNCH(kKSample, stream, (launch_early(sample_pick_kernel<T>, a.n, kPickThreads, 0, stream, 1, true, a, seg)));

@@ -3,6 +3,8 @@ tensor, with states in 32 or 8 bits and fp32 masters of bf16 weights.  The count
 so a step can be captured into a CUDA graph (after one uncaptured step) and replayed with another rate."""
 from __future__ import annotations
 
+import ctypes
+
 import torch
 
 from . import binding as b
@@ -82,7 +84,7 @@ class AdamW:
         self.beta1, self.beta2 = float(betas[0]), float(betas[1])
         self._ws = b.new_workspace(b.a3po_adamw_workspace_bytes(count), device)
         self._table = (b.A3poAdamWTensor * count)()
-        self._grads, self._grad_dt = [None] * count, b.A3PO_F32
+        self._grads, self._grad_dt, self._words, self._device = [None] * count, b.A3PO_F32, None, device.index
         at = lambda tensors, i: None if tensors is None else tensors[i].data_ptr()
         for i, w in enumerate(self.weights):
             self._table[i] = b.A3poAdamWTensor(w.data_ptr(), at(self.masters, i), None, at(self.m, i), at(self.v, i),
@@ -107,7 +109,20 @@ class AdamW:
             self._grad_dt = b._dtype_code(grads[0])
         for i, g in enumerate(grads):   # storage may have moved under a tensor that was seen before
             self._table[i].grad = g.data_ptr()
-            self._grads[i] = g
-        b.a3po_adamw_step(self._table, self._weight_dt, self._grad_dt, self.state_bits, self.lr, self.steps, self._ws,
-                          beta1=self.beta1, beta2=self.beta2, eps=self.eps, max_grad_norm=self.max_grad_norm,
-                          grad_norm=self.grad_norm, stream=stream)
+        if fresh:
+            self._grads = list(grads)
+        words = (self.lr, self.steps, self.grad_norm, self._ws)
+        if self._words is None or any(a is not c for a, c in zip(words, self._words)):
+            for t, dtype, name in ((self.lr, torch.float32, "lr"), (self.steps, torch.int64, "steps"),
+                                   (self.grad_norm, torch.float32, "grad_norm")):
+                b._want(t, dtype, name)
+                if t.numel() != 1:
+                    raise ValueError(f"{name}: expected one element")
+            self._words = words
+        if self._device != torch.cuda.current_device():
+            raise ValueError(f"expected the current device cuda:{self._device}, got cuda:{torch.cuda.current_device()}")
+        rc = b.load_library().a3po_adamw_step(
+            ctypes.addressof(self._table), len(self._table), self._weight_dt, self._grad_dt, self.state_bits, self.beta1, self.beta2,
+            self.eps, self.max_grad_norm, self.lr.data_ptr(), self.steps.data_ptr(), self.grad_norm.data_ptr(),
+            self._ws.data_ptr(), self._ws.numel(), b._stream(stream))
+        b._check("a3po_adamw_step", rc)
