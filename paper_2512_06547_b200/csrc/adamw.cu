@@ -207,12 +207,11 @@ step_numbers_kernel(const double* sums, int count, double b1, double b2, float m
 }
 
 // ------------------------------------------------------------------------------------ update
-// sqrt(x) + eps to two steps.  The fast root takes x below 2^-126 for 0, which is seen beside a tiny eps only.
-__device__ __forceinline__ float root_plus(float x, float eps) {
-  if (eps < 1e-12f) return __fsqrt_rn(x) + eps;
+// sqrt(x) to two steps; x below 2^-126 counts as 0, which is seen beside a tiny eps only.
+__device__ __forceinline__ float fast_root(float x) {
   float y;
   asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y + eps;
+  return y;
 }
 __host__ __device__ constexpr double code_value(int c) {
   return c < 8 ? static_cast<double>(c) : static_cast<double>(static_cast<long long>(8 + c % 8) << (c / 8 - 1));
@@ -329,14 +328,17 @@ adamw_kernel(const __grid_constant__ Table<CAP> t, const Numbers* numbers, doubl
     const int left = static_cast<int>(e.n - at < kBlock ? e.n - at : kBlock);
     const bool wide = e.wide && left == kBlock;
     float w[8], g[8], m[8], v[8];
-    if (sizeof(W) == 2 && e.master) load8(static_cast<const float*>(e.master) + at, lane, left, wide, w);
-    else load8(static_cast<const W*>(e.weight) + at, lane, left, wide, w);
+    auto load_weights = [&]() {
+      if (sizeof(W) == 2 && e.master) load8(static_cast<const float*>(e.master) + at, lane, left, wide, w);
+      else load8(static_cast<const W*>(e.weight) + at, lane, left, wide, w);
+    };
     load8(static_cast<const G*>(e.grad) + at, lane, left, wide, g);
     if constexpr (BITS == 32) {
       float* pm = static_cast<float*>(e.m) + at;
       float* pv = static_cast<float*>(e.v) + at;
       load8(pm, lane, left, wide, m);
       load8(pv, lane, left, wide, v);
+      load_weights();
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const float x = g[k] * s.scale;
@@ -353,13 +355,18 @@ adamw_kernel(const __grid_constant__ Table<CAP> t, const Numbers* numbers, doubl
       load8(pv, lane, left, wide, cv);
       const float old_ms = *ms, old_vs = *vs;
       new_states<true>(pm, ms, cm, old_ms, q, b1, s.g1, lane, left, wide, g, m);
+      load_weights();   // on their way during the second moments; earlier they would take registers from the first
       new_states<false>(pv, vs, cv, old_vs, q + 256, b2, s.g2, lane, left, wide, g, v);
     }
+    if (eps < 1e-12f) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float step = m[k] * s.inv_bc1 * fast_rcp(root_plus(v[k] * s.inv_bc2, eps));
-      w[k] = fmaf(-s.lr, fmaf(e.decay, w[k], step), w[k]);
+      for (int k = 0; k < 8; ++k) m[k] = m[k] * s.inv_bc1 / (__fsqrt_rn(v[k] * s.inv_bc2) + eps);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) m[k] = m[k] * s.inv_bc1 * fast_rcp(fast_root(v[k] * s.inv_bc2) + eps);
     }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = fmaf(-s.lr, fmaf(e.decay, w[k], m[k]), w[k]);
     if (sizeof(W) == 2 && e.master) store8(e.master + at, lane, left, wide, w);
     store8(static_cast<W*>(e.weight) + at, lane, left, wide, w);
   }

@@ -13,6 +13,7 @@ namespace {
 
 constexpr int kSegment = 1024;   // elements, counted from the aligned start of a row
 constexpr int kSumThreads = 256, kPickThreads = 128;
+constexpr int kSumBlocks = 3;    // per SM, all at once: every warp has the same share of the segments
 
 struct Segments {   // per row and segment, of rows that take part
   double* sum;
@@ -32,7 +33,7 @@ __device__ __forceinline__ Vec<T> select(const Vec<T> (&v)[N], int i) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kSumThreads)
+__global__ void __launch_bounds__(kSumThreads, kSumBlocks)
 sample_sums_kernel(SampleArgs a, Segments out, long long items) {
   constexpr int VE = per_vec<T>(), kVecs = kSegment / VE / kWarp;
   __shared__ SharedTable<16> table;
@@ -310,7 +311,7 @@ int stream_impl(const SampleArgs& a, const Segments& seg, cudaStream_t stream) {
   constexpr int kWarps = kSumThreads / kWarp;
   // few segments go to as many SMs as there are
   const int want = items < sm_count() * kWarps ? (items < sm_count() ? items : sm_count()) : (items + kWarps - 1) / kWarps;
-  const int most = sm_count() * 8;
+  const int most = sm_count() * kSumBlocks;
   A3PO_LAUNCH(kKSample, stream, (sample_sums_kernel<T><<<want < most ? want : most, kSumThreads, 0, stream>>>(a, seg, static_cast<long long>(items))));
   A3PO_RETURN_IF(after_launch());
   A3PO_LAUNCH(kKSample, stream, (launch_early(sample_pick_kernel<T>, a.n, kPickThreads, 0, stream, 1, true, a, seg)));
