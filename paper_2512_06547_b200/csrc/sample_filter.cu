@@ -451,11 +451,14 @@ struct Ask {
   double min_bound;   // the smallest logit that min-p keeps
 };
 
-// Steps of distance to the largest logit: a 64th of the temperature each, a 128th for top-p alone (whose bound is the sharper the
+// Steps of distance to the largest logit: a 32nd of the temperature each, a 128th for top-p alone (whose bound is the sharper the
 // finer they are; 99 % of the mass is out of its reach).
+// Rounded to the nearest step by the last bit of a sum with 2^23, whose bits are then kZeroStep + the step; what is beyond 2^24
+// steps, infinite or NaN has larger ones.
+constexpr u32 kZeroStep = 0x4b000000u;
 struct Steps {
   float max, scale;
-  __device__ __forceinline__ float distance(float l) const { return __fmul_rn(__fsub_rn(max, l), scale); }
+  __device__ __forceinline__ u32 at(float l) const { return __float_as_uint(fmaf(__fsub_rn(max, l), scale, 8388608.f)) - kZeroStep; }
 };
 
 // Among m entries and what they count for: the last one, in rank order, that is kept, when the entries before them count `before`
@@ -539,7 +542,7 @@ __device__ __forceinline__ void finish_alone(Row<T>& row, const SampleArgs& a, i
           bin[i] = -1;
           if (s0 + i < n && list[s0 + i] <= last) {
             f[i] = weigh ? fixed_of(weight(list[s0 + i])) : 1;
-            bin[i] = static_cast<int>(steps.distance(logit_of(list[s0 + i])));
+            bin[i] = static_cast<int>(steps.at(logit_of(list[s0 + i])));
             atomicAdd(&bins[bin[i]], f[i]);   // whole numbers: in any order
           }
         }
@@ -630,7 +633,7 @@ __device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a,
   constexpr int VE = per_vec<T>();
   Shared& sh = row.sh;
   const bool mass_alone = ask.by_mass && !ask.by_count;
-  const float per_t = mass_alone ? 128.f : 64.f;
+  const float per_t = mass_alone ? 128.f : 32.f;
   const Steps steps{w.max, per_t / t};
   if (w.at_inf || !(steps.scale < 1e30f)) {
     __syncthreads();   // the row's total is there (see the kernel)
@@ -638,8 +641,8 @@ __device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a,
   }
   // ---- counts, to the first block
   row.each([&](float l, int) {
-    const float x = steps.distance(l);
-    if (x < static_cast<float>(kBins)) atomicAdd(&sh.lo[static_cast<int>(x)], 1u);   // false for NaN
+    const u32 x = steps.at(l);
+    if (x < kBins) atomicAdd(&sh.lo[x], 1u);
   });
   __syncthreads();   // and the row's total is there
   const double total = sh.total;
@@ -666,7 +669,7 @@ __device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a,
     for (int i = 0; i < kMost; ++i) {
       count += got[i];
       if (mass_alone) {
-        least[i] = expf(static_cast<float>(first + i + 1) * (-1.f / per_t));
+        least[i] = expf((static_cast<float>(first + i) + 0.5f) * (-1.f / per_t));
         mass += static_cast<double>(got[i]) * static_cast<double>(least[i]);
       }
     }
@@ -703,7 +706,7 @@ __device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a,
   const u64 best = said[0], low = said_range[0];
   if (best == ~0ull) return Way::kKeys;
   const int n = static_cast<int>(best & 0xffffffffu), end = static_cast<int>(best >> 32) + 1;
-  const float limit = static_cast<float>(end);
+  const u32 limit = static_cast<u32>(end);
   const int region = kList / row.cluster;   // of the list, for each block
 
   if (n <= kList) {
@@ -712,7 +715,7 @@ __device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a,
     for (int j = row.v0 + row.lane; j < row.v1; j += kWarp) {
       const Vec<T> v = row.piece(j);
 #pragma unroll
-      for (int e = 0; e < VE; ++e) c += steps.distance(v.at(e)) < limit ? 1 : 0;
+      for (int e = 0; e < VE; ++e) c += steps.at(v.at(e)) < limit ? 1 : 0;
     }
     c = __reduce_add_sync(0xffffffffu, c);
     if (row.lane == 0) sh.warp_count[row.warp] = c;
@@ -732,7 +735,7 @@ __device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a,
         if (j < row.v1) {
           v = row.piece(j);
 #pragma unroll
-          for (int e = 0; e < VE; ++e) in |= steps.distance(v.at(e)) < limit ? 1u << e : 0u;
+          for (int e = 0; e < VE; ++e) in |= steps.at(v.at(e)) < limit ? 1u << e : 0u;
         }
         if (!__any_sync(0xffffffffu, in != 0)) continue;
         int inc = __popc(in);
@@ -786,13 +789,12 @@ __device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a,
     __syncthreads();
     for (int i = threadIdx.x; i < range; i += kThreads) own[i] = 0;
     __syncthreads();
-    const float sure = static_cast<float>(step0);
+    const u32 sure = static_cast<u32>(step0);
     row.each([&](float l, int) {
-      const float x = steps.distance(l);
-      if (x >= sure && x < limit)
-        atomicAdd(&own[static_cast<int>(x) - step0], fixed_of(w.template operator()<exact_diff<T>()>(l)));
+      const u32 x = steps.at(l) - sure;
+      if (x < static_cast<u32>(range)) atomicAdd(&own[x], fixed_of(w.template operator()<exact_diff<T>()>(l)));
     });
-    double sum = row.weigh(w, [&](float l, int) { return steps.distance(l) < sure; });
+    double sum = row.weigh(w, [&](float l, int) { return steps.at(l) < sure; });
     sum = row.block_sum(row.lane == 0 ? sum : 0.0);
     u64* sums = row.tell(static_cast<u64>(__double_as_longlong(sum)));
     row.sync();
@@ -827,28 +829,11 @@ __device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a,
   u32* taken = reinterpret_cast<u32*>(&sh.warp_count[0]);
   if (threadIdx.x == 0) *taken = 0;
   row.sync();   // nobody reads what the list takes the place of
-  const float from = static_cast<float>(step), to = static_cast<float>(step + 1);
-  auto on_step = [&](float l) {
-    const float x = steps.distance(l);
-    return x >= from && x < to;
-  };
-  int mine = 0;
-  row.each([&](float l, int) { mine += on_step(l) ? 1 : 0; });
-  int inc = mine;
-#pragma unroll
-  for (int o = 1; o < kWarp; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, inc, o);
-    if (row.lane >= o) inc += y;
-  }
-  u32 at = 0;
-  if (row.lane == kWarp - 1 && inc > 0) at = take_from_remote(taken, 0, static_cast<u32>(inc));
-  at = __shfl_sync(0xffffffffu, at, kWarp - 1) + static_cast<u32>(inc - mine);
-  if (mine > 0)
-    row.each([&](float l, int i) {
-      if (!on_step(l)) return;
-      if (at < kList) store_remote(&sh.list[at], 0, entry_of(l, i));
-      ++at;
-    });
+  row.each([&](float l, int i) {   // a hundred or so of the row
+    if (steps.at(l) != static_cast<u32>(step)) return;
+    const u32 at = take_from_remote(taken, 0, 1);
+    if (at < kList) store_remote(&sh.list[at], 0, entry_of(l, i));
+  });
   row.sync();
   if (row.rank == 0) {
     const int m = static_cast<int>(*taken);
