@@ -5,6 +5,7 @@
 //   how many logits lie at which distance from the largest, in 2,048 steps, added up in the first block.  The counts bound what
 //     top-k or top-p can keep: the first step that has, with all above it, k tokens, or the share p of the mass even if every
 //     token of a step has the least weight of the step (min-p's bound is known beforehand)
+//     The lanes' largest logits, a thousandth of all, are counted first; they bound peaked rows and small k as well
 //   few candidates (up to 2,048): the first block gets them in index order and finishes alone
 //   more: the exact mass of the steps in which top-p's border may lie, the tokens of the one step that holds the border, which the
 //     first block puts in order, and another pass over the kept ones
@@ -626,28 +627,17 @@ __device__ __forceinline__ void finish_alone(Row<T>& row, const SampleArgs& a, i
 
 enum class Way { kDone, kBorder, kKeys };   // sampled; the border is known; it is not
 
-// A row by steps.  kBorder: `border` is the last entry, in rank order, that top-k and top-p keep.  The same for the whole cluster.
-template <typename T, class W>
-__device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a, int row_id, const W& w, float t, const Ask& ask,
-                                               u64* scratch, u64& border) {
-  constexpr int VE = per_vec<T>();
+// How far the candidates reach, from counts by step (sh.lo of all blocks): the first step that has, with all above it, enough of
+// them, and the first in which top-k's or top-p's border may lie; each with the count up to it (before it), ~0 where there is none.
+struct Reach {
+  u64 end, low;
+};
+template <typename T>
+__device__ __forceinline__ Reach reach_of(Row<T>& row, const Ask& ask, double total, float per_t) {
   Shared& sh = row.sh;
   const bool mass_alone = ask.by_mass && !ask.by_count;
-  const float per_t = mass_alone ? 128.f : 32.f;
-  const Steps steps{w.max, per_t / t};
-  if (w.at_inf || !(steps.scale < 1e30f)) {
-    __syncthreads();   // the row's total is there (see the kernel)
-    return Way::kKeys;
-  }
-  // ---- counts, to the first block
-  row.each([&](float l, int) {
-    const u32 x = steps.at(l);
-    if (x < kBins) atomicAdd(&sh.lo[x], 1u);
-  });
-  __syncthreads();   // and the row's total is there
-  const double total = sh.total;
-  u64* said = row.next_slot();        // step, candidates
-  u64* said_range = row.next_slot();  // first step in which the border may lie, tokens before it
+  u64* said = row.next_slot();
+  u64* said_low = row.next_slot();
   row.sync();
   if (row.rank == 0) {
     constexpr int kMost = kBins / kThreads;
@@ -677,7 +667,7 @@ __device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a,
     double cum_mass = mass_alone ? row.scan(mass, all_mass) : 0.0;
     const double share = static_cast<double>(fmaxf(ask.top_p, 0.f)) * total;
     const double enough = share * (1.0 + 1e-5);   // expf and the distances are not exact
-    // the same mass with the weights at the near ends, which is 1 / far_near as much, is not enough
+    // with the weights at the near ends, which are this much larger, the mass is not enough either
     const double too_little = share * static_cast<double>(expf(-1.f / per_t)) * (1.0 - 1e-5);
     int min_bin = INT_MAX;   // the first step that lies below what min-p keeps
     if (ask.by_min && !ask.by_mass) {
@@ -699,81 +689,122 @@ __device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a,
     low = row.block_min(low);
     if (threadIdx.x == 0) {
       row.say(said, best);
-      row.say(said_range, low);
+      row.say(said_low, low);
     }
   }
   row.sync();
-  const u64 best = said[0], low = said_range[0];
-  if (best == ~0ull) return Way::kKeys;
-  const int n = static_cast<int>(best & 0xffffffffu), end = static_cast<int>(best >> 32) + 1;
-  const u32 limit = static_cast<u32>(end);
-  const int region = kList / row.cluster;   // of the list, for each block
+  return Reach{said[0], said_low[0]};
+}
 
-  if (n <= kList) {
-    // ---- candidates, in index order, to the first block
-    int c = 0;
-    for (int j = row.v0 + row.lane; j < row.v1; j += kWarp) {
-      const Vec<T> v = row.piece(j);
+// The tokens of the steps below `end`, in index order, to the first block, which then finishes alone: true; false: they are too
+// many (of one block).
+template <typename T, class W>
+__device__ __forceinline__ bool gather_and_finish(Row<T>& row, const SampleArgs& a, int row_id, const W& w, const Steps& steps, float t,
+                                                  double total, const Ask& ask, u32 end, u64* scratch) {
+  constexpr int VE = per_vec<T>();
+  Shared& sh = row.sh;
+  const int region = kList / row.cluster;   // of the list, for each block
+  int c = 0;
+  for (int j = row.v0 + row.lane; j < row.v1; j += kWarp) {
+    const Vec<T> v = row.piece(j);
 #pragma unroll
-      for (int e = 0; e < VE; ++e) c += steps.at(v.at(e)) < limit ? 1 : 0;
-    }
-    c = __reduce_add_sync(0xffffffffu, c);
-    if (row.lane == 0) sh.warp_count[row.warp] = c;
-    __syncthreads();
-    int block = 0, at = 0;
+    for (int e = 0; e < VE; ++e) c += steps.at(v.at(e)) < end ? 1 : 0;
+  }
+  c = __reduce_add_sync(0xffffffffu, c);
+  if (row.lane == 0) sh.warp_count[row.warp] = c;
+  __syncthreads();
+  int block = 0, at = 0;
 #pragma unroll
-    for (int i = 0; i < kWarps; ++i) {
-      if (i == row.warp) at = block;
-      block += sh.warp_count[i];
-    }
-    const u64* blocks = row.tell(static_cast<u64>(block));
-    if (c > 0) {
-      for (int j0 = row.v0; j0 < row.v1; j0 += kWarp) {
-        const int j = j0 + row.lane;
-        u32 in = 0;
-        Vec<T> v;
-        if (j < row.v1) {
-          v = row.piece(j);
+  for (int i = 0; i < kWarps; ++i) {
+    if (i == row.warp) at = block;
+    block += sh.warp_count[i];
+  }
+  const u64* blocks = row.tell(static_cast<u64>(block));
+  if (c > 0 && block <= region) {
+    for (int j0 = row.v0; j0 < row.v1; j0 += kWarp) {
+      const int j = j0 + row.lane;
+      u32 in = 0;
+      Vec<T> v;
+      if (j < row.v1) {
+        v = row.piece(j);
 #pragma unroll
-          for (int e = 0; e < VE; ++e) in |= steps.at(v.at(e)) < limit ? 1u << e : 0u;
-        }
-        if (!__any_sync(0xffffffffu, in != 0)) continue;
-        int inc = __popc(in);
+        for (int e = 0; e < VE; ++e) in |= steps.at(v.at(e)) < end ? 1u << e : 0u;
+      }
+      if (!__any_sync(0xffffffffu, in != 0)) continue;
+      int inc = __popc(in);
 #pragma unroll
-        for (int o = 1; o < kWarp; o <<= 1) {
-          const int y = __shfl_up_sync(0xffffffffu, inc, o);
-          if (row.lane >= o) inc += y;
-        }
-        int to = at + inc - __popc(in);
-        at += __shfl_sync(0xffffffffu, inc, kWarp - 1);
-        if (in) {
+      for (int o = 1; o < kWarp; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (row.lane >= o) inc += y;
+      }
+      int to = at + inc - __popc(in);
+      at += __shfl_sync(0xffffffffu, inc, kWarp - 1);
+      if (in) {
 #pragma unroll
-          for (int e = 0; e < VE; ++e) {
-            if (in >> e & 1u) {
-              if (to < region) store_remote(&sh.list[row.rank * region + to], 0, entry_of(v.at(e), row.base + j * VE + e));
-              ++to;
-            }
+        for (int e = 0; e < VE; ++e) {
+          if (in >> e & 1u) {
+            store_remote(&sh.list[row.rank * region + to], 0, entry_of(v.at(e), row.base + j * VE + e));
+            ++to;
           }
         }
       }
     }
-    row.sync();
-    bool fits = true;
-    for (int r = 0; r < row.cluster; ++r) fits &= blocks[r] <= static_cast<u64>(region);
-    if (fits) {
-      if (row.rank != 0) return Way::kDone;
-      // one behind another; the step's sums and candidates then take the list's place and what follows it
-      for (int i = threadIdx.x; i < n; i += kThreads) {
-        int from = i, r = 0;
-        while (from >= static_cast<int>(blocks[r])) from -= static_cast<int>(blocks[r++]);
-        scratch[i] = sh.list[r * region + from];
-      }
-      __syncthreads();
-      finish_alone(row, a, row_id, w, steps, t, total, ask, scratch, n, sh.list, scratch + kList);
-      return Way::kDone;
-    }
-    return Way::kKeys;   // too many of them in one block, whose histograms may be gone
   }
+  row.sync();
+  bool fits = true;
+  int n = 0;
+  for (int r = 0; r < row.cluster; ++r) {
+    fits &= blocks[r] <= static_cast<u64>(region);
+    n += static_cast<int>(blocks[r]);
+  }
+  if (!fits) return false;
+  if (row.rank != 0) return true;
+  // one behind another; the step's sums and candidates then take the list's place and what follows it
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    int from = i, r = 0;
+    while (from >= static_cast<int>(blocks[r])) from -= static_cast<int>(blocks[r++]);
+    scratch[i] = sh.list[r * region + from];
+  }
+  __syncthreads();
+  finish_alone(row, a, row_id, w, steps, t, total, ask, scratch, n, sh.list, scratch + kList);
+  return true;
+}
+
+// A row by steps.  kBorder: `border` is the last entry, in rank order, that top-k and top-p keep.  The same for the whole cluster.
+template <typename T, class W>
+__device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a, int row_id, const W& w, float t, float lane_top,
+                                               const Ask& ask, u64* scratch, u64& border) {
+  Shared& sh = row.sh;
+  const bool mass_alone = ask.by_mass && !ask.by_count;
+  const float per_t = mass_alone ? 128.f : 32.f;
+  const Steps steps{w.max, per_t / t};
+  const bool usable = !w.at_inf && steps.scale < 1e30f;
+  // ---- the lanes' largest logits alone: k of them, or the share of the mass, bound the candidates too, and are counted in no time.
+  // Peaked rows and small k end here.
+  const u32 x = steps.at(lane_top);
+  if (usable && x < kBins) atomicAdd(&sh.lo[x], 1u);
+  __syncthreads();   // and the row's total is there
+  if (!usable) return Way::kKeys;
+  const double total = sh.total;
+  const Reach near = reach_of(row, ask, total, per_t);
+  if (near.end != ~0ull &&
+      gather_and_finish(row, a, row_id, w, steps, t, total, ask, static_cast<u32>(near.end >> 32) + 1u, scratch))
+    return Way::kDone;
+  // ---- all logits
+  __syncthreads();
+  for (int i = threadIdx.x; i < kBins; i += kThreads) sh.lo[i] = 0;
+  __syncthreads();
+  row.each([&](float l, int) {
+    const u32 b = steps.at(l);
+    if (b < kBins) atomicAdd(&sh.lo[b], 1u);
+  });
+  const Reach all = reach_of(row, ask, total, per_t);
+  const u64 best = all.end, low = all.low;
+  if (best == ~0ull) return Way::kKeys;
+  const int end = static_cast<int>(best >> 32) + 1;
+  const u32 limit = static_cast<u32>(end);
+  if ((best & 0xffffffffu) <= kList)
+    return gather_and_finish(row, a, row_id, w, steps, t, total, ask, limit, scratch) ? Way::kDone : Way::kKeys;
   if ((ask.by_count && ask.by_mass) || low == ~0ull) return Way::kKeys;
 
   // ---- the step that holds the border, and what lies before it
@@ -883,7 +914,8 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
   row.v0 = min(row.warp * stretch, row.vecs);
   row.v1 = min(row.v0 + stretch, row.vecs);
   constexpr int kAtOnce = 4;
-  u32 top = key_of(-INFINITY);
+  float lane_top = -INFINITY;          // the largest of this lane's logits
+  u32 lane_pair = 0xff80ff80u;
   bool table = false;
   for (int j0 = row.v0 + row.lane; ; j0 += kWarp * kAtOnce) {
     Vec<T> v[kAtOnce];
@@ -903,12 +935,16 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
       const int j = j0 + i * kWarp;
       if (j >= row.v1) continue;
 #pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        const float x = __fadd_rn(fmaxf(v[i].at(e), -INFINITY), 0.f);
-        top = max(top, key_of(x));
-        const u32 b = __float_as_uint(x);
-        if (sizeof(T) == 4) v[i].w[e] = b;
-        else v[i].w[e / 2] = e & 1 ? (v[i].w[e / 2] & 0xffffu) | (b & 0xffff0000u) : (v[i].w[e / 2] & 0xffff0000u) | b >> 16;
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (sizeof(T) == 4) {
+          const float x = __fadd_rn(fmaxf(__uint_as_float(v[i].w[e]), -INFINITY), 0.f);
+          v[i].w[e] = __float_as_uint(x);
+          lane_top = fmaxf(lane_top, x);
+        } else {
+          asm("max.bf16x2 %0, %0, %1;" : "+r"(v[i].w[e]) : "r"(0xff80ff80u));   // passes over NaN
+          asm("add.rn.bf16x2 %0, %0, %1;" : "+r"(v[i].w[e]) : "r"(0u));
+          asm("max.bf16x2 %0, %0, %1;" : "+r"(lane_pair) : "r"(v[i].w[e]));
+        }
       }
       data[j] = make_uint4(v[i].w[0], v[i].w[1], v[i].w[2], v[i].w[3]);   // a warp reads its own stretch alone
     }
@@ -922,7 +958,8 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
   w.set_temperature(t, sh.table);
   constexpr bool kExact = exact_diff<T>();
   auto weight = [&](float x) { return w.template operator()<kExact>(x); };
-  const float own_max = of_key(__reduce_max_sync(0xffffffffu, top));
+  if (sizeof(T) == 2) lane_top = fmaxf(__uint_as_float(lane_pair << 16), __uint_as_float(lane_pair & 0xffff0000u));
+  const float own_max = of_key(__reduce_max_sync(0xffffffffu, key_of(lane_top)));
   w.set_max(own_max);
   {
     double s = 0.0;
@@ -1013,7 +1050,7 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
   bool many = false;   // more than a few thousand are kept, as far as is known
   if (ask.by_count || ask.by_mass || ask.by_min) {
     u64 border = 0;
-    const Way way = sample_by_steps(row, a, row_id, w, t, ask, reinterpret_cast<u64*>(data), border);
+    const Way way = sample_by_steps(row, a, row_id, w, t, lane_top, ask, reinterpret_cast<u64*>(data), border);
     if (way == Way::kDone) return;
     const double total = sh.total;
     if (way == Way::kBorder) {
