@@ -299,16 +299,163 @@ __device__ __forceinline__ void new_states(uint8_t* codes, float* scale, uint32_
   if (lane == 0) *scale = now;
 }
 
-template <typename W, typename G, int BITS, int CAP>
+// w' from the new moments (m is overwritten).
+__device__ __forceinline__ void apply(float (&w)[8], float (&m)[8], const float (&v)[8], const Numbers& s, float decay, float eps) {
+  if (eps < 1e-12f) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m[k] = m[k] * s.inv_bc1 / (__fsqrt_rn(v[k] * s.inv_bc2) + eps);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m[k] = m[k] * s.inv_bc1 * fast_rcp(fast_root(v[k] * s.inv_bc2) + eps);
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) w[k] = fmaf(-s.lr, fmaf(decay, w[k], m[k]), w[k]);
+}
+
+// A lane's own elements of the block that comes next, on their way into shared memory while a block is worked on: two blocks of
+// the widest types a warp, filled and read by the same lane (no barrier).
+template <typename G>
+struct Ring {
+  static constexpr int kW = 0, kG = 1024, kM = kG + kBlock * static_cast<int>(sizeof(G)), kV = kM + kBlock, kStage = kV + kBlock;
+  static constexpr int kBytes = kWarps * 2 * kStage;
+  uint32_t at;   // this warp's first stage
+  int lane;
+  template <int BYTES>
+  __device__ __forceinline__ void copy(uint32_t to, const void* p) const {
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(p) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(p), "n"(BYTES) : "memory");
+  }
+  // four elements of `SIZE` bytes at 4 lane, and at 128 + 4 lane
+  template <int SIZE>
+  __device__ __forceinline__ void copy8(uint32_t to, const void* p) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      copy<4 * SIZE>(to + (h * 32 + lane) * 4 * SIZE, static_cast<const char*>(p) + (h * 32 + lane) * 4 * SIZE);
+  }
+  __device__ __forceinline__ uint32_t stage(int s) const { return at + s * kStage; }
+  template <typename T>
+  __device__ __forceinline__ void read8(uint32_t from, float (&x)[8]) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t a = from + (h * 32 + lane) * 4 * static_cast<uint32_t>(sizeof(T));
+      if constexpr (sizeof(T) == 4) {
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(x[h * 4]), "=f"(x[h * 4 + 1]), "=f"(x[h * 4 + 2]), "=f"(x[h * 4 + 3]) : "r"(a) : "memory");
+      } else {
+        uint32_t u, v;
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(u), "=r"(v) : "r"(a) : "memory");
+        x[h * 4] = __uint_as_float(u << 16); x[h * 4 + 1] = __uint_as_float(u & 0xffff0000u);
+        x[h * 4 + 2] = __uint_as_float(v << 16); x[h * 4 + 3] = __uint_as_float(v & 0xffff0000u);
+      }
+    }
+  }
+  __device__ __forceinline__ void read8(uint32_t from, uint32_t (&c)[2]) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(c[h]) : "r"(from + (h * 32 + lane) * 4) : "memory");
+  }
+};
+
+// Where a warp's block of 256 lies.
+struct Place {
+  int entry;
+  long long at;
+  int left;     // elements, at most 256; 0: none
+  bool wide;
+};
+template <int CAP>
+__device__ __forceinline__ Place place_of(const Table<CAP>& t, int chunk, int end, int entry, int warp) {
+  Place p{entry, 0, 0, false};
+  if (chunk >= end) return p;
+  while (chunk >= t.first[p.entry + 1]) ++p.entry;
+  const Entry& e = t.e[p.entry];
+  p.at = static_cast<long long>(chunk - t.first[p.entry]) * kChunk + warp * kBlock;
+  if (p.at < e.n) p.left = static_cast<int>(e.n - p.at < kBlock ? e.n - p.at : kBlock);
+  p.wide = e.wide && p.left == kBlock;
+  return p;
+}
+
+// States of 8 bits.  18 bytes an element with fp32 gradients and masters beside bf16 weights.
+template <typename W, typename G, int CAP>
+__global__ void __launch_bounds__(kThreads, 4)
+adamw_8bit_kernel(const __grid_constant__ Table<CAP> t, const Numbers* numbers, double b1, double b2, float eps) {
+  __shared__ double q[512];   // values of the codes, first moment (with the sign) and second
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int c = threadIdx.x;
+  q[c] = c < 128 ? code_value(c) : -code_value(c - 128);
+  q[256 + c] = code_value(c);
+  __syncthreads();
+  wait_for_previous();
+  allow_next();
+  const Numbers s = *numbers;
+  if (s.skip) return;   // gradients that are not finite: nothing changes
+  const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
+  using R = Ring<G>;
+  R ring;
+  ring.at = static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + warp * 2 * R::kStage;
+  ring.lane = lane;
+  const int chunks = t.first[t.count];
+  int chunk = static_cast<int>(static_cast<long long>(chunks) * blockIdx.x / gridDim.x);
+  const int end = static_cast<int>(static_cast<long long>(chunks) * (blockIdx.x + 1) / gridDim.x);
+  float next_ms = 0.f, next_vs = 0.f;   // the scales come with the block
+  auto start = [&](const Place& p, int stage) {
+    if (p.left > 0) {
+      const Entry& e = t.e[p.entry];
+      next_ms = e.m_scale[p.at / kBlock];
+      next_vs = e.v_scale[p.at / kBlock];
+      if (p.wide) {
+        const uint32_t to = ring.stage(stage);
+        ring.template copy8<sizeof(G)>(to + R::kG, static_cast<const G*>(e.grad) + p.at);
+        ring.template copy8<1>(to + R::kM, static_cast<const uint8_t*>(e.m) + p.at);
+        ring.template copy8<1>(to + R::kV, static_cast<const uint8_t*>(e.v) + p.at);
+        if (sizeof(W) == 2 && e.master) ring.template copy8<4>(to + R::kW, e.master + p.at);
+        else ring.template copy8<sizeof(W)>(to + R::kW, static_cast<const W*>(e.weight) + p.at);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  Place next = place_of(t, chunk, end, chunk < end ? entry_of(t, chunk) : 0, warp);
+  start(next, 0);
+  for (int stage = 0; chunk < end; ++chunk, stage ^= 1) {
+    const Place p = next;
+    const float old_ms = next_ms, old_vs = next_vs;
+    next = place_of(t, chunk + 1, end, p.entry, warp);
+    start(next, stage ^ 1);
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    if (p.left == 0) continue;   // the same for the warp
+    const Entry& e = t.e[p.entry];
+    const uint32_t from = ring.stage(stage);
+    uint8_t *pm = static_cast<uint8_t*>(e.m) + p.at, *pv = static_cast<uint8_t*>(e.v) + p.at;
+    float *ms = e.m_scale + p.at / kBlock, *vs = e.v_scale + p.at / kBlock;
+    const bool master = sizeof(W) == 2 && e.master;
+    float w[8], g[8], m[8], v[8];
+    uint32_t cm[2], cv[2];
+    if (p.wide) {
+      ring.template read8<G>(from + R::kG, g);
+      ring.read8(from + R::kM, cm);
+    } else {
+      load8(static_cast<const G*>(e.grad) + p.at, lane, p.left, false, g);
+      load8(pm, lane, p.left, false, cm);
+    }
+    new_states<true>(pm, ms, cm, old_ms, q, b1, s.g1, lane, p.left, p.wide, g, m);
+    if (p.wide) ring.read8(from + R::kV, cv);
+    else load8(pv, lane, p.left, false, cv);
+    new_states<false>(pv, vs, cv, old_vs, q + 256, b2, s.g2, lane, p.left, p.wide, g, v);
+    if (p.wide) {
+      if (master) ring.template read8<float>(from + R::kW, w);
+      else ring.template read8<W>(from + R::kW, w);
+    } else {
+      if (master) load8(static_cast<const float*>(e.master) + p.at, lane, p.left, false, w);
+      else load8(static_cast<const W*>(e.weight) + p.at, lane, p.left, false, w);
+    }
+    apply(w, m, v, s, e.decay, eps);
+    if (master) store8(e.master + p.at, lane, p.left, p.wide, w);
+    store8(static_cast<W*>(e.weight) + p.at, lane, p.left, p.wide, w);
+  }
+}
+
+template <typename W, typename G, int CAP>
 __global__ void __launch_bounds__(kThreads, 4)
 adamw_kernel(const __grid_constant__ Table<CAP> t, const Numbers* numbers, double b1, double b2, float eps) {
-  __shared__ double q[BITS == 8 ? 512 : 1];   // values of the codes, first moment (with the sign) and second
-  if (BITS == 8) {
-    const int c = threadIdx.x;
-    q[c] = c < 128 ? code_value(c) : -code_value(c - 128);
-    q[256 + c] = code_value(c);
-    __syncthreads();
-  }
   wait_for_previous();
   allow_next();
   const Numbers s = *numbers;
@@ -317,58 +464,33 @@ adamw_kernel(const __grid_constant__ Table<CAP> t, const Numbers* numbers, doubl
   const int chunks = t.first[t.count];
   int chunk = static_cast<int>(static_cast<long long>(chunks) * blockIdx.x / gridDim.x);
   const int end = static_cast<int>(static_cast<long long>(chunks) * (blockIdx.x + 1) / gridDim.x);
-  int i = chunk < end ? entry_of(t, chunk) : 0;
+  int entry = chunk < end ? entry_of(t, chunk) : 0;
   const float f1 = static_cast<float>(b1), f2 = static_cast<float>(b2);
   const float h1 = static_cast<float>(1.0 - b1), h2 = static_cast<float>(1.0 - b2);
   for (; chunk < end; ++chunk) {
-    while (chunk >= t.first[i + 1]) ++i;
-    const Entry& e = t.e[i];
-    const long long at = static_cast<long long>(chunk - t.first[i]) * kChunk + warp * kBlock;
-    if (at >= e.n) continue;   // the same for the warp
-    const int left = static_cast<int>(e.n - at < kBlock ? e.n - at : kBlock);
-    const bool wide = e.wide && left == kBlock;
+    const Place p = place_of(t, chunk, end, entry, warp);
+    entry = p.entry;
+    if (p.left == 0) continue;   // the same for the warp
+    const Entry& e = t.e[p.entry];
+    const bool master = sizeof(W) == 2 && e.master;
     float w[8], g[8], m[8], v[8];
-    auto load_weights = [&]() {
-      if (sizeof(W) == 2 && e.master) load8(static_cast<const float*>(e.master) + at, lane, left, wide, w);
-      else load8(static_cast<const W*>(e.weight) + at, lane, left, wide, w);
-    };
-    load8(static_cast<const G*>(e.grad) + at, lane, left, wide, g);
-    if constexpr (BITS == 32) {
-      float* pm = static_cast<float*>(e.m) + at;
-      float* pv = static_cast<float*>(e.v) + at;
-      load8(pm, lane, left, wide, m);
-      load8(pv, lane, left, wide, v);
-      load_weights();
+    if (master) load8(static_cast<const float*>(e.master) + p.at, lane, p.left, p.wide, w);
+    else load8(static_cast<const W*>(e.weight) + p.at, lane, p.left, p.wide, w);
+    load8(static_cast<const G*>(e.grad) + p.at, lane, p.left, p.wide, g);
+    float *pm = static_cast<float*>(e.m) + p.at, *pv = static_cast<float*>(e.v) + p.at;
+    load8(pm, lane, p.left, p.wide, m);
+    load8(pv, lane, p.left, p.wide, v);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float x = g[k] * s.scale;
-        m[k] = fmaf(f1, m[k], h1 * x);
-        v[k] = fmaf(f2, v[k], h2 * x * x);
-      }
-      store8(pm, lane, left, wide, m);
-      store8(pv, lane, left, wide, v);
-    } else {
-      uint8_t *pm = static_cast<uint8_t*>(e.m) + at, *pv = static_cast<uint8_t*>(e.v) + at;
-      float *ms = e.m_scale + at / kBlock, *vs = e.v_scale + at / kBlock;
-      uint32_t cm[2], cv[2];
-      load8(pm, lane, left, wide, cm);
-      load8(pv, lane, left, wide, cv);
-      const float old_ms = *ms, old_vs = *vs;
-      new_states<true>(pm, ms, cm, old_ms, q, b1, s.g1, lane, left, wide, g, m);
-      load_weights();   // on their way during the second moments; earlier they would take registers from the first
-      new_states<false>(pv, vs, cv, old_vs, q + 256, b2, s.g2, lane, left, wide, g, v);
+    for (int k = 0; k < 8; ++k) {
+      const float x = g[k] * s.scale;
+      m[k] = fmaf(f1, m[k], h1 * x);
+      v[k] = fmaf(f2, v[k], h2 * x * x);
     }
-    if (eps < 1e-12f) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) m[k] = m[k] * s.inv_bc1 / (__fsqrt_rn(v[k] * s.inv_bc2) + eps);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) m[k] = m[k] * s.inv_bc1 * fast_rcp(fast_root(v[k] * s.inv_bc2) + eps);
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) w[k] = fmaf(-s.lr, fmaf(e.decay, w[k], m[k]), w[k]);
-    if (sizeof(W) == 2 && e.master) store8(e.master + at, lane, left, wide, w);
-    store8(static_cast<W*>(e.weight) + at, lane, left, wide, w);
+    store8(pm, lane, p.left, p.wide, m);
+    store8(pv, lane, p.left, p.wide, v);
+    apply(w, m, v, s, e.decay, eps);
+    if (master) store8(e.master + p.at, lane, p.left, p.wide, w);
+    store8(static_cast<W*>(e.weight) + p.at, lane, p.left, p.wide, w);
   }
 }
 
@@ -395,8 +517,14 @@ template <typename W, typename G, int BITS, int CAP>
 int launch_update(const Table<CAP>& t, const Numbers* numbers, double b1, double b2, float eps, cudaStream_t s) {
   const int chunks = t.first[t.count], most = sm_count() * 8;
   if (chunks == 0) return A3PO_OK;
-  A3PO_LAUNCH(kKAdamStep, s, (launch_early(adamw_kernel<W, G, BITS, CAP>, chunks < most ? chunks : most, kThreads, 0, s, 1,
-                                           true, t, numbers, b1, b2, eps)));
+  const int grid = chunks < most ? chunks : most;
+  if constexpr (BITS == 8) {
+    constexpr int kBytes = Ring<G>::kBytes;
+    static_assert(kBytes <= 48 * 1024, "no opt-in needed");
+    A3PO_LAUNCH(kKAdamStep, s, (launch_early(adamw_8bit_kernel<W, G, CAP>, grid, kThreads, kBytes, s, 1, true, t, numbers, b1, b2, eps)));
+  } else {
+    A3PO_LAUNCH(kKAdamStep, s, (launch_early(adamw_kernel<W, G, CAP>, grid, kThreads, 0, s, 1, true, t, numbers, b1, b2, eps)));
+  }
   return after_launch();
 }
 
