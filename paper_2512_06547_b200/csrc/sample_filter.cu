@@ -223,10 +223,11 @@ struct Row {
     return v;
   }
   // Sum of the weights of the logits that `in` takes: pairs, of which one that is not taken (or far below the largest) counts as
-  // its 2^-100th; a sum below 2^-60 is taken again one by one (`in` is asked twice).
+  // its 2^-100th; a sum below 2^-60 is taken again one by one.  count: how many of this thread's it takes.
   template <class W, class F>
-  __device__ __forceinline__ double weigh(const W& w, F in) const {
+  __device__ __forceinline__ double weigh(const W& w, F in, int& count) const {
     double s = 0.0;
+    count = 0;
     if (w.floor > -1e37f && fabsf(w.max) < 1e6f * -w.floor) {   // the limit below is a number well under the largest
       const float least = w.max + w.floor;
       WeightSum even, odd;
@@ -236,16 +237,20 @@ struct Row {
         for (int e = 0; e < per_vec<T>(); e += 2) {
           const int i = base + j * per_vec<T>() + e;
           const float x = v.at(e), y = v.at(e + 1);
-          w.template add<exact_diff<T>()>(f2(in(x, i) ? fmaxf(x, least) : least, in(y, i + 1) ? fmaxf(y, least) : least),
-                                          e % 4 ? odd : even);
+          const bool in_x = in(x, i), in_y = in(y, i + 1);
+          count += (in_x ? 1 : 0) + (in_y ? 1 : 0);
+          w.template add<exact_diff<T>()>(f2(in_x ? fmaxf(x, least) : least, in_y ? fmaxf(y, least) : least), e % 4 ? odd : even);
         }
       }
       s = warp_sum(even.value() + odd.value());
       if (s >= 0x1p-60) return s;
       s = 0.0;
+      count = 0;
     }
     each([&](float x, int i) {
-      if (in(x, i)) s += w.template operator()<exact_diff<T>()>(x);
+      if (!in(x, i)) return;
+      s += w.template operator()<exact_diff<T>()>(x);
+      ++count;
     });
     return warp_sum(s);
   }
@@ -255,6 +260,31 @@ struct Row {
       const Vec<T> v = piece(j);
 #pragma unroll
       for (int e = 0; e < per_vec<T>(); ++e) f(v.at(e), base + j * per_vec<T>() + e);
+    }
+  }
+
+  // The same for those that `in` takes, where they are few: a lane marks its own of 32 first, so that f runs as often as the lane
+  // with the most of them asks, not once for each place that any lane asks for.
+  template <class P, class F>
+  __device__ __forceinline__ void each_of(P in, F f) const {
+    constexpr int VE = per_vec<T>(), kPieces = kWarp / VE;
+    const T* flat = reinterpret_cast<const T*>(data);
+    for (int j0 = v0 + lane; j0 < v1; j0 += kWarp * kPieces) {
+      u32 marks = 0;
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p) {
+        const int j = j0 + p * kWarp;
+        if (j >= v1) continue;
+        const Vec<T> v = piece(j);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) marks |= in(v.at(e)) ? 1u << (p * VE + e) : 0u;
+      }
+      while (marks) {
+        const int bit = __ffs(marks) - 1;
+        marks &= marks - 1;
+        const int at = (j0 + bit / VE * kWarp) * VE + bit % VE;
+        f(to_float(flat[at]), base + at);
+      }
     }
   }
 
@@ -786,10 +816,12 @@ __device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a,
   __syncthreads();   // and the row's total is there
   if (!usable) return Way::kKeys;
   const double total = sh.total;
-  const Reach near = reach_of(row, ask, total, per_t);
-  if (near.end != ~0ull &&
-      gather_and_finish(row, a, row_id, w, steps, t, total, ask, static_cast<u32>(near.end >> 32) + 1u, scratch))
-    return Way::kDone;
+  if (!mass_alone || total < 8.0) {   // (a share of a flat row's mass is out of their reach)
+    const Reach near = reach_of(row, ask, total, per_t);
+    if (near.end != ~0ull &&
+        gather_and_finish(row, a, row_id, w, steps, t, total, ask, static_cast<u32>(near.end >> 32) + 1u, scratch))
+      return Way::kDone;
+  }
   // ---- all logits
   __syncthreads();
   for (int i = threadIdx.x; i < kBins; i += kThreads) sh.lo[i] = 0;
@@ -803,8 +835,7 @@ __device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a,
   if (best == ~0ull) return Way::kKeys;
   const int end = static_cast<int>(best >> 32) + 1;
   const u32 limit = static_cast<u32>(end);
-  if ((best & 0xffffffffu) <= kList)
-    return gather_and_finish(row, a, row_id, w, steps, t, total, ask, limit, scratch) ? Way::kDone : Way::kKeys;
+  if ((best & 0xffffffffu) <= kList && gather_and_finish(row, a, row_id, w, steps, t, total, ask, limit, scratch)) return Way::kDone;
   if ((ask.by_count && ask.by_mass) || low == ~0ull) return Way::kKeys;
 
   // ---- the step that holds the border, and what lies before it
@@ -821,11 +852,10 @@ __device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a,
     for (int i = threadIdx.x; i < range; i += kThreads) own[i] = 0;
     __syncthreads();
     const u32 sure = static_cast<u32>(step0);
-    row.each([&](float l, int) {
-      const u32 x = steps.at(l) - sure;
-      if (x < static_cast<u32>(range)) atomicAdd(&own[x], fixed_of(w.template operator()<exact_diff<T>()>(l)));
-    });
-    double sum = row.weigh(w, [&](float l, int) { return steps.at(l) < sure; });
+    row.each_of([&](float l) { return steps.at(l) - sure < static_cast<u32>(range); },
+                [&](float l, int) { atomicAdd(&own[steps.at(l) - sure], fixed_of(w.template operator()<exact_diff<T>()>(l))); });
+    int unused;
+    double sum = row.weigh(w, [&](float l, int) { return steps.at(l) < sure; }, unused);
     sum = row.block_sum(row.lane == 0 ? sum : 0.0);
     u64* sums = row.tell(static_cast<u64>(__double_as_longlong(sum)));
     row.sync();
@@ -860,11 +890,11 @@ __device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a,
   u32* taken = reinterpret_cast<u32*>(&sh.warp_count[0]);
   if (threadIdx.x == 0) *taken = 0;
   row.sync();   // nobody reads what the list takes the place of
-  row.each([&](float l, int i) {   // a hundred or so of the row
-    if (steps.at(l) != static_cast<u32>(step)) return;
-    const u32 at = take_from_remote(taken, 0, 1);
-    if (at < kList) store_remote(&sh.list[at], 0, entry_of(l, i));
-  });
+  row.each_of([&](float l) { return steps.at(l) == static_cast<u32>(step); },   // a hundred or so of the row
+              [&](float l, int i) {
+                const u32 at = take_from_remote(taken, 0, 1);
+                if (at < kList) store_remote(&sh.list[at], 0, entry_of(l, i));
+              });
   row.sync();
   if (row.rank == 0) {
     const int m = static_cast<int>(*taken);
@@ -1156,10 +1186,8 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
     __syncthreads();   // the total
   }
   const double total = sh.total;
-  auto kept = [&](float x, int i) {
-    const u32 k = tkey<T>(x);
-    return k > edge || (k == edge && i <= limit);
-  };
+  const float edge_at = of_tkey<T>(edge);
+  auto kept = [&](float x, int i) { return x > edge_at || (x == edge_at && i <= limit); };
 
   // ---- the kept weights by stretches
   double s = 0.0;
@@ -1173,8 +1201,7 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
       s = warp_sum(s);
     }
   } else if (many) {
-    row.each([&](float x, int i) { count += kept(x, i) ? 1 : 0; });
-    s = row.weigh(w, kept);
+    s = row.weigh(w, kept, count);
   } else {
     row.each([&](float x, int i) {
       if (kept(x, i)) {
