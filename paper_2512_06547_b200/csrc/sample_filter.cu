@@ -396,72 +396,65 @@ struct Row {
   }
 };
 
-// The lowest place at which the running sum of x over a warp's stretch exceeds `want`; where rounding leaves none, the last with x > 0.
-// x(l, index): 0 for what does not count.
+// Index of this warp's nth logit that `in` takes, in index order (there are that many).
 template <typename T, class F>
-__device__ __forceinline__ int find_in_stretch(const Row<T>& row, double want, F x, float& picked) {
+__device__ __forceinline__ int find_nth(const Row<T>& row, int nth, F in) {
   constexpr int VE = per_vec<T>();
-  double run = 0.0;
-  int last = -1;
-  float last_l = 0.f;
-  const int lane = row.lane;
-  for (int j0 = row.v0; j0 < row.v1; j0 += kWarp) {
-    const int j = j0 + lane;
-    double got[VE], sum = 0.0;
-    float l[VE];
-#pragma unroll
-    for (int e = 0; e < VE; ++e) {
-      got[e] = 0.0;
-      l[e] = -INFINITY;
-    }
+  int run = 0, at = -1;
+  for (int j0 = row.v0; j0 < row.v1 && run < nth; j0 += kWarp) {
+    const int j = j0 + row.lane;
+    u32 marks = 0;
     if (j < row.v1) {
       const Vec<T> v = row.piece(j);
 #pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        l[e] = v.at(e);
-        got[e] = x(l[e], row.base + j * VE + e);
-        sum += got[e];
-        if (got[e] > 0.0) {
-          last = row.base + j * VE + e;
-          last_l = l[e];
-        }
-      }
+      for (int e = 0; e < VE; ++e) marks |= in(v.at(e)) ? 1u << e : 0u;
     }
-    double inc = sum;
+    int inc = __popc(marks);
 #pragma unroll
     for (int o = 1; o < kWarp; o <<= 1) {
-      const double y = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += y;
+      const int y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (row.lane >= o) inc += y;
     }
-    double prev = __shfl_up_sync(0xffffffffu, inc, 1);
-    prev = lane ? run + prev : run;
-    inc += run;
-    const unsigned over = __ballot_sync(0xffffffffu, sum > 0.0 && inc > want);   // inc is a tree of its own in each lane
-    if (over) {
-      const int src = __ffs(over) - 1;
-      int token = last;
-      float tl = last_l;
-      if (lane == src) {
-#pragma unroll
-        for (int e = VE - 1; e >= 0; --e) {
-          double upto = prev;
-#pragma unroll
-          for (int q = 0; q <= e; ++q) upto += got[q];
-          if (upto > want && got[e] > 0.0) {
-            token = row.base + j * VE + e;
-            tl = l[e];
-          }
-        }
-      }
-      picked = __shfl_sync(0xffffffffu, tl, src);
-      return __shfl_sync(0xffffffffu, token, src);
+    int skip = nth - run - (inc - __popc(marks));   // of this lane's, the skip-th
+    if (skip >= 1 && skip <= __popc(marks)) {
+      while (--skip) marks &= marks - 1;
+      at = row.base + j * VE + __ffs(marks) - 1;
     }
-    run = __shfl_sync(0xffffffffu, inc, kWarp - 1);
+    run += __shfl_sync(0xffffffffu, inc, kWarp - 1);
   }
-  const int top = __reduce_max_sync(0xffffffffu, last);
-  const unsigned who = __ballot_sync(0xffffffffu, last == top);
-  picked = __shfl_sync(0xffffffffu, last_l, __ffs(who) - 1);
-  return top;
+  return __reduce_max_sync(0xffffffffu, at);
+}
+
+// Place (in the slice) of the first logit among the pieces v0 .. v1 at which the sum of x(logit, index) passes `want`; where rounding
+// keeps it below, of the last that counts for anything.  By all threads of the block, a piece each.
+template <typename T, class F>
+__device__ __forceinline__ int find_by_sum(Row<T>& row, int v0, int v1, double want, F x) {
+  constexpr int VE = per_vec<T>();
+  constexpr u64 kPast = 1ull << 40;
+  u64 pick = ~0ull;
+  double run = 0.0;
+  for (int j0 = v0; j0 < v1; j0 += kThreads) {
+    const int j = j0 + static_cast<int>(threadIdx.x);
+    double got[VE], sum = 0.0, all;
+    Vec<T> v;
+    if (j < v1) v = row.piece(j);
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      got[e] = j < v1 ? x(v.at(e), row.base + j * VE + e) : 0.0;
+      sum += got[e];
+    }
+    double upto = run + row.scan(sum, all);
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      upto += got[e];
+      const u64 place = static_cast<u64>(j * VE + e);
+      if (got[e] > 0.0) pick = min(pick, upto > want ? place : kPast - place);
+    }
+    pick = row.block_min(pick);
+    if (pick < kPast / 2) break;
+    run += all;
+  }
+  return static_cast<int>(pick < kPast / 2 ? pick : kPast - pick);
 }
 
 // The share that top-p asks for; 2^-48 less, so that one that is reached exactly is reached.
@@ -816,7 +809,7 @@ __device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a,
   __syncthreads();   // and the row's total is there
   if (!usable) return Way::kKeys;
   const double total = sh.total;
-  if (!mass_alone || total < 8.0) {   // (a share of a flat row's mass is out of their reach)
+  if (!mass_alone || total < 4.0) {   // (a share of a flat row's mass is out of their reach)
     const Reach near = reach_of(row, ask, total, per_t);
     if (near.end != ~0ull &&
         gather_and_finish(row, a, row_id, w, steps, t, total, ask, static_cast<u32>(near.end >> 32) + 1u, scratch))
@@ -867,8 +860,13 @@ __device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a,
       u64 found = ~0ull;
       for (int i0 = 0; i0 < range && found == ~0ull; i0 += kThreads) {
         u64 m = 0, all;
-        if (i0 + static_cast<int>(threadIdx.x) < range)
-          for (int r = 0; r < row.cluster; ++r) m += load_remote(&own[i0 + threadIdx.x], r);
+        if (i0 + static_cast<int>(threadIdx.x) < range) {
+          u64 v[kMaxCluster];   // all on their way at once
+#pragma unroll
+          for (int r = 0; r < kMaxCluster; ++r) v[r] = r < row.cluster ? load_remote(&own[i0 + threadIdx.x], r) : 0;
+#pragma unroll
+          for (int r = 0; r < kMaxCluster; ++r) m += v[r];
+        }
         const u64 pre = run + row.scan(m, all);
         const bool here = pre < need && pre + m >= need;
         if (here) sh.slot[kSlots - 1][0] = pre;
@@ -1155,9 +1153,7 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
         if (sum > ties) {
           const int from_here = ties - before - mine;   // the from_here-th of this warp's ties is the last
           if (from_here >= 1 && from_here <= c) {
-            float unused;
-            const int at = find_in_stretch(row, from_here - 0.5, [&](float x, int) { return tkey<T>(x) == edge ? 1.0 : 0.0; },
-                                           unused);
+            const int at = find_nth(row, from_here, [&](float x) { return tkey<T>(x) == edge; });
             if (row.lane == 0) row.say(said, static_cast<u64>(at));
           }
           row.sync();
@@ -1260,13 +1256,12 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
     }
     upto += x;
   }
-  if (who == row.warp) {
-    float picked;
-    const int token = find_in_stretch(row, rest - first, [&](float x, int i) { return kept(x, i) ? weight(x) : 0.0; }, picked);
-    if (row.lane == 0) {
-      const double z = picked == m ? 0.0 : (static_cast<double>(picked) - static_cast<double>(m)) / static_cast<double>(t);
-      a.put(row_id, token, z - log(total), z - log(kept_total), kept_count);
-    }
+  const int place = find_by_sum(row, min(who * stretch, row.vecs), min((who + 1) * stretch, row.vecs), rest - first,
+                                [&](float x, int i) { return kept(x, i) ? weight(x) : 0.0; });
+  if (threadIdx.x == 0) {
+    const float picked = to_float(reinterpret_cast<const T*>(data)[place]);
+    const double z = picked == m ? 0.0 : (static_cast<double>(picked) - static_cast<double>(m)) / static_cast<double>(t);
+    a.put(row_id, row.base + place, z - log(total), z - log(kept_total), kept_count);
   }
 }
 
