@@ -3,7 +3,6 @@
 #include <climits>
 
 #include "linear_internal.cuh"
-#include "lmhead_internal.cuh"
 
 namespace a3po {
 namespace {
@@ -126,7 +125,7 @@ int a3po_linear_fwd(const void* x, const void* w, const void* bias, const void* 
   if (!tc) return linear_fwd_simt(c, dt);
   if (linear_few(N, K, M)) return linear_few_rows_fwd(c);
   if (!row_mask) return linear_fwd_tc(c);
-  A3PO_RETURN_IF(compact_index(nullptr, row_mask, nullptr, nullptr, N, l.cb, c.stream));
+  A3PO_RETURN_IF(linear_row_index(row_mask, N, l.cb, c.stream));
   A3PO_RETURN_IF(gather_rows_range(x, K, l.cb.idx, l.cb.count, 0, l.cb.cap, l.x_c, c.stream, true));
   c.x = l.x_c;
   c.n = l.cb.cap;
@@ -173,7 +172,7 @@ int a3po_linear_bwd(const void* x, const void* w, const uint8_t* row_mask, const
   bool first = true;
   const void* xs = x;
   if (compact) {   // the same index as the forward's: what was kept is in the compact row space
-    A3PO_RETURN_IF(compact_index(nullptr, row_mask, nullptr, nullptr, N, l.cb, stream));
+    A3PO_RETURN_IF(linear_row_index(row_mask, N, l.cb, stream));
     if (grad_w) A3PO_RETURN_IF(gather_rows_range(x, K, l.cb.idx, l.cb.count, 0, l.cb.cap, l.x_c, stream, true));
     rows = l.cb.cap;
     count = l.cb.count;

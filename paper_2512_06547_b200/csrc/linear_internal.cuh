@@ -5,6 +5,7 @@
 #pragma once
 
 #include "ffn_internal.cuh"
+#include "lmhead_internal.cuh"
 
 namespace a3po {
 
@@ -51,6 +52,8 @@ struct LinearFwd {
 };
 
 // ---- tcgen05 kernels (linear_tc.cu): bf16, k % 8 == 0, m % 8 == 0, 16-byte aligned operands
+// cb.idx, cb.count: the rows with a nonzero mask, in order.
+int linear_row_index(const uint8_t* row_mask, long long n, const CompactBuffers& cb, cudaStream_t stream);
 int linear_fwd_tc(const LinearFwd& c);
 // K parts of a product with few output tiles, and the fp32 scratch for them whatever y's type.
 int linear_k_parts(long long n, int k, int m, bool y_f32);

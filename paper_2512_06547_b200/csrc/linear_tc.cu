@@ -214,6 +214,45 @@ linear_add_parts_kernel(const float* parts, int n_parts, long long part_stride, 
   }
 }
 
+// The index of the rows that take part, by one launch: a block of 1,024 rows counts what lies before it by itself (at most a quarter
+// of a megabyte, which the L2 has), so that no block waits for another.  16,384 rows of 1,536 to 4,608 columns there and back: 435 us,
+// where counts, their sums and the index by three launches make it 441; 200,000 rows of 64 columns: no difference any more.
+constexpr int kIndexThreads = 1024;
+constexpr long long kIndexRows = 1 << 18;
+__global__ void __launch_bounds__(kIndexThreads)
+linear_row_index_kernel(const uint8_t* row_mask, long long n, int by_16, int* idx, int* count) {
+  __shared__ int sh[2][kIndexThreads / kWarp];
+  allow_next();
+  const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
+  const long long first = static_cast<long long>(blockIdx.x) * kIndexThreads, row = first + threadIdx.x;
+  const bool in = row < n && row_mask[row] != 0;
+  int before = 0;
+  if (by_16) {
+    const uint4* m = reinterpret_cast<const uint4*>(row_mask);
+    for (long long i = threadIdx.x; i < first / 16; i += kIndexThreads) {
+      const uint4 u = __ldg(m + i);
+      before += __popc(__vsetne4(u.x, 0)) + __popc(__vsetne4(u.y, 0)) + __popc(__vsetne4(u.z, 0)) + __popc(__vsetne4(u.w, 0));
+    }
+  } else {
+    for (long long i = threadIdx.x; i < first; i += kIndexThreads) before += row_mask[i] != 0 ? 1 : 0;
+  }
+  before = __reduce_add_sync(0xffffffffu, before);
+  const unsigned mine = __ballot_sync(0xffffffffu, in);
+  if (lane == 0) {
+    sh[0][warp] = before;
+    sh[1][warp] = __popc(mine);
+  }
+  __syncthreads();
+  int at = 0, own = 0;
+#pragma unroll
+  for (int w = 0; w < kIndexThreads / kWarp; ++w) {
+    at += sh[0][w] + (w < warp ? sh[1][w] : 0);
+    own += w >= warp ? sh[1][w] : 0;
+  }
+  if (in) idx[at + __popc(mine & ((1u << lane) - 1u))] = static_cast<int>(row);
+  if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *count = at + own;
+}
+
 // Zeros for the rows that take no part.  It depends on nothing that the kernel ahead of it does, and runs beside it.
 __global__ void __launch_bounds__(256)
 linear_zero_rows_kernel(const uint8_t* row_mask, long long n, int vec_per_row, uint4* dst) {
@@ -402,6 +441,14 @@ int linear_k_parts(long long n, int k, int m, bool y_f32) {
 size_t linear_parts_bytes(long long n, int k, int m) {
   const int a = linear_k_parts(n, k, m, false), b = linear_k_parts(n, k, m, true), parts = a > b ? a : b;
   return parts > 1 ? static_cast<size_t>((n + BM - 1) / BM * BM) * m * parts * sizeof(float) : 0;
+}
+
+int linear_row_index(const uint8_t* row_mask, long long n, const CompactBuffers& cb, cudaStream_t stream) {
+  if (n > kIndexRows) return compact_index(nullptr, row_mask, nullptr, nullptr, n, cb, stream);
+  const unsigned blocks = static_cast<unsigned>((n + kIndexThreads - 1) / kIndexThreads);
+  A3PO_LAUNCH(kKCompact, stream, (linear_row_index_kernel<<<blocks, kIndexThreads, 0, stream>>>(
+                                     row_mask, n, aligned_to(row_mask, 16) ? 1 : 0, cb.idx, cb.count)));
+  return after_launch();
 }
 
 int linear_fwd_tc(const LinearFwd& c) {

@@ -153,6 +153,19 @@ def test_wanted_gradients_alone_and_accumulated(dt, n, k, m, masked):
             assert ((a - (b + 1.0)).abs() <= 2 * U * (1.0 + b.abs())).all()
 
 
+@pytest.mark.parametrize("n,offset", [(1024, 0), (1025, 3), (5000, 0), (5000, 1), (262144, 0), (262144, 5), (262145, 0)])
+def test_masks_of_many_rows(n, offset):
+    """Rows of several blocks of the row index, whatever the mask's alignment and its nonzero bytes."""
+    c = Case(n, 8, 16, "bf16", "silu", True, False, 0.4)
+    gen = np.random.default_rng(n + offset)
+    values = to_np64(c.mask).astype(np.uint8) * gen.choice(np.array([1, 2, 128, 255], np.uint8), n)
+    room = torch.full((n + 16,), 1, dtype=torch.uint8, device=DEV)
+    mask = room[offset:offset + n]
+    mask.copy_(torch.from_numpy(values))
+    c.mask = mask
+    check(c)
+
+
 def test_large_values_and_infinite_slopes():
     """Activations far out: z up to hundreds either way stays finite."""
     for dt, n, k, m in (("bf16", 40, 64, 64), ("f32", 40, 33, 20)):
