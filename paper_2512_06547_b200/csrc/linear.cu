@@ -35,6 +35,7 @@ struct Layout {
   char* dz = nullptr;
   float* sums = nullptr;   // column sums of dz by blocks of rows
   float* parts = nullptr;
+  float* w_parts = nullptr;   // apart from them: the two products run beside one another
 };
 
 bool lay_out(Arena& ar, long long n, int k, int m, a3po_dtype dt, Act act, bool masked, bool bwd, Layout* l) {
@@ -65,6 +66,8 @@ bool lay_out(Arena& ar, long long n, int k, int m, a3po_dtype dt, Act act, bool 
   const size_t parts = !bwd && linear_few(n, k, m) ? 0 : bwd ? ffn_parts_bytes(static_cast<long long>(cap), k, m)
                                                              : linear_parts_bytes(static_cast<long long>(cap), k, m);
   if (parts) l->parts = ar.take<float>(parts / sizeof(float));
+  const size_t w_parts = bwd ? linear_weight_parts_bytes(static_cast<long long>(cap), k, m) : 0;
+  if (w_parts) l->w_parts = ar.take<float>(w_parts / sizeof(float));
   return ar.ok();
 }
 
@@ -192,7 +195,7 @@ int a3po_linear_bwd(const void* x, const void* w, const uint8_t* row_mask, const
   }
   if (grad_bias) A3PO_RETURN_IF(linear_grad_bias(l.sums, (rows + kZRows - 1) / kZRows, count, M, grad_bias, accumulate, stream));
   if (!grad_x && !grad_w) return A3PO_OK;
-  return linear_grads_tc(dz, xs, w, rows, K, M, grad_x, grad_w, grad_w_dt, accumulate, l.parts, index, count, row_mask, N, first,
+  return linear_grads_tc(dz, xs, w, rows, K, M, grad_x, grad_w, grad_w_dt, accumulate, l.parts, l.w_parts, index, count, row_mask, N, first,
                          status, stream);
 }
 

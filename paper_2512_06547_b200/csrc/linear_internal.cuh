@@ -58,6 +58,9 @@ int linear_fwd_tc(const LinearFwd& c);
 // K parts of a product with few output tiles, and the fp32 scratch for them whatever y's type.
 int linear_k_parts(long long n, int k, int m, bool y_f32);
 size_t linear_parts_bytes(long long n, int k, int m);
+// Parts of the rows for the weight gradient, and the fp32 scratch for them whatever its type.
+int linear_weight_parts(long long n, int k, int m, bool grad_f32);
+size_t linear_weight_parts_bytes(long long n, int k, int m);
 // dz (bf16 [rows to the next multiple of 128][m], or null) and, of blocks of 128 rows, its column sums (fp32, or null) from dy and
 // what was kept.  Row i is row row_index[i] of dy (null: i); rows from *count (null: n) on, and rows with row_mask 0, are zeros.
 int linear_grad_z(const void* grad_y, const void* kept, long long n, int m, Act act, const int* row_index, const int* count,
@@ -68,7 +71,7 @@ int linear_grad_bias(const float* sums, long long blocks, const int* count, int 
 // grad_w[m, k] = dz^T x, grad_x = dz W (either null: not wanted), the latter's rows at row_index[i] of `rows` where that is given.
 // first: the call's first launch.
 int linear_grads_tc(const void* dz, const void* x, const void* w, long long n, int k, int m, void* grad_x, void* grad_w,
-                    a3po_dtype grad_dt, int accumulate, float* parts, const int* row_index, const int* count,
+                    a3po_dtype grad_dt, int accumulate, float* parts, float* w_parts, const int* row_index, const int* count,
                     const uint8_t* row_mask, long long rows, bool first, uint32_t* status, cudaStream_t stream);
 
 // ---- few rows (linear_few.cu)

@@ -31,6 +31,9 @@ __device__ __forceinline__ void store_32(void* p, const uint4& a, const uint4& b
 
 // Outputs that stay in fp32 are sums of 512 products at a time (see PlainEpilogue::kPromote).
 constexpr int kSumBlocks = 8;
+// Sums over fewer rows are not split.  There and back, bf16: 16,384 rows of 128 x 128 58 us split, 102 as one tile's sum, of 512 x 512
+// 84 and 134; 4,096 rows of 128 x 128 27 and 34, of 2,048 x 512 59 and 59; 1,024 rows of 128 x 128 27 and 24.
+constexpr long long kSplitRows = 4096;
 
 struct WeightGradEpilogue : StoreF32EpilogueT<kKLinearGradW> {
   static constexpr int kGroups = 2;
@@ -212,6 +215,64 @@ linear_add_parts_kernel(const float* parts, int n_parts, long long part_stride, 
     if constexpr (sizeof(OUT) == 4) *reinterpret_cast<float4*>(p.y + at) = make_float4(v[0], v[1], v[2], v[3]);
     else *reinterpret_cast<uint2*>(p.y + at) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
   }
+}
+
+// A weight gradient from the parts of a split over its rows: 4 columns per thread, the parts in index order, 8 on their way at a
+// time.  Parts that got no k-block (the rows that take part are fewer than the buffer's) were not written.
+template <typename OUT>
+__global__ void __launch_bounds__(256)
+linear_add_weight_parts_kernel(const float* parts, int n_parts, long long part_stride, long long total, const int* count, long long n,
+                               OUT* w, int accumulate) {
+  wait_for_previous();
+  allow_next();
+  const long long rows = count ? (*count < n ? *count : n) : n, k_blocks = (rows + BK - 1) / BK;
+  for (long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; i < total;
+       i += static_cast<long long>(gridDim.x) * 256) {
+    const float* src = parts + i * kAddCols;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p0 = 0; p0 < n_parts; p0 += kAddBatch) {
+      float4 a[kAddBatch];
+#pragma unroll
+      for (int k = 0; k < kAddBatch; ++k) {
+        const int p = p0 + k;
+        const bool there = p < n_parts && p * k_blocks / n_parts < (p + 1) * k_blocks / n_parts;
+        a[k] = there ? __ldcs(reinterpret_cast<const float4*>(src + p * part_stride)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll
+      for (int k = 0; k < kAddBatch; ++k) {
+        v.x += a[k].x; v.y += a[k].y; v.z += a[k].z; v.w += a[k].w;
+      }
+    }
+    if constexpr (sizeof(OUT) == 4) {
+      float4* to = reinterpret_cast<float4*>(w) + i;
+      if (accumulate) {
+        const float4 old = *to;
+        v.x += old.x; v.y += old.y; v.z += old.z; v.w += old.w;
+      }
+      *to = v;
+    } else {
+      reinterpret_cast<uint2*>(w)[i] = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+    }
+  }
+}
+
+// dz^T x in parts of the rows, then their sum.
+template <typename OUT>
+int weight_parts(const Operand& a, const Operand& b, OUT* w, int accumulate, float* parts, int n_parts, const int* count,
+                 uint32_t* status, cudaStream_t stream, Begin begin) {
+  const int m = static_cast<int>(a.mn_extent), k = static_cast<int>(b.mn_extent);
+  const long long m_pad = (m + BM - 1) / BM * BM;
+  DynRows d = rows_as_m(count, a.k_extent);
+  d.is_k = 1;
+  using Parts = StorePartsEpilogue<kKLinearGradW>;
+  A3PO_RETURN_IF((launch_gemm<Parts, true, true, 1>(a, b, 0, typename Parts::Params{parts, m, static_cast<int>(m_pad), n_parts, k}, d,
+                                                    status, stream, n_parts, begin)));
+  const long long total = static_cast<long long>(m) * (k / kAddCols), want = (total + 255) / 256;
+  const int blocks = static_cast<int>(want < sm_count() * 8ll ? want : sm_count() * 8ll);
+  A3PO_LAUNCH(kKLinearGradW, stream, (launch_early(linear_add_weight_parts_kernel<OUT>, blocks, 256, 0, stream, 1, true,
+                                                   static_cast<const float*>(parts), n_parts, m_pad * k, total, count, a.k_extent, w,
+                                                   accumulate)));
+  return after_launch();
 }
 
 // The index of the rows that take part, by one launch: a block of 1,024 rows counts what lies before it by itself (at most a quarter
@@ -438,6 +499,22 @@ int linear_k_parts(long long n, int k, int m, bool y_f32) {
   return need > 16 ? 1 : need > parts ? need : parts;
 }
 
+// A weight gradient of few tiles is a long sum over the rows for a few SMs: it is split where at most half of them have a tile, in
+// parts of 512 rows and more, and, of fp32 gradients, of 512 and less (see PlainEpilogue::kPromote) unless that makes more than
+// two rounds of parts.
+int linear_weight_parts(long long n, int k, int m, bool grad_f32) {
+  const long long k_blocks = (n + BK - 1) / BK, tiles = ((m + BM - 1ll) / BM) * ((k + BN - 1ll) / BN);
+  const int parts = k_blocks >= kSplitRows / BK ? ffn_k_parts(m, k, static_cast<int>(n)) : 1;
+  if (!grad_f32 || parts == 1) return parts;
+  const long long need = (k_blocks + kSumBlocks - 1) / kSumBlocks;
+  return need * tiles > 2ll * (sm_count() > 0 ? sm_count() : 148) ? 1 : need > parts ? static_cast<int>(need) : parts;
+}
+
+size_t linear_weight_parts_bytes(long long n, int k, int m) {
+  const int a = linear_weight_parts(n, k, m, false), b = linear_weight_parts(n, k, m, true), parts = a > b ? a : b;
+  return parts > 1 ? static_cast<size_t>((m + BM - 1) / BM * BM) * k * parts * sizeof(float) : 0;
+}
+
 size_t linear_parts_bytes(long long n, int k, int m) {
   const int a = linear_k_parts(n, k, m, false), b = linear_k_parts(n, k, m, true), parts = a > b ? a : b;
   return parts > 1 ? static_cast<size_t>((n + BM - 1) / BM * BM) * m * parts * sizeof(float) : 0;
@@ -484,12 +561,18 @@ int linear_grad_bias(const float* sums, long long blocks, const int* count, int 
 }
 
 int linear_grads_tc(const void* dz, const void* x, const void* w, long long n, int k, int m, void* grad_x, void* grad_w,
-                    a3po_dtype grad_dt, int accumulate, float* parts, const int* row_index, const int* count,
+                    a3po_dtype grad_dt, int accumulate, float* parts, float* w_parts, const int* row_index, const int* count,
                     const uint8_t* row_mask, long long rows, bool first, uint32_t* status, cudaStream_t stream) {
   Begin begin = first ? Begin::kAfter : Begin::kEarly;
   if (grad_w) {
     const Operand a{dz, m, n, m}, b{x, k, n, k};   // dz^T x
-    if (grad_dt == A3PO_F32) {
+    const int n_parts = w_parts ? linear_weight_parts(n, k, m, grad_dt == A3PO_F32) : 1;
+    if (n_parts > 1) {
+      A3PO_RETURN_IF(grad_dt == A3PO_F32 ? weight_parts(a, b, static_cast<float*>(grad_w), accumulate, w_parts, n_parts, count, status,
+                                                        stream, begin)
+                                         : weight_parts(a, b, static_cast<__nv_bfloat16*>(grad_w), 0, w_parts, n_parts, count, status,
+                                                        stream, begin));
+    } else if (grad_dt == A3PO_F32) {
       using Epi = WeightGradEpilogue;
       A3PO_RETURN_IF((weight_gemm<Epi>(a, b, typename Epi::Params{static_cast<float*>(grad_w), k, m, k, accumulate}, accumulate,
                                        count, status, stream, begin)));

@@ -34,13 +34,17 @@ struct Slice {
   uint32_t rows_on;    // k contiguous: bit i, row of element i exists and is not masked out; else: all or none
   bool k_contig;
 
+  // k contiguous: a warp takes 8 neighbours of each of 4 rows, 32 different banks of the slice's k-major rows of TILE + 4
+  static __device__ __forceinline__ int k_of(int t) { return t % 8 + t / 32 % 4 * 8; }
+  static __device__ __forceinline__ int row_of(int t) { return t / 8 % 4 + t / 128 * 4; }
+
   __device__ __forceinline__ void start(const Mat<T>& a, long long m0, long long k0) {
     const int t = threadIdx.x % kSimtThreads;
     k_contig = a.k_contig;
     rows_on = 0;
     mask = nullptr;
     if (k_contig) {
-      const long long m = m0 + t / kBK, k = k0 + t % kBK;
+      const long long m = m0 + row_of(t), k = k0 + k_of(t);
       p = a.base + m * a.ms + k;
       i_step = (kSimtThreads / kBK) * a.ms;
       k_left = a.k_dim - k;
@@ -81,8 +85,8 @@ struct Slice {
   __device__ __forceinline__ void store(float (*sh)[TILE + 4]) const {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int e = threadIdx.x % kSimtThreads + i * kSimtThreads;
-      if (k_contig) sh[e % kBK][e / kBK] = r[i]; else sh[e / TILE][e % TILE] = r[i];
+      const int t = threadIdx.x % kSimtThreads, e = t + i * kSimtThreads;
+      if (k_contig) sh[k_of(t)][row_of(t) + i * (kSimtThreads / kBK)] = r[i]; else sh[e / TILE][e % TILE] = r[i];
     }
   }
 };

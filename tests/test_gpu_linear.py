@@ -166,6 +166,21 @@ def test_masks_of_many_rows(n, offset):
     check(c)
 
 
+@pytest.mark.parametrize("n,k,m", [(2048, 136, 72), (4100, 264, 136), (9000, 8, 8)])
+@pytest.mark.parametrize("act,masked", [("none", 0.0), ("silu", 0.3), ("none", 0.995), ("silu", 0.995), ("gelu_tanh", 1.1), ("none", 1.1)])
+@pytest.mark.parametrize("grad_dt", ["bf16", "f32"])
+def test_weight_gradients_in_parts_of_the_rows(n, k, m, act, masked, grad_dt):
+    """Few tiles, many rows; of 0.995 and more masked, parts of the split are left without a row."""
+    c = Case(n, k, m, "bf16", act, True, False, masked)
+    check(c, grad_dt=grad_dt)
+    if grad_dt == "f32":
+        _, kept, _ = c.forward()
+        full, more = c.backward(kept, "f32"), c.backward(kept, "f32", start=1.0)
+        torch.cuda.synchronize()
+        for a, b in zip(more[1:3], full[1:3]):
+            assert ((a - (b + 1.0)).abs() <= 2 * U * (1.0 + b.abs())).all()
+
+
 def test_large_values_and_infinite_slopes():
     """Activations far out: z up to hundreds either way stays finite."""
     for dt, n, k, m in (("bf16", 40, 64, 64), ("f32", 40, 33, 20)):
