@@ -193,10 +193,12 @@ int a3po_linear_bwd(const void* x, const void* w, const uint8_t* row_mask, const
                                  grad_bias ? l.sums : nullptr, compact, stream));
     first = false;
   }
-  if (grad_bias) A3PO_RETURN_IF(linear_grad_bias(l.sums, (rows + kZRows - 1) / kZRows, count, M, grad_bias, accumulate, stream));
-  if (!grad_x && !grad_w) return A3PO_OK;
-  return linear_grads_tc(dz, xs, w, rows, K, M, grad_x, grad_w, grad_w_dt, accumulate, l.parts, l.w_parts, index, count, row_mask, N, first,
-                         status, stream);
+  if (grad_x || grad_w)
+    A3PO_RETURN_IF(linear_grads_tc(dz, xs, w, rows, K, M, grad_x, grad_w, grad_w_dt, accumulate, l.parts, l.w_parts, index, count,
+                                   row_mask, N, first, status, stream));
+  // the column sums are there before either product begins: they are added up beside the last of them
+  return grad_bias ? linear_grad_bias(l.sums, (rows + kZRows - 1) / kZRows, count, M, grad_bias, accumulate, grad_x || grad_w, stream)
+                   : A3PO_OK;
 }
 
 }  // extern "C"

@@ -65,8 +65,8 @@ size_t linear_weight_parts_bytes(long long n, int k, int m);
 // what was kept.  Row i is row row_index[i] of dy (null: i); rows from *count (null: n) on, and rows with row_mask 0, are zeros.
 int linear_grad_z(const void* grad_y, const void* kept, long long n, int m, Act act, const int* row_index, const int* count,
                   const uint8_t* row_mask, void* dz, float* sums, bool early, cudaStream_t stream);
-// grad_bias (+)= the sums of `blocks` blocks (rows / 128 of *count where it is given).
-int linear_grad_bias(const float* sums, long long blocks, const int* count, int m, float* grad_bias, int accumulate,
+// grad_bias (+)= the sums of `blocks` blocks (rows / 128 of *count where it is given).  beside: see Begin in gemm_tc.cuh.
+int linear_grad_bias(const float* sums, long long blocks, const int* count, int m, float* grad_bias, int accumulate, bool beside,
                      cudaStream_t stream);
 // grad_w[m, k] = dz^T x, grad_x = dz W (either null: not wanted), the latter's rows at row_index[i] of `rows` where that is given.
 // first: the call's first launch.

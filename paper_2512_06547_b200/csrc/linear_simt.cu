@@ -101,12 +101,14 @@ int bwd_typed(const T* x, const T* w, const uint8_t* mask, const float* kept, co
   const dim3 grid(static_cast<unsigned>((n + kSimtSumRows - 1) / kSimtSumRows), static_cast<unsigned>((m + 31) / 32));
   A3PO_LAUNCH(kKLinearSimt, s, (simt_grad_z_kernel<T><<<grid, 256, 0, s>>>(gy, kept, mask, n, m, act, dz, gb ? sums : nullptr)));
   A3PO_RETURN_IF(after_launch());
-  if (gb) A3PO_RETURN_IF(linear_grad_bias(sums, grid.x, nullptr, m, gb, accumulate, s));
+  // the three that follow read what that kernel wrote and share nothing else: the second and third run beside the first
   if (gw)
     A3PO_RETURN_IF(gemm<kKLinearSimt>(Mat<float>{dz, 1, m, m, n, nullptr, false}, Mat<T>{x, 1, k, k, n, mask, false}, gw, k,
                                       accumulate, s));
-  if (!gx) return A3PO_OK;
-  return gemm<kKLinearSimt>(Mat<float>{dz, m, 1, n, m, nullptr, true}, Mat<T>{w, 1, k, k, m, nullptr, false}, gx, k, 0, s);
+  if (gx)
+    A3PO_RETURN_IF(gemm<kKLinearSimt>(Mat<float>{dz, m, 1, n, m, nullptr, true}, Mat<T>{w, 1, k, k, m, nullptr, false}, gx, k, 0, s,
+                                      gw != nullptr));
+  return gb ? linear_grad_bias(sums, grid.x, nullptr, m, gb, accumulate, gw || gx, s) : A3PO_OK;
 }
 
 }  // namespace

@@ -465,9 +465,9 @@ linear_grad_z_kernel(const __nv_bfloat16* grad_y, const uint8_t* kept, long long
 
 // 32 columns per block; 32 groups of threads share the blocks of rows and are added in order.
 __global__ void __launch_bounds__(1024)
-linear_grad_bias_kernel(const float* sums, long long blocks, const int* count, int m, float* grad_bias, int accumulate) {
+linear_grad_bias_kernel(const float* sums, long long blocks, const int* count, int m, float* grad_bias, int accumulate, int beside) {
   __shared__ float part[32][33];
-  wait_for_previous();
+  if (!beside) wait_for_previous();
   allow_next();
   if (count) {
     const long long have = (static_cast<long long>(*count) + kZRows - 1) / kZRows;
@@ -486,6 +486,7 @@ linear_grad_bias_kernel(const float* sums, long long blocks, const int* count, i
     for (int i = 0; i < 32; ++i) t += part[i][x];
     grad_bias[col] = accumulate ? grad_bias[col] + t : t;
   }
+  if (beside) wait_for_previous();
 }
 
 }  // namespace
@@ -553,10 +554,10 @@ int linear_grad_z(const void* grad_y, const void* kept, long long n, int m, Act 
   return after_launch();
 }
 
-int linear_grad_bias(const float* sums, long long blocks, const int* count, int m, float* grad_bias, int accumulate,
+int linear_grad_bias(const float* sums, long long blocks, const int* count, int m, float* grad_bias, int accumulate, bool beside,
                      cudaStream_t stream) {
   A3PO_LAUNCH(kKLinearGradZ, stream, (launch_early(linear_grad_bias_kernel, static_cast<unsigned>((m + 31) / 32), 1024, 0, stream,
-                                                   1, true, sums, blocks, count, m, grad_bias, accumulate)));
+                                                   1, true, sums, blocks, count, m, grad_bias, accumulate, beside ? 1 : 0)));
   return after_launch();
 }
 

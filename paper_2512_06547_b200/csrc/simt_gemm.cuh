@@ -171,18 +171,20 @@ __device__ __forceinline__ void activation_any(int gelu, float g, float& a, floa
   slope = fmaf(a * (1.f - s), dt, s);
 }
 
-// C[m, c] (+)= sum_k A(m, k) B(c, k)
+// C[m, c] (+)= sum_k A(m, k) B(c, k).  beside: launched early behind a kernel of the same call that has waited for what this one
+// reads; it waits for that one at its end alone (see Begin in gemm_tc.cuh).
 template <typename TA, typename TB, typename TC, int R, int G>
 __global__ void __launch_bounds__(kSimtThreads* G)
-simt_gemm_kernel(Mat<TA> a, Mat<TB> b, TC* c, long long ldc, int accumulate) {
+simt_gemm_kernel(Mat<TA> a, Mat<TB> b, TC* c, long long ldc, int accumulate, int beside) {
   constexpr int kTile = 16 * R;
-  wait_for_previous();
+  if (!beside) wait_for_previous();
   allow_next();
   extern __shared__ __align__(16) uint8_t smem[];
   Tiles<R, G>& sh = *reinterpret_cast<Tiles<R, G>*>(smem);
   const long long m0 = static_cast<long long>(blockIdx.x) * kTile, n0 = static_cast<long long>(blockIdx.y) * kTile;
   float acc[R][R] = {};
   tile_product<R, G>(a, b, m0, n0, sh, acc);
+  if (beside) wait_for_previous();
   if (threadIdx.x >= kSimtThreads) return;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
@@ -224,9 +226,10 @@ int launch_tiles(K kernel, dim3 grid, bool early, cudaStream_t s, Args... args) 
 }
 
 template <int ID, typename TA, typename TB, typename TC>
-int gemm(const Mat<TA>& a, const Mat<TB>& b, TC* c, long long ldc, int accumulate, cudaStream_t s) {
+int gemm(const Mat<TA>& a, const Mat<TB>& b, TC* c, long long ldc, int accumulate, cudaStream_t s, bool beside = false) {
 #define A3PO_GEMM(R, G)                                                                                              \
-  launch_tiles<ID, R, G>(simt_gemm_kernel<TA, TB, TC, R, G>, tiles(a.m_dim, b.m_dim, 16 * R), true, s, a, b, c, ldc, accumulate)
+  launch_tiles<ID, R, G>(simt_gemm_kernel<TA, TB, TC, R, G>, tiles(a.m_dim, b.m_dim, 16 * R), true, s, a, b, c, ldc, \
+                         accumulate, beside ? 1 : 0)
   switch (shape_of(a.m_dim, b.m_dim)) {
     case Shape::kSmall: return A3PO_GEMM(2, 4);
     case Shape::kSplit4: return A3PO_GEMM(4, 4);
