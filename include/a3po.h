@@ -532,7 +532,7 @@ int a3po_linear_bwd(const void* x, const void* w, const uint8_t* row_mask, const
  * Sampling of one token per row of logits (no counterpart in the paper: the rollout's side of the policy).  What it leaves in
  * `logp` is the behaviour log-prob that the loss takes as behav_logp, by the definition of a3po_token_logprobs_fwd.
  *
- * A row with logits l (NaN counts as -inf) and temperature t, t <= 0 meaning greedy (with t = 1 below):
+ * A row with logits l (NaN counts as -inf) and temperature t, t <= 0 or NaN meaning greedy (with t = 1 below):
  *   w_i = exp((l_i - max l) / t);  tokens are ranked by l, of equal logits the lower index first
  *   top_k  keeps the k first ranks (k <= 0 or k >= V: all);
  *   top_p  keeps of those the fewest first ranks whose weights reach top_p times the sum of theirs (top_p >= 1: all);
@@ -540,7 +540,7 @@ int a3po_linear_bwd(const void* x, const void* w, const uint8_t* row_mask, const
  *   token     = the first kept i, in index order, at which the running sum of the kept weights exceeds u times their sum
  *   logp      = log(w_token / sum of all w),   kept_logp = log(w_token / sum of the kept w)
  *   n_kept    = number of kept tokens with a logit above -inf
- * Weights carry 2^-32 of their value and sums 53 bits (the mass that top_p compares: multiples of 2^-43 of the largest weight),
+ * Weights carry 2^-31 of their value and sums 53 bits (the mass that top_p compares: multiples of 2^-43 of the largest weight),
  * added in a fixed order: results are bit-identical from run to run, and a token differs from the one that exact sums give
  * only where u lies within that of a border.
  *
