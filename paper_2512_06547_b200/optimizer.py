@@ -41,7 +41,8 @@ class AdamW:
     max_grad_norm: 0 for no clipping; grad_norm holds the norm of the last step's gradients before clipping either way.  A
     step whose norm is not finite changes nothing.  state_bits: 32 or 8.  masters: True (bf16 weights) keeps an fp32
     copy of each weight, which is what is updated; a list gives the copies.  m, v, m_scales, v_scales, step: states to go on from
-    (kept and updated in place), as this object's attributes of these names hold them."""
+    (kept and updated in place), as this object's attributes of these names hold them.  The weights and states that an object was
+    made with stay its own: new contents are copied into them (lr, steps and grad_norm may be replaced)."""
 
     def __init__(self, weights, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, *, max_grad_norm=0.0, state_bits=32,
                  masters=None, m=None, v=None, m_scales=None, v_scales=None, step=None):
@@ -84,45 +85,50 @@ class AdamW:
         self.beta1, self.beta2 = float(betas[0]), float(betas[1])
         self._ws = b.new_workspace(b.a3po_adamw_workspace_bytes(count), device)
         self._table = (b.A3poAdamWTensor * count)()
-        self._grads, self._grad_dt, self._words, self._device = [None] * count, b.A3PO_F32, None, device.index
+        self._device = device.index
         at = lambda tensors, i: None if tensors is None else tensors[i].data_ptr()
         for i, w in enumerate(self.weights):
             self._table[i] = b.A3poAdamWTensor(w.data_ptr(), at(self.masters, i), None, at(self.m, i), at(self.v, i),
                                                at(self.m_scales, i), at(self.v_scales, i), w.numel(), decay[i])
+        self._rows = [(self._table[i], w, w.data_ptr(), w.numel()) for i, w in enumerate(self.weights)]
 
     def step(self, grads, *, stream=None):
         """grads: one tensor per weight, of its size, all fp32 or all bf16."""
         if len(grads) != len(self.weights):
             raise ValueError("grads: expected one tensor per weight")
-        fresh = [i for i, g in enumerate(grads) if g is not self._grads[i]]
+        device, here = self._device, torch.cuda.current_device()
         dtype = grads[0].dtype if grads else torch.float32
-        for i, g in enumerate(grads):
-            if g.dtype is not dtype:
-                raise TypeError("grads: expected tensors of one type")
-        for i in fresh:
-            g = grads[i]
-            b._want(g, dtype, "grads")
-            b._here(g)
-            if g.numel() != self.weights[i].numel():
-                raise ValueError("grads: expected the size of the weight")
-        if grads:
-            self._grad_dt = b._dtype_code(grads[0])
-        for i, g in enumerate(grads):   # storage may have moved under a tensor that was seen before
-            self._table[i].grad = g.data_ptr()
-        if fresh:
-            self._grads = list(grads)
-        words = (self.lr, self.steps, self.grad_norm, self._ws)
-        if self._words is None or any(a is not c for a, c in zip(words, self._words)):
-            for t, dtype, name in ((self.lr, torch.float32, "lr"), (self.steps, torch.int64, "steps"),
-                                   (self.grad_norm, torch.float32, "grad_norm")):
-                b._want(t, dtype, name)
-                if t.numel() != 1:
-                    raise ValueError(f"{name}: expected one element")
-            self._words = words
-        if self._device != torch.cuda.current_device():
-            raise ValueError(f"expected the current device cuda:{self._device}, got cuda:{torch.cuda.current_device()}")
+        fine = device == here
+        for g, (row, w, at, n) in zip(grads, self._rows):
+            fine &= (g.dtype is dtype and g.numel() == n and g.get_device() == device and g.is_contiguous() and w.data_ptr() == at)
+            row.grad = g.data_ptr()
+        for t, ty in ((self.lr, torch.float32), (self.steps, torch.int64), (self.grad_norm, torch.float32)):
+            fine &= t.dtype is ty and t.numel() == 1 and t.get_device() == device
+        if not fine:   # say what is wrong
+            self._refuse(grads, dtype, here)
+        grad_dt = b._dtype_code(grads[0]) if grads else b.A3PO_F32
         rc = b.load_library().a3po_adamw_step(
-            ctypes.addressof(self._table), len(self._table), self._weight_dt, self._grad_dt, self.state_bits, self.beta1, self.beta2,
+            ctypes.addressof(self._table), len(self._table), self._weight_dt, grad_dt, self.state_bits, self.beta1, self.beta2,
             self.eps, self.max_grad_norm, self.lr.data_ptr(), self.steps.data_ptr(), self.grad_norm.data_ptr(),
             self._ws.data_ptr(), self._ws.numel(), b._stream(stream))
         b._check("a3po_adamw_step", rc)
+
+    def _refuse(self, grads, dtype, here):
+        if self._device != here:
+            raise ValueError(f"expected the current device cuda:{self._device}, got cuda:{here}")
+        for g, (_, w, at, n) in zip(grads, self._rows):
+            if g.dtype is not dtype:
+                raise TypeError("grads: expected tensors of one type")
+            b._want(g, dtype, "grads")
+            b._here(g)
+            if g.numel() != n:
+                raise ValueError("grads: expected the size of the weight")
+            if w.data_ptr() != at:
+                raise ValueError("weights: a weight's storage is another than when the object was made")
+        for t, ty, name in ((self.lr, torch.float32, "lr"), (self.steps, torch.int64, "steps"),
+                            (self.grad_norm, torch.float32, "grad_norm")):
+            b._want(t, ty, name)
+            b._here(t)
+            if t.numel() != 1:
+                raise ValueError(f"{name}: expected one element")
+        raise ValueError("expected tensors on the current device")

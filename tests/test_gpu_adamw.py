@@ -219,3 +219,27 @@ def test_minimises_a_quadratic_the_same_in_8_bits():
             opt.step([w - target])
         ends.append(w.clone())
     assert float((ends[1] - ends[0]).norm()) <= 0.1 * float(ends[0].norm())
+
+
+def test_tensors_are_looked_at_in_every_step():
+    w, g = torch.zeros(600, device=DEV), torch.ones(600, device=DEV)
+    opt = AdamW([w], lr=0.1)
+    opt.step([g])
+    g.resize_(300)                                  # a tensor that the last step took
+    with pytest.raises(ValueError):
+        opt.step([g])
+    g = torch.ones(600, device=DEV)
+    kept, w.data = w.data, torch.zeros(600, device=DEV)
+    with pytest.raises(ValueError):
+        opt.step([g])
+    w.data = kept
+    for name, bad in (("lr", torch.zeros(2, device=DEV)), ("lr", torch.zeros(1)), ("steps", torch.zeros(1, device=DEV)),
+                      ("grad_norm", torch.zeros(1, dtype=torch.float64, device=DEV))):
+        good = getattr(opt, name)
+        setattr(opt, name, bad)
+        with pytest.raises((TypeError, ValueError)):
+            opt.step([g])
+        setattr(opt, name, good)
+    opt.step([g])
+    torch.cuda.synchronize()
+    assert int(opt.steps.item()) == 2 and torch.equal(w, w[:1].expand(600)) and float(w[0]) < 0.0
