@@ -30,7 +30,7 @@ namespace {
 constexpr int kThreads = 512, kWarps = kThreads / kWarp, kMaxCluster = 8;
 constexpr int kBinBits = 11, kBins = 1 << kBinBits;
 constexpr int kMaxSlice = 196608;        // bytes of a row in one block
-constexpr int kSlots = 48;
+constexpr int kSlots = 38;               // a row by every way there is uses 36, and one of a block's own
 constexpr int kList = kBins;             // candidates that one block finishes alone
 constexpr double kFixed = 8796093022208.0;   // 2^43: a weight as a whole number
 
@@ -71,6 +71,9 @@ struct Shared {
     u64 list[kList];               // the first block's: candidates (ordered bits, index)
   };
 };
+
+constexpr size_t kSharedBytes = (sizeof(Shared) + 15) / 16 * 16;   // ahead of the slice
+static_assert(kSharedBytes + kMaxSlice + 32 <= 227 * 1024, "the longest slice and the places before and behind it");
 
 __device__ __forceinline__ void store_remote(u64* here, u32 rank, u64 v) {
   const u32 at = ptx::map_to_cta(static_cast<u32>(__cvta_generic_to_shared(here)), rank);
@@ -921,7 +924,7 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
   constexpr int VE = per_vec<T>();
   extern __shared__ __align__(16) uint8_t smem[];
   Shared& sh = *reinterpret_cast<Shared*>(smem);
-  uint4* data = reinterpret_cast<uint4*>(smem + (sizeof(Shared) + 15) / 16 * 16);
+  uint4* data = reinterpret_cast<uint4*>(smem + kSharedBytes);
   const int row_id = blockIdx.x / cluster;
   if (a.row_mask && a.row_mask[row_id] == 0) {   // the same for the whole cluster
     if (blockIdx.x % cluster == 0 && threadIdx.x == 0) a.put(row_id, -1, 0.0, 0.0, 0);
@@ -1282,7 +1285,7 @@ int filter_impl(const SampleArgs& a, cudaStream_t stream) {
   // the first block's sums by step, and one step's candidates, take the slice's place
   constexpr size_t kAlone = (kBins + kList) * sizeof(u64);
   if (room < kAlone) room = kAlone;
-  const size_t smem = (sizeof(Shared) + 15) / 16 * 16 + room;
+  const size_t smem = kSharedBytes + room;
   if (cudaFuncSetAttribute(sample_filter_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) !=
       cudaSuccess) {
     cudaGetLastError();

@@ -200,6 +200,21 @@ def test_rows_apart_and_off_16_bytes(dt, start):
     check(x, u, top_k=np.full(n, 100), top_p=np.full(n, 0.9))
 
 
+@pytest.mark.parametrize("dt,v,start", [("f32", 393216, 0), ("f32", 393216, 1), ("f32", 393215, 3), ("bf16", 786432, 0),
+                                        ("bf16", 786432, 5), ("bf16", 786425, 7)])
+def test_longest_rows_with_filters(dt, v, start):
+    """Rows that fill eight SMs, one of them flat but for ties that no step of distance bounds."""
+    gen = np.random.default_rng(v + start)
+    buf = torch.from_numpy(gen.standard_normal(2 * v + 16).astype(np.float32) * 2).to(TD[dt]).to(DEV)
+    x = buf[start:start + 2 * v].view(2, v)
+    x[1] = 1.0
+    x[1, v - 5000:] = 1.5
+    u = gen.random(2)
+    check(x, u, top_k=np.array([50, 4000]))
+    check(x, u, top_p=np.array([0.9, 0.5]))
+    check(x, u, top_k=np.array([100000, 300000]), top_p=np.array([0.999, 0.7]), min_p=np.array([1e-6, 0.0]))
+
+
 @pytest.mark.parametrize("filters", [False, True])
 def test_two_streams_capture_and_repeat(filters):
     n, v = 40, 20011
