@@ -31,7 +31,7 @@ int a3po_sample(const void* logits, int64_t row_stride, const uint8_t* row_mask,
   if (N == 0) return A3PO_OK;
   const SampleArgs a{logits, row_stride, row_mask, static_cast<int>(N), V, temperature, top_k, top_p, min_p, u,
                      token, logp, kept_logp, n_kept};
-  return filters ? sample_filter(&a, dt, as_stream(stream)) : sample_stream(&a, dt, ws, as_stream(stream));
+  return filters || sample_in_one(N, V) ? sample_filter(&a, dt, as_stream(stream)) : sample_stream(&a, dt, ws, as_stream(stream));
 }
 
 }  // extern "C"

@@ -304,7 +304,9 @@ struct SampleArgs {
 // Rows without a filter (sample_stream.cu): workspace, and the two launches.
 size_t sample_stream_bytes(long long n, int v);
 int sample_stream(const void* args, a3po_dtype dt, void* ws, cudaStream_t stream);
-// Rows with filters (sample_filter.cu): a row stays in the shared memory of a cluster of blocks.
+// Rows with filters (sample_filter.cu): a row stays in the shared memory of a cluster of blocks.  sample_in_one: short and few ones
+// without filters go there too.
+bool sample_in_one(long long n, int v);
 long long sample_filter_max_v(a3po_dtype dt);
 int sample_filter(const void* args, a3po_dtype dt, cudaStream_t stream);
 

@@ -200,6 +200,20 @@ def test_rows_apart_and_off_16_bytes(dt, start):
     check(x, u, top_k=np.full(n, 100), top_p=np.full(n, 0.9))
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n,v", [(320, 33), (320, 1024), (320, 1025), (320, 4096), (700, 2048), (300, 8192)])
+def test_many_short_rows(n, v, dt):
+    """Rows by small blocks and, one logit or row further, by large ones; ties in every third, more kept than a small block holds."""
+    x, gen = make(n, v, dt, 300 + v, banned=0.05)
+    x[::3] = x[::3].float().round().to(TD[dt])
+    u = gen.random(n)
+    check(x, u)
+    check(x, u, top_k=gen.choice([1, 30, 600, v, 0], n))
+    check(x, u, top_p=gen.choice([0.2, 0.9, 0.999], n))
+    check(x, u, temperature=gen.choice([0.0, 0.3, 1.0, 5.0], n), top_k=gen.choice([0, 20, 700], n), top_p=gen.choice([0.5, 0.99], n),
+          min_p=gen.choice([0.0, 0.01], n))
+
+
 @pytest.mark.parametrize("dt,v,start", [("f32", 393216, 0), ("f32", 393216, 1), ("f32", 393215, 3), ("bf16", 786432, 0),
                                         ("bf16", 786432, 5), ("bf16", 786425, 7)])
 def test_longest_rows_with_filters(dt, v, start):
