@@ -8,7 +8,7 @@
 //     The lanes' largest logits, a thousandth of all, are counted first; they bound peaked rows and small k as well
 //   few candidates (up to 2,048): the first block gets them in index order and finishes alone
 //   more: the exact mass of the steps in which top-p's border may lie, the tokens of the one step that holds the border, which the
-//     first block puts in order, and another pass over the kept ones
+//     first block puts in order, and another pass over those between
 //   rows whose borders the steps do not bound (more tokens on one step than the block holds, a border far from the largest
 //     logit): the border's key (the logit's bits, ordered) by histograms of the key's leading bits, 11 at a time
 //
@@ -16,8 +16,8 @@
 // taken in a fixed order: results are bit-identical from run to run.
 // Bound: latency.  A row is a chain of passes of one to four microseconds and four to nine cluster barriers of half a one; for many
 // rows the instructions of the passes (40 to 70 a logit).  64 rows of 151,936 bf16: top-k 44 us, min-p 37, all three 51, settings that
-// differ by row 76, flat rows under top-p alone (tens of thousands of candidates, every pass of the list above) 84; 1,024 rows
-// 415 to 690 us; 37 rows of 32,003 in fp32, all three, 30 to 34.
+// differ by row 74, flat rows under top-p alone (tens of thousands of candidates, every pass of the list above) 76; 1,024 rows
+// 415 to 655 us; 37 rows of 32,003 in fp32, all three, 30 to 34.
 // Sums by segment for all rows first (sample_stream.cu), a block per row for those whose candidates the segments bound, and
 // this kernel for the rest only was measured: 1,024 rows 440 -> 340 us, 64 rows 44 -> 78; not kept.
 

@@ -706,10 +706,12 @@ __device__ __forceinline__ bool gather_and_finish(Row<T>& row, const SampleArgs&
   return true;
 }
 
-// A row by steps.  kBorder: `border` is the last entry, in rank order, that top-k and top-p keep.  The same for the whole cluster.
+// A row by steps.  kBorder: `border` is the last entry, in rank order, that top-k and top-p keep; where `sure` is set, the tokens of the
+// steps below its upper word, of which it counts as many as its lower word says, are kept, and their weights added up by warps in
+// sh.stretch.  The same for the whole cluster.
 template <typename T, class W>
 __device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a, int row_id, const W& w, float t, float lane_top,
-                                               const Ask& ask, u64* scratch, u64& border) {
+                                               const Ask& ask, u64* scratch, u64& border, u64& sure_out) {
   Shared& sh = row.sh;
   const bool mass_alone = ask.by_mass && !ask.by_count;
   const float per_t = mass_alone ? kMassSteps : kCountSteps;
@@ -762,6 +764,8 @@ __device__ __forceinline__ Way sample_by_steps(Row<T>& row, const SampleArgs& a,
                 [&](float l, int) { atomicAdd(&own[steps.at(l) - sure], fixed_of(w.template operator()<exact_diff<T>()>(l))); });
     int unused;
     double sum = row.weigh(w, [&](float l, int) { return steps.at(l) < sure; }, unused);
+    if (row.lane == 0) sh.stretch[row.warp] = sum;
+    sure_out = low;
     sum = row.block_sum(row.lane == 0 ? sum : 0.0);
     u64* sums = row.tell(static_cast<u64>(__double_as_longlong(sum)));
     row.sync();
@@ -989,9 +993,10 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
   u32 edge = none;
   int limit = -1;
   bool many = false;   // more than a few thousand are kept, as far as is known
+  u64 sure = 0;        // of them: see sample_by_steps
   if (ask.by_count || ask.by_mass || ask.by_min) {
     u64 border = 0;
-    const Way way = sample_by_steps(row, a, row_id, w, t, lane_top, ask, reinterpret_cast<u64*>(data), border);
+    const Way way = sample_by_steps(row, a, row_id, w, t, lane_top, ask, reinterpret_cast<u64*>(data), border, sure);
     if (way == Way::kDone) return;
     const double total = sh.total;
     if (way == Way::kBorder) {
@@ -1081,6 +1086,7 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
       });
       edge = best;
       limit = static_cast<int>(row.cluster_min(first));
+      sure = 0;
     } else if (ask.by_min) {
       float f = __double2float_ru(ask.min_bound);   // the smallest logit that stays
       if (f > m) f = m;
@@ -1089,6 +1095,7 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
       if (k > edge) {
         edge = k;
         limit = INT_MAX;
+        sure = 0;
       }
     }
   } else {
@@ -1101,7 +1108,19 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
   // ---- the kept weights by stretches
   double s = 0.0;
   int count = 0;
-  if (edge == none) {   // all of them: their sums are there
+  if (sure != 0) {   // (whichever way the border was found: their sums have taken the place of the row's) what lies between them and it
+    const Steps steps{m, kMassSteps / t};
+    const u32 from = static_cast<u32>(sure >> 32);
+    row.each_of([&](float x) { return x >= edge_at && steps.at(x) >= from; },
+                [&](float x, int i) {
+                  if (kept(x, i)) {
+                    s += weight(x);
+                    ++count;
+                  }
+                });
+    s = warp_sum(s) + sh.stretch[row.warp];
+    if (row.rank == 0 && threadIdx.x == 0) count += static_cast<int>(sure & 0xffffffffu);
+  } else if (edge == none) {   // all of them: their sums are there
     row.each([&](float x, int) { count += x > -INFINITY ? 1 : 0; });
     s = sh.stretch[row.warp] * factor(sh.stretch_max[row.warp], m);
     if (s < 0x1p-60) {   // perhaps nothing but what counts as 2^-100 there and as 0 here
