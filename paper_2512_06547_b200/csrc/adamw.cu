@@ -4,8 +4,8 @@
 //   m' = b1 m + (1 - b1) g,   v' = b2 v + (1 - b2) g^2
 //   w' = w - lr (decay w + (m' / (1 - b1^t)) / (sqrt(v' / (1 - b2^t)) + eps))
 //
-// Three launches: sums of squares (64 bits, one number per block), the numbers of the step (norm, s, bias corrections; they
-// stay on the device, so that a captured graph follows them), the update.  The tensors come as a table in the kernel's
+// Two launches: sums of squares (64 bits, one number per block), and the update, whose blocks make the numbers of the step (norm, s,
+// bias corrections) from them and from the learning rate and the count of steps on the device, so that a captured graph follows these.  The tensors come as a table in the kernel's
 // arguments: no table in device memory to keep, and a captured graph has its own.
 //
 // States are fp32, or 8 bits in blocks of 256 elements with an fp32 scale each: value = q(code) scale,
@@ -18,7 +18,7 @@
 //
 // Bound: HBM (32 bits: 30 bytes an element with fp32 gradients and masters beside bf16 weights, 18 with 8 bits, and 4 more for
 // the norm); with states of 8 bits the issue slots are about as far.  255 million weights: norm 169 us (6.0 TB/s), update 1,260
-// (6.1 TB/s), with 8 bits 950 (4.8 TB/s).  A few small tensors are three launches, 10 us.
+// (6.1 TB/s), with 8 bits 950 (4.8 TB/s).  A few small tensors are two launches, 8 us.
 
 #include <cfloat>
 #include <climits>
@@ -51,10 +51,23 @@ struct Table {
   int count;
 };
 
-struct Numbers {   // of the step, device memory
+struct Numbers {   // of the step
   double g1, g2;   // (1 - b1) s and (1 - b2) s^2
   float scale, lr, inv_bc1, inv_bc2;
   int skip;
+};
+// What they are made of.  Every block of an update makes them for itself, from the same sums in the same order; the count of steps
+// comes from a copy that the norm's first launch makes, so that the last update's first block may write the new one at any time.
+struct StepArgs {
+  const double* sums;
+  int count;             // of sums
+  float max_norm;
+  double b1, b2;
+  float eps;
+  const float* lr;
+  const long long* old_step;
+  long long* step;       // null: an update that another follows
+  float* grad_norm;
 };
 
 // Entry that holds a chunk.
@@ -143,10 +156,11 @@ __device__ __forceinline__ void store8(uint8_t* p, int lane, int left, bool wide
 // ------------------------------------------------------------------------------------ norm
 template <typename G, int CAP>
 __global__ void __launch_bounds__(kThreads)
-grad_norm_kernel(const __grid_constant__ Table<CAP> t, double* sums, int later) {
+grad_norm_kernel(const __grid_constant__ Table<CAP> t, double* sums, const long long* step, long long* old_step) {
   __shared__ double part[kWarps];
-  if (later) wait_for_previous();
+  if (!step) wait_for_previous();   // else the call's first launch
   allow_next();
+  if (step && blockIdx.x == 0 && threadIdx.x == 0) *old_step = *step;
   const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
   const int chunks = t.first[t.count];
   int chunk = static_cast<int>(static_cast<long long>(chunks) * blockIdx.x / gridDim.x);
@@ -176,35 +190,38 @@ grad_norm_kernel(const __grid_constant__ Table<CAP> t, double* sums, int later) 
 }
 
 // ------------------------------------------------------------------------------------ numbers of the step
-__global__ void __launch_bounds__(kThreads)
-step_numbers_kernel(const double* sums, int count, double b1, double b2, float max_norm, const float* lr, long long* step,
-                    float* grad_norm, Numbers* out) {
+// By all threads, with barriers.  out: shared.  Not inlined: its powers are none of the update's registers' business.
+__device__ __noinline__ void step_numbers(const StepArgs a, Numbers& out) {
   __shared__ double part[kWarps];
-  wait_for_previous();
-  allow_next();
   double s = 0.0;
-  for (int i = threadIdx.x; i < count; i += kThreads) s += sums[i];
+  for (int i = threadIdx.x; i < a.count; i += kThreads) s += a.sums[i];
   s = warp_sum(s);
   if (threadIdx.x % kWarp == 0) part[threadIdx.x / kWarp] = s;
   __syncthreads();
-  if (threadIdx.x != 0) return;
-  s = 0.0;
+  const long long t = *a.old_step + 1;
+  if (threadIdx.x < 2) {   // a warp's lanes: the two powers at once
+    const double b = threadIdx.x ? a.b2 : a.b1;
+    const float inv = static_cast<float>(1.0 / (1.0 - pow(b, static_cast<double>(t))));
+    if (threadIdx.x) out.inv_bc2 = inv; else out.inv_bc1 = inv;
+  }
+  if (threadIdx.x == 0) {
+    s = 0.0;
 #pragma unroll
-  for (int k = 0; k < kWarps; ++k) s += part[k];
-  const double norm = sqrt(s);
-  float scale = 1.f;
-  if (max_norm > 0.f) scale = static_cast<float>(fmin(static_cast<double>(max_norm) / (norm + 1e-6), 1.0));
-  const bool skip = !isfinite(norm);
-  if (grad_norm) *grad_norm = static_cast<float>(norm);
-  const long long t = *step + 1;
-  if (!skip) *step = t;
-  out->g1 = (1.0 - b1) * scale;
-  out->g2 = (1.0 - b2) * scale * scale;
-  out->scale = scale;
-  out->lr = *lr;
-  out->inv_bc1 = static_cast<float>(1.0 / (1.0 - pow(b1, static_cast<double>(t))));
-  out->inv_bc2 = static_cast<float>(1.0 / (1.0 - pow(b2, static_cast<double>(t))));
-  out->skip = skip;
+    for (int k = 0; k < kWarps; ++k) s += part[k];
+    const double norm = sqrt(s);
+    float scale = 1.f;
+    if (a.max_norm > 0.f) scale = static_cast<float>(fmin(static_cast<double>(a.max_norm) / (norm + 1e-6), 1.0));
+    out.g1 = (1.0 - a.b1) * scale;
+    out.g2 = (1.0 - a.b2) * scale * scale;
+    out.scale = scale;
+    out.lr = *a.lr;
+    out.skip = !isfinite(norm);
+    if (a.step && blockIdx.x == 0) {
+      if (a.grad_norm) *a.grad_norm = static_cast<float>(norm);
+      if (!out.skip) *a.step = t;
+    }
+  }
+  __syncthreads();
 }
 
 // ------------------------------------------------------------------------------------ update
@@ -379,16 +396,18 @@ __device__ __forceinline__ Place place_of(const Table<CAP>& t, int chunk, int en
 // next block is loaded into registers only once the one before it is done.
 template <typename W, typename G, int CAP>
 __global__ void __launch_bounds__(kThreads, 4)
-adamw_8bit_kernel(const __grid_constant__ Table<CAP> t, const Numbers* numbers, double b1, double b2, float eps) {
+adamw_8bit_kernel(const __grid_constant__ Table<CAP> t, const StepArgs step) {
   __shared__ double q[512];   // values of the codes, first moment (with the sign) and second
-  extern __shared__ __align__(16) uint8_t smem[];
+  extern __shared__ __align__(128) uint8_t smem[];   // rows of 128 bytes: 950 us, 1,020 where a copy's row lies across two of them
   const int c = threadIdx.x;
   q[c] = c < 128 ? code_value(c) : -code_value(c - 128);
   q[256 + c] = code_value(c);
   __syncthreads();
   wait_for_previous();
   allow_next();
-  const Numbers s = *numbers;
+  __shared__ Numbers made;
+  step_numbers(step, made);
+  const Numbers s = made;
   if (s.skip) return;   // gradients that are not finite: nothing changes
   const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
   using R = Ring<G>;
@@ -438,10 +457,10 @@ adamw_8bit_kernel(const __grid_constant__ Table<CAP> t, const Numbers* numbers, 
       load8(static_cast<const G*>(e.grad) + p.at, lane, p.left, false, g);
       load8(pm, lane, p.left, false, cm);
     }
-    new_states<true>(pm, ms, cm, old_ms, q, b1, s.g1, lane, p.left, p.wide, g, m);
+    new_states<true>(pm, ms, cm, old_ms, q, step.b1, s.g1, lane, p.left, p.wide, g, m);
     if (p.wide) ring.read8(from + R::kV, cv);
     else load8(pv, lane, p.left, false, cv);
-    new_states<false>(pv, vs, cv, old_vs, q + 256, b2, s.g2, lane, p.left, p.wide, g, v);
+    new_states<false>(pv, vs, cv, old_vs, q + 256, step.b2, s.g2, lane, p.left, p.wide, g, v);
     if (p.wide) {
       if (master) ring.template read8<float>(from + R::kW, w);
       else ring.template read8<W>(from + R::kW, w);
@@ -449,7 +468,7 @@ adamw_8bit_kernel(const __grid_constant__ Table<CAP> t, const Numbers* numbers, 
       if (master) load8(static_cast<const float*>(e.master) + p.at, lane, p.left, false, w);
       else load8(static_cast<const W*>(e.weight) + p.at, lane, p.left, false, w);
     }
-    apply(w, m, v, s, e.decay, eps);
+    apply(w, m, v, s, e.decay, step.eps);
     if (master) store8(e.master + p.at, lane, p.left, p.wide, w);
     store8(static_cast<W*>(e.weight) + p.at, lane, p.left, p.wide, w);
   }
@@ -457,18 +476,19 @@ adamw_8bit_kernel(const __grid_constant__ Table<CAP> t, const Numbers* numbers, 
 
 template <typename W, typename G, int CAP>
 __global__ void __launch_bounds__(kThreads, 4)
-adamw_kernel(const __grid_constant__ Table<CAP> t, const Numbers* numbers, double b1, double b2, float eps) {
+adamw_kernel(const __grid_constant__ Table<CAP> t, const StepArgs step) {
   wait_for_previous();
   allow_next();
-  const Numbers s = *numbers;
+  __shared__ Numbers s;
+  step_numbers(step, s);
   if (s.skip) return;   // gradients that are not finite: nothing changes
   const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
   const int chunks = t.first[t.count];
   int chunk = static_cast<int>(static_cast<long long>(chunks) * blockIdx.x / gridDim.x);
   const int end = static_cast<int>(static_cast<long long>(chunks) * (blockIdx.x + 1) / gridDim.x);
   int entry = chunk < end ? entry_of(t, chunk) : 0;
-  const float f1 = static_cast<float>(b1), f2 = static_cast<float>(b2);
-  const float h1 = static_cast<float>(1.0 - b1), h2 = static_cast<float>(1.0 - b2);
+  const float f1 = static_cast<float>(step.b1), f2 = static_cast<float>(step.b2);
+  const float h1 = static_cast<float>(1.0 - step.b1), h2 = static_cast<float>(1.0 - step.b2);
   for (; chunk < end; ++chunk) {
     const Place p = place_of(t, chunk, end, entry, warp);
     entry = p.entry;
@@ -490,7 +510,7 @@ adamw_kernel(const __grid_constant__ Table<CAP> t, const Numbers* numbers, doubl
     }
     store8(pm, lane, p.left, p.wide, m);
     store8(pv, lane, p.left, p.wide, v);
-    apply(w, m, v, s, e.decay, eps);
+    apply(w, m, v, s, e.decay, step.eps);
     if (master) store8(e.master + p.at, lane, p.left, p.wide, w);
     store8(static_cast<W*>(e.weight) + p.at, lane, p.left, p.wide, w);
   }
@@ -516,55 +536,56 @@ void fill(Table<CAP>* t, const a3po_adamw_tensor* tensors, int count, size_t ws,
 }
 
 template <typename W, typename G, int BITS, int CAP>
-int launch_update(const Table<CAP>& t, const Numbers* numbers, double b1, double b2, float eps, cudaStream_t s) {
+int launch_update(const Table<CAP>& t, const StepArgs& step, cudaStream_t s) {
   const int chunks = t.first[t.count], most = sm_count() * 8;
-  if (chunks == 0) return A3PO_OK;
-  const int grid = chunks < most ? chunks : most;
+  if (chunks == 0 && !step.step) return A3PO_OK;
+  const int grid = chunks < 1 ? 1 : chunks < most ? chunks : most;
   if constexpr (BITS == 8) {
     constexpr int kBytes = Ring<G>::kBytes;
     static_assert(kBytes <= 48 * 1024, "no opt-in needed");
-    A3PO_LAUNCH(kKAdamStep, s, (launch_early(adamw_8bit_kernel<W, G, CAP>, grid, kThreads, kBytes, s, 1, true, t, numbers, b1, b2, eps)));
+    A3PO_LAUNCH(kKAdamStep, s, (launch_early(adamw_8bit_kernel<W, G, CAP>, grid, kThreads, kBytes, s, 1, true, t, step)));
   } else {
-    A3PO_LAUNCH(kKAdamStep, s, (launch_early(adamw_kernel<W, G, CAP>, grid, kThreads, 0, s, 1, true, t, numbers, b1, b2, eps)));
+    A3PO_LAUNCH(kKAdamStep, s, (launch_early(adamw_kernel<W, G, CAP>, grid, kThreads, 0, s, 1, true, t, step)));
   }
   return after_launch();
 }
 
 template <int CAP>
-int update(const a3po_adamw_tensor* tensors, int count, a3po_dtype wdt, a3po_dtype gdt, int bits, const Numbers* numbers,
-           double b1, double b2, float eps, cudaStream_t s) {
+int update(const a3po_adamw_tensor* tensors, int count, a3po_dtype wdt, a3po_dtype gdt, int bits, const StepArgs& step,
+           cudaStream_t s) {
   using B = __nv_bfloat16;
   Table<CAP> t;
   fill(&t, tensors, count, wdt == A3PO_F32 ? 4 : 2, gdt == A3PO_F32 ? 4 : 2, bits);
 #define A3PO_UPDATE(W, G)                                                                                      \
-  (bits == 8 ? launch_update<W, G, 8>(t, numbers, b1, b2, eps, s) : launch_update<W, G, 32>(t, numbers, b1, b2, eps, s))
+  (bits == 8 ? launch_update<W, G, 8>(t, step, s) : launch_update<W, G, 32>(t, step, s))
   if (wdt == A3PO_F32) return gdt == A3PO_F32 ? A3PO_UPDATE(float, float) : A3PO_UPDATE(float, B);
   return gdt == A3PO_F32 ? A3PO_UPDATE(B, float) : A3PO_UPDATE(B, B);
 #undef A3PO_UPDATE
 }
 
-// Sums of squares of one table; returns their number through `blocks`.
+// Sums of squares of one table; returns their number through `blocks`.  step: the call's first launch, which copies it.
 template <int CAP>
-int norm_sums(const a3po_adamw_tensor* tensors, int count, a3po_dtype gdt, double* sums, int room, bool later, int* blocks,
-              cudaStream_t s) {
+int norm_sums(const a3po_adamw_tensor* tensors, int count, a3po_dtype gdt, double* sums, int room, const long long* step,
+              long long* old_step, int* blocks, cudaStream_t s) {
   Table<CAP> t;
   fill(&t, tensors, count, 1, gdt == A3PO_F32 ? 4 : 2, 8);
   for (int i = 0; i < count; ++i) t.e[i].wide = aligned4(tensors[i].grad, gdt == A3PO_F32 ? 4 : 2);
   const int chunks = t.first[t.count];
   int grid = sm_count() * 6 < chunks ? sm_count() * 6 : chunks;
   if (grid > room) grid = room;
+  if (step && grid < 1) grid = 1;
   *blocks = grid;
   if (grid == 0) return A3PO_OK;
   if (gdt == A3PO_F32)
-    A3PO_LAUNCH(kKAdamNorm, s, (launch_early(grad_norm_kernel<float, CAP>, grid, kThreads, 0, s, 1, later, t, sums, later ? 1 : 0)));
+    A3PO_LAUNCH(kKAdamNorm, s, (launch_early(grad_norm_kernel<float, CAP>, grid, kThreads, 0, s, 1, !step, t, sums, step, old_step)));
   else
-    A3PO_LAUNCH(kKAdamNorm, s, (launch_early(grad_norm_kernel<__nv_bfloat16, CAP>, grid, kThreads, 0, s, 1, later, t, sums,
-                                             later ? 1 : 0)));
+    A3PO_LAUNCH(kKAdamNorm, s, (launch_early(grad_norm_kernel<__nv_bfloat16, CAP>, grid, kThreads, 0, s, 1, !step, t, sums, step,
+                                             old_step)));
   return after_launch();
 }
 
-int norm_room(int count) {   // sums: kNormBlocks for each table of kLargeTable tensors
-  return (count + kLargeTable - 1) / kLargeTable * kNormBlocks;
+int norm_room(int count) {   // sums: kNormBlocks for each table of kLargeTable tensors, and for none
+  return (count > 0 ? (count + kLargeTable - 1) / kLargeTable : 1) * kNormBlocks;
 }
 
 // Four codes per thread and step where the pointers allow it.  Bound: HBM, 5 bytes an element (255 million: 235 us, 5.4 TB/s).
@@ -595,7 +616,7 @@ extern "C" {
 
 size_t a3po_adamw_workspace_bytes(int count) {
   if (count < 0) return 0;
-  return round_up(sizeof(Numbers), 256) + round_up(static_cast<size_t>(norm_room(count)) * sizeof(double), 256) + 256;
+  return 256 /* the count of steps */ + round_up(static_cast<size_t>(norm_room(count)) * sizeof(double), 256) + 256;
 }
 
 int a3po_adamw_step(const a3po_adamw_tensor* tensors, int count, a3po_dtype weight_dt, a3po_dtype grad_dt, int state_bits,
@@ -625,30 +646,32 @@ int a3po_adamw_step(const a3po_adamw_tensor* tensors, int count, a3po_dtype weig
   if (sm_count() <= 0) return A3PO_ERR_NO_DEVICE;
   cudaStream_t stream = as_stream(stream_);
   Arena ar(ws, ws_bytes);
-  Numbers* numbers = ar.take<Numbers>(1);
+  long long* old_step = ar.take<long long>(1);
   double* sums = ar.take<double>(static_cast<size_t>(norm_room(count)));
   if (!ar.ok()) return A3PO_ERR_WORKSPACE;
-  int total = 0;
-  bool launched = false;
-  if (max_grad_norm > 0.f || grad_norm) {
-    for (int i = 0; i < count; i += kLargeTable) {
-      const int part = count - i < kLargeTable ? count - i : kLargeTable;
-      int blocks = 0;
-      if (part <= kSmallTable) A3PO_RETURN_IF(norm_sums<kSmallTable>(tensors + i, part, grad_dt, sums + total, kNormBlocks, launched, &blocks, stream));
-      else A3PO_RETURN_IF(norm_sums<kLargeTable>(tensors + i, part, grad_dt, sums + total, kNormBlocks, launched, &blocks, stream));
-      total += blocks;
-      launched |= blocks > 0;
-    }
-  }
-  A3PO_LAUNCH(kKAdamNorm, stream, (launch_early(step_numbers_kernel, 1, kThreads, 0, stream, 1, launched,
-                                                static_cast<const double*>(sums), total, beta1, beta2, max_grad_norm, lr,
-                                                reinterpret_cast<long long*>(step), grad_norm, numbers)));
-  A3PO_RETURN_IF(after_launch());
-  for (int i = 0; i < count; i += kLargeTable) {
-    const int part = count - i < kLargeTable ? count - i : kLargeTable;
-    if (part <= kSmallTable) A3PO_RETURN_IF(update<kSmallTable>(tensors + i, part, weight_dt, grad_dt, state_bits, numbers, beta1, beta2, eps, stream));
-    else A3PO_RETURN_IF(update<kLargeTable>(tensors + i, part, weight_dt, grad_dt, state_bits, numbers, beta1, beta2, eps, stream));
-  }
+  // without a norm the first launch sees no tensors: it copies the count of steps, and the norm is 0
+  const int normed = max_grad_norm > 0.f || grad_norm ? count : 0;
+  int total = 0, at = 0;
+  do {
+    const int part = normed - at < kLargeTable ? normed - at : kLargeTable;
+    const long long* first = at == 0 ? reinterpret_cast<const long long*>(step) : nullptr;
+    int blocks = 0;
+    if (part <= kSmallTable)
+      A3PO_RETURN_IF(norm_sums<kSmallTable>(tensors + at, part, grad_dt, sums + total, kNormBlocks, first, old_step, &blocks, stream));
+    else
+      A3PO_RETURN_IF(norm_sums<kLargeTable>(tensors + at, part, grad_dt, sums + total, kNormBlocks, first, old_step, &blocks, stream));
+    total += blocks;
+    at += part;
+  } while (at < normed);
+  StepArgs args{sums, total, max_grad_norm, beta1, beta2, eps, lr, old_step, nullptr, grad_norm};
+  at = 0;
+  do {
+    const int part = count - at < kLargeTable ? count - at : kLargeTable;
+    if (at + part == count) args.step = reinterpret_cast<long long*>(step);
+    if (part <= kSmallTable) A3PO_RETURN_IF(update<kSmallTable>(tensors + at, part, weight_dt, grad_dt, state_bits, args, stream));
+    else A3PO_RETURN_IF(update<kLargeTable>(tensors + at, part, weight_dt, grad_dt, state_bits, args, stream));
+    at += part;
+  } while (at < count);
   return A3PO_OK;
 }
 
