@@ -187,17 +187,18 @@ int a3po_linear_bwd(const void* x, const void* w, const uint8_t* row_mask, const
   }
   if (row_mask) xs = l.x_c;
   const void* dz = grad_y;
+  const bool few = rows <= kZRows;   // a block's sums are the bias gradient
   if (l.dz || grad_bias) {
     if (l.dz) dz = l.dz;
     A3PO_RETURN_IF(linear_grad_z(grad_y, kept, rows, M, act, index, count, compact ? nullptr : row_mask, l.dz,
-                                 grad_bias ? l.sums : nullptr, compact, stream));
+                                 !grad_bias || few ? grad_bias : l.sums, few && accumulate, compact, stream));
     first = false;
   }
   if (grad_x || grad_w)
     A3PO_RETURN_IF(linear_grads_tc(dz, xs, w, rows, K, M, grad_x, grad_w, grad_w_dt, accumulate, l.parts, l.w_parts, index, count,
                                    row_mask, N, first, status, stream));
   // the column sums are there before either product begins: they are added up beside the last of them
-  return grad_bias ? linear_grad_bias(l.sums, (rows + kZRows - 1) / kZRows, count, M, grad_bias, accumulate, grad_x || grad_w, stream)
+  return grad_bias && !few ? linear_grad_bias(l.sums, (rows + kZRows - 1) / kZRows, count, M, grad_bias, accumulate, grad_x || grad_w, stream)
                    : A3PO_OK;
 }
 

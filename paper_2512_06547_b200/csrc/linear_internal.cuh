@@ -62,9 +62,9 @@ size_t linear_parts_bytes(long long n, int k, int m);
 int linear_weight_parts(long long n, int k, int m, bool grad_f32);
 size_t linear_weight_parts_bytes(long long n, int k, int m);
 // dz (bf16 [rows to the next multiple of 128][m], or null) and, of blocks of 128 rows, its column sums (fp32, or null) from dy and
-// what was kept.  Row i is row row_index[i] of dy (null: i); rows from *count (null: n) on, and rows with row_mask 0, are zeros.
+// what was kept (add: added to what is there).  Row i is row row_index[i] of dy (null: i); rows from *count (null: n) on, and rows with row_mask 0, are zeros.
 int linear_grad_z(const void* grad_y, const void* kept, long long n, int m, Act act, const int* row_index, const int* count,
-                  const uint8_t* row_mask, void* dz, float* sums, bool early, cudaStream_t stream);
+                  const uint8_t* row_mask, void* dz, float* sums, int add, bool early, cudaStream_t stream);
 // grad_bias (+)= the sums of `blocks` blocks (rows / 128 of *count where it is given).  beside: see Begin in gemm_tc.cuh.
 int linear_grad_bias(const float* sums, long long blocks, const int* count, int m, float* grad_bias, int accumulate, bool beside,
                      cudaStream_t stream);

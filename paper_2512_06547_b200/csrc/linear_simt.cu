@@ -49,7 +49,7 @@ simt_linear_kernel(Mat<T> x, Mat<T> w, const T* bias, const T* residual, int act
 // dz[r][c] in fp32 and, of kSimtSumRows rows at a time, its column sums.
 template <typename T>
 __global__ void __launch_bounds__(256)
-simt_grad_z_kernel(const T* gy, const float* kept, const uint8_t* mask, long long n, int m, int act, float* dz, float* sums) {
+simt_grad_z_kernel(const T* gy, const float* kept, const uint8_t* mask, long long n, int m, int act, float* dz, float* sums, int add) {
   __shared__ float part[8][33];
   allow_next();
   const int x = threadIdx.x % 32, ty = threadIdx.x / 32;
@@ -75,7 +75,8 @@ simt_grad_z_kernel(const T* gy, const float* kept, const uint8_t* mask, long lon
     t = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) t += part[i][x];
-    sums[static_cast<long long>(blockIdx.x) * m + c] = t;
+    float* to = sums + static_cast<long long>(blockIdx.x) * m + c;
+    *to = add ? *to + t : t;
   }
 }
 
@@ -100,7 +101,9 @@ template <typename T, typename TG>
 int bwd_typed(const T* x, const T* w, const uint8_t* mask, const float* kept, const T* gy, long long n, int k, int m, int act,
               float* dz, float* sums, T* gx, TG* gw, float* gb, int accumulate, cudaStream_t s) {
   const dim3 grid(static_cast<unsigned>((n + kSimtSumRows - 1) / kSimtSumRows), static_cast<unsigned>((m + 31) / 32));
-  A3PO_LAUNCH(kKLinearSimt, s, (simt_grad_z_kernel<T><<<grid, 256, 0, s>>>(gy, kept, mask, n, m, act, dz, gb ? sums : nullptr)));
+  const bool few = grid.x == 1;   // a block's sums are the bias gradient
+  A3PO_LAUNCH(kKLinearSimt, s, (simt_grad_z_kernel<T><<<grid, 256, 0, s>>>(gy, kept, mask, n, m, act, dz, !gb || few ? gb : sums,
+                                                                         few && accumulate)));
   A3PO_RETURN_IF(after_launch());
   // the three that follow read what that kernel wrote and share nothing else: the second and third run beside the first
   if (gw)
@@ -109,7 +112,7 @@ int bwd_typed(const T* x, const T* w, const uint8_t* mask, const float* kept, co
   if (gx)
     A3PO_RETURN_IF(gemm<kKLinearSimt>(Mat<float>{dz, m, 1, n, m, nullptr, true}, Mat<T>{w, 1, k, k, m, nullptr, false}, gx, k, 0, s,
                                       gw != nullptr));
-  return gb ? linear_grad_bias(sums, grid.x, nullptr, m, gb, accumulate, gw || gx, s) : A3PO_OK;
+  return gb && !few ? linear_grad_bias(sums, grid.x, nullptr, m, gb, accumulate, gw || gx, s) : A3PO_OK;
 }
 
 }  // namespace

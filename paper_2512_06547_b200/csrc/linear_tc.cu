@@ -387,14 +387,14 @@ constexpr int kGradCols = 64;
 template <int ACT>
 __global__ void __launch_bounds__(kZRows)
 linear_grad_z_kernel(const __nv_bfloat16* grad_y, const uint8_t* kept, long long n, int m, const int* row_index,
-                     const int* count, const uint8_t* row_mask, __nv_bfloat16* dz, float* sums) {
+                     const int* count, const uint8_t* row_mask, __nv_bfloat16* dz, float* sums, int add) {
   __shared__ __align__(16) uint4 tile[kZRows * 8];
   __shared__ float part[kZRows / kWarp][kGradCols];
   wait_for_previous();
   allow_next();
   const long long rows = count ? (*count < n ? *count : n) : n;
   const long long row0 = static_cast<long long>(blockIdx.x) * kZRows;
-  if (row0 >= rows) return;
+  if (row0 >= rows && gridDim.x > 1) return;   // one block of rows writes its sums, the bias gradient, whatever the mask leaves
   const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
   const int c0 = blockIdx.y * kGradCols, j = threadIdx.x % 8;   // this thread's piece of a row while rows are copied
   const bool in = c0 + j * 8 < m;
@@ -464,7 +464,8 @@ linear_grad_z_kernel(const __nv_bfloat16* grad_y, const uint8_t* kept, long long
     float t = 0.f;
 #pragma unroll
     for (int w = 0; w < kZRows / kWarp; ++w) t += part[w][threadIdx.x];
-    sums[static_cast<long long>(blockIdx.x) * m + c0 + threadIdx.x] = t;
+    float* to = sums + static_cast<long long>(blockIdx.x) * m + c0 + threadIdx.x;
+    *to = add ? *to + t : t;
   }
 }
 
@@ -545,13 +546,13 @@ int linear_fwd_tc(const LinearFwd& c) {
 }
 
 int linear_grad_z(const void* grad_y, const void* kept, long long n, int m, Act act, const int* row_index, const int* count,
-                  const uint8_t* row_mask, void* dz, float* sums, bool early, cudaStream_t stream) {
+                  const uint8_t* row_mask, void* dz, float* sums, int add, bool early, cudaStream_t stream) {
   const dim3 grid(static_cast<unsigned>((n + kZRows - 1) / kZRows), static_cast<unsigned>((m + kGradCols - 1) / kGradCols));
   using B = __nv_bfloat16;
 #define A3PO_GRAD_Z(ACT)                                                                                                  \
   A3PO_LAUNCH(kKLinearGradZ, stream, (launch_early(linear_grad_z_kernel<ACT>, grid, dim3(kZRows), 0, stream, 1, early,         \
                                                    static_cast<const B*>(grad_y), static_cast<const uint8_t*>(kept), n, m, \
-                                                   row_index, count, row_mask, static_cast<B*>(dz), sums)))
+                                                   row_index, count, row_mask, static_cast<B*>(dz), sums, add)))
   if (act == kActNone) A3PO_GRAD_Z(kActNone);
   else if (act == kActSilu) A3PO_GRAD_Z(kActSilu);
   else A3PO_GRAD_Z(kActGelu);

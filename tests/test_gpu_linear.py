@@ -128,13 +128,13 @@ def test_fp32_pipes(dt, n, k, m, act, bias, residual, masked):
     check(Case(n, k, m, dt, act, bias, residual, masked), y_dt="f32" if m % 2 else None, grad_dt="f32" if n % 2 else None)
 
 
-@pytest.mark.parametrize("dt,n,k,m", [("bf16", 20, 64, 40), ("bf16", 200, 264, 136), ("f32", 50, 31, 20)])
+@pytest.mark.parametrize("dt,n,k,m", [("bf16", 20, 64, 40), ("bf16", 100, 64, 136), ("bf16", 200, 264, 136), ("f32", 50, 31, 20), ("f32", 90, 31, 20)])
 @pytest.mark.parametrize("act", ["none", "silu"])
 def test_no_row_takes_part(dt, n, k, m, act):
     check(Case(n, k, m, dt, act, True, True, 1.1))
 
 
-@pytest.mark.parametrize("dt,n,k,m", [("bf16", 20, 64, 40), ("bf16", 200, 264, 136), ("f32", 50, 31, 20)])
+@pytest.mark.parametrize("dt,n,k,m", [("bf16", 20, 64, 40), ("bf16", 128, 64, 136), ("bf16", 129, 64, 136), ("bf16", 200, 264, 136), ("f32", 64, 31, 20), ("f32", 65, 31, 20)])
 @pytest.mark.parametrize("masked", [0.0, 0.4])
 def test_wanted_gradients_alone_and_accumulated(dt, n, k, m, masked):
     for act in ("none", "gelu_tanh"):
