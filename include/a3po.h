@@ -573,8 +573,15 @@ int a3po_sample(const void* logits, int64_t row_stride, const uint8_t* row_mask,
  *   m, v     state_bits = 32: fp32.  state_bits = 8: one byte per element in blocks of 256, with fp32 scales of
  *            ceil(n / 256) blocks in m_scale and v_scale (all bytes and scales 0: states of 0).  A byte stands for
  *            q(c) scale with q(c) = c below 8, else (8 + c mod 8) 2^(c div 8 - 1); in m bit 7 is the sign and c the rest.
- *            New states are rounded to the nearest q of scale = (largest of the block) / q(largest code), halves to the even
- *            code; a second moment above 0 is not rounded to 0.  The update itself uses the states before rounding.
+ *            New states become codes of scale = (largest of the block) / q(largest code).  Steps 1 to 32 take the nearest q, halves
+ *            the even code.  Later steps take the q below or the one above it at random, with the probabilities that make
+ *            the code right on average: the share of a step in an average is then down to 1 - beta, and a nearest code does not
+ *            follow an average that moves by less than half a step between codes (1/32 to 1/16 of a value).  The random number
+ *            of element e of a block is word e mod 4 of Philox4x32-10 with key 0 and counter (32 times the tensor's place in the call
+ *            + e mod 128 div 4, block, t, upper bits of t xor 2^24 times the block's): its upper 16 bits are the first moment's for
+ *            e < 128 and the second's for the others, its lower ones the other's; they and half of the last bit are added as a
+ *            share of the step between the codes, and the rest is cut off.  A second moment above 0 is not stored as 0.
+ *            The update itself uses the states before rounding.
  *   weight_decay   of this tensor
  * Pointers are aligned to their elements; tensors whose pointers allow it (four elements) move in wide pieces.  Tensors must not
  * overlap one another.  The table is read by the host during the call and travels in the kernels' arguments.

@@ -183,6 +183,53 @@ def state_encode(x, signed):
     return codes, scales
 
 
+def _philox4x32_10_of(counter, key):
+    """philox4x32_10 for arrays: counter of four (uint64 arrays or numbers), key of two numbers; four uint64 arrays."""
+    c, k = [np.asarray(x, dtype=np.uint64) for x in counter], [int(x) & U32 for x in key]
+    low, half = np.uint64(U32), np.uint64(32)
+    for _ in range(10):
+        a, b = np.uint64(0xD2511F53) * c[0], np.uint64(0xCD9E8D57) * c[2]
+        c = [(b >> half) ^ c[1] ^ np.uint64(k[0]), b & low, (a >> half) ^ c[3] ^ np.uint64(k[1]), a & low]
+        k = [(k[0] + 0x9E3779B9) & U32, (k[1] + 0xBB67AE85) & U32]
+    return c
+
+
+def state_random(n, signed, step, tensor=0):
+    """[n]: the shares in (0, 1) by which the states of a call's tensor are rounded in step number `step`.  Element e of a block
+    of 256: word e % 4 of the Philox block with counter (32 tensor + e % 128 // 4, block, step, upper bits of the step xor 2^24 times
+    the block's) and key 0; first moments take the upper half in the block's first 128 elements and the lower in the others, second
+    moments the other."""
+    e, block = np.arange(n) % STATE_BLOCK, np.arange(n) // STATE_BLOCK
+    last = (step >> 32) ^ ((block >> 32) << 24)
+    words = _philox4x32_10_of((32 * tensor + e % 128 // 4, block & U32, np.full(n, step & U32), last), (0, 0))
+    word = np.choose(e % 4, words)
+    half = np.where((e < 128) == signed, word >> np.uint64(16), word & np.uint64(0xFFFF))
+    return (half.astype(np.float64) + 0.5) / 65536
+
+
+def state_encode_at_random(x, signed, step, tensor=0):
+    """As state_encode, but cut off after the random share of the step to the next code is added."""
+    x = np.asarray(x, dtype=np.float64)
+    table = state_table(128 if signed else 256)
+    share = state_random(x.size, signed, step, tensor)
+    codes, scales = np.zeros(x.size, dtype=np.uint8), np.zeros(-(-x.size // STATE_BLOCK), dtype=np.float32)
+    for i in range(scales.size):
+        at = slice(i * STATE_BLOCK, (i + 1) * STATE_BLOCK)
+        part = x[at]
+        scales[i] = np.float32(np.abs(part).max() / table[-1])
+        a = np.abs(part) / np.float64(scales[i]) if scales[i] > 0 else np.zeros(part.size)
+        c = np.searchsorted(table, a, side="right") - 1
+        up = np.minimum(c + 1, table.size - 1)
+        way = np.where(up > c, (a - table[c]) / np.maximum(table[up] - table[c], 1.0), 0.0)
+        c = np.where(way + share[at] >= 1, up, c)
+        if signed:
+            c = np.where(part < 0, c + 128, c)
+        elif scales[i] > 0:
+            c = np.where(part > 0, np.maximum(c, 1), c)
+        codes[at] = c
+    return codes, scales
+
+
 def adamw(w, g, m, v, t, lr, beta1, beta2, eps, decay, scale=1.0):
     """One step on one tensor (t: number of this step): w', m', v'."""
     g = np.asarray(g, dtype=np.float64) * scale

@@ -13,17 +13,24 @@
 // at most 1/16 of a value); second moment: codes to 255, q to 1.6e10, so that the smallest square root that is not 0 is
 // 1/127,000 of the largest.  A second moment above 0 is stored as 1 at least: 0 would leave eps alone under a first moment
 // that is not 0.  A block is a warp's work: its largest value is a warp reduction.
+// Rounding: to the nearest code in the first 32 steps, at random after them.  A gradient's share in an average is
+// (1 - b) / (1 - b^t), at least 1 / t and 1 - b in the long run, and half a step between codes is 1/32 to 1/16 of a value: with b2 =
+// 0.999 a nearest code hardly follows gradients that fall (v is 22 times too large 2,500 steps after they fell to a tenth).  At random,
+// up with the probability that makes the code right on average, E v is the 32-bit v at every step.  The random numbers are
+// Philox's for (step, tensor, element) and hang on nothing else: 16 bits and half of the last for each rounding, one call for
+// a lane's eight elements, whose words serve the first moment of one element and the second of another.
 // What is rounded to a code is computed in 64 bits, as a code is a step of several percent and two evaluations in 32 bits
 // would disagree about one in 10^5 of them; the update itself is fp32.
 //
 // Bound: HBM (32 bits: 30 bytes an element with fp32 gradients and masters beside bf16 weights, 18 with 8 bits, and 4 more for
 // the norm); with states of 8 bits the issue slots are about as far.  255 million weights: norm 169 us (6.0 TB/s), update 1,260
-// (6.1 TB/s), with 8 bits 950 (4.8 TB/s).  A few small tensors are two launches, 8 us.
+// (6.1 TB/s), with 8 bits 950 (4.8 TB/s) to the nearest code and 980 at random.  A few small tensors are two launches, 8 us.
 
 #include <cfloat>
 #include <climits>
 
 #include "a3po_common.cuh"
+#include "row_ops.cuh"
 
 namespace a3po {
 namespace {
@@ -33,6 +40,7 @@ constexpr int kThreads = 256, kWarps = kThreads / kWarp;
 constexpr int kChunk = kWarps * kBlock;     // elements that a block takes at a time
 constexpr int kNormBlocks = 2048;           // sums of squares at most
 constexpr int kSmallTable = 32, kLargeTable = 400;
+constexpr long long kNearestSteps = 32;     // see above
 
 struct Entry {
   void* weight;
@@ -55,6 +63,7 @@ struct Numbers {   // of the step
   double g1, g2;   // (1 - b1) s and (1 - b2) s^2
   float scale, lr, inv_bc1, inv_bc2;
   int skip;
+  long long t;     // this step's number
 };
 // What they are made of.  Every block of an update makes them for itself, from the same sums in the same order; the count of steps
 // comes from a copy that the norm's first launch makes, so that the last update's first block may write the new one at any time.
@@ -68,6 +77,7 @@ struct StepArgs {
   const long long* old_step;
   long long* step;       // null: an update that another follows
   float* grad_norm;
+  int first_tensor;      // of the table, in the call
 };
 
 // Entry that holds a chunk.
@@ -215,6 +225,7 @@ __device__ __noinline__ void step_numbers(const StepArgs a, Numbers& out) {
     out.g2 = (1.0 - a.b2) * scale * scale;
     out.scale = scale;
     out.lr = *a.lr;
+    out.t = t;
     out.skip = !isfinite(norm);
     if (a.step && blockIdx.x == 0) {
       if (a.grad_norm) *a.grad_norm = static_cast<float>(norm);
@@ -248,6 +259,39 @@ __device__ __forceinline__ int code_of(double x, int top) {
   const int c = (hi + 0xffff + (odd | more)) >> 17;
   return min(c - ((kEight >> 17) - (small ? 0 : 8)), top);
 }
+// x (in units of the scale) and a share of the step to the next code (odd multiples of 2^-17 of it), cut off.
+__device__ __forceinline__ int code_at_random(double x, uint32_t share, int top) {
+  const bool small = __double2hiint(x) < kEight;
+  if (small) x += 8.0;
+  return min(((__double2hiint(x) + static_cast<int>(share)) >> 17) - ((kEight >> 17) - (small ? 0 : 8)), top);
+}
+// What a lane's elements are rounded by: a word for each of the first four, which their counterparts in the block's other half share:
+// the first moments take its upper half for the former and its lower for the latter, the second moments the other one.
+// A word belongs to an element's place in the block, whoever holds it: a lane with every 32nd element asks the lanes that have its
+// elements among their neighbours.
+struct Random {
+  uint32_t w[4];
+  __device__ __forceinline__ void draw(long long t, int tensor, long long block, int lane, bool wide) {
+    const uint32_t far = static_cast<uint32_t>(block >> 32) << 24;   // 0 but for tensors of 2^40 elements
+    const PhiloxState ph{0u, 0u, static_cast<uint32_t>(t), static_cast<uint32_t>(t >> 32) ^ far};
+    const uint4 u = ph.draw(static_cast<uint32_t>(tensor) * kWarp + static_cast<uint32_t>(lane), static_cast<uint32_t>(block));
+    w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+    if (!wide) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int from = lane / 4 + 8 * i;
+        const uint32_t x = __shfl_sync(0xffffffffu, u.x, from), y = __shfl_sync(0xffffffffu, u.y, from);
+        const uint32_t z = __shfl_sync(0xffffffffu, u.z, from), v = __shfl_sync(0xffffffffu, u.w, from);
+        w[i] = lane % 4 == 0 ? x : lane % 4 == 1 ? y : lane % 4 == 2 ? z : v;
+      }
+    }
+  }
+  // 16 random bits and half of the last: of the 17 bits of a number's upper word below a code's
+  template <bool FIRST>
+  __device__ __forceinline__ uint32_t share(int k) const {
+    return ((k < 4) == FIRST ? w[k % 4] >> 15 : w[k % 4] << 1 & 0x1ffffu) | 1u;
+  }
+};
 __device__ __forceinline__ uint32_t min3u(uint32_t a, uint32_t b, uint32_t c) { return __vimin3_u32(a, b, c); }
 __device__ __forceinline__ uint32_t max3u(uint32_t a, uint32_t b, uint32_t c) { return __vimax3_u32(a, b, c); }
 // Largest over the warp of eight non-negative numbers a lane, ordered as their bits are: the upper words first, then the lower
@@ -275,9 +319,10 @@ __device__ __forceinline__ double reciprocal(float x) {
 }
 
 // New first (second) moments of a block of 256, in 64 bits, stored as codes and a scale; out: their fp32 values.
-template <bool FIRST>
+template <bool FIRST, bool RANDOM>
 __device__ __forceinline__ void new_states(uint8_t* codes, float* scale, uint32_t (&c)[2], float old, const double* q, double b,
-                                           double more, int lane, int left, bool wide, const float (&g)[8], float (&out)[8]) {
+                                           double more, int lane, int left, bool wide, const Random& random, const float (&g)[8],
+                                           float (&out)[8]) {
   constexpr int kTop = FIRST ? 127 : 255;
   const double was = b * static_cast<double>(old);
   double x[8];
@@ -294,8 +339,17 @@ __device__ __forceinline__ void new_states(uint8_t* codes, float* scale, uint32_
   for (int k = 0; k < 8; k += 2)
     least = min3u(least, static_cast<uint32_t>(__double2hiint(fabs(x[k]) * inv)), static_cast<uint32_t>(__double2hiint(fabs(x[k + 1]) * inv)));
   uint32_t byte[8];
-  if (__all_sync(0xffffffffu, least >= static_cast<uint32_t>(kEight)) && now >= FLT_MIN) {
-    // all codes from 8 on (nearly every block): the leading four bits and nothing else
+  const bool usual = __all_sync(0xffffffffu, least >= static_cast<uint32_t>(kEight)) && now >= FLT_MIN;   // nearly every block
+  if (RANDOM && usual) {
+    // the leading four bits; the largest is 2^-24 past the last code at most, too little for any share to make it another
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t hi = static_cast<uint32_t>(__double2hiint(fabs(x[k]) * inv));
+      byte[k] = (hi + random.share<FIRST>(k) - (static_cast<uint32_t>((kEight >> 17) - 8) << 17)) >> 17;
+      if (FIRST) byte[k] |= static_cast<uint32_t>(__double2hiint(x[k])) >> 24 & 0x80u;
+    }
+  } else if (usual) {
+    // the leading four bits, rounded, and nothing else
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const unsigned long long u = static_cast<unsigned long long>(__double_as_longlong(fabs(x[k]) * inv));
@@ -305,7 +359,8 @@ __device__ __forceinline__ void new_states(uint8_t* codes, float* scale, uint32_
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      byte[k] = static_cast<uint32_t>(code_of(fabs(x[k]) * inv, kTop));
+      const double a = fabs(x[k]) * inv;
+      byte[k] = static_cast<uint32_t>(RANDOM ? code_at_random(a, random.share<FIRST>(k), kTop) : code_of(a, kTop));
       if (FIRST) byte[k] |= x[k] < 0.0 ? 128u : 0u;
       else if (byte[k] == 0 && x[k] > 0.0 && now > 0.f) byte[k] = 1;
     }
@@ -392,23 +447,11 @@ __device__ __forceinline__ Place place_of(const Table<CAP>& t, int chunk, int en
   return p;
 }
 
-// States of 8 bits.  18 bytes an element with fp32 gradients and masters beside bf16 weights: 950 us for 255 million, 1,016 when the
-// next block is loaded into registers only once the one before it is done.
-template <typename W, typename G, int CAP>
-__global__ void __launch_bounds__(kThreads, 4)
-adamw_8bit_kernel(const __grid_constant__ Table<CAP> t, const StepArgs step) {
-  __shared__ double q[512];   // values of the codes, first moment (with the sign) and second
-  extern __shared__ __align__(128) uint8_t smem[];   // rows of 128 bytes: 950 us, 1,020 where a copy's row lies across two of them
-  const int c = threadIdx.x;
-  q[c] = c < 128 ? code_value(c) : -code_value(c - 128);
-  q[256 + c] = code_value(c);
-  __syncthreads();
-  wait_for_previous();
-  allow_next();
-  __shared__ Numbers made;
-  step_numbers(step, made);
+// RANDOM: codes are rounded at random.  A function of its own for each of the two, so that neither holds the other's registers.
+template <bool RANDOM, typename W, typename G, int CAP>
+__device__ __forceinline__ void update_8bit(const Table<CAP>& t, const StepArgs& step, const Numbers& made, const double* q, uint8_t* smem) {
   const Numbers s = made;
-  if (s.skip) return;   // gradients that are not finite: nothing changes
+  const long long t_now = made.t;
   const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
   using R = Ring<G>;
   R ring;
@@ -450,6 +493,8 @@ adamw_8bit_kernel(const __grid_constant__ Table<CAP> t, const StepArgs step) {
     const bool master = sizeof(W) == 2 && e.master;
     float w[8], g[8], m[8], v[8];
     uint32_t cm[2], cv[2];
+    Random random;
+    if (RANDOM) random.draw(t_now, step.first_tensor + p.entry, p.at / kBlock, lane, p.wide);
     if (p.wide) {
       ring.template read8<G>(from + R::kG, g);
       ring.read8(from + R::kM, cm);
@@ -457,10 +502,10 @@ adamw_8bit_kernel(const __grid_constant__ Table<CAP> t, const StepArgs step) {
       load8(static_cast<const G*>(e.grad) + p.at, lane, p.left, false, g);
       load8(pm, lane, p.left, false, cm);
     }
-    new_states<true>(pm, ms, cm, old_ms, q, step.b1, s.g1, lane, p.left, p.wide, g, m);
+    new_states<true, RANDOM>(pm, ms, cm, old_ms, q, step.b1, s.g1, lane, p.left, p.wide, random, g, m);
     if (p.wide) ring.read8(from + R::kV, cv);
     else load8(pv, lane, p.left, false, cv);
-    new_states<false>(pv, vs, cv, old_vs, q + 256, step.b2, s.g2, lane, p.left, p.wide, g, v);
+    new_states<false, RANDOM>(pv, vs, cv, old_vs, q + 256, step.b2, s.g2, lane, p.left, p.wide, random, g, v);
     if (p.wide) {
       if (master) ring.template read8<float>(from + R::kW, w);
       else ring.template read8<W>(from + R::kW, w);
@@ -472,6 +517,27 @@ adamw_8bit_kernel(const __grid_constant__ Table<CAP> t, const StepArgs step) {
     if (master) store8(e.master + p.at, lane, p.left, p.wide, w);
     store8(static_cast<W*>(e.weight) + p.at, lane, p.left, p.wide, w);
   }
+}
+
+// States of 8 bits.  18 bytes an element with fp32 gradients and masters beside bf16 weights: 980 us for 255 million, 1,060 with the
+// registers of four blocks per SM; 950 and 1,016 to the nearest code (the latter when the next block is loaded into registers only
+// once the one before it is done).
+template <typename W, typename G, int CAP>
+__global__ void __launch_bounds__(kThreads, 3)
+adamw_8bit_kernel(const __grid_constant__ Table<CAP> t, const StepArgs step) {
+  __shared__ double q[512];   // values of the codes, first moment (with the sign) and second
+  extern __shared__ __align__(128) uint8_t smem[];   // rows of 128 bytes: 950 us, 1,020 where a copy's row lies across two of them
+  const int c = threadIdx.x;
+  q[c] = c < 128 ? code_value(c) : -code_value(c - 128);
+  q[256 + c] = code_value(c);
+  __syncthreads();
+  wait_for_previous();
+  allow_next();
+  __shared__ Numbers made;
+  step_numbers(step, made);
+  if (made.skip) return;   // gradients that are not finite: nothing changes
+  if (made.t <= kNearestSteps) update_8bit<false, W, G>(t, step, made, q, smem);
+  else update_8bit<true, W, G>(t, step, made, q, smem);
 }
 
 template <typename W, typename G, int CAP>
@@ -663,11 +729,12 @@ int a3po_adamw_step(const a3po_adamw_tensor* tensors, int count, a3po_dtype weig
     total += blocks;
     at += part;
   } while (at < normed);
-  StepArgs args{sums, total, max_grad_norm, beta1, beta2, eps, lr, old_step, nullptr, grad_norm};
+  StepArgs args{sums, total, max_grad_norm, beta1, beta2, eps, lr, old_step, nullptr, grad_norm, 0};
   at = 0;
   do {
     const int part = count - at < kLargeTable ? count - at : kLargeTable;
     if (at + part == count) args.step = reinterpret_cast<long long*>(step);
+    args.first_tensor = at;
     if (part <= kSmallTable) A3PO_RETURN_IF(update<kSmallTable>(tensors + at, part, weight_dt, grad_dt, state_bits, args, stream));
     else A3PO_RETURN_IF(update<kLargeTable>(tensors + at, part, weight_dt, grad_dt, state_bits, args, stream));
     at += part;
