@@ -20,8 +20,12 @@ PolicySampler runs the forward half on the rows whose next token is wanted, and 
     logits       = hidden W^T                                        a3po_linear_fwd (fp32)
     token, logp  = temperature, top-k, top-p, min-p; random numbers  a3po_sample
 
-where logp is what the loss takes as behav_logp.  PolicyTail.optimizer makes an AdamW over the pass's parameters, and
-PolicyTail.update takes its step with the gradients that the last pass left.
+where logp is what the loss takes as behav_logp.  It is a log-prob at the row's temperature t (1 for a greedy row), so a pass over
+rows that were drawn at another one than 1 takes inv_temperature = 1 / t: both sides of the importance weight are then the same
+policy's.  Rows of unlike temperatures need passes of their own, whose losses are means over their rows.
+
+PolicyTail.optimizer makes an AdamW over the pass's parameters, and PolicyTail.update takes its step with the gradients that the
+last pass left.
 """
 from __future__ import annotations
 
@@ -63,10 +67,11 @@ class PolicyTail:
                                       b.a3po_gated_ffn_workspace_bytes(n, h, f, dt, True, False),
                                       b.a3po_gated_ffn_workspace_bytes(n, h, f, dt, True, True)), device)
 
-    def __call__(self, r0, params, batch, rng=None, *, accumulate_grads=False):
+    def __call__(self, r0, params, batch, rng=None, *, inv_temperature=1.0, accumulate_grads=False):
         """One pass.  batch: targets, behav_logp, versions, current_version, adv, mask, clip_eps as a3po_train_step takes
-        them.  Returns a dict of this object's own buffers: loss, stats, logp, status, grad_r0 and grads (by parameter,
-        fp32; added to what they hold with accumulate_grads)."""
+        them; inv_temperature: of the policy that is trained, the one that behav_logp was drawn at.  Returns a dict of this
+        object's own buffers: loss, stats, logp, status, grad_r0 and grads (by parameter, fp32; added to what they hold
+        with accumulate_grads)."""
         if not self.beta and (params.get("beta_in") is not None or params.get("beta_out") is not None):
             raise ValueError("params hold a beta, but this PolicyTail was made without gradients for it (beta=True)")
         mask, g = batch["mask"], self.grads
@@ -80,7 +85,7 @@ class PolicyTail:
         b.a3po_train_step(self.hidden, params["w"], batch["targets"], batch["behav_logp"], batch["versions"],
                           batch["current_version"], batch["adv"], mask, batch["clip_eps"], self.logp, self.lse,
                           self.grad_logp, self.loss, self.grad_hidden, g["w"], self.ws, stats=self.stats,
-                          accumulate_grad_w=accumulate_grads, status=self.status)
+                          accumulate_grad_w=accumulate_grads, inv_temperature=inv_temperature, status=self.status)
         b.a3po_dropout_norm_bwd(self.r1, self.p, rng, params["gamma_out"], self.rstd_out, self.grad_hidden,
                                 self.grad_r1, self.grad_y, g["gamma_out"], self.ws, mean=self.mean_out,
                                 grad_beta=g.get("beta_out"), accumulate_grad_w=accumulate_grads, **norm)
