@@ -29,6 +29,8 @@ namespace {
 
 constexpr int kMaxCluster = 8;
 constexpr int kMaxSlice = 196608;        // bytes of a row in one block
+constexpr int kNarrowRow = 1024;            // logits of a row that goes to a small block,
+constexpr long long kNarrowBytes = 16384;   // and its bytes where there are more rows than large blocks that run at once
 constexpr double kFixed = 8796093022208.0;   // 2^43: a weight as a whole number
 
 using u32 = uint32_t;
@@ -102,12 +104,14 @@ __device__ __forceinline__ u64 warp_sum64(u64 v) {
 namespace wide {
 constexpr int kThreads = 512, kBlocks = 2, kBinBits = 11;
 constexpr float kCountSteps = 32.f, kMassSteps = 128.f;
+constexpr size_t kLongestSlice = kMaxSlice;
 #include "sample_rows.cuh"
 }  // namespace wide
 
 namespace narrow {
 constexpr int kThreads = 128, kBlocks = 7, kBinBits = 9;
 constexpr float kCountSteps = 16.f, kMassSteps = 32.f;
+constexpr size_t kLongestSlice = kNarrowBytes;
 #include "sample_rows.cuh"
 }  // namespace narrow
 
@@ -115,8 +119,6 @@ constexpr float kCountSteps = 16.f, kMassSteps = 32.f;
 // have shorter ones up to about 1,024 logits.  All three filters, 129, 1,000 and 4,096 logits in fp32: 64 rows 11, 13 and 48 us by
 // small blocks, 15, 17 and 25 by large ones; 2,048 rows, which are several rounds of large blocks, 41, 34 and 101 against 109, 98
 // and 137 (1,000 rows of 8,192: 96 and 85).
-constexpr int kNarrowRow = 1024;
-constexpr long long kNarrowBytes = 16384;   // of more rows than large blocks that run at once
 
 template <typename T>
 int filter_impl(const SampleArgs& a, cudaStream_t stream) {

@@ -4,6 +4,7 @@
 //   kThreads                  a block's threads;   kBlocks   blocks that share an SM
 //   kBinBits                  a histogram has 2^kBinBits = 4 kThreads bins, and one block finishes that many candidates alone
 //   kCountSteps, kMassSteps   see Steps
+//   kLongestSlice             bytes of a row that one block holds at most
 constexpr int kWarps = kThreads / kWarp, kBins = 1 << kBinBits;
 constexpr int kSlots = 20 + 6 * ((32 + kBinBits - 1) / kBinBits);   // more than a row by every way there is uses
 constexpr int kList = kBins;             // candidates that one block finishes alone
@@ -26,7 +27,14 @@ struct Shared {
 };
 
 constexpr size_t kSharedBytes = (sizeof(Shared) + 15) / 16 * 16;   // ahead of the slice
-static_assert(kSharedBytes + kMaxSlice + 32 <= 227 * 1024, "the longest slice and the places before and behind it");
+// Bytes behind it: the slice and the places before and behind it; the first block's sums by step, and one step's candidates, take its
+// place.
+constexpr size_t room_of(size_t slice) {
+  const size_t alone = (kBins + kList) * sizeof(u64), room = (slice + 47) / 16 * 16;
+  return room < alone ? alone : room;
+}
+constexpr size_t kMostShared = kSharedBytes + room_of(kLongestSlice);
+static_assert(kMostShared <= 227 * 1024, "the longest slice");
 
 template <typename T>
 struct Row {
@@ -1200,12 +1208,10 @@ sample_filter_kernel(SampleArgs a, int cluster, int slice) {
 template <typename T>
 int launch(const SampleArgs& a, int cluster, cudaStream_t stream) {
   const int slice = ((a.v + cluster - 1) / cluster + 7) / 8 * 8;
-  size_t room = (static_cast<size_t>(slice) * sizeof(T) + 47) / 16 * 16;
-  // the first block's sums by step, and one step's candidates, take the slice's place
-  constexpr size_t kAlone = (kBins + kList) * sizeof(u64);
-  if (room < kAlone) room = kAlone;
-  const size_t smem = kSharedBytes + room;
-  if (cudaFuncSetAttribute(sample_filter_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) !=
+  const size_t smem = kSharedBytes + room_of(static_cast<size_t>(slice) * sizeof(T));   // kMostShared at most
+  // The limit belongs to the kernel, not to the call: every call sets the same one, so that none lowers it between another
+  // thread's setting it and its launch.
+  if (cudaFuncSetAttribute(sample_filter_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMostShared)) !=
       cudaSuccess) {
     cudaGetLastError();
     return A3PO_ERR_CUDA;
