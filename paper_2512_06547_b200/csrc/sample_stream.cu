@@ -181,6 +181,7 @@ sample_pick_kernel(SampleArgs a, Segments in) {
   const int row = blockIdx.x, lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp;
   if (a.row_mask && a.row_mask[row] == 0) {
     if (threadIdx.x == 0) a.put(row, -1, 0.0, 0.0, 0);
+    wait_for_previous();   // what follows in the stream waits for this kernel alone, and may write what the one before it reads
     return;
   }
   fill_table(table, threadIdx.x, kPickThreads);
