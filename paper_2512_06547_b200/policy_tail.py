@@ -100,16 +100,20 @@ class PolicyTail:
                 "grad_r0": self.grad_r0, "grads": g}
 
     def optimizer(self, params, *, weight_decay=0.01, **kw):
-        """AdamW over `params` (in the order of self.grads), with fp32 masters of bf16 weights; norms do not decay.  kw as for
-        AdamW."""
-        weights = [params[k] for k in self.grads]
+        """AdamW over `params` (in the order of self.grads, without a beta that they do not hold), with fp32 masters of bf16 weights;
+        norms do not decay.  kw as for AdamW."""
+        names = [k for k in self.grads if params.get(k) is not None or k not in ("beta_in", "beta_out")]
+        weights = [params[k] for k in names]
         if self.dtype != torch.float32:
             kw.setdefault("masters", True)
-        return AdamW(weights, weight_decay=[float(weight_decay) if w.dim() > 1 else 0.0 for w in weights], **kw)
+        made = AdamW(weights, weight_decay=[float(weight_decay) if w.dim() > 1 else 0.0 for w in weights], **kw)
+        made.names = names
+        return made
 
     def update(self, optimizer):
-        """The optimizer's step with the gradients that the last pass left (fp32), on the current stream."""
-        optimizer.step(list(self.grads.values()))
+        """The optimizer's step with the gradients that the last pass left (fp32), on the current stream: of the parameters that
+        self.optimizer made it for, else of all in the order of self.grads."""
+        optimizer.step([self.grads[k] for k in getattr(optimizer, "names", self.grads)])
 
 
 class PolicySampler:
