@@ -92,17 +92,18 @@ class AdamW:
         for i, w in enumerate(self.weights):
             self._table[i] = b.A3poAdamWTensor(w.data_ptr(), at(self.masters, i), None, at(self.m, i), at(self.v, i),
                                                at(self.m_scales, i), at(self.v_scales, i), w.numel(), decay[i])
-        self._rows = [(self._table[i], w, w.data_ptr(), w.numel()) for i, w in enumerate(self.weights)]
+        self._rows = [(self._table[i], w, w.data_ptr(), w.numel(), w.shape) for i, w in enumerate(self.weights)]
 
     def step(self, grads, *, stream=None):
-        """grads: one tensor per weight, of its size, all fp32 or all bf16."""
+        """grads: one tensor per weight, of its shape or flat, all fp32 or all bf16."""
         if len(grads) != len(self.weights):
             raise ValueError("grads: expected one tensor per weight")
         device, here = self._device, torch.cuda.current_device()
         dtype = grads[0].dtype if grads else torch.float32
         fine = device == here
-        for g, (row, w, at, n) in zip(grads, self._rows):
-            fine &= (g.dtype is dtype and g.numel() == n and g.get_device() == device and g.is_contiguous() and w.data_ptr() == at)
+        for g, (row, w, at, n, shape) in zip(grads, self._rows):
+            fine &= (g.dtype is dtype and (g.shape == shape or g.shape == (n,)) and g.get_device() == device and g.is_contiguous()
+                     and w.data_ptr() == at)
             row.grad = g.data_ptr()
         for t, ty in ((self.lr, torch.float32), (self.steps, torch.int64), (self.grad_norm, torch.float32)):
             fine &= t.dtype is ty and t.numel() == 1 and t.get_device() == device
@@ -118,13 +119,13 @@ class AdamW:
     def _refuse(self, grads, dtype, here):
         if self._device != here:
             raise ValueError(f"expected the current device cuda:{self._device}, got cuda:{here}")
-        for g, (_, w, at, n) in zip(grads, self._rows):
+        for g, (_, w, at, n, shape) in zip(grads, self._rows):
             if g.dtype is not dtype:
                 raise TypeError("grads: expected tensors of one type")
             b._want(g, dtype, "grads")
             b._here(g)
-            if g.numel() != n:
-                raise ValueError("grads: expected the size of the weight")
+            if g.shape != shape and g.shape != (n,):
+                raise ValueError(f"grads: expected the weight's shape {tuple(shape)}, or its elements in a row, got {tuple(g.shape)}")
             if w.data_ptr() != at:
                 raise ValueError("weights: a weight's storage is another than when the object was made")
         for t, ty, name in ((self.lr, torch.float32, "lr"), (self.steps, torch.int64, "steps"),
