@@ -64,7 +64,7 @@ class AdamW:
         if len(decay) != count:
             raise ValueError("weight_decay: expected a number or one per weight")
         if masters is True:
-            masters = [w.float() for w in self.weights]
+            masters = [w.detach().float() for w in self.weights]
         if masters is not None and masters is not False:
             if dtype == torch.float32:
                 raise ValueError("masters: fp32 weights are their own")
