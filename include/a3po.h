@@ -533,7 +533,7 @@ int a3po_linear_bwd(const void* x, const void* w, const uint8_t* row_mask, const
  * `logp` is the behaviour log-prob that the loss takes as behav_logp, by the definition of a3po_token_logprobs_fwd with
  * inv_temperature = 1 / t (1 for a greedy row): a policy that is sampled at t is trained at t, or its importance weights are biased.
  *
- * A row with logits l (NaN counts as -inf) and temperature t, t <= 0 or NaN meaning greedy (with t = 1 below):
+ * A row with logits l (NaN counts as -inf) and temperature t, t <= 0 or NaN meaning greedy (with t = 1 below), above 1e30 as 1e30:
  *   w_i = exp((l_i - max l) / t);  tokens are ranked by l, of equal logits the lower index first
  *   top_k  keeps the k first ranks (k <= 0 or k >= V: all);
  *   top_p  keeps of those the fewest first ranks whose weights reach top_p times the sum of theirs (top_p >= 1: all);

@@ -291,11 +291,11 @@ struct SampleArgs {
     if (kept_logp) kept_logp[row] = static_cast<float>(klp);
     if (n_kept) n_kept[row] = kept;
   }
-  // Temperature of a row; 1 where it is greedy.
+  // Temperature of a row; 1 where it is greedy.  An infinite one would make 0 times infinity of an infinite logit and of min-p = 1.
   __device__ __forceinline__ float temp(int row, bool& greedy) const {
     const float t = temperature ? temperature[row] : 1.f;
     greedy = !(t > 0.f);
-    return greedy ? 1.f : t;
+    return greedy ? 1.f : fminf(t, 1e30f);
   }
 };
 
