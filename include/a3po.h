@@ -543,7 +543,8 @@ int a3po_linear_bwd(const void* x, const void* w, const uint8_t* row_mask, const
  *   n_kept    = number of kept tokens with a logit above -inf
  * Weights carry 2^-31 of their value and sums 53 bits (the mass that top_p compares: multiples of 2^-43 of the largest weight),
  * added in a fixed order: results are bit-identical from run to run, and a token differs from the one that exact sums give
- * only where u lies within that of a border.
+ * only where u lies within that of a border.  Weights of bf16 logits are off by up to 2^-24 |l_i - max l| / t more where one of the
+ * two is that much smaller than the other (2^-15) that their difference is not an fp32 number.
  *
  * logits [N, V], dtype `dt`, rows row_stride >= V elements apart, pointer aligned to its elements.  temperature, top_k, top_p,
  * min_p: [N] or NULL (1, off, off, off); u fp32 [N] in [0, 1) (below 0 or NaN: 0; from 1 on: the last kept token).

@@ -8,7 +8,8 @@
 // with d = l - m and e its rounding error (both fp32; two-sum of Knuth) and y = (d + e) log2(e) / t, the sum of d log2(e) / t and
 // 1.5 2^16 rounds y to k + j / 128, two fused products leave f = y - k - j / 128 with |f| <= 2^-8 exact to 2^-32, and
 //   w = 2^k T[j] (1 + p),  T[j] = 2^(j / 128) in 64 bits,  p = 2^f - 1 from the first three terms of its series.
-// The error is that of f and p: half a step of fp32 numbers of at most 0.004, below 2^-31 of w.  d = 0 gives 1 exactly.  Sums
+// The error is that of f and p: half a step of fp32 numbers of at most 0.004, below 2^-31 of w (and for bf16 logits that of d, see
+// exact_diff below).  d = 0 gives 1 exactly.  Sums
 // take T in 64 bits and T p, 400 times smaller, in 32, so that no value is converted between the two types, and the fp32 part
 // runs on pairs: 14 (bf16) to 17 instructions per logit, of which one is a 64-bit one (39 without the pairs, with checks for what
 // a warp's logits do not hold, and with conflicts on a table that is not there once per lane of a half-warp).
@@ -184,8 +185,9 @@ struct Weights {
   }
 };
 
-// The difference of two bf16 numbers is an fp32 number unless one is 2^16 times smaller than the other; the rounding (2^-25
-// of the difference, of logits that are close to 0 beside the largest) is left in.
+// The difference of two bf16 numbers is an fp32 number unless one is about 2^15 times smaller than the other, a logit that is close
+// to 0 beside the largest; the rounding, 2^-24 of the difference and so 2^-24 |l - m| / t of the weight, is left in (with it the
+// fp32 form's three instructions a logit more, 14 to 17).
 template <typename T> constexpr bool exact_diff() { return sizeof(T) == 2; }
 
 // Logits are read 16 bytes at a time from the 16-byte boundary at or below the row's (or slice's) first element on: `head`
