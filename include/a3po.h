@@ -547,7 +547,8 @@ int a3po_linear_bwd(const void* x, const void* w, const uint8_t* row_mask, const
  * two is that much smaller than the other (2^-15) that their difference is not an fp32 number.
  *
  * logits [N, V], dtype `dt`, rows row_stride >= V elements apart, pointer aligned to its elements.  temperature, top_k, top_p,
- * min_p: [N] or NULL (1, off, off, off); u fp32 [N] in [0, 1) (below 0 or NaN: 0; from 1 on: the last kept token).
+ * min_p: [N] or NULL (1, off, off, off); u fp32 [N] in [0, 1) (below 0 or NaN: 0; from 1 on: the last kept token whose
+ * weight is not 0 in 64 bits).
  * token int32 [N]; logp, kept_logp fp32 [N] and n_kept int32 [N] or NULL.  A row with row_mask 0 (uint8 [N] or NULL) is not read;
  * it, and a row without a logit above -inf, gets token -1, logp 0, kept_logp 0, n_kept 0.
  * With any of top_k, top_p, min_p a row has to fit the shared memory of eight SMs: V <= 393,216 (fp32) or 786,432 (bf16), else

@@ -908,26 +908,26 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         for (int nt = it.n_begin; nt < it.n_end && ok; ++nt) {
           int kb0 = 0, kb1;
           do {
-          kb1 = Epi::kPromote > 0 ? min(kb0 + Epi::kPromote, k_blocks) : k_blocks;
-          if (!mbar_wait(&tmem_empty_bar[acc], acc_phase ^ 1u, abort_flag)) { ok = false; break; }
-          tcgen05_fence_after_sync();
-          const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(acc * BN);
-          for (int kb = kb0; kb < kb1; ++kb) {
-            if (!mbar_wait(&full_bar[stage], phase, abort_flag)) { ok = false; break; }
+            kb1 = Epi::kPromote > 0 ? min(kb0 + Epi::kPromote, k_blocks) : k_blocks;
+            if (!mbar_wait(&tmem_empty_bar[acc], acc_phase ^ 1u, abort_flag)) { ok = false; break; }
             tcgen05_fence_after_sync();
-            const uint32_t sa = smem_u32(smem_a + stage * kABytes);
-            const uint32_t sb = smem_u32(smem_b + stage * (kBBytes / 2));
-            const uint64_t desc_a = A_MN ? umma_desc_mn_major_sw128(sa, kMnBlockBytes) : umma_desc_k_major_sw128(sa);
-            const uint64_t desc_b = B_MN ? umma_desc_mn_major_sw128(sb, kMnBlockBytes) : umma_desc_k_major_sw128(sb);
+            const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(acc * BN);
+            for (int kb = kb0; kb < kb1; ++kb) {
+              if (!mbar_wait(&full_bar[stage], phase, abort_flag)) { ok = false; break; }
+              tcgen05_fence_after_sync();
+              const uint32_t sa = smem_u32(smem_a + stage * kABytes);
+              const uint32_t sb = smem_u32(smem_b + stage * (kBBytes / 2));
+              const uint64_t desc_a = A_MN ? umma_desc_mn_major_sw128(sa, kMnBlockBytes) : umma_desc_k_major_sw128(sa);
+              const uint64_t desc_b = B_MN ? umma_desc_mn_major_sw128(sb, kMnBlockBytes) : umma_desc_k_major_sw128(sb);
 #pragma unroll
-            for (int k = 0; k < BK / 16; ++k)
-              umma_bf16_pair(tmem_d, desc_a + a_step * k, desc_b + b_step * k, idesc, ((kb - kb0) | k) != 0 ? 1u : 0u);
-            umma_commit_pair(&empty_bar[stage], 3);   // both CTAs may refill the stage
-            if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
-          }
-          if (ok) umma_commit_pair(&tmem_full_bar[acc], 3);
-          if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
-          kb0 = kb1;
+              for (int k = 0; k < BK / 16; ++k)
+                umma_bf16_pair(tmem_d, desc_a + a_step * k, desc_b + b_step * k, idesc, ((kb - kb0) | k) != 0 ? 1u : 0u);
+              umma_commit_pair(&empty_bar[stage], 3);   // both CTAs may refill the stage
+              if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
+            }
+            if (ok) umma_commit_pair(&tmem_full_bar[acc], 3);
+            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+            kb0 = kb1;
           } while (Epi::kPromote > 0 && kb0 < k_blocks && ok);
         }
       }

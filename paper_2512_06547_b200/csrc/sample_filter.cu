@@ -14,8 +14,8 @@
 //
 // Masses that are compared are whole numbers of 2^-43, so that they do not depend on the order of atomics, and all other sums are
 // taken in a fixed order: results are bit-identical from run to run.
-// Bound: latency.  A row is a chain of passes of one to four microseconds and four to nine cluster barriers of half a one; for many
-// rows the instructions of the passes (40 to 70 a logit).  64 rows of 151,936 bf16: top-k 44 us, min-p 37, all three 51, settings that
+// Bound: latency.  A row is a chain of passes of one to four microseconds and four to twelve cluster barriers of half a one; for many
+// rows the instructions of the passes (40 to 78 a logit).  64 rows of 151,936 bf16: top-k 44 us, min-p 37, all three 51, settings that
 // differ by row 74, flat rows under top-p alone (tens of thousands of candidates, every pass of the list above) 76; 1,024 rows
 // 415 to 655 us; 37 rows of 32,003 in fp32, all three, 30 to 34.
 // Sums by segment for all rows first (sample_stream.cu), a block per row for those whose candidates the segments bound, and

@@ -38,13 +38,14 @@ class AdamW:
     """weights: contiguous tensors of one type (fp32 or bf16), updated in place by step(grads).
 
     lr: a number, or an fp32 device scalar that the caller changes between steps.  weight_decay: a number, or one per weight.
-    max_grad_norm: 0 for no clipping; grad_norm holds the norm of the last step's gradients before clipping either way.  A
-    step whose norm is not finite changes nothing.  state_bits: 32 or 8; from
-    step 33 on, states of 8 bits are rounded at random (by numbers that the step, the place of the weight and the element give), so
-    that they follow their averages whatever the betas.  masters: True (bf16 weights) keeps an fp32
-    copy of each weight, which is what is updated; a list gives the copies.  m, v, m_scales, v_scales, step: states to go on from
-    (kept and updated in place), as this object's attributes of these names hold them.  The weights and states that an object was
-    made with stay its own: new contents are copied into them (lr, steps and grad_norm may be replaced)."""
+    max_grad_norm: 0 for no clipping; grad_norm holds the norm of the last step's gradients before clipping either way.  The norm is
+    over this object's gradients: weights of another type, in an object of their own, are clipped by themselves.  A step whose
+    norm is not finite changes nothing.  state_bits: 32 or 8; from step 33 on, states of 8 bits are rounded at random (by numbers
+    that the step, the place of the weight and the element give), so that they follow their averages whatever the betas.
+    masters: True (bf16 weights) keeps an fp32 copy of each weight, which is what is updated; a list gives the copies.
+    m, v, m_scales, v_scales, step: states to go on from (kept and updated in place), as this object's attributes of these names
+    hold them.  The weights and states that an object was made with stay its own: new contents are copied into them (lr, steps and
+    grad_norm may be replaced)."""
 
     def __init__(self, weights, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, *, max_grad_norm=0.0, state_bits=32,
                  masters=None, m=None, v=None, m_scales=None, v_scales=None, step=None):
